@@ -160,11 +160,16 @@ def _split(rows, seqs):
     return out
 
 
+def _pow2(e):
+    """2^e, -126 <= e <= 127, as float32: the exponent's bits."""
+    return ((e.int() + 127) << 23).view(torch.float32)
+
+
 def _encode(x):
     """Codes (as float8) and stored exponents of rows x [..., head_dim], in 32 bits."""
     m, e = torch.frexp(x.abs().amax(-1))
     e = torch.where(m == 0, torch.zeros_like(e), (e - 9 + (m > 0.875).to(e.dtype)).clamp(min=-126))
-    return torch.ldexp(x, -e.unsqueeze(-1)).to(torch.float8_e4m3fn), (e + 127).to(torch.uint8)
+    return (x * _pow2(-e).unsqueeze(-1)).to(torch.float8_e4m3fn), (e + 127).to(torch.uint8)
 
 
 def _cache_type(case):
@@ -236,7 +241,7 @@ def prepare(case, seed):
 # ---------------------------------------------------------------------------
 
 def _decode(codes, exps):
-    return torch.ldexp(codes.float(), exps.int().unsqueeze(-1) - 127)
+    return codes.float() * _pow2(exps.int() - 127).unsqueeze(-1)
 
 
 def _positions(st, pool, exps, s, n):
