@@ -222,7 +222,8 @@ ADEPT_API adept_status adept_set_cross_source(adept_model* m, int n_seq, const i
 
 /* ---- helpers (not part of the method; used by tests and the benchmark) ---- */
 
-/* Message of the last failing call on `m` (or of the last failed load when m is NULL). */
+/* Message of the last failing call on `m`; with m NULL, of the calling thread's last failed load or
+ * call on an adept_kv_cache. */
 ADEPT_API const char* adept_last_error(const adept_model* m);
 ADEPT_API const char* adept_status_string(adept_status s);
 
@@ -381,6 +382,83 @@ ADEPT_API adept_status adept_hsm_train_read(adept_model* m, int what, int param,
                                   void* stream);
 /* Element count of HSM parameter `param` (0..12), or -1. */
 ADEPT_API int64_t adept_hsm_param_numel(const adept_model* m, int param);
+
+/* ---- operators on a caller-owned paged K/V cache ---------------------------------------
+ * The cache of one layer (or of anything that keys and values are kept of), in the layout of the
+ * models' own: K and V as [n_blocks][n_kv_heads][block_tokens][head_dim], position p of sequence b
+ * in block d_block_table[b][p / block_tokens], slot p % block_tokens.  kv_type:
+ *   ADEPT_KV_F32, ADEPT_KV_BF16   plain elements
+ *   ADEPT_KV_E4M3                 one byte an element and one exponent byte per (position, head) in
+ *     d_k_exp / d_v_exp [n_blocks][n_kv_heads][block_tokens]: value = e4m3 * 2^(byte - 127).  Written
+ *     from x: with a = max |x| over the head's finite elements, a = m 2^E, m in [1/2, 1), the
+ *     exponent is e = E - 9, E - 8 where m > 7/8 (so that a 2^-e <= 448), at least -126, and 0 for
+ *     a = 0; an element is e4m3(x 2^-e), rounded once, to nearest even.  NaN stays NaN; an infinity
+ *     is stored as NaN.  What is read back is exact in fp32, and in bf16 above its subnormals (only
+ *     an element that rounded up to 2^128 reads back as infinity).
+ * The buffers are the caller's, on the current device; d_k and d_v start on 16 bytes.  The calls
+ * allocate nothing, hold no state between calls and can be captured into a graph; calls on one
+ * cache are ordered by their streams as any other work on shared buffers is.
+ * d_err (may be NULL): a device word that kernels set where an input read on the device is out of
+ * range (zero it first); adept_kv_check reports and clears it. */
+enum { ADEPT_KV_F32 = 0, ADEPT_KV_BF16 = 1, ADEPT_KV_E4M3 = 2 };
+typedef struct {
+  int kv_type;              /* ADEPT_KV_* */
+  int n_blocks;
+  int n_kv_heads;
+  int head_dim;             /* 32, 64 or 128 */
+  int block_tokens;
+  int n_seq;                /* rows of the block table */
+  int max_blocks_per_seq;   /* its columns */
+  void* d_k;
+  void* d_v;
+  uint8_t* d_k_exp;         /* ADEPT_KV_E4M3 only */
+  uint8_t* d_v_exp;
+  const int32_t* d_block_table;
+  uint32_t* d_err;
+} adept_kv_cache;
+
+/* Writes n_rows rows of K and of V (row r: n_kv_heads * head_dim elements of ADEPT_DTYPE_* dtype at
+ * d_k + r * ld_k, so that rows may lie inside a wider product) to position d_pos[r] of sequence
+ * d_seq[r], in the cache's type.  d_seq[r] < 0: the row is left out.  A sequence, position or block
+ * out of range flags DEVICE_INPUT and leaves the row out.  Each (sequence, position) at most once
+ * a call: of two rows with the same one the entry may mix both.
+ * Errors: INVALID_ARG (bad cache, n_rows < 0, NULL or misaligned pointers, a stride below a row), CUDA. */
+ADEPT_API adept_status adept_kv_append(const adept_kv_cache* c, int n_rows, int dtype, const void* d_k, int64_t ld_k,
+                             const void* d_v, int64_t ld_v, const int32_t* d_seq, const int32_t* d_pos, void* stream);
+/* The other way: the entries at (d_seq[r], d_pos[r]) into rows of ADEPT_DTYPE_* dtype (a row with
+ * d_seq[r] < 0, or out of range, is not written; an entry may be asked for more than once). */
+ADEPT_API adept_status adept_kv_gather(const adept_kv_cache* c, int n_rows, int dtype, void* d_k, int64_t ld_k, void* d_v,
+                             int64_t ld_v, const int32_t* d_seq, const int32_t* d_pos, void* stream);
+
+/* Causal attention of a chunk of new tokens whose K and V are in the cache already.  Sequence b
+ * (row b of the block table) brings the rows d_q_start[b] .. d_q_start[b + 1] - 1 of Q: its last
+ * positions, up to d_kv_len[b] - 1.  The row at position p attends positions 0 .. p: query head h
+ * with KV head h / (n_heads / n_kv_heads), scores q.k / sqrt(head_dim).  A sequence may bring no row
+ * (it is not read), one (a generation step) or thousands; a row at a position below 0 gives zeros.
+ * What is behind a row's position (the chunk's later tokens, unwritten slots) does not enter it,
+ * whatever it holds; a NaN or infinite V entry that a row does attend makes that output NaN or
+ * infinite.
+ *   d_q, d_out   [n_rows][ld] (n_heads * head_dim elements a row): bf16, or fp32 for an fp32 cache;
+ *                they must not overlap.  Rows that no sequence holds are not written.
+ *   d_q_start [n_seq + 1], d_kv_len [n_seq]   int32, read on the device
+ *   max_q_len, max_kv_len   bounds on a sequence's rows and positions; a sequence beyond them, or with
+ *                rows outside 0 .. n_rows, flags DEVICE_INPUT and is left out, as is a key whose block
+ *                is out of range
+ *   d_ws         adept_chunk_attention_workspace bytes on 16 bytes (NULL where that is 0), of any
+ *                contents; calls that may overlap on the GPU need one each
+ * For the same lengths a call's results are the same bits every time.
+ * Errors: INVALID_ARG (bad cache, n_heads no multiple of n_kv_heads, max_kv_len above the table, a
+ * stride below a row, NULL or misaligned pointers, a workspace too small), CAPACITY (n_rows *
+ * n_heads above 2^30), CUDA. */
+ADEPT_API adept_status adept_chunk_attention(const adept_kv_cache* c, int n_heads, int n_rows, const void* d_q, int64_t ld_q,
+                                   const int32_t* d_q_start, const int32_t* d_kv_len, int max_q_len, int max_kv_len,
+                                   void* d_out, int64_t ld_out, void* d_ws, int64_t ws_bytes, void* stream);
+/* Bytes of d_ws that such a call needs, or -1 (bad arguments). */
+ADEPT_API int64_t adept_chunk_attention_workspace(const adept_kv_cache* c, int n_heads, int n_rows, int max_q_len,
+                                        int max_kv_len);
+/* Synchronise `stream`, then read and clear the cache's error word: DEVICE_INPUT, TIMEOUT or OK.
+ * Errors: INVALID_ARG (no error word), CUDA. */
+ADEPT_API adept_status adept_kv_check(const adept_kv_cache* c, void* stream);
 
 /* ---- failure injection (tests of the error paths; no GPU fault is involved) ------------
  * adept_set_wait_limit: limit, in SM cycles, of the kernels' bounded waits on pipeline

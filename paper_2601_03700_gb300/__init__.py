@@ -7,6 +7,7 @@ call raises.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 from typing import Dict, Optional
@@ -38,6 +39,7 @@ ABI_SYMBOLS = [
     "adept_calibrate_threshold", "adept_hsm_train_init", "adept_hsm_train_step", "adept_hsm_train_read",
     "adept_hsm_param_numel", "adept_hsm_train_step_cls", "adept_set_wait_limit", "adept_set_alloc_fail_after",
     "adept_span_read", "adept_set_cross_source",
+    "adept_kv_append", "adept_kv_gather", "adept_chunk_attention", "adept_chunk_attention_workspace", "adept_kv_check",
 ]
 
 
@@ -71,6 +73,14 @@ class AdeptAdamW(ctypes.Structure):
 
 class AdeptTensorTable(ctypes.Structure):
     _fields_ = [("tensors", ctypes.POINTER(AdeptTensor)), ("n_tensors", ctypes.c_int)]
+
+
+class AdeptKVCache(ctypes.Structure):
+    _fields_ = [("kv_type", ctypes.c_int), ("n_blocks", ctypes.c_int), ("n_kv_heads", ctypes.c_int),
+                ("head_dim", ctypes.c_int), ("block_tokens", ctypes.c_int), ("n_seq", ctypes.c_int),
+                ("max_blocks_per_seq", ctypes.c_int), ("d_k", ctypes.c_void_p), ("d_v", ctypes.c_void_p),
+                ("d_k_exp", ctypes.c_void_p), ("d_v_exp", ctypes.c_void_p), ("d_block_table", ctypes.c_void_p),
+                ("d_err", ctypes.c_void_p)]
 
 
 _lib = None
@@ -130,6 +140,16 @@ def load_library(path: str = LIB_PATH):
     lib.adept_set_alloc_fail_after.restype = None
     lib.adept_hsm_param_numel.argtypes = [vp, c_int]
     lib.adept_hsm_param_numel.restype = ctypes.c_int64
+    kvp, i64 = ctypes.POINTER(AdeptKVCache), ctypes.c_int64
+    for fn in (lib.adept_kv_append, lib.adept_kv_gather):
+        fn.argtypes = [kvp, c_int, c_int, vp, i64, vp, i64, i32p, i32p, st]
+        fn.restype = c_int
+    lib.adept_chunk_attention.argtypes = [kvp, c_int, c_int, vp, i64, i32p, i32p, c_int, c_int, vp, i64, vp, i64, st]
+    lib.adept_chunk_attention.restype = c_int
+    lib.adept_chunk_attention_workspace.argtypes = [kvp, c_int, c_int, c_int, c_int]
+    lib.adept_chunk_attention_workspace.restype = i64
+    lib.adept_kv_check.argtypes = [kvp, st]
+    lib.adept_kv_check.restype = c_int
     for name in ABI_SYMBOLS:
         fn = getattr(lib, name)
         if fn.restype is ctypes.c_int or name in ("adept_model_load", "adept_prefill", "adept_decode_step",
@@ -362,6 +382,143 @@ def adept_set_wait_limit(cycles: int):
 
 def adept_set_alloc_fail_after(n: int):
     load_library().adept_set_alloc_fail_after(int(n))
+
+
+# ---------------------------------------------------------------------------
+# operators on a caller-owned paged K/V cache
+# ---------------------------------------------------------------------------
+
+KV_TYPES = {"f32": 0, "bf16": 1, "e4m3": 2}
+_KV_TORCH = {0: torch.float32, 1: torch.bfloat16, 2: torch.uint8}
+
+
+class KVCache:
+    """A paged K/V cache in device tensors (adept_kv_cache): k, v [n_blocks, n_kv_heads, block_tokens, head_dim]
+    (uint8 e4m3 codes for dtype "e4m3", with k_exp, v_exp [n_blocks, n_kv_heads, block_tokens], uint8), block_table
+    [n_seq, max_blocks_per_seq] int32 (-1: no block) and err, the error word.  Tables and entries are the caller's to
+    set; the tensors stay where they are for the cache's life."""
+
+    def __init__(self, n_blocks: int, n_kv_heads: int, head_dim: int, n_seq: int, max_blocks_per_seq: int,
+                 dtype: str = "bf16", block_tokens: int = 16, device="cuda"):
+        if dtype not in KV_TYPES:
+            raise ValueError(f"dtype {dtype!r} unknown ({', '.join(KV_TYPES)})")
+        t = KV_TYPES[dtype]
+        shape = (n_blocks, n_kv_heads, block_tokens, head_dim)
+        self.dtype = dtype
+        self.k = torch.zeros(shape, dtype=_KV_TORCH[t], device=device)
+        self.v = torch.zeros_like(self.k)
+        self.k_exp = self.v_exp = None
+        if dtype == "e4m3":   # 127: a scale of 1
+            self.k_exp = torch.full(shape[:3], 127, dtype=torch.uint8, device=device)
+            self.v_exp = torch.full_like(self.k_exp, 127)
+        self.block_table = torch.full((n_seq, max_blocks_per_seq), -1, dtype=torch.int32, device=device)
+        self.err = torch.zeros(1, dtype=torch.int32, device=device)
+        self.device = self.k.device
+        self.n_seq, self.n_kv_heads, self.head_dim = n_seq, n_kv_heads, head_dim
+        p = lambda x: None if x is None else x.data_ptr()  # noqa: E731
+        self._c = AdeptKVCache(t, n_blocks, n_kv_heads, head_dim, block_tokens, n_seq, max_blocks_per_seq, p(self.k),
+                               p(self.v), p(self.k_exp), p(self.v_exp), p(self.block_table), p(self.err))
+        self.ref = ctypes.byref(self._c)
+
+    def attention_workspace(self, n_heads: int, n_rows: int, max_q_len: int, max_kv_len: int) -> Optional[torch.Tensor]:
+        """A workspace for adept_chunk_attention calls of these sizes (None: none needed)."""
+        n = load_library().adept_chunk_attention_workspace(self.ref, n_heads, n_rows, max_q_len, max_kv_len)
+        if n < 0:
+            _check(load_library(), None, 1)
+        return torch.empty(n, dtype=torch.uint8, device=self.device) if n else None
+
+    def check(self, stream=None):
+        adept_kv_check(self, stream)
+
+
+def _on(cache: KVCache):
+    """The cache's device as the current one."""
+    if cache.device.type != "cuda":
+        raise ValueError(f"the cache is on {cache.device}: the operators need a GPU")
+    return contextlib.nullcontext() if torch.cuda.current_device() == cache.device.index else torch.cuda.device(cache.device)
+
+
+def _rows(cache: KVCache, name: str, t: torch.Tensor, heads: int):
+    """(rows, row stride, dtype) of [rows, heads, head_dim], or [rows, heads * head_dim], dense within a row."""
+    w = heads * cache.head_dim
+    if t.device != cache.device:
+        raise ValueError(f"{name} is on {t.device}, the cache on {cache.device}")
+    if t.dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError(f"{name} must be float32 or bfloat16")
+    if t.dim() == 3 and tuple(t.shape[1:]) == (heads, cache.head_dim):
+        dense = t.stride(2) == 1 and (heads == 1 or t.stride(1) == cache.head_dim)
+    elif t.dim() == 2 and t.shape[1] == w:
+        dense = t.stride(1) == 1
+    else:
+        raise ValueError(f"{name} must be [rows, {heads}, {cache.head_dim}]")
+    n = t.shape[0]
+    ld = t.stride(0) if n > 1 else w
+    if n and (not dense or ld < w):
+        raise ValueError(f"the rows of {name} must be dense and must not overlap")
+    return n, ld, 1 if t.dtype == torch.bfloat16 else 0
+
+
+def _index(cache: KVCache, name: str, t: torch.Tensor, n: int):
+    if t.dtype != torch.int32 or t.device != cache.device or t.dim() != 1 or t.numel() != n or not t.is_contiguous():
+        raise ValueError(f"{name} must be {n} contiguous int32 values on {cache.device}")
+    return t.data_ptr()
+
+
+def _kv_rows(fn, cache, k, v, seq, pos, stream):
+    lib = load_library()
+    n, ld_k, dt = _rows(cache, "k", k, cache.n_kv_heads)
+    n_v, ld_v, dt_v = _rows(cache, "v", v, cache.n_kv_heads)
+    if n != n_v or dt != dt_v:
+        raise ValueError("k and v must have the same rows and type")
+    with _on(cache):
+        _check(lib, None, fn(cache.ref, n, dt, k.data_ptr(), ld_k, v.data_ptr(), ld_v, _index(cache, "seq", seq, n),
+                             _index(cache, "pos", pos, n), _stream(stream)))
+
+
+def adept_kv_append(cache: KVCache, k: torch.Tensor, v: torch.Tensor, seq: torch.Tensor, pos: torch.Tensor, stream=None):
+    """Rows k, v [rows, n_kv_heads, head_dim] (row-strided views allowed) to position pos[r] of sequence seq[r]
+    (< 0: left out), in the cache's type."""
+    _kv_rows(load_library().adept_kv_append, cache, k, v, seq, pos, stream)
+
+
+def adept_kv_gather(cache: KVCache, seq: torch.Tensor, pos: torch.Tensor, k_out: torch.Tensor, v_out: torch.Tensor,
+                    stream=None):
+    """The entries at (seq[r], pos[r]) into rows of k_out, v_out (float32 or bfloat16)."""
+    _kv_rows(load_library().adept_kv_gather, cache, k_out, v_out, seq, pos, stream)
+
+
+def adept_chunk_attention(cache: KVCache, q: torch.Tensor, q_start: torch.Tensor, kv_len: torch.Tensor, max_q_len: int,
+                          max_kv_len: int, out: torch.Tensor, workspace: Optional[torch.Tensor] = None, stream=None):
+    """Causal attention of each sequence's newest tokens, rows q_start[b] .. q_start[b + 1] of q [rows, n_heads, head_dim],
+    over its kv_len[b] cached positions, into out.  workspace: KVCache.attention_workspace of these sizes (None: one is
+    made for the call)."""
+    lib = load_library()
+    want = torch.float32 if cache.dtype == "f32" else torch.bfloat16
+    if q.dtype != want or out.dtype != want:
+        raise ValueError(f"q and out of a {cache.dtype} cache are {want}")
+    heads = q.shape[1] if q.dim() == 3 else q.shape[-1] // cache.head_dim
+    n, ld_q, _ = _rows(cache, "q", q, heads)
+    n_o, ld_o, _ = _rows(cache, "out", out, heads)
+    if n != n_o:
+        raise ValueError("q and out must have the same rows")
+    qs, kl = _index(cache, "q_start", q_start, cache.n_seq + 1), _index(cache, "kv_len", kv_len, cache.n_seq)
+    with _on(cache):
+        if workspace is None:
+            s = stream if stream is None or hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream))
+            with torch.cuda.stream(s):   # (the call's stream: memory that it alone reuses)
+                workspace = cache.attention_workspace(heads, n, max_q_len, max_kv_len)
+        elif workspace.device != cache.device or not workspace.is_contiguous():
+            raise ValueError(f"workspace must be contiguous on {cache.device}")
+        ws, nb = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
+        _check(lib, None, lib.adept_chunk_attention(cache.ref, heads, n, q.data_ptr(), ld_q, qs, kl, int(max_q_len),
+                                                    int(max_kv_len), out.data_ptr(), ld_o, ws, nb, _stream(stream)))
+
+
+def adept_kv_check(cache: KVCache, stream=None):
+    """Waits for the stream and raises where a kernel flagged an input out of range since the last check."""
+    lib = load_library()
+    with _on(cache):
+        _check(lib, None, lib.adept_kv_check(cache.ref, _stream(stream)))
 
 
 # ---------------------------------------------------------------------------

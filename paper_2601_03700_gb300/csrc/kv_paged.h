@@ -1,0 +1,164 @@
+// A paged K/V cache given by its pointers (adept_kv_cache), and the launchers of the kernels that
+// write it (kv_store.cu) and attend over it (attention_chunk.cu, attention_chunk_tc.cu).
+#pragma once
+#include "common.cuh"
+
+namespace adept {
+
+enum KvType : int { KV_F32 = 0, KV_BF16 = 1, KV_E4M3 = 2 };
+
+// K and V as [n_blocks][n_kv_heads][block_tokens][head_dim].  KV_E4M3: one byte per element and, in k_exp / v_exp
+// [n_blocks][n_kv_heads][block_tokens], the exponent e (+ 127) of each (position, head): value = code * 2^e.
+struct KvPaged {
+  void* k;
+  void* v;
+  uint8_t* k_exp;
+  uint8_t* v_exp;
+  const int* table;   // [n_seq][max_blocks]
+  unsigned* err;      // error word (NULL: none)
+  int type, n_blocks, n_kv_heads, head_dim, block_tokens, n_seq, max_blocks;
+  __device__ __forceinline__ void flag(unsigned bits) const {
+    if (err) atomicOr(err, bits);
+  }
+};
+
+// Rows of K and V into the cache at (seq[r], pos[r]); seq[r] < 0: the row is left out.  src_bf16: element type of the
+// rows (else fp32); ld in elements.
+cudaError_t launch_kv_append(cudaStream_t st, const KvPaged& c, int n_rows, int src_bf16, const void* k, long long ld_k,
+                             const void* v, long long ld_v, const int* seq, const int* pos);
+// The entries at (seq[r], pos[r]) back as rows (a row with seq[r] < 0 is not written).
+cudaError_t launch_kv_gather(cudaStream_t st, const KvPaged& c, int n_rows, int dst_bf16, void* k, long long ld_k, void* v,
+                             long long ld_v, const int* seq, const int* pos);
+
+// One attention call: the new tokens of n_seq sequences (rows q_start[b] .. q_start[b + 1]), the last of sequence b's
+// kv_len[b] cached positions, each attending its own position and those before it.
+struct ChunkCall {
+  KvPaged c;
+  const void* q;      // [n_rows][ld_q], head h at column h * head_dim (bf16; fp32 for an fp32 cache)
+  void* out;          // [n_rows][ld_out], the same type
+  long long ld_q, ld_out;
+  const int* q_start;
+  const int* kv_len;
+  int n_rows, n_heads, max_q, max_kv;
+  float scale_log2;   // log2(e) / sqrt(head_dim)
+  float* part;        // workspace
+};
+size_t chunk_workspace(const KvPaged& c, int n_heads, int n_rows, int max_q, int max_kv);
+cudaError_t launch_chunk_attention(cudaStream_t st, const ChunkCall& a, int* launches);
+
+// ---------------------------------------------------------------------------------------------
+// Work split.  A tile is up to tq new tokens of one sequence (all query heads of a group of one KV head); its keys are
+// taken in units of `unit`.  A call with fewer tiles than the GPU holds CTAs (`target`) splits each sequence's keys into equal
+// runs so that at most `target` items exist; an item of a split tile leaves a partial (maximum, sum, weighted V) in slot
+// `item` of the workspace, joined in split order by a second launch.  The split follows from the device's lengths, so a
+// captured launch stays balanced when they change.
+// ---------------------------------------------------------------------------------------------
+struct SplitPlan {
+  int tq, groups, unit, target;   // tokens per tile; head groups; keys per unit; items aimed at
+};
+struct SplitItem {
+  int seq, q0, c, len;        // sequence, its first row, new tokens, cached positions
+  int tile, group;            // token tile, head group
+  int split, n_split;         // this item's run of keys, and how many
+  int u0, u1;                 // its units of keys
+  int slot0;                  // slot of the tile's first split
+};
+
+// Lengths of sequence b, or no work (c = 0) where they are out of bounds.
+__device__ __forceinline__ void chunk_seq(const ChunkCall& a, int b, int& q0, int& c, int& len) {
+  q0 = a.q_start[b];
+  c = a.q_start[b + 1] - q0;
+  len = a.kv_len[b];
+  const int cap = min(a.max_kv, a.c.max_blocks * a.c.block_tokens);
+  if (q0 < 0 || c < 0 || c > a.max_q || q0 > a.n_rows - c || len < 0 || len > cap) {
+    a.c.flag(ERRW_POS);
+    c = 0;
+    len = 0;
+  }
+}
+
+// Item `id` of the plan (joined: tile `id`, its splits taken together), looked up by one converged warp; false: none.
+__device__ __forceinline__ bool split_find(const ChunkCall& a, const SplitPlan& p, int id, bool joined, SplitItem& it) {
+  const int lane = threadIdx.x & 31, n_seq = a.c.n_seq;
+  long long base = 0, tot = 0;
+  int q0 = 0, c = 0, len = 0;
+  for (int b0 = 0; b0 < n_seq; b0 += 32) {
+    const int b = b0 + lane;
+    q0 = c = len = 0;
+    if (b < n_seq) chunk_seq(a, b, q0, c, len);
+    const long long t = (long long)((c + p.tq - 1) / p.tq) * p.groups;
+    base += t;
+    tot += t * ((len + p.unit - 1) / p.unit);
+  }
+#pragma unroll
+  for (int o = 16; o; o >>= 1) {
+    base += __shfl_xor_sync(0xffffffffu, base, o);
+    tot += __shfl_xor_sync(0xffffffffu, tot, o);
+  }
+  // run length S: sum over tiles of ceil(units / S) <= tot / S + base <= target
+  long long S = 1ll << 40;
+  if (base < p.target) S = max(1ll, (tot + (p.target - base) - 1) / (p.target - base));
+  long long before = 0;
+  long long slots = 0;
+  for (int b0 = 0; b0 < n_seq; b0 += 32) {
+    const int b = b0 + lane;
+    if (n_seq > 32) {
+      q0 = c = len = 0;
+      if (b < n_seq) chunk_seq(a, b, q0, c, len);
+    }
+    const int tiles = (c + p.tq - 1) / p.tq, units = (len + p.unit - 1) / p.unit;
+    int ns = (int)min((long long)units, (units + S - 1) / S);
+    ns = max(ns, 1);
+    const long long n_it = (long long)tiles * p.groups * ns, mine = joined ? (long long)tiles * p.groups : n_it;
+    long long inc = mine, sl = n_it;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const long long u = __shfl_up_sync(0xffffffffu, inc, o), w = __shfl_up_sync(0xffffffffu, sl, o);
+      if (lane >= o) {
+        inc += u;
+        sl += w;
+      }
+    }
+    const long long lo = before + inc - mine;
+    const bool hit = id >= lo && id < lo + mine;
+    const unsigned who = __ballot_sync(0xffffffffu, hit);
+    if (who) {
+      const int src = __ffs(who) - 1;
+      const long long s0 = slots + sl - n_it;
+      const int lo_ = __shfl_sync(0xffffffffu, (int)lo, src), s0_ = __shfl_sync(0xffffffffu, (int)s0, src);
+      it.seq = b0 + src;
+      it.q0 = __shfl_sync(0xffffffffu, q0, src);
+      it.c = __shfl_sync(0xffffffffu, c, src);
+      it.len = __shfl_sync(0xffffffffu, len, src);
+      it.n_split = __shfl_sync(0xffffffffu, ns, src);
+      const int un = __shfl_sync(0xffffffffu, units, src), nt = __shfl_sync(0xffffffffu, tiles, src);
+      int r = id - lo_;
+      it.split = 0;
+      if (!joined) {
+        it.split = r % it.n_split;
+        r /= it.n_split;
+      }
+      // the last tiles (the longest) come first, all head groups of one together
+      const int tg = r;
+      it.group = r % p.groups;
+      it.tile = nt - 1 - r / p.groups;
+      it.slot0 = s0_ + tg * it.n_split;
+      const int per = (un + it.n_split - 1) / it.n_split;
+      it.u0 = min(un, it.split * per);
+      it.u1 = min(un, it.u0 + per);
+      return true;
+    }
+    before += __shfl_sync(0xffffffffu, inc, 31);
+    slots += __shfl_sync(0xffffffffu, sl, 31);
+  }
+  return false;
+}
+// Items there can be at most: the target, or one per tile where there are more tiles.
+static inline long long split_items(const SplitPlan& p, int n_seq, int n_rows, int max_q) {
+  const long long by_seq = (long long)n_seq * ((max_q + p.tq - 1) / p.tq);
+  const long long by_rows = n_rows / p.tq + (long long)n_seq;
+  const long long tiles = (by_seq < by_rows ? by_seq : by_rows) * p.groups;
+  return tiles > p.target ? tiles : p.target;
+}
+
+}  // namespace adept

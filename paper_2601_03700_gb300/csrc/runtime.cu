@@ -2305,6 +2305,8 @@ void model_set_error(adept_model* m, const char* msg) {
   if (m) m->err = msg;
 }
 
+void global_set_error(const char* msg) { g_load_error = msg; }
+
 void model_add_launches(adept_model* m, int n) {
   if (m) m->launches += n;
 }
