@@ -169,6 +169,433 @@ __global__ void __launch_bounds__(CG_KEYS) chunk_any_kernel(const __grid_constan
 }
 
 // ---------------------------------------------------------------------------------------------
+// bf16 queries over bf16 or e4m3 entries in blocks of 16 positions: warp-level matrix instructions (m16n8k16), for the calls
+// that are a stream of K and V (steps, checks of a few tokens).  CTA = a tile of 16 rows (token x query head of the KV
+// head's group) x a run of keys, CF_WARPS warps taking blocks in turn, each with a softmax and sums of its own, merged in
+// warp order at the end.
+//
+// K and V go from memory straight into the registers that the matrix instruction takes: the order of the head's dimensions
+// inside q.k is free, so a thread's B fragments of S = Q K^T are whole 16-byte pieces of its key's row (Q is loaded in the
+// same order), and the columns of O are dealt out so that a thread's B fragments of O = P V are 16-byte pieces of four keys'
+// rows, pairs of keys packed by byte permutes.  No shared memory, no barrier in the loop; the next block's K is under way
+// while the softmax runs, the next V during the next S.  An exponent of K scales S, one of V scales P: e4m3 -> bf16 is exact.
+// ---------------------------------------------------------------------------------------------
+constexpr int CF_WARPS = 4, CF_ROWS = 16;
+constexpr float CF_RAISE = 8.f;   // the running maximum is raised once a score exceeds it by 2^8: weights stay below 256
+
+template <int BYTES>
+struct Words {
+  uint32_t w[BYTES / 4];
+};
+template <int BYTES>
+__device__ __forceinline__ Words<BYTES> ldg(const void* p) {
+  Words<BYTES> r;
+  if constexpr (BYTES == 16)
+    asm volatile("ld.global.L1::no_allocate.v4.b32 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(r.w[0]), "=r"(r.w[1]), "=r"(r.w[2]), "=r"(r.w[3]) : "l"(p));
+  else if constexpr (BYTES == 8)
+    asm volatile("ld.global.L1::no_allocate.v2.b32 {%0, %1}, [%2];" : "=r"(r.w[0]), "=r"(r.w[1]) : "l"(p));
+  else
+    asm volatile("ld.global.L1::no_allocate.b32 %0, [%1];" : "=r"(r.w[0]) : "l"(p));
+  return r;
+}
+// (volatile: stays behind the loads that precede it in the source)
+__device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// Two e4m3 codes (low 16 bits) as two bf16: exact, NaN stays NaN.
+__device__ __forceinline__ uint32_t e4m3x2_bf16x2(uint32_t codes) {
+  const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)codes, __NV_E4M3);
+  const float2 f = __half22float2(__half2(h));
+  const __nv_bfloat162 b = __floats2bfloat162_rn(f.x, f.y);
+  return *reinterpret_cast<const uint32_t*>(&b);
+}
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
+  const __nv_bfloat162 x = __floats2bfloat162_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&x);
+}
+
+template <int DH, int KT>
+struct FewShape {
+  static constexpr int ES = KT == KV_BF16 ? 2 : 1;
+  static constexpr int NB = KT == KV_BF16 ? 1 : 2;         // blocks of 16 keys per warp and round
+  static constexpr int UNIT = CF_WARPS * NB * 16;
+  static constexpr int KVEC = DH * ES / 4 < 16 ? DH * ES / 4 : 16, KN = DH * ES / 4 / KVEC, KE = KVEC / ES;   // K pieces of a thread
+  static constexpr int VVEC = DH * ES / 8 < 16 ? DH * ES / 8 : 16, VN = DH * ES / 8 / VVEC, VE = VVEC / ES;   // V pieces
+  static constexpr int SMEM = CF_WARPS * CF_ROWS * (DH + 4) * 4;
+};
+
+template <int DH, int KT>
+__global__ void __launch_bounds__(CF_WARPS * 32, 2) chunk_few_kernel(const __grid_constant__ ChunkCall a,
+                                                                     const __grid_constant__ SplitPlan p, int per_tok, int sub) {
+  using F = FewShape<DH, KT>;
+  constexpr int KS = DH / 16;
+  __shared__ SplitItem s_it;
+  __shared__ int s_have;
+  __shared__ float s_m[CF_WARPS][CF_ROWS], s_l[CF_WARPS][CF_ROWS];
+  extern __shared__ float s_o[];   // [warp][row][DH + 4]
+  PDL_ENTRY();
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
+  if (warp == 0) {
+    SplitItem it;
+    const bool have = split_find(a, p, (int)blockIdx.x, false, it);
+    if (lane == 0) {
+      s_it = it;
+      s_have = have;
+    }
+  }
+  __syncthreads();
+  if (!s_have) return;
+  const SplitItem it = s_it;
+  const int group = a.n_heads / a.c.n_kv_heads, kvh = it.group / sub, g0 = it.group % sub * per_tok;
+  const int past = it.len - it.c, j0 = it.tile * p.tq, n = min(p.tq, it.c - j0);
+  const int n_row = n * per_tok;   // rows of the tile in use (those with g0 + r % per_tok >= group hold nothing)
+
+  // this thread's two rows (g, g + 8): Q fragments, and the keys each attends
+  uint32_t qf[KS][4];
+  int lim[2];
+#pragma unroll
+  for (int r2 = 0; r2 < 2; ++r2) {
+    const int r = g + 8 * r2, j = r / per_tok, gq = g0 + r % per_tok;
+    const bool on = r < n_row && gq < group;
+    lim[r2] = on ? max(past + j0 + j + 1, 0) : 0;
+    const bf16* q = (const bf16*)a.q + (size_t)(it.q0 + j0 + j) * a.ld_q + (size_t)(kvh * group + gq) * DH;
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      constexpr int SP = F::KE / 4;   // k-steps of a piece
+      const int dim = (s / SP * 4 + t) * F::KE + s % SP * 4;
+      uint2 x = make_uint2(0, 0);
+      if (on) x = *reinterpret_cast<const uint2*>(q + dim);
+      qf[s][r2] = x.x;
+      qf[s][2 + r2] = x.y;
+    }
+  }
+  const int lim_lo = max(past + j0 + 1, 0), lim_hi = max(past + j0 + n, 0);   // of the tile's first and last token
+  const int k_end = min(min(it.u1 * F::UNIT, it.len), lim_hi);                // keys that anyone attends
+  const int b_end = (k_end + 15) >> 4;
+  const size_t blk_stride = (size_t)a.c.n_kv_heads * 16;
+  const int* table = a.c.table + (size_t)it.seq * a.c.max_blocks;
+
+  float o[DH / 8][4], m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+#pragma unroll
+  for (int j = 0; j < DH / 8; ++j) o[j][0] = o[j][1] = o[j][2] = o[j][3] = 0.f;
+
+  // a round: NB blocks
+  struct Round {
+    Words<F::KVEC> k[F::NB][2][F::KN];
+    Words<F::VVEC> v[F::NB][4][F::VN];
+    uint32_t ke[F::NB], ve[F::NB];   // exponents of keys 2t, 2t + 1 (low half) and 8 + 2t, 9 + 2t
+  } R;
+  long long at[F::NB];   // entry 0 of the round's blocks, -1: not there
+  const int first = it.u0 * (F::UNIT / 16) + warp * F::NB;
+  // table entries of the next 32 rounds' blocks of this warp: a lane each
+  auto look = [&](int b) {
+    int blk = -1;
+    if (b < b_end) {
+      blk = table[b];
+      if (blk < 0 || blk >= a.c.n_blocks) {
+        a.c.flag(ERRW_POS);
+        blk = -1;
+      }
+    }
+    return blk;
+  };
+  constexpr int STEP = CF_WARPS * F::NB, AHEAD = 32 / F::NB;
+  int tab = -1, round = 0;
+  auto blocks_of = [&](int b) {   // blocks b .. b + NB - 1, round number `round`
+    if (round % AHEAD == 0) tab = look(b + lane / F::NB * STEP + lane % F::NB);
+#pragma unroll
+    for (int i = 0; i < F::NB; ++i) {
+      const int blk = __shfl_sync(0xffffffffu, tab, round % AHEAD * F::NB + i);
+      at[i] = blk < 0 ? -1 : (long long)blk * blk_stride + kvh * 16;
+    }
+    ++round;
+  };
+  auto load_k = [&]() {
+#pragma unroll
+    for (int i = 0; i < F::NB; ++i) {
+      if (at[i] < 0) continue;
+#pragma unroll
+      for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+        for (int c = 0; c < F::KN; ++c)
+          R.k[i][nt][c] = ldg<F::KVEC>((const char*)a.c.k + ((size_t)at[i] + nt * 8 + g) * (DH * F::ES) + (c * 4 + t) * F::KVEC);
+      if constexpr (KT == KV_E4M3) {
+        const uint8_t* e = a.c.k_exp + at[i] + 2 * t;
+        R.ke[i] = *reinterpret_cast<const uint16_t*>(e) | (uint32_t) * reinterpret_cast<const uint16_t*>(e + 8) << 16;
+      }
+    }
+  };
+  auto load_v = [&]() {
+#pragma unroll
+    for (int i = 0; i < F::NB; ++i) {
+      if (at[i] < 0) continue;
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+#pragma unroll
+        for (int c = 0; c < F::VN; ++c)
+          R.v[i][k][c] = ldg<F::VVEC>((const char*)a.c.v + ((size_t)at[i] + 2 * t + (k & 1) + (k >> 1) * 8) * (DH * F::ES) +
+                                      (c * 8 + g) * F::VVEC);
+      if constexpr (KT == KV_E4M3) {
+        const uint8_t* e = a.c.v_exp + at[i] + 2 * t;
+        R.ve[i] = *reinterpret_cast<const uint16_t*>(e) | (uint32_t) * reinterpret_cast<const uint16_t*>(e + 8) << 16;
+      }
+    }
+  };
+  // (words of blocks that are not there are never read into sums: zero from the start)
+#pragma unroll
+  for (int i = 0; i < F::NB; ++i) {
+#pragma unroll
+    for (int x = 0; x < 2 * F::KN; ++x)
+#pragma unroll
+      for (int w = 0; w < F::KVEC / 4; ++w) R.k[i][x / F::KN][x % F::KN].w[w] = 0;
+#pragma unroll
+    for (int x = 0; x < 4 * F::VN; ++x)
+#pragma unroll
+      for (int w = 0; w < F::VVEC / 4; ++w) R.v[i][x / F::VN][x % F::VN].w[w] = 0;
+    R.ke[i] = R.ve[i] = 0;
+  }
+
+  if (first < b_end) {
+    blocks_of(first);
+    load_k();
+    load_v();
+  }
+  for (int b = first; b < b_end; b += STEP) {
+    bool here[F::NB], edge = false;   // edge: some key of the round is not everyone's
+#pragma unroll
+    for (int i = 0; i < F::NB; ++i) {
+      here[i] = at[i] >= 0;
+      edge |= !here[i];
+    }
+    edge |= (b + F::NB) * 16 > lim_lo || (b + F::NB) * 16 > k_end;
+    // S = Q K^T
+    float s[2 * F::NB][4];
+#pragma unroll
+    for (int i = 0; i < F::NB; ++i)
+#pragma unroll
+      for (int nt = 0; nt < 2; ++nt) {
+        float(&d)[4] = s[2 * i + nt];
+        d[0] = d[1] = d[2] = d[3] = 0.f;
+#pragma unroll
+        for (int c = 0; c < F::KN; ++c)
+#pragma unroll
+          for (int w = 0; w < F::KE / 4; ++w) {
+            const int ks = c * (F::KE / 4) + w;
+            if constexpr (KT == KV_BF16) {
+              mma16816(d, qf[ks], R.k[i][nt][c].w[2 * w], R.k[i][nt][c].w[2 * w + 1]);
+            } else {
+              const uint32_t x = R.k[i][nt][c].w[w];
+              mma16816(d, qf[ks], e4m3x2_bf16x2(x & 0xffffu), e4m3x2_bf16x2(x >> 16));
+            }
+          }
+        if constexpr (KT == KV_E4M3) {
+          const float e0 = exp_scale((R.ke[i] >> (nt * 16)) & 0xff) * a.scale_log2;
+          const float e1 = exp_scale((R.ke[i] >> (nt * 16 + 8)) & 0xff) * a.scale_log2;
+          d[0] *= e0; d[1] *= e1; d[2] *= e0; d[3] *= e1;
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) d[e] *= a.scale_log2;
+        }
+      }
+    const bool more = b + STEP < b_end;
+    if (more) {
+      blocks_of(b + STEP);
+      load_k();
+    }
+    unsigned att = ~0u;   // bit (tile, element): the row attends the key
+    if (edge) {
+      att = 0;
+#pragma unroll
+      for (int x = 0; x < 2 * F::NB; ++x)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int key = b * 16 + x * 8 + 2 * t + (e & 1);
+          const bool on = here[x / 2] && key < min(lim[e >> 1], k_end);
+          att |= (unsigned)on << (x * 4 + e);
+          if (!on) s[x][e] = -INFINITY;
+        }
+    }
+    // softmax of the two rows
+    float mx[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+    for (int x = 0; x < 2 * F::NB; ++x) {
+      mx[0] = fmaxf(mx[0], fmaxf(s[x][0], s[x][1]));
+      mx[1] = fmaxf(mx[1], fmaxf(s[x][2], s[x][3]));
+    }
+    float ref[2];
+    bool raise = false;
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+      mx[r] = fmaxf(mx[r], __shfl_xor_sync(0xffffffffu, mx[r], 1));
+      mx[r] = fmaxf(mx[r], __shfl_xor_sync(0xffffffffu, mx[r], 2));
+      raise |= mx[r] > m[r] + CF_RAISE || (m[r] == -INFINITY && mx[r] > m[r]);
+    }
+    if (__any_sync(0xffffffffu, raise)) {
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        const float mn = fmaxf(m[r], mx[r]), f = mn == -INFINITY ? 1.f : ex2_approx(m[r] - mn);
+        m[r] = mn;
+        l[r] *= f;
+#pragma unroll
+        for (int j = 0; j < DH / 8; ++j) {
+          o[j][2 * r] *= f;
+          o[j][2 * r + 1] *= f;
+        }
+      }
+    }
+#pragma unroll
+    for (int r = 0; r < 2; ++r) ref[r] = m[r] == -INFINITY ? 0.f : m[r];
+#pragma unroll
+    for (int x = 0; x < 2 * F::NB; ++x)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        s[x][e] = ex2_approx(s[x][e] - ref[e >> 1]);
+        l[e >> 1] += s[x][e];
+      }
+    // O += P V
+#pragma unroll
+    for (int i = 0; i < F::NB; ++i) {
+      uint32_t pf[4];
+      if constexpr (KT == KV_E4M3) {
+        const float e0 = exp_scale(R.ve[i] & 0xff), e1 = exp_scale((R.ve[i] >> 8) & 0xff);
+        const float e2 = exp_scale((R.ve[i] >> 16) & 0xff), e3 = exp_scale(R.ve[i] >> 24);
+        pf[0] = pack_bf16(s[2 * i][0] * e0, s[2 * i][1] * e1);
+        pf[1] = pack_bf16(s[2 * i][2] * e0, s[2 * i][3] * e1);
+        pf[2] = pack_bf16(s[2 * i + 1][0] * e2, s[2 * i + 1][1] * e3);
+        pf[3] = pack_bf16(s[2 * i + 1][2] * e2, s[2 * i + 1][3] * e3);
+      } else {
+        pf[0] = pack_bf16(s[2 * i][0], s[2 * i][1]);
+        pf[1] = pack_bf16(s[2 * i][2], s[2 * i][3]);
+        pf[2] = pack_bf16(s[2 * i + 1][0], s[2 * i + 1][1]);
+        pf[3] = pack_bf16(s[2 * i + 1][2], s[2 * i + 1][3]);
+      }
+      bool poison = false;
+      if (edge) {
+        // V of keys that nobody here attends counts as zero; a NaN or infinite one that only some rows attend must
+        // not reach the others through 0 * NaN: it counts as zero and is put into the sums of its rows as NaN
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const int key = (b + i) * 16 + 2 * t + (k & 1) + (k >> 1) * 8;
+          const bool off = !here[i] || key >= k_end;
+#pragma unroll
+          for (int c = 0; c < F::VN; ++c)
+#pragma unroll
+            for (int w = 0; w < F::VVEC / 4; ++w) {
+              uint32_t& x = R.v[i][k][c].w[w];
+              if (off) x = 0;
+              if constexpr (KT == KV_BF16)
+                poison |= __vcmpeq2(x & 0x7f807f80u, 0x7f807f80u) != 0;
+              else
+                poison |= __vcmpeq4(x & 0x7f7f7f7fu, 0x7f7f7f7fu) != 0;
+            }
+        }
+        if constexpr (KT == KV_E4M3) {
+          // (an exponent of such a key must not make its weight of 0 a NaN)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const unsigned lo = att >> (2 * i * 4 + (e & 1) * 2 + (e >> 1) * 4);
+            if (!(lo & 1u)) pf[e] &= 0xffff0000u;
+            if (!(lo & 2u)) pf[e] &= 0x0000ffffu;
+          }
+        }
+        poison = __any_sync(0xffffffffu, poison);
+      }
+      uint32_t ones[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {   // fragment e: row half e & 1, key tile e >> 1
+        const unsigned bits = att >> ((2 * i + (e >> 1)) * 4 + (e & 1) * 2);
+        ones[e] = (bits & 1u ? 0x3f80u : 0u) | (bits & 2u ? 0x3f800000u : 0u);
+      }
+      auto pv = [&](int j, uint32_t b0, uint32_t b1) {
+        if (!poison) {
+          mma16816(o[j], pf, b0, b1);
+          return;
+        }
+        const uint32_t n0 = __vcmpeq2(b0 & 0x7f807f80u, 0x7f807f80u), n1 = __vcmpeq2(b1 & 0x7f807f80u, 0x7f807f80u);
+        mma16816(o[j], pf, b0 & ~n0, b1 & ~n1);
+        float cnt[4] = {0.f, 0.f, 0.f, 0.f};
+        mma16816(cnt, ones, n0 & 0x3f803f80u, n1 & 0x3f803f80u);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (cnt[e] > 0.f) o[j][e] = NAN;
+      };
+#pragma unroll
+      for (int c = 0; c < F::VN; ++c)
+#pragma unroll
+        for (int w = 0; w < F::VVEC / 4; ++w) {
+          const uint32_t k0 = R.v[i][0][c].w[w], k1 = R.v[i][1][c].w[w], k2 = R.v[i][2][c].w[w], k3 = R.v[i][3][c].w[w];
+          if constexpr (KT == KV_BF16) {
+            const int j = c * F::VE + 2 * w;
+            pv(j, __byte_perm(k0, k1, 0x5410), __byte_perm(k2, k3, 0x5410));
+            pv(j + 1, __byte_perm(k0, k1, 0x7632), __byte_perm(k2, k3, 0x7632));
+          } else {
+            const int j = c * F::VE + 4 * w;
+            const uint32_t x0 = __byte_perm(k0, k1, 0x5140), x1 = __byte_perm(k2, k3, 0x5140);
+            const uint32_t y0 = __byte_perm(k0, k1, 0x7362), y1 = __byte_perm(k2, k3, 0x7362);
+            pv(j, e4m3x2_bf16x2(x0 & 0xffffu), e4m3x2_bf16x2(x1 & 0xffffu));
+            pv(j + 1, e4m3x2_bf16x2(x0 >> 16), e4m3x2_bf16x2(x1 >> 16));
+            pv(j + 2, e4m3x2_bf16x2(y0 & 0xffffu), e4m3x2_bf16x2(y1 & 0xffffu));
+            pv(j + 3, e4m3x2_bf16x2(y0 >> 16), e4m3x2_bf16x2(y1 >> 16));
+          }
+        }
+    }
+    if (more) load_v();
+  }
+
+  // merge of the warps, in warp order
+#pragma unroll
+  for (int r = 0; r < 2; ++r) {
+    l[r] += __shfl_xor_sync(0xffffffffu, l[r], 1);
+    l[r] += __shfl_xor_sync(0xffffffffu, l[r], 2);
+    if (t == 0) {
+      s_m[warp][g + 8 * r] = m[r];
+      s_l[warp][g + 8 * r] = l[r];
+    }
+  }
+  constexpr int LD = DH + 4;
+#pragma unroll
+  for (int j = 0; j < DH / 8; ++j) {
+    const int c = j / F::VE, e = j % F::VE;
+#pragma unroll
+    for (int x = 0; x < 4; ++x)
+      s_o[(warp * CF_ROWS + g + 8 * (x >> 1)) * LD + (c * 8 + 2 * t + (x & 1)) * F::VE + e] = o[j][x];
+  }
+  __syncthreads();
+  const PartView pv(a, p, CF_ROWS, DH, it.slot0 + it.split);
+  for (int i = tid; i < n_row * (DH / 4); i += CF_WARPS * 32) {
+    const int r = i / (DH / 4), d = i % (DH / 4) * 4, j = r / per_tok, gq = g0 + r % per_tok;
+    if (gq >= group) continue;
+    float M = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < CF_WARPS; ++w) M = fmaxf(M, s_m[w][r]);
+    const float mref = M == -INFINITY ? 0.f : M;
+    float L = 0.f, x[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < CF_WARPS; ++w) {
+      const float f = ex2_approx(s_m[w][r] - mref);
+      const float4 v = *reinterpret_cast<const float4*>(&s_o[(w * CF_ROWS + r) * LD + d]);
+      L += f * s_l[w][r];
+      x[0] += f * v.x;
+      x[1] += f * v.y;
+      x[2] += f * v.z;
+      x[3] += f * v.w;
+    }
+    if (it.n_split > 1) {
+      *reinterpret_cast<float4*>(pv.o + r * DH + d) = make_float4(x[0], x[1], x[2], x[3]);
+      if (d == 0) *reinterpret_cast<float2*>(pv.ml + r * 2) = make_float2(M, L);
+    } else {
+      const float inv = past + j0 + j < 0 ? 0.f : 1.f / L;
+      uint2 y = make_uint2(pack_bf16(x[0] * inv, x[1] * inv), pack_bf16(x[2] * inv, x[3] * inv));
+      *reinterpret_cast<uint2*>((bf16*)a.out + (size_t)(it.q0 + j0 + j) * a.ld_out + (size_t)(kvh * group + gq) * DH + d) = y;
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------------------------
 // Join of split tiles: CTA = one tile; per row the splits' partials in split order.
 //   M = max m_i,  out = sum_i 2^(m_i - M) O_i / sum_i 2^(m_i - M) l_i
 // ---------------------------------------------------------------------------------------------
@@ -228,36 +655,47 @@ int chunk_sms() {
   return sms;
 }
 
-// How a call is run: its plan, rows of a tile and query heads of a tile's token.
+// How a call is run: its kernel, plan, rows of a tile, query heads of a tile's token and head groups per KV head.
+enum ChunkKind { CHUNK_ANY, CHUNK_FEW };
 struct ChunkHow {
+  ChunkKind kind;
   SplitPlan p;
   int rows, per_tok, sub;
   bool may_split;
 };
-ChunkHow chunk_how(const KvPaged& c, int n_heads, int n_rows, int max_q, int max_kv) {
+ChunkHow chunk_how(const KvPaged& c, int n_heads, int max_kv, bool aligned) {
+  const int group = n_heads / c.n_kv_heads;
   ChunkHow w;
-  w.rows = CG_ROWS;
-  w.per_tok = 1;
-  w.sub = n_heads / c.n_kv_heads;
-  w.p = SplitPlan{CG_ROWS, n_heads, CG_KEYS, chunk_sms() * 4};
-  (void)n_rows;
-  (void)max_q;
+  if (c.type != KV_F32 && c.block_tokens == 16 && aligned) {
+    w.kind = CHUNK_FEW;
+    w.rows = CF_ROWS;
+    w.per_tok = std::min(group, CF_ROWS);
+    w.sub = cdiv(group, w.per_tok);
+    w.p = SplitPlan{CF_ROWS / w.per_tok, c.n_kv_heads * w.sub, CF_WARPS * 16 * (c.type == KV_BF16 ? 1 : 2), chunk_sms() * 2};
+  } else {
+    w.kind = CHUNK_ANY;
+    w.rows = CG_ROWS;
+    w.per_tok = 1;
+    w.sub = group;
+    w.p = SplitPlan{CG_ROWS, n_heads, CG_KEYS, chunk_sms() * 4};
+  }
   w.may_split = max_kv > w.p.unit;
   return w;
 }
-
-}  // namespace
-
-size_t chunk_workspace(const KvPaged& c, int n_heads, int n_rows, int max_q, int max_kv) {
-  const ChunkHow w = chunk_how(c, n_heads, n_rows, max_q, max_kv);
-  return w.may_split ? (size_t)w.p.target * w.rows * (c.head_dim + 2) * sizeof(float) : 0;
+size_t how_bytes(const ChunkHow& w, int dh) {
+  return w.may_split ? (size_t)w.p.target * w.rows * (dh + 2) * sizeof(float) : 0;
 }
 
 template <int DH, int KT, typename T>
-static cudaError_t chunk_t(cudaStream_t st, const ChunkCall& a, const ChunkHow& w, int* launches) {
-  const long long items = split_items(w.p, a.c.n_seq, a.n_rows, a.max_q);
+cudaError_t chunk_t(cudaStream_t st, const ChunkCall& a, const ChunkHow& w, int* launches) {
+  const dim3 grid((unsigned)split_items(w.p, a.c.n_seq, a.n_rows, a.max_q));
   *launches = 1;
-  cudaError_t e = launch_k(chunk_any_kernel<DH, KT, T>, dim3((unsigned)items), dim3(CG_KEYS), 0, st, a, w.p);
+  cudaError_t e = cudaErrorInvalidValue;
+  if (w.kind == CHUNK_ANY) {
+    e = launch_k(chunk_any_kernel<DH, KT, T>, grid, dim3(CG_KEYS), 0, st, a, w.p);
+  } else if constexpr (KT != KV_F32) {
+    e = launch_k(chunk_few_kernel<DH, KT>, grid, dim3(CF_WARPS * 32), FewShape<DH, KT>::SMEM, st, a, w.p, w.per_tok, w.sub);
+  }
   if (e == cudaSuccess && w.may_split) {
     *launches = 2;
     e = launch_k(chunk_join_kernel<DH, T>, dim3((unsigned)w.p.target), dim3(128), 0, st, a, w.p, w.rows, w.per_tok, w.sub);
@@ -265,8 +703,19 @@ static cudaError_t chunk_t(cudaStream_t st, const ChunkCall& a, const ChunkHow& 
   return e;
 }
 
+}  // namespace
+
+// (whatever kernel the rows' alignment picks)
+size_t chunk_workspace(const KvPaged& c, int n_heads, int n_rows, int max_q, int max_kv) {
+  (void)n_rows;
+  (void)max_q;
+  return std::max(how_bytes(chunk_how(c, n_heads, max_kv, true), c.head_dim),
+                  how_bytes(chunk_how(c, n_heads, max_kv, false), c.head_dim));
+}
+
 cudaError_t launch_chunk_attention(cudaStream_t st, const ChunkCall& a, int* launches) {
-  const ChunkHow w = chunk_how(a.c, a.n_heads, a.n_rows, a.max_q, a.max_kv);
+  const bool aligned = (((uintptr_t)a.q | (uintptr_t)a.out) & 15) == 0 && a.ld_q % 8 == 0 && a.ld_out % 8 == 0;
+  const ChunkHow w = chunk_how(a.c, a.n_heads, a.max_kv, aligned);
 #define CH_DH(D)                                                                   \
   case D:                                                                          \
     if (a.c.type == KV_F32) return chunk_t<D, KV_F32, float>(st, a, w, launches);  \
