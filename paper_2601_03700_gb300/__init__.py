@@ -413,7 +413,8 @@ class KVCache:
             self.v_exp = torch.full_like(self.k_exp, 127)
         self.block_table = torch.full((n_seq, max_blocks_per_seq), -1, dtype=torch.int32, device=device)
         self.err = torch.zeros(1, dtype=torch.int32, device=device)
-        self.device = self.k.device
+        self.device, self.index = self.k.device, self.k.get_device()   # (index < 0: not a GPU)
+        self.q_dtype = torch.float32 if dtype == "f32" else torch.bfloat16
         self.n_seq, self.n_kv_heads, self.head_dim = n_seq, n_kv_heads, head_dim
         p = lambda x: None if x is None else x.data_ptr()  # noqa: E731
         self._c = AdeptKVCache(t, n_blocks, n_kv_heads, head_dim, block_tokens, n_seq, max_blocks_per_seq, p(self.k),
@@ -431,48 +432,61 @@ class KVCache:
         adept_kv_check(self, stream)
 
 
-def _on(cache: KVCache):
-    """The cache's device as the current one."""
-    if cache.device.type != "cuda":
-        raise ValueError(f"the cache is on {cache.device}: the operators need a GPU")
-    return contextlib.nullcontext() if torch.cuda.current_device() == cache.device.index else torch.cuda.device(cache.device)
-
-
 def _rows(cache: KVCache, name: str, t: torch.Tensor, heads: int):
-    """(rows, row stride, dtype) of [rows, heads, head_dim], or [rows, heads * head_dim], dense within a row."""
-    w = heads * cache.head_dim
-    if t.device != cache.device:
+    """(rows, row stride) of [rows, heads, head_dim], or [rows, heads * head_dim], dense within a row, on the cache's GPU."""
+    shape, st, dh = t.shape, t.stride(), cache.head_dim
+    w = heads * dh
+    if t.get_device() != cache.index:
         raise ValueError(f"{name} is on {t.device}, the cache on {cache.device}")
-    if t.dtype not in (torch.float32, torch.bfloat16):
-        raise ValueError(f"{name} must be float32 or bfloat16")
-    if t.dim() == 3 and tuple(t.shape[1:]) == (heads, cache.head_dim):
-        dense = t.stride(2) == 1 and (heads == 1 or t.stride(1) == cache.head_dim)
-    elif t.dim() == 2 and t.shape[1] == w:
-        dense = t.stride(1) == 1
+    if len(shape) == 3 and shape[1] == heads and shape[2] == dh:
+        dense = st[2] == 1 and (heads == 1 or st[1] == dh)
+    elif len(shape) == 2 and shape[1] == w:
+        dense = st[1] == 1
     else:
-        raise ValueError(f"{name} must be [rows, {heads}, {cache.head_dim}]")
-    n = t.shape[0]
-    ld = t.stride(0) if n > 1 else w
+        raise ValueError(f"{name} must be [rows, {heads}, {dh}]")
+    n = shape[0]
+    ld = st[0] if n > 1 else w
     if n and (not dense or ld < w):
         raise ValueError(f"the rows of {name} must be dense and must not overlap")
-    return n, ld, 1 if t.dtype == torch.bfloat16 else 0
+    return n, ld
 
 
 def _index(cache: KVCache, name: str, t: torch.Tensor, n: int):
-    if t.dtype != torch.int32 or t.device != cache.device or t.dim() != 1 or t.numel() != n or not t.is_contiguous():
+    if t.dtype is not torch.int32 or t.get_device() != cache.index or t.shape != (n,) or not t.is_contiguous():
         raise ValueError(f"{name} must be {n} contiguous int32 values on {cache.device}")
     return t.data_ptr()
 
 
+def _call(cache: KVCache, fn, stream, *args):
+    """fn(cache, *args, stream) with the cache's device as the current one."""
+    if cache.index < 0:
+        raise ValueError(f"the cache is on {cache.device}: the operators need a GPU")
+    lib = _lib
+    if torch.cuda.current_device() == cache.index:
+        st = fn(cache.ref, *args, _raw_stream(cache.index) if stream is None else _stream(stream))
+    else:
+        with torch.cuda.device(cache.index):
+            st = fn(cache.ref, *args, _raw_stream(cache.index) if stream is None else _stream(stream))
+    if st != ADEPT_OK:
+        _check(lib, None, st)
+
+
+def _raw_stream(index: int) -> int:
+    return torch.cuda.current_stream(index).cuda_stream
+
+
+if hasattr(torch._C, "_cuda_getCurrentRawStream"):   # the same number without a Stream object (a third of a call's time)
+    _raw_stream = torch._C._cuda_getCurrentRawStream
+
+
 def _kv_rows(fn, cache, k, v, seq, pos, stream):
-    lib = load_library()
-    n, ld_k, dt = _rows(cache, "k", k, cache.n_kv_heads)
-    n_v, ld_v, dt_v = _rows(cache, "v", v, cache.n_kv_heads)
-    if n != n_v or dt != dt_v:
-        raise ValueError("k and v must have the same rows and type")
-    with _on(cache):
-        _check(lib, None, fn(cache.ref, n, dt, k.data_ptr(), ld_k, v.data_ptr(), ld_v, _index(cache, "seq", seq, n),
-                             _index(cache, "pos", pos, n), _stream(stream)))
+    n, ld_k = _rows(cache, "k", k, cache.n_kv_heads)
+    n_v, ld_v = _rows(cache, "v", v, cache.n_kv_heads)
+    dt = k.dtype
+    if n != n_v or v.dtype is not dt or (dt is not torch.bfloat16 and dt is not torch.float32):
+        raise ValueError("k and v must have the same rows and type, float32 or bfloat16")
+    _call(cache, fn, stream, n, 1 if dt is torch.bfloat16 else 0, k.data_ptr(), ld_k, v.data_ptr(), ld_v,
+          _index(cache, "seq", seq, n), _index(cache, "pos", pos, n))
 
 
 def adept_kv_append(cache: KVCache, k: torch.Tensor, v: torch.Tensor, seq: torch.Tensor, pos: torch.Tensor, stream=None):
@@ -493,32 +507,28 @@ def adept_chunk_attention(cache: KVCache, q: torch.Tensor, q_start: torch.Tensor
     over its kv_len[b] cached positions, into out.  workspace: KVCache.attention_workspace of these sizes (None: one is
     made for the call)."""
     lib = load_library()
-    want = torch.float32 if cache.dtype == "f32" else torch.bfloat16
-    if q.dtype != want or out.dtype != want:
-        raise ValueError(f"q and out of a {cache.dtype} cache are {want}")
+    if q.dtype is not cache.q_dtype or out.dtype is not cache.q_dtype:
+        raise ValueError(f"q and out of a {cache.dtype} cache are {cache.q_dtype}")
     heads = q.shape[1] if q.dim() == 3 else q.shape[-1] // cache.head_dim
-    n, ld_q, _ = _rows(cache, "q", q, heads)
-    n_o, ld_o, _ = _rows(cache, "out", out, heads)
+    n, ld_q = _rows(cache, "q", q, heads)
+    n_o, ld_o = _rows(cache, "out", out, heads)
     if n != n_o:
         raise ValueError("q and out must have the same rows")
-    qs, kl = _index(cache, "q_start", q_start, cache.n_seq + 1), _index(cache, "kv_len", kv_len, cache.n_seq)
-    with _on(cache):
-        if workspace is None:
-            s = stream if stream is None or hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream))
-            with torch.cuda.stream(s):   # (the call's stream: memory that it alone reuses)
-                workspace = cache.attention_workspace(heads, n, max_q_len, max_kv_len)
-        elif workspace.device != cache.device or not workspace.is_contiguous():
-            raise ValueError(f"workspace must be contiguous on {cache.device}")
-        ws, nb = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
-        _check(lib, None, lib.adept_chunk_attention(cache.ref, heads, n, q.data_ptr(), ld_q, qs, kl, int(max_q_len),
-                                                    int(max_kv_len), out.data_ptr(), ld_o, ws, nb, _stream(stream)))
+    if workspace is None:
+        s = stream if stream is None or hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream))
+        with torch.cuda.stream(s):   # (the call's stream: memory that it alone reuses)
+            workspace = cache.attention_workspace(heads, n, max_q_len, max_kv_len)
+    elif workspace.get_device() != cache.index or not workspace.is_contiguous():
+        raise ValueError(f"workspace must be contiguous on {cache.device}")
+    ws, nb = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.nbytes)
+    _call(cache, lib.adept_chunk_attention, stream, heads, n, q.data_ptr(), ld_q,
+          _index(cache, "q_start", q_start, cache.n_seq + 1), _index(cache, "kv_len", kv_len, cache.n_seq), max_q_len,
+          max_kv_len, out.data_ptr(), ld_o, ws, nb)
 
 
 def adept_kv_check(cache: KVCache, stream=None):
     """Waits for the stream and raises where a kernel flagged an input out of range since the last check."""
-    lib = load_library()
-    with _on(cache):
-        _check(lib, None, lib.adept_kv_check(cache.ref, _stream(stream)))
+    _call(cache, load_library().adept_kv_check, stream)
 
 
 # ---------------------------------------------------------------------------

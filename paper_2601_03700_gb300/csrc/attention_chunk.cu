@@ -656,16 +656,20 @@ int chunk_sms() {
 }
 
 // How a call is run: its kernel, plan, rows of a tile, query heads of a tile's token and head groups per KV head.
-enum ChunkKind { CHUNK_ANY, CHUNK_FEW };
+enum ChunkKind { CHUNK_ANY, CHUNK_FEW, CHUNK_TC };
 struct ChunkHow {
   ChunkKind kind;
   SplitPlan p;
   int rows, per_tok, sub;
   bool may_split;
 };
-ChunkHow chunk_how(const KvPaged& c, int n_heads, int max_kv, bool aligned) {
+ChunkHow chunk_how(const KvPaged& c, int n_heads, int max_q, int max_kv, bool aligned) {
   const int group = n_heads / c.n_kv_heads;
-  ChunkHow w;
+  ChunkHow w{};
+  if (aligned && (long long)max_q * group > CF_ROWS && chunk_tc_takes(c, n_heads)) {
+    w.kind = CHUNK_TC;
+    return w;
+  }
   if (c.type != KV_F32 && c.block_tokens == 16 && aligned) {
     w.kind = CHUNK_FEW;
     w.rows = CF_ROWS;
@@ -682,8 +686,9 @@ ChunkHow chunk_how(const KvPaged& c, int n_heads, int max_kv, bool aligned) {
   w.may_split = max_kv > w.p.unit;
   return w;
 }
-size_t how_bytes(const ChunkHow& w, int dh) {
-  return w.may_split ? (size_t)w.p.target * w.rows * (dh + 2) * sizeof(float) : 0;
+size_t how_bytes(const ChunkHow& w, const KvPaged& c) {
+  if (w.kind == CHUNK_TC) return chunk_tc_workspace(c);
+  return w.may_split ? (size_t)w.p.target * w.rows * (c.head_dim + 2) * sizeof(float) : 0;
 }
 
 template <int DH, int KT, typename T>
@@ -708,14 +713,13 @@ cudaError_t chunk_t(cudaStream_t st, const ChunkCall& a, const ChunkHow& w, int*
 // (whatever kernel the rows' alignment picks)
 size_t chunk_workspace(const KvPaged& c, int n_heads, int n_rows, int max_q, int max_kv) {
   (void)n_rows;
-  (void)max_q;
-  return std::max(how_bytes(chunk_how(c, n_heads, max_kv, true), c.head_dim),
-                  how_bytes(chunk_how(c, n_heads, max_kv, false), c.head_dim));
+  return std::max(how_bytes(chunk_how(c, n_heads, max_q, max_kv, true), c), how_bytes(chunk_how(c, n_heads, max_q, max_kv, false), c));
 }
 
 cudaError_t launch_chunk_attention(cudaStream_t st, const ChunkCall& a, int* launches) {
   const bool aligned = (((uintptr_t)a.q | (uintptr_t)a.out) & 15) == 0 && a.ld_q % 8 == 0 && a.ld_out % 8 == 0;
-  const ChunkHow w = chunk_how(a.c, a.n_heads, a.max_kv, aligned);
+  const ChunkHow w = chunk_how(a.c, a.n_heads, a.max_q, a.max_kv, aligned);
+  if (w.kind == CHUNK_TC) return launch_chunk_tc(st, a, launches);
 #define CH_DH(D)                                                                   \
   case D:                                                                          \
     if (a.c.type == KV_F32) return chunk_t<D, KV_F32, float>(st, a, w, launches);  \

@@ -1,0 +1,793 @@
+// Attention of a chunk of new tokens over a paged K/V cache on the tcgen05 tensor cores (what it computes:
+// attention_chunk.cu), for the calls whose sequences bring more rows than a warp-level tile.
+//
+// Tile: two sub-tiles of 128 rows (row = token x query head of one KV head's group, all of one sequence) x key tiles of 128.
+// Per key tile and sub-tile S = Q K^T (M 128, N 128, K d_h) and O += P V (P from tensor memory, V as stored, MN-major).
+// The two sub-tiles alternate: while the softmax of one runs, the tensor core works on the other.  Tensor memory (512
+// columns): S of sub-tile 0 and 1 (128 each), O of 0 and 1 (128 each); P (bf16, 64 columns) takes the place of its S.
+//
+// Warps:   0..3, 4..7   softmax of sub-tile 0 and 1, a thread per row (its TMEM lane): 128 scores in registers, running
+//                       maximum (raised only by more than 2^8), exp2, sum, P to tensor memory; at the end O / l
+//          8            issues the matrix instructions:  PV_0(j) S_0(j+1) PV_1(j) S_1(j+1)  (in issue order on the tensor
+//                       core, so S_0(j+1) may overwrite P_0(j), and a completed S(j+1) means a completed PV(j))
+//          9 ..         K and V.  bf16: 9 and 10 fetch K and V blocks by TMA, 10 mends the V tiles at the causal edge.  e4m3:
+//                       9..15 read codes, turn them into bf16 (exactly: code * 2^e) and store the swizzled tiles.
+//
+// The causal edge: from the first row's position on, a key tile holds keys that not every row attends, or none does.  Scores are
+// masked there.  V entries that nobody attends become zero; a NaN or infinite one is replaced by zero and its key noted per
+// column (the least one), and a row that attends that key gets NaN in that column at the end: 0 * NaN reaches nobody else.
+//
+// Work: every (tile, KV head) is a row of key tiles; all of them in a row are cut into equal runs, one per CTA (one CTA per SM),
+// so the GPU is evenly loaded whatever the mix of lengths.  A run holds whole tiles and at most two parts of tiles, whose
+// (maximum, sum, weighted V) go to the workspace and are joined in order by a second launch.
+// Every wait is bounded; a CTA that gives up sets the error word, drains its copies and matrix instructions and leaves.
+#define ADEPT_TU_ID 13
+#include "kv_paged.h"
+#include "gemm_tc.h"
+#include "tc_ptx.cuh"
+
+#include <cuda_fp8.h>
+
+#include <algorithm>
+#include <cstring>
+
+namespace adept {
+namespace {
+
+constexpr int CT_BM = 128, CT_BN = 128, CT_ROWS = 2 * CT_BM;
+constexpr float CT_RAISE = 8.f;
+constexpr long long CT_DRAIN_CYCLES = 4000000000LL;
+
+template <int DH, int KT>
+struct CtShape {
+  static constexpr int LOADERS = KT == KV_BF16 ? 2 : 7;            // warps 9 ..
+  static constexpr int THREADS = (9 + LOADERS) * 32;
+  static constexpr int HALVES = DH / 64;
+  static constexpr int Q_BYTES = HALVES * CT_BM * 128;             // one sub-tile: [half][row][128 B]
+  static constexpr int KV_BYTES = HALVES * CT_BN * 128;            // one K or V stage: [half][key][128 B]
+  static constexpr int OFF_K = 2 * Q_BYTES, OFF_V = OFF_K + 2 * KV_BYTES, TOTAL = OFF_V + 2 * KV_BYTES;
+};
+
+struct CtParams {
+  ChunkCall a;
+  CUtensorMap kmap, vmap;   // bf16: the pools as [n_blocks * n_kv_heads * 16][d_h], box {64, 16}
+  int ts;                   // tokens of a sub-tile
+  int runs;                 // CTAs
+  unsigned* no_err;         // where time-outs go without an error word (the workspace's last word)
+};
+
+// ---- the key tiles of all tiles in a row ----
+
+// sum over i in [0, n) of floor((a i + b) / m), a, b >= 0
+__device__ long long floor_sum(long long n, long long m, long long a, long long b) {
+  long long r = 0;
+  while (n > 0) {
+    r += (n - 1) * n / 2 * (a / m) + n * (b / m);
+    a %= m;
+    b %= m;
+    const long long y = a * n + b;
+    n = y / m;
+    b = y % m;
+    const long long x = m;
+    m = a;
+    a = x;
+    if (m == 0) break;
+  }
+  return r;
+}
+// Key tiles of token tile t (at least one: a tile without keys has zeros to write).
+__device__ __forceinline__ int ct_units(int c, int len, int tq, int t) {
+  return max(1, (len - c + min((t + 1) * tq, c) + CT_BN - 1) / CT_BN);
+}
+__device__ long long ct_seq_units(int c, int len, int tq) {
+  const int tiles = (c + tq - 1) / tq;
+  if (tiles == 0) return 0;
+  const long long last = ct_units(c, len, tq, tiles - 1);
+  if (tiles == 1) return last;
+  if (len - c + tq < 1) {   // (first tiles without keys: one by one)
+    long long r = 0;
+    for (int t = 0; t < tiles; ++t) r += ct_units(c, len, tq, t);
+    return r;
+  }
+  return last + floor_sum(tiles - 1, CT_BN, tq, (long long)(len - c) + tq + CT_BN - 1);
+}
+
+struct CtTile {
+  int seq, q0, c, len, tile, kvh;
+  long long u0;   // first unit of the tile
+  int units;
+};
+// All units, taken together by a converged warp.
+__device__ long long ct_total(const ChunkCall& a, int tq) {
+  long long tot = 0;
+  for (int b = threadIdx.x & 31; b < a.c.n_seq; b += 32) {
+    int q0, c, len;
+    chunk_seq(a, b, q0, c, len);
+    tot += ct_seq_units(c, len, tq) * a.c.n_kv_heads;
+  }
+#pragma unroll
+  for (int o = 16; o; o >>= 1) tot += __shfl_xor_sync(0xffffffffu, tot, o);
+  return tot;
+}
+// The tile that unit u lies in.
+__device__ void ct_find(const ChunkCall& a, int tq, long long u, CtTile& x) {
+  const int lane = threadIdx.x & 31;
+  long long before = 0;
+  for (int b0 = 0; b0 < a.c.n_seq; b0 += 32) {
+    int q0 = 0, c = 0, len = 0;
+    if (b0 + lane < a.c.n_seq) chunk_seq(a, b0 + lane, q0, c, len);
+    const long long mine = ct_seq_units(c, len, tq) * a.c.n_kv_heads;
+    long long inc = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const long long v = __shfl_up_sync(0xffffffffu, inc, o);
+      if (lane >= o) inc += v;
+    }
+    const unsigned who = __ballot_sync(0xffffffffu, u < before + inc);
+    if (!who) {
+      before += __shfl_sync(0xffffffffu, inc, 31);
+      continue;
+    }
+    const int src = __ffs(who) - 1;
+    before += __shfl_sync(0xffffffffu, inc - mine, src);
+    x.seq = b0 + src;
+    x.q0 = __shfl_sync(0xffffffffu, q0, src);
+    x.c = __shfl_sync(0xffffffffu, c, src);
+    x.len = __shfl_sync(0xffffffffu, len, src);
+    const int tiles = (x.c + tq - 1) / tq;
+    for (int t0 = 0; t0 < tiles; t0 += 32) {
+      const int t = t0 + lane;
+      const long long n = t < tiles ? (long long)ct_units(x.c, x.len, tq, t) * a.c.n_kv_heads : 0;
+      long long in2 = n;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const long long v = __shfl_up_sync(0xffffffffu, in2, o);
+        if (lane >= o) in2 += v;
+      }
+      const unsigned w2 = __ballot_sync(0xffffffffu, u < before + in2);
+      if (!w2) {
+        before += __shfl_sync(0xffffffffu, in2, 31);
+        continue;
+      }
+      const int s2 = __ffs(w2) - 1;
+      before += __shfl_sync(0xffffffffu, in2 - n, s2);
+      x.tile = t0 + s2;
+      x.units = ct_units(x.c, x.len, tq, x.tile);
+      x.kvh = (int)((u - before) / x.units);
+      x.u0 = before + (long long)x.kvh * x.units;
+      return;
+    }
+    return;
+  }
+}
+// Run i of `runs` (fewer where there are few units).
+constexpr int CT_MIN_RUN = 2;
+__device__ __forceinline__ int ct_runs(long long total, int runs) {
+  return (int)min((long long)runs, (total + CT_MIN_RUN - 1) / CT_MIN_RUN);
+}
+__device__ __forceinline__ long long ct_start(long long total, int runs, int i) { return total * i / runs; }
+
+// Slot s of the workspace: 256 (m, l) pairs, and behind all of those 256 rows of weighted V.
+__device__ __forceinline__ float* ct_ml(const CtParams& p, int slot) { return p.a.part + (size_t)slot * CT_ROWS * 2; }
+__device__ __forceinline__ float* ct_o(const CtParams& p, int slot, int dh) {
+  return p.a.part + (size_t)p.runs * 2 * CT_ROWS * 2 + (size_t)slot * CT_ROWS * dh;
+}
+
+__device__ __forceinline__ float ct_exp2i(int b) {   // 2^(b - 127)
+  return b ? __uint_as_float((unsigned)b << 23) : __uint_as_float(0x400000u);
+}
+__device__ __forceinline__ uint32_t ct_bf16x2(uint32_t codes, __nv_bfloat162 scale) {
+  const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)codes, __NV_E4M3);
+  const float2 f = __half22float2(__half2(h));
+  const __nv_bfloat162 r = __hmul2(__floats2bfloat162_rn(f.x, f.y), scale);
+  return *reinterpret_cast<const uint32_t*>(&r);
+}
+// Non-finite bf16 of a pair: 0xffff in its half.
+__device__ __forceinline__ uint32_t ct_bad2(uint32_t x) { return __vcmpeq2(x & 0x7f807f80u, 0x7f807f80u); }
+
+// A CTA's part of one tile: key tiles j_lo .. j_hi.
+struct CtSeg {
+  CtTile x;
+  int j_lo, j_hi, past, t0, n_tok;
+  int lim_lo, k_end;   // keys of the tile's first and of its last token (nobody attends beyond)
+  int nt[2], n_it;     // key tiles with keys: per sub-tile, of the segment
+  int slot;
+  bool whole, bad;     // the whole tile; some block is not there
+  const int* table;
+  // key tile j (from the segment's first) holds keys that are not everybody's
+  __device__ __forceinline__ bool edge(int j) const {
+    return bad || (j_lo + j + 1) * CT_BN > lim_lo || (j_lo + j + 1) * CT_BN > k_end;
+  }
+  __device__ __forceinline__ bool there(const KvPaged& c, int key) const {
+    const int blk = table[key >> 4];
+    return blk >= 0 && blk < c.n_blocks;
+  }
+};
+
+template <int DH, int KT>
+__global__ void __launch_bounds__(CtShape<DH, KT>::THREADS, 1) chunk_tc_kernel(const __grid_constant__ CtParams p) {
+  using L = CtShape<DH, KT>;
+  extern __shared__ __align__(1024) uint8_t ct_raw[];
+  __shared__ __align__(8) uint64_t k_full[2], v_full[2], k_empty[2], v_empty[2], s_full[2], p_full[2], o_full[2], v_fix[2], drain;
+  __shared__ uint32_t s_tmem;
+  __shared__ int s_abort, s_bad, s_poisoned;
+  __shared__ int s_pk[DH];   // least key with a non-finite V entry, per column (causal edge)
+  __shared__ CtTile s_tile;
+  __shared__ long long s_total;
+
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const long long wlim = wait_limit();
+  volatile int* abort_flag = &s_abort;
+  uint8_t* sm = ct_raw + ((1024 - (smem_u32(ct_raw) & 1023)) & 1023);
+  uint8_t *sQ = sm, *sK = sm + L::OFF_K, *sV = sm + L::OFF_V;
+  const ChunkCall& a = p.a;
+  unsigned* err = a.c.err ? a.c.err : p.no_err;
+
+  if (tid == 0) {
+    constexpr int arrivals = KT == KV_BF16 ? 1 : L::LOADERS;
+    for (int s = 0; s < 2; ++s) {
+      mbar_init(&k_full[s], arrivals);
+      mbar_init(&v_full[s], arrivals);
+      mbar_init(&k_empty[s], 1);
+      mbar_init(&v_empty[s], 1);
+      mbar_init(&s_full[s], 1);
+      mbar_init(&p_full[s], 4);
+      mbar_init(&o_full[s], 1);
+      mbar_init(&v_fix[s], 1);
+    }
+    mbar_init(&drain, 1);
+    s_abort = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 8) {
+    tmem_alloc(&s_tmem, 512);
+    tmem_relinquish();
+  }
+  pdl_wait();
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  pdl_launch_dependents();   // after the tensor memory is held
+  const uint32_t tmem = s_tmem;
+
+  const int group = a.n_heads / a.c.n_kv_heads, ts = p.ts, tq = 2 * ts;
+  if (warp == 0) {
+    const long long tot = ct_total(a, tq);
+    if (lane == 0) s_total = tot;
+  }
+  __syncthreads();
+  const int runs = ct_runs(s_total, p.runs), run = (int)blockIdx.x;
+  long long u = run < runs ? ct_start(s_total, runs, run) : 0;
+  const long long u_end = run < runs ? ct_start(s_total, runs, run + 1) : 0;
+
+  // Entered by every warp with the one before it behind: the segment that begins with unit u, its Q in place.
+  auto begin = [&](CtSeg& g) {
+    if (warp == 0) {
+      CtTile x{};
+      ct_find(a, tq, u, x);
+      if (lane == 0) s_tile = x;
+    }
+    if (tid == 0) {
+      s_bad = 0;
+      s_poisoned = 0;
+    }
+    if (tid < DH) s_pk[tid] = 0x7fffffff;
+    __syncthreads();
+    g.x = s_tile;
+    g.j_lo = (int)(u - g.x.u0);
+    g.j_hi = (int)min((long long)g.x.units, u_end - g.x.u0);
+    g.whole = g.j_lo == 0 && g.j_hi == g.x.units;
+    g.slot = run * 2 + (g.j_lo == 0 ? 1 : 0);
+    g.past = g.x.len - g.x.c;
+    g.t0 = g.x.tile * tq;
+    g.n_tok = min(tq, g.x.c - g.t0);
+    g.lim_lo = max(g.past + g.t0 + 1, 0);
+    g.k_end = max(g.past + g.t0 + g.n_tok, 0);
+    const int k_end0 = max(g.past + g.t0 + min(ts, g.n_tok), 0);
+    g.nt[0] = max(min(g.j_hi, (k_end0 + CT_BN - 1) / CT_BN) - g.j_lo, 0);
+    g.nt[1] = g.n_tok > ts ? max(min(g.j_hi, (g.k_end + CT_BN - 1) / CT_BN) - g.j_lo, 0) : 0;
+    g.n_it = max(g.nt[0], g.nt[1]);
+    g.table = a.c.table + (size_t)g.x.seq * a.c.max_blocks;
+    // Q: rows (token, head of the group), 16-byte pieces at their swizzled places; rows that hold nothing are zero.  And a
+    // look at the table: a block that is not there makes every key tile an edge.
+    for (int i = tid; i < CT_ROWS * (DH / 8); i += L::THREADS) {
+      const int r = i / (DH / 8), ch = i % (DH / 8), sub = r >> 7, rr = r & 127;
+      const int j = sub * ts + rr / group;
+      uint4 w = make_uint4(0, 0, 0, 0);
+      if (rr < ts * group && j < g.n_tok)
+        w = *reinterpret_cast<const uint4*>((const bf16*)a.q + (size_t)(g.x.q0 + g.t0 + j) * a.ld_q +
+                                            (size_t)(g.x.kvh * group + rr % group) * DH + ch * 8);
+      *reinterpret_cast<uint4*>(sQ + sub * L::Q_BYTES + (ch >> 3) * CT_BM * 128 + rr * 128 + (((ch & 7) ^ (rr & 7)) << 4)) = w;
+    }
+    for (int b = g.j_lo * 8 + tid; b < min((g.k_end + 15) / 16, (g.j_lo + g.n_it) * 8); b += L::THREADS)
+      if (!g.there(a.c, b * 16)) {
+        a.c.flag(ERRW_POS);
+        s_bad = 1;
+      }
+    fence_async_shared();
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    g.bad = s_bad != 0;
+  };
+  // Every warp is through with the segment; false: a role gave up, everybody leaves.
+  auto end = [&](const CtSeg& g, bool ok) {
+    u = g.x.u0 + g.j_hi;
+    tc_fence_before();
+    const bool stop = __syncthreads_or(!ok) != 0;
+    tc_fence_after();
+    return !stop;
+  };
+
+  if (warp < 8) {
+    // ---- softmax of a row per thread
+    if constexpr (KT == KV_E4M3) asm volatile("setmaxnreg.inc.sync.aligned.u32 176;");
+    const int sub = warp >> 2, r = tid & 127;
+    const uint32_t base = tmem + ((uint32_t)((warp & 3) * 32) << 16), s_col = base + (uint32_t)(sub * 128),
+                   o_col = base + 256u + (uint32_t)(sub * 128);
+    const float sc = a.scale_log2;
+    int ns = 0, no = 0;   // S tiles, outputs so far
+    CtSeg g{};
+    bool ok = true;
+    while (u < u_end) {
+      begin(g);
+      const int tok = sub * ts + r / group;
+      const bool mine = r < ts * group && tok < g.n_tok;
+      const int lim = mine ? max(g.past + g.t0 + tok + 1, 0) : 0;
+      const int sub_lo = max(g.past + g.t0 + sub * ts + 1, 0);   // keys of the sub-tile's first token
+      const int n_my = g.nt[sub];
+      float m = -INFINITY, l = 0.f;
+      for (int j = 0; j < n_my; ++j) {
+        if (!(ok = mbar_wait_warp(&s_full[sub], (uint32_t)(ns & 1), abort_flag, err, wlim))) break;
+        ++ns;
+        tc_fence_after();
+        float s0[64], s1[64];
+        tmem_ld64(s_col, s0);
+        tmem_ld64(s_col + 64, s1);
+        const int k0 = (g.j_lo + j) * CT_BN;
+        if (g.bad || k0 + CT_BN > sub_lo) {
+          const int nk_r = lim - k0;
+          unsigned gone = 0;   // blocks that are not there
+          if (g.bad)
+            for (int b = 0; b < 8; ++b)
+              if (k0 + b * 16 < g.k_end && !g.there(a.c, k0 + b * 16)) gone |= 1u << b;
+#pragma unroll
+          for (int e = 0; e < 64; ++e) {
+            if (e >= nk_r || (gone >> (e >> 4) & 1)) s0[e] = -INFINITY;
+            if (64 + e >= nk_r || (gone >> (4 + (e >> 4)) & 1)) s1[e] = -INFINITY;
+          }
+        }
+        float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+        for (int e = 0; e < 64; ++e) {
+          mx[e & 3] = fmaxf(mx[e & 3], s0[e]);
+          mx[e & 3] = fmaxf(mx[e & 3], s1[e]);
+        }
+        const float tmax = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * sc;
+        float m_new = m;
+        if (tmax > m && (m == -INFINITY || tmax - m > CT_RAISE)) m_new = tmax;
+        const float f = (m == -INFINITY || m_new == m) ? 1.f : ex2_approx(m - m_new);
+        if (__any_sync(0xffffffffu, f != 1.f)) {   // (S of this tile is complete, so O of the one before it is)
+#pragma unroll 1
+          for (int c = 0; c < DH / 32; ++c) {
+            float v[32];
+            tmem_ld32(o_col + (uint32_t)(c * 32), v);
+#pragma unroll
+            for (int e = 0; e < 32; ++e) v[e] *= f;
+            tmem_st32(o_col + (uint32_t)(c * 32), v);
+          }
+          l *= f;
+        }
+        m = m_new;
+        const float ref = m == -INFINITY ? 0.f : m;
+        float sum[4] = {0.f, 0.f, 0.f, 0.f};
+        uint32_t pk[32];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          float(&s)[64] = h ? s1 : s0;
+#pragma unroll
+          for (int e = 0; e < 64; e += 2) {
+            const float p0 = ex2_approx(fmaf(s[e], sc, -ref)), p1 = ex2_approx(fmaf(s[e + 1], sc, -ref));
+            sum[(e >> 1) & 3] += p0 + p1;
+            const __nv_bfloat162 pr = __floats2bfloat162_rn(p0, p1);
+            pk[e >> 1] = *reinterpret_cast<const uint32_t*>(&pr);
+          }
+          tmem_st32u(s_col + (uint32_t)(h * 32), pk);
+        }
+        tmem_st_wait();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&p_full[sub]);
+        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+      }
+      // O / l, or the part
+      if (ok && n_my > 0) {
+        ok = mbar_wait_warp(&o_full[sub], (uint32_t)(no & 1), abort_flag, err, wlim);
+        ++no;
+      }
+      tc_fence_after();
+      const bool poisoned = s_poisoned != 0;
+      const float inv = lim == 0 ? 0.f : 1.f / l;
+      if (!g.whole && mine && ok) {
+        float* ml = ct_ml(p, g.slot) + (sub * 128 + r) * 2;
+        ml[0] = m;
+        ml[1] = l;
+      }
+#pragma unroll 1
+      for (int c = 0; c < DH / 32; ++c) {
+        float v[32];
+        if (n_my > 0) {   // (the same for the whole warp)
+          tmem_ld32(o_col + (uint32_t)(c * 32), v);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 32; ++e) v[e] = 0.f;
+        }
+        if (poisoned) {
+#pragma unroll
+          for (int e = 0; e < 32; ++e)
+            if (s_pk[c * 32 + e] < lim) v[e] = NAN;
+        }
+        if (mine && ok) {
+          if (g.whole) {
+            uint32_t w[16];
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+              const __nv_bfloat162 pr = __floats2bfloat162_rn(v[2 * e] * inv, v[2 * e + 1] * inv);
+              w[e] = *reinterpret_cast<const uint32_t*>(&pr);
+            }
+            uint4* o = reinterpret_cast<uint4*>((bf16*)a.out + (size_t)(g.x.q0 + g.t0 + tok) * a.ld_out +
+                                                (size_t)(g.x.kvh * group + r % group) * DH + c * 32);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] = make_uint4(w[4 * e], w[4 * e + 1], w[4 * e + 2], w[4 * e + 3]);
+          } else {
+            float4* o = reinterpret_cast<float4*>(ct_o(p, g.slot, DH) + (size_t)(sub * 128 + r) * DH + c * 32);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) o[e] = make_float4(v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]);
+          }
+        }
+        __syncwarp();
+      }
+      if (!end(g, ok)) break;
+    }
+  } else if (warp == 8) {
+    // ---- matrix instructions
+    if constexpr (KT == KV_E4M3) asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
+    constexpr uint32_t IDESC_S = umma_idesc(CT_BN, false), IDESC_O = umma_idesc(DH, true);
+    int nk = 0, nv = 0, np[2] = {0, 0}, nf[2] = {0, 0};   // K, V, P tiles and mended V tiles (per stage) so far
+    auto commit = [&](uint64_t* bar) {
+      if (elect_one()) umma_commit(bar);
+      __syncwarp();
+    };
+    CtSeg g{};
+    bool ok = true;
+    while (u < u_end) {
+      begin(g);
+      for (int j = -1; j < g.n_it && ok; ++j) {
+        const int kn = nk, vn = nv;
+        if (j + 1 < g.n_it) {
+          if (!(ok = mbar_wait_warp(&k_full[kn & 1], (uint32_t)((kn >> 1) & 1), abort_flag, err, wlim))) break;
+          ++nk;
+        }
+        if (j >= 0) {
+          if (!(ok = mbar_wait_warp(&v_full[vn & 1], (uint32_t)((vn >> 1) & 1), abort_flag, err, wlim))) break;
+          if (KT == KV_BF16 && g.edge(j)) {
+            if (!(ok = mbar_wait_warp(&v_fix[vn & 1], (uint32_t)(nf[vn & 1] & 1), abort_flag, err, wlim))) break;
+            ++nf[vn & 1];
+          }
+          ++nv;
+        }
+#pragma unroll
+        for (int sub = 0; sub < 2; ++sub) {
+          if (!ok) break;
+          if (j >= 0 && j < g.nt[sub]) {
+            if (!(ok = mbar_wait_warp(&p_full[sub], (uint32_t)(np[sub] & 1), abort_flag, err, wlim))) break;
+            ++np[sub];
+            tc_fence_after();
+            if (elect_one()) {
+              const uint32_t pa = tmem + (uint32_t)(sub * 128);
+#pragma unroll
+              for (int kk = 0; kk < CT_BN / 16; ++kk) {
+                const uint64_t vb = sdesc_mn_sw128(smem_u32(sV + (vn & 1) * L::KV_BYTES + kk * 16 * 128), (uint32_t)(CT_BN * 128));
+                umma_bf16_ts(tmem + 256u + (uint32_t)(sub * 128), pa + (uint32_t)(kk * 8), vb, IDESC_O, (j > 0 || kk > 0) ? 1u : 0u);
+              }
+              if (j == g.nt[sub] - 1) umma_commit(&o_full[sub]);
+            }
+            __syncwarp();
+          }
+          if (j + 1 < g.nt[sub]) {
+            tc_fence_after();
+            if (elect_one()) {
+#pragma unroll
+              for (int kk = 0; kk < DH / 16; ++kk) {
+                const uint64_t qa = sdesc_sw128(smem_u32(sQ + sub * L::Q_BYTES + (kk >> 2) * CT_BM * 128) + (kk & 3) * 32);
+                const uint64_t kb = sdesc_sw128(smem_u32(sK + (kn & 1) * L::KV_BYTES + (kk >> 2) * CT_BN * 128) + (kk & 3) * 32);
+                umma_bf16(tmem + (uint32_t)(sub * 128), qa, kb, IDESC_S, kk > 0 ? 1u : 0u);
+              }
+              umma_commit(&s_full[sub]);
+            }
+            __syncwarp();
+          }
+        }
+        if (!ok) break;
+        if (j + 1 < g.n_it) commit(&k_empty[kn & 1]);
+        if (j >= 0) commit(&v_empty[vn & 1]);
+      }
+      if (!end(g, ok)) break;
+    }
+    // every matrix instruction has completed before tensor memory is given back
+    if (elect_one()) {
+      umma_commit(&drain);
+      const long long c0 = clock64();
+      while (!mbar_try_wait(&drain, 0) && clock64() - c0 < CT_DRAIN_CYCLES) {
+      }
+    }
+    __syncwarp();
+  } else if constexpr (KT == KV_BF16) {
+    // ---- TMA producers: K (warp 9), V (warp 10, which also mends the V tiles at the edge)
+    const bool kw = warp == 9;
+    uint64_t *full = kw ? k_full : v_full, *empty = kw ? k_empty : v_empty;
+    const CUtensorMap* map = kw ? &p.kmap : &p.vmap;
+    uint8_t* dst0 = kw ? sK : sV;
+    int cnt = 0;   // tiles sent so far
+    CtSeg g{};
+    bool ok = true;
+    // V tile j, in stage s (its phase of v_full): entries nobody attends to zero, non-finite ones noted
+    auto mend = [&](int j, int vi) {
+      const int s = vi & 1;
+      if (!mbar_wait_warp(&v_full[s], (uint32_t)((vi >> 1) & 1), abort_flag, err, wlim)) return false;
+      uint8_t* v = sV + s * L::KV_BYTES;
+      const int k0 = (g.j_lo + j) * CT_BN;
+      for (int i = lane; i < L::HALVES * CT_BN * 8; i += 32) {   // 16-byte pieces
+        const int hf = i / (CT_BN * 8), key = i / 8 % CT_BN, pc = (i & 7) ^ (key & 7);
+        uint4* w = reinterpret_cast<uint4*>(v + hf * CT_BN * 128 + key * 128 + ((i & 7) << 4));
+        if (k0 + key >= g.k_end || (g.bad && !g.there(a.c, k0 + key))) {
+          *w = make_uint4(0, 0, 0, 0);
+          continue;
+        }
+        uint4 y = *w;
+        const uint32_t b[4] = {ct_bad2(y.x), ct_bad2(y.y), ct_bad2(y.z), ct_bad2(y.w)};
+        if (b[0] | b[1] | b[2] | b[3]) {
+          *w = make_uint4(y.x & ~b[0], y.y & ~b[1], y.z & ~b[2], y.w & ~b[3]);
+          for (int e = 0; e < 8; ++e)
+            if (b[e >> 1] >> ((e & 1) * 16) & 1) atomicMin(&s_pk[hf * 64 + pc * 8 + e], k0 + key);
+          s_poisoned = 1;
+        }
+      }
+      fence_async_shared();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&v_fix[s]);
+      return true;
+    };
+    while (u < u_end) {
+      begin(g);
+      for (int j = 0; j <= g.n_it && ok; ++j) {
+        if (!kw && j > 0 && g.edge(j - 1) && !(ok = mend(j - 1, cnt - 1))) break;
+        if (j == g.n_it) break;
+        const int s = cnt & 1;
+        int row = -1;
+        if (lane < 8) {
+          const int b = (g.j_lo + j) * 8 + lane;
+          if (b * 16 < g.k_end && g.there(a.c, b * 16)) row = (g.table[b] * a.c.n_kv_heads + g.x.kvh) * 16;
+        }
+        const unsigned on = __ballot_sync(0xffffffffu, row >= 0);
+        int rows8[8];
+#pragma unroll
+        for (int b = 0; b < 8; ++b) rows8[b] = __shfl_sync(0xffffffffu, row, b);
+        if (cnt >= 2 && !(ok = mbar_wait_warp(&empty[s], (uint32_t)(((cnt >> 1) - 1) & 1), abort_flag, err, wlim))) break;
+        if (elect_one()) {
+          // (blocks that are not fetched leave the stage's old contents: masked in S, mended in V)
+          mbar_expect_tx(&full[s], (uint32_t)(__popc(on) * 16 * 128 * L::HALVES));
+          for (int b = 0; b < 8; ++b)
+            if (on >> b & 1)
+              for (int hf = 0; hf < L::HALVES; ++hf)
+                tma_load_2d(map, &full[s], dst0 + s * L::KV_BYTES + hf * CT_BN * 128 + b * 16 * 128, hf * 64, rows8[b]);
+        }
+        __syncwarp();
+        ++cnt;
+      }
+      if (!end(g, ok)) break;
+    }
+    // every copy sent has landed before the CTA ends
+    if (lane == 0) {
+      for (int t = max(0, cnt - 2); t < cnt; ++t) {
+        const long long c0 = clock64();
+        while (!mbar_try_wait(&full[t & 1], (uint32_t)((t >> 1) & 1)) && clock64() - c0 < CT_DRAIN_CYCLES) {
+        }
+      }
+    }
+    __syncwarp();
+  } else {
+    // ---- e4m3: codes to registers a tile ahead, then bf16 into the swizzled stage; K and V in turn
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
+    constexpr int PIECES = CT_BN * (DH / 16), LT = L::LOADERS * 32, PER = (PIECES + LT - 1) / LT;
+    const int lt = tid - 9 * 32;
+    int cnt[2] = {0, 0};   // K, V tiles so far
+    uint4 w[PER];
+    int ex[PER];
+    CtSeg g{};
+    bool ok = true;
+    auto fetch = [&](int t) {   // t: 2 j (K) or 2 j + 1 (V)
+      const uint8_t* from = (const uint8_t*)(t & 1 ? a.c.v : a.c.k);
+      const uint8_t* eb = t & 1 ? a.c.v_exp : a.c.k_exp;
+#pragma unroll
+      for (int i = 0; i < PER; ++i) {
+        const int pc = lt + i * LT, k = (g.j_lo + (t >> 1)) * CT_BN + pc / (DH / 16);
+        w[i] = make_uint4(0, 0, 0, 0);
+        ex[i] = 127;
+        if (pc < PIECES && k < g.k_end) {
+          const int blk = g.table[k >> 4];
+          if (blk >= 0 && blk < a.c.n_blocks) {
+            const size_t e = ((size_t)blk * a.c.n_kv_heads + g.x.kvh) * 16 + (k & 15);
+            w[i] = *reinterpret_cast<const uint4*>(from + e * DH + pc % (DH / 16) * 16);
+            ex[i] = eb[e];
+          }
+        }
+      }
+    };
+    while (u < u_end) {
+      begin(g);
+      if (g.n_it > 0) fetch(0);
+      for (int t = 0; t < 2 * g.n_it && ok; ++t) {
+        const int is_v = t & 1, n = cnt[is_v], s = n & 1;
+        if (n >= 2 && !(ok = mbar_wait_warp(is_v ? &v_empty[s] : &k_empty[s], (uint32_t)(((n >> 1) - 1) & 1), abort_flag, err, wlim)))
+          break;
+        uint8_t* dst = (is_v ? sV : sK) + s * L::KV_BYTES;
+        const bool look = is_v && g.edge(t >> 1);
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+          const int pc = lt + i * LT;
+          if (pc < PIECES) {
+            const int key = pc / (DH / 16), c0 = pc % (DH / 16) * 2;   // two 8-element pieces
+            const __nv_bfloat162 sc = __float2bfloat162_rn(ct_exp2i(ex[i]));
+            const uint32_t cw[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
+            uint32_t y[8];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+              y[2 * q] = ct_bf16x2(cw[q] & 0xffffu, sc);
+              y[2 * q + 1] = ct_bf16x2(cw[q] >> 16, sc);
+            }
+            if (look) {
+#pragma unroll
+              for (int q = 0; q < 8; ++q) {
+                const uint32_t b = ct_bad2(y[q]);
+                if (b) {
+                  y[q] &= ~b;
+                  const int k = (g.j_lo + (t >> 1)) * CT_BN + key;
+                  if (b & 1) atomicMin(&s_pk[c0 * 8 + 2 * q], k);
+                  if (b >> 16) atomicMin(&s_pk[c0 * 8 + 2 * q + 1], k);
+                  s_poisoned = 1;
+                }
+              }
+            }
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              const int ch = c0 + h;
+              *reinterpret_cast<uint4*>(dst + (ch >> 3) * CT_BN * 128 + key * 128 + (((ch & 7) ^ (key & 7)) << 4)) =
+                  make_uint4(y[4 * h], y[4 * h + 1], y[4 * h + 2], y[4 * h + 3]);
+            }
+          }
+        }
+        if (t + 1 < 2 * g.n_it) fetch(t + 1);
+        fence_async_shared();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(is_v ? &v_full[s] : &k_full[s]);
+        cnt[is_v] = n + 1;
+      }
+      if (!end(g, ok)) break;
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (warp == 8) tmem_dealloc(tmem, 512);
+}
+
+// Join of the tiles that runs share: CTA (i, y) takes the tile that run i begins inside of, where i is the first such run, and
+// a quarter of its rows.
+template <int DH>
+__global__ void __launch_bounds__(256) chunk_tc_join_kernel(const __grid_constant__ CtParams p) {
+  __shared__ CtTile s_tile;
+  __shared__ long long s_total;
+  PDL_ENTRY();
+  const ChunkCall& a = p.a;
+  const int tid = threadIdx.x, tq = 2 * p.ts, run = (int)blockIdx.x + 1;
+  if (tid < 32) {
+    const long long tot = ct_total(a, tq);
+    CtTile x{};
+    x.units = 0;
+    const int runs = ct_runs(tot, p.runs);
+    if (run < runs) ct_find(a, tq, ct_start(tot, runs, run), x);
+    if (tid == 0) {
+      s_total = tot;
+      s_tile = x;
+    }
+  }
+  __syncthreads();
+  const CtTile x = s_tile;
+  const long long total = s_total;
+  const int runs = ct_runs(total, p.runs);
+  if (run >= runs) return;
+  const long long b0 = ct_start(total, runs, run);
+  if (b0 == x.u0 || ct_start(total, runs, run - 1) > x.u0) return;   // begins with the tile; not the first run inside
+  // parts: run - 1 (the tile's beginning), run, ... while they begin before the tile's end
+  int n_part = 2;
+  while (run + n_part - 1 < runs && ct_start(total, runs, run + n_part - 1) < x.u0 + x.units) ++n_part;
+  const int group = a.n_heads / a.c.n_kv_heads, past = x.len - x.c, t0 = x.tile * tq, n_tok = min(tq, x.c - t0);
+  for (int i = tid + blockIdx.y * 256; i < CT_ROWS * (DH / 4); i += 256 * gridDim.y) {
+    const int r = i / (DH / 4), d = i % (DH / 4) * 4, sub = r >> 7, rr = r & 127, tok = sub * p.ts + rr / group;
+    if (rr >= p.ts * group || tok >= n_tok) continue;
+    float M = -INFINITY;
+    for (int k = 0; k < n_part; ++k) M = fmaxf(M, __ldcg(ct_ml(p, (run - 1 + k) * 2 + (k == 0)) + r * 2));
+    const float ref = M == -INFINITY ? 0.f : M;
+    float l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int k = 0; k < n_part; ++k) {
+      const int slot = (run - 1 + k) * 2 + (k == 0);
+      const float2 ml = __ldcg(reinterpret_cast<const float2*>(ct_ml(p, slot) + r * 2));
+      const float4 v = __ldcg(reinterpret_cast<const float4*>(ct_o(p, slot, DH) + (size_t)r * DH + d));
+      const float w = ex2_approx(ml.x - ref);
+      l += w * ml.y;
+      o[0] += w * v.x;
+      o[1] += w * v.y;
+      o[2] += w * v.z;
+      o[3] += w * v.w;
+    }
+    const float inv = past + t0 + tok < 0 ? 0.f : 1.f / l;
+    const __nv_bfloat162 y0 = __floats2bfloat162_rn(o[0] * inv, o[1] * inv), y1 = __floats2bfloat162_rn(o[2] * inv, o[3] * inv);
+    *reinterpret_cast<uint2*>((bf16*)a.out + (size_t)(x.q0 + t0 + tok) * a.ld_out + (size_t)(x.kvh * group + rr % group) * DH + d) =
+        make_uint2(*reinterpret_cast<const uint32_t*>(&y0), *reinterpret_cast<const uint32_t*>(&y1));
+  }
+}
+
+template <int DH, int KT>
+cudaError_t launch_t(cudaStream_t st, const CtParams& p) {
+  using L = CtShape<DH, KT>;
+  constexpr int smem = L::TOTAL + 1024;
+  cudaError_t e = cudaFuncSetAttribute(chunk_tc_kernel<DH, KT>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  if (e != cudaSuccess) return e;
+  e = launch_k(chunk_tc_kernel<DH, KT>, dim3(p.runs), dim3(L::THREADS), smem, st, p);
+  if (e != cudaSuccess) return e;
+  return launch_k(chunk_tc_join_kernel<DH>, dim3(std::max(1, p.runs - 1), 4), dim3(256), 0, st, p);
+}
+
+int ct_sms() {
+  static const int sms = [] {
+    int dev = 0, n = 0;
+    cudaGetDevice(&dev);
+    cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev);
+    return std::max(1, n);
+  }();
+  return sms;
+}
+
+}  // namespace
+
+bool chunk_tc_takes(const KvPaged& c, int n_heads) {
+  return c.type != KV_F32 && c.block_tokens == 16 && (c.head_dim == 64 || c.head_dim == 128) &&
+         n_heads / c.n_kv_heads <= CT_BM && (long long)c.n_blocks * c.n_kv_heads * 16 < (1ll << 31) && tc_gemm_supported();
+}
+
+static size_t ct_part_floats(int dh) { return (size_t)ct_sms() * 2 * CT_ROWS * (dh + 2); }
+size_t chunk_tc_workspace(const KvPaged& c) { return (ct_part_floats(c.head_dim) + 4) * sizeof(float); }
+
+cudaError_t launch_chunk_tc(cudaStream_t st, const ChunkCall& a, int* launches) {
+  CtParams p;
+  memset(&p, 0, sizeof p);
+  p.a = a;
+  p.ts = CT_BM / (a.n_heads / a.c.n_kv_heads);
+  p.runs = ct_sms();
+  const int dh = a.c.head_dim;
+  p.no_err = (unsigned*)(a.part + ct_part_floats(dh));
+  if (a.c.type == KV_BF16) {
+    const uint64_t rows = (uint64_t)a.c.n_blocks * a.c.n_kv_heads * 16;
+    if (!tc_encode_2d(&p.kmap, a.c.k, (uint64_t)dh, rows, (uint64_t)dh * 2, 16) ||
+        !tc_encode_2d(&p.vmap, a.c.v, (uint64_t)dh, rows, (uint64_t)dh * 2, 16))
+      return cudaErrorInvalidValue;
+  }
+  *launches = 2;
+  if (a.c.type == KV_BF16) return dh == 128 ? launch_t<128, KV_BF16>(st, p) : launch_t<64, KV_BF16>(st, p);
+  return dh == 128 ? launch_t<128, KV_E4M3>(st, p) : launch_t<64, KV_E4M3>(st, p);
+}
+
+ADEPT_WAIT_LIMIT_SETTER(ct)
+
+}  // namespace adept

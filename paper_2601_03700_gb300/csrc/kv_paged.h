@@ -45,6 +45,11 @@ struct ChunkCall {
 };
 size_t chunk_workspace(const KvPaged& c, int n_heads, int n_rows, int max_q, int max_kv);
 cudaError_t launch_chunk_attention(cudaStream_t st, const ChunkCall& a, int* launches);
+// The tcgen05 kernel (attention_chunk_tc.cu): what it takes (rows on 16 bytes besides), its workspace, its launches.
+bool chunk_tc_takes(const KvPaged& c, int n_heads);
+size_t chunk_tc_workspace(const KvPaged& c);
+cudaError_t launch_chunk_tc(cudaStream_t st, const ChunkCall& a, int* launches);
+cudaError_t set_wait_limit_ct(long long cycles);
 
 // ---------------------------------------------------------------------------------------------
 // Work split.  A tile is up to tq new tokens of one sequence (all query heads of a group of one KV head); its keys are

@@ -227,8 +227,9 @@ def test_inputs_out_of_range_are_flagged_and_left_out():
         assert torch.equal(out[:5], good[:5]) and (out[5:] == -7).all()
         out = call(lens=[40, -1, 50])
         assert torch.equal(out[:3], good[:3]) and (out[3:5] == -7).all() and torch.equal(out[5:], good[5:])
-        out = call(starts=[0, 3, 2, 9], max_q=9)  # sequence 1 would have -1 rows
-        assert torch.equal(out[:2], good[:2])
+        # sequence 1 would have -1 rows (the bound of 9 rows may pick another kernel: held against the reference)
+        out = call(starts=[0, 3, 2, 9], max_q=9)
+        assert_attention(c, q[:2], [0, 2, 2, 2], [39, 0, 0], out[:2])
         call(starts=[0, 3, 5, 10], max_q=9)      # a row behind the last
         call(starts=[-1, 3, 5, 9], max_q=9)
         for blk in (-1, 10 ** 6):
