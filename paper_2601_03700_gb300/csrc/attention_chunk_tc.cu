@@ -58,17 +58,16 @@ struct CtParams {
 
 // ---- the key tiles of all tiles in a row ----
 
-// sum over i in [0, n) of floor((a i + b) / m), a, b >= 0
-__device__ long long floor_sum(long long n, long long m, long long a, long long b) {
+// sum over i in [0, n) of floor((a i + b) / m); a n + b below 2^32
+__device__ long long floor_sum(unsigned n, unsigned m, unsigned a, unsigned b) {
   long long r = 0;
   while (n > 0) {
-    r += (n - 1) * n / 2 * (a / m) + n * (b / m);
+    r += (long long)(n - 1) * n / 2 * (a / m) + (long long)n * (b / m);
     a %= m;
     b %= m;
-    const long long y = a * n + b;
+    const unsigned y = a * n + b, x = m;
     n = y / m;
     b = y % m;
-    const long long x = m;
     m = a;
     a = x;
     if (m == 0) break;
@@ -89,7 +88,7 @@ __device__ long long ct_seq_units(int c, int len, int tq) {
     for (int t = 0; t < tiles; ++t) r += ct_units(c, len, tq, t);
     return r;
   }
-  return last + floor_sum(tiles - 1, CT_BN, tq, (long long)(len - c) + tq + CT_BN - 1);
+  return last + floor_sum((unsigned)tiles - 1, CT_BN, (unsigned)tq, (unsigned)(len - c + tq + CT_BN - 1));
 }
 
 struct CtTile {
@@ -167,10 +166,28 @@ __device__ __forceinline__ int ct_runs(long long total, int runs) {
 }
 __device__ __forceinline__ long long ct_start(long long total, int runs, int i) { return total * i / runs; }
 
-// Slot s of the workspace: 256 (m, l) pairs, and behind all of those 256 rows of weighted V.
-__device__ __forceinline__ float* ct_ml(const CtParams& p, int slot) { return p.a.part + (size_t)slot * CT_ROWS * 2; }
-__device__ __forceinline__ float* ct_o(const CtParams& p, int slot, int dh) {
-  return p.a.part + (size_t)p.runs * 2 * CT_ROWS * 2 + (size_t)slot * CT_ROWS * dh;
+// Workspace: a note per run on the tile it begins inside of; per slot (two a run) 256 (m, l) pairs; and per slot 256 rows of
+// weighted V, four columns of all rows after the other (a warp of rows writes whole lines).
+struct CtNote {
+  long long u0;       // first unit of the tile, -1: the run begins with a tile, or is empty
+  int row0, kvh, pos0, n_tok;   // the tile's first row of Q, KV head, first position, tokens
+  int pad[2];         // (32 bytes: what follows is read 16 at a time)
+};
+struct CtWs {
+  CtNote* note;
+  float* ml;
+  float* o;
+  __device__ CtWs(const CtParams& p)
+      : note((CtNote*)p.a.part), ml(p.a.part + (size_t)p.runs * (sizeof(CtNote) / 4)), o(ml + (size_t)p.runs * 2 * CT_ROWS * 2) {}
+  __device__ __forceinline__ float2* ml_at(int slot, int r) const {
+    return reinterpret_cast<float2*>(ml) + (size_t)slot * CT_ROWS + r;
+  }
+  __device__ __forceinline__ float4* o_at(int slot, int dh, int d4, int r) const {
+    return reinterpret_cast<float4*>(o) + ((size_t)slot * (dh / 4) + d4) * CT_ROWS + r;
+  }
+};
+constexpr size_t ct_ws_floats(int runs, int dh) {
+  return (size_t)runs * (sizeof(CtNote) / 4) + (size_t)runs * 2 * CT_ROWS * (dh + 2);
 }
 
 __device__ __forceinline__ float ct_exp2i(int b) {   // 2^(b - 127)
@@ -182,25 +199,56 @@ __device__ __forceinline__ uint32_t ct_bf16x2(uint32_t codes, __nv_bfloat162 sca
   const __nv_bfloat162 r = __hmul2(__floats2bfloat162_rn(f.x, f.y), scale);
   return *reinterpret_cast<const uint32_t*>(&r);
 }
-// Non-finite bf16 of a pair: 0xffff in its half.
+// Non-finite bf16 of a pair: 0xffff in its half; and whether there is one (a carry out of an exponent of all ones).
 __device__ __forceinline__ uint32_t ct_bad2(uint32_t x) { return __vcmpeq2(x & 0x7f807f80u, 0x7f807f80u); }
+__device__ __forceinline__ uint32_t ct_any_bad2(uint32_t x) { return ((x & 0x7f807f80u) + 0x00800080u) & 0x80008000u; }
+
+// Two fp32 at once.
+__device__ __forceinline__ uint64_t f2_pack(float a, float b) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ void f2_unpack(uint64_t x, float& a, float& b) {
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(x));
+}
+__device__ __forceinline__ uint64_t f2_fma(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ uint64_t f2_add(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+// 16 bytes of global memory to shared memory, zeros where `on` is false.
+__device__ __forceinline__ void cp_async16(void* dst, const void* src, bool on) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(dst)), "l"(src), "r"(on ? 16 : 0) : "memory");
+}
 
 // A CTA's part of one tile: key tiles j_lo .. j_hi.
 struct CtSeg {
   CtTile x;
   int j_lo, j_hi, past, t0, n_tok;
   int lim_lo, k_end;   // keys of the tile's first and of its last token (nobody attends beyond)
-  int nt[2], n_it;     // key tiles with keys: per sub-tile, of the segment
+  int nt0, nt1, n_it;  // key tiles with keys: per sub-tile, of the segment
   int slot;
-  bool whole, bad;     // the whole tile; some block is not there
+  bool whole;          // the whole tile
   const int* table;
+  __device__ __forceinline__ int nt(int sub) const { return sub ? nt1 : nt0; }
   // key tile j (from the segment's first) holds keys that are not everybody's
-  __device__ __forceinline__ bool edge(int j) const {
-    return bad || (j_lo + j + 1) * CT_BN > lim_lo || (j_lo + j + 1) * CT_BN > k_end;
-  }
-  __device__ __forceinline__ bool there(const KvPaged& c, int key) const {
-    const int blk = table[key >> 4];
-    return blk >= 0 && blk < c.n_blocks;
+  __device__ __forceinline__ bool edge(int j) const { return (j_lo + j + 1) * CT_BN > lim_lo || (j_lo + j + 1) * CT_BN > k_end; }
+  // the row of key block b (from the sequence's first) in the pools seen as rows of d_h, -1: nobody's, -2: not there
+  __device__ __forceinline__ int row_of(const KvPaged& c, int b) const {
+    if (b * 16 >= k_end) return -1;
+    const int blk = table[b];
+    return blk >= 0 && blk < c.n_blocks ? (blk * c.n_kv_heads + x.kvh) * 16 : -2;
   }
 };
 
@@ -208,12 +256,14 @@ template <int DH, int KT>
 __global__ void __launch_bounds__(CtShape<DH, KT>::THREADS, 1) chunk_tc_kernel(const __grid_constant__ CtParams p) {
   using L = CtShape<DH, KT>;
   extern __shared__ __align__(1024) uint8_t ct_raw[];
-  __shared__ __align__(8) uint64_t k_full[2], v_full[2], k_empty[2], v_empty[2], s_full[2], p_full[2], o_full[2], v_fix[2], drain;
+  __shared__ __align__(8) uint64_t k_full[2], v_full[2], k_empty[2], v_empty[2], s_full[2], p_half[2], p_full[2], o_full[2], v_fix[2], drain;
   __shared__ uint32_t s_tmem;
-  __shared__ int s_abort, s_bad, s_poisoned;
+  __shared__ int s_abort, s_poisoned;
+  __shared__ int s_gone[4];      // blocks of a key tile that are not there, by tile % 4
+  __shared__ int s_tok[CT_ROWS], s_off[CT_ROWS];   // token of a row in the tile (-1: none), its head's first column in the group
   __shared__ int s_pk[DH];   // least key with a non-finite V entry, per column (causal edge)
   __shared__ CtTile s_tile;
-  __shared__ long long s_total;
+  __shared__ long long s_u0, s_u1;
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const long long wlim = wait_limit();
@@ -231,6 +281,7 @@ __global__ void __launch_bounds__(CtShape<DH, KT>::THREADS, 1) chunk_tc_kernel(c
       mbar_init(&k_empty[s], 1);
       mbar_init(&v_empty[s], 1);
       mbar_init(&s_full[s], 1);
+      mbar_init(&p_half[s], 4);
       mbar_init(&p_full[s], 4);
       mbar_init(&o_full[s], 1);
       mbar_init(&v_fix[s], 1);
@@ -253,24 +304,32 @@ __global__ void __launch_bounds__(CtShape<DH, KT>::THREADS, 1) chunk_tc_kernel(c
   const int group = a.n_heads / a.c.n_kv_heads, ts = p.ts, tq = 2 * ts;
   if (warp == 0) {
     const long long tot = ct_total(a, tq);
-    if (lane == 0) s_total = tot;
+    if (lane == 0) {
+      const int runs = ct_runs(tot, p.runs), run = (int)blockIdx.x;
+      s_u0 = run < runs ? ct_start(tot, runs, run) : 0;
+      s_u1 = run < runs ? ct_start(tot, runs, run + 1) : 0;
+      if (run >= runs) CtWs(p).note[run].u0 = -1;
+    }
+  } else if (warp < 9) {
+    const int r = tid - 32, rr = r & 127, tk = rr / group;   // (a row per thread of warps 1..8)
+    s_tok[r] = tk < ts ? (r >> 7) * ts + tk : -1;
+    s_off[r] = rr % group * DH;
   }
   __syncthreads();
-  const int runs = ct_runs(s_total, p.runs), run = (int)blockIdx.x;
-  long long u = run < runs ? ct_start(s_total, runs, run) : 0;
-  const long long u_end = run < runs ? ct_start(s_total, runs, run + 1) : 0;
+  const int run = (int)blockIdx.x;
+  const long long u_end = s_u1;
+  long long u = s_u0;
+  bool first_seg = true;
 
-  // Entered by every warp with the one before it behind: the segment that begins with unit u, its Q in place.
+  // Entered by every warp with the segment before it behind: the one that begins with unit u.  Warps 0..8 leave with its Q in
+  // place (rows (token, head of the group), 16-byte pieces at their swizzled places, rows that hold nothing zero).
   auto begin = [&](CtSeg& g) {
     if (warp == 0) {
       CtTile x{};
       ct_find(a, tq, u, x);
       if (lane == 0) s_tile = x;
     }
-    if (tid == 0) {
-      s_bad = 0;
-      s_poisoned = 0;
-    }
+    if (tid == 0) s_poisoned = 0;
     if (tid < DH) s_pk[tid] = 0x7fffffff;
     __syncthreads();
     g.x = s_tile;
@@ -284,31 +343,29 @@ __global__ void __launch_bounds__(CtShape<DH, KT>::THREADS, 1) chunk_tc_kernel(c
     g.lim_lo = max(g.past + g.t0 + 1, 0);
     g.k_end = max(g.past + g.t0 + g.n_tok, 0);
     const int k_end0 = max(g.past + g.t0 + min(ts, g.n_tok), 0);
-    g.nt[0] = max(min(g.j_hi, (k_end0 + CT_BN - 1) / CT_BN) - g.j_lo, 0);
-    g.nt[1] = g.n_tok > ts ? max(min(g.j_hi, (g.k_end + CT_BN - 1) / CT_BN) - g.j_lo, 0) : 0;
-    g.n_it = max(g.nt[0], g.nt[1]);
+    g.nt0 = max(min(g.j_hi, (k_end0 + CT_BN - 1) / CT_BN) - g.j_lo, 0);
+    g.nt1 = g.n_tok > ts ? max(min(g.j_hi, (g.k_end + CT_BN - 1) / CT_BN) - g.j_lo, 0) : 0;
+    g.n_it = max(g.nt0, g.nt1);
     g.table = a.c.table + (size_t)g.x.seq * a.c.max_blocks;
-    // Q: rows (token, head of the group), 16-byte pieces at their swizzled places; rows that hold nothing are zero.  And a
-    // look at the table: a block that is not there makes every key tile an edge.
-    for (int i = tid; i < CT_ROWS * (DH / 8); i += L::THREADS) {
-      const int r = i / (DH / 8), ch = i % (DH / 8), sub = r >> 7, rr = r & 127;
-      const int j = sub * ts + rr / group;
-      uint4 w = make_uint4(0, 0, 0, 0);
-      if (rr < ts * group && j < g.n_tok)
-        w = *reinterpret_cast<const uint4*>((const bf16*)a.q + (size_t)(g.x.q0 + g.t0 + j) * a.ld_q +
-                                            (size_t)(g.x.kvh * group + rr % group) * DH + ch * 8);
-      *reinterpret_cast<uint4*>(sQ + sub * L::Q_BYTES + (ch >> 3) * CT_BM * 128 + rr * 128 + (((ch & 7) ^ (rr & 7)) << 4)) = w;
-    }
-    for (int b = g.j_lo * 8 + tid; b < min((g.k_end + 15) / 16, (g.j_lo + g.n_it) * 8); b += L::THREADS)
-      if (!g.there(a.c, b * 16)) {
-        a.c.flag(ERRW_POS);
-        s_bad = 1;
+    if (first_seg && tid == 0)
+      CtWs(p).note[run] = CtNote{g.j_lo > 0 ? g.x.u0 : -1, g.x.q0 + g.t0, g.x.kvh, g.past + g.t0, g.n_tok, {0, 0}};
+    first_seg = false;
+    if (warp < 9) {
+      const bf16* q = (const bf16*)a.q + (size_t)(g.x.q0 + g.t0) * a.ld_q + (size_t)g.x.kvh * group * DH;
+      const int live = g.n_tok > ts ? CT_ROWS : CT_BM;
+#pragma unroll 4
+      for (int i = tid; i < live * (DH / 8); i += 9 * 32) {
+        const int r = i / (DH / 8), ch = i % (DH / 8), rr = r & 127, tk = s_tok[r];
+        const bool on = tk >= 0 && tk < g.n_tok;
+        cp_async16(sQ + (r >> 7) * L::Q_BYTES + (ch >> 3) * CT_BM * 128 + rr * 128 + (((ch & 7) ^ (rr & 7)) << 4),
+                   q + (on ? tk * a.ld_q + s_off[r] + ch * 8 : 0), on);
       }
-    fence_async_shared();
-    tc_fence_before();
-    __syncthreads();
-    tc_fence_after();
-    g.bad = s_bad != 0;
+      asm volatile("cp.async.wait_all;" ::: "memory");
+      fence_async_shared();
+      tc_fence_before();
+      asm volatile("bar.sync 1, 288;" ::: "memory");
+      tc_fence_after();
+    }
   };
   // Every warp is through with the segment; false: a role gave up, everybody leaves.
   auto end = [&](const CtSeg& g, bool ok) {
@@ -326,44 +383,40 @@ __global__ void __launch_bounds__(CtShape<DH, KT>::THREADS, 1) chunk_tc_kernel(c
     const uint32_t base = tmem + ((uint32_t)((warp & 3) * 32) << 16), s_col = base + (uint32_t)(sub * 128),
                    o_col = base + 256u + (uint32_t)(sub * 128);
     const float sc = a.scale_log2;
-    int ns = 0, no = 0;   // S tiles, outputs so far
+    int ns = 0, no = 0, kt = 0;   // S tiles, outputs, key tiles so far
     CtSeg g{};
     bool ok = true;
     while (u < u_end) {
       begin(g);
-      const int tok = sub * ts + r / group;
-      const bool mine = r < ts * group && tok < g.n_tok;
+      const int tok = s_tok[sub * 128 + r];
+      const bool mine = tok >= 0 && tok < g.n_tok;
       const int lim = mine ? max(g.past + g.t0 + tok + 1, 0) : 0;
       const int sub_lo = max(g.past + g.t0 + sub * ts + 1, 0);   // keys of the sub-tile's first token
-      const int n_my = g.nt[sub];
+      const int n_my = g.nt(sub);
       float m = -INFINITY, l = 0.f;
-      for (int j = 0; j < n_my; ++j) {
+      for (int j = 0; j < n_my; ++j, ++kt) {
         if (!(ok = mbar_wait_warp(&s_full[sub], (uint32_t)(ns & 1), abort_flag, err, wlim))) break;
         ++ns;
         tc_fence_after();
-        float s0[64], s1[64];
-        tmem_ld64(s_col, s0);
-        tmem_ld64(s_col + 64, s1);
-        const int k0 = (g.j_lo + j) * CT_BN;
-        if (g.bad || k0 + CT_BN > sub_lo) {
+        float s[CT_BN];
+        tmem_ld128(s_col, s);
+        const int k0 = (g.j_lo + j) * CT_BN, gone = s_gone[kt & 3];
+        if (k0 + CT_BN > sub_lo || gone) {
           const int nk_r = lim - k0;
-          unsigned gone = 0;   // blocks that are not there
-          if (g.bad)
-            for (int b = 0; b < 8; ++b)
-              if (k0 + b * 16 < g.k_end && !g.there(a.c, k0 + b * 16)) gone |= 1u << b;
 #pragma unroll
-          for (int e = 0; e < 64; ++e) {
-            if (e >= nk_r || (gone >> (e >> 4) & 1)) s0[e] = -INFINITY;
-            if (64 + e >= nk_r || (gone >> (4 + (e >> 4)) & 1)) s1[e] = -INFINITY;
-          }
+          for (int e = 0; e < CT_BN; ++e)
+            if (e >= nk_r || (gone >> (e >> 4) & 1)) s[e] = -INFINITY;
         }
-        float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+        float mx[8];
 #pragma unroll
-        for (int e = 0; e < 64; ++e) {
-          mx[e & 3] = fmaxf(mx[e & 3], s0[e]);
-          mx[e & 3] = fmaxf(mx[e & 3], s1[e]);
-        }
-        const float tmax = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * sc;
+        for (int e = 0; e < 8; ++e) mx[e] = max3(s[e], s[e + 8], s[e + 16]);
+#pragma unroll
+        for (int e = 24; e < CT_BN - 8; e += 16)
+#pragma unroll
+          for (int q = 0; q < 8; ++q) mx[q] = max3(mx[q], s[e + q], s[e + 8 + q]);
+#pragma unroll
+        for (int q = 0; q < 8; ++q) mx[q] = fmaxf(mx[q], s[CT_BN - 8 + q]);
+        const float tmax = fmaxf(max3(max3(mx[0], mx[1], mx[2]), mx[3], mx[4]), max3(mx[5], mx[6], mx[7])) * sc;
         float m_new = m;
         if (tmax > m && (m == -INFINITY || tmax - m > CT_RAISE)) m_new = tmax;
         const float f = (m == -INFINITY || m_new == m) ? 1.f : ex2_approx(m - m_new);
@@ -380,26 +433,33 @@ __global__ void __launch_bounds__(CtShape<DH, KT>::THREADS, 1) chunk_tc_kernel(c
         }
         m = m_new;
         const float ref = m == -INFINITY ? 0.f : m;
-        float sum[4] = {0.f, 0.f, 0.f, 0.f};
-        uint32_t pk[32];
+        const uint64_t sc2 = f2_pack(sc, sc), ref2 = f2_pack(-ref, -ref);
+        uint64_t sum[4] = {0, 0, 0, 0};
+        // P in two halves: O += P V of the first half's keys runs beside the second half's exponentials
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          float(&s)[64] = h ? s1 : s0;
+          uint32_t pk[32];
 #pragma unroll
           for (int e = 0; e < 64; e += 2) {
-            const float p0 = ex2_approx(fmaf(s[e], sc, -ref)), p1 = ex2_approx(fmaf(s[e + 1], sc, -ref));
-            sum[(e >> 1) & 3] += p0 + p1;
+            float p0, p1;
+            f2_unpack(f2_fma(f2_pack(s[h * 64 + e], s[h * 64 + e + 1]), sc2, ref2), p0, p1);
+            p0 = ex2_approx(p0);
+            p1 = ex2_approx(p1);
+            sum[(e >> 1) & 3] = f2_add(sum[(e >> 1) & 3], f2_pack(p0, p1));
             const __nv_bfloat162 pr = __floats2bfloat162_rn(p0, p1);
             pk[e >> 1] = *reinterpret_cast<const uint32_t*>(&pr);
           }
           tmem_st32u(s_col + (uint32_t)(h * 32), pk);
+          tmem_st_wait();
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(h ? &p_full[sub] : &p_half[sub]);
         }
-        tmem_st_wait();
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&p_full[sub]);
-        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+        float l0, l1;
+        f2_unpack(f2_add(f2_add(sum[0], sum[1]), f2_add(sum[2], sum[3])), l0, l1);
+        l += l0 + l1;
       }
+      if (ok) kt += g.n_it - n_my;   // (the segment's key tiles: what s_gone goes by)
       // O / l, or the part
       if (ok && n_my > 0) {
         ok = mbar_wait_warp(&o_full[sub], (uint32_t)(no & 1), abort_flag, err, wlim);
@@ -408,13 +468,13 @@ __global__ void __launch_bounds__(CtShape<DH, KT>::THREADS, 1) chunk_tc_kernel(c
       tc_fence_after();
       const bool poisoned = s_poisoned != 0;
       const float inv = lim == 0 ? 0.f : 1.f / l;
-      if (!g.whole && mine && ok) {
-        float* ml = ct_ml(p, g.slot) + (sub * 128 + r) * 2;
-        ml[0] = m;
-        ml[1] = l;
-      }
+      const CtWs ws(p);
+      if (!g.whole && mine && ok) *ws.ml_at(g.slot, sub * 128 + r) = make_float2(m, l);
+      // (a finished tile's rows go through the warp's 32 rows of Q's place, so that whole lines are written)
+      uint8_t* stage = sQ + sub * L::Q_BYTES + (warp & 3) * 32 * (DH * 2);
+      const bool any = sub == 0 || g.n_tok > ts;
 #pragma unroll 1
-      for (int c = 0; c < DH / 32; ++c) {
+      for (int c = 0; any && c < DH / 32; ++c) {
         float v[32];
         if (n_my > 0) {   // (the same for the whole warp)
           tmem_ld32(o_col + (uint32_t)(c * 32), v);
@@ -427,25 +487,34 @@ __global__ void __launch_bounds__(CtShape<DH, KT>::THREADS, 1) chunk_tc_kernel(c
           for (int e = 0; e < 32; ++e)
             if (s_pk[c * 32 + e] < lim) v[e] = NAN;
         }
-        if (mine && ok) {
-          if (g.whole) {
-            uint32_t w[16];
+        if (g.whole) {
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-              const __nv_bfloat162 pr = __floats2bfloat162_rn(v[2 * e] * inv, v[2 * e + 1] * inv);
-              w[e] = *reinterpret_cast<const uint32_t*>(&pr);
+          for (int e = 0; e < 4; ++e) {
+            uint32_t w[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+              const __nv_bfloat162 pr = __floats2bfloat162_rn(v[8 * e + 2 * q] * inv, v[8 * e + 2 * q + 1] * inv);
+              w[q] = *reinterpret_cast<const uint32_t*>(&pr);
             }
-            uint4* o = reinterpret_cast<uint4*>((bf16*)a.out + (size_t)(g.x.q0 + g.t0 + tok) * a.ld_out +
-                                                (size_t)(g.x.kvh * group + r % group) * DH + c * 32);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) o[e] = make_uint4(w[4 * e], w[4 * e + 1], w[4 * e + 2], w[4 * e + 3]);
-          } else {
-            float4* o = reinterpret_cast<float4*>(ct_o(p, g.slot, DH) + (size_t)(sub * 128 + r) * DH + c * 32);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) o[e] = make_float4(v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]);
+            *reinterpret_cast<uint4*>(stage + lane * (DH * 2) + (((c * 4 + e) ^ (lane & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
           }
+        } else if (mine && ok) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            *ws.o_at(g.slot, DH, c * 8 + e, sub * 128 + r) = make_float4(v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]);
         }
         __syncwarp();
+      }
+      if (any && g.whole && ok) {
+        bf16* out = (bf16*)a.out + (size_t)(g.x.q0 + g.t0) * a.ld_out + (size_t)g.x.kvh * group * DH;
+        constexpr int PR = DH / 8;   // 16-byte pieces of a row
+#pragma unroll 4
+        for (int i = lane; i < 32 * PR; i += 32) {
+          const int rr = i / PR, pc = i % PR, row = (warp & 7) * 32 + rr, tk = s_tok[row];
+          if (tk >= 0 && tk < g.n_tok)
+            *reinterpret_cast<uint4*>(out + tk * a.ld_out + s_off[row] + pc * 8) =
+                *reinterpret_cast<const uint4*>(stage + rr * (DH * 2) + ((pc ^ (rr & 7)) << 4));
+        }
       }
       if (!end(g, ok)) break;
     }
@@ -470,7 +539,7 @@ __global__ void __launch_bounds__(CtShape<DH, KT>::THREADS, 1) chunk_tc_kernel(c
         }
         if (j >= 0) {
           if (!(ok = mbar_wait_warp(&v_full[vn & 1], (uint32_t)((vn >> 1) & 1), abort_flag, err, wlim))) break;
-          if (KT == KV_BF16 && g.edge(j)) {
+          if (KT == KV_BF16 && (g.edge(j) || s_gone[vn & 3])) {
             if (!(ok = mbar_wait_warp(&v_fix[vn & 1], (uint32_t)(nf[vn & 1] & 1), abort_flag, err, wlim))) break;
             ++nf[vn & 1];
           }
@@ -479,22 +548,26 @@ __global__ void __launch_bounds__(CtShape<DH, KT>::THREADS, 1) chunk_tc_kernel(c
 #pragma unroll
         for (int sub = 0; sub < 2; ++sub) {
           if (!ok) break;
-          if (j >= 0 && j < g.nt[sub]) {
-            if (!(ok = mbar_wait_warp(&p_full[sub], (uint32_t)(np[sub] & 1), abort_flag, err, wlim))) break;
-            ++np[sub];
-            tc_fence_after();
-            if (elect_one()) {
-              const uint32_t pa = tmem + (uint32_t)(sub * 128);
+          if (j >= 0 && j < g.nt(sub)) {
 #pragma unroll
-              for (int kk = 0; kk < CT_BN / 16; ++kk) {
-                const uint64_t vb = sdesc_mn_sw128(smem_u32(sV + (vn & 1) * L::KV_BYTES + kk * 16 * 128), (uint32_t)(CT_BN * 128));
-                umma_bf16_ts(tmem + 256u + (uint32_t)(sub * 128), pa + (uint32_t)(kk * 8), vb, IDESC_O, (j > 0 || kk > 0) ? 1u : 0u);
+            for (int h = 0; h < 2; ++h) {
+              if (!(ok = mbar_wait_warp(h ? &p_full[sub] : &p_half[sub], (uint32_t)(np[sub] & 1), abort_flag, err, wlim))) break;
+              tc_fence_after();
+              if (elect_one()) {
+                const uint32_t pa = tmem + (uint32_t)(sub * 128);
+#pragma unroll
+                for (int kk = h * 4; kk < h * 4 + 4; ++kk) {
+                  const uint64_t vb = sdesc_mn_sw128(smem_u32(sV + (vn & 1) * L::KV_BYTES + kk * 16 * 128), (uint32_t)(CT_BN * 128));
+                  umma_bf16_ts(tmem + 256u + (uint32_t)(sub * 128), pa + (uint32_t)(kk * 8), vb, IDESC_O, (j > 0 || kk > 0) ? 1u : 0u);
+                }
+                if (h == 1 && j == g.nt(sub) - 1) umma_commit(&o_full[sub]);
               }
-              if (j == g.nt[sub] - 1) umma_commit(&o_full[sub]);
+              __syncwarp();
             }
-            __syncwarp();
+            if (!ok) break;
+            ++np[sub];
           }
-          if (j + 1 < g.nt[sub]) {
+          if (j + 1 < g.nt(sub)) {
             tc_fence_after();
             if (elect_one()) {
 #pragma unroll
@@ -531,25 +604,40 @@ __global__ void __launch_bounds__(CtShape<DH, KT>::THREADS, 1) chunk_tc_kernel(c
     int cnt = 0;   // tiles sent so far
     CtSeg g{};
     bool ok = true;
-    // V tile j, in stage s (its phase of v_full): entries nobody attends to zero, non-finite ones noted
-    auto mend = [&](int j, int vi) {
+    // V tile j (the vi-th, blocks `gone` of it not there): entries nobody attends to zero, non-finite ones noted
+    auto mend = [&](int j, int vi, int gone) {
       const int s = vi & 1;
       if (!mbar_wait_warp(&v_full[s], (uint32_t)((vi >> 1) & 1), abort_flag, err, wlim)) return false;
       uint8_t* v = sV + s * L::KV_BYTES;
-      const int k0 = (g.j_lo + j) * CT_BN;
-      for (int i = lane; i < L::HALVES * CT_BN * 8; i += 32) {   // 16-byte pieces
-        const int hf = i / (CT_BN * 8), key = i / 8 % CT_BN, pc = (i & 7) ^ (key & 7);
-        uint4* w = reinterpret_cast<uint4*>(v + hf * CT_BN * 128 + key * 128 + ((i & 7) << 4));
-        if (k0 + key >= g.k_end || (g.bad && !g.there(a.c, k0 + key))) {
-          *w = make_uint4(0, 0, 0, 0);
-          continue;
+      const int k0 = (g.j_lo + j) * CT_BN, n_key = min(g.k_end - k0, CT_BN);
+      auto piece = [&](int hf, int key, int c) { return reinterpret_cast<uint4*>(v + hf * CT_BN * 128 + key * 128 + (c << 4)); };
+      // (first to zero: what was not fetched may hold anything)
+      for (int i = n_key * 8 + lane; i < CT_BN * 8; i += 32)
+        for (int hf = 0; hf < L::HALVES; ++hf) *piece(hf, i >> 3, i & 7) = make_uint4(0, 0, 0, 0);
+      if (gone)
+        for (int i = lane; i < CT_BN * 8; i += 32)
+          if (gone >> (i >> 7) & 1)
+            for (int hf = 0; hf < L::HALVES; ++hf) *piece(hf, i >> 3, i & 7) = make_uint4(0, 0, 0, 0);
+      __syncwarp();
+#pragma unroll 1
+      for (int i0 = 0; i0 < n_key * 8; i0 += 128) {   // 16 keys: a fetched block, or zeros
+        uint4 y[4 * L::HALVES];
+        uint32_t any = 0;
+#pragma unroll
+        for (int q = 0; q < 4 * L::HALVES; ++q) {
+          y[q] = *piece(q >> 2, (i0 >> 3) + (q & 3) * 4 + (lane >> 3), lane & 7);
+          any |= ct_any_bad2(y[q].x) | ct_any_bad2(y[q].y) | ct_any_bad2(y[q].z) | ct_any_bad2(y[q].w);
         }
-        uint4 y = *w;
-        const uint32_t b[4] = {ct_bad2(y.x), ct_bad2(y.y), ct_bad2(y.z), ct_bad2(y.w)};
-        if (b[0] | b[1] | b[2] | b[3]) {
-          *w = make_uint4(y.x & ~b[0], y.y & ~b[1], y.z & ~b[2], y.w & ~b[3]);
-          for (int e = 0; e < 8; ++e)
-            if (b[e >> 1] >> ((e & 1) * 16) & 1) atomicMin(&s_pk[hf * 64 + pc * 8 + e], k0 + key);
+        if (any) {
+#pragma unroll
+          for (int q = 0; q < 4 * L::HALVES; ++q) {
+            const int key = (i0 >> 3) + (q & 3) * 4 + (lane >> 3), col = (q >> 2) * 64 + (((lane & 7) ^ (key & 7)) << 3);
+            const uint32_t b[4] = {ct_bad2(y[q].x), ct_bad2(y[q].y), ct_bad2(y[q].z), ct_bad2(y[q].w)};
+            *piece(q >> 2, key, lane & 7) = make_uint4(y[q].x & ~b[0], y[q].y & ~b[1], y[q].z & ~b[2], y[q].w & ~b[3]);
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+              if (b[e >> 1] >> ((e & 1) * 16) & 1) atomicMin(&s_pk[col + e], k0 + key);
+          }
           s_poisoned = 1;
         }
       }
@@ -560,21 +648,21 @@ __global__ void __launch_bounds__(CtShape<DH, KT>::THREADS, 1) chunk_tc_kernel(c
     };
     while (u < u_end) {
       begin(g);
+      int gone = 0, gone_prev = 0;
       for (int j = 0; j <= g.n_it && ok; ++j) {
-        if (!kw && j > 0 && g.edge(j - 1) && !(ok = mend(j - 1, cnt - 1))) break;
+        gone_prev = gone;
+        if (!kw && j > 0 && (g.edge(j - 1) || gone_prev) && !(ok = mend(j - 1, cnt - 1, gone_prev))) break;
         if (j == g.n_it) break;
-        const int s = cnt & 1;
-        int row = -1;
-        if (lane < 8) {
-          const int b = (g.j_lo + j) * 8 + lane;
-          if (b * 16 < g.k_end && g.there(a.c, b * 16)) row = (g.table[b] * a.c.n_kv_heads + g.x.kvh) * 16;
-        }
+        const int s = cnt & 1, row = lane < 8 ? g.row_of(a.c, (g.j_lo + j) * 8 + lane) : -1;
         const unsigned on = __ballot_sync(0xffffffffu, row >= 0);
+        gone = (int)__ballot_sync(0xffffffffu, row == -2);
+        if (gone && lane == 0) a.c.flag(ERRW_POS);
         int rows8[8];
 #pragma unroll
         for (int b = 0; b < 8; ++b) rows8[b] = __shfl_sync(0xffffffffu, row, b);
         if (cnt >= 2 && !(ok = mbar_wait_warp(&empty[s], (uint32_t)(((cnt >> 1) - 1) & 1), abort_flag, err, wlim))) break;
         if (elect_one()) {
+          if (kw) s_gone[cnt & 3] = gone;   // (tile cnt - 4 is through: its K stage has been freed twice over)
           // (blocks that are not fetched leave the stage's old contents: masked in S, mended in V)
           mbar_expect_tx(&full[s], (uint32_t)(__popc(on) * 16 * 128 * L::HALVES));
           for (int b = 0; b < 8; ++b)
@@ -667,6 +755,14 @@ __global__ void __launch_bounds__(CtShape<DH, KT>::THREADS, 1) chunk_tc_kernel(c
             }
           }
         }
+        if (!is_v && warp == 9) {
+          const int row = lane < 8 ? g.row_of(a.c, (g.j_lo + (t >> 1)) * 8 + lane) : -1;
+          const int gone = (int)__ballot_sync(0xffffffffu, row == -2);
+          if (lane == 0) {
+            if (gone) a.c.flag(ERRW_POS);
+            s_gone[n & 3] = gone;
+          }
+        }
         if (t + 1 < 2 * g.n_it) fetch(t + 1);
         fence_async_shared();
         __syncwarp();
@@ -682,58 +778,62 @@ __global__ void __launch_bounds__(CtShape<DH, KT>::THREADS, 1) chunk_tc_kernel(c
   if (warp == 8) tmem_dealloc(tmem, 512);
 }
 
-// Join of the tiles that runs share: CTA (i, y) takes the tile that run i begins inside of, where i is the first such run, and
-// a quarter of its rows.
+// Join of the tiles that runs share: CTA (i, y) takes the tile that run i + 1 is the first to begin inside of, an eighth of its
+// rows.  Parts: run i's (the tile's beginning), run i + 1's, ... in order.
+constexpr int CJ_SPLIT = 8;
 template <int DH>
 __global__ void __launch_bounds__(256) chunk_tc_join_kernel(const __grid_constant__ CtParams p) {
-  __shared__ CtTile s_tile;
-  __shared__ long long s_total;
   PDL_ENTRY();
-  const ChunkCall& a = p.a;
-  const int tid = threadIdx.x, tq = 2 * p.ts, run = (int)blockIdx.x + 1;
-  if (tid < 32) {
-    const long long tot = ct_total(a, tq);
-    CtTile x{};
-    x.units = 0;
-    const int runs = ct_runs(tot, p.runs);
-    if (run < runs) ct_find(a, tq, ct_start(tot, runs, run), x);
-    if (tid == 0) {
-      s_total = tot;
-      s_tile = x;
-    }
-  }
-  __syncthreads();
-  const CtTile x = s_tile;
-  const long long total = s_total;
-  const int runs = ct_runs(total, p.runs);
-  if (run >= runs) return;
-  const long long b0 = ct_start(total, runs, run);
-  if (b0 == x.u0 || ct_start(total, runs, run - 1) > x.u0) return;   // begins with the tile; not the first run inside
-  // parts: run - 1 (the tile's beginning), run, ... while they begin before the tile's end
+  const CtWs ws(p);
+  const int run = (int)blockIdx.x + 1, tid = threadIdx.x;
+  const CtNote n = ws.note[run];
+  if (n.u0 < 0 || ws.note[run - 1].u0 == n.u0) return;
   int n_part = 2;
-  while (run + n_part - 1 < runs && ct_start(total, runs, run + n_part - 1) < x.u0 + x.units) ++n_part;
-  const int group = a.n_heads / a.c.n_kv_heads, past = x.len - x.c, t0 = x.tile * tq, n_tok = min(tq, x.c - t0);
-  for (int i = tid + blockIdx.y * 256; i < CT_ROWS * (DH / 4); i += 256 * gridDim.y) {
-    const int r = i / (DH / 4), d = i % (DH / 4) * 4, sub = r >> 7, rr = r & 127, tok = sub * p.ts + rr / group;
-    if (rr >= p.ts * group || tok >= n_tok) continue;
-    float M = -INFINITY;
-    for (int k = 0; k < n_part; ++k) M = fmaxf(M, __ldcg(ct_ml(p, (run - 1 + k) * 2 + (k == 0)) + r * 2));
-    const float ref = M == -INFINITY ? 0.f : M;
-    float l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int k = 0; k < n_part; ++k) {
-      const int slot = (run - 1 + k) * 2 + (k == 0);
-      const float2 ml = __ldcg(reinterpret_cast<const float2*>(ct_ml(p, slot) + r * 2));
-      const float4 v = __ldcg(reinterpret_cast<const float4*>(ct_o(p, slot, DH) + (size_t)r * DH + d));
-      const float w = ex2_approx(ml.x - ref);
-      l += w * ml.y;
-      o[0] += w * v.x;
-      o[1] += w * v.y;
-      o[2] += w * v.z;
-      o[3] += w * v.w;
+  while (run + n_part - 1 < p.runs && ws.note[run + n_part - 1].u0 == n.u0) ++n_part;
+  const ChunkCall& a = p.a;
+  const int group = a.n_heads / a.c.n_kv_heads;
+  constexpr int ROWS = CT_ROWS / CJ_SPLIT;
+  // a warp takes 8 rows x 4 pieces of 4 columns: whole lines of the parts, whole sectors of the output
+  const int lane = tid & 31, rl = lane & 7, dl = lane >> 3;
+  for (int w = tid >> 5; w < ROWS / 8 * (DH / 16); w += 8) {
+    const int r = (int)blockIdx.y * ROWS + w % (ROWS / 8) * 8 + rl, d4 = w / (ROWS / 8) * 4 + dl;
+    const int rr = r & 127, tk = rr / group, tok = (r >> 7) * p.ts + tk;
+    if (tk >= p.ts || tok >= n.n_tok) continue;
+    float M = -INFINITY, l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int k0 = 0; k0 < n_part; k0 += 4) {
+      float2 ml[4];
+      float4 v[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        ml[k] = make_float2(-INFINITY, 0.f);
+        v[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (k0 + k < n_part) {
+          const int slot = (run - 1 + k0 + k) * 2 + (k0 + k == 0);
+          ml[k] = __ldcg(ws.ml_at(slot, r));
+          v[k] = __ldcg(ws.o_at(slot, DH, d4, r));
+        }
+      }
+      float mn = M;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) mn = fmaxf(mn, ml[k].x);
+      const float ref = mn == -INFINITY ? 0.f : mn, f = ex2_approx(M - ref);
+      M = mn;
+      l *= f;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] *= f;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float x = ex2_approx(ml[k].x - ref);
+        l += x * ml[k].y;
+        o[0] += x * v[k].x;
+        o[1] += x * v[k].y;
+        o[2] += x * v[k].z;
+        o[3] += x * v[k].w;
+      }
     }
-    const float inv = past + t0 + tok < 0 ? 0.f : 1.f / l;
+    const float inv = n.pos0 + tok < 0 ? 0.f : 1.f / l;
     const __nv_bfloat162 y0 = __floats2bfloat162_rn(o[0] * inv, o[1] * inv), y1 = __floats2bfloat162_rn(o[2] * inv, o[3] * inv);
-    *reinterpret_cast<uint2*>((bf16*)a.out + (size_t)(x.q0 + t0 + tok) * a.ld_out + (size_t)(x.kvh * group + rr % group) * DH + d) =
+    *reinterpret_cast<uint2*>((bf16*)a.out + (size_t)(n.row0 + tok) * a.ld_out + (size_t)(n.kvh * group + rr % group) * DH + d4 * 4) =
         make_uint2(*reinterpret_cast<const uint32_t*>(&y0), *reinterpret_cast<const uint32_t*>(&y1));
   }
 }
@@ -746,7 +846,7 @@ cudaError_t launch_t(cudaStream_t st, const CtParams& p) {
   if (e != cudaSuccess) return e;
   e = launch_k(chunk_tc_kernel<DH, KT>, dim3(p.runs), dim3(L::THREADS), smem, st, p);
   if (e != cudaSuccess) return e;
-  return launch_k(chunk_tc_join_kernel<DH>, dim3(std::max(1, p.runs - 1), 4), dim3(256), 0, st, p);
+  return launch_k(chunk_tc_join_kernel<DH>, dim3(std::max(1, p.runs - 1), CJ_SPLIT), dim3(256), 0, st, p);
 }
 
 int ct_sms() {
@@ -766,8 +866,7 @@ bool chunk_tc_takes(const KvPaged& c, int n_heads) {
          n_heads / c.n_kv_heads <= CT_BM && (long long)c.n_blocks * c.n_kv_heads * 16 < (1ll << 31) && tc_gemm_supported();
 }
 
-static size_t ct_part_floats(int dh) { return (size_t)ct_sms() * 2 * CT_ROWS * (dh + 2); }
-size_t chunk_tc_workspace(const KvPaged& c) { return (ct_part_floats(c.head_dim) + 4) * sizeof(float); }
+size_t chunk_tc_workspace(const KvPaged& c) { return (ct_ws_floats(ct_sms(), c.head_dim) + 4) * sizeof(float); }
 
 cudaError_t launch_chunk_tc(cudaStream_t st, const ChunkCall& a, int* launches) {
   CtParams p;
@@ -776,7 +875,7 @@ cudaError_t launch_chunk_tc(cudaStream_t st, const ChunkCall& a, int* launches) 
   p.ts = CT_BM / (a.n_heads / a.c.n_kv_heads);
   p.runs = ct_sms();
   const int dh = a.c.head_dim;
-  p.no_err = (unsigned*)(a.part + ct_part_floats(dh));
+  p.no_err = (unsigned*)(a.part + ct_ws_floats(p.runs, dh));
   if (a.c.type == KV_BF16) {
     const uint64_t rows = (uint64_t)a.c.n_blocks * a.c.n_kv_heads * 16;
     if (!tc_encode_2d(&p.kmap, a.c.k, (uint64_t)dh, rows, (uint64_t)dh * 2, 16) ||
