@@ -519,72 +519,63 @@ __global__ void __launch_bounds__(CtShape<DH, KT>::THREADS, 1) chunk_tc_kernel(c
       if (!end(g, ok)) break;
     }
   } else if (warp == 8) {
-    // ---- matrix instructions
+    // ---- matrix instructions: one thread for a whole segment (a warp that meets at every wait took 3900 cycles a key tile to
+    // issue what the tensor core does in 2048), descriptors made once and moved by their address field
     if constexpr (KT == KV_E4M3) asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
     constexpr uint32_t IDESC_S = umma_idesc(CT_BN, false), IDESC_O = umma_idesc(DH, true);
+    const uint64_t dq = sdesc_sw128(smem_u32(sQ)), dk = sdesc_sw128(smem_u32(sK)), dv = sdesc_mn_sw128(smem_u32(sV), CT_BN * 128);
     int nk = 0, nv = 0, np[2] = {0, 0}, nf[2] = {0, 0};   // K, V, P tiles and mended V tiles (per stage) so far
-    auto commit = [&](uint64_t* bar) {
-      if (elect_one()) umma_commit(bar);
-      __syncwarp();
-    };
     CtSeg g{};
     bool ok = true;
     while (u < u_end) {
       begin(g);
-      for (int j = -1; j < g.n_it && ok; ++j) {
-        const int kn = nk, vn = nv;
-        if (j + 1 < g.n_it) {
-          if (!(ok = mbar_wait_warp(&k_full[kn & 1], (uint32_t)((kn >> 1) & 1), abort_flag, err, wlim))) break;
-          ++nk;
-        }
-        if (j >= 0) {
-          if (!(ok = mbar_wait_warp(&v_full[vn & 1], (uint32_t)((vn >> 1) & 1), abort_flag, err, wlim))) break;
-          if (KT == KV_BF16 && (g.edge(j) || s_gone[vn & 3])) {
-            if (!(ok = mbar_wait_warp(&v_fix[vn & 1], (uint32_t)(nf[vn & 1] & 1), abort_flag, err, wlim))) break;
-            ++nf[vn & 1];
+      if (elect_one()) {
+        auto wait = [&](uint64_t* bar, int phase) { return ok = mbar_wait(bar, (uint32_t)(phase & 1), abort_flag, err, wlim); };
+        for (int j = -1; j < g.n_it; ++j) {
+          const int kn = nk, vn = nv, ks = kn & 1, vs = vn & 1;
+          if (j + 1 < g.n_it) {
+            if (!wait(&k_full[ks], kn >> 1)) break;
+            ++nk;
           }
-          ++nv;
-        }
+          if (j >= 0) {
+            if (!wait(&v_full[vs], vn >> 1)) break;
+            if (KT == KV_BF16 && (g.edge(j) || s_gone[vn & 3]) && !wait(&v_fix[vs], nf[vs]++)) break;
+            ++nv;
+          }
+          const uint64_t dks = dk + (uint64_t)(ks * (L::KV_BYTES >> 4)), dvs = dv + (uint64_t)(vs * (L::KV_BYTES >> 4));
 #pragma unroll
-        for (int sub = 0; sub < 2; ++sub) {
-          if (!ok) break;
-          if (j >= 0 && j < g.nt(sub)) {
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              if (!(ok = mbar_wait_warp(h ? &p_full[sub] : &p_half[sub], (uint32_t)(np[sub] & 1), abort_flag, err, wlim))) break;
+          for (int sub = 0; sub < 2; ++sub) {
+            if (j >= 0 && j < g.nt(sub)) {
+              const uint32_t pa = tmem + (uint32_t)(sub * 128), oa = tmem + 256u + (uint32_t)(sub * 128);
+              if (!wait(&p_half[sub], np[sub])) break;
               tc_fence_after();
-              if (elect_one()) {
-                const uint32_t pa = tmem + (uint32_t)(sub * 128);
 #pragma unroll
-                for (int kk = h * 4; kk < h * 4 + 4; ++kk) {
-                  const uint64_t vb = sdesc_mn_sw128(smem_u32(sV + (vn & 1) * L::KV_BYTES + kk * 16 * 128), (uint32_t)(CT_BN * 128));
-                  umma_bf16_ts(tmem + 256u + (uint32_t)(sub * 128), pa + (uint32_t)(kk * 8), vb, IDESC_O, (j > 0 || kk > 0) ? 1u : 0u);
-                }
-                if (h == 1 && j == g.nt(sub) - 1) umma_commit(&o_full[sub]);
-              }
-              __syncwarp();
+              for (int kk = 0; kk < 4; ++kk)
+                umma_bf16_ts(oa, pa + (uint32_t)(kk * 8), dvs + (uint64_t)(kk * (16 * 128 >> 4)), IDESC_O, (j > 0 || kk > 0) ? 1u : 0u);
+              if (!wait(&p_full[sub], np[sub])) break;
+              tc_fence_after();
+#pragma unroll
+              for (int kk = 4; kk < 8; ++kk)
+                umma_bf16_ts(oa, pa + (uint32_t)(kk * 8), dvs + (uint64_t)(kk * (16 * 128 >> 4)), IDESC_O, 1u);
+              if (j == g.nt(sub) - 1) umma_commit(&o_full[sub]);
+              ++np[sub];
             }
-            if (!ok) break;
-            ++np[sub];
-          }
-          if (j + 1 < g.nt(sub)) {
-            tc_fence_after();
-            if (elect_one()) {
+            if (j + 1 < g.nt(sub)) {
+              tc_fence_after();
 #pragma unroll
               for (int kk = 0; kk < DH / 16; ++kk) {
-                const uint64_t qa = sdesc_sw128(smem_u32(sQ + sub * L::Q_BYTES + (kk >> 2) * CT_BM * 128) + (kk & 3) * 32);
-                const uint64_t kb = sdesc_sw128(smem_u32(sK + (kn & 1) * L::KV_BYTES + (kk >> 2) * CT_BN * 128) + (kk & 3) * 32);
-                umma_bf16(tmem + (uint32_t)(sub * 128), qa, kb, IDESC_S, kk > 0 ? 1u : 0u);
+                const uint64_t at = (uint64_t)(((kk >> 2) * CT_BM * 128 + (kk & 3) * 32) >> 4);
+                umma_bf16(tmem + (uint32_t)(sub * 128), dq + (uint64_t)(sub * (L::Q_BYTES >> 4)) + at, dks + at, IDESC_S, kk > 0 ? 1u : 0u);
               }
               umma_commit(&s_full[sub]);
             }
-            __syncwarp();
           }
+          if (!ok) break;
+          if (j + 1 < g.n_it) umma_commit(&k_empty[ks]);
+          if (j >= 0) umma_commit(&v_empty[vs]);
         }
-        if (!ok) break;
-        if (j + 1 < g.n_it) commit(&k_empty[kn & 1]);
-        if (j >= 0) commit(&v_empty[vn & 1]);
       }
+      __syncwarp();
       if (!end(g, ok)) break;
     }
     // every matrix instruction has completed before tensor memory is given back
