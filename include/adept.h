@@ -395,7 +395,7 @@ ADEPT_API int64_t adept_hsm_param_numel(const adept_model* m, int param);
  *     a = 0; an element is e4m3(x 2^-e), rounded once, to nearest even.  NaN stays NaN; an infinity
  *     is stored as NaN.  What is read back is exact in fp32, and in bf16 above its subnormals (only
  *     an element that rounded up to 2^128 reads back as infinity).
- * The buffers are the caller's, on the current device; d_k and d_v start on 16 bytes.  The calls
+ * The buffers are the caller's, on the current device; d_k, d_v and the exponents start on 16 bytes.  The calls
  * allocate nothing, hold no state between calls and can be captured into a graph; calls on one
  * cache are ordered by their streams as any other work on shared buffers is.
  * d_err (may be NULL): a device word that kernels set where an input read on the device is out of

@@ -9,7 +9,9 @@
 // (negative, out of range) are left out and flagged.
 //
 // The split of the work, and the join of split tiles, are in kv_paged.h.
+#define ADEPT_TU_ID 14
 #include "kv_paged.h"
+#include "tc_ptx.cuh"
 
 #include <cuda_fp8.h>
 
@@ -174,71 +176,131 @@ __global__ void __launch_bounds__(CG_KEYS) chunk_any_kernel(const __grid_constan
 // head's group) x a run of keys, CF_WARPS warps taking blocks in turn, each with a softmax and sums of its own, merged in
 // warp order at the end.
 //
-// K and V go from memory straight into the registers that the matrix instruction takes: the order of the head's dimensions
-// inside q.k is free, so a thread's B fragments of S = Q K^T are whole 16-byte pieces of its key's row (Q is loaded in the
-// same order), and the columns of O are dealt out so that a thread's B fragments of O = P V are 16-byte pieces of four keys'
-// rows, pairs of keys packed by byte permutes.  No shared memory, no barrier in the loop; the next block's K is under way
-// while the softmax runs, the next V during the next S.  An exponent of K scales S, one of V scales P: e4m3 -> bf16 is exact.
+// A head's 16 positions of a block are one contiguous piece of the pool: each warp keeps CF_STAGES of them (K, V, exponents)
+// under way by bulk copies into a ring of its own, so no warp waits for another, and no register holds what is under way.
+// From the ring the words go straight into fragments: the order of the head's dimensions inside q.k is free, so a thread's
+// B fragments of S = Q K^T are whole 16-byte pieces of its key's row (Q is loaded in the same order), and the columns of O are
+// dealt out so that a thread's B fragments of O = P V are 16-byte pieces of four keys' rows, pairs of keys packed by byte
+// permutes.
+// e4m3: K as fp16, one conversion for two codes (bf16 takes four instructions), with Q as fp16 too, each row moved by a power
+// of two so that its largest element lies in [2^14, 2^15): exact down to 2^-28 of it.  V as bf16, since P has to keep bf16's
+// range (a position of little weight may hold a V of any size).  K's exponent scales S, V's scales P.
 // ---------------------------------------------------------------------------------------------
 constexpr int CF_WARPS = 4, CF_ROWS = 16;
 constexpr float CF_RAISE = 8.f;   // the running maximum is raised once a score exceeds it by 2^8: weights stay below 256
+constexpr long long CF_DRAIN_CYCLES = 4000000000LL;
 
 template <int BYTES>
 struct Words {
   uint32_t w[BYTES / 4];
 };
 template <int BYTES>
-__device__ __forceinline__ Words<BYTES> ldg(const void* p) {
+__device__ __forceinline__ Words<BYTES> lds(const void* p) {
   Words<BYTES> r;
-  if constexpr (BYTES == 16)
-    asm volatile("ld.global.L1::no_allocate.v4.b32 {%0, %1, %2, %3}, [%4];"
-                 : "=r"(r.w[0]), "=r"(r.w[1]), "=r"(r.w[2]), "=r"(r.w[3]) : "l"(p));
-  else if constexpr (BYTES == 8)
-    asm volatile("ld.global.L1::no_allocate.v2.b32 {%0, %1}, [%2];" : "=r"(r.w[0]), "=r"(r.w[1]) : "l"(p));
-  else
-    asm volatile("ld.global.L1::no_allocate.b32 %0, [%1];" : "=r"(r.w[0]) : "l"(p));
+  if constexpr (BYTES == 16) {
+    const uint4 x = *reinterpret_cast<const uint4*>(p);
+    r.w[0] = x.x; r.w[1] = x.y; r.w[2] = x.z; r.w[3] = x.w;
+  } else if constexpr (BYTES == 8) {
+    const uint2 x = *reinterpret_cast<const uint2*>(p);
+    r.w[0] = x.x; r.w[1] = x.y;
+  } else {
+    r.w[0] = *reinterpret_cast<const uint32_t*>(p);
+  }
   return r;
 }
-// (volatile: stays behind the loads that precede it in the source)
+template <bool F16>
 __device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-  asm volatile(
-      "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+  if constexpr (F16)
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+  else
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-// Two e4m3 codes (low 16 bits) as two bf16: exact, NaN stays NaN.
-__device__ __forceinline__ uint32_t e4m3x2_bf16x2(uint32_t codes) {
+// Two e4m3 codes (low 16 bits) as two fp16, as two bf16: exact, NaN stays NaN.
+__device__ __forceinline__ uint32_t e4m3x2_f16x2(uint32_t codes) {
   const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)codes, __NV_E4M3);
-  const float2 f = __half22float2(__half2(h));
-  const __nv_bfloat162 b = __floats2bfloat162_rn(f.x, f.y);
-  return *reinterpret_cast<const uint32_t*>(&b);
+  return (uint32_t)h.x | (uint32_t)h.y << 16;
 }
 __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
   const __nv_bfloat162 x = __floats2bfloat162_rn(a, b);
   return *reinterpret_cast<const uint32_t*>(&x);
+}
+__device__ __forceinline__ uint32_t e4m3x2_bf16x2(uint32_t codes) {
+  const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)codes, __NV_E4M3);
+  const float2 f = __half22float2(__half2(h));
+  return pack_bf16(f.x, f.y);
+}
+__device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_u32(dst)),
+               "l"(src), "r"(bytes), "r"(smem_u32(bar))
+               : "memory");
+}
+
+// A bounded wait of the whole warp for a stage; false: it did not land in time, or another warp gave up.
+__device__ __forceinline__ bool cf_wait(uint64_t* bar, unsigned parity, volatile int* abort_flag, unsigned* err, long long lim) {
+  if (mbar_try_wait(bar, parity)) return true;
+  const long long t0 = clock64();
+  while (!mbar_try_wait(bar, parity)) {
+    if (*abort_flag) return false;
+    if (clock64() - t0 > lim) {
+      if (err) atomicOr(err, ERRW_TIMEOUT);
+      return false;
+    }
+  }
+  return true;
+}
+// Words of four keys' rows (0, 1 and 8, 9 of a fragment) to B fragments: f(column of the word, b0, b1), all bf16.
+template <int KT, typename F>
+__device__ __forceinline__ void cf_pairs(uint32_t k0, uint32_t k1, uint32_t k2, uint32_t k3, F f) {
+  if constexpr (KT == KV_BF16) {
+    f(0, __byte_perm(k0, k1, 0x5410), __byte_perm(k2, k3, 0x5410));
+    f(1, __byte_perm(k0, k1, 0x7632), __byte_perm(k2, k3, 0x7632));
+  } else {
+    const uint32_t x0 = __byte_perm(k0, k1, 0x5140), x1 = __byte_perm(k2, k3, 0x5140);
+    const uint32_t y0 = __byte_perm(k0, k1, 0x7362), y1 = __byte_perm(k2, k3, 0x7362);
+    f(0, e4m3x2_bf16x2(x0 & 0xffffu), e4m3x2_bf16x2(x1 & 0xffffu));
+    f(1, e4m3x2_bf16x2(x0 >> 16), e4m3x2_bf16x2(x1 >> 16));
+    f(2, e4m3x2_bf16x2(y0 & 0xffffu), e4m3x2_bf16x2(y1 & 0xffffu));
+    f(3, e4m3x2_bf16x2(y0 >> 16), e4m3x2_bf16x2(y1 >> 16));
+  }
 }
 
 template <int DH, int KT>
 struct FewShape {
   static constexpr int ES = KT == KV_BF16 ? 2 : 1;
   static constexpr int NB = KT == KV_BF16 ? 1 : 2;         // blocks of 16 keys per warp and round
+  static constexpr int STAGES = 2 * NB;                    // blocks in a warp's ring
   static constexpr int UNIT = CF_WARPS * NB * 16;
   static constexpr int KVEC = DH * ES / 4 < 16 ? DH * ES / 4 : 16, KN = DH * ES / 4 / KVEC, KE = KVEC / ES;   // K pieces of a thread
   static constexpr int VVEC = DH * ES / 8 < 16 ? DH * ES / 8 : 16, VN = DH * ES / 8 / VVEC, VE = VVEC / ES;   // V pieces
-  static constexpr int SMEM = CF_WARPS * CF_ROWS * (DH + 4) * 4;
+  static constexpr int BLOCK = 16 * DH * ES;               // bytes of a block of one head
+  static constexpr int STAGE = 2 * BLOCK + (KT == KV_E4M3 ? 32 : 0);   // K, V, exponents
+  static constexpr int RING = CF_WARPS * STAGES * STAGE, MERGE = CF_WARPS * CF_ROWS * (DH + 4) * 4;
+  static constexpr int SMEM = RING > MERGE ? RING : MERGE;
 };
 
 template <int DH, int KT>
-__global__ void __launch_bounds__(CF_WARPS * 32, 2) chunk_few_kernel(const __grid_constant__ ChunkCall a,
+__global__ void __launch_bounds__(CF_WARPS * 32, 3) chunk_few_kernel(const __grid_constant__ ChunkCall a,
                                                                      const __grid_constant__ SplitPlan p, int per_tok, int sub) {
   using F = FewShape<DH, KT>;
   constexpr int KS = DH / 16;
+  constexpr bool F16 = KT == KV_E4M3;   // S in fp16
   __shared__ SplitItem s_it;
-  __shared__ int s_have;
+  __shared__ int s_have, s_abort;
   __shared__ float s_m[CF_WARPS][CF_ROWS], s_l[CF_WARPS][CF_ROWS];
-  extern __shared__ float s_o[];   // [warp][row][DH + 4]
-  PDL_ENTRY();
+  __shared__ __align__(8) uint64_t s_full[CF_WARPS][F::STAGES];
+  extern __shared__ __align__(128) uint8_t s_dyn[];   // the rings; then [warp][row][DH + 4] floats
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
+  if (tid < CF_WARPS * F::STAGES) {
+    mbar_init(&s_full[tid / F::STAGES][tid % F::STAGES], 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (tid == 0) s_abort = 0;
+  const long long wlim = wait_limit();
+  PDL_ENTRY();
   if (warp == 0) {
     SplitItem it;
     const bool have = split_find(a, p, (int)blockIdx.x, false, it);
@@ -253,15 +315,62 @@ __global__ void __launch_bounds__(CF_WARPS * 32, 2) chunk_few_kernel(const __gri
   const int group = a.n_heads / a.c.n_kv_heads, kvh = it.group / sub, g0 = it.group % sub * per_tok;
   const int past = it.len - it.c, j0 = it.tile * p.tq, n = min(p.tq, it.c - j0);
   const int n_row = n * per_tok;   // rows of the tile in use (those with g0 + r % per_tok >= group hold nothing)
+  const int lim_lo = max(past + j0 + 1, 0), lim_hi = max(past + j0 + n, 0);   // keys of the tile's first and last token
+  const int k_end = min(min(it.u1 * F::UNIT, it.len), lim_hi);                // keys that anyone attends
+  const int b_end = (k_end + 15) >> 4;
+  const int* table = a.c.table + (size_t)it.seq * a.c.max_blocks;
+  unsigned* err = a.c.err;
 
-  // this thread's two rows (g, g + 8): Q fragments, and the keys each attends
+  // ---- the warp's ring: its blocks in order, NB of them a round
+  constexpr int STEP = CF_WARPS * F::NB;
+  const int first = it.u0 * (F::UNIT / 16) + warp * F::NB;
+  uint8_t* ring = s_dyn + warp * F::STAGES * F::STAGE;
+  // table entries of the warp's next 32 blocks, a lane each (block i of the warp: first + i / NB * STEP + i % NB)
+  int tab = -1, sent = 0, landed = 0;
+  unsigned there = 0;   // bit i % 32: block i is there (what is sent and not yet used: at most STAGES)
+  auto send = [&]() {   // block `sent` of the warp into its stage
+    const int i = sent;
+    if (i % 32 == 0) {
+      const int b = first + (i + lane) / F::NB * STEP + (i + lane) % F::NB;
+      tab = -1;
+      if (b < b_end) {
+        tab = table[b];
+        if (tab < 0 || tab >= a.c.n_blocks) {
+          a.c.flag(ERRW_POS);
+          tab = -1;
+        }
+      }
+    }
+    const int blk = __shfl_sync(0xffffffffu, tab, i % 32);
+    there = blk >= 0 ? there | 1u << (i % 32) : there & ~(1u << (i % 32));
+    if (blk >= 0 && lane == 0) {
+      uint8_t* st = ring + i % F::STAGES * F::STAGE;
+      uint64_t* bar = &s_full[warp][i % F::STAGES];
+      const size_t e = ((size_t)blk * a.c.n_kv_heads + kvh) * 16;
+      mbar_expect_tx(bar, F::STAGE);
+      bulk_load(st, (const uint8_t*)a.c.k + e * (DH * F::ES), F::BLOCK, bar);
+      bulk_load(st + F::BLOCK, (const uint8_t*)a.c.v + e * (DH * F::ES), F::BLOCK, bar);
+      if constexpr (KT == KV_E4M3) {
+        bulk_load(st + 2 * F::BLOCK, a.c.k_exp + e, 16, bar);
+        bulk_load(st + 2 * F::BLOCK + 16, a.c.v_exp + e, 16, bar);
+      }
+    }
+    ++sent;
+  };
+  // blocks of this warp (whole rounds; those past b_end are not there)
+  const int n_blk = first < b_end ? (b_end - first + STEP - 1) / STEP * F::NB : 0;
+  for (int i = 0; i < F::STAGES && i < n_blk; ++i) send();
+
+  // ---- this thread's two rows (g, g + 8): Q fragments, and the keys each attends
   uint32_t qf[KS][4];
   int lim[2];
+  float rs[2];   // what a row's S is multiplied by
 #pragma unroll
   for (int r2 = 0; r2 < 2; ++r2) {
     const int r = g + 8 * r2, j = r / per_tok, gq = g0 + r % per_tok;
     const bool on = r < n_row && gq < group;
     lim[r2] = on ? max(past + j0 + j + 1, 0) : 0;
+    rs[r2] = a.scale_log2;
     const bf16* q = (const bf16*)a.q + (size_t)(it.q0 + j0 + j) * a.ld_q + (size_t)(kvh * group + gq) * DH;
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
@@ -272,104 +381,53 @@ __global__ void __launch_bounds__(CF_WARPS * 32, 2) chunk_few_kernel(const __gri
       qf[s][r2] = x.x;
       qf[s][2 + r2] = x.y;
     }
+    if constexpr (F16) {
+      unsigned top = 0;   // exponent field of the row's largest finite element
+#pragma unroll
+      for (int s = 0; s < KS; ++s)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const unsigned lo = (qf[s][r2 + 2 * h] >> 7) & 0xffu, hi = (qf[s][r2 + 2 * h] >> 23) & 0xffu;
+          top = max(top, max(lo == 255u ? 0u : lo, hi == 255u ? 0u : hi));
+        }
+      top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+      top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+      const int e = max((int)top, 15);                                      // (rows below 2^-112 keep fewer bits)
+      const float up = __uint_as_float((unsigned)(127 + 14 + 127 - e) << 23);   // 2^(14 - (e - 127))
+      rs[r2] = a.scale_log2 * __uint_as_float((unsigned)(e < 15 ? 1 : e - 14) << 23);   // 2^((e - 127) - 14)
+#pragma unroll
+      for (int s = 0; s < KS; ++s)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          uint32_t& w = qf[s][r2 + 2 * h];
+          const __half2 y = __floats2half2_rn(__uint_as_float(w << 16) * up, __uint_as_float(w & 0xffff0000u) * up);
+          w = *reinterpret_cast<const uint32_t*>(&y);
+        }
+    }
   }
-  const int lim_lo = max(past + j0 + 1, 0), lim_hi = max(past + j0 + n, 0);   // of the tile's first and last token
-  const int k_end = min(min(it.u1 * F::UNIT, it.len), lim_hi);                // keys that anyone attends
-  const int b_end = (k_end + 15) >> 4;
-  const size_t blk_stride = (size_t)a.c.n_kv_heads * 16;
-  const int* table = a.c.table + (size_t)it.seq * a.c.max_blocks;
 
   float o[DH / 8][4], m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
 #pragma unroll
   for (int j = 0; j < DH / 8; ++j) o[j][0] = o[j][1] = o[j][2] = o[j][3] = 0.f;
 
-  // a round: NB blocks
-  struct Round {
-    Words<F::KVEC> k[F::NB][2][F::KN];
-    Words<F::VVEC> v[F::NB][4][F::VN];
-    uint32_t ke[F::NB], ve[F::NB];   // exponents of keys 2t, 2t + 1 (low half) and 8 + 2t, 9 + 2t
-  } R;
-  long long at[F::NB];   // entry 0 of the round's blocks, -1: not there
-  const int first = it.u0 * (F::UNIT / 16) + warp * F::NB;
-  // table entries of the next 32 rounds' blocks of this warp: a lane each
-  auto look = [&](int b) {
-    int blk = -1;
-    if (b < b_end) {
-      blk = table[b];
-      if (blk < 0 || blk >= a.c.n_blocks) {
-        a.c.flag(ERRW_POS);
-        blk = -1;
-      }
-    }
-    return blk;
-  };
-  constexpr int STEP = CF_WARPS * F::NB, AHEAD = 32 / F::NB;
-  int tab = -1, round = 0;
-  auto blocks_of = [&](int b) {   // blocks b .. b + NB - 1, round number `round`
-    if (round % AHEAD == 0) tab = look(b + lane / F::NB * STEP + lane % F::NB);
-#pragma unroll
-    for (int i = 0; i < F::NB; ++i) {
-      const int blk = __shfl_sync(0xffffffffu, tab, round % AHEAD * F::NB + i);
-      at[i] = blk < 0 ? -1 : (long long)blk * blk_stride + kvh * 16;
-    }
-    ++round;
-  };
-  auto load_k = [&]() {
-#pragma unroll
-    for (int i = 0; i < F::NB; ++i) {
-      if (at[i] < 0) continue;
-#pragma unroll
-      for (int nt = 0; nt < 2; ++nt)
-#pragma unroll
-        for (int c = 0; c < F::KN; ++c)
-          R.k[i][nt][c] = ldg<F::KVEC>((const char*)a.c.k + ((size_t)at[i] + nt * 8 + g) * (DH * F::ES) + (c * 4 + t) * F::KVEC);
-      if constexpr (KT == KV_E4M3) {
-        const uint8_t* e = a.c.k_exp + at[i] + 2 * t;
-        R.ke[i] = *reinterpret_cast<const uint16_t*>(e) | (uint32_t) * reinterpret_cast<const uint16_t*>(e + 8) << 16;
-      }
-    }
-  };
-  auto load_v = [&]() {
-#pragma unroll
-    for (int i = 0; i < F::NB; ++i) {
-      if (at[i] < 0) continue;
-#pragma unroll
-      for (int k = 0; k < 4; ++k)
-#pragma unroll
-        for (int c = 0; c < F::VN; ++c)
-          R.v[i][k][c] = ldg<F::VVEC>((const char*)a.c.v + ((size_t)at[i] + 2 * t + (k & 1) + (k >> 1) * 8) * (DH * F::ES) +
-                                      (c * 8 + g) * F::VVEC);
-      if constexpr (KT == KV_E4M3) {
-        const uint8_t* e = a.c.v_exp + at[i] + 2 * t;
-        R.ve[i] = *reinterpret_cast<const uint16_t*>(e) | (uint32_t) * reinterpret_cast<const uint16_t*>(e + 8) << 16;
-      }
-    }
-  };
-  // (words of blocks that are not there are never read into sums: zero from the start)
-#pragma unroll
-  for (int i = 0; i < F::NB; ++i) {
-#pragma unroll
-    for (int x = 0; x < 2 * F::KN; ++x)
-#pragma unroll
-      for (int w = 0; w < F::KVEC / 4; ++w) R.k[i][x / F::KN][x % F::KN].w[w] = 0;
-#pragma unroll
-    for (int x = 0; x < 4 * F::VN; ++x)
-#pragma unroll
-      for (int w = 0; w < F::VVEC / 4; ++w) R.v[i][x / F::VN][x % F::VN].w[w] = 0;
-    R.ke[i] = R.ve[i] = 0;
-  }
-
-  if (first < b_end) {
-    blocks_of(first);
-    load_k();
-    load_v();
-  }
-  for (int b = first; b < b_end; b += STEP) {
+  bool ok = true;
+  unsigned cf_phase = 0;   // bit s: parity of stage s's next copy
+  for (int i0 = 0; i0 < n_blk; i0 += F::NB) {
+    const int b = first + i0 / F::NB * STEP;
     bool here[F::NB], edge = false;   // edge: some key of the round is not everyone's
+    const uint8_t* st[F::NB];
 #pragma unroll
     for (int i = 0; i < F::NB; ++i) {
-      here[i] = at[i] >= 0;
+      const int x = i0 + i, sg = x % F::STAGES;
+      here[i] = there >> (x % 32) & 1;
       edge |= !here[i];
+      st[i] = ring + sg * F::STAGE;
+      if (here[i] && ok && (ok = cf_wait(&s_full[warp][sg], cf_phase >> sg & 1u, &s_abort, err, wlim))) cf_phase ^= 1u << sg;
+      landed += ok;
+    }
+    if (!__all_sync(0xffffffffu, ok)) {
+      ok = false;
+      break;
     }
     edge |= (b + F::NB) * 16 > lim_lo || (b + F::NB) * 16 > k_end;
     // S = Q K^T
@@ -380,32 +438,28 @@ __global__ void __launch_bounds__(CF_WARPS * 32, 2) chunk_few_kernel(const __gri
       for (int nt = 0; nt < 2; ++nt) {
         float(&d)[4] = s[2 * i + nt];
         d[0] = d[1] = d[2] = d[3] = 0.f;
+        Words<F::KVEC> k[F::KN];
+#pragma unroll
+        for (int c = 0; c < F::KN; ++c) k[c] = lds<F::KVEC>(st[i] + (nt * 8 + g) * (DH * F::ES) + (c * 4 + t) * F::KVEC);
 #pragma unroll
         for (int c = 0; c < F::KN; ++c)
 #pragma unroll
           for (int w = 0; w < F::KE / 4; ++w) {
             const int ks = c * (F::KE / 4) + w;
-            if constexpr (KT == KV_BF16) {
-              mma16816(d, qf[ks], R.k[i][nt][c].w[2 * w], R.k[i][nt][c].w[2 * w + 1]);
-            } else {
-              const uint32_t x = R.k[i][nt][c].w[w];
-              mma16816(d, qf[ks], e4m3x2_bf16x2(x & 0xffffu), e4m3x2_bf16x2(x >> 16));
-            }
+            if constexpr (KT == KV_BF16)
+              mma16816<false>(d, qf[ks], k[c].w[2 * w], k[c].w[2 * w + 1]);
+            else
+              mma16816<true>(d, qf[ks], e4m3x2_f16x2(k[c].w[w] & 0xffffu), e4m3x2_f16x2(k[c].w[w] >> 16));
           }
         if constexpr (KT == KV_E4M3) {
-          const float e0 = exp_scale((R.ke[i] >> (nt * 16)) & 0xff) * a.scale_log2;
-          const float e1 = exp_scale((R.ke[i] >> (nt * 16 + 8)) & 0xff) * a.scale_log2;
-          d[0] *= e0; d[1] *= e1; d[2] *= e0; d[3] *= e1;
+          const uint32_t e = *reinterpret_cast<const uint16_t*>(st[i] + 2 * F::BLOCK + nt * 8 + 2 * t);
+          const float e0 = exp_scale(e & 0xff), e1 = exp_scale(e >> 8);
+          d[0] *= e0 * rs[0]; d[1] *= e1 * rs[0]; d[2] *= e0 * rs[1]; d[3] *= e1 * rs[1];
         } else {
 #pragma unroll
-          for (int e = 0; e < 4; ++e) d[e] *= a.scale_log2;
+          for (int e = 0; e < 4; ++e) d[e] *= rs[0];
         }
       }
-    const bool more = b + STEP < b_end;
-    if (more) {
-      blocks_of(b + STEP);
-      load_k();
-    }
     unsigned att = ~0u;   // bit (tile, element): the row attends the key
     if (edge) {
       att = 0;
@@ -461,8 +515,9 @@ __global__ void __launch_bounds__(CF_WARPS * 32, 2) chunk_few_kernel(const __gri
     for (int i = 0; i < F::NB; ++i) {
       uint32_t pf[4];
       if constexpr (KT == KV_E4M3) {
-        const float e0 = exp_scale(R.ve[i] & 0xff), e1 = exp_scale((R.ve[i] >> 8) & 0xff);
-        const float e2 = exp_scale((R.ve[i] >> 16) & 0xff), e3 = exp_scale(R.ve[i] >> 24);
+        const uint8_t* ve = st[i] + 2 * F::BLOCK + 16 + 2 * t;
+        const uint32_t x = *reinterpret_cast<const uint16_t*>(ve), y = *reinterpret_cast<const uint16_t*>(ve + 8);
+        const float e0 = exp_scale(x & 0xff), e1 = exp_scale(x >> 8), e2 = exp_scale(y & 0xff), e3 = exp_scale(y >> 8);
         pf[0] = pack_bf16(s[2 * i][0] * e0, s[2 * i][1] * e1);
         pf[1] = pack_bf16(s[2 * i][2] * e0, s[2 * i][3] * e1);
         pf[2] = pack_bf16(s[2 * i + 1][0] * e2, s[2 * i + 1][1] * e3);
@@ -473,80 +528,76 @@ __global__ void __launch_bounds__(CF_WARPS * 32, 2) chunk_few_kernel(const __gri
         pf[2] = pack_bf16(s[2 * i + 1][0], s[2 * i + 1][1]);
         pf[3] = pack_bf16(s[2 * i + 1][2], s[2 * i + 1][3]);
       }
-      bool poison = false;
-      if (edge) {
-        // V of keys that nobody here attends counts as zero; a NaN or infinite one that only some rows attend must
-        // not reach the others through 0 * NaN: it counts as zero and is put into the sums of its rows as NaN
+      const uint8_t* vb = st[i] + F::BLOCK + g * F::VVEC;
+      auto row = [&](int k, int c) { return lds<F::VVEC>(vb + (2 * t + (k & 1) + (k >> 1) * 8) * (DH * F::ES) + c * 8 * F::VVEC); };
+      if (!edge) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const int key = (b + i) * 16 + 2 * t + (k & 1) + (k >> 1) * 8;
-          const bool off = !here[i] || key >= k_end;
+        for (int c = 0; c < F::VN; ++c) {
+          const Words<F::VVEC> v0 = row(0, c), v1 = row(1, c), v2 = row(2, c), v3 = row(3, c);
 #pragma unroll
-          for (int c = 0; c < F::VN; ++c)
-#pragma unroll
-            for (int w = 0; w < F::VVEC / 4; ++w) {
-              uint32_t& x = R.v[i][k][c].w[w];
-              if (off) x = 0;
-              if constexpr (KT == KV_BF16)
-                poison |= __vcmpeq2(x & 0x7f807f80u, 0x7f807f80u) != 0;
-              else
-                poison |= __vcmpeq4(x & 0x7f7f7f7fu, 0x7f7f7f7fu) != 0;
-            }
-        }
-        if constexpr (KT == KV_E4M3) {
-          // (an exponent of such a key must not make its weight of 0 a NaN)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const unsigned lo = att >> (2 * i * 4 + (e & 1) * 2 + (e >> 1) * 4);
-            if (!(lo & 1u)) pf[e] &= 0xffff0000u;
-            if (!(lo & 2u)) pf[e] &= 0x0000ffffu;
+          for (int w = 0; w < F::VVEC / 4; ++w) {
+            cf_pairs<KT>(v0.w[w], v1.w[w], v2.w[w], v3.w[w], [&](int e, uint32_t b0, uint32_t b1) {
+              mma16816<false>(o[c * F::VE + w * (4 / F::ES) + e], pf, b0, b1);
+            });
           }
         }
-        poison = __any_sync(0xffffffffu, poison);
+        continue;
       }
+      // V of keys that nobody here attends counts as zero; a NaN or infinite one that only some rows attend must not reach
+      // the others through 0 * NaN: it counts as zero, and is put into the sums of its rows as NaN
       uint32_t ones[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e) {   // fragment e: row half e & 1, key tile e >> 1
         const unsigned bits = att >> ((2 * i + (e >> 1)) * 4 + (e & 1) * 2);
         ones[e] = (bits & 1u ? 0x3f80u : 0u) | (bits & 2u ? 0x3f800000u : 0u);
+        pf[e] &= (bits & 1u ? 0xffffu : 0u) | (bits & 2u ? 0xffff0000u : 0u);   // (an exponent of no entry may be anything)
       }
-      auto pv = [&](int j, uint32_t b0, uint32_t b1) {
-        if (!poison) {
-          mma16816(o[j], pf, b0, b1);
-          return;
+#pragma unroll
+      for (int c = 0; c < F::VN; ++c) {
+        Words<F::VVEC> v[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          v[k] = row(k, c);
+          if (!here[i] || (b + i) * 16 + 2 * t + (k & 1) + (k >> 1) * 8 >= k_end)
+#pragma unroll
+            for (int w = 0; w < F::VVEC / 4; ++w) v[k].w[w] = 0;
         }
-        const uint32_t n0 = __vcmpeq2(b0 & 0x7f807f80u, 0x7f807f80u), n1 = __vcmpeq2(b1 & 0x7f807f80u, 0x7f807f80u);
-        mma16816(o[j], pf, b0 & ~n0, b1 & ~n1);
-        float cnt[4] = {0.f, 0.f, 0.f, 0.f};
-        mma16816(cnt, ones, n0 & 0x3f803f80u, n1 & 0x3f803f80u);
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (cnt[e] > 0.f) o[j][e] = NAN;
-      };
+        for (int w = 0; w < F::VVEC / 4; ++w)
+          cf_pairs<KT>(v[0].w[w], v[1].w[w], v[2].w[w], v[3].w[w], [&](int e, uint32_t b0, uint32_t b1) {
+            float(&d)[4] = o[c * F::VE + w * (4 / F::ES) + e];
+            const uint32_t n0 = __vcmpeq2(b0 & 0x7f807f80u, 0x7f807f80u), n1 = __vcmpeq2(b1 & 0x7f807f80u, 0x7f807f80u);
+            mma16816<false>(d, pf, b0 & ~n0, b1 & ~n1);
+            if (__any_sync(0xffffffffu, (n0 | n1) != 0)) {
+              float cnt[4] = {0.f, 0.f, 0.f, 0.f};
+              mma16816<false>(cnt, ones, n0 & 0x3f803f80u, n1 & 0x3f803f80u);
 #pragma unroll
-      for (int c = 0; c < F::VN; ++c)
-#pragma unroll
-        for (int w = 0; w < F::VVEC / 4; ++w) {
-          const uint32_t k0 = R.v[i][0][c].w[w], k1 = R.v[i][1][c].w[w], k2 = R.v[i][2][c].w[w], k3 = R.v[i][3][c].w[w];
-          if constexpr (KT == KV_BF16) {
-            const int j = c * F::VE + 2 * w;
-            pv(j, __byte_perm(k0, k1, 0x5410), __byte_perm(k2, k3, 0x5410));
-            pv(j + 1, __byte_perm(k0, k1, 0x7632), __byte_perm(k2, k3, 0x7632));
-          } else {
-            const int j = c * F::VE + 4 * w;
-            const uint32_t x0 = __byte_perm(k0, k1, 0x5140), x1 = __byte_perm(k2, k3, 0x5140);
-            const uint32_t y0 = __byte_perm(k0, k1, 0x7362), y1 = __byte_perm(k2, k3, 0x7362);
-            pv(j, e4m3x2_bf16x2(x0 & 0xffffu), e4m3x2_bf16x2(x1 & 0xffffu));
-            pv(j + 1, e4m3x2_bf16x2(x0 >> 16), e4m3x2_bf16x2(x1 >> 16));
-            pv(j + 2, e4m3x2_bf16x2(y0 & 0xffffu), e4m3x2_bf16x2(y1 & 0xffffu));
-            pv(j + 3, e4m3x2_bf16x2(y0 >> 16), e4m3x2_bf16x2(y1 >> 16));
-          }
-        }
+              for (int x = 0; x < 4; ++x)
+                if (cnt[x] > 0.f) d[x] = NAN;
+            }
+          });
+      }
     }
-    if (more) load_v();
+    __syncwarp();   // everybody has read the round's stages
+#pragma unroll
+    for (int i = 0; i < F::NB; ++i)
+      if (sent < n_blk) send();
   }
+  if (!ok) {   // a copy did not land in time: what is sent lands before the CTA leaves
+    s_abort = 1;
+    if (lane == 0)
+      for (int i = landed; i < sent; ++i) {
+        const long long c0 = clock64();
+        while ((there >> (i % 32) & 1) && !mbar_try_wait(&s_full[warp][i % F::STAGES], cf_phase >> (i % F::STAGES) & 1u) &&
+               clock64() - c0 < CF_DRAIN_CYCLES) {
+        }
+      }
+    __syncwarp();
+  }
+  __syncthreads();   // the rings' place is free
 
   // merge of the warps, in warp order
+  float* s_o = reinterpret_cast<float*>(s_dyn);
 #pragma unroll
   for (int r = 0; r < 2; ++r) {
     l[r] += __shfl_xor_sync(0xffffffffu, l[r], 1);
@@ -562,7 +613,8 @@ __global__ void __launch_bounds__(CF_WARPS * 32, 2) chunk_few_kernel(const __gri
     const int c = j / F::VE, e = j % F::VE;
 #pragma unroll
     for (int x = 0; x < 4; ++x)
-      s_o[(warp * CF_ROWS + g + 8 * (x >> 1)) * LD + (c * 8 + 2 * t + (x & 1)) * F::VE + e] = o[j][x];
+      if (g + 8 * (x >> 1) < n_row)
+        s_o[(warp * CF_ROWS + g + 8 * (x >> 1)) * LD + (c * 8 + 2 * t + (x & 1)) * F::VE + e] = o[j][x];
   }
   __syncthreads();
   const PartView pv(a, p, CF_ROWS, DH, it.slot0 + it.split);
@@ -675,7 +727,7 @@ ChunkHow chunk_how(const KvPaged& c, int n_heads, int max_q, int max_kv, bool al
     w.rows = CF_ROWS;
     w.per_tok = std::min(group, CF_ROWS);
     w.sub = cdiv(group, w.per_tok);
-    w.p = SplitPlan{CF_ROWS / w.per_tok, c.n_kv_heads * w.sub, CF_WARPS * 16 * (c.type == KV_BF16 ? 1 : 2), chunk_sms() * 2};
+    w.p = SplitPlan{CF_ROWS / w.per_tok, c.n_kv_heads * w.sub, CF_WARPS * 16 * (c.type == KV_BF16 ? 1 : 2), chunk_sms() * 3};
   } else {
     w.kind = CHUNK_ANY;
     w.rows = CG_ROWS;
@@ -699,7 +751,9 @@ cudaError_t chunk_t(cudaStream_t st, const ChunkCall& a, const ChunkHow& w, int*
   if (w.kind == CHUNK_ANY) {
     e = launch_k(chunk_any_kernel<DH, KT, T>, grid, dim3(CG_KEYS), 0, st, a, w.p);
   } else if constexpr (KT != KV_F32) {
-    e = launch_k(chunk_few_kernel<DH, KT>, grid, dim3(CF_WARPS * 32), FewShape<DH, KT>::SMEM, st, a, w.p, w.per_tok, w.sub);
+    constexpr int smem = FewShape<DH, KT>::SMEM;
+    e = cudaFuncSetAttribute(chunk_few_kernel<DH, KT>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e == cudaSuccess) e = launch_k(chunk_few_kernel<DH, KT>, grid, dim3(CF_WARPS * 32), smem, st, a, w.p, w.per_tok, w.sub);
   }
   if (e == cudaSuccess && w.may_split) {
     *launches = 2;
@@ -733,5 +787,7 @@ cudaError_t launch_chunk_attention(cudaStream_t st, const ChunkCall& a, int* lau
 #undef CH_DH
   return cudaErrorInvalidValue;
 }
+
+ADEPT_WAIT_LIMIT_SETTER(cf)
 
 }  // namespace adept

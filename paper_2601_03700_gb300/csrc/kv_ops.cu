@@ -36,6 +36,8 @@ adept_status view_of(const adept_kv_cache* c, KvPaged* v) {
   if (((uintptr_t)c->d_k | (uintptr_t)c->d_v) & 15) return bad(ADEPT_ERR_INVALID_ARG, "K and V must start on 16 bytes");
   if (c->kv_type == ADEPT_KV_E4M3 && (!c->d_k_exp || !c->d_v_exp))
     return bad(ADEPT_ERR_INVALID_ARG, "an e4m3 cache needs its exponents");
+  if (c->kv_type == ADEPT_KV_E4M3 && (((uintptr_t)c->d_k_exp | (uintptr_t)c->d_v_exp) & 15))
+    return bad(ADEPT_ERR_INVALID_ARG, "the exponents must start on 16 bytes");
   *v = KvPaged{c->d_k, c->d_v, c->d_k_exp, c->d_v_exp, c->d_block_table, c->d_err, c->kv_type, c->n_blocks, c->n_kv_heads,
                c->head_dim, c->block_tokens, c->n_seq, c->max_blocks_per_seq};
   return ADEPT_OK;

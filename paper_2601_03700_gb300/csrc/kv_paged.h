@@ -50,6 +50,7 @@ bool chunk_tc_takes(const KvPaged& c, int n_heads);
 size_t chunk_tc_workspace(const KvPaged& c);
 cudaError_t launch_chunk_tc(cudaStream_t st, const ChunkCall& a, int* launches);
 cudaError_t set_wait_limit_ct(long long cycles);
+cudaError_t set_wait_limit_cf(long long cycles);
 
 // ---------------------------------------------------------------------------------------------
 // Work split.  A tile is up to tq new tokens of one sequence (all query heads of a group of one KV head); its keys are

@@ -2091,7 +2091,7 @@ adept_status adept_set_wait_limit(int64_t cycles) {
   if (cycles < 0) return fail(nullptr, ADEPT_ERR_INVALID_ARG, "wait limit %lld < 0", (long long)cycles);
   const long long v = cycles == 0 ? WAIT_LIMIT_DEFAULT : (long long)cycles;
   for (cudaError_t e : {set_wait_limit_tc(v), set_wait_limit_dg(v), set_wait_limit_ds(v), set_wait_limit_sw(v),
-                        set_wait_limit_pg(v), set_wait_limit_ct(v)})
+                        set_wait_limit_pg(v), set_wait_limit_ct(v), set_wait_limit_cf(v)})
     if (e != cudaSuccess) return fail(nullptr, ADEPT_ERR_CUDA, "setting the wait limit: %s", cudaGetErrorString(e));
   return ADEPT_OK;
 }
