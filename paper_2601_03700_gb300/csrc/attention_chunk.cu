@@ -648,15 +648,39 @@ __global__ void __launch_bounds__(CF_WARPS * 32, 3) chunk_few_kernel(const __gri
 }
 
 // ---------------------------------------------------------------------------------------------
-// Join of split tiles: CTA = one tile; per row the splits' partials in split order.
+// Join of split tiles: CTA = one tile; per row the splits' partials, taken in turn by as many groups of threads as the tile's
+// live elements leave room for, the groups joined in order at the end.
 //   M = max m_i,  out = sum_i 2^(m_i - M) O_i / sum_i 2^(m_i - M) l_i
+// Four partials' loads are under way at a time: with one at a time a join of 14 took 9 us, most of it memory latency.
 // ---------------------------------------------------------------------------------------------
+constexpr int CJ_THREADS = 256;
+struct JoinAcc {
+  float m, l, o[4];
+  __device__ __forceinline__ void add(const float (&mi)[4], const float (&li)[4], const float4 (&oi)[4]) {
+    const float mn = fmaxf(fmaxf(fmaxf(mi[0], mi[1]), fmaxf(mi[2], mi[3])), m), ref = mn == -INFINITY ? 0.f : mn;
+    const float f = ex2_approx(m - ref);   // (nothing yet, or a split without keys: 2^-inf = 0)
+    m = mn;
+    l *= f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] *= f;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const float w = ex2_approx(mi[k] - ref);
+      l += w * li[k];
+      o[0] += w * oi[k].x;
+      o[1] += w * oi[k].y;
+      o[2] += w * oi[k].z;
+      o[3] += w * oi[k].w;
+    }
+  }
+};
 template <int DH, typename T>
-__global__ void __launch_bounds__(128) chunk_join_kernel(const __grid_constant__ ChunkCall a, const __grid_constant__ SplitPlan p,
-                                                         int rows, int per_tok, int sub) {
+__global__ void __launch_bounds__(CJ_THREADS) chunk_join_kernel(const __grid_constant__ ChunkCall a,
+                                                                const __grid_constant__ SplitPlan p, int rows, int per_tok, int sub) {
   // rows: of a tile; per_tok: query heads of a tile's token; sub: tiles' head groups per KV head
   __shared__ SplitItem s_it;
   __shared__ int s_have;
+  __shared__ float s_acc[6][CJ_THREADS];
   PDL_ENTRY();
   const int tid = threadIdx.x;
   if (tid < 32) {
@@ -673,27 +697,57 @@ __global__ void __launch_bounds__(128) chunk_join_kernel(const __grid_constant__
   const int group = a.n_heads / a.c.n_kv_heads;
   const int past = it.len - it.c, j0 = it.tile * p.tq, n = min(p.tq, it.c - j0);
   const PartView pv(a, p, rows, DH, it.slot0);
-  for (int i = tid; i < n * per_tok * (DH / 4); i += 128) {
+  const int live = n * per_tok * (DH / 4);                       // elements of four columns
+  const int groups = max(1, min(CJ_THREADS / live, (it.n_split + 3) / 4));
+  const int gr = live < CJ_THREADS ? tid / live : 0;
+  for (int i = live < CJ_THREADS ? tid % live : tid; i < live; i += CJ_THREADS) {
     const int r = i / (DH / 4), d = i % (DH / 4) * 4, j = r / per_tok, g = it.group % sub * per_tok + r % per_tok;
-    if (g >= group) continue;
-    const int h = it.group / sub * group + g;
-    float M = -INFINITY;
-    for (int s = 0; s < it.n_split; ++s) M = fmaxf(M, __ldcg(pv.ml + ((size_t)s * rows + r) * 2));
-    float L = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
-    const float ref = M == -INFINITY ? 0.f : M;
-    for (int s = 0; s < it.n_split; ++s) {
-      const float2 ml = __ldcg(reinterpret_cast<const float2*>(pv.ml + ((size_t)s * rows + r) * 2));
-      const float4 x = __ldcg(reinterpret_cast<const float4*>(pv.o + ((size_t)s * rows + r) * DH + d));
-      const float w = exp2f(ml.x - ref);   // (a split without keys: 2^-inf = 0)
-      L += w * ml.y;
-      o[0] += w * x.x;
-      o[1] += w * x.y;
-      o[2] += w * x.z;
-      o[3] += w * x.w;
+    JoinAcc x{-INFINITY, 0.f, {0.f, 0.f, 0.f, 0.f}};
+    if (gr < groups) {
+      for (int s0 = gr * 4; s0 < it.n_split; s0 += groups * 4) {
+        float m[4], l[4];
+        float4 o[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          m[k] = -INFINITY;
+          l[k] = 0.f;
+          o[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+          if (s0 + k < it.n_split) {
+            const float2 ml = __ldcg(reinterpret_cast<const float2*>(pv.ml + ((size_t)(s0 + k) * rows + r) * 2));
+            m[k] = ml.x;
+            l[k] = ml.y;
+            o[k] = __ldcg(reinterpret_cast<const float4*>(pv.o + ((size_t)(s0 + k) * rows + r) * DH + d));
+          }
+        }
+        x.add(m, l, o);
+      }
     }
+    if (groups > 1) {   // (live < CJ_THREADS: every thread is here once)
+      s_acc[0][tid] = x.m;
+      s_acc[1][tid] = x.l;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s_acc[2 + e][tid] = x.o[e];
+      __syncthreads();
+      if (gr > 0) return;
+      for (int k0 = 1; k0 < groups; k0 += 4) {
+        float m[4], l[4];
+        float4 o[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const int at = (k0 + k) * live + i;
+          const bool on = k0 + k < groups;
+          m[k] = on ? s_acc[0][at] : -INFINITY;
+          l[k] = on ? s_acc[1][at] : 0.f;
+          o[k] = on ? make_float4(s_acc[2][at], s_acc[3][at], s_acc[4][at], s_acc[5][at]) : make_float4(0.f, 0.f, 0.f, 0.f);
+        }
+        x.add(m, l, o);
+      }
+    }
+    if (gr > 0 || g >= group) continue;
+    const int h = it.group / sub * group + g;
     T* dst = (T*)a.out + (size_t)(it.q0 + j0 + j) * a.ld_out + (size_t)h * DH + d;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) dst[e] = from_f<T>(past + j0 + j < 0 ? 0.f : o[e] / L);
+    for (int e = 0; e < 4; ++e) dst[e] = from_f<T>(past + j0 + j < 0 ? 0.f : x.o[e] / x.l);
   }
 }
 
@@ -757,7 +811,7 @@ cudaError_t chunk_t(cudaStream_t st, const ChunkCall& a, const ChunkHow& w, int*
   }
   if (e == cudaSuccess && w.may_split) {
     *launches = 2;
-    e = launch_k(chunk_join_kernel<DH, T>, dim3((unsigned)w.p.target), dim3(128), 0, st, a, w.p, w.rows, w.per_tok, w.sub);
+    e = launch_k(chunk_join_kernel<DH, T>, dim3((unsigned)w.p.target), dim3(CJ_THREADS), 0, st, a, w.p, w.rows, w.per_tok, w.sub);
   }
   return e;
 }
