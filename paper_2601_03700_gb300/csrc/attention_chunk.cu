@@ -343,7 +343,7 @@ __global__ void __launch_bounds__(CF_WARPS * 32, 3) chunk_few_kernel(const __gri
     }
     const int blk = __shfl_sync(0xffffffffu, tab, i % 32);
     there = blk >= 0 ? there | 1u << (i % 32) : there & ~(1u << (i % 32));
-    if (blk >= 0 && lane == 0) {
+    if (blk >= 0 && elect_one()) {
       uint8_t* st = ring + i % F::STAGES * F::STAGE;
       uint64_t* bar = &s_full[warp][i % F::STAGES];
       const size_t e = ((size_t)blk * a.c.n_kv_heads + kvh) * 16;
@@ -355,12 +355,9 @@ __global__ void __launch_bounds__(CF_WARPS * 32, 3) chunk_few_kernel(const __gri
         bulk_load(st + 2 * F::BLOCK + 16, a.c.v_exp + e, 16, bar);
       }
     }
+    __syncwarp();
     ++sent;
   };
-  // blocks of this warp (whole rounds; those past b_end are not there)
-  const int n_blk = first < b_end ? (b_end - first + STEP - 1) / STEP * F::NB : 0;
-  for (int i = 0; i < F::STAGES && i < n_blk; ++i) send();
-
   // ---- this thread's two rows (g, g + 8): Q fragments, and the keys each attends
   uint32_t qf[KS][4];
   int lim[2];
@@ -381,7 +378,14 @@ __global__ void __launch_bounds__(CF_WARPS * 32, 3) chunk_few_kernel(const __gri
       qf[s][r2] = x.x;
       qf[s][2 + r2] = x.y;
     }
-    if constexpr (F16) {
+  }
+  // blocks of this warp (whole rounds; those past b_end are not there)
+  const int n_blk = first < b_end ? (b_end - first + STEP - 1) / STEP * F::NB : 0;
+  for (int i = 0; i < F::STAGES && i < n_blk; ++i) send();
+
+  if constexpr (F16) {
+#pragma unroll
+    for (int r2 = 0; r2 < 2; ++r2) {
       unsigned top = 0;   // exponent field of the row's largest finite element
 #pragma unroll
       for (int s = 0; s < KS; ++s)
@@ -394,7 +398,7 @@ __global__ void __launch_bounds__(CF_WARPS * 32, 3) chunk_few_kernel(const __gri
       top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
       const int e = max((int)top, 15);                                      // (rows below 2^-112 keep fewer bits)
       const float up = __uint_as_float((unsigned)(127 + 14 + 127 - e) << 23);   // 2^(14 - (e - 127))
-      rs[r2] = a.scale_log2 * __uint_as_float((unsigned)(e < 15 ? 1 : e - 14) << 23);   // 2^((e - 127) - 14)
+      rs[r2] = a.scale_log2 * __uint_as_float((unsigned)(e - 14) << 23);   // 2^((e - 127) - 14)
 #pragma unroll
       for (int s = 0; s < KS; ++s)
 #pragma unroll

@@ -83,29 +83,31 @@ __device__ __forceinline__ void chunk_seq(const ChunkCall& a, int b, int& q0, in
   }
 }
 
-// Item `id` of the plan (joined: tile `id`, its splits taken together), looked up by one converged warp; false: none.
+// Item `id` of the plan (joined: tile `id`, its splits taken together), looked up by one converged warp; false: none.  32-bit
+// sums by one instruction each: in 64 bits, with shuffles, the look-up took 4000 cycles of a call of 15000.
 __device__ __forceinline__ bool split_find(const ChunkCall& a, const SplitPlan& p, int id, bool joined, SplitItem& it) {
   const int lane = threadIdx.x & 31, n_seq = a.c.n_seq;
-  long long base = 0, tot = 0;
+  unsigned base = 0, tot = 0;
+  bool huge = false;   // more units than the sum holds: no split
   int q0 = 0, c = 0, len = 0;
   for (int b0 = 0; b0 < n_seq; b0 += 32) {
     const int b = b0 + lane;
     q0 = c = len = 0;
     if (b < n_seq) chunk_seq(a, b, q0, c, len);
-    const long long t = (long long)((c + p.tq - 1) / p.tq) * p.groups;
+    const unsigned t = (unsigned)((c + p.tq - 1) / p.tq) * p.groups;
+    const unsigned long long w = (unsigned long long)t * ((len + p.unit - 1) / p.unit);
     base += t;
-    tot += t * ((len + p.unit - 1) / p.unit);
+    huge |= w + tot >= 1u << 26;
+    tot += (unsigned)w;
   }
-#pragma unroll
-  for (int o = 16; o; o >>= 1) {
-    base += __shfl_xor_sync(0xffffffffu, base, o);
-    tot += __shfl_xor_sync(0xffffffffu, tot, o);
-  }
+  base = __reduce_add_sync(0xffffffffu, min(base, 1u << 26));
+  tot = __reduce_add_sync(0xffffffffu, tot);
+  huge = __any_sync(0xffffffffu, huge) != 0;
   // run length S: sum over tiles of ceil(units / S) <= tot / S + base <= target
-  long long S = 1ll << 40;
-  if (base < p.target) S = max(1ll, (tot + (p.target - base) - 1) / (p.target - base));
-  long long before = 0;
-  long long slots = 0;
+  unsigned S = 1u << 30;
+  const unsigned target = (unsigned)p.target;
+  if (base < target && !huge) S = max(1u, (tot + (target - base) - 1) / (target - base));
+  int before = 0, slots = 0;   // of the sequences before these 32
   for (int b0 = 0; b0 < n_seq; b0 += 32) {
     const int b = b0 + lane;
     if (n_seq > 32) {
@@ -113,49 +115,49 @@ __device__ __forceinline__ bool split_find(const ChunkCall& a, const SplitPlan& 
       if (b < n_seq) chunk_seq(a, b, q0, c, len);
     }
     const int tiles = (c + p.tq - 1) / p.tq, units = (len + p.unit - 1) / p.unit;
-    int ns = (int)min((long long)units, (units + S - 1) / S);
-    ns = max(ns, 1);
-    const long long n_it = (long long)tiles * p.groups * ns, mine = joined ? (long long)tiles * p.groups : n_it;
-    long long inc = mine, sl = n_it;
+    const int ns = max((int)(((unsigned)units + S - 1) / S), 1);
+    const int n_it = tiles * p.groups * ns, mine = joined ? tiles * p.groups : n_it;
+    int inc = mine, sl = n_it;
+    if (n_seq > 1) {
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const long long u = __shfl_up_sync(0xffffffffu, inc, o), w = __shfl_up_sync(0xffffffffu, sl, o);
-      if (lane >= o) {
-        inc += u;
-        sl += w;
+      for (int o = 1; o < 32; o <<= 1) {
+        const int u = __shfl_up_sync(0xffffffffu, inc, o), w = __shfl_up_sync(0xffffffffu, sl, o);
+        if (lane >= o) {
+          inc += u;
+          sl += w;
+        }
       }
     }
-    const long long lo = before + inc - mine;
-    const bool hit = id >= lo && id < lo + mine;
-    const unsigned who = __ballot_sync(0xffffffffu, hit);
+    const int lo = before + inc - mine;
+    const unsigned who = __ballot_sync(0xffffffffu, id >= lo && id < lo + mine);
     if (who) {
       const int src = __ffs(who) - 1;
-      const long long s0 = slots + sl - n_it;
-      const int lo_ = __shfl_sync(0xffffffffu, (int)lo, src), s0_ = __shfl_sync(0xffffffffu, (int)s0, src);
+      const int s0 = __shfl_sync(0xffffffffu, slots + sl - n_it, src);
+      int r = id - __shfl_sync(0xffffffffu, lo, src);
       it.seq = b0 + src;
       it.q0 = __shfl_sync(0xffffffffu, q0, src);
       it.c = __shfl_sync(0xffffffffu, c, src);
       it.len = __shfl_sync(0xffffffffu, len, src);
       it.n_split = __shfl_sync(0xffffffffu, ns, src);
       const int un = __shfl_sync(0xffffffffu, units, src), nt = __shfl_sync(0xffffffffu, tiles, src);
-      int r = id - lo_;
       it.split = 0;
       if (!joined) {
-        it.split = r % it.n_split;
-        r /= it.n_split;
+        const int k = r / it.n_split;
+        it.split = r - k * it.n_split;
+        r = k;
       }
       // the last tiles (the longest) come first, all head groups of one together
-      const int tg = r;
-      it.group = r % p.groups;
-      it.tile = nt - 1 - r / p.groups;
-      it.slot0 = s0_ + tg * it.n_split;
+      const int back = r / p.groups;
+      it.group = r - back * p.groups;
+      it.tile = nt - 1 - back;
+      it.slot0 = s0 + r * it.n_split;
       const int per = (un + it.n_split - 1) / it.n_split;
       it.u0 = min(un, it.split * per);
       it.u1 = min(un, it.u0 + per);
       return true;
     }
-    before += __shfl_sync(0xffffffffu, inc, 31);
-    slots += __shfl_sync(0xffffffffu, sl, 31);
+    before += __shfl_sync(0xffffffffu, inc, n_seq > 1 ? 31 : 0);
+    slots += __shfl_sync(0xffffffffu, sl, n_seq > 1 ? 31 : 0);
   }
   return false;
 }

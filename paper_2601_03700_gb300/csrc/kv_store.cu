@@ -6,54 +6,73 @@
 // or fp32 is exact (4 significant bits).  A scale of 24 bits would gain nothing: e4m3's relative step does not depend on the
 // scale.  NaN stays NaN; e4m3 has no infinity, an infinite element is stored as NaN.
 //
-// Bound by HBM: each element is read once and written once.  A vector (head_dim elements of K or of V) is held by
-// head_dim / 8 threads, 8 elements each.
+// Bound by HBM: each element is read once and written once.  A thread holds 16 elements of a vector (head_dim elements of K or of
+// V of one position), KS_ITEMS vectors at a time with every load issued before the first is used; a CTA takes whole rows, so
+// a row's place in the cache is looked up by neighbours together.
 #include "kv_paged.h"
 
 #include <cuda_fp8.h>
 
+#include <type_traits>
+
 namespace adept {
 namespace {
 
-constexpr int KS_THREADS = 256;
+constexpr int KS_THREADS = 256, KS_ITEMS = 4, KS_EL = 16;
 
-template <typename T, bool VEC>
-__device__ __forceinline__ void load8(const T* p, float (&x)[8]) {
-  if constexpr (VEC && sizeof(T) == 2) {
-    const uint4 w = *reinterpret_cast<const uint4*>(p);
-    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+// 16 elements as they lie in memory (VEC: by 16 bytes), and as fp32.
+template <typename T>
+struct Piece {
+  uint32_t w[KS_EL * sizeof(T) / 4];
+  __device__ __forceinline__ void f32(float (&x)[KS_EL]) const {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      x[2 * i] = __uint_as_float(u[i] << 16);
-      x[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
+    for (int i = 0; i < KS_EL; ++i) {
+      if constexpr (sizeof(T) == 2)
+        x[i] = __uint_as_float(i & 1 ? w[i >> 1] & 0xffff0000u : w[i >> 1] << 16);
+      else
+        x[i] = __uint_as_float(w[i]);
     }
-  } else if constexpr (VEC) {
-    const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
-    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
-    x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = to_f<T>(p[i]);
   }
-}
-template <typename T, bool VEC>
-__device__ __forceinline__ void store8(T* p, const float (&x)[8]) {
-  if constexpr (VEC && sizeof(T) == 2) {
-    uint32_t u[4];
+  __device__ __forceinline__ void from(const float (&x)[KS_EL]) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const __nv_bfloat162 h = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
-      u[i] = *reinterpret_cast<const uint32_t*>(&h);
+    for (int i = 0; i < KS_EL; ++i) {
+      if constexpr (sizeof(T) == 2) {
+        const __nv_bfloat162 h = __floats2bfloat162_rn(x[i & ~1], x[i | 1]);
+        w[i >> 1] = *reinterpret_cast<const uint32_t*>(&h);
+      } else {
+        w[i] = __float_as_uint(x[i]);
+      }
     }
-    *reinterpret_cast<uint4*>(p) = make_uint4(u[0], u[1], u[2], u[3]);
-  } else if constexpr (VEC) {
-    reinterpret_cast<float4*>(p)[0] = make_float4(x[0], x[1], x[2], x[3]);
-    reinterpret_cast<float4*>(p)[1] = make_float4(x[4], x[5], x[6], x[7]);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) p[i] = from_f<T>(x[i]);
   }
-}
+  template <bool VEC>
+  __device__ __forceinline__ void load(const T* p) {
+    if constexpr (VEC) {
+#pragma unroll
+      for (int i = 0; i < (int)sizeof(w) / 16; ++i) {
+        const uint4 v = reinterpret_cast<const uint4*>(p)[i];
+        w[4 * i] = v.x; w[4 * i + 1] = v.y; w[4 * i + 2] = v.z; w[4 * i + 3] = v.w;
+      }
+    } else {
+      float x[KS_EL];
+#pragma unroll
+      for (int i = 0; i < KS_EL; ++i) x[i] = to_f<T>(p[i]);
+      from(x);
+    }
+  }
+  template <bool VEC>
+  __device__ __forceinline__ void store(T* p) const {
+    if constexpr (VEC) {
+#pragma unroll
+      for (int i = 0; i < (int)sizeof(w) / 16; ++i)
+        reinterpret_cast<uint4*>(p)[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+    } else {
+      float x[KS_EL];
+      f32(x);
+#pragma unroll
+      for (int i = 0; i < KS_EL; ++i) p[i] = from_f<T>(x[i]);
+    }
+  }
+};
 
 // Entry (position, head 0) of row r, as an index of [block][head][slot], or -1.
 __device__ __forceinline__ long long entry0(const KvPaged& c, int seq, int pos) {
@@ -68,111 +87,152 @@ __device__ __forceinline__ long long entry0(const KvPaged& c, int seq, int pos) 
   return (long long)blk * c.n_kv_heads * c.block_tokens + pos % c.block_tokens;
 }
 
-// Thread group of TPV = head_dim / 8 threads per vector; a vector index is (row, K or V, head).
+// Item i of a CTA's rows: row, K or V, head, 16 elements of the head.
+template <int DH>
+struct Item {
+  int r, is_v, h, sub;
+  __device__ __forceinline__ Item(int i, int hk, int per_row) {
+    r = i / per_row;
+    const int w = i - r * per_row, vec = w / (DH / KS_EL);
+    sub = w % (DH / KS_EL);
+    is_v = vec >= hk;
+    h = vec - (is_v ? hk : 0);
+  }
+};
+
 template <int DH, typename T, int KT, bool VEC>
-__global__ void __launch_bounds__(KS_THREADS) kv_append_kernel(KvPaged c, int n_rows, const T* k, long long ld_k, const T* v,
-                                                               long long ld_v, const int* seq, const int* pos) {
+__global__ void __launch_bounds__(KS_THREADS) kv_append_kernel(KvPaged c, int n_rows, int rows_cta, const T* k, long long ld_k,
+                                                               const T* v, long long ld_v, const int* seq, const int* pos) {
   PDL_ENTRY();
-  constexpr int TPV = DH / 8;
-  const int sub = threadIdx.x % TPV, hk = c.n_kv_heads;
-  const long long n_vec = (long long)n_rows * 2 * hk;
-  const long long step = (long long)gridDim.x * (KS_THREADS / TPV);
-  // (whole warps leave the loop together: the vectors of a warp are padded up to it)
-  const long long n_pad = (n_vec + 32 / TPV - 1) / (32 / TPV) * (32 / TPV);
-  for (long long i = (long long)blockIdx.x * (KS_THREADS / TPV) + threadIdx.x / TPV; i < n_pad; i += step) {
-    const bool in = i < n_vec;
-    const long long ii = in ? i : n_vec - 1;
-    const long long r = ii / (2 * hk);
-    const int w = (int)(ii - r * (2 * hk)), is_v = w >= hk, h = is_v ? w - hk : w;
-    float x[8];
-    load8<T, VEC>((is_v ? v + r * ld_v : k + r * ld_k) + (size_t)h * DH + sub * 8, x);
-    const long long e0 = in ? entry0(c, seq[r], pos[r]) : -1;
-    const size_t e = (size_t)(e0 + (long long)h * c.block_tokens);
-    if constexpr (KT == KV_E4M3) {
-      float a = 0.f;
+  constexpr int TPV = DH / KS_EL;   // threads of a vector: neighbours
+  const int hk = c.n_kv_heads, per_row = 2 * hk * TPV, row0 = (int)blockIdx.x * rows_cta;
+  const int total = min(rows_cta, n_rows - row0) * per_row;
+  for (int i0 = 0; i0 < total; i0 += KS_THREADS * KS_ITEMS) {
+    Piece<T> x[KS_ITEMS];
+    long long e[KS_ITEMS];   // the vector's entry, -1: not written
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float b = fabsf(x[j]);
-        a = fmaxf(a, b == INFINITY ? 0.f : b);   // (fmaxf leaves NaN out)
-      }
+    for (int q = 0; q < KS_ITEMS; ++q) {
+      const int i = i0 + q * KS_THREADS + threadIdx.x;
+      const Item<DH> it(min(i, total - 1), hk, per_row);
+      const long long r = row0 + it.r;
+      x[q].template load<VEC>((it.is_v ? v + r * ld_v : k + r * ld_k) + (size_t)it.h * DH + it.sub * KS_EL);
+      e[q] = i < total ? entry0(c, seq[r], pos[r]) : -1;
+      if (e[q] >= 0) e[q] += (long long)it.h * c.block_tokens;
+    }
 #pragma unroll
-      for (int o = TPV / 2; o; o >>= 1) a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, o));
-      const unsigned bits = __float_as_uint(a);
-      int ex = (int)(bits >> 23) - 127 - 8 + ((bits & 0x7fffffu) > 0x600000u ? 1 : 0);
-      ex = a == 0.f ? 0 : max(ex, -126);
-      const float s = __uint_as_float((unsigned)(127 - ex) << 23);
-      uint32_t out[2];
+    for (int q = 0; q < KS_ITEMS; ++q) {
+      const Item<DH> it(min(i0 + q * KS_THREADS + (int)threadIdx.x, total - 1), hk, per_row);
+      void* pool = it.is_v ? c.v : c.k;
+      const size_t at = (size_t)e[q] * DH + it.sub * KS_EL;
+      float y[KS_EL];
+      x[q].f32(y);
+      if constexpr (KT == KV_E4M3) {
+        float a = 0.f;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        float y0 = x[2 * j] * s, y1 = x[2 * j + 1] * s;
-        if (fabsf(x[2 * j]) == INFINITY) y0 = NAN;
-        if (fabsf(x[2 * j + 1]) == INFINITY) y1 = NAN;
-        const uint32_t two = __nv_cvt_float2_to_fp8x2(make_float2(y0, y1), __NV_SATFINITE, __NV_E4M3);
-        if (j & 1)
-          out[j >> 1] |= two << 16;
-        else
-          out[j >> 1] = two;
+        for (int j = 0; j < KS_EL; ++j) {
+          const float b = fabsf(y[j]);
+          a = fmaxf(a, b == INFINITY ? 0.f : b);   // (fmaxf leaves NaN out)
+        }
+#pragma unroll
+        for (int o = TPV / 2; o; o >>= 1) a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, o));
+        const unsigned bits = __float_as_uint(a);
+        int ex = (int)(bits >> 23) - 127 - 8 + ((bits & 0x7fffffu) > 0x600000u ? 1 : 0);
+        ex = a == 0.f ? 0 : max(ex, -126);
+        const float s = __uint_as_float((unsigned)(127 - ex) << 23);
+        uint32_t out[KS_EL / 4];
+#pragma unroll
+        for (int j = 0; j < KS_EL / 2; ++j) {
+          float y0 = y[2 * j] * s, y1 = y[2 * j + 1] * s;
+          if (fabsf(y[2 * j]) == INFINITY) y0 = NAN;
+          if (fabsf(y[2 * j + 1]) == INFINITY) y1 = NAN;
+          const uint32_t two = __nv_cvt_float2_to_fp8x2(make_float2(y0, y1), __NV_SATFINITE, __NV_E4M3);
+          if (j & 1)
+            out[j >> 1] |= two << 16;
+          else
+            out[j >> 1] = two;
+        }
+        if (e[q] >= 0) {
+          *reinterpret_cast<uint4*>((uint8_t*)pool + at) = make_uint4(out[0], out[1], out[2], out[3]);
+          if (it.sub == 0) (it.is_v ? c.v_exp : c.k_exp)[e[q]] = (uint8_t)(ex + 127);
+        }
+      } else if (e[q] >= 0) {
+        using C = typename std::conditional<KT == KV_BF16, bf16, float>::type;
+        Piece<C> z;
+        z.from(y);
+        z.template store<true>((C*)pool + at);
       }
-      if (e0 >= 0) {
-        *reinterpret_cast<uint2*>((uint8_t*)(is_v ? c.v : c.k) + e * DH + sub * 8) = make_uint2(out[0], out[1]);
-        if (sub == 0) (is_v ? c.v_exp : c.k_exp)[e] = (uint8_t)(ex + 127);
-      }
-    } else if (e0 >= 0) {
-      if constexpr (KT == KV_BF16)
-        store8<bf16, true>((bf16*)(is_v ? c.v : c.k) + e * DH + sub * 8, x);
-      else
-        store8<float, true>((float*)(is_v ? c.v : c.k) + e * DH + sub * 8, x);
     }
   }
 }
 
 template <int DH, typename T, int KT, bool VEC>
-__global__ void __launch_bounds__(KS_THREADS) kv_gather_kernel(KvPaged c, int n_rows, T* k, long long ld_k, T* v,
+__global__ void __launch_bounds__(KS_THREADS) kv_gather_kernel(KvPaged c, int n_rows, int rows_cta, T* k, long long ld_k, T* v,
                                                                long long ld_v, const int* seq, const int* pos) {
   PDL_ENTRY();
-  constexpr int TPV = DH / 8;
-  const int sub = threadIdx.x % TPV, hk = c.n_kv_heads;
-  const long long n_vec = (long long)n_rows * 2 * hk;
-  const long long step = (long long)gridDim.x * (KS_THREADS / TPV);
-  for (long long i = (long long)blockIdx.x * (KS_THREADS / TPV) + threadIdx.x / TPV; i < n_vec; i += step) {
-    const long long r = i / (2 * hk);
-    const int w = (int)(i - r * (2 * hk)), is_v = w >= hk, h = is_v ? w - hk : w;
-    const long long e0 = entry0(c, seq[r], pos[r]);
-    if (e0 < 0) continue;
-    const size_t e = (size_t)(e0 + (long long)h * c.block_tokens);
-    float x[8];
-    if constexpr (KT == KV_E4M3) {
-      const uint2 codes = *reinterpret_cast<const uint2*>((const uint8_t*)(is_v ? c.v : c.k) + e * DH + sub * 8);
-      // 2^e with e down to -127 (a byte of 0 is the subnormal 2^-127)
-      const int b = (is_v ? c.v_exp : c.k_exp)[e];
-      const float s = b ? __uint_as_float((unsigned)b << 23) : __uint_as_float(0x400000u);
+  constexpr int TPV = DH / KS_EL;
+  const int hk = c.n_kv_heads, per_row = 2 * hk * TPV, row0 = (int)blockIdx.x * rows_cta;
+  const int total = min(rows_cta, n_rows - row0) * per_row;
+  using C = typename std::conditional<KT == KV_F32, float, bf16>::type;
+  for (int i0 = 0; i0 < total; i0 += KS_THREADS * KS_ITEMS) {
+    Piece<C> x[KS_ITEMS];   // (e4m3: 16 codes in the first four words)
+    int ex[KS_ITEMS];
+    bool on[KS_ITEMS];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const uint32_t word = j < 2 ? codes.x : codes.y;
-        const __half2_raw hr = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(word >> (j & 1 ? 16 : 0)), __NV_E4M3);
-        const float2 f = __half22float2(__half2(hr));
-        x[2 * j] = f.x * s;
-        x[2 * j + 1] = f.y * s;
+    for (int q = 0; q < KS_ITEMS; ++q) {
+      const int i = i0 + q * KS_THREADS + threadIdx.x;
+      const Item<DH> it(min(i, total - 1), hk, per_row);
+      const long long r = row0 + it.r, e0 = i < total ? entry0(c, seq[r], pos[r]) : -1;
+      on[q] = e0 >= 0;
+      if (!on[q]) continue;
+      const size_t e = (size_t)(e0 + (long long)it.h * c.block_tokens), at = e * DH + it.sub * KS_EL;
+      const void* pool = it.is_v ? c.v : c.k;
+      if constexpr (KT == KV_E4M3) {
+        const uint4 w = *reinterpret_cast<const uint4*>((const uint8_t*)pool + at);
+        x[q].w[0] = w.x; x[q].w[1] = w.y; x[q].w[2] = w.z; x[q].w[3] = w.w;
+        ex[q] = (it.is_v ? c.v_exp : c.k_exp)[e];
+      } else {
+        x[q].template load<true>((const C*)pool + at);
       }
-    } else if constexpr (KT == KV_BF16) {
-      load8<bf16, true>((const bf16*)(is_v ? c.v : c.k) + e * DH + sub * 8, x);
-    } else {
-      load8<float, true>((const float*)(is_v ? c.v : c.k) + e * DH + sub * 8, x);
     }
-    store8<T, VEC>((is_v ? v + r * ld_v : k + r * ld_k) + (size_t)h * DH + sub * 8, x);
+#pragma unroll
+    for (int q = 0; q < KS_ITEMS; ++q) {
+      if (!on[q]) continue;
+      const Item<DH> it(i0 + q * KS_THREADS + (int)threadIdx.x, hk, per_row);
+      const long long r = row0 + it.r;
+      float y[KS_EL];
+      if constexpr (KT == KV_E4M3) {
+        // 2^e with e down to -127 (a byte of 0 is the subnormal 2^-127)
+        const float s = ex[q] ? __uint_as_float((unsigned)ex[q] << 23) : __uint_as_float(0x400000u);
+#pragma unroll
+        for (int j = 0; j < KS_EL / 2; ++j) {
+          const __half2_raw hr = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(x[q].w[j >> 1] >> (j & 1 ? 16 : 0)), __NV_E4M3);
+          const float2 f = __half22float2(__half2(hr));
+          y[2 * j] = f.x * s;
+          y[2 * j + 1] = f.y * s;
+        }
+      } else {
+        x[q].f32(y);
+      }
+      Piece<T> z;
+      z.from(y);
+      z.template store<VEC>((it.is_v ? v + r * ld_v : k + r * ld_k) + (size_t)it.h * DH + it.sub * KS_EL);
+    }
   }
 }
 
-int ks_grid(const KvPaged& c, int n_rows) {
+// Rows of a CTA: one pass of all its threads, where there are rows enough for two CTAs an SM; else fewer (a step's 8 rows of 32
+// heads: one each).
+int ks_rows(const KvPaged& c, int n_rows) {
   static const int sms = [] {
     int dev = 0, n = 0;
     cudaGetDevice(&dev);
     cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev);
     return n > 0 ? n : 1;
   }();
-  const long long per = KS_THREADS / (c.head_dim / 8), n = ((long long)n_rows * 2 * c.n_kv_heads + per - 1) / per;
-  const long long most = (long long)sms * 8;
-  return (int)(n < most ? n : most);
+  const int per_row = 2 * c.n_kv_heads * (c.head_dim / KS_EL), full = KS_THREADS * KS_ITEMS / per_row;
+  const int spread = n_rows / (2 * sms);
+  const int r = full < spread ? full : spread;
+  return r > 1 ? r : 1;
 }
 
 bool rows_aligned(const void* k, long long ld_k, const void* v, long long ld_v, int esz) {
@@ -183,13 +243,15 @@ template <int DH, typename T, int KT>
 cudaError_t append_t(cudaStream_t st, const KvPaged& c, int n, const void* k, long long ld_k, const void* v, long long ld_v,
                      const int* seq, const int* pos) {
   auto kern = rows_aligned(k, ld_k, v, ld_v, (int)sizeof(T)) ? kv_append_kernel<DH, T, KT, true> : kv_append_kernel<DH, T, KT, false>;
-  return launch_k(kern, dim3(ks_grid(c, n)), dim3(KS_THREADS), 0, st, c, n, (const T*)k, ld_k, (const T*)v, ld_v, seq, pos);
+  const int rows = ks_rows(c, n);
+  return launch_k(kern, dim3((unsigned)cdiv(n, rows)), dim3(KS_THREADS), 0, st, c, n, rows, (const T*)k, ld_k, (const T*)v, ld_v, seq, pos);
 }
 template <int DH, typename T, int KT>
 cudaError_t gather_t(cudaStream_t st, const KvPaged& c, int n, void* k, long long ld_k, void* v, long long ld_v, const int* seq,
                      const int* pos) {
   auto kern = rows_aligned(k, ld_k, v, ld_v, (int)sizeof(T)) ? kv_gather_kernel<DH, T, KT, true> : kv_gather_kernel<DH, T, KT, false>;
-  return launch_k(kern, dim3(ks_grid(c, n)), dim3(KS_THREADS), 0, st, c, n, (T*)k, ld_k, (T*)v, ld_v, seq, pos);
+  const int rows = ks_rows(c, n);
+  return launch_k(kern, dim3((unsigned)cdiv(n, rows)), dim3(KS_THREADS), 0, st, c, n, rows, (T*)k, ld_k, (T*)v, ld_v, seq, pos);
 }
 
 #define KS_DISPATCH(F, BF, ...)                                                                   \
