@@ -765,29 +765,23 @@ int chunk_sms() {
   return sms;
 }
 
-// How a call is run: its kernel, plan, rows of a tile, query heads of a tile's token and head groups per KV head.
-enum ChunkKind { CHUNK_ANY, CHUNK_FEW, CHUNK_TC };
+// How the CUDA-core and the few-row kernel run a call: plan, rows of a tile, query heads of a tile's token, head groups per KV head.
 struct ChunkHow {
-  ChunkKind kind;
+  bool few;
   SplitPlan p;
   int rows, per_tok, sub;
   bool may_split;
 };
-ChunkHow chunk_how(const KvPaged& c, int n_heads, int max_q, int max_kv, bool aligned) {
+ChunkHow chunk_how(const KvPaged& c, int n_heads, int max_kv, bool aligned) {
   const int group = n_heads / c.n_kv_heads;
-  ChunkHow w{};
-  if (aligned && (long long)max_q * group > CF_ROWS && chunk_tc_takes(c, n_heads)) {
-    w.kind = CHUNK_TC;
-    return w;
-  }
-  if (c.type != KV_F32 && c.block_tokens == 16 && aligned) {
-    w.kind = CHUNK_FEW;
+  ChunkHow w;
+  w.few = c.type != KV_F32 && c.block_tokens == 16 && aligned;
+  if (w.few) {
     w.rows = CF_ROWS;
     w.per_tok = std::min(group, CF_ROWS);
     w.sub = cdiv(group, w.per_tok);
     w.p = SplitPlan{CF_ROWS / w.per_tok, c.n_kv_heads * w.sub, CF_WARPS * 16 * (c.type == KV_BF16 ? 1 : 2), chunk_sms() * 3};
   } else {
-    w.kind = CHUNK_ANY;
     w.rows = CG_ROWS;
     w.per_tok = 1;
     w.sub = group;
@@ -797,16 +791,24 @@ ChunkHow chunk_how(const KvPaged& c, int n_heads, int max_q, int max_kv, bool al
   return w;
 }
 size_t how_bytes(const ChunkHow& w, const KvPaged& c) {
-  if (w.kind == CHUNK_TC) return chunk_tc_workspace(c);
   return w.may_split ? (size_t)w.p.target * w.rows * (c.head_dim + 2) * sizeof(float) : 0;
 }
+// The most new tokens of a sequence whose rows are one tile of the few-row kernel.
+int few_tokens(const KvPaged& c, int n_heads) { return std::max(1, CF_ROWS / (n_heads / c.n_kv_heads)); }
+bool use_tc(const KvPaged& c, int n_heads, int max_q, int max_kv, bool aligned) {
+  return aligned && max_q > few_tokens(c, n_heads) && chunk_tc_takes(c, n_heads, max_kv);
+}
+// Sequences of few tokens in a call that also has longer ones: left to the tcgen05 kernel over bf16 entries (its tiles are
+// mostly empty then, but it reads K and V at the rate of the memory all the same), while 8-bit entries, which would have to
+// be widened for it, go to the few-row kernel.
+bool use_both(const KvPaged& c) { return c.type == KV_E4M3 && c.n_seq > 1; }
 
 template <int DH, int KT, typename T>
 cudaError_t chunk_t(cudaStream_t st, const ChunkCall& a, const ChunkHow& w, int* launches) {
-  const dim3 grid((unsigned)split_items(w.p, a.c.n_seq, a.n_rows, a.max_q));
-  *launches = 1;
+  const dim3 grid((unsigned)split_items(w.p, a.c.n_seq, a.n_rows, std::min(a.max_q, a.c_hi)));
   cudaError_t e = cudaErrorInvalidValue;
-  if (w.kind == CHUNK_ANY) {
+  ++*launches;
+  if (!w.few) {
     e = launch_k(chunk_any_kernel<DH, KT, T>, grid, dim3(CG_KEYS), 0, st, a, w.p);
   } else if constexpr (KT != KV_F32) {
     constexpr int smem = FewShape<DH, KT>::SMEM;
@@ -814,24 +816,14 @@ cudaError_t chunk_t(cudaStream_t st, const ChunkCall& a, const ChunkHow& w, int*
     if (e == cudaSuccess) e = launch_k(chunk_few_kernel<DH, KT>, grid, dim3(CF_WARPS * 32), smem, st, a, w.p, w.per_tok, w.sub);
   }
   if (e == cudaSuccess && w.may_split) {
-    *launches = 2;
+    ++*launches;
     e = launch_k(chunk_join_kernel<DH, T>, dim3((unsigned)w.p.target), dim3(CJ_THREADS), 0, st, a, w.p, w.rows, w.per_tok, w.sub);
   }
   return e;
 }
 
-}  // namespace
-
-// (whatever kernel the rows' alignment picks)
-size_t chunk_workspace(const KvPaged& c, int n_heads, int n_rows, int max_q, int max_kv) {
-  (void)n_rows;
-  return std::max(how_bytes(chunk_how(c, n_heads, max_q, max_kv, true), c), how_bytes(chunk_how(c, n_heads, max_q, max_kv, false), c));
-}
-
-cudaError_t launch_chunk_attention(cudaStream_t st, const ChunkCall& a, int* launches) {
-  const bool aligned = (((uintptr_t)a.q | (uintptr_t)a.out) & 15) == 0 && a.ld_q % 8 == 0 && a.ld_out % 8 == 0;
-  const ChunkHow w = chunk_how(a.c, a.n_heads, a.max_q, a.max_kv, aligned);
-  if (w.kind == CHUNK_TC) return launch_chunk_tc(st, a, launches);
+cudaError_t chunk_simple(cudaStream_t st, const ChunkCall& a, bool aligned, int* launches) {
+  const ChunkHow w = chunk_how(a.c, a.n_heads, a.max_kv, aligned);
 #define CH_DH(D)                                                                   \
   case D:                                                                          \
     if (a.c.type == KV_F32) return chunk_t<D, KV_F32, float>(st, a, w, launches);  \
@@ -844,6 +836,36 @@ cudaError_t launch_chunk_attention(cudaStream_t st, const ChunkCall& a, int* lau
   }
 #undef CH_DH
   return cudaErrorInvalidValue;
+}
+
+size_t round256(size_t x) { return (x + 255) / 256 * 256; }
+
+}  // namespace
+
+// (whatever kernel the rows' alignment picks)
+size_t chunk_workspace(const KvPaged& c, int n_heads, int max_q, int max_kv) {
+  const size_t any = how_bytes(chunk_how(c, n_heads, max_kv, false), c), few = how_bytes(chunk_how(c, n_heads, max_kv, true), c);
+  size_t tc = few;
+  if (use_tc(c, n_heads, max_q, max_kv, true)) tc = (use_both(c) ? round256(few) : 0) + chunk_tc_workspace(c, max_kv);
+  return std::max(any, tc);
+}
+
+cudaError_t launch_chunk_attention(cudaStream_t st, const ChunkCall& a0, int* launches) {
+  ChunkCall a = a0;
+  a.c_lo = 1;
+  a.c_hi = a.max_q;
+  *launches = 0;
+  const bool aligned = (((uintptr_t)a.q | (uintptr_t)a.out) & 15) == 0 && a.ld_q % 8 == 0 && a.ld_out % 8 == 0;
+  if (!use_tc(a.c, a.n_heads, a.max_q, a.max_kv, aligned)) return chunk_simple(st, a, aligned, launches);
+  if (use_both(a.c)) {
+    a.c_hi = few_tokens(a.c, a.n_heads);
+    const cudaError_t e = chunk_simple(st, a, aligned, launches);
+    if (e != cudaSuccess) return e;
+    a.c_lo = a.c_hi + 1;
+    a.c_hi = a.max_q;
+    a.part = (float*)((char*)a.part + round256(how_bytes(chunk_how(a.c, a.n_heads, a.max_kv, true), a.c)));
+  }
+  return launch_chunk_tc(st, a, launches);
 }
 
 ADEPT_WAIT_LIMIT_SETTER(cf)

@@ -10,8 +10,7 @@
 //                       maximum (raised only by more than 2^8), exp2, sum, P to tensor memory; at the end O / l
 //          8            issues the matrix instructions:  PV_0(j) S_0(j+1) PV_1(j) S_1(j+1)  (in issue order on the tensor
 //                       core, so S_0(j+1) may overwrite P_0(j), and a completed S(j+1) means a completed PV(j))
-//          9 ..         K and V.  bf16: 9 and 10 fetch K and V blocks by TMA, 10 mends the V tiles at the causal edge.  e4m3:
-//                       9..15 read codes, turn them into bf16 (exactly: code * 2^e) and store the swizzled tiles.
+//          9, 10        fetch K and V blocks by TMA; 10 mends the V tiles at the causal edge
 //
 // The causal edge: from the first row's position on, a key tile holds keys that not every row attends, or none does.  Scores are
 // masked there.  V entries that nobody attends become zero; a NaN or infinite one is replaced by zero and its key noted per
@@ -20,6 +19,9 @@
 // Work: every (tile, KV head) is a row of key tiles; all of them in a row are cut into equal runs, one per CTA (one CTA per SM),
 // so the GPU is evenly loaded whatever the mix of lengths.  A run holds whole tiles and at most two parts of tiles, whose
 // (maximum, sum, weighted V) go to the workspace and are joined in order by a second launch.
+// 8-bit entries: a launch of its own first turns the positions of this kernel's sequences into bf16 (exactly: code * 2^e) in the
+// workspace, once for all the tiles that read them.  Turned by warps of this kernel, tile by tile, they came at 9000 cycles
+// a key tile (2048 of matrix instructions): a mixed batch took 121 us.
 // Every wait is bounded; a CTA that gives up sets the error word, drains its copies and matrix instructions and leaves.
 #define ADEPT_TU_ID 13
 #include "kv_paged.h"
@@ -38,10 +40,9 @@ constexpr int CT_BM = 128, CT_BN = 128, CT_ROWS = 2 * CT_BM;
 constexpr float CT_RAISE = 8.f;
 constexpr long long CT_DRAIN_CYCLES = 4000000000LL;
 
-template <int DH, int KT>
+template <int DH>
 struct CtShape {
-  static constexpr int LOADERS = KT == KV_BF16 ? 2 : 7;            // warps 9 ..
-  static constexpr int THREADS = (9 + LOADERS) * 32;
+  static constexpr int THREADS = 11 * 32;
   static constexpr int HALVES = DH / 64;
   static constexpr int Q_BYTES = HALVES * CT_BM * 128;             // one sub-tile: [half][row][128 B]
   static constexpr int KV_BYTES = HALVES * CT_BN * 128;            // one K or V stage: [half][key][128 B]
@@ -53,6 +54,7 @@ struct CtParams {
   CUtensorMap kmap, vmap;   // bf16: the pools as [n_blocks * n_kv_heads * 16][d_h], box {64, 16}
   int ts;                   // tokens of a sub-tile
   int runs;                 // CTAs
+  int wide;                 // > 0: the maps are of widened entries, `wide` blocks per sequence in order
   unsigned* no_err;         // where time-outs go without an error word (the workspace's last word)
 };
 
@@ -190,15 +192,6 @@ constexpr size_t ct_ws_floats(int runs, int dh) {
   return (size_t)runs * (sizeof(CtNote) / 4) + (size_t)runs * 2 * CT_ROWS * (dh + 2);
 }
 
-__device__ __forceinline__ float ct_exp2i(int b) {   // 2^(b - 127)
-  return b ? __uint_as_float((unsigned)b << 23) : __uint_as_float(0x400000u);
-}
-__device__ __forceinline__ uint32_t ct_bf16x2(uint32_t codes, __nv_bfloat162 scale) {
-  const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)codes, __NV_E4M3);
-  const float2 f = __half22float2(__half2(h));
-  const __nv_bfloat162 r = __hmul2(__floats2bfloat162_rn(f.x, f.y), scale);
-  return *reinterpret_cast<const uint32_t*>(&r);
-}
 // Non-finite bf16 of a pair: 0xffff in its half; and whether there is one (a carry out of an exponent of all ones).
 __device__ __forceinline__ uint32_t ct_bad2(uint32_t x) { return __vcmpeq2(x & 0x7f807f80u, 0x7f807f80u); }
 __device__ __forceinline__ uint32_t ct_any_bad2(uint32_t x) { return ((x & 0x7f807f80u) + 0x00800080u) & 0x80008000u; }
@@ -245,16 +238,17 @@ struct CtSeg {
   // key tile j (from the segment's first) holds keys that are not everybody's
   __device__ __forceinline__ bool edge(int j) const { return (j_lo + j + 1) * CT_BN > lim_lo || (j_lo + j + 1) * CT_BN > k_end; }
   // the row of key block b (from the sequence's first) in the pools seen as rows of d_h, -1: nobody's, -2: not there
-  __device__ __forceinline__ int row_of(const KvPaged& c, int b) const {
+  __device__ __forceinline__ int row_of(const KvPaged& c, int wide, int b) const {
     if (b * 16 >= k_end) return -1;
     const int blk = table[b];
-    return blk >= 0 && blk < c.n_blocks ? (blk * c.n_kv_heads + x.kvh) * 16 : -2;
+    if (blk < 0 || blk >= c.n_blocks) return -2;
+    return ((wide ? x.seq * wide + b : blk) * c.n_kv_heads + x.kvh) * 16;
   }
 };
 
-template <int DH, int KT>
-__global__ void __launch_bounds__(CtShape<DH, KT>::THREADS, 1) chunk_tc_kernel(const __grid_constant__ CtParams p) {
-  using L = CtShape<DH, KT>;
+template <int DH>
+__global__ void __launch_bounds__(CtShape<DH>::THREADS, 1) chunk_tc_kernel(const __grid_constant__ CtParams p) {
+  using L = CtShape<DH>;
   extern __shared__ __align__(1024) uint8_t ct_raw[];
   __shared__ __align__(8) uint64_t k_full[2], v_full[2], k_empty[2], v_empty[2], s_full[2], p_half[2], p_full[2], o_full[2], v_fix[2], drain;
   __shared__ uint32_t s_tmem;
@@ -274,10 +268,9 @@ __global__ void __launch_bounds__(CtShape<DH, KT>::THREADS, 1) chunk_tc_kernel(c
   unsigned* err = a.c.err ? a.c.err : p.no_err;
 
   if (tid == 0) {
-    constexpr int arrivals = KT == KV_BF16 ? 1 : L::LOADERS;
     for (int s = 0; s < 2; ++s) {
-      mbar_init(&k_full[s], arrivals);
-      mbar_init(&v_full[s], arrivals);
+      mbar_init(&k_full[s], 1);
+      mbar_init(&v_full[s], 1);
       mbar_init(&k_empty[s], 1);
       mbar_init(&v_empty[s], 1);
       mbar_init(&s_full[s], 1);
@@ -378,7 +371,6 @@ __global__ void __launch_bounds__(CtShape<DH, KT>::THREADS, 1) chunk_tc_kernel(c
 
   if (warp < 8) {
     // ---- softmax of a row per thread
-    if constexpr (KT == KV_E4M3) asm volatile("setmaxnreg.inc.sync.aligned.u32 176;");
     const int sub = warp >> 2, r = tid & 127;
     const uint32_t base = tmem + ((uint32_t)((warp & 3) * 32) << 16), s_col = base + (uint32_t)(sub * 128),
                    o_col = base + 256u + (uint32_t)(sub * 128);
@@ -521,7 +513,6 @@ __global__ void __launch_bounds__(CtShape<DH, KT>::THREADS, 1) chunk_tc_kernel(c
   } else if (warp == 8) {
     // ---- matrix instructions: one thread for a whole segment (a warp that meets at every wait took 3900 cycles a key tile to
     // issue what the tensor core does in 2048), descriptors made once and moved by their address field
-    if constexpr (KT == KV_E4M3) asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
     constexpr uint32_t IDESC_S = umma_idesc(CT_BN, false), IDESC_O = umma_idesc(DH, true);
     const uint64_t dq = sdesc_sw128(smem_u32(sQ)), dk = sdesc_sw128(smem_u32(sK)), dv = sdesc_mn_sw128(smem_u32(sV), CT_BN * 128);
     int nk = 0, nv = 0, np[2] = {0, 0}, nf[2] = {0, 0};   // K, V, P tiles and mended V tiles (per stage) so far
@@ -539,7 +530,7 @@ __global__ void __launch_bounds__(CtShape<DH, KT>::THREADS, 1) chunk_tc_kernel(c
           }
           if (j >= 0) {
             if (!wait(&v_full[vs], vn >> 1)) break;
-            if (KT == KV_BF16 && (g.edge(j) || s_gone[vn & 3]) && !wait(&v_fix[vs], nf[vs]++)) break;
+            if ((g.edge(j) || s_gone[vn & 3]) && !wait(&v_fix[vs], nf[vs]++)) break;
             ++nv;
           }
           const uint64_t dks = dk + (uint64_t)(ks * (L::KV_BYTES >> 4)), dvs = dv + (uint64_t)(vs * (L::KV_BYTES >> 4));
@@ -586,7 +577,7 @@ __global__ void __launch_bounds__(CtShape<DH, KT>::THREADS, 1) chunk_tc_kernel(c
       }
     }
     __syncwarp();
-  } else if constexpr (KT == KV_BF16) {
+  } else {
     // ---- TMA producers: K (warp 9), V (warp 10, which also mends the V tiles at the edge)
     const bool kw = warp == 9;
     uint64_t *full = kw ? k_full : v_full, *empty = kw ? k_empty : v_empty;
@@ -644,7 +635,7 @@ __global__ void __launch_bounds__(CtShape<DH, KT>::THREADS, 1) chunk_tc_kernel(c
         gone_prev = gone;
         if (!kw && j > 0 && (g.edge(j - 1) || gone_prev) && !(ok = mend(j - 1, cnt - 1, gone_prev))) break;
         if (j == g.n_it) break;
-        const int s = cnt & 1, row = lane < 8 ? g.row_of(a.c, (g.j_lo + j) * 8 + lane) : -1;
+        const int s = cnt & 1, row = lane < 8 ? g.row_of(a.c, p.wide, (g.j_lo + j) * 8 + lane) : -1;
         const unsigned on = __ballot_sync(0xffffffffu, row >= 0);
         gone = (int)__ballot_sync(0xffffffffu, row == -2);
         if (gone && lane == 0) a.c.flag(ERRW_POS);
@@ -675,98 +666,47 @@ __global__ void __launch_bounds__(CtShape<DH, KT>::THREADS, 1) chunk_tc_kernel(c
       }
     }
     __syncwarp();
-  } else {
-    // ---- e4m3: codes to registers a tile ahead, then bf16 into the swizzled stage; K and V in turn
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
-    constexpr int PIECES = CT_BN * (DH / 16), LT = L::LOADERS * 32, PER = (PIECES + LT - 1) / LT;
-    const int lt = tid - 9 * 32;
-    int cnt[2] = {0, 0};   // K, V tiles so far
-    uint4 w[PER];
-    int ex[PER];
-    CtSeg g{};
-    bool ok = true;
-    auto fetch = [&](int t) {   // t: 2 j (K) or 2 j + 1 (V)
-      const uint8_t* from = (const uint8_t*)(t & 1 ? a.c.v : a.c.k);
-      const uint8_t* eb = t & 1 ? a.c.v_exp : a.c.k_exp;
-#pragma unroll
-      for (int i = 0; i < PER; ++i) {
-        const int pc = lt + i * LT, k = (g.j_lo + (t >> 1)) * CT_BN + pc / (DH / 16);
-        w[i] = make_uint4(0, 0, 0, 0);
-        ex[i] = 127;
-        if (pc < PIECES && k < g.k_end) {
-          const int blk = g.table[k >> 4];
-          if (blk >= 0 && blk < a.c.n_blocks) {
-            const size_t e = ((size_t)blk * a.c.n_kv_heads + g.x.kvh) * 16 + (k & 15);
-            w[i] = *reinterpret_cast<const uint4*>(from + e * DH + pc % (DH / 16) * 16);
-            ex[i] = eb[e];
-          }
-        }
-      }
-    };
-    while (u < u_end) {
-      begin(g);
-      if (g.n_it > 0) fetch(0);
-      for (int t = 0; t < 2 * g.n_it && ok; ++t) {
-        const int is_v = t & 1, n = cnt[is_v], s = n & 1;
-        if (n >= 2 && !(ok = mbar_wait_warp(is_v ? &v_empty[s] : &k_empty[s], (uint32_t)(((n >> 1) - 1) & 1), abort_flag, err, wlim)))
-          break;
-        uint8_t* dst = (is_v ? sV : sK) + s * L::KV_BYTES;
-        const bool look = is_v && g.edge(t >> 1);
-#pragma unroll
-        for (int i = 0; i < PER; ++i) {
-          const int pc = lt + i * LT;
-          if (pc < PIECES) {
-            const int key = pc / (DH / 16), c0 = pc % (DH / 16) * 2;   // two 8-element pieces
-            const __nv_bfloat162 sc = __float2bfloat162_rn(ct_exp2i(ex[i]));
-            const uint32_t cw[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
-            uint32_t y[8];
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-              y[2 * q] = ct_bf16x2(cw[q] & 0xffffu, sc);
-              y[2 * q + 1] = ct_bf16x2(cw[q] >> 16, sc);
-            }
-            if (look) {
-#pragma unroll
-              for (int q = 0; q < 8; ++q) {
-                const uint32_t b = ct_bad2(y[q]);
-                if (b) {
-                  y[q] &= ~b;
-                  const int k = (g.j_lo + (t >> 1)) * CT_BN + key;
-                  if (b & 1) atomicMin(&s_pk[c0 * 8 + 2 * q], k);
-                  if (b >> 16) atomicMin(&s_pk[c0 * 8 + 2 * q + 1], k);
-                  s_poisoned = 1;
-                }
-              }
-            }
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              const int ch = c0 + h;
-              *reinterpret_cast<uint4*>(dst + (ch >> 3) * CT_BN * 128 + key * 128 + (((ch & 7) ^ (key & 7)) << 4)) =
-                  make_uint4(y[4 * h], y[4 * h + 1], y[4 * h + 2], y[4 * h + 3]);
-            }
-          }
-        }
-        if (!is_v && warp == 9) {
-          const int row = lane < 8 ? g.row_of(a.c, (g.j_lo + (t >> 1)) * 8 + lane) : -1;
-          const int gone = (int)__ballot_sync(0xffffffffu, row == -2);
-          if (lane == 0) {
-            if (gone) a.c.flag(ERRW_POS);
-            s_gone[n & 3] = gone;
-          }
-        }
-        if (t + 1 < 2 * g.n_it) fetch(t + 1);
-        fence_async_shared();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(is_v ? &v_full[s] : &k_full[s]);
-        cnt[is_v] = n + 1;
-      }
-      if (!end(g, ok)) break;
-    }
   }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   if (warp == 8) tmem_dealloc(tmem, 512);
+}
+
+// Entries of 8 bits as bf16: CTA = a block of positions of one sequence, K (z = 0) or V, all heads, 16 elements a thread and turn.
+constexpr int CW_THREADS = 256;
+template <int DH>
+__global__ void __launch_bounds__(CW_THREADS) chunk_widen_kernel(const __grid_constant__ CtParams p, bf16* k_out, bf16* v_out) {
+  PDL_ENTRY();
+  const ChunkCall& a = p.a;
+  const int b = (int)blockIdx.x, seq = (int)blockIdx.y;
+  int q0, c, len;
+  chunk_seq(a, seq, q0, c, len);
+  if (c == 0 || b * 16 >= len) return;
+  const int blk = a.c.table[(size_t)seq * a.c.max_blocks + b];
+  if (blk < 0 || blk >= a.c.n_blocks) return;
+  const int n = a.c.n_kv_heads * 16 * (DH / 16);
+  const size_t from = (size_t)blk * a.c.n_kv_heads * 16, to = ((size_t)seq * p.wide + b) * a.c.n_kv_heads * 16;
+  const uint8_t* codes = (const uint8_t*)(blockIdx.z ? a.c.v : a.c.k) + from * DH;
+  const uint8_t* exps = (blockIdx.z ? a.c.v_exp : a.c.k_exp) + from;
+  bf16* out = (blockIdx.z ? v_out : k_out) + to * DH;
+#pragma unroll 4
+  for (int i = threadIdx.x; i < n; i += CW_THREADS) {
+    const uint4 w = reinterpret_cast<const uint4*>(codes)[i];
+    const int e = exps[i / (DH / 16)];
+    const float s = e ? __uint_as_float((unsigned)e << 23) : __uint_as_float(0x400000u);   // 2^(e - 127)
+    const uint32_t x[4] = {w.x, w.y, w.z, w.w};
+    uint32_t y[8];
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+      const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(x[q >> 1] >> (q & 1 ? 16 : 0)), __NV_E4M3);
+      const float2 f = __half22float2(__half2(h));
+      const __nv_bfloat162 r = __floats2bfloat162_rn(f.x * s, f.y * s);
+      y[q] = *reinterpret_cast<const uint32_t*>(&r);
+    }
+    reinterpret_cast<uint4*>(out)[2 * i] = make_uint4(y[0], y[1], y[2], y[3]);
+    reinterpret_cast<uint4*>(out)[2 * i + 1] = make_uint4(y[4], y[5], y[6], y[7]);
+  }
 }
 
 // Join of the tiles that runs share: CTA (i, y) takes the tile that run i + 1 is the first to begin inside of, an eighth of its
@@ -829,17 +769,6 @@ __global__ void __launch_bounds__(256) chunk_tc_join_kernel(const __grid_constan
   }
 }
 
-template <int DH, int KT>
-cudaError_t launch_t(cudaStream_t st, const CtParams& p) {
-  using L = CtShape<DH, KT>;
-  constexpr int smem = L::TOTAL + 1024;
-  cudaError_t e = cudaFuncSetAttribute(chunk_tc_kernel<DH, KT>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-  if (e != cudaSuccess) return e;
-  e = launch_k(chunk_tc_kernel<DH, KT>, dim3(p.runs), dim3(L::THREADS), smem, st, p);
-  if (e != cudaSuccess) return e;
-  return launch_k(chunk_tc_join_kernel<DH>, dim3(std::max(1, p.runs - 1), CJ_SPLIT), dim3(256), 0, st, p);
-}
-
 int ct_sms() {
   static const int sms = [] {
     int dev = 0, n = 0;
@@ -850,14 +779,45 @@ int ct_sms() {
   return sms;
 }
 
-}  // namespace
-
-bool chunk_tc_takes(const KvPaged& c, int n_heads) {
-  return c.type != KV_F32 && c.block_tokens == 16 && (c.head_dim == 64 || c.head_dim == 128) &&
-         n_heads / c.n_kv_heads <= CT_BM && (long long)c.n_blocks * c.n_kv_heads * 16 < (1ll << 31) && tc_gemm_supported();
+// Workspace: the parts, a word for time-outs, the widened K and V.
+size_t ct_parts_bytes(int dh) { return (ct_ws_floats(ct_sms(), dh) * 4 + 16 + 255) / 256 * 256; }
+size_t ct_wide_bytes(const KvPaged& c, int max_kv) {   // of K, or of V
+  return c.type == KV_E4M3 ? (size_t)c.n_seq * cdiv(max_kv, 16) * c.n_kv_heads * 16 * c.head_dim * 2 : 0;
 }
 
-size_t chunk_tc_workspace(const KvPaged& c) { return (ct_ws_floats(ct_sms(), c.head_dim) + 4) * sizeof(float); }
+template <int DH>
+cudaError_t launch_t(cudaStream_t st, CtParams& p, int* launches) {
+  constexpr int smem = CtShape<DH>::TOTAL + 1024;
+  const KvPaged& c = p.a.c;
+  cudaError_t e = cudaFuncSetAttribute(chunk_tc_kernel<DH>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  if (e != cudaSuccess) return e;
+  void *k = c.k, *v = c.v;
+  uint64_t rows = (uint64_t)c.n_blocks * c.n_kv_heads * 16;
+  if (c.type == KV_E4M3) {
+    p.wide = cdiv(p.a.max_kv, 16);
+    rows = (uint64_t)c.n_seq * p.wide * c.n_kv_heads * 16;
+    k = (char*)p.a.part + ct_parts_bytes(DH);
+    v = (char*)k + ct_wide_bytes(c, p.a.max_kv);
+    e = launch_k(chunk_widen_kernel<DH>, dim3(p.wide, c.n_seq, 2), dim3(CW_THREADS), 0, st, p, (bf16*)k, (bf16*)v);
+    if (e != cudaSuccess) return e;
+    ++*launches;
+  }
+  if (!tc_encode_2d(&p.kmap, k, DH, rows, DH * 2, 16) || !tc_encode_2d(&p.vmap, v, DH, rows, DH * 2, 16)) return cudaErrorInvalidValue;
+  e = launch_k(chunk_tc_kernel<DH>, dim3(p.runs), dim3(CtShape<DH>::THREADS), smem, st, p);
+  if (e != cudaSuccess) return e;
+  *launches += 2;
+  return launch_k(chunk_tc_join_kernel<DH>, dim3(std::max(1, p.runs - 1), CJ_SPLIT), dim3(256), 0, st, p);
+}
+
+}  // namespace
+
+bool chunk_tc_takes(const KvPaged& c, int n_heads, int max_kv) {
+  const long long blocks = c.type == KV_E4M3 ? (long long)c.n_seq * cdiv(max_kv, 16) : c.n_blocks;
+  return c.type != KV_F32 && c.block_tokens == 16 && (c.head_dim == 64 || c.head_dim == 128) &&
+         n_heads / c.n_kv_heads <= CT_BM && blocks * c.n_kv_heads * 16 < (1ll << 31) && c.n_seq < 65536 && tc_gemm_supported();
+}
+
+size_t chunk_tc_workspace(const KvPaged& c, int max_kv) { return ct_parts_bytes(c.head_dim) + 2 * ct_wide_bytes(c, max_kv); }
 
 cudaError_t launch_chunk_tc(cudaStream_t st, const ChunkCall& a, int* launches) {
   CtParams p;
@@ -865,17 +825,8 @@ cudaError_t launch_chunk_tc(cudaStream_t st, const ChunkCall& a, int* launches) 
   p.a = a;
   p.ts = CT_BM / (a.n_heads / a.c.n_kv_heads);
   p.runs = ct_sms();
-  const int dh = a.c.head_dim;
-  p.no_err = (unsigned*)(a.part + ct_ws_floats(p.runs, dh));
-  if (a.c.type == KV_BF16) {
-    const uint64_t rows = (uint64_t)a.c.n_blocks * a.c.n_kv_heads * 16;
-    if (!tc_encode_2d(&p.kmap, a.c.k, (uint64_t)dh, rows, (uint64_t)dh * 2, 16) ||
-        !tc_encode_2d(&p.vmap, a.c.v, (uint64_t)dh, rows, (uint64_t)dh * 2, 16))
-      return cudaErrorInvalidValue;
-  }
-  *launches = 2;
-  if (a.c.type == KV_BF16) return dh == 128 ? launch_t<128, KV_BF16>(st, p) : launch_t<64, KV_BF16>(st, p);
-  return dh == 128 ? launch_t<128, KV_E4M3>(st, p) : launch_t<64, KV_E4M3>(st, p);
+  p.no_err = (unsigned*)(a.part + ct_ws_floats(p.runs, a.c.head_dim));
+  return a.c.head_dim == 128 ? launch_t<128>(st, p, launches) : launch_t<64>(st, p, launches);
 }
 
 ADEPT_WAIT_LIMIT_SETTER(ct)

@@ -99,7 +99,7 @@ adept_status adept_kv_gather(const adept_kv_cache* c, int n_rows, int dtype, voi
 int64_t adept_chunk_attention_workspace(const adept_kv_cache* c, int n_heads, int n_rows, int max_q_len, int max_kv_len) {
   KvPaged v;
   if (view_of(c, &v) != ADEPT_OK || call_ok(v, n_heads, n_rows, max_q_len, max_kv_len) != ADEPT_OK) return -1;
-  return (int64_t)chunk_workspace(v, n_heads, n_rows, max_q_len, max_kv_len);
+  return (int64_t)chunk_workspace(v, n_heads, max_q_len, max_kv_len);
 }
 
 adept_status adept_chunk_attention(const adept_kv_cache* c, int n_heads, int n_rows, const void* d_q, int64_t ld_q,
@@ -115,7 +115,7 @@ adept_status adept_chunk_attention(const adept_kv_cache* c, int n_heads, int n_r
   if (ld_q < w || ld_out < w) return bad(ADEPT_ERR_INVALID_ARG, "row stride below the %lld elements of a row", (long long)w);
   const uintptr_t m = a.c.type == KV_F32 ? 3 : 1;
   if (((uintptr_t)d_q | (uintptr_t)d_out) & m) return bad(ADEPT_ERR_INVALID_ARG, "misaligned rows");
-  const int64_t need = (int64_t)chunk_workspace(a.c, n_heads, n_rows, max_q_len, max_kv_len);
+  const int64_t need = (int64_t)chunk_workspace(a.c, n_heads, max_q_len, max_kv_len);
   if (need > 0 && (!d_ws || ws_bytes < need || ((uintptr_t)d_ws & 15)))
     return bad(ADEPT_ERR_INVALID_ARG, "workspace of %lld bytes, on 16 bytes, needed (adept_chunk_attention_workspace)", (long long)need);
   a.q = d_q;

@@ -40,14 +40,15 @@ struct ChunkCall {
   const int* q_start;
   const int* kv_len;
   int n_rows, n_heads, max_q, max_kv;
+  int c_lo, c_hi;     // the launch's sequences: those with c_lo to c_hi new tokens
   float scale_log2;   // log2(e) / sqrt(head_dim)
   float* part;        // workspace
 };
-size_t chunk_workspace(const KvPaged& c, int n_heads, int n_rows, int max_q, int max_kv);
+size_t chunk_workspace(const KvPaged& c, int n_heads, int max_q, int max_kv);
 cudaError_t launch_chunk_attention(cudaStream_t st, const ChunkCall& a, int* launches);
 // The tcgen05 kernel (attention_chunk_tc.cu): what it takes (rows on 16 bytes besides), its workspace, its launches.
-bool chunk_tc_takes(const KvPaged& c, int n_heads);
-size_t chunk_tc_workspace(const KvPaged& c);
+bool chunk_tc_takes(const KvPaged& c, int n_heads, int max_kv);
+size_t chunk_tc_workspace(const KvPaged& c, int max_kv);
 cudaError_t launch_chunk_tc(cudaStream_t st, const ChunkCall& a, int* launches);
 cudaError_t set_wait_limit_ct(long long cycles);
 cudaError_t set_wait_limit_cf(long long cycles);
@@ -70,7 +71,7 @@ struct SplitItem {
   int slot0;                  // slot of the tile's first split
 };
 
-// Lengths of sequence b, or no work (c = 0) where they are out of bounds.
+// Lengths of sequence b, or no work (c = 0) where they are out of bounds or not this launch's.
 __device__ __forceinline__ void chunk_seq(const ChunkCall& a, int b, int& q0, int& c, int& len) {
   q0 = a.q_start[b];
   c = a.q_start[b + 1] - q0;
@@ -79,8 +80,9 @@ __device__ __forceinline__ void chunk_seq(const ChunkCall& a, int b, int& q0, in
   if (q0 < 0 || c < 0 || c > a.max_q || q0 > a.n_rows - c || len < 0 || len > cap) {
     a.c.flag(ERRW_POS);
     c = 0;
-    len = 0;
   }
+  if (c < a.c_lo || c > a.c_hi) c = 0;
+  if (c == 0) len = 0;
 }
 
 // Item `id` of the plan (joined: tile `id`, its splits taken together), looked up by one converged warp; false: none.  32-bit
