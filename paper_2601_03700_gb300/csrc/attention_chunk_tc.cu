@@ -10,7 +10,7 @@
 //                       maximum (raised only by more than 2^8), exp2, sum, P to tensor memory; at the end O / l
 //          8            issues the matrix instructions:  PV_0(j) S_0(j+1) PV_1(j) S_1(j+1)  (in issue order on the tensor
 //                       core, so S_0(j+1) may overwrite P_0(j), and a completed S(j+1) means a completed PV(j))
-//          9, 10        fetch K and V blocks by TMA; 10 mends the V tiles at the causal edge
+//          9, 10        fetch K and V blocks by TMA; 10 mends the V tiles at the causal edge (11: idle)
 //
 // The causal edge: from the first row's position on, a key tile holds keys that not every row attends, or none does.  Scores are
 // masked there.  V entries that nobody attends become zero; a NaN or infinite one is replaced by zero and its key noted per
@@ -42,16 +42,18 @@ constexpr long long CT_DRAIN_CYCLES = 4000000000LL;
 
 template <int DH>
 struct CtShape {
-  static constexpr int THREADS = 11 * 32;
+  static constexpr int THREADS = 12 * 32;   // (three whole warpgroups, for setmaxnreg)
   static constexpr int HALVES = DH / 64;
   static constexpr int Q_BYTES = HALVES * CT_BM * 128;             // one sub-tile: [half][row][128 B]
   static constexpr int KV_BYTES = HALVES * CT_BN * 128;            // one K or V stage: [half][key][128 B]
-  static constexpr int OFF_K = 2 * Q_BYTES, OFF_V = OFF_K + 2 * KV_BYTES, TOTAL = OFF_V + 2 * KV_BYTES;
+  static constexpr int OFF_K = 2 * Q_BYTES, OFF_V = OFF_K + 2 * KV_BYTES, OFF_ST = OFF_V + 2 * KV_BYTES;
+  static constexpr int TOTAL = OFF_ST + 8 * 2048;                  // 32 rows x 64 bytes of output per softmax warp
 };
 
 struct CtParams {
   ChunkCall a;
-  CUtensorMap kmap, vmap;   // bf16: the pools as [n_blocks * n_kv_heads * 16][d_h], box {64, 16}
+  CUtensorMap kmap, vmap;   // K and V as [n_blocks * n_kv_heads * 16][d_h], box {64, 16}
+  CUtensorMap qmap;         // Q as [n_rows][n_heads][d_h], box {64, heads of a group, ts}
   int ts;                   // tokens of a sub-tile
   int runs;                 // CTAs
   int wide;                 // > 0: the maps are of widened entries, `wide` blocks per sequence in order
@@ -106,9 +108,9 @@ __device__ long long ct_total(const ChunkCall& a, int tq) {
     chunk_seq(a, b, q0, c, len);
     tot += ct_seq_units(c, len, tq) * a.c.n_kv_heads;
   }
-#pragma unroll
-  for (int o = 16; o; o >>= 1) tot += __shfl_xor_sync(0xffffffffu, tot, o);
-  return tot;
+  // (24 bits and the rest: one instruction each)
+  return __reduce_add_sync(0xffffffffu, (unsigned)(tot & 0xffffff)) +
+         ((long long)__reduce_add_sync(0xffffffffu, (unsigned)(tot >> 24)) << 24);
 }
 // The tile that unit u lies in.
 __device__ void ct_find(const ChunkCall& a, int tq, long long u, CtTile& x) {
@@ -160,6 +162,18 @@ __device__ void ct_find(const ChunkCall& a, int tq, long long u, CtTile& x) {
     }
     return;
   }
+}
+// The tile behind x.
+__device__ __forceinline__ void ct_next(const ChunkCall& a, int tq, CtTile& x) {
+  x.u0 += x.units;
+  if (++x.kvh < a.c.n_kv_heads) return;
+  x.kvh = 0;
+  if (++x.tile * tq >= x.c) {
+    x.tile = 0;
+    x.c = 0;
+    while (x.c == 0 && ++x.seq < a.c.n_seq) chunk_seq(a, x.seq, x.q0, x.c, x.len);
+  }
+  x.units = ct_units(x.c, x.len, tq, x.tile);
 }
 // Run i of `runs` (fewer where there are few units).
 constexpr int CT_MIN_RUN = 2;
@@ -220,10 +234,6 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
   return r;
 }
-// 16 bytes of global memory to shared memory, zeros where `on` is false.
-__device__ __forceinline__ void cp_async16(void* dst, const void* src, bool on) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(dst)), "l"(src), "r"(on ? 16 : 0) : "memory");
-}
 
 // A CTA's part of one tile: key tiles j_lo .. j_hi.
 struct CtSeg {
@@ -231,9 +241,24 @@ struct CtSeg {
   int j_lo, j_hi, past, t0, n_tok;
   int lim_lo, k_end;   // keys of the tile's first and of its last token (nobody attends beyond)
   int nt0, nt1, n_it;  // key tiles with keys: per sub-tile, of the segment
-  int slot;
   bool whole;          // the whole tile
   const int* table;
+  __device__ __forceinline__ void set(const ChunkCall& a, int ts, const CtTile& tile, long long u, long long u_end) {
+    x = tile;
+    j_lo = (int)(u - x.u0);
+    j_hi = (int)min((long long)x.units, u_end - x.u0);
+    whole = j_lo == 0 && j_hi == x.units;
+    past = x.len - x.c;
+    t0 = x.tile * 2 * ts;
+    n_tok = min(2 * ts, x.c - t0);
+    lim_lo = max(past + t0 + 1, 0);
+    k_end = max(past + t0 + n_tok, 0);
+    const int k_end0 = max(past + t0 + min(ts, n_tok), 0);
+    nt0 = max(min(j_hi, (k_end0 + CT_BN - 1) / CT_BN) - j_lo, 0);
+    nt1 = n_tok > ts ? max(min(j_hi, (k_end + CT_BN - 1) / CT_BN) - j_lo, 0) : 0;
+    n_it = max(nt0, nt1);
+    table = a.c.table + (size_t)x.seq * a.c.max_blocks;
+  }
   __device__ __forceinline__ int nt(int sub) const { return sub ? nt1 : nt0; }
   // key tile j (from the segment's first) holds keys that are not everybody's
   __device__ __forceinline__ bool edge(int j) const { return (j_lo + j + 1) * CT_BN > lim_lo || (j_lo + j + 1) * CT_BN > k_end; }
@@ -246,16 +271,29 @@ struct CtSeg {
   }
 };
 
+__device__ __forceinline__ void tma_load_q(const CUtensorMap* tm, uint64_t* bar, void* dst, int col, int head, int row) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(
+          smem_u32(dst)),
+      "l"((uint64_t)tm), "r"(col), "r"(head), "r"(row), "r"(smem_u32(bar)));
+}
+
+// The segments of a CTA follow each other without a stop: every role walks the tiles by itself, and meets the others at
+// barriers only: Q full / free, a K or V stage full / free, S, P (two halves), O.  (With a stop of all warps, a
+// look-up and Q's loads by all threads at each of a run's two or three segments, a call of ten key tiles a CTA took 70000
+// cycles, 27000 of them on key tiles.)
 template <int DH>
 __global__ void __launch_bounds__(CtShape<DH>::THREADS, 1) chunk_tc_kernel(const __grid_constant__ CtParams p) {
   using L = CtShape<DH>;
   extern __shared__ __align__(1024) uint8_t ct_raw[];
-  __shared__ __align__(8) uint64_t k_full[2], v_full[2], k_empty[2], v_empty[2], s_full[2], p_half[2], p_full[2], o_full[2], v_fix[2], drain;
+  __shared__ __align__(8) uint64_t q_full, q_free, k_full[2], v_full[2], k_empty[2], v_empty[2], s_full[2], p_half[2], p_full[2],
+      o_full[2], v_fix[2], drain;
   __shared__ uint32_t s_tmem;
-  __shared__ int s_abort, s_poisoned;
+  __shared__ int s_abort;
   __shared__ int s_gone[4];      // blocks of a key tile that are not there, by tile % 4
+  __shared__ int s_pk[4][DH];    // least key with a non-finite V entry, per column (causal edge), by segment with keys % 4
+  __shared__ int s_poisoned[4];
   __shared__ int s_tok[CT_ROWS], s_off[CT_ROWS];   // token of a row in the tile (-1: none), its head's first column in the group
-  __shared__ int s_pk[DH];   // least key with a non-finite V entry, per column (causal edge)
   __shared__ CtTile s_tile;
   __shared__ long long s_u0, s_u1;
 
@@ -268,6 +306,8 @@ __global__ void __launch_bounds__(CtShape<DH>::THREADS, 1) chunk_tc_kernel(const
   unsigned* err = a.c.err ? a.c.err : p.no_err;
 
   if (tid == 0) {
+    mbar_init(&q_full, 1);
+    mbar_init(&q_free, 1);
     for (int s = 0; s < 2; ++s) {
       mbar_init(&k_full[s], 1);
       mbar_init(&v_full[s], 1);
@@ -283,116 +323,70 @@ __global__ void __launch_bounds__(CtShape<DH>::THREADS, 1) chunk_tc_kernel(const
     s_abort = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
+  const int group = a.n_heads / a.c.n_kv_heads, ts = p.ts, tq = 2 * ts, run = (int)blockIdx.x;
   if (warp == 8) {
     tmem_alloc(&s_tmem, 512);
     tmem_relinquish();
   }
+  if (warp < 8) {   // (a row per thread)
+    const int rr = tid & 127, tk = rr / group;
+    s_tok[tid] = tk < ts ? (tid >> 7) * ts + tk : -1;
+    s_off[tid] = rr % group * DH;
+  }
   pdl_wait();
+  if (warp == 9) {
+    const long long tot = ct_total(a, tq);
+    const int runs = ct_runs(tot, p.runs);
+    const long long u0 = run < runs ? ct_start(tot, runs, run) : 0, u1 = run < runs ? ct_start(tot, runs, run + 1) : 0;
+    CtTile x{};
+    if (u0 < u1) ct_find(a, tq, u0, x);
+    if (lane == 0) {
+      s_u0 = u0;
+      s_u1 = u1;
+      s_tile = x;
+      // the join's note: what tile this run begins inside of
+      const int t0 = x.tile * tq;
+      CtWs(p).note[run] = CtNote{u0 < u1 && u0 > x.u0 ? x.u0 : -1, x.q0 + t0, x.kvh, x.len - x.c + t0, min(tq, x.c - t0), {0, 0}};
+    }
+  }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   pdl_launch_dependents();   // after the tensor memory is held
   const uint32_t tmem = s_tmem;
-
-  const int group = a.n_heads / a.c.n_kv_heads, ts = p.ts, tq = 2 * ts;
-  if (warp == 0) {
-    const long long tot = ct_total(a, tq);
-    if (lane == 0) {
-      const int runs = ct_runs(tot, p.runs), run = (int)blockIdx.x;
-      s_u0 = run < runs ? ct_start(tot, runs, run) : 0;
-      s_u1 = run < runs ? ct_start(tot, runs, run + 1) : 0;
-      if (run >= runs) CtWs(p).note[run].u0 = -1;
-    }
-  } else if (warp < 9) {
-    const int r = tid - 32, rr = r & 127, tk = rr / group;   // (a row per thread of warps 1..8)
-    s_tok[r] = tk < ts ? (r >> 7) * ts + tk : -1;
-    s_off[r] = rr % group * DH;
-  }
-  __syncthreads();
-  const int run = (int)blockIdx.x;
   const long long u_end = s_u1;
   long long u = s_u0;
-  bool first_seg = true;
+  CtTile x = s_tile;
+  CtSeg g{};
+  bool ok = true;
 
-  // Entered by every warp with the segment before it behind: the one that begins with unit u.  Warps 0..8 leave with its Q in
-  // place (rows (token, head of the group), 16-byte pieces at their swizzled places, rows that hold nothing zero).
-  auto begin = [&](CtSeg& g) {
-    if (warp == 0) {
-      CtTile x{};
-      ct_find(a, tq, u, x);
-      if (lane == 0) s_tile = x;
-    }
-    if (tid == 0) s_poisoned = 0;
-    if (tid < DH) s_pk[tid] = 0x7fffffff;
-    __syncthreads();
-    g.x = s_tile;
-    g.j_lo = (int)(u - g.x.u0);
-    g.j_hi = (int)min((long long)g.x.units, u_end - g.x.u0);
-    g.whole = g.j_lo == 0 && g.j_hi == g.x.units;
-    g.slot = run * 2 + (g.j_lo == 0 ? 1 : 0);
-    g.past = g.x.len - g.x.c;
-    g.t0 = g.x.tile * tq;
-    g.n_tok = min(tq, g.x.c - g.t0);
-    g.lim_lo = max(g.past + g.t0 + 1, 0);
-    g.k_end = max(g.past + g.t0 + g.n_tok, 0);
-    const int k_end0 = max(g.past + g.t0 + min(ts, g.n_tok), 0);
-    g.nt0 = max(min(g.j_hi, (k_end0 + CT_BN - 1) / CT_BN) - g.j_lo, 0);
-    g.nt1 = g.n_tok > ts ? max(min(g.j_hi, (g.k_end + CT_BN - 1) / CT_BN) - g.j_lo, 0) : 0;
-    g.n_it = max(g.nt0, g.nt1);
-    g.table = a.c.table + (size_t)g.x.seq * a.c.max_blocks;
-    if (first_seg && tid == 0)
-      CtWs(p).note[run] = CtNote{g.j_lo > 0 ? g.x.u0 : -1, g.x.q0 + g.t0, g.x.kvh, g.past + g.t0, g.n_tok, {0, 0}};
-    first_seg = false;
-    if (warp < 9) {
-      const bf16* q = (const bf16*)a.q + (size_t)(g.x.q0 + g.t0) * a.ld_q + (size_t)g.x.kvh * group * DH;
-      const int live = g.n_tok > ts ? CT_ROWS : CT_BM;
-#pragma unroll 4
-      for (int i = tid; i < live * (DH / 8); i += 9 * 32) {
-        const int r = i / (DH / 8), ch = i % (DH / 8), rr = r & 127, tk = s_tok[r];
-        const bool on = tk >= 0 && tk < g.n_tok;
-        cp_async16(sQ + (r >> 7) * L::Q_BYTES + (ch >> 3) * CT_BM * 128 + rr * 128 + (((ch & 7) ^ (rr & 7)) << 4),
-                   q + (on ? tk * a.ld_q + s_off[r] + ch * 8 : 0), on);
-      }
-      asm volatile("cp.async.wait_all;" ::: "memory");
-      fence_async_shared();
-      tc_fence_before();
-      asm volatile("bar.sync 1, 288;" ::: "memory");
-      tc_fence_after();
-    }
-  };
-  // Every warp is through with the segment; false: a role gave up, everybody leaves.
-  auto end = [&](const CtSeg& g, bool ok) {
-    u = g.x.u0 + g.j_hi;
-    tc_fence_before();
-    const bool stop = __syncthreads_or(!ok) != 0;
-    tc_fence_after();
-    return !stop;
-  };
-
+  // 384 x 168 registers at launch: 256 x 208 + 128 x 88
   if (warp < 8) {
     // ---- softmax of a row per thread
-    const int sub = warp >> 2, r = tid & 127;
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+    const int sub = warp >> 2, r = tid & 127, tok = s_tok[tid];
     const uint32_t base = tmem + ((uint32_t)((warp & 3) * 32) << 16), s_col = base + (uint32_t)(sub * 128),
                    o_col = base + 256u + (uint32_t)(sub * 128);
     const float sc = a.scale_log2;
+    const CtWs ws(p);
+    uint8_t* stage = sm + L::OFF_ST + warp * 2048;
     int ns = 0, no = 0, kt = 0;   // S tiles, outputs, key tiles so far
-    CtSeg g{};
-    bool ok = true;
+    int seg = -1;   // segments with keys so far
     while (u < u_end) {
-      begin(g);
-      const int tok = s_tok[sub * 128 + r];
+      g.set(a, ts, x, u, u_end);
+      seg += g.n_it > 0;
       const bool mine = tok >= 0 && tok < g.n_tok;
       const int lim = mine ? max(g.past + g.t0 + tok + 1, 0) : 0;
       const int sub_lo = max(g.past + g.t0 + sub * ts + 1, 0);   // keys of the sub-tile's first token
       const int n_my = g.nt(sub);
       float m = -INFINITY, l = 0.f;
-      for (int j = 0; j < n_my; ++j, ++kt) {
+      for (int j = 0; j < n_my; ++j) {
         if (!(ok = mbar_wait_warp(&s_full[sub], (uint32_t)(ns & 1), abort_flag, err, wlim))) break;
         ++ns;
         tc_fence_after();
         float s[CT_BN];
         tmem_ld128(s_col, s);
-        const int k0 = (g.j_lo + j) * CT_BN, gone = s_gone[kt & 3];
+        const int k0 = (g.j_lo + j) * CT_BN, gone = s_gone[(kt + j) & 3];
         if (k0 + CT_BN > sub_lo || gone) {
           const int nk_r = lim - k0;
 #pragma unroll
@@ -451,77 +445,75 @@ __global__ void __launch_bounds__(CtShape<DH>::THREADS, 1) chunk_tc_kernel(const
         f2_unpack(f2_add(f2_add(sum[0], sum[1]), f2_add(sum[2], sum[3])), l0, l1);
         l += l0 + l1;
       }
-      if (ok) kt += g.n_it - n_my;   // (the segment's key tiles: what s_gone goes by)
+      if (!ok) break;
+      kt += g.n_it;   // (the segment's key tiles: what s_gone goes by)
       // O / l, or the part
-      if (ok && n_my > 0) {
-        ok = mbar_wait_warp(&o_full[sub], (uint32_t)(no & 1), abort_flag, err, wlim);
+      float v[DH];
+      if (n_my > 0) {   // (the same for the whole warp)
+        if (!(ok = mbar_wait_warp(&o_full[sub], (uint32_t)(no & 1), abort_flag, err, wlim))) break;
         ++no;
+        tc_fence_after();
+        if constexpr (DH == 128) tmem_ld128(o_col, v);
+        else tmem_ld64(o_col, v);
+      } else {
+#pragma unroll
+        for (int e = 0; e < DH; ++e) v[e] = 0.f;
       }
-      tc_fence_after();
-      const bool poisoned = s_poisoned != 0;
-      const float inv = lim == 0 ? 0.f : 1.f / l;
-      const CtWs ws(p);
-      if (!g.whole && mine && ok) *ws.ml_at(g.slot, sub * 128 + r) = make_float2(m, l);
-      // (a finished tile's rows go through the warp's 32 rows of Q's place, so that whole lines are written)
-      uint8_t* stage = sQ + sub * L::Q_BYTES + (warp & 3) * 32 * (DH * 2);
-      const bool any = sub == 0 || g.n_tok > ts;
-#pragma unroll 1
-      for (int c = 0; any && c < DH / 32; ++c) {
-        float v[32];
-        if (n_my > 0) {   // (the same for the whole warp)
-          tmem_ld32(o_col + (uint32_t)(c * 32), v);
-        } else {
+      if (n_my > 0 && s_poisoned[seg & 3]) {
 #pragma unroll
-          for (int e = 0; e < 32; ++e) v[e] = 0.f;
-        }
-        if (poisoned) {
-#pragma unroll
-          for (int e = 0; e < 32; ++e)
-            if (s_pk[c * 32 + e] < lim) v[e] = NAN;
-        }
+        for (int e = 0; e < DH; ++e)
+          if (s_pk[seg & 3][e] < lim) v[e] = NAN;
+      }
+      if (sub == 0 || g.n_tok > ts) {
         if (g.whole) {
+          // through the warp's stage, 32 columns at a time, so that whole sectors are written
+          const float inv = lim == 0 ? 0.f : 1.f / l;
+          bf16* out = (bf16*)a.out + (size_t)(g.x.q0 + g.t0) * a.ld_out + (size_t)g.x.kvh * group * DH;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            uint32_t w[4];
+          for (int c = 0; c < DH / 32; ++c) {
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-              const __nv_bfloat162 pr = __floats2bfloat162_rn(v[8 * e + 2 * q] * inv, v[8 * e + 2 * q + 1] * inv);
-              w[q] = *reinterpret_cast<const uint32_t*>(&pr);
+            for (int e = 0; e < 4; ++e) {
+              uint32_t w[4];
+#pragma unroll
+              for (int q = 0; q < 4; ++q) {
+                const __nv_bfloat162 pr = __floats2bfloat162_rn(v[c * 32 + 8 * e + 2 * q] * inv, v[c * 32 + 8 * e + 2 * q + 1] * inv);
+                w[q] = *reinterpret_cast<const uint32_t*>(&pr);
+              }
+              *reinterpret_cast<uint4*>(stage + lane * 64 + ((e ^ ((lane >> 1) & 3)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
             }
-            *reinterpret_cast<uint4*>(stage + lane * (DH * 2) + (((c * 4 + e) ^ (lane & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
-          }
-        } else if (mine && ok) {
+            __syncwarp();
 #pragma unroll
-          for (int e = 0; e < 8; ++e)
-            *ws.o_at(g.slot, DH, c * 8 + e, sub * 128 + r) = make_float4(v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]);
+            for (int k = 0; k < 4; ++k) {
+              const int rr = k * 8 + (lane >> 2), pc = lane & 3, row = warp * 32 + rr, tk = s_tok[row];
+              if (tk >= 0 && tk < g.n_tok)
+                *reinterpret_cast<uint4*>(out + tk * a.ld_out + s_off[row] + c * 32 + pc * 8) =
+                    *reinterpret_cast<const uint4*>(stage + rr * 64 + ((pc ^ ((rr >> 1) & 3)) << 4));
+            }
+            __syncwarp();
+          }
+        } else if (mine) {
+          const int slot = run * 2 + (g.j_lo == 0 ? 1 : 0);
+          *ws.ml_at(slot, sub * 128 + r) = make_float2(m, l);
+#pragma unroll
+          for (int e = 0; e < DH / 4; ++e)
+            *ws.o_at(slot, DH, e, sub * 128 + r) = make_float4(v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]);
         }
-        __syncwarp();
       }
-      if (any && g.whole && ok) {
-        bf16* out = (bf16*)a.out + (size_t)(g.x.q0 + g.t0) * a.ld_out + (size_t)g.x.kvh * group * DH;
-        constexpr int PR = DH / 8;   // 16-byte pieces of a row
-#pragma unroll 4
-        for (int i = lane; i < 32 * PR; i += 32) {
-          const int rr = i / PR, pc = i % PR, row = (warp & 7) * 32 + rr, tk = s_tok[row];
-          if (tk >= 0 && tk < g.n_tok)
-            *reinterpret_cast<uint4*>(out + tk * a.ld_out + s_off[row] + pc * 8) =
-                *reinterpret_cast<const uint4*>(stage + rr * (DH * 2) + ((pc ^ (rr & 7)) << 4));
-        }
-      }
-      if (!end(g, ok)) break;
+      ct_next(a, tq, x);
+      u = x.u0;
     }
   } else if (warp == 8) {
-    // ---- matrix instructions: one thread for a whole segment (a warp that meets at every wait took 3900 cycles a key tile to
-    // issue what the tensor core does in 2048), descriptors made once and moved by their address field
+    // ---- matrix instructions: one thread (a warp that meets at every wait took 3900 cycles a key tile to issue what the tensor
+    // core does in 2048), descriptors made once and moved by their address field
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
     constexpr uint32_t IDESC_S = umma_idesc(CT_BN, false), IDESC_O = umma_idesc(DH, true);
     const uint64_t dq = sdesc_sw128(smem_u32(sQ)), dk = sdesc_sw128(smem_u32(sK)), dv = sdesc_mn_sw128(smem_u32(sV), CT_BN * 128);
-    int nk = 0, nv = 0, np[2] = {0, 0}, nf[2] = {0, 0};   // K, V, P tiles and mended V tiles (per stage) so far
-    CtSeg g{};
-    bool ok = true;
-    while (u < u_end) {
-      begin(g);
-      if (elect_one()) {
-        auto wait = [&](uint64_t* bar, int phase) { return ok = mbar_wait(bar, (uint32_t)(phase & 1), abort_flag, err, wlim); };
+    if (elect_one()) {
+      int nq = 0, nk = 0, nv = 0, np[2] = {0, 0}, nf[2] = {0, 0};   // Q, K, V, P so far, mended V per stage
+      auto wait = [&](uint64_t* bar, int phase) { return ok = mbar_wait(bar, (uint32_t)(phase & 1), abort_flag, err, wlim); };
+      while (u < u_end && ok) {
+        g.set(a, ts, x, u, u_end);
+        if (g.n_it > 0 && !wait(&q_full, nq++)) break;
         for (int j = -1; j < g.n_it; ++j) {
           const int kn = nk, vn = nv, ks = kn & 1, vs = vn & 1;
           if (j + 1 < g.n_it) {
@@ -539,6 +531,7 @@ __global__ void __launch_bounds__(CtShape<DH>::THREADS, 1) chunk_tc_kernel(const
             if (j >= 0 && j < g.nt(sub)) {
               const uint32_t pa = tmem + (uint32_t)(sub * 128), oa = tmem + 256u + (uint32_t)(sub * 128);
               if (!wait(&p_half[sub], np[sub])) break;
+              // (a P of this segment: its warps have read O of the segment before)
               tc_fence_after();
 #pragma unroll
               for (int kk = 0; kk < 4; ++kk)
@@ -548,8 +541,8 @@ __global__ void __launch_bounds__(CtShape<DH>::THREADS, 1) chunk_tc_kernel(const
 #pragma unroll
               for (int kk = 4; kk < 8; ++kk)
                 umma_bf16_ts(oa, pa + (uint32_t)(kk * 8), dvs + (uint64_t)(kk * (16 * 128 >> 4)), IDESC_O, 1u);
-              if (j == g.nt(sub) - 1) umma_commit(&o_full[sub]);
               ++np[sub];
+              if (j == g.nt(sub) - 1) umma_commit(&o_full[sub]);
             }
             if (j + 1 < g.nt(sub)) {
               tc_fence_after();
@@ -563,31 +556,31 @@ __global__ void __launch_bounds__(CtShape<DH>::THREADS, 1) chunk_tc_kernel(const
           }
           if (!ok) break;
           if (j + 1 < g.n_it) umma_commit(&k_empty[ks]);
+          if (j + 1 == g.n_it - 1) umma_commit(&q_free);   // the segment's last S
           if (j >= 0) umma_commit(&v_empty[vs]);
         }
+        ct_next(a, tq, x);
+        u = x.u0;
       }
-      __syncwarp();
-      if (!end(g, ok)) break;
-    }
-    // every matrix instruction has completed before tensor memory is given back
-    if (elect_one()) {
+      // every matrix instruction has completed before tensor memory is given back
       umma_commit(&drain);
       const long long c0 = clock64();
       while (!mbar_try_wait(&drain, 0) && clock64() - c0 < CT_DRAIN_CYCLES) {
       }
     }
     __syncwarp();
+  } else if (warp == 11) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
   } else {
-    // ---- TMA producers: K (warp 9), V (warp 10, which also mends the V tiles at the edge)
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+    // ---- TMA producers: Q and K (warp 9), V (warp 10, which also mends the V tiles at the edge)
     const bool kw = warp == 9;
     uint64_t *full = kw ? k_full : v_full, *empty = kw ? k_empty : v_empty;
     const CUtensorMap* map = kw ? &p.kmap : &p.vmap;
     uint8_t* dst0 = kw ? sK : sV;
-    int cnt = 0;   // tiles sent so far
-    CtSeg g{};
-    bool ok = true;
+    int cnt = 0, nq = 0;   // tiles, Qs sent so far
     // V tile j (the vi-th, blocks `gone` of it not there): entries nobody attends to zero, non-finite ones noted
-    auto mend = [&](int j, int vi, int gone) {
+    auto mend = [&](int j, int vi, int gone, int par) {
       const int s = vi & 1;
       if (!mbar_wait_warp(&v_full[s], (uint32_t)((vi >> 1) & 1), abort_flag, err, wlim)) return false;
       uint8_t* v = sV + s * L::KV_BYTES;
@@ -618,9 +611,9 @@ __global__ void __launch_bounds__(CtShape<DH>::THREADS, 1) chunk_tc_kernel(const
             *piece(q >> 2, key, lane & 7) = make_uint4(y[q].x & ~b[0], y[q].y & ~b[1], y[q].z & ~b[2], y[q].w & ~b[3]);
 #pragma unroll
             for (int e = 0; e < 8; ++e)
-              if (b[e >> 1] >> ((e & 1) * 16) & 1) atomicMin(&s_pk[col + e], k0 + key);
+              if (b[e >> 1] >> ((e & 1) * 16) & 1) atomicMin(&s_pk[par][col + e], k0 + key);
           }
-          s_poisoned = 1;
+          s_poisoned[par] = 1;
         }
       }
       fence_async_shared();
@@ -628,12 +621,14 @@ __global__ void __launch_bounds__(CtShape<DH>::THREADS, 1) chunk_tc_kernel(const
       if (lane == 0) mbar_arrive(&v_fix[s]);
       return true;
     };
-    while (u < u_end) {
-      begin(g);
+    int seg = -1;   // segments with keys so far
+    while (u < u_end && ok) {
+      g.set(a, ts, x, u, u_end);
+      seg += g.n_it > 0;
       int gone = 0, gone_prev = 0;
       for (int j = 0; j <= g.n_it && ok; ++j) {
         gone_prev = gone;
-        if (!kw && j > 0 && (g.edge(j - 1) || gone_prev) && !(ok = mend(j - 1, cnt - 1, gone_prev))) break;
+        if (!kw && j > 0 && (g.edge(j - 1) || gone_prev) && !(ok = mend(j - 1, cnt - 1, gone_prev, seg & 3))) break;
         if (j == g.n_it) break;
         const int s = cnt & 1, row = lane < 8 ? g.row_of(a.c, p.wide, (g.j_lo + j) * 8 + lane) : -1;
         const unsigned on = __ballot_sync(0xffffffffu, row >= 0);
@@ -643,6 +638,11 @@ __global__ void __launch_bounds__(CtShape<DH>::THREADS, 1) chunk_tc_kernel(const
 #pragma unroll
         for (int b = 0; b < 8; ++b) rows8[b] = __shfl_sync(0xffffffffu, row, b);
         if (cnt >= 2 && !(ok = mbar_wait_warp(&empty[s], (uint32_t)(((cnt >> 1) - 1) & 1), abort_flag, err, wlim))) break;
+        if (!kw && j == 0) {   // the segment's notes (V of two tiles ago is through, so the segment before the last is written)
+          for (int e = lane; e < DH; e += 32) s_pk[seg & 3][e] = 0x7fffffff;
+          if (lane == 0) s_poisoned[seg & 3] = 0;
+          __syncwarp();
+        }
         if (elect_one()) {
           if (kw) s_gone[cnt & 3] = gone;   // (tile cnt - 4 is through: its K stage has been freed twice over)
           // (blocks that are not fetched leave the stage's old contents: masked in S, mended in V)
@@ -654,8 +654,21 @@ __global__ void __launch_bounds__(CtShape<DH>::THREADS, 1) chunk_tc_kernel(const
         }
         __syncwarp();
         ++cnt;
+        if (kw && j == 0) {   // Q, once S of the segment before is through
+          if (nq > 0 && !(ok = mbar_wait_warp(&q_free, (uint32_t)((nq - 1) & 1), abort_flag, err, wlim))) break;
+          if (elect_one()) {
+            const int subs = g.n_tok > ts ? 2 : 1;
+            mbar_expect_tx(&q_full, (uint32_t)(subs * L::HALVES * ts * group * 128));
+            for (int b = 0; b < subs; ++b)
+              for (int hf = 0; hf < L::HALVES; ++hf)
+                tma_load_q(&p.qmap, &q_full, sQ + b * L::Q_BYTES + hf * CT_BM * 128, hf * 64, g.x.kvh * group, g.x.q0 + g.t0 + b * ts);
+          }
+          __syncwarp();
+          ++nq;
+        }
       }
-      if (!end(g, ok)) break;
+      ct_next(a, tq, x);
+      u = x.u0;
     }
     // every copy sent has landed before the CTA ends
     if (lane == 0) {
@@ -663,6 +676,9 @@ __global__ void __launch_bounds__(CtShape<DH>::THREADS, 1) chunk_tc_kernel(const
         const long long c0 = clock64();
         while (!mbar_try_wait(&full[t & 1], (uint32_t)((t >> 1) & 1)) && clock64() - c0 < CT_DRAIN_CYCLES) {
         }
+      }
+      const long long c0 = clock64();
+      while (nq > 0 && !mbar_try_wait(&q_full, (uint32_t)((nq - 1) & 1)) && clock64() - c0 < CT_DRAIN_CYCLES) {
       }
     }
     __syncwarp();
@@ -802,7 +818,12 @@ cudaError_t launch_t(cudaStream_t st, CtParams& p, int* launches) {
     if (e != cudaSuccess) return e;
     ++*launches;
   }
-  if (!tc_encode_2d(&p.kmap, k, DH, rows, DH * 2, 16) || !tc_encode_2d(&p.vmap, v, DH, rows, DH * 2, 16)) return cudaErrorInvalidValue;
+  const uint64_t kv_dims[2] = {DH, rows}, kv_strides[1] = {DH * 2};
+  const uint64_t q_dims[3] = {DH, (uint64_t)p.a.n_heads, (uint64_t)p.a.n_rows}, q_strides[2] = {DH * 2, (uint64_t)p.a.ld_q * 2};
+  const uint32_t kv_box[2] = {64, 16}, q_box[3] = {64, (uint32_t)(p.a.n_heads / c.n_kv_heads), (uint32_t)p.ts};
+  if (!tc_encode_plain(&p.kmap, k, 2, kv_dims, kv_strides, kv_box) || !tc_encode_plain(&p.vmap, v, 2, kv_dims, kv_strides, kv_box) ||
+      !tc_encode_plain(&p.qmap, p.a.q, 3, q_dims, q_strides, q_box))
+    return cudaErrorInvalidValue;
   e = launch_k(chunk_tc_kernel<DH>, dim3(p.runs), dim3(CtShape<DH>::THREADS), smem, st, p);
   if (e != cudaSuccess) return e;
   *launches += 2;

@@ -562,6 +562,25 @@ bool tc_encode_weight_3d(CUtensorMap* m, const void* base, int K, int rows, size
   return encode_3d(m, base, (uint64_t)K, (uint64_t)rows, (uint64_t)row_bytes, (uint32_t)box_rows, (uint32_t)kc);
 }
 
+bool tc_encode_plain(CUtensorMap* m, const void* base, int rank, const uint64_t* dims, const uint64_t* strides, const uint32_t* box) {
+  init_once();
+  if (!g_encode || ((uintptr_t)base & 15)) return false;
+  cuuint64_t d[3], st[2];
+  cuuint32_t b[3], es[3] = {1, 1, 1};
+  for (int i = 0; i < rank; ++i) {
+    if (dims[i] == 0) return false;
+    d[i] = dims[i];
+    b[i] = box[i];
+    if (i + 1 < rank) {
+      if (strides[i] & 15) return false;
+      st[i] = strides[i];
+    }
+  }
+  return g_encode(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, (cuuint32_t)rank, const_cast<void*>(base), d, st, b, es,
+                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 // Tile width for row bounds max_rows: the widest that still gives every SM a tile; *tiles
 // the tile count at that width.
 static int pick_bn(const GemmProblem* probs, int n_probs, const int* max_rows, long long* tiles_out) {

@@ -20,4 +20,6 @@ bool tc_encode_2d(CUtensorMap* m, const void* base, uint64_t inner, uint64_t out
 // 3-D view {64, rows, K/64} of a K-major bf16 matrix with box {64, box_rows, kc}, 128-byte
 // swizzle: one copy brings kc 64-wide k chunks of box_rows rows.  False if unsupported.
 bool tc_encode_weight_3d(CUtensorMap* m, const void* base, int K, int rows, size_t row_bytes, int box_rows, int kc);
+// Any bf16 view (rank 2 or 3, strides in bytes of the outer dimensions) and box, 128-byte swizzle; made anew at every call.
+bool tc_encode_plain(CUtensorMap* m, const void* base, int rank, const uint64_t* dims, const uint64_t* strides, const uint32_t* box);
 }  // namespace adept
