@@ -148,6 +148,21 @@ ADEPT_API adept_status adept_decode_step(adept_model* m, int batch, const int32_
                                float* d_logits_out, int32_t* d_next_token_out, float* d_sim_out,
                                void* stream);
 
+/* The next chunk of each of sequences 0..batch-1, appended behind what the sequence holds: a
+ * conversation's next turn, a piece of a long prompt, proposed tokens to check, or, after
+ * adept_seq_reserve with lengths 0, prompts of different lengths.  h_lens[b] >= 0 new tokens of sequence
+ * b (at least one token in all); d_tokens, d_forced_exit, d_exit_layer_out and d_sim_out hold the
+ * sum of h_lens rows, sequence-major; the rest as in adept_prefill (of which it is the continuation:
+ * a prompt in one call or in pieces gives the same states, exits and cache up to rounding).
+ * d_logits_out, d_next_token_out: row b is sequence b's last new token; rows of sequences without new
+ * tokens are not written.  Decoder families only; not with ADEPT_OPT_ALL_AT_ONCE.
+ * The first call allocates its workspace (outside any capture).
+ * Errors: INVALID_ARG (NULL pointers, a negative length, no token, a sequence not reserved), CAPACITY
+ * (batch > max_batch, a sequence beyond max_seq, more tokens than the pass workspace), OOM. */
+ADEPT_API adept_status adept_extend(adept_model* m, int batch, const int32_t* h_lens, const int32_t* d_tokens, float delta,
+                          const int32_t* d_forced_exit, int32_t* d_exit_layer_out, float* d_logits_out,
+                          int32_t* d_next_token_out, float* d_sim_out, void* stream);
+
 /* Threshold calibration (Sec. 4.1: delta is set to meet the computation budget; Sec. 5.1):
  * bisection on delta in [lo, hi] over prompt passes of the calibration batch d_tokens
  * [batch, prompt_len] (threshold exits, no forced exits) until the batch's reduction in
@@ -441,6 +456,9 @@ ADEPT_API adept_status adept_kv_gather(const adept_kv_cache* c, int n_rows, int 
  *   d_q, d_out   [n_rows][ld] (n_heads * head_dim elements a row): bf16, or fp32 for an fp32 cache;
  *                they must not overlap.  Rows that no sequence holds are not written.
  *   d_q_start [n_seq + 1], d_kv_len [n_seq]   int32, read on the device
+ *   d_row_pos [n_rows] or NULL   int32, read on the device: the rows' own positions, ascending within a
+ *                sequence, each below its d_kv_len (rows of tokens that are still active where others have
+ *                left); NULL: the last positions
  *   max_q_len, max_kv_len   bounds on a sequence's rows and positions; a sequence beyond them, or with
  *                rows outside 0 .. n_rows, flags DEVICE_INPUT and is left out, as is a key whose block
  *                is out of range
@@ -451,8 +469,8 @@ ADEPT_API adept_status adept_kv_gather(const adept_kv_cache* c, int n_rows, int 
  * stride below a row, NULL or misaligned pointers, a workspace too small), CAPACITY (n_rows *
  * n_heads above 2^30), CUDA. */
 ADEPT_API adept_status adept_chunk_attention(const adept_kv_cache* c, int n_heads, int n_rows, const void* d_q, int64_t ld_q,
-                                   const int32_t* d_q_start, const int32_t* d_kv_len, int max_q_len, int max_kv_len,
-                                   void* d_out, int64_t ld_out, void* d_ws, int64_t ws_bytes, void* stream);
+                                   const int32_t* d_q_start, const int32_t* d_kv_len, const int32_t* d_row_pos,
+                                   int max_q_len, int max_kv_len, void* d_out, int64_t ld_out, void* d_ws, int64_t ws_bytes, void* stream);
 /* Bytes of d_ws that such a call needs, or -1 (bad arguments). */
 ADEPT_API int64_t adept_chunk_attention_workspace(const adept_kv_cache* c, int n_heads, int n_rows, int max_q_len,
                                         int max_kv_len);

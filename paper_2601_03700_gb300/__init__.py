@@ -40,6 +40,7 @@ ABI_SYMBOLS = [
     "adept_hsm_param_numel", "adept_hsm_train_step_cls", "adept_set_wait_limit", "adept_set_alloc_fail_after",
     "adept_span_read", "adept_set_cross_source",
     "adept_kv_append", "adept_kv_gather", "adept_chunk_attention", "adept_chunk_attention_workspace", "adept_kv_check",
+    "adept_extend",
 ]
 
 
@@ -140,11 +141,13 @@ def load_library(path: str = LIB_PATH):
     lib.adept_set_alloc_fail_after.restype = None
     lib.adept_hsm_param_numel.argtypes = [vp, c_int]
     lib.adept_hsm_param_numel.restype = ctypes.c_int64
+    lib.adept_extend.argtypes = [vp, c_int, ctypes.POINTER(ctypes.c_int32), i32p, c_float, i32p, i32p, fp, i32p, fp, st]
+    lib.adept_extend.restype = c_int
     kvp, i64 = ctypes.POINTER(AdeptKVCache), ctypes.c_int64
     for fn in (lib.adept_kv_append, lib.adept_kv_gather):
         fn.argtypes = [kvp, c_int, c_int, vp, i64, vp, i64, i32p, i32p, st]
         fn.restype = c_int
-    lib.adept_chunk_attention.argtypes = [kvp, c_int, c_int, vp, i64, i32p, i32p, c_int, c_int, vp, i64, vp, i64, st]
+    lib.adept_chunk_attention.argtypes = [kvp, c_int, c_int, vp, i64, i32p, i32p, i32p, c_int, c_int, vp, i64, vp, i64, st]
     lib.adept_chunk_attention.restype = c_int
     lib.adept_chunk_attention_workspace.argtypes = [kvp, c_int, c_int, c_int, c_int]
     lib.adept_chunk_attention_workspace.restype = i64
@@ -240,6 +243,17 @@ def adept_decode_step(m, batch: int, tokens: torch.Tensor, delta: float, forced:
     lib = load_library()
     _check(lib, m, lib.adept_decode_step(m, batch, _ptr(tokens), float(delta), _ptr(forced), _ptr(exit_layer_out),
                                           _ptr(logits_out), _ptr(next_token_out), _ptr(sim_out), _stream(stream)))
+
+
+def adept_extend(m, lens, tokens: torch.Tensor, delta: float, forced: Optional[torch.Tensor] = None,
+                 exit_layer_out: Optional[torch.Tensor] = None, logits_out: Optional[torch.Tensor] = None,
+                 next_token_out: Optional[torch.Tensor] = None, sim_out: Optional[torch.Tensor] = None, stream=None):
+    """The next lens[b] tokens of each sequence behind what it holds (tokens: all of them, sequence-major)."""
+    lib = load_library()
+    n = len(lens)
+    arr = (ctypes.c_int32 * n)(*[int(x) for x in lens])
+    _check(lib, m, lib.adept_extend(m, n, arr, _ptr(tokens), float(delta), _ptr(forced), _ptr(exit_layer_out),
+                                     _ptr(logits_out), _ptr(next_token_out), _ptr(sim_out), _stream(stream)))
 
 
 def adept_skip_kv_fill(m, n_tokens: int, h_mapped: torch.Tensor, exit_layer: torch.Tensor, seq: torch.Tensor,
@@ -502,9 +516,11 @@ def adept_kv_gather(cache: KVCache, seq: torch.Tensor, pos: torch.Tensor, k_out:
 
 
 def adept_chunk_attention(cache: KVCache, q: torch.Tensor, q_start: torch.Tensor, kv_len: torch.Tensor, max_q_len: int,
-                          max_kv_len: int, out: torch.Tensor, workspace: Optional[torch.Tensor] = None, stream=None):
+                          max_kv_len: int, out: torch.Tensor, workspace: Optional[torch.Tensor] = None,
+                          row_pos: Optional[torch.Tensor] = None, stream=None):
     """Causal attention of each sequence's newest tokens, rows q_start[b] .. q_start[b + 1] of q [rows, n_heads, head_dim],
-    over its kv_len[b] cached positions, into out.  workspace: KVCache.attention_workspace of these sizes (None: one is
+    over its kv_len[b] cached positions, into out.  row_pos: the rows' own positions, ascending within a sequence (None:
+    the last ones).  workspace: KVCache.attention_workspace of these sizes (None: one is
     made for the call)."""
     lib = load_library()
     if q.dtype is not cache.q_dtype or out.dtype is not cache.q_dtype:
@@ -514,6 +530,8 @@ def adept_chunk_attention(cache: KVCache, q: torch.Tensor, q_start: torch.Tensor
     n_o, ld_o = _rows(cache, "out", out, heads)
     if n != n_o:
         raise ValueError("q and out must have the same rows")
+    if out.data_ptr() == q.data_ptr() and n:
+        raise ValueError("q and out must not overlap")
     if workspace is None:
         s = stream if stream is None or hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream))
         with torch.cuda.stream(s):   # (the call's stream: memory that it alone reuses)
@@ -522,8 +540,8 @@ def adept_chunk_attention(cache: KVCache, q: torch.Tensor, q_start: torch.Tensor
         raise ValueError(f"workspace must be contiguous on {cache.device}")
     ws, nb = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.nbytes)
     _call(cache, lib.adept_chunk_attention, stream, heads, n, q.data_ptr(), ld_q,
-          _index(cache, "q_start", q_start, cache.n_seq + 1), _index(cache, "kv_len", kv_len, cache.n_seq), max_q_len,
-          max_kv_len, out.data_ptr(), ld_o, ws, nb)
+          _index(cache, "q_start", q_start, cache.n_seq + 1), _index(cache, "kv_len", kv_len, cache.n_seq),
+          None if row_pos is None else _index(cache, "row_pos", row_pos, n), max_q_len, max_kv_len, out.data_ptr(), ld_o, ws, nb)
 
 
 def adept_kv_check(cache: KVCache, stream=None):
@@ -566,6 +584,19 @@ class Model:
         adept_prefill(self.h, B, P, tokens.to(torch.int32).contiguous().view(-1), delta,
                       None if forced is None else forced.to(torch.int32).contiguous().view(-1), ex, lg, nx, sim,
                       stream)
+        return ex, lg, nx, sim
+
+    def extend(self, lens, tokens: torch.Tensor, delta: float, forced: Optional[torch.Tensor] = None, stream=None):
+        """The next lens[b] tokens of each sequence (tokens: sum(lens), sequence-major); rows of logits and next tokens
+        of sequences without new ones are zero."""
+        n = int(sum(int(x) for x in lens))
+        if tokens.numel() != n or (forced is not None and forced.numel() != n):
+            raise ValueError(f"tokens (and forced exits) must have sum(lens) = {n} elements")
+        ex, lg, nx, sim = self._outs(n, len(lens), tokens.device)
+        lg.zero_()
+        nx.zero_()
+        adept_extend(self.h, lens, tokens.to(torch.int32).contiguous().view(-1), delta,
+                     None if forced is None else forced.to(torch.int32).contiguous().view(-1), ex, lg, nx, sim, stream)
         return ex, lg, nx, sim
 
     def decode_step(self, tokens: torch.Tensor, delta: float, forced: Optional[torch.Tensor] = None, stream=None):

@@ -1,5 +1,5 @@
 // Attention of a chunk of new tokens over a paged K/V cache: sequence b brings c_b >= 0 new tokens, the last of its kv_len_b
-// cached positions; the token at position p attends positions 0..p.
+// cached positions (or given ones of them); the token at position p attends positions 0..p.
 //
 //   out = sum_k exp(s_k - m) v_k / sum_k exp(s_k - m),   s_k = q . k_k / sqrt(head_dim),   m = max s_k
 //
@@ -70,10 +70,12 @@ __global__ void __launch_bounds__(CG_KEYS) chunk_any_kernel(const __grid_constan
   const SplitItem it = s_it;
   const int h = it.group, kvh = h / (a.n_heads / a.c.n_kv_heads), bt = a.c.block_tokens;
   const int j0 = it.tile * CG_ROWS, n = min(CG_ROWS, it.c - j0);
-  const int past = it.len - it.c;   // row j's position is past + j
+  int lim[CG_ROWS];   // keys that each row attends
+#pragma unroll
+  for (int r = 0; r < CG_ROWS; ++r) lim[r] = r < n ? chunk_lim(a, it.q0, it.c, it.len, j0 + r) : 0;
   for (int i = tid; i < n * DH; i += CG_KEYS)
     s_q[i / DH][i % DH] = to_f<T>(((const T*)a.q)[(size_t)(it.q0 + j0 + i / DH) * a.ld_q + (size_t)h * DH + i % DH]);
-  const int k_end = min(it.u1 * CG_KEYS, min(it.len, past + j0 + n));
+  const int k_end = min(it.u1 * CG_KEYS, max(max(lim[0], lim[1]), max(lim[2], lim[3])));
   constexpr int KG = CG_KEYS / DH > 0 ? CG_KEYS / DH : 1;   // key groups of the weighted sum
   const int d = tid % DH, kg = tid / DH;
   float acc[CG_ROWS], m = -INFINITY, l = 0.f;   // (m, l of row `warp`)
@@ -108,7 +110,7 @@ __global__ void __launch_bounds__(CG_KEYS) chunk_any_kernel(const __grid_constan
     }
 #pragma unroll
     for (int r = 0; r < CG_ROWS; ++r)
-      s_p[r][tid] = e >= 0 && r < n && key <= past + j0 + r ? dot[r] * ks * a.scale_log2 : -INFINITY;
+      s_p[r][tid] = e >= 0 && key < lim[r] ? dot[r] * ks * a.scale_log2 : -INFINITY;
     __syncthreads();
     {
       float v[CG_KEYS / 32], mx = m;
@@ -141,7 +143,7 @@ __global__ void __launch_bounds__(CG_KEYS) chunk_any_kernel(const __grid_constan
       if (KT == KV_E4M3) x *= s_vs[k];
 #pragma unroll
       for (int r = 0; r < CG_ROWS; ++r)
-        if (k0 + k <= past + j0 + r) acc[r] = fmaf(s_p[r][k], x, acc[r]);
+        if (k0 + k < lim[r]) acc[r] = fmaf(s_p[r][k], x, acc[r]);
     }
     __syncthreads();
   }
@@ -164,7 +166,7 @@ __global__ void __launch_bounds__(CG_KEYS) chunk_any_kernel(const __grid_constan
         pv.o[r * DH + tid] = o;
       else
         ((T*)a.out)[(size_t)(it.q0 + j0 + r) * a.ld_out + (size_t)h * DH + tid] =
-            from_f<T>(past + j0 + r < 0 ? 0.f : o / sum);
+            from_f<T>(lim[r] == 0 ? 0.f : o / sum);
     }
     __syncthreads();
   }
@@ -313,9 +315,10 @@ __global__ void __launch_bounds__(CF_WARPS * 32, 3) chunk_few_kernel(const __gri
   if (!s_have) return;
   const SplitItem it = s_it;
   const int group = a.n_heads / a.c.n_kv_heads, kvh = it.group / sub, g0 = it.group % sub * per_tok;
-  const int past = it.len - it.c, j0 = it.tile * p.tq, n = min(p.tq, it.c - j0);
+  const int j0 = it.tile * p.tq, n = min(p.tq, it.c - j0);
   const int n_row = n * per_tok;   // rows of the tile in use (those with g0 + r % per_tok >= group hold nothing)
-  const int lim_lo = max(past + j0 + 1, 0), lim_hi = max(past + j0 + n, 0);   // keys of the tile's first and last token
+  auto keys_of = [&](int j) { return chunk_lim(a, it.q0, it.c, it.len, j0 + j); };
+  const int lim_lo = keys_of(0), lim_hi = keys_of(n - 1);                     // keys of the tile's first and last token
   const int k_end = min(min(it.u1 * F::UNIT, it.len), lim_hi);                // keys that anyone attends
   const int b_end = (k_end + 15) >> 4;
   const int* table = a.c.table + (size_t)it.seq * a.c.max_blocks;
@@ -366,7 +369,7 @@ __global__ void __launch_bounds__(CF_WARPS * 32, 3) chunk_few_kernel(const __gri
   for (int r2 = 0; r2 < 2; ++r2) {
     const int r = g + 8 * r2, j = r / per_tok, gq = g0 + r % per_tok;
     const bool on = r < n_row && gq < group;
-    lim[r2] = on ? max(past + j0 + j + 1, 0) : 0;
+    lim[r2] = on ? keys_of(j) : 0;
     rs[r2] = a.scale_log2;
     const bf16* q = (const bf16*)a.q + (size_t)(it.q0 + j0 + j) * a.ld_q + (size_t)(kvh * group + gq) * DH;
 #pragma unroll
@@ -644,7 +647,7 @@ __global__ void __launch_bounds__(CF_WARPS * 32, 3) chunk_few_kernel(const __gri
       *reinterpret_cast<float4*>(pv.o + r * DH + d) = make_float4(x[0], x[1], x[2], x[3]);
       if (d == 0) *reinterpret_cast<float2*>(pv.ml + r * 2) = make_float2(M, L);
     } else {
-      const float inv = past + j0 + j < 0 ? 0.f : 1.f / L;
+      const float inv = keys_of(j) == 0 ? 0.f : 1.f / L;
       uint2 y = make_uint2(pack_bf16(x[0] * inv, x[1] * inv), pack_bf16(x[2] * inv, x[3] * inv));
       *reinterpret_cast<uint2*>((bf16*)a.out + (size_t)(it.q0 + j0 + j) * a.ld_out + (size_t)(kvh * group + gq) * DH + d) = y;
     }
@@ -699,7 +702,7 @@ __global__ void __launch_bounds__(CJ_THREADS) chunk_join_kernel(const __grid_con
   if (!s_have || s_it.n_split <= 1) return;
   const SplitItem it = s_it;
   const int group = a.n_heads / a.c.n_kv_heads;
-  const int past = it.len - it.c, j0 = it.tile * p.tq, n = min(p.tq, it.c - j0);
+  const int j0 = it.tile * p.tq, n = min(p.tq, it.c - j0);
   const PartView pv(a, p, rows, DH, it.slot0);
   const int live = n * per_tok * (DH / 4);                       // elements of four columns
   const int groups = max(1, min(CJ_THREADS / live, (it.n_split + 3) / 4));
@@ -751,7 +754,7 @@ __global__ void __launch_bounds__(CJ_THREADS) chunk_join_kernel(const __grid_con
     const int h = it.group / sub * group + g;
     T* dst = (T*)a.out + (size_t)(it.q0 + j0 + j) * a.ld_out + (size_t)h * DH + d;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) dst[e] = from_f<T>(past + j0 + j < 0 ? 0.f : x.o[e] / x.l);
+    for (int e = 0; e < 4; ++e) dst[e] = from_f<T>(chunk_lim(a, it.q0, it.c, it.len, j0 + j) == 0 ? 0.f : x.o[e] / x.l);
   }
 }
 

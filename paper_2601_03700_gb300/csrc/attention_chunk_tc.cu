@@ -78,18 +78,20 @@ __device__ long long floor_sum(unsigned n, unsigned m, unsigned a, unsigned b) {
   }
   return r;
 }
-// Key tiles of token tile t (at least one: a tile without keys has zeros to write).
-__device__ __forceinline__ int ct_units(int c, int len, int tq, int t) {
-  return max(1, (len - c + min((t + 1) * tq, c) + CT_BN - 1) / CT_BN);
+// Key tiles of token tile t (at least one: a tile without keys has zeros to write; with given positions, those of the whole
+// sequence).
+__device__ __forceinline__ int ct_units(bool given, int c, int len, int tq, int t) {
+  return max(1, (given ? len + CT_BN - 1 : len - c + min((t + 1) * tq, c) + CT_BN - 1) / CT_BN);
 }
-__device__ long long ct_seq_units(int c, int len, int tq) {
+__device__ long long ct_seq_units(bool given, int c, int len, int tq) {
   const int tiles = (c + tq - 1) / tq;
   if (tiles == 0) return 0;
-  const long long last = ct_units(c, len, tq, tiles - 1);
+  if (given) return (long long)tiles * ct_units(true, c, len, tq, 0);
+  const long long last = ct_units(false, c, len, tq, tiles - 1);
   if (tiles == 1) return last;
   if (len - c + tq < 1) {   // (first tiles without keys: one by one)
     long long r = 0;
-    for (int t = 0; t < tiles; ++t) r += ct_units(c, len, tq, t);
+    for (int t = 0; t < tiles; ++t) r += ct_units(false, c, len, tq, t);
     return r;
   }
   return last + floor_sum((unsigned)tiles - 1, CT_BN, (unsigned)tq, (unsigned)(len - c + tq + CT_BN - 1));
@@ -106,7 +108,7 @@ __device__ long long ct_total(const ChunkCall& a, int tq) {
   for (int b = threadIdx.x & 31; b < a.c.n_seq; b += 32) {
     int q0, c, len;
     chunk_seq(a, b, q0, c, len);
-    tot += ct_seq_units(c, len, tq) * a.c.n_kv_heads;
+    tot += ct_seq_units(a.row_pos, c, len, tq) * a.c.n_kv_heads;
   }
   // (24 bits and the rest: one instruction each)
   return __reduce_add_sync(0xffffffffu, (unsigned)(tot & 0xffffff)) +
@@ -119,7 +121,7 @@ __device__ void ct_find(const ChunkCall& a, int tq, long long u, CtTile& x) {
   for (int b0 = 0; b0 < a.c.n_seq; b0 += 32) {
     int q0 = 0, c = 0, len = 0;
     if (b0 + lane < a.c.n_seq) chunk_seq(a, b0 + lane, q0, c, len);
-    const long long mine = ct_seq_units(c, len, tq) * a.c.n_kv_heads;
+    const long long mine = ct_seq_units(a.row_pos, c, len, tq) * a.c.n_kv_heads;
     long long inc = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -140,7 +142,7 @@ __device__ void ct_find(const ChunkCall& a, int tq, long long u, CtTile& x) {
     const int tiles = (x.c + tq - 1) / tq;
     for (int t0 = 0; t0 < tiles; t0 += 32) {
       const int t = t0 + lane;
-      const long long n = t < tiles ? (long long)ct_units(x.c, x.len, tq, t) * a.c.n_kv_heads : 0;
+      const long long n = t < tiles ? (long long)ct_units(a.row_pos, x.c, x.len, tq, t) * a.c.n_kv_heads : 0;
       long long in2 = n;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
@@ -155,7 +157,7 @@ __device__ void ct_find(const ChunkCall& a, int tq, long long u, CtTile& x) {
       const int s2 = __ffs(w2) - 1;
       before += __shfl_sync(0xffffffffu, in2 - n, s2);
       x.tile = t0 + s2;
-      x.units = ct_units(x.c, x.len, tq, x.tile);
+      x.units = ct_units(a.row_pos, x.c, x.len, tq, x.tile);
       x.kvh = (int)((u - before) / x.units);
       x.u0 = before + (long long)x.kvh * x.units;
       return;
@@ -173,7 +175,7 @@ __device__ __forceinline__ void ct_next(const ChunkCall& a, int tq, CtTile& x) {
     x.c = 0;
     while (x.c == 0 && ++x.seq < a.c.n_seq) chunk_seq(a, x.seq, x.q0, x.c, x.len);
   }
-  x.units = ct_units(x.c, x.len, tq, x.tile);
+  x.units = ct_units(a.row_pos, x.c, x.len, tq, x.tile);
 }
 // Run i of `runs` (fewer where there are few units).
 constexpr int CT_MIN_RUN = 2;
@@ -238,7 +240,7 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
 // A CTA's part of one tile: key tiles j_lo .. j_hi.
 struct CtSeg {
   CtTile x;
-  int j_lo, j_hi, past, t0, n_tok;
+  int j_lo, j_hi, t0, n_tok;
   int lim_lo, k_end;   // keys of the tile's first and of its last token (nobody attends beyond)
   int nt0, nt1, n_it;  // key tiles with keys: per sub-tile, of the segment
   bool whole;          // the whole tile
@@ -248,17 +250,18 @@ struct CtSeg {
     j_lo = (int)(u - x.u0);
     j_hi = (int)min((long long)x.units, u_end - x.u0);
     whole = j_lo == 0 && j_hi == x.units;
-    past = x.len - x.c;
     t0 = x.tile * 2 * ts;
     n_tok = min(2 * ts, x.c - t0);
-    lim_lo = max(past + t0 + 1, 0);
-    k_end = max(past + t0 + n_tok, 0);
-    const int k_end0 = max(past + t0 + min(ts, n_tok), 0);
+    lim_lo = keys(a, 0);
+    k_end = keys(a, n_tok - 1);
+    const int k_end0 = keys(a, min(ts, n_tok) - 1);
     nt0 = max(min(j_hi, (k_end0 + CT_BN - 1) / CT_BN) - j_lo, 0);
     nt1 = n_tok > ts ? max(min(j_hi, (k_end + CT_BN - 1) / CT_BN) - j_lo, 0) : 0;
     n_it = max(nt0, nt1);
     table = a.c.table + (size_t)x.seq * a.c.max_blocks;
   }
+  // keys that token `tok` of the tile attends
+  __device__ __forceinline__ int keys(const ChunkCall& a, int tok) const { return chunk_lim(a, x.q0, x.c, x.len, t0 + tok); }
   __device__ __forceinline__ int nt(int sub) const { return sub ? nt1 : nt0; }
   // key tile j (from the segment's first) holds keys that are not everybody's
   __device__ __forceinline__ bool edge(int j) const { return (j_lo + j + 1) * CT_BN > lim_lo || (j_lo + j + 1) * CT_BN > k_end; }
@@ -376,8 +379,8 @@ __global__ void __launch_bounds__(CtShape<DH>::THREADS, 1) chunk_tc_kernel(const
       g.set(a, ts, x, u, u_end);
       seg += g.n_it > 0;
       const bool mine = tok >= 0 && tok < g.n_tok;
-      const int lim = mine ? max(g.past + g.t0 + tok + 1, 0) : 0;
-      const int sub_lo = max(g.past + g.t0 + sub * ts + 1, 0);   // keys of the sub-tile's first token
+      const int lim = mine ? g.keys(a, tok) : 0;
+      const int sub_lo = sub * ts < g.n_tok ? g.keys(a, sub * ts) : 0;   // keys of the sub-tile's first token
       const int n_my = g.nt(sub);
       float m = -INFINITY, l = 0.f;
       for (int j = 0; j < n_my; ++j) {
@@ -778,7 +781,7 @@ __global__ void __launch_bounds__(256) chunk_tc_join_kernel(const __grid_constan
         o[3] += x * v[k].w;
       }
     }
-    const float inv = n.pos0 + tok < 0 ? 0.f : 1.f / l;
+    const float inv = (a.row_pos ? a.row_pos[n.row0 + tok] : n.pos0 + tok) < 0 ? 0.f : 1.f / l;
     const __nv_bfloat162 y0 = __floats2bfloat162_rn(o[0] * inv, o[1] * inv), y1 = __floats2bfloat162_rn(o[2] * inv, o[3] * inv);
     *reinterpret_cast<uint2*>((bf16*)a.out + (size_t)(n.row0 + tok) * a.ld_out + (size_t)(n.kvh * group + rr % group) * DH + d4 * 4) =
         make_uint2(*reinterpret_cast<const uint32_t*>(&y0), *reinterpret_cast<const uint32_t*>(&y1));

@@ -29,10 +29,16 @@ static __device__ __forceinline__ float exit_similarity(int metric, float ns, fl
 
 // Token -> (sequence, position) maps, identity row map, the pass's counters (all rows
 // active), if sim is given NaN for every (token, layer) similarity, and if tok_exit is
-// given N as every token's exit layer so far.
+// given N as every token's exit layer so far.  ext (else NULL): ragged chunks behind what ext_n
+// sequences hold: first token per sequence and the count [ext_n + 1], then the lengths before the pass.
 void launch_pass_init(cudaStream_t st, int n_tok, int prompt_len, int* tok_seq, int* tok_pos, int* row_tok, int* seq_len,
                       int seq_cap, int max_pos, unsigned* err, int* ctr, int n_ctr, float* sim, int n_layers,
-                      int* tok_exit);
+                      int* tok_exit, const int* ext = nullptr, int ext_n = 0);
+// Per sequence of such a pass the first active row (row_start [ext_n + 1]), and the active rows' positions.
+void launch_chunk_rows(cudaStream_t st, const int* n_rows, int max_rows, const int* row_tok, const int* tok_pos, const int* ext,
+                       int ext_n, int* row_start, int* row_pos);
+// The token of each chunk whose state the output head takes.
+void launch_chunk_head_rows(cudaStream_t st, int batch, const int* ext, int* rows);
 // xhat: the embedded rows as the first layer's attention input (decoders: standardised by smode,
 // seps) in the model's type, [n_tok][D].
 void launch_embed(cudaStream_t st, int dt, const int* tokens, int n_tok, const int* tok_pos, const void* E,

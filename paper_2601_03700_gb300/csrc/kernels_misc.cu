@@ -14,12 +14,15 @@ namespace adept {
 // ---------------------------------------------------------------------------
 // pass set-up: token -> (sequence, position), identity row map, counters
 // ---------------------------------------------------------------------------
-// Thread t's part: counter t, token t.
+// Thread t's part: counter t, token t.  ext (else NULL): a pass of ragged chunks behind what the sequences hold, of ext_n
+// sequences: first token per sequence and the token count [ext_n + 1], then the lengths before the pass [ext_n].
 __device__ __forceinline__ void pass_init(int t, int n_tok, int prompt_len, int decode, int* tok_seq, int* tok_pos,
                                           int* row_tok, int* seq_len, int seq_cap, int max_pos, unsigned* err, int* ctr,
-                                          int n_ctr, float* sim, int n_layers, int* tok_exit) {
+                                          int n_ctr, float* sim, int n_layers, int* tok_exit, const int* ext = nullptr,
+                                          int ext_n = 0) {
   // the pass's counters: all active, nothing exited
   if (t < n_ctr) ctr[t] = t == CTR_ACTIVE ? n_tok : 0;
+  if (ext && t < ext_n) seq_len[t] = ext[ext_n + 1 + t] + ext[t + 1] - ext[t];
   if (t >= n_tok) return;
   // every token active: its exit layer so far is N
   if (tok_exit) tok_exit[t] = n_layers;
@@ -31,6 +34,15 @@ __device__ __forceinline__ void pass_init(int t, int n_tok, int prompt_len, int 
     s = t;
     p = seq_len[t];
     seq_len[t] = p + 1;
+  } else if (ext) {
+    int lo = 0, hi = ext_n - 1;   // the last sequence that begins at or before t
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (ext[mid] <= t) lo = mid;
+      else hi = mid - 1;
+    }
+    s = lo;
+    p = ext[ext_n + 1 + s] + t - ext[s];
   } else {
     s = t / prompt_len;
     p = t % prompt_len;
@@ -46,10 +58,28 @@ __device__ __forceinline__ void pass_init(int t, int n_tok, int prompt_len, int 
 }
 __global__ void pass_init_kernel(int n_tok, int prompt_len, int* tok_seq, int* tok_pos, int* row_tok, int* seq_len,
                                  int seq_cap, int max_pos, unsigned* err, int* ctr, int n_ctr, float* sim, int n_layers,
-                                 int* tok_exit) {
+                                 int* tok_exit, const int* ext, int ext_n) {
   PDL_ENTRY();
   pass_init(blockIdx.x * blockDim.x + threadIdx.x, n_tok, prompt_len, 0, tok_seq, tok_pos, row_tok, seq_len, seq_cap,
-            max_pos, err, ctr, n_ctr, sim, n_layers, tok_exit);
+            max_pos, err, ctr, n_ctr, sim, n_layers, tok_exit, ext, ext_n);
+}
+
+// The active rows of a pass of ragged chunks as an attention call takes them: first active row per sequence (rows are in token
+// order) and their positions.
+__global__ void chunk_rows_kernel(const int* n_rows, const int* row_tok, const int* tok_pos, const int* ext, int ext_n,
+                                  int* row_start, int* row_pos) {
+  PDL_ENTRY();
+  const int t = blockIdx.x * blockDim.x + threadIdx.x, n = *n_rows;
+  if (t < n) row_pos[t] = tok_pos[row_tok[t]];
+  if (t <= ext_n) {
+    int lo = 0, hi = n;   // the first row of a token at or behind the sequence's first
+    while (lo < hi) {
+      const int mid = (lo + hi) >> 1;
+      if (row_tok[mid] < ext[t]) lo = mid + 1;
+      else hi = mid;
+    }
+    row_start[t] = lo;
+  }
 }
 
 // ---------------------------------------------------------------------------
@@ -820,6 +850,12 @@ __global__ void head_rows_kernel(int batch, int prompt_len, int last, int* rows)
   const int b = blockIdx.x * blockDim.x + threadIdx.x;
   if (b < batch) rows[b] = b * prompt_len + (last ? prompt_len - 1 : 0);
 }
+// The last token of each ragged chunk (of an empty one: some token).
+__global__ void chunk_head_rows_kernel(int batch, const int* ext, int* rows) {
+  PDL_ENTRY();
+  const int b = blockIdx.x * blockDim.x + threadIdx.x;
+  if (b < batch) rows[b] = max(ext[b + 1] - 1, 0);
+}
 
 // ---------------------------------------------------------------------------
 // skipped-layer fill input: bucket tokens by exit layer (ascending) so that the rows of
@@ -1028,9 +1064,19 @@ __global__ void __launch_bounds__(256) read_kv_kernel(KVCacheView c, int row_byt
 // ---------------------------------------------------------------------------
 void launch_pass_init(cudaStream_t st, int n_tok, int prompt_len, int* tok_seq, int* tok_pos, int* row_tok, int* seq_len,
                       int seq_cap, int max_pos, unsigned* err, int* ctr, int n_ctr, float* sim, int n_layers,
-                      int* tok_exit) {
-  launch_k(pass_init_kernel, cdiv(std::max(n_tok, n_ctr), 256), 256, 0, st, n_tok, prompt_len, tok_seq, tok_pos,
-           row_tok, seq_len, seq_cap, max_pos, err, ctr, n_ctr, sim, n_layers, tok_exit);
+                      int* tok_exit, const int* ext, int ext_n) {
+  launch_k(pass_init_kernel, cdiv(std::max({n_tok, n_ctr, ext_n}), 256), 256, 0, st, n_tok, prompt_len, tok_seq, tok_pos,
+           row_tok, seq_len, seq_cap, max_pos, err, ctr, n_ctr, sim, n_layers, tok_exit, ext, ext_n);
+}
+
+void launch_chunk_rows(cudaStream_t st, const int* n_rows, int max_rows, const int* row_tok, const int* tok_pos, const int* ext,
+                       int ext_n, int* row_start, int* row_pos) {
+  launch_k(chunk_rows_kernel, cdiv(std::max(max_rows, ext_n + 1), 256), 256, 0, st, n_rows, row_tok, tok_pos, ext, ext_n,
+           row_start, row_pos);
+}
+
+void launch_chunk_head_rows(cudaStream_t st, int batch, const int* ext, int* rows) {
+  launch_k(chunk_head_rows_kernel, cdiv(batch, 128), 128, 0, st, batch, ext, rows);
 }
 
 void launch_embed(cudaStream_t st, int dt, const int* tokens, int n_tok, const int* tok_pos, const void* E,

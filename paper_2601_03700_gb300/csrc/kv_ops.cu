@@ -103,8 +103,8 @@ int64_t adept_chunk_attention_workspace(const adept_kv_cache* c, int n_heads, in
 }
 
 adept_status adept_chunk_attention(const adept_kv_cache* c, int n_heads, int n_rows, const void* d_q, int64_t ld_q,
-                                   const int32_t* d_q_start, const int32_t* d_kv_len, int max_q_len, int max_kv_len,
-                                   void* d_out, int64_t ld_out, void* d_ws, int64_t ws_bytes, void* stream) {
+                                   const int32_t* d_q_start, const int32_t* d_kv_len, const int32_t* d_row_pos,
+                                   int max_q_len, int max_kv_len, void* d_out, int64_t ld_out, void* d_ws, int64_t ws_bytes, void* stream) {
   ChunkCall a{};
   adept_status s = view_of(c, &a.c);
   if (s == ADEPT_OK) s = call_ok(a.c, n_heads, n_rows, max_q_len, max_kv_len);
@@ -124,6 +124,7 @@ adept_status adept_chunk_attention(const adept_kv_cache* c, int n_heads, int n_r
   a.ld_out = ld_out;
   a.q_start = d_q_start;
   a.kv_len = d_kv_len;
+  a.row_pos = d_row_pos;
   a.n_rows = n_rows;
   a.n_heads = n_heads;
   a.max_q = max_q_len;

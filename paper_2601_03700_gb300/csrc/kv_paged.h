@@ -30,8 +30,8 @@ cudaError_t launch_kv_append(cudaStream_t st, const KvPaged& c, int n_rows, int 
 cudaError_t launch_kv_gather(cudaStream_t st, const KvPaged& c, int n_rows, int dst_bf16, void* k, long long ld_k, void* v,
                              long long ld_v, const int* seq, const int* pos);
 
-// One attention call: the new tokens of n_seq sequences (rows q_start[b] .. q_start[b + 1]), the last of sequence b's
-// kv_len[b] cached positions, each attending its own position and those before it.
+// One attention call: the new tokens of n_seq sequences (rows q_start[b] .. q_start[b + 1]) at the last of sequence b's
+// kv_len[b] cached positions, or at those that row_pos gives, each attending its own position and those before it.
 struct ChunkCall {
   KvPaged c;
   const void* q;      // [n_rows][ld_q], head h at column h * head_dim (bf16; fp32 for an fp32 cache)
@@ -39,6 +39,7 @@ struct ChunkCall {
   long long ld_q, ld_out;
   const int* q_start;
   const int* kv_len;
+  const int* row_pos;   // position per row, ascending within a sequence (NULL: the last ones)
   int n_rows, n_heads, max_q, max_kv;
   int c_lo, c_hi;     // the launch's sequences: those with c_lo to c_hi new tokens
   float scale_log2;   // log2(e) / sqrt(head_dim)
@@ -83,6 +84,11 @@ __device__ __forceinline__ void chunk_seq(const ChunkCall& a, int b, int& q0, in
   }
   if (c < a.c_lo || c > a.c_hi) c = 0;
   if (c == 0) len = 0;
+}
+
+// Keys that new token j of a sequence attends.
+__device__ __forceinline__ int chunk_lim(const ChunkCall& a, int q0, int c, int len, int j) {
+  return a.row_pos ? min(max(a.row_pos[q0 + j] + 1, 0), len) : max(len - c + j + 1, 0);
 }
 
 // Item `id` of the plan (joined: tile `id`, its splits taken together), looked up by one converged warp; false: none.  32-bit

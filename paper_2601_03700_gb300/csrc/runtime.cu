@@ -145,6 +145,11 @@ struct adept_model {
   float* logits_ws = nullptr;
   float* attn_ws = nullptr;
   int* attn_ctr = nullptr;       // generation-step attention arrival counters (zero between launches)
+  // adept_extend (made at its first call): per sequence the first token and the length before, first active row; positions of
+  // the active rows; workspace of the chunk attention
+  std::vector<int> h_ext;
+  int *d_ext = nullptr, *ext_start = nullptr, *ext_pos = nullptr;
+  float* ext_ws = nullptr;
   int32_t* calib_exit = nullptr; // threshold calibration: exit layers of a calibration pass
   // standardisation statistics of X_out handed from the O projection to the FFN input
   float2* tile_stats = nullptr;                // [DG_MAX_M][D / 32] (mean, M2) of X_out tiles
@@ -1071,10 +1076,49 @@ static GemmProblem kv_problem(adept_model* m, int layer0, const void* xs, int a_
   return p;
 }
 
+// A pass of ragged chunks behind what the sequences hold: bounds on a sequence's new tokens and positions.
+struct ExtendPass {
+  int max_len, max_kv;
+};
+
+static KvPaged paged_view(const adept_model* m, int layer0, int n_seq) {
+  const size_t off = (size_t)layer0 * m->n_blocks * m->Hkv * m->cfg.kv_block_tokens * m->dh * m->esz;
+  return KvPaged{(char*)m->k_pool + off, (char*)m->v_pool + off, nullptr, nullptr, m->d_block_table, m->err_word,
+                 m->dt == ADEPT_DTYPE_BF16 ? KV_BF16 : KV_F32, m->n_blocks, m->Hkv, m->dh, m->cfg.kv_block_tokens, n_seq,
+                 m->max_blocks_per_seq};
+}
+
+// Attention of the active rows of a pass of ragged chunks (a row's position is its token's, those of tokens that left are
+// missing) over layer layer0's cache.
+static void extend_attention(adept_model* m, cudaStream_t st, const ExtendPass& e, int layer0, int batch, const int* n_rows,
+                             int max_rows, const int* row_tok) {
+  launch_chunk_rows(st, n_rows, max_rows, row_tok, m->tok_pos, m->d_ext, batch, m->ext_start, m->ext_pos);
+  ChunkCall a{};
+  a.c = paged_view(m, layer0, batch);
+  a.q = m->q;
+  a.out = m->att;
+  a.ld_q = a.ld_out = m->Dq;
+  a.q_start = m->ext_start;
+  a.kv_len = m->d_seq_len;
+  a.row_pos = m->ext_pos;
+  a.n_rows = max_rows;
+  a.n_heads = m->H;
+  a.max_q = e.max_len;
+  a.max_kv = e.max_kv;
+  a.scale_log2 = 1.4426950408889634f / sqrtf((float)m->dh);
+  a.part = m->ext_ws;
+  int n = 0;
+  const cudaError_t err = launch_chunk_attention(st, a, &n);
+  m->launches += 1 + n;
+  if (err != cudaSuccess) m->deferred = fail(m, ADEPT_ERR_CUDA, "chunk attention: %s", cudaGetErrorString(err));
+}
+
 // One early-exit pass over n_tok tokens.  The threshold delta is read from m->d_delta
-// (device memory), so a captured generation step does not depend on it.
+// (device memory), so a captured generation step does not depend on it.  ext: the tokens are
+// the sequences' next chunks (m->d_ext), not prompts.
 static adept_status run_pass(adept_model* m, int n_tok, int batch, int prompt_len, bool decode, const int32_t* tokens,
-                             const int32_t* forced, int32_t* exit_out, float* sim_out, cudaStream_t st) {
+                             const int32_t* forced, int32_t* exit_out, float* sim_out, cudaStream_t st,
+                             const ExtendPass* ext = nullptr) {
   m->gemm_cls = decode ? ADEPT_PROF_GEMM_DECODE : ADEPT_PROF_GEMM_PREFILL;
   const adept_config& c = m->cfg;
   const int N = m->N, D = m->D, Dq = m->Dq, Dkv = m->Dkv;
@@ -1095,7 +1139,7 @@ static adept_status run_pass(adept_model* m, int n_tok, int batch, int prompt_le
   if (!decode) {   // (a generation step's is part of its first launch)
     launch_pass_init(st, n_tok, prompt_len, m->tok_seq, m->tok_pos, m->row_tok[0], m->d_seq_len,
                      m->max_blocks_per_seq * c.kv_block_tokens, fam == ADEPT_FAMILY_LLAMA ? 0 : c.max_pos, m->err_word,
-                     m->ctr, ctr_words(N), sim_out, N, stop ? m->tok_exit : nullptr);
+                     m->ctr, ctr_words(N), sim_out, N, stop ? m->tok_exit : nullptr, ext ? m->d_ext : nullptr, batch);
     m->launches += 1;
   }
   // the producer of each layer's input (the embedding, then the exit step) also writes it as the
@@ -1195,11 +1239,15 @@ static adept_status run_pass(adept_model* m, int n_tok, int batch, int prompt_le
     {
       cudaEvent_t b = nullptr;
       prof_begin(m, ADEPT_PROF_ATTENTION, st, &b);
-      launch_attention(st, m->dt, m->q, Dq, m->att, Dq, act, mr, rt, m->tok_seq, m->tok_pos, m->d_seq_len, cv, l0,
-                       m->H, causal, decode_keys, m->attn_ws, m->attn_ctr, m->err_word, stop ? m->tok_exit : nullptr,
-                       prompt_len, m->use_attn_tc ? m->T_max : 0, N);
+      if (ext) {
+        extend_attention(m, st, *ext, l0, batch, m->ctr + CTR_ACTIVE + par, mr, rt);
+      } else {
+        launch_attention(st, m->dt, m->q, Dq, m->att, Dq, act, mr, rt, m->tok_seq, m->tok_pos, m->d_seq_len, cv, l0,
+                         m->H, causal, decode_keys, m->attn_ws, m->attn_ctr, m->err_word, stop ? m->tok_exit : nullptr,
+                         prompt_len, m->use_attn_tc ? m->T_max : 0, N);
+        m->launches += 1;
+      }
       prof_end(m, ADEPT_PROF_ATTENTION, st, b, 0, 0);
-      m->launches += 1;
     }
     // O projection + residual
     GemmProblem p;
@@ -1336,14 +1384,15 @@ static adept_status run_pass(adept_model* m, int n_tok, int batch, int prompt_le
 }
 
 static adept_status run_head(adept_model* m, int batch, int prompt_len, bool decode, float* logits, int32_t* next,
-                             cudaStream_t st) {
+                             cudaStream_t st, const int* ext = nullptr) {
   const adept_config& c = m->cfg;
   const int D = m->D;
   const bool enc = c.family == ADEPT_FAMILY_BERT;
   float* out = logits ? logits : m->logits_ws;
   const bool rows_ready = !enc && decode && m->xhead_ready;   // head input already in xhead
   if (!rows_ready) {
-    launch_head_rows(st, batch, decode ? 1 : prompt_len, enc ? 0 : 1, m->head_rows);
+    if (ext) launch_chunk_head_rows(st, batch, ext, m->head_rows);
+    else launch_head_rows(st, batch, decode ? 1 : prompt_len, enc ? 0 : 1, m->head_rows);
     m->launches += 1;
   }
   const DevRange rows{nullptr, nullptr, batch};
@@ -1820,6 +1869,78 @@ adept_status adept_prefill(adept_model* m, int batch, int prompt_len, const int3
   TRY(run_pass(m, batch * prompt_len, batch, prompt_len, false, d_tokens, d_forced_exit, d_exit_layer_out, d_sim_out,
                st));
   TRY(run_head(m, batch, prompt_len, false, d_logits_out, d_next_token_out, st));
+  span_collect(m, st);
+  return check_launch(m);
+}
+
+static adept_status extend_init(adept_model* m) {
+  if (m->ext_ws) return ADEPT_OK;
+  const int B = m->cfg.max_batch;
+  // (the bound over every batch and length)
+  const size_t ws = std::max(chunk_workspace(paged_view(m, 0, B), m->H, m->T_max, m->max_blocks_per_seq * m->cfg.kv_block_tokens),
+                             chunk_workspace(paged_view(m, 0, B), m->H, 1, m->max_blocks_per_seq * m->cfg.kv_block_tokens));
+  if (!m->d_ext) TRY(dalloc_t(m, &m->d_ext, (size_t)2 * B + 1));
+  if (!m->ext_start) TRY(dalloc_t(m, &m->ext_start, (size_t)B + 1));
+  if (!m->ext_pos) TRY(dalloc_t(m, &m->ext_pos, (size_t)m->T_max));
+  return dalloc(m, (void**)&m->ext_ws, std::max<size_t>(ws, 16));
+}
+
+adept_status adept_extend(adept_model* m, int batch, const int32_t* h_lens, const int32_t* d_tokens, float delta,
+                          const int32_t* d_forced_exit, int32_t* d_exit_layer_out, float* d_logits_out,
+                          int32_t* d_next_token_out, float* d_sim_out, void* stream) {
+  if (!m) return ADEPT_ERR_INVALID_ARG;
+  g_pdl = !m->profile;
+  if (m->cfg.family == ADEPT_FAMILY_BERT) return fail(m, ADEPT_ERR_INVALID_ARG, "adept_extend needs a decoder model");
+  if (!h_lens || !d_tokens) return fail(m, ADEPT_ERR_INVALID_ARG, "h_lens or d_tokens is NULL");
+  if (batch < 1) return fail(m, ADEPT_ERR_INVALID_ARG, "batch must be positive");
+  if (batch > m->cfg.max_batch) return fail(m, ADEPT_ERR_CAPACITY, "batch %d > max_batch %d", batch, m->cfg.max_batch);
+  if (std::isnan(delta)) return fail(m, ADEPT_ERR_INVALID_ARG, "delta is NaN");
+  if (m->all_at_once)
+    return fail(m, ADEPT_ERR_INVALID_ARG, "all-at-once exits are defined for whole prompts (adept_prefill)");
+  TRY(check_cross_set(m, batch));
+  long long total = 0;
+  ExtendPass e{0, 0};
+  for (int b = 0; b < batch; ++b) {
+    if (h_lens[b] < 0) return fail(m, ADEPT_ERR_INVALID_ARG, "length %d of sequence %d", h_lens[b], b);
+    if (h_lens[b] == 0) continue;
+    if (m->seq_blocks[b].empty())
+      return fail(m, ADEPT_ERR_INVALID_ARG, "sequence %d is not reserved (adept_prefill or adept_seq_reserve)", b);
+    if ((long long)m->h_seq_len[b] + h_lens[b] > m->cfg.max_seq)
+      return fail(m, ADEPT_ERR_CAPACITY, "sequence %d: %d positions and %d new tokens, max_seq %d", b, m->h_seq_len[b], h_lens[b],
+                  m->cfg.max_seq);
+    total += h_lens[b];
+    e.max_len = std::max(e.max_len, h_lens[b]);
+    e.max_kv = std::max(e.max_kv, m->h_seq_len[b] + h_lens[b]);
+  }
+  if (total < 1) return fail(m, ADEPT_ERR_INVALID_ARG, "no sequence has a new token");
+  if (total > m->T_max)
+    return fail(m, ADEPT_ERR_CAPACITY, "%lld new tokens above the pass workspace (%d rows)", total, m->T_max);
+  TRY(extend_init(m));
+  cudaStream_t st = (cudaStream_t)stream;
+  m->h_ext.assign((size_t)2 * batch + 1, 0);
+  for (int b = 0; b < batch; ++b) {
+    m->h_ext[b + 1] = m->h_ext[b] + h_lens[b];
+    m->h_ext[batch + 1 + b] = m->h_seq_len[b];
+    e.max_kv = std::max(e.max_kv, m->h_seq_len[b]);   // (sequences without new tokens stay within the bound)
+  }
+  CUDA_TRY(m, cudaMemcpyAsync(m->d_ext, m->h_ext.data(), m->h_ext.size() * sizeof(int), cudaMemcpyHostToDevice, st));
+  launch_set_float(st, m->d_delta, delta);
+  m->launches += 1;
+  TRY(run_pass(m, (int)total, batch, 0, false, d_tokens, d_forced_exit, d_exit_layer_out, d_sim_out, st, &e));
+  for (int b = 0; b < batch; ++b) m->h_seq_len[b] += h_lens[b];
+  // the head over all rows; where a sequence brought nothing its outputs are left as they were
+  bool all = true;
+  for (int b = 0; b < batch; ++b) all &= h_lens[b] > 0;
+  TRY(run_head(m, batch, 0, false, all ? d_logits_out : m->logits_ws, d_next_token_out ? (all ? d_next_token_out : m->dec_tok) : nullptr,
+               st, m->d_ext));
+  for (int b = 0; b < batch && !all; ++b) {
+    if (h_lens[b] == 0) continue;
+    if (d_logits_out)
+      CUDA_TRY(m, cudaMemcpyAsync(d_logits_out + (size_t)b * m->V, m->logits_ws + (size_t)b * m->V, (size_t)m->V * sizeof(float),
+                                  cudaMemcpyDeviceToDevice, st));
+    if (d_next_token_out)
+      CUDA_TRY(m, cudaMemcpyAsync(d_next_token_out + b, m->dec_tok + b, sizeof(int32_t), cudaMemcpyDeviceToDevice, st));
+  }
   span_collect(m, st);
   return check_launch(m);
 }

@@ -185,6 +185,34 @@ def test_later_positions_may_hold_anything(dtype, heads, hk, dh, new, past, bad)
     assert torch.equal(out[:, :heads - heads // hk], clean[:, :heads - heads // hk])
 
 
+@pytest.mark.parametrize("dtype,heads,hk,dh", [("f32", 4, 2, 64), ("bf16", 8, 2, 128), ("bf16", 6, 6, 64), ("e4m3", 8, 2, 128),
+                                               ("bf16", 4, 4, 32)])
+@pytest.mark.parametrize("new,keep", [([6, 1, 0, 9], 0.6), ([700, 40, 1, 3], 0.5), ([300, 2, 260, 0], 0.95)])
+def test_rows_at_given_positions(dtype, heads, hk, dh, new, keep):
+    """Rows of some of a chunk's tokens only, at their own positions: the same rows of the whole chunk's reference."""
+    past = [130, 0, 77, 500]
+    lens = [a + b for a, b in zip(new, past)]
+    c = make_cache(dtype, hk, dh, lens, 50)
+    q, starts = make_q(dtype, new, heads, dh, 51)
+    want, tol = R.attention(c, q, starts, lens)
+    g = torch.Generator().manual_seed(52)
+    pick = torch.rand(sum(new), generator=g) < keep
+    pos = torch.cat([torch.arange(p, p + n) for n, p in zip(new, past)])
+    rows = pick.nonzero().flatten()
+    st = [int((rows < s).sum()) for s in starts]
+    sub = torch.cat([q[rows.cuda()], q[:2]])                 # two rows behind the last sequence's
+    out = torch.full_like(sub, -7.0)
+    row_pos = _i32(pos[rows].tolist() + [0, 0])
+    adept.adept_chunk_attention(c, sub, _i32(st), _i32(lens), max(new), max(lens), out, row_pos=row_pos)
+    c.check()
+    assert (out[len(rows):] == -7).all()
+    err = (out[:len(rows)].double() - want[rows.cuda()]).abs()
+    assert (err <= tol[rows.cuda()] + 1e-30).all()
+    again = torch.full_like(sub, -7.0)
+    adept.adept_chunk_attention(c, sub, _i32(st), _i32(lens), max(new), max(lens), again, row_pos=row_pos)
+    assert torch.equal(out, again)
+
+
 @pytest.mark.parametrize("dtype,heads,hk,dh", [("f32", 2, 1, 64), ("bf16", 8, 2, 128), ("e4m3", 4, 4, 64)])
 def test_rows_without_keys_are_zero(dtype, heads, hk, dh):
     c = make_cache(dtype, hk, dh, [4, 0, 20], 13)
@@ -473,3 +501,25 @@ def test_offsets_past_32_bits(dtype):
         q, starts = make_q(dtype, [new], 16, dh, 36)
         out = attend(c, q, starts, [128])
         assert_attention(small, q, starts, [128], out)
+
+
+@pytest.mark.parametrize("dtype,new", [("bf16", [1]), ("e4m3", [2]), ("bf16", [200]), ("e4m3", [150])])
+def test_waits_of_one_cycle(dtype, new):
+    """A wait that has to be taken up again gives up at once: the call either comes through (the hardware's own wait was long
+    enough) or reports the time-out, its copies landed; the next call is whole again."""
+    lens = [n + 700 for n in new]
+    c = make_cache(dtype, 4, 128, lens, 60)
+    q, starts = make_q(dtype, new, 8, 128, 61)
+    want = attend(c, q, starts, lens)
+    try:
+        adept.adept_set_wait_limit(1)
+        out = attend(c, q, starts, lens)
+        try:
+            c.check()
+            assert torch.equal(out, want)
+        except adept.AdeptError as e:
+            assert e.status == 5
+    finally:
+        adept.adept_set_wait_limit(0)
+    assert torch.equal(attend(c, q, starts, lens), want)
+    c.check()
