@@ -1,792 +1,13 @@
-// Attention of a chunk of new tokens over a paged K/V cache on the tcgen05 tensor cores (what it computes:
-// attention_chunk.cu), for the calls whose sequences bring more rows than a warp-level tile.
-//
-// Tile: two sub-tiles of 128 rows (row = token x query head of one KV head's group, all of one sequence) x key tiles of 128.
-// Per key tile and sub-tile S = Q K^T (M 128, N 128, K d_h) and O += P V (P from tensor memory, V as stored, MN-major).
-// The two sub-tiles alternate: while the softmax of one runs, the tensor core works on the other.  Tensor memory (512
-// columns): S of sub-tile 0 and 1 (128 each), O of 0 and 1 (128 each); P (bf16, 64 columns) takes the place of its S.
-//
-// Warps:   0..3, 4..7   softmax of sub-tile 0 and 1, a thread per row (its TMEM lane): 128 scores in registers, running
-//                       maximum (raised only by more than 2^8), exp2, sum, P to tensor memory; at the end O / l
-//          8            issues the matrix instructions:  PV_0(j) S_0(j+1) PV_1(j) S_1(j+1)  (in issue order on the tensor
-//                       core, so S_0(j+1) may overwrite P_0(j), and a completed S(j+1) means a completed PV(j))
-//          9, 10        fetch K and V blocks by TMA; 10 mends the V tiles at the causal edge (11: idle)
-//
-// The causal edge: from the first row's position on, a key tile holds keys that not every row attends, or none does.  Scores are
-// masked there.  V entries that nobody attends become zero; a NaN or infinite one is replaced by zero and its key noted per
-// column (the least one), and a row that attends that key gets NaN in that column at the end: 0 * NaN reaches nobody else.
-//
-// Work: every (tile, KV head) is a row of key tiles; all of them in a row are cut into equal runs, one per CTA (one CTA per SM),
-// so the GPU is evenly loaded whatever the mix of lengths.  A run holds whole tiles and at most two parts of tiles, whose
-// (maximum, sum, weighted V) go to the workspace and are joined in order by a second launch.
-// 8-bit entries: a launch of its own first turns the positions of this kernel's sequences into bf16 (exactly: code * 2^e) in the
-// workspace, once for all the tiles that read them.  Turned by warps of this kernel, tile by tile, they came at 9000 cycles
-// a key tile (2048 of matrix instructions): a mixed batch took 121 us.
-// Every wait is bounded; a CTA that gives up sets the error word, drains its copies and matrix instructions and leaves.
+// Launches of the tcgen05 chunk attention (attention_chunk_tc.cuh): what it takes, its workspace, its launches.
 #define ADEPT_TU_ID 13
-#include "kv_paged.h"
+#include "attention_chunk_tc.cuh"
 #include "gemm_tc.h"
-#include "tc_ptx.cuh"
-
-#include <cuda_fp8.h>
 
 #include <algorithm>
 #include <cstring>
 
 namespace adept {
 namespace {
-
-constexpr int CT_BM = 128, CT_BN = 128, CT_ROWS = 2 * CT_BM;
-constexpr float CT_RAISE = 8.f;
-constexpr long long CT_DRAIN_CYCLES = 4000000000LL;
-
-template <int DH>
-struct CtShape {
-  static constexpr int THREADS = 12 * 32;   // (three whole warpgroups, for setmaxnreg)
-  static constexpr int HALVES = DH / 64;
-  static constexpr int Q_BYTES = HALVES * CT_BM * 128;             // one sub-tile: [half][row][128 B]
-  static constexpr int KV_BYTES = HALVES * CT_BN * 128;            // one K or V stage: [half][key][128 B]
-  static constexpr int OFF_K = 2 * Q_BYTES, OFF_V = OFF_K + 2 * KV_BYTES, OFF_ST = OFF_V + 2 * KV_BYTES;
-  static constexpr int TOTAL = OFF_ST + 8 * 2048;                  // 32 rows x 64 bytes of output per softmax warp
-};
-
-struct CtParams {
-  ChunkCall a;
-  CUtensorMap kmap, vmap;   // K and V as [n_blocks * n_kv_heads * 16][d_h], box {64, 16}
-  CUtensorMap qmap;         // Q as [n_rows][n_heads][d_h], box {64, heads of a group, ts}
-  int ts;                   // tokens of a sub-tile
-  int runs;                 // CTAs
-  int wide;                 // > 0: the maps are of widened entries, `wide` blocks per sequence in order
-  unsigned* no_err;         // where time-outs go without an error word (the workspace's last word)
-};
-
-// ---- the key tiles of all tiles in a row ----
-
-// sum over i in [0, n) of floor((a i + b) / m); a n + b below 2^32
-__device__ long long floor_sum(unsigned n, unsigned m, unsigned a, unsigned b) {
-  long long r = 0;
-  while (n > 0) {
-    r += (long long)(n - 1) * n / 2 * (a / m) + (long long)n * (b / m);
-    a %= m;
-    b %= m;
-    const unsigned y = a * n + b, x = m;
-    n = y / m;
-    b = y % m;
-    m = a;
-    a = x;
-    if (m == 0) break;
-  }
-  return r;
-}
-// Key tiles of token tile t (at least one: a tile without keys has zeros to write; with given positions, those of the whole
-// sequence).
-__device__ __forceinline__ int ct_units(bool given, int c, int len, int tq, int t) {
-  return max(1, (given ? len + CT_BN - 1 : len - c + min((t + 1) * tq, c) + CT_BN - 1) / CT_BN);
-}
-__device__ long long ct_seq_units(bool given, int c, int len, int tq) {
-  const int tiles = (c + tq - 1) / tq;
-  if (tiles == 0) return 0;
-  if (given) return (long long)tiles * ct_units(true, c, len, tq, 0);
-  const long long last = ct_units(false, c, len, tq, tiles - 1);
-  if (tiles == 1) return last;
-  if (len - c + tq < 1) {   // (first tiles without keys: one by one)
-    long long r = 0;
-    for (int t = 0; t < tiles; ++t) r += ct_units(false, c, len, tq, t);
-    return r;
-  }
-  return last + floor_sum((unsigned)tiles - 1, CT_BN, (unsigned)tq, (unsigned)(len - c + tq + CT_BN - 1));
-}
-
-struct CtTile {
-  int seq, q0, c, len, tile, kvh;
-  long long u0;   // first unit of the tile
-  int units;
-};
-// All units, taken together by a converged warp.
-__device__ long long ct_total(const ChunkCall& a, int tq) {
-  long long tot = 0;
-  for (int b = threadIdx.x & 31; b < a.c.n_seq; b += 32) {
-    int q0, c, len;
-    chunk_seq(a, b, q0, c, len);
-    tot += ct_seq_units(a.row_pos, c, len, tq) * a.c.n_kv_heads;
-  }
-  // (24 bits and the rest: one instruction each)
-  return __reduce_add_sync(0xffffffffu, (unsigned)(tot & 0xffffff)) +
-         ((long long)__reduce_add_sync(0xffffffffu, (unsigned)(tot >> 24)) << 24);
-}
-// The tile that unit u lies in.
-__device__ void ct_find(const ChunkCall& a, int tq, long long u, CtTile& x) {
-  const int lane = threadIdx.x & 31;
-  long long before = 0;
-  for (int b0 = 0; b0 < a.c.n_seq; b0 += 32) {
-    int q0 = 0, c = 0, len = 0;
-    if (b0 + lane < a.c.n_seq) chunk_seq(a, b0 + lane, q0, c, len);
-    const long long mine = ct_seq_units(a.row_pos, c, len, tq) * a.c.n_kv_heads;
-    long long inc = mine;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const long long v = __shfl_up_sync(0xffffffffu, inc, o);
-      if (lane >= o) inc += v;
-    }
-    const unsigned who = __ballot_sync(0xffffffffu, u < before + inc);
-    if (!who) {
-      before += __shfl_sync(0xffffffffu, inc, 31);
-      continue;
-    }
-    const int src = __ffs(who) - 1;
-    before += __shfl_sync(0xffffffffu, inc - mine, src);
-    x.seq = b0 + src;
-    x.q0 = __shfl_sync(0xffffffffu, q0, src);
-    x.c = __shfl_sync(0xffffffffu, c, src);
-    x.len = __shfl_sync(0xffffffffu, len, src);
-    const int tiles = (x.c + tq - 1) / tq;
-    for (int t0 = 0; t0 < tiles; t0 += 32) {
-      const int t = t0 + lane;
-      const long long n = t < tiles ? (long long)ct_units(a.row_pos, x.c, x.len, tq, t) * a.c.n_kv_heads : 0;
-      long long in2 = n;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const long long v = __shfl_up_sync(0xffffffffu, in2, o);
-        if (lane >= o) in2 += v;
-      }
-      const unsigned w2 = __ballot_sync(0xffffffffu, u < before + in2);
-      if (!w2) {
-        before += __shfl_sync(0xffffffffu, in2, 31);
-        continue;
-      }
-      const int s2 = __ffs(w2) - 1;
-      before += __shfl_sync(0xffffffffu, in2 - n, s2);
-      x.tile = t0 + s2;
-      x.units = ct_units(a.row_pos, x.c, x.len, tq, x.tile);
-      x.kvh = (int)((u - before) / x.units);
-      x.u0 = before + (long long)x.kvh * x.units;
-      return;
-    }
-    return;
-  }
-}
-// The tile behind x.
-__device__ __forceinline__ void ct_next(const ChunkCall& a, int tq, CtTile& x) {
-  x.u0 += x.units;
-  if (++x.kvh < a.c.n_kv_heads) return;
-  x.kvh = 0;
-  if (++x.tile * tq >= x.c) {
-    x.tile = 0;
-    x.c = 0;
-    while (x.c == 0 && ++x.seq < a.c.n_seq) chunk_seq(a, x.seq, x.q0, x.c, x.len);
-  }
-  x.units = ct_units(a.row_pos, x.c, x.len, tq, x.tile);
-}
-// Run i of `runs` (fewer where there are few units).
-constexpr int CT_MIN_RUN = 2;
-__device__ __forceinline__ int ct_runs(long long total, int runs) {
-  return (int)min((long long)runs, (total + CT_MIN_RUN - 1) / CT_MIN_RUN);
-}
-__device__ __forceinline__ long long ct_start(long long total, int runs, int i) { return total * i / runs; }
-
-// Workspace: a note per run on the tile it begins inside of; per slot (two a run) 256 (m, l) pairs; and per slot 256 rows of
-// weighted V, four columns of all rows after the other (a warp of rows writes whole lines).
-struct CtNote {
-  long long u0;       // first unit of the tile, -1: the run begins with a tile, or is empty
-  int row0, kvh, pos0, n_tok;   // the tile's first row of Q, KV head, first position, tokens
-  int pad[2];         // (32 bytes: what follows is read 16 at a time)
-};
-struct CtWs {
-  CtNote* note;
-  float* ml;
-  float* o;
-  __device__ CtWs(const CtParams& p)
-      : note((CtNote*)p.a.part), ml(p.a.part + (size_t)p.runs * (sizeof(CtNote) / 4)), o(ml + (size_t)p.runs * 2 * CT_ROWS * 2) {}
-  __device__ __forceinline__ float2* ml_at(int slot, int r) const {
-    return reinterpret_cast<float2*>(ml) + (size_t)slot * CT_ROWS + r;
-  }
-  __device__ __forceinline__ float4* o_at(int slot, int dh, int d4, int r) const {
-    return reinterpret_cast<float4*>(o) + ((size_t)slot * (dh / 4) + d4) * CT_ROWS + r;
-  }
-};
-constexpr size_t ct_ws_floats(int runs, int dh) {
-  return (size_t)runs * (sizeof(CtNote) / 4) + (size_t)runs * 2 * CT_ROWS * (dh + 2);
-}
-
-// Non-finite bf16 of a pair: 0xffff in its half; and whether there is one (a carry out of an exponent of all ones).
-__device__ __forceinline__ uint32_t ct_bad2(uint32_t x) { return __vcmpeq2(x & 0x7f807f80u, 0x7f807f80u); }
-__device__ __forceinline__ uint32_t ct_any_bad2(uint32_t x) { return ((x & 0x7f807f80u) + 0x00800080u) & 0x80008000u; }
-
-// Two fp32 at once.
-__device__ __forceinline__ uint64_t f2_pack(float a, float b) {
-  uint64_t r;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
-  return r;
-}
-__device__ __forceinline__ void f2_unpack(uint64_t x, float& a, float& b) {
-  asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(x));
-}
-__device__ __forceinline__ uint64_t f2_fma(uint64_t a, uint64_t b, uint64_t c) {
-  uint64_t r;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-  return r;
-}
-__device__ __forceinline__ uint64_t f2_add(uint64_t a, uint64_t b) {
-  uint64_t r;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-  return r;
-}
-__device__ __forceinline__ float max3(float a, float b, float c) {
-  float r;
-  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
-  return r;
-}
-
-// A CTA's part of one tile: key tiles j_lo .. j_hi.
-struct CtSeg {
-  CtTile x;
-  int j_lo, j_hi, t0, n_tok;
-  int lim_lo, k_end;   // keys of the tile's first and of its last token (nobody attends beyond)
-  int nt0, nt1, n_it;  // key tiles with keys: per sub-tile, of the segment
-  bool whole;          // the whole tile
-  const int* table;
-  __device__ __forceinline__ void set(const ChunkCall& a, int ts, const CtTile& tile, long long u, long long u_end) {
-    x = tile;
-    j_lo = (int)(u - x.u0);
-    j_hi = (int)min((long long)x.units, u_end - x.u0);
-    whole = j_lo == 0 && j_hi == x.units;
-    t0 = x.tile * 2 * ts;
-    n_tok = min(2 * ts, x.c - t0);
-    lim_lo = keys(a, 0);
-    k_end = keys(a, n_tok - 1);
-    const int k_end0 = keys(a, min(ts, n_tok) - 1);
-    nt0 = max(min(j_hi, (k_end0 + CT_BN - 1) / CT_BN) - j_lo, 0);
-    nt1 = n_tok > ts ? max(min(j_hi, (k_end + CT_BN - 1) / CT_BN) - j_lo, 0) : 0;
-    n_it = max(nt0, nt1);
-    table = a.c.table + (size_t)x.seq * a.c.max_blocks;
-  }
-  // keys that token `tok` of the tile attends
-  __device__ __forceinline__ int keys(const ChunkCall& a, int tok) const { return chunk_lim(a, x.q0, x.c, x.len, t0 + tok); }
-  __device__ __forceinline__ int nt(int sub) const { return sub ? nt1 : nt0; }
-  // key tile j (from the segment's first) holds keys that are not everybody's
-  __device__ __forceinline__ bool edge(int j) const { return (j_lo + j + 1) * CT_BN > lim_lo || (j_lo + j + 1) * CT_BN > k_end; }
-  // the row of key block b (from the sequence's first) in the pools seen as rows of d_h, -1: nobody's, -2: not there
-  __device__ __forceinline__ int row_of(const KvPaged& c, int wide, int b) const {
-    if (b * 16 >= k_end) return -1;
-    const int blk = table[b];
-    if (blk < 0 || blk >= c.n_blocks) return -2;
-    return ((wide ? x.seq * wide + b : blk) * c.n_kv_heads + x.kvh) * 16;
-  }
-};
-
-__device__ __forceinline__ void tma_load_q(const CUtensorMap* tm, uint64_t* bar, void* dst, int col, int head, int row) {
-  asm volatile(
-      "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(
-          smem_u32(dst)),
-      "l"((uint64_t)tm), "r"(col), "r"(head), "r"(row), "r"(smem_u32(bar)));
-}
-
-// The segments of a CTA follow each other without a stop: every role walks the tiles by itself, and meets the others at
-// barriers only: Q full / free, a K or V stage full / free, S, P (two halves), O.  (With a stop of all warps, a
-// look-up and Q's loads by all threads at each of a run's two or three segments, a call of ten key tiles a CTA took 70000
-// cycles, 27000 of them on key tiles.)
-template <int DH>
-__global__ void __launch_bounds__(CtShape<DH>::THREADS, 1) chunk_tc_kernel(const __grid_constant__ CtParams p) {
-  using L = CtShape<DH>;
-  extern __shared__ __align__(1024) uint8_t ct_raw[];
-  __shared__ __align__(8) uint64_t q_full, q_free, k_full[2], v_full[2], k_empty[2], v_empty[2], s_full[2], p_half[2], p_full[2],
-      o_full[2], v_fix[2], drain;
-  __shared__ uint32_t s_tmem;
-  __shared__ int s_abort;
-  __shared__ int s_gone[4];      // blocks of a key tile that are not there, by tile % 4
-  __shared__ int s_pk[4][DH];    // least key with a non-finite V entry, per column (causal edge), by segment with keys % 4
-  __shared__ int s_poisoned[4];
-  __shared__ int s_tok[CT_ROWS], s_off[CT_ROWS];   // token of a row in the tile (-1: none), its head's first column in the group
-  __shared__ CtTile s_tile;
-  __shared__ long long s_u0, s_u1;
-
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const long long wlim = wait_limit();
-  volatile int* abort_flag = &s_abort;
-  uint8_t* sm = ct_raw + ((1024 - (smem_u32(ct_raw) & 1023)) & 1023);
-  uint8_t *sQ = sm, *sK = sm + L::OFF_K, *sV = sm + L::OFF_V;
-  const ChunkCall& a = p.a;
-  unsigned* err = a.c.err ? a.c.err : p.no_err;
-
-  if (tid == 0) {
-    mbar_init(&q_full, 1);
-    mbar_init(&q_free, 1);
-    for (int s = 0; s < 2; ++s) {
-      mbar_init(&k_full[s], 1);
-      mbar_init(&v_full[s], 1);
-      mbar_init(&k_empty[s], 1);
-      mbar_init(&v_empty[s], 1);
-      mbar_init(&s_full[s], 1);
-      mbar_init(&p_half[s], 4);
-      mbar_init(&p_full[s], 4);
-      mbar_init(&o_full[s], 1);
-      mbar_init(&v_fix[s], 1);
-    }
-    mbar_init(&drain, 1);
-    s_abort = 0;
-    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-  }
-  const int group = a.n_heads / a.c.n_kv_heads, ts = p.ts, tq = 2 * ts, run = (int)blockIdx.x;
-  if (warp == 8) {
-    tmem_alloc(&s_tmem, 512);
-    tmem_relinquish();
-  }
-  if (warp < 8) {   // (a row per thread)
-    const int rr = tid & 127, tk = rr / group;
-    s_tok[tid] = tk < ts ? (tid >> 7) * ts + tk : -1;
-    s_off[tid] = rr % group * DH;
-  }
-  pdl_wait();
-  if (warp == 9) {
-    const long long tot = ct_total(a, tq);
-    const int runs = ct_runs(tot, p.runs);
-    const long long u0 = run < runs ? ct_start(tot, runs, run) : 0, u1 = run < runs ? ct_start(tot, runs, run + 1) : 0;
-    CtTile x{};
-    if (u0 < u1) ct_find(a, tq, u0, x);
-    if (lane == 0) {
-      s_u0 = u0;
-      s_u1 = u1;
-      s_tile = x;
-      // the join's note: what tile this run begins inside of
-      const int t0 = x.tile * tq;
-      CtWs(p).note[run] = CtNote{u0 < u1 && u0 > x.u0 ? x.u0 : -1, x.q0 + t0, x.kvh, x.len - x.c + t0, min(tq, x.c - t0), {0, 0}};
-    }
-  }
-  tc_fence_before();
-  __syncthreads();
-  tc_fence_after();
-  pdl_launch_dependents();   // after the tensor memory is held
-  const uint32_t tmem = s_tmem;
-  const long long u_end = s_u1;
-  long long u = s_u0;
-  CtTile x = s_tile;
-  CtSeg g{};
-  bool ok = true;
-
-  // 384 x 168 registers at launch: 256 x 208 + 128 x 88
-  if (warp < 8) {
-    // ---- softmax of a row per thread
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
-    const int sub = warp >> 2, r = tid & 127, tok = s_tok[tid];
-    const uint32_t base = tmem + ((uint32_t)((warp & 3) * 32) << 16), s_col = base + (uint32_t)(sub * 128),
-                   o_col = base + 256u + (uint32_t)(sub * 128);
-    const float sc = a.scale_log2;
-    const CtWs ws(p);
-    uint8_t* stage = sm + L::OFF_ST + warp * 2048;
-    int ns = 0, no = 0, kt = 0;   // S tiles, outputs, key tiles so far
-    int seg = -1;   // segments with keys so far
-    while (u < u_end) {
-      g.set(a, ts, x, u, u_end);
-      seg += g.n_it > 0;
-      const bool mine = tok >= 0 && tok < g.n_tok;
-      const int lim = mine ? g.keys(a, tok) : 0;
-      const int sub_lo = sub * ts < g.n_tok ? g.keys(a, sub * ts) : 0;   // keys of the sub-tile's first token
-      const int n_my = g.nt(sub);
-      float m = -INFINITY, l = 0.f;
-      for (int j = 0; j < n_my; ++j) {
-        if (!(ok = mbar_wait_warp(&s_full[sub], (uint32_t)(ns & 1), abort_flag, err, wlim))) break;
-        ++ns;
-        tc_fence_after();
-        float s[CT_BN];
-        tmem_ld128(s_col, s);
-        const int k0 = (g.j_lo + j) * CT_BN, gone = s_gone[(kt + j) & 3];
-        if (k0 + CT_BN > sub_lo || gone) {
-          const int nk_r = lim - k0;
-#pragma unroll
-          for (int e = 0; e < CT_BN; ++e)
-            if (e >= nk_r || (gone >> (e >> 4) & 1)) s[e] = -INFINITY;
-        }
-        float mx[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) mx[e] = max3(s[e], s[e + 8], s[e + 16]);
-#pragma unroll
-        for (int e = 24; e < CT_BN - 8; e += 16)
-#pragma unroll
-          for (int q = 0; q < 8; ++q) mx[q] = max3(mx[q], s[e + q], s[e + 8 + q]);
-#pragma unroll
-        for (int q = 0; q < 8; ++q) mx[q] = fmaxf(mx[q], s[CT_BN - 8 + q]);
-        const float tmax = fmaxf(max3(max3(mx[0], mx[1], mx[2]), mx[3], mx[4]), max3(mx[5], mx[6], mx[7])) * sc;
-        float m_new = m;
-        if (tmax > m && (m == -INFINITY || tmax - m > CT_RAISE)) m_new = tmax;
-        const float f = (m == -INFINITY || m_new == m) ? 1.f : ex2_approx(m - m_new);
-        if (__any_sync(0xffffffffu, f != 1.f)) {   // (S of this tile is complete, so O of the one before it is)
-#pragma unroll 1
-          for (int c = 0; c < DH / 32; ++c) {
-            float v[32];
-            tmem_ld32(o_col + (uint32_t)(c * 32), v);
-#pragma unroll
-            for (int e = 0; e < 32; ++e) v[e] *= f;
-            tmem_st32(o_col + (uint32_t)(c * 32), v);
-          }
-          l *= f;
-        }
-        m = m_new;
-        const float ref = m == -INFINITY ? 0.f : m;
-        const uint64_t sc2 = f2_pack(sc, sc), ref2 = f2_pack(-ref, -ref);
-        uint64_t sum[4] = {0, 0, 0, 0};
-        // P in two halves: O += P V of the first half's keys runs beside the second half's exponentials
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          uint32_t pk[32];
-#pragma unroll
-          for (int e = 0; e < 64; e += 2) {
-            float p0, p1;
-            f2_unpack(f2_fma(f2_pack(s[h * 64 + e], s[h * 64 + e + 1]), sc2, ref2), p0, p1);
-            p0 = ex2_approx(p0);
-            p1 = ex2_approx(p1);
-            sum[(e >> 1) & 3] = f2_add(sum[(e >> 1) & 3], f2_pack(p0, p1));
-            const __nv_bfloat162 pr = __floats2bfloat162_rn(p0, p1);
-            pk[e >> 1] = *reinterpret_cast<const uint32_t*>(&pr);
-          }
-          tmem_st32u(s_col + (uint32_t)(h * 32), pk);
-          tmem_st_wait();
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(h ? &p_full[sub] : &p_half[sub]);
-        }
-        float l0, l1;
-        f2_unpack(f2_add(f2_add(sum[0], sum[1]), f2_add(sum[2], sum[3])), l0, l1);
-        l += l0 + l1;
-      }
-      if (!ok) break;
-      kt += g.n_it;   // (the segment's key tiles: what s_gone goes by)
-      // O / l, or the part
-      float v[DH];
-      if (n_my > 0) {   // (the same for the whole warp)
-        if (!(ok = mbar_wait_warp(&o_full[sub], (uint32_t)(no & 1), abort_flag, err, wlim))) break;
-        ++no;
-        tc_fence_after();
-        if constexpr (DH == 128) tmem_ld128(o_col, v);
-        else tmem_ld64(o_col, v);
-      } else {
-#pragma unroll
-        for (int e = 0; e < DH; ++e) v[e] = 0.f;
-      }
-      if (n_my > 0 && s_poisoned[seg & 3]) {
-#pragma unroll
-        for (int e = 0; e < DH; ++e)
-          if (s_pk[seg & 3][e] < lim) v[e] = NAN;
-      }
-      if (sub == 0 || g.n_tok > ts) {
-        if (g.whole) {
-          // through the warp's stage, 32 columns at a time, so that whole sectors are written
-          const float inv = lim == 0 ? 0.f : 1.f / l;
-          bf16* out = (bf16*)a.out + (size_t)(g.x.q0 + g.t0) * a.ld_out + (size_t)g.x.kvh * group * DH;
-#pragma unroll
-          for (int c = 0; c < DH / 32; ++c) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              uint32_t w[4];
-#pragma unroll
-              for (int q = 0; q < 4; ++q) {
-                const __nv_bfloat162 pr = __floats2bfloat162_rn(v[c * 32 + 8 * e + 2 * q] * inv, v[c * 32 + 8 * e + 2 * q + 1] * inv);
-                w[q] = *reinterpret_cast<const uint32_t*>(&pr);
-              }
-              *reinterpret_cast<uint4*>(stage + lane * 64 + ((e ^ ((lane >> 1) & 3)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
-            }
-            __syncwarp();
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              const int rr = k * 8 + (lane >> 2), pc = lane & 3, row = warp * 32 + rr, tk = s_tok[row];
-              if (tk >= 0 && tk < g.n_tok)
-                *reinterpret_cast<uint4*>(out + tk * a.ld_out + s_off[row] + c * 32 + pc * 8) =
-                    *reinterpret_cast<const uint4*>(stage + rr * 64 + ((pc ^ ((rr >> 1) & 3)) << 4));
-            }
-            __syncwarp();
-          }
-        } else if (mine) {
-          const int slot = run * 2 + (g.j_lo == 0 ? 1 : 0);
-          *ws.ml_at(slot, sub * 128 + r) = make_float2(m, l);
-#pragma unroll
-          for (int e = 0; e < DH / 4; ++e)
-            *ws.o_at(slot, DH, e, sub * 128 + r) = make_float4(v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]);
-        }
-      }
-      ct_next(a, tq, x);
-      u = x.u0;
-    }
-  } else if (warp == 8) {
-    // ---- matrix instructions: one thread (a warp that meets at every wait took 3900 cycles a key tile to issue what the tensor
-    // core does in 2048), descriptors made once and moved by their address field
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
-    constexpr uint32_t IDESC_S = umma_idesc(CT_BN, false), IDESC_O = umma_idesc(DH, true);
-    const uint64_t dq = sdesc_sw128(smem_u32(sQ)), dk = sdesc_sw128(smem_u32(sK)), dv = sdesc_mn_sw128(smem_u32(sV), CT_BN * 128);
-    if (elect_one()) {
-      int nq = 0, nk = 0, nv = 0, np[2] = {0, 0}, nf[2] = {0, 0};   // Q, K, V, P so far, mended V per stage
-      auto wait = [&](uint64_t* bar, int phase) { return ok = mbar_wait(bar, (uint32_t)(phase & 1), abort_flag, err, wlim); };
-      while (u < u_end && ok) {
-        g.set(a, ts, x, u, u_end);
-        if (g.n_it > 0 && !wait(&q_full, nq++)) break;
-        for (int j = -1; j < g.n_it; ++j) {
-          const int kn = nk, vn = nv, ks = kn & 1, vs = vn & 1;
-          if (j + 1 < g.n_it) {
-            if (!wait(&k_full[ks], kn >> 1)) break;
-            ++nk;
-          }
-          if (j >= 0) {
-            if (!wait(&v_full[vs], vn >> 1)) break;
-            if ((g.edge(j) || s_gone[vn & 3]) && !wait(&v_fix[vs], nf[vs]++)) break;
-            ++nv;
-          }
-          const uint64_t dks = dk + (uint64_t)(ks * (L::KV_BYTES >> 4)), dvs = dv + (uint64_t)(vs * (L::KV_BYTES >> 4));
-#pragma unroll
-          for (int sub = 0; sub < 2; ++sub) {
-            if (j >= 0 && j < g.nt(sub)) {
-              const uint32_t pa = tmem + (uint32_t)(sub * 128), oa = tmem + 256u + (uint32_t)(sub * 128);
-              if (!wait(&p_half[sub], np[sub])) break;
-              // (a P of this segment: its warps have read O of the segment before)
-              tc_fence_after();
-#pragma unroll
-              for (int kk = 0; kk < 4; ++kk)
-                umma_bf16_ts(oa, pa + (uint32_t)(kk * 8), dvs + (uint64_t)(kk * (16 * 128 >> 4)), IDESC_O, (j > 0 || kk > 0) ? 1u : 0u);
-              if (!wait(&p_full[sub], np[sub])) break;
-              tc_fence_after();
-#pragma unroll
-              for (int kk = 4; kk < 8; ++kk)
-                umma_bf16_ts(oa, pa + (uint32_t)(kk * 8), dvs + (uint64_t)(kk * (16 * 128 >> 4)), IDESC_O, 1u);
-              ++np[sub];
-              if (j == g.nt(sub) - 1) umma_commit(&o_full[sub]);
-            }
-            if (j + 1 < g.nt(sub)) {
-              tc_fence_after();
-#pragma unroll
-              for (int kk = 0; kk < DH / 16; ++kk) {
-                const uint64_t at = (uint64_t)(((kk >> 2) * CT_BM * 128 + (kk & 3) * 32) >> 4);
-                umma_bf16(tmem + (uint32_t)(sub * 128), dq + (uint64_t)(sub * (L::Q_BYTES >> 4)) + at, dks + at, IDESC_S, kk > 0 ? 1u : 0u);
-              }
-              umma_commit(&s_full[sub]);
-            }
-          }
-          if (!ok) break;
-          if (j + 1 < g.n_it) umma_commit(&k_empty[ks]);
-          if (j + 1 == g.n_it - 1) umma_commit(&q_free);   // the segment's last S
-          if (j >= 0) umma_commit(&v_empty[vs]);
-        }
-        ct_next(a, tq, x);
-        u = x.u0;
-      }
-      // every matrix instruction has completed before tensor memory is given back
-      umma_commit(&drain);
-      const long long c0 = clock64();
-      while (!mbar_try_wait(&drain, 0) && clock64() - c0 < CT_DRAIN_CYCLES) {
-      }
-    }
-    __syncwarp();
-  } else if (warp == 11) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
-  } else {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
-    // ---- TMA producers: Q and K (warp 9), V (warp 10, which also mends the V tiles at the edge)
-    const bool kw = warp == 9;
-    uint64_t *full = kw ? k_full : v_full, *empty = kw ? k_empty : v_empty;
-    const CUtensorMap* map = kw ? &p.kmap : &p.vmap;
-    uint8_t* dst0 = kw ? sK : sV;
-    int cnt = 0, nq = 0;   // tiles, Qs sent so far
-    // V tile j (the vi-th, blocks `gone` of it not there): entries nobody attends to zero, non-finite ones noted
-    auto mend = [&](int j, int vi, int gone, int par) {
-      const int s = vi & 1;
-      if (!mbar_wait_warp(&v_full[s], (uint32_t)((vi >> 1) & 1), abort_flag, err, wlim)) return false;
-      uint8_t* v = sV + s * L::KV_BYTES;
-      const int k0 = (g.j_lo + j) * CT_BN, n_key = min(g.k_end - k0, CT_BN);
-      auto piece = [&](int hf, int key, int c) { return reinterpret_cast<uint4*>(v + hf * CT_BN * 128 + key * 128 + (c << 4)); };
-      // (first to zero: what was not fetched may hold anything)
-      for (int i = n_key * 8 + lane; i < CT_BN * 8; i += 32)
-        for (int hf = 0; hf < L::HALVES; ++hf) *piece(hf, i >> 3, i & 7) = make_uint4(0, 0, 0, 0);
-      if (gone)
-        for (int i = lane; i < CT_BN * 8; i += 32)
-          if (gone >> (i >> 7) & 1)
-            for (int hf = 0; hf < L::HALVES; ++hf) *piece(hf, i >> 3, i & 7) = make_uint4(0, 0, 0, 0);
-      __syncwarp();
-#pragma unroll 1
-      for (int i0 = 0; i0 < n_key * 8; i0 += 128) {   // 16 keys: a fetched block, or zeros
-        uint4 y[4 * L::HALVES];
-        uint32_t any = 0;
-#pragma unroll
-        for (int q = 0; q < 4 * L::HALVES; ++q) {
-          y[q] = *piece(q >> 2, (i0 >> 3) + (q & 3) * 4 + (lane >> 3), lane & 7);
-          any |= ct_any_bad2(y[q].x) | ct_any_bad2(y[q].y) | ct_any_bad2(y[q].z) | ct_any_bad2(y[q].w);
-        }
-        if (any) {
-#pragma unroll
-          for (int q = 0; q < 4 * L::HALVES; ++q) {
-            const int key = (i0 >> 3) + (q & 3) * 4 + (lane >> 3), col = (q >> 2) * 64 + (((lane & 7) ^ (key & 7)) << 3);
-            const uint32_t b[4] = {ct_bad2(y[q].x), ct_bad2(y[q].y), ct_bad2(y[q].z), ct_bad2(y[q].w)};
-            *piece(q >> 2, key, lane & 7) = make_uint4(y[q].x & ~b[0], y[q].y & ~b[1], y[q].z & ~b[2], y[q].w & ~b[3]);
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-              if (b[e >> 1] >> ((e & 1) * 16) & 1) atomicMin(&s_pk[par][col + e], k0 + key);
-          }
-          s_poisoned[par] = 1;
-        }
-      }
-      fence_async_shared();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&v_fix[s]);
-      return true;
-    };
-    int seg = -1;   // segments with keys so far
-    while (u < u_end && ok) {
-      g.set(a, ts, x, u, u_end);
-      seg += g.n_it > 0;
-      int gone = 0, gone_prev = 0;
-      for (int j = 0; j <= g.n_it && ok; ++j) {
-        gone_prev = gone;
-        if (!kw && j > 0 && (g.edge(j - 1) || gone_prev) && !(ok = mend(j - 1, cnt - 1, gone_prev, seg & 3))) break;
-        if (j == g.n_it) break;
-        const int s = cnt & 1, row = lane < 8 ? g.row_of(a.c, p.wide, (g.j_lo + j) * 8 + lane) : -1;
-        const unsigned on = __ballot_sync(0xffffffffu, row >= 0);
-        gone = (int)__ballot_sync(0xffffffffu, row == -2);
-        if (gone && lane == 0) a.c.flag(ERRW_POS);
-        int rows8[8];
-#pragma unroll
-        for (int b = 0; b < 8; ++b) rows8[b] = __shfl_sync(0xffffffffu, row, b);
-        if (cnt >= 2 && !(ok = mbar_wait_warp(&empty[s], (uint32_t)(((cnt >> 1) - 1) & 1), abort_flag, err, wlim))) break;
-        if (!kw && j == 0) {   // the segment's notes (V of two tiles ago is through, so the segment before the last is written)
-          for (int e = lane; e < DH; e += 32) s_pk[seg & 3][e] = 0x7fffffff;
-          if (lane == 0) s_poisoned[seg & 3] = 0;
-          __syncwarp();
-        }
-        if (elect_one()) {
-          if (kw) s_gone[cnt & 3] = gone;   // (tile cnt - 4 is through: its K stage has been freed twice over)
-          // (blocks that are not fetched leave the stage's old contents: masked in S, mended in V)
-          mbar_expect_tx(&full[s], (uint32_t)(__popc(on) * 16 * 128 * L::HALVES));
-          for (int b = 0; b < 8; ++b)
-            if (on >> b & 1)
-              for (int hf = 0; hf < L::HALVES; ++hf)
-                tma_load_2d(map, &full[s], dst0 + s * L::KV_BYTES + hf * CT_BN * 128 + b * 16 * 128, hf * 64, rows8[b]);
-        }
-        __syncwarp();
-        ++cnt;
-        if (kw && j == 0) {   // Q, once S of the segment before is through
-          if (nq > 0 && !(ok = mbar_wait_warp(&q_free, (uint32_t)((nq - 1) & 1), abort_flag, err, wlim))) break;
-          if (elect_one()) {
-            const int subs = g.n_tok > ts ? 2 : 1;
-            mbar_expect_tx(&q_full, (uint32_t)(subs * L::HALVES * ts * group * 128));
-            for (int b = 0; b < subs; ++b)
-              for (int hf = 0; hf < L::HALVES; ++hf)
-                tma_load_q(&p.qmap, &q_full, sQ + b * L::Q_BYTES + hf * CT_BM * 128, hf * 64, g.x.kvh * group, g.x.q0 + g.t0 + b * ts);
-          }
-          __syncwarp();
-          ++nq;
-        }
-      }
-      ct_next(a, tq, x);
-      u = x.u0;
-    }
-    // every copy sent has landed before the CTA ends
-    if (lane == 0) {
-      for (int t = max(0, cnt - 2); t < cnt; ++t) {
-        const long long c0 = clock64();
-        while (!mbar_try_wait(&full[t & 1], (uint32_t)((t >> 1) & 1)) && clock64() - c0 < CT_DRAIN_CYCLES) {
-        }
-      }
-      const long long c0 = clock64();
-      while (nq > 0 && !mbar_try_wait(&q_full, (uint32_t)((nq - 1) & 1)) && clock64() - c0 < CT_DRAIN_CYCLES) {
-      }
-    }
-    __syncwarp();
-  }
-  tc_fence_before();
-  __syncthreads();
-  tc_fence_after();
-  if (warp == 8) tmem_dealloc(tmem, 512);
-}
-
-// Entries of 8 bits as bf16: CTA = a block of positions of one sequence, K (z = 0) or V, all heads, 16 elements a thread and turn.
-constexpr int CW_THREADS = 256;
-template <int DH>
-__global__ void __launch_bounds__(CW_THREADS) chunk_widen_kernel(const __grid_constant__ CtParams p, bf16* k_out, bf16* v_out) {
-  PDL_ENTRY();
-  const ChunkCall& a = p.a;
-  const int b = (int)blockIdx.x, seq = (int)blockIdx.y;
-  int q0, c, len;
-  chunk_seq(a, seq, q0, c, len);
-  if (c == 0 || b * 16 >= len) return;
-  const int blk = a.c.table[(size_t)seq * a.c.max_blocks + b];
-  if (blk < 0 || blk >= a.c.n_blocks) return;
-  const int n = a.c.n_kv_heads * 16 * (DH / 16);
-  const size_t from = (size_t)blk * a.c.n_kv_heads * 16, to = ((size_t)seq * p.wide + b) * a.c.n_kv_heads * 16;
-  const uint8_t* codes = (const uint8_t*)(blockIdx.z ? a.c.v : a.c.k) + from * DH;
-  const uint8_t* exps = (blockIdx.z ? a.c.v_exp : a.c.k_exp) + from;
-  bf16* out = (blockIdx.z ? v_out : k_out) + to * DH;
-#pragma unroll 4
-  for (int i = threadIdx.x; i < n; i += CW_THREADS) {
-    const uint4 w = reinterpret_cast<const uint4*>(codes)[i];
-    const int e = exps[i / (DH / 16)];
-    const float s = e ? __uint_as_float((unsigned)e << 23) : __uint_as_float(0x400000u);   // 2^(e - 127)
-    const uint32_t x[4] = {w.x, w.y, w.z, w.w};
-    uint32_t y[8];
-#pragma unroll
-    for (int q = 0; q < 8; ++q) {
-      const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(x[q >> 1] >> (q & 1 ? 16 : 0)), __NV_E4M3);
-      const float2 f = __half22float2(__half2(h));
-      const __nv_bfloat162 r = __floats2bfloat162_rn(f.x * s, f.y * s);
-      y[q] = *reinterpret_cast<const uint32_t*>(&r);
-    }
-    reinterpret_cast<uint4*>(out)[2 * i] = make_uint4(y[0], y[1], y[2], y[3]);
-    reinterpret_cast<uint4*>(out)[2 * i + 1] = make_uint4(y[4], y[5], y[6], y[7]);
-  }
-}
-
-// Join of the tiles that runs share: CTA (i, y) takes the tile that run i + 1 is the first to begin inside of, an eighth of its
-// rows.  Parts: run i's (the tile's beginning), run i + 1's, ... in order.
-constexpr int CJ_SPLIT = 8;
-template <int DH>
-__global__ void __launch_bounds__(256) chunk_tc_join_kernel(const __grid_constant__ CtParams p) {
-  PDL_ENTRY();
-  const CtWs ws(p);
-  const int run = (int)blockIdx.x + 1, tid = threadIdx.x;
-  const CtNote n = ws.note[run];
-  if (n.u0 < 0 || ws.note[run - 1].u0 == n.u0) return;
-  int n_part = 2;
-  while (run + n_part - 1 < p.runs && ws.note[run + n_part - 1].u0 == n.u0) ++n_part;
-  const ChunkCall& a = p.a;
-  const int group = a.n_heads / a.c.n_kv_heads;
-  constexpr int ROWS = CT_ROWS / CJ_SPLIT;
-  // a warp takes 8 rows x 4 pieces of 4 columns: whole lines of the parts, whole sectors of the output
-  const int lane = tid & 31, rl = lane & 7, dl = lane >> 3;
-  for (int w = tid >> 5; w < ROWS / 8 * (DH / 16); w += 8) {
-    const int r = (int)blockIdx.y * ROWS + w % (ROWS / 8) * 8 + rl, d4 = w / (ROWS / 8) * 4 + dl;
-    const int rr = r & 127, tk = rr / group, tok = (r >> 7) * p.ts + tk;
-    if (tk >= p.ts || tok >= n.n_tok) continue;
-    float M = -INFINITY, l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int k0 = 0; k0 < n_part; k0 += 4) {
-      float2 ml[4];
-      float4 v[4];
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        ml[k] = make_float2(-INFINITY, 0.f);
-        v[k] = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (k0 + k < n_part) {
-          const int slot = (run - 1 + k0 + k) * 2 + (k0 + k == 0);
-          ml[k] = __ldcg(ws.ml_at(slot, r));
-          v[k] = __ldcg(ws.o_at(slot, DH, d4, r));
-        }
-      }
-      float mn = M;
-#pragma unroll
-      for (int k = 0; k < 4; ++k) mn = fmaxf(mn, ml[k].x);
-      const float ref = mn == -INFINITY ? 0.f : mn, f = ex2_approx(M - ref);
-      M = mn;
-      l *= f;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) o[e] *= f;
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const float x = ex2_approx(ml[k].x - ref);
-        l += x * ml[k].y;
-        o[0] += x * v[k].x;
-        o[1] += x * v[k].y;
-        o[2] += x * v[k].z;
-        o[3] += x * v[k].w;
-      }
-    }
-    const float inv = (a.row_pos ? a.row_pos[n.row0 + tok] : n.pos0 + tok) < 0 ? 0.f : 1.f / l;
-    const __nv_bfloat162 y0 = __floats2bfloat162_rn(o[0] * inv, o[1] * inv), y1 = __floats2bfloat162_rn(o[2] * inv, o[3] * inv);
-    *reinterpret_cast<uint2*>((bf16*)a.out + (size_t)(n.row0 + tok) * a.ld_out + (size_t)(n.kvh * group + rr % group) * DH + d4 * 4) =
-        make_uint2(*reinterpret_cast<const uint32_t*>(&y0), *reinterpret_cast<const uint32_t*>(&y1));
-  }
-}
 
 int ct_sms() {
   static const int sms = [] {
