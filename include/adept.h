@@ -52,6 +52,7 @@ enum { ADEPT_FAMILY_LLAMA = 0,   /* RMSNorm pre-norm, RoPE, SwiGLU, untied head 
        ADEPT_FAMILY_BERT = 2 };  /* post-LN encoder, bidirectional, pooler + classifier */
 
 enum { ADEPT_DTYPE_F32 = 0, ADEPT_DTYPE_BF16 = 1 };
+enum { ADEPT_KV_F32 = 0, ADEPT_KV_BF16 = 1, ADEPT_KV_E4M3 = 2 };   /* element types of a K/V cache (adept_kv_cache) */
 
 typedef struct {
   int family;          /* ADEPT_FAMILY_* */
@@ -79,6 +80,10 @@ typedef struct {
   int max_src;         /* > 0 (GPT-2 family only): an encoder-decoder decoder whose layers
                           cross-attend to up to max_src encoder states per sequence
                           (adept_set_cross_source); 0: no cross-attention */
+  int kv_type;         /* 0: the cache holds the model's type; ADEPT_KV_E4M3 (bf16 decoders, blocks of 16):
+                          8-bit floats with an exponent per position and head, half the memory and half of what
+                          attention reads; one layer's cache in bf16 besides, for staging (not for the
+                          cross-attention's source cache) */
 } adept_config;
 
 /* One named weight tensor.  `data` may be a host or a device pointer (it is read
@@ -199,7 +204,7 @@ ADEPT_API adept_status adept_skip_kv_fill(adept_model* m, int n_tokens, const vo
  * working set in a fixed file-scope device array of ADEPT_NOALLOC_SCRATCH_BYTES bytes
  * (16 MiB, held by every GPU that loads the library until the process exits) and calls
  * no cudaMalloc, cudaFree or other allocating routine.  Same arguments and results as
- * adept_skip_kv_fill; bf16 models only.
+ * adept_skip_kv_fill; bf16 models only, without an 8-bit cache.
  *  - Limit: n_tokens * (d_model * 2 + 4) bytes plus about 3 KiB must fit the array
  *    (about 2000 tokens at d_model 4096, 10900 at d_model 768); larger calls return
  *    ADEPT_ERR_CAPACITY with the limit in adept_last_error and enqueue nothing.
@@ -248,7 +253,7 @@ ADEPT_API adept_status adept_seq_reserve(adept_model* m, int batch, const int32_
 
 /* Copy K and V of `n_pos` positions starting at pos0 of sequence `seq` at layer
  * `layer` (1-based) out of the paged cache into d_k_out / d_v_out, each
- * [n_pos, n_kv_heads, head_dim] in the model dtype. */
+ * [n_pos, n_kv_heads, head_dim] in the model dtype (what an 8-bit cache holds: exactly). */
 ADEPT_API adept_status adept_read_kv(adept_model* m, int layer, int seq, int pos0, int n_pos,
                            void* d_k_out, void* d_v_out, void* stream);
 
@@ -415,7 +420,6 @@ ADEPT_API int64_t adept_hsm_param_numel(const adept_model* m, int param);
  * cache are ordered by their streams as any other work on shared buffers is.
  * d_err (may be NULL): a device word that kernels set where an input read on the device is out of
  * range (zero it first); adept_kv_check reports and clears it. */
-enum { ADEPT_KV_F32 = 0, ADEPT_KV_BF16 = 1, ADEPT_KV_E4M3 = 2 };
 typedef struct {
   int kv_type;              /* ADEPT_KV_* */
   int n_blocks;

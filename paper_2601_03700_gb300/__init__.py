@@ -20,6 +20,7 @@ LIB_PATH = os.path.join(_PKG, "libadept.so")
 ADEPT_OK = 0
 STATUS_NAMES = {0: "OK", 1: "INVALID_ARG", 2: "OOM", 3: "CAPACITY", 4: "CUDA", 5: "TIMEOUT", 6: "DEVICE_INPUT"}
 FAMILY = {"llama": 0, "gpt2": 1, "bert": 2}
+KV_TYPES = {"f32": 0, "bf16": 1, "e4m3": 2}
 OPT_HSM_IDENTITY, OPT_PROFILE, OPT_GEMM_SIMT, OPT_DECODE_GRAPH, OPT_DECODE_GEMM = 1, 2, 3, 4, 5
 OPT_EXIT_METRIC, OPT_ALL_AT_ONCE, OPT_STOP_ENTIRELY, OPT_DECODE_STREAM, OPT_DECODE_TILED = 7, 8, 9, 10, 11
 OPT_SPAN_TIMER, OPT_ATTN_TC, OPT_FUSED_EXIT = 12, 13, 14
@@ -59,7 +60,7 @@ class AdeptConfig(ctypes.Structure):
         ("rope_theta", ctypes.c_float), ("hsm_eps", ctypes.c_float), ("hsm_m1", ctypes.c_int),
         ("hsm_m2", ctypes.c_int), ("kv_block_tokens", ctypes.c_int), ("max_batch", ctypes.c_int),
         ("max_seq", ctypes.c_int), ("kv_pool_blocks", ctypes.c_int), ("max_pass_tokens", ctypes.c_int),
-        ("block_shuffle_seed", ctypes.c_uint64), ("max_src", ctypes.c_int),
+        ("block_shuffle_seed", ctypes.c_uint64), ("max_src", ctypes.c_int), ("kv_type", ctypes.c_int),
     ]
 
 
@@ -202,7 +203,8 @@ def make_config(cfg) -> AdeptConfig:
         hsm_eps=float(g("hsm_eps", 1e-6)), hsm_m1=g("hsm_m1"), hsm_m2=g("hsm_m2"),
         kv_block_tokens=g("kv_block_tokens", 16), max_batch=g("max_batch"), max_seq=g("max_seq"),
         kv_pool_blocks=g("kv_pool_blocks", 0) or 0, max_pass_tokens=g("max_pass_tokens", 0) or 0,
-        block_shuffle_seed=int(g("block_shuffle_seed", 0) or 0), max_src=int(g("max_src", 0) or 0))
+        block_shuffle_seed=int(g("block_shuffle_seed", 0) or 0), max_src=int(g("max_src", 0) or 0),
+        kv_type=KV_TYPES["e4m3"] if g("kv_type", 0) == "e4m3" else int(g("kv_type", 0) or 0))
 
 
 # ---------------------------------------------------------------------------
@@ -402,7 +404,6 @@ def adept_set_alloc_fail_after(n: int):
 # operators on a caller-owned paged K/V cache
 # ---------------------------------------------------------------------------
 
-KV_TYPES = {"f32": 0, "bf16": 1, "e4m3": 2}
 _KV_TORCH = {0: torch.float32, 1: torch.bfloat16, 2: torch.uint8}
 
 

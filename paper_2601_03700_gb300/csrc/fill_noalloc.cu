@@ -76,6 +76,10 @@ extern "C" ADEPT_API adept_status adept_skip_kv_fill_noalloc(adept_model* m, int
     model_set_error(m, "adept_skip_kv_fill_noalloc: model has more layers than the fixed view holds");
     return ADEPT_ERR_INVALID_ARG;
   }
+  if (v.kv8) {
+    model_set_error(m, "adept_skip_kv_fill_noalloc: not with an 8-bit cache (adept_skip_kv_fill)");
+    return ADEPT_ERR_INVALID_ARG;
+  }
   if (v.dtype != ADEPT_DTYPE_BF16 || !tc_gemm_supported()) {
     model_set_error(m, "adept_skip_kv_fill_noalloc: needs a bf16 model on an sm_100-family GPU");
     return ADEPT_ERR_INVALID_ARG;

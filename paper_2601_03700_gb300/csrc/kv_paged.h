@@ -26,9 +26,13 @@ struct KvPaged {
 // rows (else fp32); ld in elements.
 cudaError_t launch_kv_append(cudaStream_t st, const KvPaged& c, int n_rows, int src_bf16, const void* k, long long ld_k,
                              const void* v, long long ld_v, const int* seq, const int* pos);
-// The entries at (seq[r], pos[r]) back as rows (a row with seq[r] < 0 is not written).
+// The entries at (seq[r], pos[r]) back as rows (a row with seq[r] < 0 is not written); seq NULL: position pos0 + r of seq0.
 cudaError_t launch_kv_gather(cudaStream_t st, const KvPaged& c, int n_rows, int dst_bf16, void* k, long long ld_k, void* v,
-                             long long ld_v, const int* seq, const int* pos);
+                             long long ld_v, const int* seq, const int* pos, int seq0 = 0, int pos0 = 0);
+// bf16 entries that a pass left in a staging cache (layers src_layer0 ..) into the 8-bit cache c (of the first of n_layers
+// layers): rows [0, n_rows[y]) of layer y (NULL: max_rows), row r token row_tok[r] (NULL: r) at (tok_seq, tok_pos).
+cudaError_t launch_kv_requant(cudaStream_t st, const KVCacheView& src, int src_layer0, const KvPaged& c, int n_layers,
+                              const int* n_rows, int max_rows, const int* row_tok, const int* tok_seq, const int* tok_pos);
 
 // One attention call: the new tokens of n_seq sequences (rows q_start[b] .. q_start[b + 1]) at the last of sequence b's
 // kv_len[b] cached positions, or at those that row_pos gives, each attending its own position and those before it.

@@ -100,6 +100,39 @@ struct Item {
   }
 };
 
+// 16 elements of a vector that TPV neighbouring threads hold, into entry `e` of K or V (-1: nowhere).
+template <int DH>
+__device__ __forceinline__ void store_e4m3(const KvPaged& c, bool is_v, long long e, int sub, const float (&y)[KS_EL]) {
+  float a = 0.f;
+#pragma unroll
+  for (int j = 0; j < KS_EL; ++j) {
+    const float b = fabsf(y[j]);
+    a = fmaxf(a, b == INFINITY ? 0.f : b);   // (fmaxf leaves NaN out)
+  }
+#pragma unroll
+  for (int o = DH / KS_EL / 2; o; o >>= 1) a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, o));
+  const unsigned bits = __float_as_uint(a);
+  int ex = (int)(bits >> 23) - 127 - 8 + ((bits & 0x7fffffu) > 0x600000u ? 1 : 0);
+  ex = a == 0.f ? 0 : max(ex, -126);
+  const float s = __uint_as_float((unsigned)(127 - ex) << 23);
+  uint32_t out[KS_EL / 4];
+#pragma unroll
+  for (int j = 0; j < KS_EL / 2; ++j) {
+    float y0 = y[2 * j] * s, y1 = y[2 * j + 1] * s;
+    if (fabsf(y[2 * j]) == INFINITY) y0 = NAN;
+    if (fabsf(y[2 * j + 1]) == INFINITY) y1 = NAN;
+    const uint32_t two = __nv_cvt_float2_to_fp8x2(make_float2(y0, y1), __NV_SATFINITE, __NV_E4M3);
+    if (j & 1)
+      out[j >> 1] |= two << 16;
+    else
+      out[j >> 1] = two;
+  }
+  if (e >= 0) {
+    *reinterpret_cast<uint4*>((uint8_t*)(is_v ? c.v : c.k) + (size_t)e * DH + sub * KS_EL) = make_uint4(out[0], out[1], out[2], out[3]);
+    if (sub == 0) (is_v ? c.v_exp : c.k_exp)[e] = (uint8_t)(ex + 127);
+  }
+}
+
 template <int DH, typename T, int KT, bool VEC>
 __global__ void __launch_bounds__(KS_THREADS) kv_append_kernel(KvPaged c, int n_rows, int rows_cta, const T* k, long long ld_k,
                                                                const T* v, long long ld_v, const int* seq, const int* pos) {
@@ -122,52 +155,53 @@ __global__ void __launch_bounds__(KS_THREADS) kv_append_kernel(KvPaged c, int n_
 #pragma unroll
     for (int q = 0; q < KS_ITEMS; ++q) {
       const Item<DH> it(min(i0 + q * KS_THREADS + (int)threadIdx.x, total - 1), hk, per_row);
-      void* pool = it.is_v ? c.v : c.k;
-      const size_t at = (size_t)e[q] * DH + it.sub * KS_EL;
       float y[KS_EL];
       x[q].f32(y);
       if constexpr (KT == KV_E4M3) {
-        float a = 0.f;
-#pragma unroll
-        for (int j = 0; j < KS_EL; ++j) {
-          const float b = fabsf(y[j]);
-          a = fmaxf(a, b == INFINITY ? 0.f : b);   // (fmaxf leaves NaN out)
-        }
-#pragma unroll
-        for (int o = TPV / 2; o; o >>= 1) a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, o));
-        const unsigned bits = __float_as_uint(a);
-        int ex = (int)(bits >> 23) - 127 - 8 + ((bits & 0x7fffffu) > 0x600000u ? 1 : 0);
-        ex = a == 0.f ? 0 : max(ex, -126);
-        const float s = __uint_as_float((unsigned)(127 - ex) << 23);
-        uint32_t out[KS_EL / 4];
-#pragma unroll
-        for (int j = 0; j < KS_EL / 2; ++j) {
-          float y0 = y[2 * j] * s, y1 = y[2 * j + 1] * s;
-          if (fabsf(y[2 * j]) == INFINITY) y0 = NAN;
-          if (fabsf(y[2 * j + 1]) == INFINITY) y1 = NAN;
-          const uint32_t two = __nv_cvt_float2_to_fp8x2(make_float2(y0, y1), __NV_SATFINITE, __NV_E4M3);
-          if (j & 1)
-            out[j >> 1] |= two << 16;
-          else
-            out[j >> 1] = two;
-        }
-        if (e[q] >= 0) {
-          *reinterpret_cast<uint4*>((uint8_t*)pool + at) = make_uint4(out[0], out[1], out[2], out[3]);
-          if (it.sub == 0) (it.is_v ? c.v_exp : c.k_exp)[e[q]] = (uint8_t)(ex + 127);
-        }
+        store_e4m3<DH>(c, it.is_v, e[q], it.sub, y);
       } else if (e[q] >= 0) {
         using C = typename std::conditional<KT == KV_BF16, bf16, float>::type;
         Piece<C> z;
         z.from(y);
-        z.template store<true>((C*)pool + at);
+        z.template store<true>((C*)(it.is_v ? c.v : c.k) + (size_t)e[q] * DH + it.sub * KS_EL);
       }
     }
   }
 }
 
+// bf16 entries of a staging cache into an 8-bit one: rows [0, n_rows[y]) of layer y (n_rows NULL: max_rows), row r token
+// row_tok[r] (NULL: r) at (tok_seq, tok_pos).  Layer y of the source is src_layer0 + y.
+template <int DH>
+__global__ void __launch_bounds__(KS_THREADS) kv_requant_kernel(KVCacheView src, int src_layer0, KvPaged c, const int* n_rows,
+                                                                int max_rows, int rows_cta, const int* row_tok,
+                                                                const int* tok_seq, const int* tok_pos) {
+  PDL_ENTRY();
+  constexpr int TPV = DH / KS_EL;
+  const int y = (int)blockIdx.y, n = n_rows ? min(n_rows[y], max_rows) : max_rows;
+  const int hk = c.n_kv_heads, per_row = 2 * hk * TPV, row0 = (int)blockIdx.x * rows_cta;
+  const int total = min(rows_cta, n - row0) * per_row;
+  const long long layer = (long long)y * c.n_blocks * hk * c.block_tokens;   // entries
+  for (int i0 = 0; i0 < total; i0 += KS_THREADS) {
+    const int i = i0 + (int)threadIdx.x;
+    const Item<DH> it(min(i, total - 1), hk, per_row);
+    const int tok = row_tok ? row_tok[row0 + it.r] : row0 + it.r, seq = tok_seq[tok], pos = tok_pos[tok];
+    const long long from = src.checked_base(src_layer0 + y, seq, pos);
+    const long long e0 = i < total && from >= 0 ? entry0(c, seq, pos) : -1;
+    float x[KS_EL];
+#pragma unroll
+    for (int j = 0; j < KS_EL; ++j) x[j] = 0.f;
+    if (e0 >= 0) {
+      Piece<bf16> w;
+      w.template load<true>((const bf16*)(it.is_v ? src.v : src.k) + from + (size_t)it.h * src.head_stride() + it.sub * KS_EL);
+      w.f32(x);
+    }
+    store_e4m3<DH>(c, it.is_v, e0 < 0 ? -1 : layer + e0 + (long long)it.h * c.block_tokens, it.sub, x);
+  }
+}
+
 template <int DH, typename T, int KT, bool VEC>
 __global__ void __launch_bounds__(KS_THREADS) kv_gather_kernel(KvPaged c, int n_rows, int rows_cta, T* k, long long ld_k, T* v,
-                                                               long long ld_v, const int* seq, const int* pos) {
+                                                               long long ld_v, const int* seq, const int* pos, int seq0, int pos0) {
   PDL_ENTRY();
   constexpr int TPV = DH / KS_EL;
   const int hk = c.n_kv_heads, per_row = 2 * hk * TPV, row0 = (int)blockIdx.x * rows_cta;
@@ -181,7 +215,8 @@ __global__ void __launch_bounds__(KS_THREADS) kv_gather_kernel(KvPaged c, int n_
     for (int q = 0; q < KS_ITEMS; ++q) {
       const int i = i0 + q * KS_THREADS + threadIdx.x;
       const Item<DH> it(min(i, total - 1), hk, per_row);
-      const long long r = row0 + it.r, e0 = i < total ? entry0(c, seq[r], pos[r]) : -1;
+      const long long r = row0 + it.r;
+      const long long e0 = i >= total ? -1 : seq ? entry0(c, seq[r], pos[r]) : entry0(c, seq0, pos0 + (int)r);
       on[q] = e0 >= 0;
       if (!on[q]) continue;
       const size_t e = (size_t)(e0 + (long long)it.h * c.block_tokens), at = e * DH + it.sub * KS_EL;
@@ -248,10 +283,10 @@ cudaError_t append_t(cudaStream_t st, const KvPaged& c, int n, const void* k, lo
 }
 template <int DH, typename T, int KT>
 cudaError_t gather_t(cudaStream_t st, const KvPaged& c, int n, void* k, long long ld_k, void* v, long long ld_v, const int* seq,
-                     const int* pos) {
+                     const int* pos, int seq0, int pos0) {
   auto kern = rows_aligned(k, ld_k, v, ld_v, (int)sizeof(T)) ? kv_gather_kernel<DH, T, KT, true> : kv_gather_kernel<DH, T, KT, false>;
   const int rows = ks_rows(c, n);
-  return launch_k(kern, dim3((unsigned)cdiv(n, rows)), dim3(KS_THREADS), 0, st, c, n, rows, (T*)k, ld_k, (T*)v, ld_v, seq, pos);
+  return launch_k(kern, dim3((unsigned)cdiv(n, rows)), dim3(KS_THREADS), 0, st, c, n, rows, (T*)k, ld_k, (T*)v, ld_v, seq, pos, seq0, pos0);
 }
 
 #define KS_DISPATCH(F, BF, ...)                                                                   \
@@ -285,8 +320,16 @@ cudaError_t launch_kv_append(cudaStream_t st, const KvPaged& c, int n_rows, int 
 }
 
 cudaError_t launch_kv_gather(cudaStream_t st, const KvPaged& c, int n_rows, int dst_bf16, void* k, long long ld_k, void* v,
-                             long long ld_v, const int* seq, const int* pos) {
-  KS_DISPATCH(gather_t, dst_bf16, st, c, n_rows, k, ld_k, v, ld_v, seq, pos);
+                             long long ld_v, const int* seq, const int* pos, int seq0, int pos0) {
+  KS_DISPATCH(gather_t, dst_bf16, st, c, n_rows, k, ld_k, v, ld_v, seq, pos, seq0, pos0);
+}
+
+cudaError_t launch_kv_requant(cudaStream_t st, const KVCacheView& src, int src_layer0, const KvPaged& c, int n_layers,
+                              const int* n_rows, int max_rows, const int* row_tok, const int* tok_seq, const int* tok_pos) {
+  auto kern = c.head_dim == 128 ? kv_requant_kernel<128> : c.head_dim == 64 ? kv_requant_kernel<64> : kv_requant_kernel<32>;
+  const int rows = ks_rows(c, max_rows);
+  return launch_k(kern, dim3((unsigned)cdiv(max_rows, rows), (unsigned)n_layers), dim3(KS_THREADS), 0, st, src, src_layer0, c, n_rows,
+                  max_rows, rows, row_tok, tok_seq, tok_pos);
 }
 
 }  // namespace adept

@@ -8,7 +8,7 @@ namespace adept {
 constexpr int FILL_VIEW_MAX_LAYERS = 256;
 
 struct FillView {
-  int n_layers, d_model, d_q, d_kv, head_dim, dtype, norm_mode, rope;
+  int n_layers, d_model, d_q, d_kv, head_dim, dtype, norm_mode, rope, kv8;
   float norm_eps;
   const float2* rope_table;
   KVCacheView cache;

@@ -113,6 +113,13 @@ struct adept_model {
   // paged KV cache
   void *k_pool = nullptr, *v_pool = nullptr;
   int n_blocks = 0, max_blocks_per_seq = 0;
+  // 8-bit cache (cfg.kv_type): k_pool / v_pool hold e4m3 codes, these the exponents.  The products' epilogues write bf16
+  // entries to a staging cache, from which a launch per layer quantises them: for prompts and chunks one layer's cache (st_*,
+  // same block table), for generation steps a block per sequence and layer (sp_*, a table whose row b is all b)
+  bool kv8 = false;
+  uint8_t *k_exp = nullptr, *v_exp = nullptr;
+  void *st_k = nullptr, *st_v = nullptr, *sp_k = nullptr, *sp_v = nullptr;
+  int *sp_table = nullptr, *sp_iota = nullptr;   // sp_iota: 0 .. max_batch (a step's first token per sequence)
   int* d_block_table = nullptr;
   std::vector<int> h_block_table, free_list, h_seq_len;
   std::vector<std::vector<int>> seq_blocks;
@@ -291,6 +298,22 @@ static KVCacheView cache_view(const adept_model* m) {
   c.head_dim = m->dh;
   c.block_tokens = m->cfg.kv_block_tokens;
   c.max_batch = m->cfg.max_batch;
+  return c;
+}
+
+// The cache that the epilogues of layer layer0's K/V products write, and its layer there.
+static KVCacheView write_view(const adept_model* m, bool step, int layer0, int* layer_there) {
+  KVCacheView c = cache_view(m);
+  *layer_there = layer0;
+  if (!m->kv8) return c;
+  c.k = step ? m->sp_k : m->st_k;
+  c.v = step ? m->sp_v : m->st_v;
+  if (step) {
+    c.block_table = m->sp_table;
+    c.n_blocks = m->cfg.max_batch;
+  } else {
+    *layer_there = 0;
+  }
   return c;
 }
 
@@ -642,6 +665,10 @@ static adept_status validate_cfg(adept_config* c) {
     return fail(nullptr, ADEPT_ERR_INVALID_ARG, "max_batch * max_seq too large");
   if (c->max_src < 0 || (c->max_src > 0 && c->family != ADEPT_FAMILY_GPT2))
     return fail(nullptr, ADEPT_ERR_INVALID_ARG, "cross-attention (max_src > 0) is defined for GPT-2-family decoders");
+  if (c->kv_type != 0 && c->kv_type != ADEPT_KV_E4M3) return fail(nullptr, ADEPT_ERR_INVALID_ARG, "kv_type %d unknown", c->kv_type);
+  if (c->kv_type == ADEPT_KV_E4M3 &&
+      (c->dtype != ADEPT_DTYPE_BF16 || c->family == ADEPT_FAMILY_BERT || c->kv_block_tokens != 16))
+    return fail(nullptr, ADEPT_ERR_INVALID_ARG, "an 8-bit cache needs a bf16 decoder and blocks of 16 positions");
   if ((long long)c->max_batch * c->max_src > (1LL << 24))
     return fail(nullptr, ADEPT_ERR_INVALID_ARG, "max_batch * max_src too large");
   return ADEPT_OK;
@@ -824,8 +851,26 @@ static adept_status alloc_runtime(adept_model* m) {
   m->max_blocks_per_seq = cdiv(c.max_seq, c.kv_block_tokens);
   m->n_blocks = c.kv_pool_blocks > 0 ? c.kv_pool_blocks : c.max_batch * m->max_blocks_per_seq;
   const size_t per_layer = (size_t)m->n_blocks * m->Hkv * c.kv_block_tokens * m->dh;
-  TRY(dalloc(m, &m->k_pool, per_layer * m->N * m->esz));
-  TRY(dalloc(m, &m->v_pool, per_layer * m->N * m->esz));
+  m->kv8 = c.kv_type == ADEPT_KV_E4M3;
+  const size_t kv_esz = m->kv8 ? 1 : m->esz;
+  TRY(dalloc(m, &m->k_pool, per_layer * m->N * kv_esz));
+  TRY(dalloc(m, &m->v_pool, per_layer * m->N * kv_esz));
+  if (m->kv8) {
+    const size_t exps = per_layer / m->dh * m->N, step = (size_t)m->N * c.max_batch * m->Hkv * c.kv_block_tokens * m->dh * m->esz;
+    TRY(dalloc_t(m, &m->k_exp, exps));
+    TRY(dalloc_t(m, &m->v_exp, exps));
+    TRY(dalloc(m, &m->st_k, per_layer * m->esz));
+    TRY(dalloc(m, &m->st_v, per_layer * m->esz));
+    TRY(dalloc(m, &m->sp_k, step));
+    TRY(dalloc(m, &m->sp_v, step));
+    std::vector<int> tab((size_t)c.max_batch * m->max_blocks_per_seq), iota(c.max_batch + 1);
+    for (size_t i = 0; i < tab.size(); ++i) tab[i] = (int)(i / m->max_blocks_per_seq);
+    for (size_t i = 0; i < iota.size(); ++i) iota[i] = (int)i;
+    TRY(dalloc_t(m, &m->sp_table, tab.size()));
+    TRY(dalloc_t(m, &m->sp_iota, iota.size()));
+    CUDA_TRY(m, cudaMemcpy(m->sp_table, tab.data(), tab.size() * sizeof(int), cudaMemcpyHostToDevice));
+    CUDA_TRY(m, cudaMemcpy(m->sp_iota, iota.data(), iota.size() * sizeof(int), cudaMemcpyHostToDevice));
+  }
   m->h_block_table.assign((size_t)c.max_batch * m->max_blocks_per_seq, -1);
   TRY(dalloc_t(m, &m->d_block_table, m->h_block_table.size()));
   CUDA_TRY(m, cudaMemcpy(m->d_block_table, m->h_block_table.data(), m->h_block_table.size() * sizeof(int),
@@ -1056,7 +1101,7 @@ static void run_hsm(adept_model* m, cudaStream_t st, DevRange rows, int max_rows
 
 // KV-only projection problem of layer `layer0` for the rows of `xs` (K-major x~ rows).
 static GemmProblem kv_problem(adept_model* m, int layer0, const void* xs, int a_rows, DevRange rows,
-                              const int* row_tok, const int* tok_seq, const int* tok_pos) {
+                              const int* row_tok, const int* tok_seq, const int* tok_pos, bool step) {
   GemmProblem p;
   memset(&p, 0, sizeof p);
   const LayerW& w = m->L[layer0];
@@ -1070,7 +1115,7 @@ static GemmProblem kv_problem(adept_model* m, int layer0, const void* xs, int a_
   p.epi = epi_base();
   p.epi.kind = EPI_KV; p.epi.bias = w.b_qkv + m->Dq;
   p.epi.row_tok = row_tok; p.epi.tok_seq = tok_seq; p.epi.tok_pos = tok_pos;
-  p.epi.cache = cache_view(m); p.epi.layer0 = layer0;
+  p.epi.cache = write_view(m, step, layer0, &p.epi.layer0);
   p.epi.n_q_cols = 0; p.epi.n_kv_cols = m->Dkv; p.epi.head_dim = m->dh;
   p.epi.rope = m->cfg.family == ADEPT_FAMILY_LLAMA; p.epi.rope_table = m->rope_table;
   return p;
@@ -1082,17 +1127,34 @@ struct ExtendPass {
 };
 
 static KvPaged paged_view(const adept_model* m, int layer0, int n_seq) {
-  const size_t off = (size_t)layer0 * m->n_blocks * m->Hkv * m->cfg.kv_block_tokens * m->dh * m->esz;
-  return KvPaged{(char*)m->k_pool + off, (char*)m->v_pool + off, nullptr, nullptr, m->d_block_table, m->err_word,
-                 m->dt == ADEPT_DTYPE_BF16 ? KV_BF16 : KV_F32, m->n_blocks, m->Hkv, m->dh, m->cfg.kv_block_tokens, n_seq,
+  const size_t ents = (size_t)layer0 * m->n_blocks * m->Hkv * m->cfg.kv_block_tokens, off = ents * m->dh * (m->kv8 ? 1 : m->esz);
+  return KvPaged{(char*)m->k_pool + off, (char*)m->v_pool + off, m->kv8 ? m->k_exp + ents : nullptr,
+                 m->kv8 ? m->v_exp + ents : nullptr, m->d_block_table, m->err_word,
+                 m->kv8 ? KV_E4M3 : m->dt == ADEPT_DTYPE_BF16 ? KV_BF16 : KV_F32, m->n_blocks, m->Hkv, m->dh, m->cfg.kv_block_tokens, n_seq,
                  m->max_blocks_per_seq};
 }
 
+// An error of a launch inside a pass: check_launch reports it.
+static void note_error(adept_model* m, cudaError_t e, const char* what) {
+  if (e != cudaSuccess) m->deferred = fail(m, ADEPT_ERR_CUDA, "%s: %s", what, cudaGetErrorString(e));
+}
+
+// 8-bit cache: what the epilogues left in the staging cache of layers layer0 .. layer0 + n_layers - 1, quantised.
+static void requant(adept_model* m, cudaStream_t st, bool step, int layer0, int n_layers, const int* n_rows, int max_rows,
+                    const int* row_tok, const int* tok_seq, const int* tok_pos) {
+  int there = 0;
+  const KVCacheView src = write_view(m, step, layer0, &there);
+  note_error(m, launch_kv_requant(st, src, there, paged_view(m, layer0, m->cfg.max_batch), n_layers, n_rows, max_rows, row_tok,
+                                  tok_seq, tok_pos),
+             "quantising the cache");
+  m->launches += 1;
+}
+
 // Attention of the active rows of a pass of ragged chunks (a row's position is its token's, those of tokens that left are
-// missing) over layer layer0's cache.
-static void extend_attention(adept_model* m, cudaStream_t st, const ExtendPass& e, int layer0, int batch, const int* n_rows,
-                             int max_rows, const int* row_tok) {
-  launch_chunk_rows(st, n_rows, max_rows, row_tok, m->tok_pos, m->d_ext, batch, m->ext_start, m->ext_pos);
+// missing) over layer layer0's cache.  first: first token per sequence.
+static void extend_attention(adept_model* m, cudaStream_t st, const ExtendPass& e, const int* first, int layer0, int batch,
+                             const int* n_rows, int max_rows, const int* row_tok) {
+  launch_chunk_rows(st, n_rows, max_rows, row_tok, m->tok_pos, first, batch, m->ext_start, m->ext_pos);
   ChunkCall a{};
   a.c = paged_view(m, layer0, batch);
   a.q = m->q;
@@ -1110,7 +1172,7 @@ static void extend_attention(adept_model* m, cudaStream_t st, const ExtendPass& 
   int n = 0;
   const cudaError_t err = launch_chunk_attention(st, a, &n);
   m->launches += 1 + n;
-  if (err != cudaSuccess) m->deferred = fail(m, ADEPT_ERR_CUDA, "chunk attention: %s", cudaGetErrorString(err));
+  note_error(m, err, "chunk attention");
 }
 
 // One early-exit pass over n_tok tokens.  The threshold delta is read from m->d_delta
@@ -1152,6 +1214,7 @@ static adept_status run_pass(adept_model* m, int n_tok, int batch, int prompt_le
                m->V, eps, m->X_in[0], m->err_word, m->xn, amode, eps);
   m->launches += 1;
   const KVCacheView cv = cache_view(m);
+  const ExtendPass step_pass{1, std::min(c.max_seq, m->max_blocks_per_seq * c.kv_block_tokens)};
   const int causal = fam != ADEPT_FAMILY_BERT;
   // generation step: the split-KV attention grid covers the reserved capacity (CTAs past a
   // sequence's length return at once), which keeps every launch of a step step-invariant
@@ -1207,12 +1270,12 @@ static adept_status run_pass(adept_model* m, int n_tok, int batch, int prompt_le
     pr[0].epi = epi_base();
     pr[0].epi.kind = EPI_QKV; pr[0].epi.bias = w.b_qkv; pr[0].epi.out_t = m->q; pr[0].epi.ld_t = Dq;
     pr[0].epi.row_tok = rt; pr[0].epi.tok_seq = m->tok_seq; pr[0].epi.tok_pos = m->tok_pos;
-    pr[0].epi.cache = cv; pr[0].epi.layer0 = l0; pr[0].epi.n_q_cols = Dq; pr[0].epi.n_kv_cols = Dkv;
+    pr[0].epi.cache = write_view(m, decode, l0, &pr[0].epi.layer0); pr[0].epi.n_q_cols = Dq; pr[0].epi.n_kv_cols = Dkv;
     pr[0].epi.head_dim = m->dh; pr[0].epi.rope = fam == ADEPT_FAMILY_LLAMA; pr[0].epi.rope_table = m->rope_table;
     // attention input: xn, standardised (gain folded into W_qkv)
     if (!decode && i >= 3 && !stop) {
       pr[1] = kv_problem(m, l0, m->xfill, n_tok, DevRange{nullptr, m->ctr + CTR_EXITED, 0}, m->exit_tok, m->tok_seq,
-                         m->tok_pos);
+                         m->tok_pos, false);
       gemm(m, st, pr, 2, mrs, m->gemm_cls);
     } else {
       bool done = false;
@@ -1235,12 +1298,15 @@ static adept_status run_pass(adept_model* m, int n_tok, int batch, int prompt_le
       }
       if (!done) gemm(m, st, pr, 1, mrs, m->gemm_cls);
     }
+    // 8-bit cache: a prompt's or chunk's tokens all have their entries now (active, or filled beside), a step's active ones
+    if (m->kv8)
+      requant(m, st, decode, l0, 1, decode ? m->ctr + CTR_ACTIVE + par : nullptr, n_tok, decode ? rt : nullptr, m->tok_seq, m->tok_pos);
     // attention over every cached position of layer i
     {
       cudaEvent_t b = nullptr;
       prof_begin(m, ADEPT_PROF_ATTENTION, st, &b);
-      if (ext) {
-        extend_attention(m, st, *ext, l0, batch, m->ctr + CTR_ACTIVE + par, mr, rt);
+      if (ext || m->kv8) {
+        extend_attention(m, st, ext ? *ext : step_pass, ext ? m->d_ext : m->sp_iota, l0, batch, m->ctr + CTR_ACTIVE + par, mr, rt);
       } else {
         launch_attention(st, m->dt, m->q, Dq, m->att, Dq, act, mr, rt, m->tok_seq, m->tok_pos, m->d_seq_len, cv, l0,
                          m->H, causal, decode_keys, m->attn_ws, m->attn_ctr, m->err_word, stop ? m->tok_exit : nullptr,
@@ -1364,7 +1430,7 @@ static adept_status run_pass(adept_model* m, int n_tok, int batch, int prompt_le
     std::vector<int> mrs;
     for (int r = 3; r <= N; ++r) {
       probs.push_back(kv_problem(m, r - 1, m->xfill, n_tok, DevRange{nullptr, m->ctr + CTR_PREFIX + r - 1, 0}, m->exit_tok,
-                                 m->tok_seq, m->tok_pos));
+                                 m->tok_seq, m->tok_pos, true));
       mrs.push_back(n_tok);
     }
     // one weight-streaming launch over the skipped layers when the rows fit it, else the
@@ -1379,6 +1445,7 @@ static adept_status run_pass(adept_model* m, int n_tok, int batch, int prompt_le
       if (done) m->launches += 1;
     }
     if (!done) gemm(m, st, probs.data(), (int)probs.size(), mrs.data(), ADEPT_PROF_KV_FILL);
+    if (m->kv8) requant(m, st, true, 2, N - 2, m->ctr + CTR_PREFIX + 2, n_tok, m->exit_tok, m->tok_seq, m->tok_pos);
   }
   return ADEPT_OK;
 }
@@ -1757,6 +1824,29 @@ static bool adamw_ok(const adept_adamw* hp) {
 }
 
 
+static adept_status extend_init(adept_model* m) {
+  if (m->ext_ws) return ADEPT_OK;
+  const int B = m->cfg.max_batch;
+  // (the bound over every batch and length)
+  const size_t ws = std::max(chunk_workspace(paged_view(m, 0, B), m->H, m->T_max, m->max_blocks_per_seq * m->cfg.kv_block_tokens),
+                             chunk_workspace(paged_view(m, 0, B), m->H, 1, m->max_blocks_per_seq * m->cfg.kv_block_tokens));
+  if (!m->d_ext) TRY(dalloc_t(m, &m->d_ext, (size_t)2 * B + 1));
+  if (!m->ext_start) TRY(dalloc_t(m, &m->ext_start, (size_t)B + 1));
+  if (!m->ext_pos) TRY(dalloc_t(m, &m->ext_pos, (size_t)m->T_max));
+  return dalloc(m, (void**)&m->ext_ws, std::max<size_t>(ws, 16));
+}
+
+// The chunks of a pass to the device: first token per sequence and the count, then the lengths before it.
+static adept_status put_chunks(adept_model* m, int batch, const int32_t* lens, const int* before, cudaStream_t st) {
+  m->h_ext.assign((size_t)2 * batch + 1, 0);
+  for (int b = 0; b < batch; ++b) {
+    m->h_ext[b + 1] = m->h_ext[b] + lens[b];
+    m->h_ext[batch + 1 + b] = before[b];
+  }
+  CUDA_TRY(m, cudaMemcpyAsync(m->d_ext, m->h_ext.data(), m->h_ext.size() * sizeof(int), cudaMemcpyHostToDevice, st));
+  return ADEPT_OK;
+}
+
 // ---------------------------------------------------------------------------
 // C ABI
 // ---------------------------------------------------------------------------
@@ -1808,6 +1898,7 @@ adept_status adept_model_load(const adept_config* cfg_in, const adept_tensor_tab
   adept_status s = load_weights(m, ld);
   if (s == ADEPT_OK) s = alloc_runtime(m);
   if (s == ADEPT_OK) s = make_tiled(m, ld.st);
+  if (s == ADEPT_OK && m->kv8) s = extend_init(m);   // (its passes all attend by the chunk kernels)
   if (s == ADEPT_OK) {
     cudaError_t e = cudaStreamSynchronize(ld.st);
     if (e != cudaSuccess) s = fail(m, ADEPT_ERR_CUDA, "load: %s", cudaGetErrorString(e));
@@ -1866,23 +1957,16 @@ adept_status adept_prefill(adept_model* m, int batch, int prompt_len, const int3
   TRY(reserve_seqs(m, batch, lens.data(), st));
   launch_set_float(st, m->d_delta, delta);
   m->launches += 1;
+  const ExtendPass e{prompt_len, prompt_len};
+  if (m->kv8) {   // (as chunks behind nothing)
+    const std::vector<int> none(batch, 0);
+    TRY(put_chunks(m, batch, lens.data(), none.data(), st));
+  }
   TRY(run_pass(m, batch * prompt_len, batch, prompt_len, false, d_tokens, d_forced_exit, d_exit_layer_out, d_sim_out,
-               st));
+               st, m->kv8 ? &e : nullptr));
   TRY(run_head(m, batch, prompt_len, false, d_logits_out, d_next_token_out, st));
   span_collect(m, st);
   return check_launch(m);
-}
-
-static adept_status extend_init(adept_model* m) {
-  if (m->ext_ws) return ADEPT_OK;
-  const int B = m->cfg.max_batch;
-  // (the bound over every batch and length)
-  const size_t ws = std::max(chunk_workspace(paged_view(m, 0, B), m->H, m->T_max, m->max_blocks_per_seq * m->cfg.kv_block_tokens),
-                             chunk_workspace(paged_view(m, 0, B), m->H, 1, m->max_blocks_per_seq * m->cfg.kv_block_tokens));
-  if (!m->d_ext) TRY(dalloc_t(m, &m->d_ext, (size_t)2 * B + 1));
-  if (!m->ext_start) TRY(dalloc_t(m, &m->ext_start, (size_t)B + 1));
-  if (!m->ext_pos) TRY(dalloc_t(m, &m->ext_pos, (size_t)m->T_max));
-  return dalloc(m, (void**)&m->ext_ws, std::max<size_t>(ws, 16));
 }
 
 adept_status adept_extend(adept_model* m, int batch, const int32_t* h_lens, const int32_t* d_tokens, float delta,
@@ -1917,13 +2001,8 @@ adept_status adept_extend(adept_model* m, int batch, const int32_t* h_lens, cons
     return fail(m, ADEPT_ERR_CAPACITY, "%lld new tokens above the pass workspace (%d rows)", total, m->T_max);
   TRY(extend_init(m));
   cudaStream_t st = (cudaStream_t)stream;
-  m->h_ext.assign((size_t)2 * batch + 1, 0);
-  for (int b = 0; b < batch; ++b) {
-    m->h_ext[b + 1] = m->h_ext[b] + h_lens[b];
-    m->h_ext[batch + 1 + b] = m->h_seq_len[b];
-    e.max_kv = std::max(e.max_kv, m->h_seq_len[b]);   // (sequences without new tokens stay within the bound)
-  }
-  CUDA_TRY(m, cudaMemcpyAsync(m->d_ext, m->h_ext.data(), m->h_ext.size() * sizeof(int), cudaMemcpyHostToDevice, st));
+  for (int b = 0; b < batch; ++b) e.max_kv = std::max(e.max_kv, m->h_seq_len[b]);   // (sequences without new tokens too)
+  TRY(put_chunks(m, batch, h_lens, m->h_seq_len.data(), st));
   launch_set_float(st, m->d_delta, delta);
   m->launches += 1;
   TRY(run_pass(m, (int)total, batch, 0, false, d_tokens, d_forced_exit, d_exit_layer_out, d_sim_out, st, &e));
@@ -2142,8 +2221,16 @@ adept_status adept_skip_kv_fill(adept_model* m, int n_tokens, const void* d_h_ma
   std::vector<GemmProblem> probs;
   std::vector<int> mrs;
   for (int r = 2; r <= m->N; ++r) {
-    probs.push_back(kv_problem(m, r - 1, m->fill_x, m->fill_cap, DevRange{nullptr, m->fill_start + r, 0}, m->fill_tok, d_seq, d_pos));
+    probs.push_back(kv_problem(m, r - 1, m->fill_x, m->fill_cap, DevRange{nullptr, m->fill_start + r, 0}, m->fill_tok, d_seq, d_pos, false));
     mrs.push_back(n_tokens);
+    if (m->kv8) {   // (one layer's staging cache: layer by layer)
+      gemm(m, st, &probs.back(), 1, &mrs.back(), ADEPT_PROF_KV_FILL);
+      requant(m, st, false, r - 1, 1, m->fill_start + r, n_tokens, m->fill_tok, d_seq, d_pos);
+    }
+  }
+  if (m->kv8) {
+    span_collect(m, st);
+    return check_launch(m);
   }
   // algorithmic work of this launch is only known on the device; the benchmark supplies it.
   // A few tokens: one weight-streaming launch over the layers; else the grouped tcgen05 GEMM.
@@ -2179,6 +2266,14 @@ adept_status adept_read_kv(adept_model* m, int layer, int seq, int pos0, int n_p
     return fail(m, ADEPT_ERR_INVALID_ARG, "sequence %d not reserved", seq);
   if (pos0 < 0 || n_pos < 0 || pos0 + n_pos > m->max_blocks_per_seq * m->cfg.kv_block_tokens)
     return fail(m, ADEPT_ERR_INVALID_ARG, "position range out of the reserved blocks");
+  if (m->kv8) {
+    PdlScope pdl(!m->profile);
+    if (n_pos > 0)
+      note_error(m, launch_kv_gather((cudaStream_t)stream, paged_view(m, layer - 1, m->cfg.max_batch), n_pos, 1, d_k_out,
+                                     (long long)m->Dkv, d_v_out, (long long)m->Dkv, nullptr, nullptr, seq, pos0),
+                 "reading the cache");
+    return check_launch(m);
+  }
   launch_read_kv((cudaStream_t)stream, m->dt, cache_view(m), layer - 1, seq, pos0, n_pos, d_k_out, d_v_out);
   return check_launch(m);
 }
@@ -2404,6 +2499,7 @@ extern "C" ADEPT_API void adept_debug_ktrace(void* dev_buf, unsigned* dev_cnt, u
 namespace adept {
 bool model_fill_view(adept_model* m, FillView* v) {
   if (!m || m->N > FILL_VIEW_MAX_LAYERS) return false;
+  v->kv8 = m->kv8;
   v->n_layers = m->N;
   v->d_model = m->D;
   v->d_q = m->Dq;

@@ -112,3 +112,19 @@ def test_binding_checks_tensors(lib):
                                         row_pos=bad.get("row_pos"))
     with pytest.raises(ValueError, match="overlap"):
         adept.adept_chunk_attention(c, q, s, n, 3, 3, q, ws)
+
+
+def test_models_that_an_8_bit_cache_does_not_fit(lib):
+    import paper_2601_03700_gb300 as adept
+    import synth
+    for kw, word in ((dict(dtype="f32"), "8-bit"), (dict(dtype="bf16", kv_block_tokens=8), "8-bit"),
+                     (dict(dtype="bf16", family=synth.BERT, max_pos=128, n_classes=2), "8-bit")):
+        cfg = synth.tiny_config(**kw)
+        cfg.kv_type = "e4m3"
+        with pytest.raises(adept.AdeptError, match=word) as ei:
+            adept.adept_model_load(cfg, {})
+        assert ei.value.status == 1
+    cfg = synth.tiny_config(dtype="bf16")
+    cfg.kv_type = 1
+    with pytest.raises(adept.AdeptError, match="kv_type"):
+        adept.adept_model_load(cfg, {})
