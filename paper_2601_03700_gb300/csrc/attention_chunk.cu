@@ -688,7 +688,8 @@ __global__ void __launch_bounds__(CJ_THREADS) chunk_join_kernel(const __grid_con
   __shared__ SplitItem s_it;
   __shared__ int s_have;
   __shared__ float s_acc[6][CJ_THREADS];
-  PDL_ENTRY();
+  // The look-up runs beside the partials' kernel: it reads the lengths only, which that kernel has waited for before it let
+  // this one start.
   const int tid = threadIdx.x;
   if (tid < 32) {
     SplitItem it;
@@ -698,6 +699,10 @@ __global__ void __launch_bounds__(CJ_THREADS) chunk_join_kernel(const __grid_con
       s_have = have;
     }
   }
+  KT_BEGIN();
+  pdl_wait();
+  KT_WAITED();
+  pdl_launch_dependents();
   __syncthreads();
   if (!s_have || s_it.n_split <= 1) return;
   const SplitItem it = s_it;

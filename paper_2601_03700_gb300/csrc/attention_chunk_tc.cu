@@ -38,7 +38,7 @@ cudaError_t launch_t(cudaStream_t st, CtParams& p, int* launches) {
     rows = (uint64_t)c.n_seq * p.wide * c.n_kv_heads * 16;
     k = (char*)p.a.part + ct_parts_bytes(DH);
     v = (char*)k + ct_wide_bytes(c, p.a.max_kv);
-    e = launch_k(chunk_widen_kernel<DH>, dim3(p.wide, c.n_seq, 2), dim3(CW_THREADS), 0, st, p, (bf16*)k, (bf16*)v);
+    e = launch_k(chunk_widen_kernel<DH>, dim3((unsigned)std::min<long long>(ct_sms() * 8, 2ll * p.wide * c.n_seq)), dim3(CW_THREADS), 0, st, p, (bf16*)k, (bf16*)v);
     if (e != cudaSuccess) return e;
     ++*launches;
   }
@@ -59,10 +59,16 @@ cudaError_t launch_t(cudaStream_t st, CtParams& p, int* launches) {
 bool chunk_tc_takes(const KvPaged& c, int n_heads, int max_kv) {
   const long long blocks = c.type == KV_E4M3 ? (long long)c.n_seq * cdiv(max_kv, 16) : c.n_blocks;
   return c.type != KV_F32 && c.block_tokens == 16 && (c.head_dim == 64 || c.head_dim == 128) &&
-         n_heads / c.n_kv_heads <= CT_BM && blocks * c.n_kv_heads * 16 < (1ll << 31) && c.n_seq < 65536 && tc_gemm_supported();
+         n_heads / c.n_kv_heads <= CT_BM && blocks * c.n_kv_heads * 16 < (1ll << 31) && tc_gemm_supported();
 }
 
 size_t chunk_tc_workspace(const KvPaged& c, int max_kv) { return ct_parts_bytes(c.head_dim) + 2 * ct_wide_bytes(c, max_kv); }
+
+bool chunk_tc_fits(const KvPaged& c, int n_heads, int n_rows, int max_q, int max_kv) {
+  const long long tq = 2 * (CT_BM / (n_heads / c.n_kv_heads));
+  const long long tiles = std::min(c.n_seq * ((max_q + tq - 1) / tq), n_rows / tq + c.n_seq);
+  return tiles * c.n_kv_heads * std::max(1, cdiv(max_kv, CT_BN)) < (1ll << 31);
+}
 
 cudaError_t launch_chunk_tc(cudaStream_t st, const ChunkCall& a, int* launches) {
   CtParams p;

@@ -10,7 +10,7 @@
 //                       maximum (raised only by more than 2^8), exp2, sum, P to tensor memory; at the end O / l
 //          8            issues the matrix instructions:  PV_0(j) S_0(j+1) PV_1(j) S_1(j+1)  (in issue order on the tensor
 //                       core, so S_0(j+1) may overwrite P_0(j), and a completed S(j+1) means a completed PV(j))
-//          9, 10        fetch K and V blocks by TMA; 10 mends the V tiles at the causal edge (11: idle)
+//          9, 10, 11    fetch K blocks, V blocks and Q by TMA; 10 mends the V tiles at the causal edge
 //
 // The causal edge: from the first row's position on, a key tile holds keys that not every row attends, or none does.  Scores are
 // masked there.  V entries that nobody attends become zero; a NaN or infinite one is replaced by zero and its key noted per
@@ -60,11 +60,12 @@ struct CtParams {
 
 // ---- the key tiles of all tiles in a row ----
 
-// sum over i in [0, n) of floor((a i + b) / m); a n + b below 2^32
-__device__ long long floor_sum(unsigned n, unsigned m, unsigned a, unsigned b) {
-  long long r = 0;
+// (Units fit 31 bits: the launcher refuses calls beyond.)
+// sum over i in [0, n) of floor((a i + b) / m); the sum, and a n + b, below 2^32
+__device__ unsigned floor_sum(unsigned n, unsigned m, unsigned a, unsigned b) {
+  unsigned r = 0;
   while (n > 0) {
-    r += (long long)(n - 1) * n / 2 * (a / m) + (long long)n * (b / m);
+    r += (n & 1 ? (n - 1) / 2 * n : n / 2 * (n - 1)) * (a / m) + n * (b / m);
     a %= m;
     b %= m;
     const unsigned y = a * n + b, x = m;
@@ -81,52 +82,53 @@ __device__ long long floor_sum(unsigned n, unsigned m, unsigned a, unsigned b) {
 __device__ __forceinline__ int ct_units(bool given, int c, int len, int tq, int t) {
   return max(1, (given ? len + CT_BN - 1 : len - c + min((t + 1) * tq, c) + CT_BN - 1) / CT_BN);
 }
-__device__ long long ct_seq_units(bool given, int c, int len, int tq) {
+__device__ int ct_seq_units(bool given, int c, int len, int tq) {
   const int tiles = (c + tq - 1) / tq;
   if (tiles == 0) return 0;
-  if (given) return (long long)tiles * ct_units(true, c, len, tq, 0);
-  const long long last = ct_units(false, c, len, tq, tiles - 1);
+  if (given) return tiles * ct_units(true, c, len, tq, 0);
+  const int last = ct_units(false, c, len, tq, tiles - 1);
   if (tiles == 1) return last;
   if (len - c + tq < 1) {   // (first tiles without keys: one by one)
-    long long r = 0;
+    int r = 0;
     for (int t = 0; t < tiles; ++t) r += ct_units(false, c, len, tq, t);
     return r;
   }
-  return last + floor_sum((unsigned)tiles - 1, CT_BN, (unsigned)tq, (unsigned)(len - c + tq + CT_BN - 1));
+  return last + (int)floor_sum((unsigned)tiles - 1, CT_BN, (unsigned)tq, (unsigned)(len - c + tq + CT_BN - 1));
 }
 
 struct CtTile {
   int seq, q0, c, len, tile, kvh;
-  long long u0;   // first unit of the tile
-  int units;
+  int u0, units;   // first unit of the tile; its units
 };
+// Inclusive sum over the lanes.
+__device__ __forceinline__ int warp_scan(int v) {
+  const int lane = threadIdx.x & 31;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int u = __shfl_up_sync(0xffffffffu, v, o);
+    if (lane >= o) v += u;
+  }
+  return v;
+}
 // All units, taken together by a converged warp.
-__device__ long long ct_total(const ChunkCall& a, int tq) {
-  long long tot = 0;
+__device__ int ct_total(const ChunkCall& a, int tq) {
+  int tot = 0;
   for (int b = threadIdx.x & 31; b < a.c.n_seq; b += 32) {
     int q0, c, len;
     chunk_seq(a, b, q0, c, len);
     tot += ct_seq_units(a.row_pos, c, len, tq) * a.c.n_kv_heads;
   }
-  // (24 bits and the rest: one instruction each)
-  return __reduce_add_sync(0xffffffffu, (unsigned)(tot & 0xffffff)) +
-         ((long long)__reduce_add_sync(0xffffffffu, (unsigned)(tot >> 24)) << 24);
+  return (int)__reduce_add_sync(0xffffffffu, (unsigned)tot);
 }
 // The tile that unit u lies in.
-__device__ void ct_find(const ChunkCall& a, int tq, long long u, CtTile& x) {
+__device__ void ct_find(const ChunkCall& a, int tq, int u, CtTile& x) {
   const int lane = threadIdx.x & 31;
-  long long before = 0;
+  int before = 0;
   for (int b0 = 0; b0 < a.c.n_seq; b0 += 32) {
     int q0 = 0, c = 0, len = 0;
     if (b0 + lane < a.c.n_seq) chunk_seq(a, b0 + lane, q0, c, len);
-    const long long mine = ct_seq_units(a.row_pos, c, len, tq) * a.c.n_kv_heads;
-    long long inc = mine;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const long long v = __shfl_up_sync(0xffffffffu, inc, o);
-      if (lane >= o) inc += v;
-    }
-    const unsigned who = __ballot_sync(0xffffffffu, u < before + inc);
+    const int mine = ct_seq_units(a.row_pos, c, len, tq) * a.c.n_kv_heads, inc = a.c.n_seq > 1 ? warp_scan(mine) : mine;
+    const unsigned who = __ballot_sync(0xffffffffu, lane < a.c.n_seq - b0 && u < before + inc);
     if (!who) {
       before += __shfl_sync(0xffffffffu, inc, 31);
       continue;
@@ -139,14 +141,7 @@ __device__ void ct_find(const ChunkCall& a, int tq, long long u, CtTile& x) {
     x.len = __shfl_sync(0xffffffffu, len, src);
     const int tiles = (x.c + tq - 1) / tq;
     for (int t0 = 0; t0 < tiles; t0 += 32) {
-      const int t = t0 + lane;
-      const long long n = t < tiles ? (long long)ct_units(a.row_pos, x.c, x.len, tq, t) * a.c.n_kv_heads : 0;
-      long long in2 = n;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const long long v = __shfl_up_sync(0xffffffffu, in2, o);
-        if (lane >= o) in2 += v;
-      }
+      const int t = t0 + lane, n = t < tiles ? ct_units(a.row_pos, x.c, x.len, tq, t) * a.c.n_kv_heads : 0, in2 = warp_scan(n);
       const unsigned w2 = __ballot_sync(0xffffffffu, u < before + in2);
       if (!w2) {
         before += __shfl_sync(0xffffffffu, in2, 31);
@@ -156,8 +151,8 @@ __device__ void ct_find(const ChunkCall& a, int tq, long long u, CtTile& x) {
       before += __shfl_sync(0xffffffffu, in2 - n, s2);
       x.tile = t0 + s2;
       x.units = ct_units(a.row_pos, x.c, x.len, tq, x.tile);
-      x.kvh = (int)((u - before) / x.units);
-      x.u0 = before + (long long)x.kvh * x.units;
+      x.kvh = (u - before) / x.units;
+      x.u0 = before + x.kvh * x.units;
       return;
     }
     return;
@@ -175,19 +170,17 @@ __device__ __forceinline__ void ct_next(const ChunkCall& a, int tq, CtTile& x) {
   }
   x.units = ct_units(a.row_pos, x.c, x.len, tq, x.tile);
 }
-// Run i of `runs` (fewer where there are few units).
+// Run i of `runs` (fewer where there are few units): equal shares, the first ones a unit longer.
 constexpr int CT_MIN_RUN = 2;
-__device__ __forceinline__ int ct_runs(long long total, int runs) {
-  return (int)min((long long)runs, (total + CT_MIN_RUN - 1) / CT_MIN_RUN);
-}
-__device__ __forceinline__ long long ct_start(long long total, int runs, int i) { return total * i / runs; }
+__device__ __forceinline__ int ct_runs(int total, int runs) { return min(runs, (total + CT_MIN_RUN - 1) / CT_MIN_RUN); }
+__device__ __forceinline__ int ct_start(int total, int runs, int i) { return total / runs * i + min(i, total % runs); }
 
 // Workspace: a note per run on the tile it begins inside of; per slot (two a run) 256 (m, l) pairs; and per slot 256 rows of
 // weighted V, four columns of all rows after the other (a warp of rows writes whole lines).
 struct CtNote {
-  long long u0;       // first unit of the tile, -1: the run begins with a tile, or is empty
+  int u0;             // first unit of the tile, -1: the run begins with a tile, or is empty
   int row0, kvh, pos0, n_tok;   // the tile's first row of Q, KV head, first position, tokens
-  int pad[2];         // (32 bytes: what follows is read 16 at a time)
+  int pad[3];         // (32 bytes: what follows is read 16 at a time)
 };
 struct CtWs {
   CtNote* note;
@@ -243,10 +236,10 @@ struct CtSeg {
   int nt0, nt1, n_it;  // key tiles with keys: per sub-tile, of the segment
   bool whole;          // the whole tile
   const int* table;
-  __device__ __forceinline__ void set(const ChunkCall& a, int ts, const CtTile& tile, long long u, long long u_end) {
+  __device__ __forceinline__ void set(const ChunkCall& a, int ts, const CtTile& tile, int u, int u_end) {
     x = tile;
-    j_lo = (int)(u - x.u0);
-    j_hi = (int)min((long long)x.units, u_end - x.u0);
+    j_lo = u - x.u0;
+    j_hi = min(x.units, u_end - x.u0);
     whole = j_lo == 0 && j_hi == x.units;
     t0 = x.tile * 2 * ts;
     n_tok = min(2 * ts, x.c - t0);
@@ -296,7 +289,7 @@ __global__ void __launch_bounds__(CtShape<DH>::THREADS, 1) chunk_tc_kernel(const
   __shared__ int s_poisoned[4];
   __shared__ int s_tok[CT_ROWS], s_off[CT_ROWS];   // token of a row in the tile (-1: none), its head's first column in the group
   __shared__ CtTile s_tile;
-  __shared__ long long s_u0, s_u1;
+  __shared__ int s_u0, s_u1;
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const long long wlim = wait_limit();
@@ -325,6 +318,10 @@ __global__ void __launch_bounds__(CtShape<DH>::THREADS, 1) chunk_tc_kernel(const
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   const int group = a.n_heads / a.c.n_kv_heads, ts = p.ts, tq = 2 * ts, run = (int)blockIdx.x;
+  if (tid >= 352 && tid < 355) {   // the maps' first use is a fetch of its own
+    const CUtensorMap* map = tid == 352 ? &p.kmap : tid == 353 ? &p.vmap : &p.qmap;
+    asm volatile("prefetch.tensormap [%0];" ::"l"((uint64_t)map) : "memory");
+  }
   if (warp == 8) {
     tmem_alloc(&s_tmem, 512);
     tmem_relinquish();
@@ -336,9 +333,8 @@ __global__ void __launch_bounds__(CtShape<DH>::THREADS, 1) chunk_tc_kernel(const
   }
   pdl_wait();
   if (warp == 9) {
-    const long long tot = ct_total(a, tq);
-    const int runs = ct_runs(tot, p.runs);
-    const long long u0 = run < runs ? ct_start(tot, runs, run) : 0, u1 = run < runs ? ct_start(tot, runs, run + 1) : 0;
+    const int tot = ct_total(a, tq), runs = ct_runs(tot, p.runs);
+    const int u0 = run < runs ? ct_start(tot, runs, run) : 0, u1 = run < runs ? ct_start(tot, runs, run + 1) : 0;
     CtTile x{};
     if (u0 < u1) ct_find(a, tq, u0, x);
     if (lane == 0) {
@@ -347,7 +343,7 @@ __global__ void __launch_bounds__(CtShape<DH>::THREADS, 1) chunk_tc_kernel(const
       s_tile = x;
       // the join's note: what tile this run begins inside of
       const int t0 = x.tile * tq;
-      CtWs(p).note[run] = CtNote{u0 < u1 && u0 > x.u0 ? x.u0 : -1, x.q0 + t0, x.kvh, x.len - x.c + t0, min(tq, x.c - t0), {0, 0}};
+      CtWs(p).note[run] = CtNote{u0 < u1 && u0 > x.u0 ? x.u0 : -1, x.q0 + t0, x.kvh, x.len - x.c + t0, min(tq, x.c - t0), {0, 0, 0}};
     }
   }
   tc_fence_before();
@@ -355,8 +351,8 @@ __global__ void __launch_bounds__(CtShape<DH>::THREADS, 1) chunk_tc_kernel(const
   tc_fence_after();
   pdl_launch_dependents();   // after the tensor memory is held
   const uint32_t tmem = s_tmem;
-  const long long u_end = s_u1;
-  long long u = s_u0;
+  const int u_end = s_u1;
+  int u = s_u0;
   CtTile x = s_tile;
   CtSeg g{};
   bool ok = true;
@@ -571,15 +567,40 @@ __global__ void __launch_bounds__(CtShape<DH>::THREADS, 1) chunk_tc_kernel(const
     }
     __syncwarp();
   } else if (warp == 11) {
+    // ---- TMA producer of Q: a segment's, once S of the one before it is through
     asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+    int nq = 0;
+    while (u < u_end) {
+      g.set(a, ts, x, u, u_end);
+      if (g.n_it > 0) {
+        if (nq > 0 && !mbar_wait_warp(&q_free, (uint32_t)((nq - 1) & 1), abort_flag, err, wlim)) break;
+        if (elect_one()) {
+          const int subs = g.n_tok > ts ? 2 : 1;
+          mbar_expect_tx(&q_full, (uint32_t)(subs * L::HALVES * ts * group * 128));
+          for (int b = 0; b < subs; ++b)
+            for (int hf = 0; hf < L::HALVES; ++hf)
+              tma_load_q(&p.qmap, &q_full, sQ + b * L::Q_BYTES + hf * CT_BM * 128, hf * 64, g.x.kvh * group, g.x.q0 + g.t0 + b * ts);
+        }
+        __syncwarp();
+        ++nq;
+      }
+      ct_next(a, tq, x);
+      u = x.u0;
+    }
+    if (lane == 0) {   // (landed before the CTA ends)
+      const long long c0 = clock64();
+      while (nq > 0 && !mbar_try_wait(&q_full, (uint32_t)((nq - 1) & 1)) && clock64() - c0 < CT_DRAIN_CYCLES) {
+      }
+    }
+    __syncwarp();
   } else {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
-    // ---- TMA producers: Q and K (warp 9), V (warp 10, which also mends the V tiles at the edge)
+    // ---- TMA producers: K (warp 9), V (warp 10, which also mends the V tiles at the edge)
     const bool kw = warp == 9;
     uint64_t *full = kw ? k_full : v_full, *empty = kw ? k_empty : v_empty;
     const CUtensorMap* map = kw ? &p.kmap : &p.vmap;
     uint8_t* dst0 = kw ? sK : sV;
-    int cnt = 0, nq = 0;   // tiles, Qs sent so far
+    int cnt = 0;   // tiles sent so far
     // V tile j (the vi-th, blocks `gone` of it not there): entries nobody attends to zero, non-finite ones noted
     auto mend = [&](int j, int vi, int gone, int par) {
       const int s = vi & 1;
@@ -655,18 +676,6 @@ __global__ void __launch_bounds__(CtShape<DH>::THREADS, 1) chunk_tc_kernel(const
         }
         __syncwarp();
         ++cnt;
-        if (kw && j == 0) {   // Q, once S of the segment before is through
-          if (nq > 0 && !(ok = mbar_wait_warp(&q_free, (uint32_t)((nq - 1) & 1), abort_flag, err, wlim))) break;
-          if (elect_one()) {
-            const int subs = g.n_tok > ts ? 2 : 1;
-            mbar_expect_tx(&q_full, (uint32_t)(subs * L::HALVES * ts * group * 128));
-            for (int b = 0; b < subs; ++b)
-              for (int hf = 0; hf < L::HALVES; ++hf)
-                tma_load_q(&p.qmap, &q_full, sQ + b * L::Q_BYTES + hf * CT_BM * 128, hf * 64, g.x.kvh * group, g.x.q0 + g.t0 + b * ts);
-          }
-          __syncwarp();
-          ++nq;
-        }
       }
       ct_next(a, tq, x);
       u = x.u0;
@@ -678,9 +687,6 @@ __global__ void __launch_bounds__(CtShape<DH>::THREADS, 1) chunk_tc_kernel(const
         while (!mbar_try_wait(&full[t & 1], (uint32_t)((t >> 1) & 1)) && clock64() - c0 < CT_DRAIN_CYCLES) {
         }
       }
-      const long long c0 = clock64();
-      while (nq > 0 && !mbar_try_wait(&q_full, (uint32_t)((nq - 1) & 1)) && clock64() - c0 < CT_DRAIN_CYCLES) {
-      }
     }
     __syncwarp();
   }
@@ -690,39 +696,88 @@ __global__ void __launch_bounds__(CtShape<DH>::THREADS, 1) chunk_tc_kernel(const
   if (warp == 8) tmem_dealloc(tmem, 512);
 }
 
-// Entries of 8 bits as bf16: CTA = a block of positions of one sequence, K (z = 0) or V, all heads, 16 elements a thread and turn.
+// Entries of 8 bits as bf16.  Work: the blocks of positions of this launch's sequences, K and V apart, all heads of one at a time;
+// CTA i of n takes the i-th of n equal runs of them (the lengths are known on the device only).
 constexpr int CW_THREADS = 256;
 template <int DH>
 __global__ void __launch_bounds__(CW_THREADS) chunk_widen_kernel(const __grid_constant__ CtParams p, bf16* k_out, bf16* v_out) {
   PDL_ENTRY();
+  __shared__ int s_seq, s_blk, s_len;
+  __shared__ long long s_u0, s_u1;
   const ChunkCall& a = p.a;
-  const int b = (int)blockIdx.x, seq = (int)blockIdx.y;
-  int q0, c, len;
-  chunk_seq(a, seq, q0, c, len);
-  if (c == 0 || b * 16 >= len) return;
-  const int blk = a.c.table[(size_t)seq * a.c.max_blocks + b];
-  if (blk < 0 || blk >= a.c.n_blocks) return;
-  const int n = a.c.n_kv_heads * 16 * (DH / 16);
-  const size_t from = (size_t)blk * a.c.n_kv_heads * 16, to = ((size_t)seq * p.wide + b) * a.c.n_kv_heads * 16;
-  const uint8_t* codes = (const uint8_t*)(blockIdx.z ? a.c.v : a.c.k) + from * DH;
-  const uint8_t* exps = (blockIdx.z ? a.c.v_exp : a.c.k_exp) + from;
-  bf16* out = (blockIdx.z ? v_out : k_out) + to * DH;
-#pragma unroll 4
-  for (int i = threadIdx.x; i < n; i += CW_THREADS) {
-    const uint4 w = reinterpret_cast<const uint4*>(codes)[i];
-    const int e = exps[i / (DH / 16)];
-    const float s = e ? __uint_as_float((unsigned)e << 23) : __uint_as_float(0x400000u);   // 2^(e - 127)
-    const uint32_t x[4] = {w.x, w.y, w.z, w.w};
-    uint32_t y[8];
-#pragma unroll
-    for (int q = 0; q < 8; ++q) {
-      const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(x[q >> 1] >> (q & 1 ? 16 : 0)), __NV_E4M3);
-      const float2 f = __half22float2(__half2(h));
-      const __nv_bfloat162 r = __floats2bfloat162_rn(f.x * s, f.y * s);
-      y[q] = *reinterpret_cast<const uint32_t*>(&r);
+  const int lane = threadIdx.x & 31;
+  if (threadIdx.x < 32) {
+    long long tot = 0;
+    for (int b = lane; b < a.c.n_seq; b += 32) {
+      int q0, c, len;
+      chunk_seq(a, b, q0, c, len);
+      tot += (len + 15) / 16;
     }
-    reinterpret_cast<uint4*>(out)[2 * i] = make_uint4(y[0], y[1], y[2], y[3]);
-    reinterpret_cast<uint4*>(out)[2 * i + 1] = make_uint4(y[4], y[5], y[6], y[7]);
+    tot = __reduce_add_sync(0xffffffffu, (unsigned)(tot & 0xffffff)) + ((long long)__reduce_add_sync(0xffffffffu, (unsigned)(tot >> 24)) << 24);
+    const long long u0 = 2 * tot * blockIdx.x / gridDim.x, u1 = 2 * tot * (blockIdx.x + 1) / gridDim.x;
+    long long before = 0;
+    for (int b0 = 0; b0 < a.c.n_seq && u0 < u1; b0 += 32) {   // the sequence that block u0 / 2 is of
+      int q0 = 0, c = 0, len = 0;
+      if (b0 + lane < a.c.n_seq) chunk_seq(a, b0 + lane, q0, c, len);
+      const int mine = (len + 15) / 16;
+      long long inc = mine;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const long long v = __shfl_up_sync(0xffffffffu, inc, o);
+        if (lane >= o) inc += v;
+      }
+      const unsigned who = __ballot_sync(0xffffffffu, u0 / 2 < before + inc);
+      if (who) {
+        if (lane == __ffs(who) - 1) {
+          s_seq = b0 + lane;
+          s_blk = (int)(u0 / 2 - before - (inc - mine));
+          s_len = len;
+        }
+        break;
+      }
+      before += __shfl_sync(0xffffffffu, inc, 31);
+    }
+    if (lane == 0) {
+      s_u0 = u0;
+      s_u1 = u1;
+    }
+  }
+  __syncthreads();
+  int seq = s_seq, b = s_blk, len = s_len;
+  const int n = a.c.n_kv_heads * 16 * (DH / 16);
+  for (long long u = s_u0; u < s_u1; ++u) {
+    const int blk = a.c.table[(size_t)seq * a.c.max_blocks + b], is_v = (int)(u & 1);
+    if (blk >= 0 && blk < a.c.n_blocks) {
+      const size_t from = (size_t)blk * a.c.n_kv_heads * 16, to = ((size_t)seq * p.wide + b) * a.c.n_kv_heads * 16;
+      const uint8_t* codes = (const uint8_t*)(is_v ? a.c.v : a.c.k) + from * DH;
+      const uint8_t* exps = (is_v ? a.c.v_exp : a.c.k_exp) + from;
+      bf16* out = (is_v ? v_out : k_out) + to * DH;
+#pragma unroll 4
+      for (int i = threadIdx.x; i < n; i += CW_THREADS) {
+        const uint4 w = reinterpret_cast<const uint4*>(codes)[i];
+        const int e = exps[i / (DH / 16)];
+        const float s = e ? __uint_as_float((unsigned)e << 23) : __uint_as_float(0x400000u);   // 2^(e - 127)
+        const uint32_t x[4] = {w.x, w.y, w.z, w.w};
+        uint32_t y[8];
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+          const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(x[q >> 1] >> (q & 1 ? 16 : 0)), __NV_E4M3);
+          const float2 f = __half22float2(__half2(h));
+          const __nv_bfloat162 r = __floats2bfloat162_rn(f.x * s, f.y * s);
+          y[q] = *reinterpret_cast<const uint32_t*>(&r);
+        }
+        reinterpret_cast<uint4*>(out)[2 * i] = make_uint4(y[0], y[1], y[2], y[3]);
+        reinterpret_cast<uint4*>(out)[2 * i + 1] = make_uint4(y[4], y[5], y[6], y[7]);
+      }
+    }
+    if (is_v && ++b * 16 >= len) {
+      b = 0;
+      len = 0;
+      while (len == 0 && ++seq < a.c.n_seq) {
+        int q0, c;
+        chunk_seq(a, seq, q0, c, len);
+      }
+    }
   }
 }
 

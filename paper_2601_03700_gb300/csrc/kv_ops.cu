@@ -69,6 +69,8 @@ adept_status call_ok(const KvPaged& v, int n_heads, int n_rows, int max_q, int m
   if (max_kv > v.max_blocks * v.block_tokens)
     return bad(ADEPT_ERR_INVALID_ARG, "max_kv_len %d above the %d positions of a sequence", max_kv, v.max_blocks * v.block_tokens);
   if ((long long)n_rows * n_heads > (1ll << 30)) return bad(ADEPT_ERR_CAPACITY, "n_rows * n_heads above 2^30");
+  if (n_heads / v.n_kv_heads <= 128 && !chunk_tc_fits(v, n_heads, n_rows, max_q, max_kv))
+    return bad(ADEPT_ERR_CAPACITY, "a call of more than 2^31 tiles");
   return ADEPT_OK;
 }
 

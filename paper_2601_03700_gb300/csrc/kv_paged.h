@@ -54,6 +54,8 @@ cudaError_t launch_chunk_attention(cudaStream_t st, const ChunkCall& a, int* lau
 // The tcgen05 kernel (attention_chunk_tc.cu): what it takes (rows on 16 bytes besides), its workspace, its launches.
 bool chunk_tc_takes(const KvPaged& c, int n_heads, int max_kv);
 size_t chunk_tc_workspace(const KvPaged& c, int max_kv);
+// Whether a call's (tile, KV head, key tile) triples fit 31 bits (hours of work otherwise).
+bool chunk_tc_fits(const KvPaged& c, int n_heads, int n_rows, int max_q, int max_kv);
 cudaError_t launch_chunk_tc(cudaStream_t st, const ChunkCall& a, int* launches);
 cudaError_t set_wait_limit_ct(long long cycles);
 cudaError_t set_wait_limit_cf(long long cycles);
@@ -78,9 +80,9 @@ struct SplitItem {
 
 // Lengths of sequence b, or no work (c = 0) where they are out of bounds or not this launch's.
 __device__ __forceinline__ void chunk_seq(const ChunkCall& a, int b, int& q0, int& c, int& len) {
-  q0 = a.q_start[b];
-  c = a.q_start[b + 1] - q0;
-  len = a.kv_len[b];
+  q0 = __ldcg(a.q_start + b);   // (past L1: a join reads them before its dependency wait)
+  c = __ldcg(a.q_start + b + 1) - q0;
+  len = __ldcg(a.kv_len + b);
   const int cap = min(a.max_kv, a.c.max_blocks * a.c.block_tokens);
   if (q0 < 0 || c < 0 || c > a.max_q || q0 > a.n_rows - c || len < 0 || len > cap) {
     a.c.flag(ERRW_POS);

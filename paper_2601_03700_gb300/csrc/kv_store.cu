@@ -92,7 +92,7 @@ template <int DH>
 struct Item {
   int r, is_v, h, sub;
   __device__ __forceinline__ Item(int i, int hk, int per_row) {
-    r = i / per_row;
+    r = (int)(((float)i + 0.5f) * (1.f / (float)per_row));   // (i < 2^21: exact)
     const int w = i - r * per_row, vec = w / (DH / KS_EL);
     sub = w % (DH / KS_EL);
     is_v = vec >= hk;
