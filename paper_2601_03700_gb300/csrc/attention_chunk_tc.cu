@@ -67,7 +67,7 @@ size_t chunk_tc_workspace(const KvPaged& c, int max_kv) { return ct_parts_bytes(
 bool chunk_tc_fits(const KvPaged& c, int n_heads, int n_rows, int max_q, int max_kv) {
   const long long tq = 2 * (CT_BM / (n_heads / c.n_kv_heads));
   const long long tiles = std::min(c.n_seq * ((max_q + tq - 1) / tq), n_rows / tq + c.n_seq);
-  return tiles * c.n_kv_heads * std::max(1, cdiv(max_kv, CT_BN)) < (1ll << 31);
+  return tiles * c.n_kv_heads * (CT_TILE + cdiv(max_kv, CT_BN)) < (1ll << 31);
 }
 
 cudaError_t launch_chunk_tc(cudaStream_t st, const ChunkCall& a, int* launches) {

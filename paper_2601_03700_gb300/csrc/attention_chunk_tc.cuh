@@ -77,10 +77,12 @@ __device__ unsigned floor_sum(unsigned n, unsigned m, unsigned a, unsigned b) {
   }
   return r;
 }
-// Key tiles of token tile t (at least one: a tile without keys has zeros to write; with given positions, those of the whole
-// sequence).
+// Units of token tile t: its key tiles (with given positions, those of the whole sequence), and CT_TILE for what every tile costs
+// (its queries' way in, its output's way out: two to three key tiles' time.  Without that, 37 tokens on nothing beside 512 on 1531
+// put six tiles of one unit on the first SM: 49 us, 35 without the 37).
+constexpr int CT_TILE = 2;
 __device__ __forceinline__ int ct_units(bool given, int c, int len, int tq, int t) {
-  return max(1, (given ? len + CT_BN - 1 : len - c + min((t + 1) * tq, c) + CT_BN - 1) / CT_BN);
+  return CT_TILE + max(0, (given ? len + CT_BN - 1 : len - c + min((t + 1) * tq, c) + CT_BN - 1) / CT_BN);
 }
 __device__ int ct_seq_units(bool given, int c, int len, int tq) {
   const int tiles = (c + tq - 1) / tq;
@@ -93,7 +95,7 @@ __device__ int ct_seq_units(bool given, int c, int len, int tq) {
     for (int t = 0; t < tiles; ++t) r += ct_units(false, c, len, tq, t);
     return r;
   }
-  return last + (int)floor_sum((unsigned)tiles - 1, CT_BN, (unsigned)tq, (unsigned)(len - c + tq + CT_BN - 1));
+  return last + (tiles - 1) * CT_TILE + (int)floor_sum((unsigned)tiles - 1, CT_BN, (unsigned)tq, (unsigned)(len - c + tq + CT_BN - 1));
 }
 
 struct CtTile {
@@ -170,8 +172,10 @@ __device__ __forceinline__ void ct_next(const ChunkCall& a, int tq, CtTile& x) {
   }
   x.units = ct_units(a.row_pos, x.c, x.len, tq, x.tile);
 }
-// Run i of `runs` (fewer where there are few units): equal shares, the first ones a unit longer.
-constexpr int CT_MIN_RUN = 2;
+// Run i of `runs` (fewer where there are few units): equal shares, the first ones a unit longer; a run that would begin within the
+// first units of a tile, before any of its key tiles is through, begins with the tile (ct_snap).
+constexpr int CT_MIN_RUN = CT_TILE + 1;
+__device__ __forceinline__ int ct_snap(int u, const CtTile& x) { return u - x.u0 <= CT_TILE ? x.u0 : u; }
 __device__ __forceinline__ int ct_runs(int total, int runs) { return min(runs, (total + CT_MIN_RUN - 1) / CT_MIN_RUN); }
 __device__ __forceinline__ int ct_start(int total, int runs, int i) { return total / runs * i + min(i, total % runs); }
 
@@ -238,9 +242,9 @@ struct CtSeg {
   const int* table;
   __device__ __forceinline__ void set(const ChunkCall& a, int ts, const CtTile& tile, int u, int u_end) {
     x = tile;
-    j_lo = u - x.u0;
-    j_hi = min(x.units, u_end - x.u0);
-    whole = j_lo == 0 && j_hi == x.units;
+    j_lo = max(u - x.u0 - CT_TILE, 0);
+    j_hi = min(x.units, u_end - x.u0) - CT_TILE;
+    whole = u == x.u0 && u_end - x.u0 >= x.units;
     t0 = x.tile * 2 * ts;
     n_tok = min(2 * ts, x.c - t0);
     lim_lo = keys(a, 0);
@@ -332,18 +336,22 @@ __global__ void __launch_bounds__(CtShape<DH>::THREADS, 1) chunk_tc_kernel(const
     s_off[tid] = rr % group * DH;
   }
   pdl_wait();
-  if (warp == 9) {
-    const int tot = ct_total(a, tq), runs = ct_runs(tot, p.runs);
-    const int u0 = run < runs ? ct_start(tot, runs, run) : 0, u1 = run < runs ? ct_start(tot, runs, run + 1) : 0;
+  if (warp == 9 || warp == 10) {   // where the run begins, where it ends
+    const int tot = ct_total(a, tq), runs = ct_runs(tot, p.runs), i = min(run + warp - 9, runs);
     CtTile x{};
-    if (u0 < u1) ct_find(a, tq, u0, x);
+    int u0 = tot;
+    if (i < runs) {
+      const int at = ct_start(tot, runs, i);
+      ct_find(a, tq, at, x);
+      u0 = ct_snap(at, x);
+    }
     if (lane == 0) {
-      s_u0 = u0;
-      s_u1 = u1;
-      s_tile = x;
-      // the join's note: what tile this run begins inside of
-      const int t0 = x.tile * tq;
-      CtWs(p).note[run] = CtNote{u0 < u1 && u0 > x.u0 ? x.u0 : -1, x.q0 + t0, x.kvh, x.len - x.c + t0, min(tq, x.c - t0), {0, 0, 0}};
+      if (warp == 9) {
+        s_u0 = u0;
+        s_tile = x;
+      } else {
+        s_u1 = u0;
+      }
     }
   }
   tc_fence_before();
@@ -354,6 +362,10 @@ __global__ void __launch_bounds__(CtShape<DH>::THREADS, 1) chunk_tc_kernel(const
   const int u_end = s_u1;
   int u = s_u0;
   CtTile x = s_tile;
+  if (tid == 0) {   // the join's note: what tile this run begins inside of
+    const int t0 = x.tile * tq;
+    CtWs(p).note[run] = CtNote{u < u_end && u > x.u0 ? x.u0 : -1, x.q0 + t0, x.kvh, x.len - x.c + t0, min(tq, x.c - t0), {0, 0, 0}};
+  }
   CtSeg g{};
   bool ok = true;
 
@@ -489,7 +501,7 @@ __global__ void __launch_bounds__(CtShape<DH>::THREADS, 1) chunk_tc_kernel(const
             __syncwarp();
           }
         } else if (mine) {
-          const int slot = run * 2 + (g.j_lo == 0 ? 1 : 0);
+          const int slot = run * 2 + (u == g.x.u0 ? 1 : 0);
           *ws.ml_at(slot, sub * 128 + r) = make_float2(m, l);
 #pragma unroll
           for (int e = 0; e < DH / 4; ++e)
