@@ -436,12 +436,18 @@ class KVCache:
                                p(self.v), p(self.k_exp), p(self.v_exp), p(self.block_table), p(self.err))
         self.ref = ctypes.byref(self._c)
 
-    def attention_workspace(self, n_heads: int, n_rows: int, max_q_len: int, max_kv_len: int) -> Optional[torch.Tensor]:
-        """A workspace for adept_chunk_attention calls of these sizes (None: none needed)."""
+    def attention_workspace(self, n_heads: int, n_rows: int, max_q_len: int, max_kv_len: int,
+                            stream=None) -> Optional[torch.Tensor]:
+        """A workspace for adept_chunk_attention calls of these sizes on `stream` (None: none needed)."""
         n = load_library().adept_chunk_attention_workspace(self.ref, n_heads, n_rows, max_q_len, max_kv_len)
         if n < 0:
             _check(load_library(), None, 1)
-        return torch.empty(n, dtype=torch.uint8, device=self.device) if n else None
+        if n == 0:
+            return None
+        if stream is not None and not hasattr(stream, "cuda_stream"):
+            stream = torch.cuda.ExternalStream(int(stream))
+        with torch.cuda.stream(stream):   # (memory of the call's stream, which alone reuses it)
+            return torch.empty(n, dtype=torch.uint8, device=self.device)
 
     def check(self, stream=None):
         adept_kv_check(self, stream)
@@ -534,9 +540,7 @@ def adept_chunk_attention(cache: KVCache, q: torch.Tensor, q_start: torch.Tensor
     if out.data_ptr() == q.data_ptr() and n:
         raise ValueError("q and out must not overlap")
     if workspace is None:
-        s = stream if stream is None or hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream))
-        with torch.cuda.stream(s):   # (the call's stream: memory that it alone reuses)
-            workspace = cache.attention_workspace(heads, n, max_q_len, max_kv_len)
+        workspace = cache.attention_workspace(heads, n, max_q_len, max_kv_len, stream)
     elif workspace.get_device() != cache.index or not workspace.is_contiguous():
         raise ValueError(f"workspace must be contiguous on {cache.device}")
     ws, nb = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.nbytes)
