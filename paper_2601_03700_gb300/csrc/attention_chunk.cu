@@ -187,6 +187,11 @@ __global__ void __launch_bounds__(CG_KEYS) chunk_any_kernel(const __grid_constan
 // e4m3: K as fp16, one conversion for two codes (bf16 takes four instructions), with Q as fp16 too, each row moved by a power
 // of two so that its largest element lies in [2^14, 2^15): exact down to 2^-28 of it.  V as bf16, since P has to keep bf16's
 // range (a position of little weight may hold a V of any size).  K's exponent scales S, V's scales P.
+//
+// A tile's keys are split over CTAs even where they are few (12 heads of 64, 333 keys: 6.8 us split and joined, 9.0 by 12 CTAs;
+// 1000 keys 7.1 and 19.2), in one of two ways.  Where a cluster of up to 8 CTAs a tile is enough (cs > 1), its CTAs take
+// equal shares and join through distributed shared memory, in one launch.  Else each tile gets as many as balance the GPU
+// (split_find), whose partials a second launch joins.
 // ---------------------------------------------------------------------------------------------
 constexpr int CF_WARPS = 4, CF_ROWS = 16;
 constexpr float CF_RAISE = 8.f;   // the running maximum is raised once a score exceeds it by 2^8: weights stay below 256
@@ -241,6 +246,26 @@ __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t b
                : "memory");
 }
 
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// The value at `p` in the shared memory of the cluster's CTA `rank`.
+__device__ __forceinline__ uint32_t cluster_addr(const void* p, int rank) {
+  uint32_t a;
+  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_u32(p)), "r"(rank));
+  return a;
+}
+__device__ __forceinline__ float ld_cluster(const float* p, int rank) {
+  float v;
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(cluster_addr(p, rank)) : "memory");
+  return v;
+}
+__device__ __forceinline__ float4 ld_cluster4(const float* p, int rank) {
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+               : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(cluster_addr(p, rank)) : "memory");
+  return v;
+}
 // A bounded wait of the whole warp for a stage; false: it did not land in time, or another warp gave up.
 __device__ __forceinline__ bool cf_wait(uint64_t* bar, unsigned parity, volatile int* abort_flag, unsigned* err, long long lim) {
   if (mbar_try_wait(bar, parity)) return true;
@@ -286,13 +311,15 @@ struct FewShape {
 
 template <int DH, int KT>
 __global__ void __launch_bounds__(CF_WARPS * 32, 3) chunk_few_kernel(const __grid_constant__ ChunkCall a,
-                                                                     const __grid_constant__ SplitPlan p, int per_tok, int sub) {
+                                                                     const __grid_constant__ SplitPlan p, int per_tok, int sub,
+                                                                     int cs) {
   using F = FewShape<DH, KT>;
   constexpr int KS = DH / 16;
   constexpr bool F16 = KT == KV_E4M3;   // S in fp16
   __shared__ SplitItem s_it;
   __shared__ int s_have, s_abort;
   __shared__ float s_m[CF_WARPS][CF_ROWS], s_l[CF_WARPS][CF_ROWS];
+  __shared__ float s_cm[CF_ROWS], s_cl[CF_ROWS];   // of the CTA, for its cluster
   __shared__ __align__(8) uint64_t s_full[CF_WARPS][F::STAGES];
   extern __shared__ __align__(128) uint8_t s_dyn[];   // the rings; then [warp][row][DH + 4] floats
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
@@ -303,16 +330,24 @@ __global__ void __launch_bounds__(CF_WARPS * 32, 3) chunk_few_kernel(const __gri
   if (tid == 0) s_abort = 0;
   const long long wlim = wait_limit();
   PDL_ENTRY();
+  const int rank = cs > 1 ? (int)blockIdx.x % cs : 0;
   if (warp == 0) {
     SplitItem it;
-    const bool have = split_find(a, p, (int)blockIdx.x, false, it);
+    const bool have = split_find(a, p, (int)blockIdx.x / cs, cs > 1, it);
+    if (cs > 1 && have) {
+      const int per = (it.units + cs - 1) / cs;
+      it.split = rank;
+      it.n_split = cs;
+      it.u0 = min(it.units, rank * per);
+      it.u1 = min(it.units, it.u0 + per);
+    }
     if (lane == 0) {
       s_it = it;
       s_have = have;
     }
   }
   __syncthreads();
-  if (!s_have) return;
+  if (!s_have) return;   // (all CTAs of a cluster)
   const SplitItem it = s_it;
   const int group = a.n_heads / a.c.n_kv_heads, kvh = it.group / sub, g0 = it.group % sub * per_tok;
   const int j0 = it.tile * p.tq, n = min(p.tq, it.c - j0);
@@ -643,7 +678,13 @@ __global__ void __launch_bounds__(CF_WARPS * 32, 3) chunk_few_kernel(const __gri
       x[2] += f * v.z;
       x[3] += f * v.w;
     }
-    if (it.n_split > 1) {
+    if (cs > 1) {   // into the place of the first warp's sums, which this thread alone has read
+      *reinterpret_cast<float4*>(&s_o[r * LD + d]) = make_float4(x[0], x[1], x[2], x[3]);
+      if (d == 0) {
+        s_cm[r] = M;
+        s_cl[r] = L;
+      }
+    } else if (it.n_split > 1) {
       *reinterpret_cast<float4*>(pv.o + r * DH + d) = make_float4(x[0], x[1], x[2], x[3]);
       if (d == 0) *reinterpret_cast<float2*>(pv.ml + r * 2) = make_float2(M, L);
     } else {
@@ -651,6 +692,44 @@ __global__ void __launch_bounds__(CF_WARPS * 32, 3) chunk_few_kernel(const __gri
       uint2 y = make_uint2(pack_bf16(x[0] * inv, x[1] * inv), pack_bf16(x[2] * inv, x[3] * inv));
       *reinterpret_cast<uint2*>((bf16*)a.out + (size_t)(it.q0 + j0 + j) * a.ld_out + (size_t)(kvh * group + gq) * DH + d) = y;
     }
+  }
+  if (cs > 1) {
+    // join over the cluster, in rank order: each CTA a share of the elements, all ranks' loads under way together
+    cluster_sync();
+    for (int i = tid + rank * (CF_WARPS * 32); i < n_row * (DH / 4); i += CF_WARPS * 32 * cs) {
+      const int r = i / (DH / 4), d = i % (DH / 4) * 4, j = r / per_tok, gq = g0 + r % per_tok;
+      if (gq >= group) continue;
+      float m8[8], l8[8];
+      float4 x8[8];
+      float M = -INFINITY;
+#pragma unroll
+      for (int c = 0; c < 8; ++c) {
+        m8[c] = -INFINITY;
+        l8[c] = 0.f;
+        x8[c] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (c < cs) {
+          m8[c] = ld_cluster(&s_cm[r], c);
+          l8[c] = ld_cluster(&s_cl[r], c);
+          x8[c] = ld_cluster4(&s_o[r * LD + d], c);
+        }
+        M = fmaxf(M, m8[c]);
+      }
+      const float mref = M == -INFINITY ? 0.f : M;
+      float L = 0.f, x[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int c = 0; c < 8; ++c) {
+        const float f = ex2_approx(m8[c] - mref);
+        L += f * l8[c];
+        x[0] += f * x8[c].x;
+        x[1] += f * x8[c].y;
+        x[2] += f * x8[c].z;
+        x[3] += f * x8[c].w;
+      }
+      const float inv = keys_of(j) == 0 ? 0.f : 1.f / L;
+      *reinterpret_cast<uint2*>((bf16*)a.out + (size_t)(it.q0 + j0 + j) * a.ld_out + (size_t)(kvh * group + gq) * DH + d) =
+          make_uint2(pack_bf16(x[0] * inv, x[1] * inv), pack_bf16(x[2] * inv, x[3] * inv));
+    }
+    cluster_sync();   // (a CTA's shared memory stays until all have read it)
   }
 }
 
@@ -811,17 +890,48 @@ bool use_tc(const KvPaged& c, int n_heads, int max_q, int max_kv, bool aligned) 
 // be widened for it, go to the few-row kernel.
 bool use_both(const KvPaged& c) { return c.type == KV_E4M3 && c.n_seq > 1; }
 
+template <int DH, int KT>
+struct FewTag {};
+
 template <int DH, int KT, typename T>
 cudaError_t chunk_t(cudaStream_t st, const ChunkCall& a, const ChunkHow& w, int* launches) {
-  const dim3 grid((unsigned)split_items(w.p, a.c.n_seq, a.n_rows, std::min(a.max_q, a.c_hi)));
+  const int max_c = std::min(a.max_q, a.c_hi);
+  const dim3 grid((unsigned)split_items(w.p, a.c.n_seq, a.n_rows, max_c));
   cudaError_t e = cudaErrorInvalidValue;
   ++*launches;
   if (!w.few) {
     e = launch_k(chunk_any_kernel<DH, KT, T>, grid, dim3(CG_KEYS), 0, st, a, w.p);
   } else if constexpr (KT != KV_F32) {
     constexpr int smem = FewShape<DH, KT>::SMEM;
-    e = cudaFuncSetAttribute(chunk_few_kernel<DH, KT>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-    if (e == cudaSuccess) e = launch_k(chunk_few_kernel<DH, KT>, grid, dim3(CF_WARPS * 32), smem, st, a, w.p, w.per_tok, w.sub);
+    e = smem_once<FewTag<DH, KT>>(chunk_few_kernel<DH, KT>, smem);
+    if (e != cudaSuccess) return e;
+    // A cluster per tile: the largest of 8, 4, 2 CTAs whose clusters find room at once, where that leaves a CTA a few rounds
+    // (4 at heads of 128, 2 at 64, 1 at 32).  One call of a token each in a captured graph, cluster and split: 12 heads of 64,
+    // 500 keys 5.6 and 7.0 us, 1000 keys 6.3 and 7.2, 2000 keys 7.7 and 7.5; 32 heads of 128 on 8, 500 keys 6.8 and 8.4,
+    // 2000 keys 9.1 and 11.4, 4000 keys 12.8 and 13.8, 3 sequences of up to 4000 14.3 and 14.4.  Clusters that had no room at
+    // once (8 sequences, 512 CTAs): 14.2 and 10.0.
+    SplitPlan one = w.p;
+    one.target = 0;
+    const long long tiles = split_items(one, a.c.n_seq, a.n_rows, max_c), units = cdiv(a.max_kv, w.p.unit);
+    int cs = 8;
+    while (cs > 1 && tiles * cs > w.p.target) cs >>= 1;
+    if (cs > 1 && w.may_split && units * 32 <= DH * cs) {
+      cudaLaunchConfig_t cfg = {};
+      cfg.gridDim = dim3((unsigned)(tiles * cs));
+      cfg.blockDim = dim3(CF_WARPS * 32);
+      cfg.dynamicSmemBytes = smem;
+      cfg.stream = st;
+      cudaLaunchAttribute at[2];
+      at[0].id = cudaLaunchAttributeClusterDimension;
+      at[0].val.clusterDim.x = (unsigned)cs;
+      at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+      at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+      at[1].val.programmaticStreamSerializationAllowed = 1;
+      cfg.attrs = at;
+      cfg.numAttrs = g_pdl ? 2 : 1;
+      return cudaLaunchKernelEx(&cfg, chunk_few_kernel<DH, KT>, a, w.p, w.per_tok, w.sub, cs);
+    }
+    e = launch_k(chunk_few_kernel<DH, KT>, grid, dim3(CF_WARPS * 32), smem, st, a, w.p, w.per_tok, w.sub, 1);
   }
   if (e == cudaSuccess && w.may_split) {
     ++*launches;

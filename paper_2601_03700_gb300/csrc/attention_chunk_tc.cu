@@ -29,7 +29,7 @@ template <int DH>
 cudaError_t launch_t(cudaStream_t st, CtParams& p, int* launches) {
   constexpr int smem = CtShape<DH>::TOTAL + 1024;
   const KvPaged& c = p.a.c;
-  cudaError_t e = cudaFuncSetAttribute(chunk_tc_kernel<DH>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  cudaError_t e = smem_once<CtShape<DH>>(chunk_tc_kernel<DH>, smem);
   if (e != cudaSuccess) return e;
   void *k = c.k, *v = c.v;
   uint64_t rows = (uint64_t)c.n_blocks * c.n_kv_heads * 16;

@@ -3,6 +3,8 @@
 #pragma once
 #include "common.cuh"
 
+#include <atomic>
+
 namespace adept {
 
 enum KvType : int { KV_F32 = 0, KV_BF16 = 1, KV_E4M3 = 2 };
@@ -74,7 +76,7 @@ struct SplitItem {
   int seq, q0, c, len;        // sequence, its first row, new tokens, cached positions
   int tile, group;            // token tile, head group
   int split, n_split;         // this item's run of keys, and how many
-  int u0, u1;                 // its units of keys
+  int units, u0, u1;          // the sequence's units of keys; this item's
   int slot0;                  // slot of the tile's first split
 };
 
@@ -154,6 +156,7 @@ __device__ __forceinline__ bool split_find(const ChunkCall& a, const SplitPlan& 
       it.len = __shfl_sync(0xffffffffu, len, src);
       it.n_split = __shfl_sync(0xffffffffu, ns, src);
       const int un = __shfl_sync(0xffffffffu, units, src), nt = __shfl_sync(0xffffffffu, tiles, src);
+      it.units = un;
       it.split = 0;
       if (!joined) {
         const int k = r / it.n_split;
@@ -175,6 +178,20 @@ __device__ __forceinline__ bool split_find(const ChunkCall& a, const SplitPlan& 
   }
   return false;
 }
+// Sets a kernel's dynamic shared memory, once per device (Tag: a type of the kernel's own).
+template <typename Tag, typename K>
+inline cudaError_t smem_once(K* kernel, int bytes) {
+  static std::atomic<unsigned long long> done{0};   // bit per device
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  const unsigned long long bit = dev < 64 ? 1ull << dev : 0;
+  if (bit && (done.load() & bit)) return cudaSuccess;
+  e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e == cudaSuccess) done.fetch_or(bit);
+  return e;
+}
+
 // Items there can be at most: the target, or one per tile where there are more tiles.
 static inline long long split_items(const SplitPlan& p, int n_seq, int n_rows, int max_q) {
   const long long by_seq = (long long)n_seq * ((max_q + p.tq - 1) / p.tq);
