@@ -329,7 +329,10 @@ __global__ void __launch_bounds__(CF_WARPS * 32, 3) chunk_few_kernel(const __gri
   }
   if (tid == 0) s_abort = 0;
   const long long wlim = wait_limit();
-  PDL_ENTRY();
+  KT_BEGIN();
+  if (!a.late) pdl_wait();
+  KT_WAITED();
+  pdl_launch_dependents();
   const int rank = cs > 1 ? (int)blockIdx.x % cs : 0;
   if (warp == 0) {
     SplitItem it;
@@ -347,7 +350,10 @@ __global__ void __launch_bounds__(CF_WARPS * 32, 3) chunk_few_kernel(const __gri
     }
   }
   __syncthreads();
-  if (!s_have) return;   // (all CTAs of a cluster)
+  if (!s_have) {   // (all CTAs of a cluster)
+    if (a.late) pdl_wait();
+    return;
+  }
   const SplitItem it = s_it;
   const int group = a.n_heads / a.c.n_kv_heads, kvh = it.group / sub, g0 = it.group % sub * per_tok;
   const int j0 = it.tile * p.tq, n = min(p.tq, it.c - j0);
@@ -731,6 +737,7 @@ __global__ void __launch_bounds__(CF_WARPS * 32, 3) chunk_few_kernel(const __gri
     }
     cluster_sync();   // (a CTA's shared memory stays until all have read it)
   }
+  if (a.late) pdl_wait();
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -767,8 +774,8 @@ __global__ void __launch_bounds__(CJ_THREADS) chunk_join_kernel(const __grid_con
   __shared__ SplitItem s_it;
   __shared__ int s_have;
   __shared__ float s_acc[6][CJ_THREADS];
-  // The look-up runs beside the partials' kernel: it reads the lengths only, which that kernel has waited for before it let
-  // this one start.
+  // The look-up runs beside the partials' kernel: it reads the lengths only, which that kernel, or the one before it, has
+  // waited for before it let its follower start.
   const int tid = threadIdx.x;
   if (tid < 32) {
     SplitItem it;
@@ -972,18 +979,26 @@ cudaError_t launch_chunk_attention(cudaStream_t st, const ChunkCall& a0, int* la
   ChunkCall a = a0;
   a.c_lo = 1;
   a.c_hi = a.max_q;
+  a.late = 0;
   *launches = 0;
   const bool aligned = (((uintptr_t)a.q | (uintptr_t)a.out) & 15) == 0 && a.ld_q % 8 == 0 && a.ld_out % 8 == 0;
   if (!use_tc(a.c, a.n_heads, a.max_q, a.max_kv, aligned)) return chunk_simple(st, a, aligned, launches);
+  if (a.c.type != KV_E4M3) return launch_chunk_tc(st, a, launches);
+  ChunkCall t = a;   // the tcgen05 kernel's share
   if (use_both(a.c)) {
     a.c_hi = few_tokens(a.c, a.n_heads);
-    const cudaError_t e = chunk_simple(st, a, aligned, launches);
-    if (e != cudaSuccess) return e;
-    a.c_lo = a.c_hi + 1;
-    a.c_hi = a.max_q;
-    a.part = (float*)((char*)a.part + round256(how_bytes(chunk_how(a.c, a.n_heads, a.max_kv, true), a.c)));
+    t.c_lo = a.c_hi + 1;
+    t.part = (float*)((char*)a.part + round256(how_bytes(chunk_how(a.c, a.n_heads, a.max_kv, true), a.c)));
   }
-  return launch_chunk_tc(st, a, launches);
+  cudaError_t e = launch_chunk_widen(st, t, launches);
+  // The few-row kernel needs nothing of the widening: it fills the SMs as that leaves them (late).  Its join waits for both,
+  // then lets the tcgen05 kernel start, which so needs not wait for the join in turn.
+  if (use_both(a.c) && e == cudaSuccess) {
+    a.late = 1;
+    e = chunk_simple(st, a, aligned, launches);
+    t.late = *launches == 3;   // (there is a join)
+  }
+  return e == cudaSuccess ? launch_chunk_tc(st, t, launches) : e;
 }
 
 ADEPT_WAIT_LIMIT_SETTER(cf)

@@ -25,6 +25,9 @@ size_t ct_wide_bytes(const KvPaged& c, int max_kv) {   // of K, or of V
   return c.type == KV_E4M3 ? (size_t)c.n_seq * cdiv(max_kv, 16) * c.n_kv_heads * 16 * c.head_dim * 2 : 0;
 }
 
+void* wide_k(const ChunkCall& a) { return (char*)a.part + ct_parts_bytes(a.c.head_dim); }
+void* wide_v(const ChunkCall& a) { return (char*)wide_k(a) + ct_wide_bytes(a.c, a.max_kv); }
+
 template <int DH>
 cudaError_t launch_t(cudaStream_t st, CtParams& p, int* launches) {
   constexpr int smem = CtShape<DH>::TOTAL + 1024;
@@ -36,11 +39,8 @@ cudaError_t launch_t(cudaStream_t st, CtParams& p, int* launches) {
   if (c.type == KV_E4M3) {
     p.wide = cdiv(p.a.max_kv, 16);
     rows = (uint64_t)c.n_seq * p.wide * c.n_kv_heads * 16;
-    k = (char*)p.a.part + ct_parts_bytes(DH);
-    v = (char*)k + ct_wide_bytes(c, p.a.max_kv);
-    e = launch_k(chunk_widen_kernel<DH>, dim3((unsigned)std::min<long long>(ct_sms() * 8, 2ll * p.wide * c.n_seq)), dim3(CW_THREADS), 0, st, p, (bf16*)k, (bf16*)v);
-    if (e != cudaSuccess) return e;
-    ++*launches;
+    k = wide_k(p.a);
+    v = wide_v(p.a);
   }
   const uint64_t kv_dims[2] = {DH, rows}, kv_strides[1] = {DH * 2};
   const uint64_t q_dims[3] = {DH, (uint64_t)p.a.n_heads, (uint64_t)p.a.n_rows}, q_strides[2] = {DH * 2, (uint64_t)p.a.ld_q * 2};
@@ -68,6 +68,14 @@ bool chunk_tc_fits(const KvPaged& c, int n_heads, int n_rows, int max_q, int max
   const long long tq = 2 * (CT_BM / (n_heads / c.n_kv_heads));
   const long long tiles = std::min(c.n_seq * ((max_q + tq - 1) / tq), n_rows / tq + c.n_seq);
   return tiles * c.n_kv_heads * (CT_TILE + cdiv(max_kv, CT_BN)) < (1ll << 31);
+}
+
+cudaError_t launch_chunk_widen(cudaStream_t st, const ChunkCall& a, int* launches) {
+  const int wide = cdiv(a.max_kv, 16);
+  const dim3 grid((unsigned)std::min<long long>(ct_sms() * 8, 2ll * wide * a.c.n_seq));
+  ++*launches;
+  return launch_k(a.c.head_dim == 128 ? chunk_widen_kernel<128> : chunk_widen_kernel<64>, grid, dim3(CW_THREADS), 0, st, a, wide,
+                  (bf16*)wide_k(a), (bf16*)wide_v(a));
 }
 
 cudaError_t launch_chunk_tc(cudaStream_t st, const ChunkCall& a, int* launches) {

@@ -335,7 +335,7 @@ __global__ void __launch_bounds__(CtShape<DH>::THREADS, 1) chunk_tc_kernel(const
     s_tok[tid] = tk < ts ? (tid >> 7) * ts + tk : -1;
     s_off[tid] = rr % group * DH;
   }
-  pdl_wait();
+  if (!a.late) pdl_wait();
   if (warp == 9 || warp == 10) {   // where the run begins, where it ends
     const int tot = ct_total(a, tq), runs = ct_runs(tot, p.runs), i = min(run + warp - 9, runs);
     CtTile x{};
@@ -706,17 +706,18 @@ __global__ void __launch_bounds__(CtShape<DH>::THREADS, 1) chunk_tc_kernel(const
   __syncthreads();
   tc_fence_after();
   if (warp == 8) tmem_dealloc(tmem, 512);
+  if (a.late) pdl_wait();
 }
 
 // Entries of 8 bits as bf16.  Work: the blocks of positions of this launch's sequences, K and V apart, all heads of one at a time;
 // CTA i of n takes the i-th of n equal runs of them (the lengths are known on the device only).
 constexpr int CW_THREADS = 256;
 template <int DH>
-__global__ void __launch_bounds__(CW_THREADS) chunk_widen_kernel(const __grid_constant__ CtParams p, bf16* k_out, bf16* v_out) {
+__global__ void __launch_bounds__(CW_THREADS) chunk_widen_kernel(const __grid_constant__ ChunkCall a, int wide, bf16* k_out,
+                                                                 bf16* v_out) {
   PDL_ENTRY();
   __shared__ int s_seq, s_blk, s_len;
   __shared__ long long s_u0, s_u1;
-  const ChunkCall& a = p.a;
   const int lane = threadIdx.x & 31;
   if (threadIdx.x < 32) {
     long long tot = 0;
@@ -760,7 +761,7 @@ __global__ void __launch_bounds__(CW_THREADS) chunk_widen_kernel(const __grid_co
   for (long long u = s_u0; u < s_u1; ++u) {
     const int blk = a.c.table[(size_t)seq * a.c.max_blocks + b], is_v = (int)(u & 1);
     if (blk >= 0 && blk < a.c.n_blocks) {
-      const size_t from = (size_t)blk * a.c.n_kv_heads * 16, to = ((size_t)seq * p.wide + b) * a.c.n_kv_heads * 16;
+      const size_t from = (size_t)blk * a.c.n_kv_heads * 16, to = ((size_t)seq * wide + b) * a.c.n_kv_heads * 16;
       const uint8_t* codes = (const uint8_t*)(is_v ? a.c.v : a.c.k) + from * DH;
       const uint8_t* exps = (is_v ? a.c.v_exp : a.c.k_exp) + from;
       bf16* out = (is_v ? v_out : k_out) + to * DH;

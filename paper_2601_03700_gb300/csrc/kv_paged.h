@@ -48,6 +48,7 @@ struct ChunkCall {
   const int* row_pos;   // position per row, ascending within a sequence (NULL: the last ones)
   int n_rows, n_heads, max_q, max_kv;
   int c_lo, c_hi;     // the launch's sequences: those with c_lo to c_hi new tokens
+  int late;           // the launch needs nothing of the one before it: it waits for that at its end, for those behind it
   float scale_log2;   // log2(e) / sqrt(head_dim)
   float* part;        // workspace
 };
@@ -58,6 +59,8 @@ bool chunk_tc_takes(const KvPaged& c, int n_heads, int max_kv);
 size_t chunk_tc_workspace(const KvPaged& c, int max_kv);
 // Whether a call's (tile, KV head, key tile) triples fit 31 bits (hours of work otherwise).
 bool chunk_tc_fits(const KvPaged& c, int n_heads, int n_rows, int max_q, int max_kv);
+// (the widening of 8-bit entries to bf16 in the workspace, which goes first, is a launch of its own)
+cudaError_t launch_chunk_widen(cudaStream_t st, const ChunkCall& a, int* launches);
 cudaError_t launch_chunk_tc(cudaStream_t st, const ChunkCall& a, int* launches);
 cudaError_t set_wait_limit_ct(long long cycles);
 cudaError_t set_wait_limit_cf(long long cycles);
