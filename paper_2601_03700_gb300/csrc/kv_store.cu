@@ -7,8 +7,11 @@
 // scale.  NaN stays NaN; e4m3 has no infinity, an infinite element is stored as NaN.
 //
 // Bound by HBM: each element is read once and written once.  A thread holds 16 elements of a vector (head_dim elements of K or of
-// V of one position), KS_ITEMS vectors at a time with every load issued before the first is used; a CTA takes whole rows, so
-// a row's place in the cache is looked up by neighbours together.
+// V of one position), two vectors at a time with every load issued before the first is used.  A CTA takes whole rows, or a
+// part of one where there are few.  What hides the look-ups (row -> position -> block -> entry, one load behind the other) is
+// many small CTAs at different stages of that: 3 x 30011 rows of 32 heads of 128 from 8 bits to bf16 (738 MB) took 143 us with
+// 256 threads of four vectors, 137 with 256 of two, 125 with 128 of two (5.9 TB/s), 127 with 128 of one, 123 with 64 of two (which
+// writes 2048 rows in 41 us where 128 threads take 37).
 #include "kv_paged.h"
 
 #include <cuda_fp8.h>
@@ -18,7 +21,7 @@
 namespace adept {
 namespace {
 
-constexpr int KS_THREADS = 256, KS_ITEMS = 4, KS_EL = 16;
+constexpr int KS_THREADS = 128, KS_ITEMS = 2, KS_EL = 16;
 
 // 16 elements as they lie in memory (VEC: by 16 bytes), and as fp32.
 template <typename T>
@@ -140,7 +143,8 @@ __global__ void __launch_bounds__(KS_THREADS) kv_append_kernel(KvPaged c, int n_
   constexpr int TPV = DH / KS_EL;   // threads of a vector: neighbours
   const int hk = c.n_kv_heads, per_row = 2 * hk * TPV, row0 = (int)blockIdx.x * rows_cta;
   const int total = min(rows_cta, n_rows - row0) * per_row;
-  for (int i0 = 0; i0 < total; i0 += KS_THREADS * KS_ITEMS) {
+  constexpr int PASS = KS_THREADS * KS_ITEMS;
+  for (int i0 = (int)blockIdx.z * PASS; i0 < total; i0 += (int)gridDim.z * PASS) {
     Piece<T> x[KS_ITEMS];
     long long e[KS_ITEMS];   // the vector's entry, -1: not written
 #pragma unroll
@@ -181,7 +185,7 @@ __global__ void __launch_bounds__(KS_THREADS) kv_requant_kernel(KVCacheView src,
   const int hk = c.n_kv_heads, per_row = 2 * hk * TPV, row0 = (int)blockIdx.x * rows_cta;
   const int total = min(rows_cta, n - row0) * per_row;
   const long long layer = (long long)y * c.n_blocks * hk * c.block_tokens;   // entries
-  for (int i0 = 0; i0 < total; i0 += KS_THREADS) {
+  for (int i0 = (int)blockIdx.z * KS_THREADS; i0 < total; i0 += (int)gridDim.z * KS_THREADS) {
     const int i = i0 + (int)threadIdx.x;
     const Item<DH> it(min(i, total - 1), hk, per_row);
     const int tok = row_tok ? row_tok[row0 + it.r] : row0 + it.r, seq = tok_seq[tok], pos = tok_pos[tok];
@@ -207,7 +211,8 @@ __global__ void __launch_bounds__(KS_THREADS) kv_gather_kernel(KvPaged c, int n_
   const int hk = c.n_kv_heads, per_row = 2 * hk * TPV, row0 = (int)blockIdx.x * rows_cta;
   const int total = min(rows_cta, n_rows - row0) * per_row;
   using C = typename std::conditional<KT == KV_F32, float, bf16>::type;
-  for (int i0 = 0; i0 < total; i0 += KS_THREADS * KS_ITEMS) {
+  constexpr int PASS = KS_THREADS * KS_ITEMS;
+  for (int i0 = (int)blockIdx.z * PASS; i0 < total; i0 += (int)gridDim.z * PASS) {
     Piece<C> x[KS_ITEMS];   // (e4m3: 16 codes in the first four words)
     int ex[KS_ITEMS];
     bool on[KS_ITEMS];
@@ -255,18 +260,20 @@ __global__ void __launch_bounds__(KS_THREADS) kv_gather_kernel(KvPaged c, int n_
   }
 }
 
-// Rows of a CTA: one pass of all its threads, where there are rows enough for two CTAs an SM; else fewer (a step's 8 rows of 32
-// heads: one each).
-int ks_rows(const KvPaged& c, int n_rows) {
+// Rows of a CTA: one pass of all its threads, at least one row, where there are rows enough for two CTAs an SM.  Where there are
+// not, the passes of a row that is longer than one get a CTA each (z): 8 rows of 32 heads of 128 written and read back took 5.5 us
+// by 16 CTAs, 8.2 by 8; 30000 rows 285 us by a CTA a row, 304 by two.
+int ks_rows(const KvPaged& c, int n_rows, int pass, int* z) {
   static const int sms = [] {
     int dev = 0, n = 0;
     cudaGetDevice(&dev);
     cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev);
     return n > 0 ? n : 1;
   }();
-  const int per_row = 2 * c.n_kv_heads * (c.head_dim / KS_EL), full = KS_THREADS * KS_ITEMS / per_row;
+  const int per_row = 2 * c.n_kv_heads * (c.head_dim / KS_EL), full = pass / per_row;
   const int spread = n_rows / (2 * sms);
   const int r = full < spread ? full : spread;
+  *z = spread < 1 ? cdiv(per_row, pass) : 1;
   return r > 1 ? r : 1;
 }
 
@@ -278,15 +285,17 @@ template <int DH, typename T, int KT>
 cudaError_t append_t(cudaStream_t st, const KvPaged& c, int n, const void* k, long long ld_k, const void* v, long long ld_v,
                      const int* seq, const int* pos) {
   auto kern = rows_aligned(k, ld_k, v, ld_v, (int)sizeof(T)) ? kv_append_kernel<DH, T, KT, true> : kv_append_kernel<DH, T, KT, false>;
-  const int rows = ks_rows(c, n);
-  return launch_k(kern, dim3((unsigned)cdiv(n, rows)), dim3(KS_THREADS), 0, st, c, n, rows, (const T*)k, ld_k, (const T*)v, ld_v, seq, pos);
+  int z;
+  const int rows = ks_rows(c, n, KS_THREADS * KS_ITEMS, &z);
+  return launch_k(kern, dim3((unsigned)cdiv(n, rows), 1, (unsigned)z), dim3(KS_THREADS), 0, st, c, n, rows, (const T*)k, ld_k, (const T*)v, ld_v, seq, pos);
 }
 template <int DH, typename T, int KT>
 cudaError_t gather_t(cudaStream_t st, const KvPaged& c, int n, void* k, long long ld_k, void* v, long long ld_v, const int* seq,
                      const int* pos, int seq0, int pos0) {
   auto kern = rows_aligned(k, ld_k, v, ld_v, (int)sizeof(T)) ? kv_gather_kernel<DH, T, KT, true> : kv_gather_kernel<DH, T, KT, false>;
-  const int rows = ks_rows(c, n);
-  return launch_k(kern, dim3((unsigned)cdiv(n, rows)), dim3(KS_THREADS), 0, st, c, n, rows, (T*)k, ld_k, (T*)v, ld_v, seq, pos, seq0, pos0);
+  int z;
+  const int rows = ks_rows(c, n, KS_THREADS * KS_ITEMS, &z);
+  return launch_k(kern, dim3((unsigned)cdiv(n, rows), 1, (unsigned)z), dim3(KS_THREADS), 0, st, c, n, rows, (T*)k, ld_k, (T*)v, ld_v, seq, pos, seq0, pos0);
 }
 
 #define KS_DISPATCH(F, BF, ...)                                                                   \
@@ -327,8 +336,9 @@ cudaError_t launch_kv_gather(cudaStream_t st, const KvPaged& c, int n_rows, int 
 cudaError_t launch_kv_requant(cudaStream_t st, const KVCacheView& src, int src_layer0, const KvPaged& c, int n_layers,
                               const int* n_rows, int max_rows, const int* row_tok, const int* tok_seq, const int* tok_pos) {
   auto kern = c.head_dim == 128 ? kv_requant_kernel<128> : c.head_dim == 64 ? kv_requant_kernel<64> : kv_requant_kernel<32>;
-  const int rows = ks_rows(c, max_rows);
-  return launch_k(kern, dim3((unsigned)cdiv(max_rows, rows), (unsigned)n_layers), dim3(KS_THREADS), 0, st, src, src_layer0, c, n_rows,
+  int z;
+  const int rows = ks_rows(c, max_rows, KS_THREADS, &z);
+  return launch_k(kern, dim3((unsigned)cdiv(max_rows, rows), (unsigned)n_layers, (unsigned)z), dim3(KS_THREADS), 0, st, src, src_layer0, c, n_rows,
                   max_rows, rows, row_tok, tok_seq, tok_pos);
 }
 
