@@ -13,7 +13,7 @@
 #include "kv_paged.h"
 #include "tc_ptx.cuh"
 
-#include <cuda_fp8.h>
+#include <cuda_fp16.h>
 
 #include <algorithm>
 
@@ -34,10 +34,6 @@ __device__ __forceinline__ float kv_elem(const void* p, size_t i) {
   else if constexpr (KT == KV_BF16) return __bfloat162float(((const bf16*)p)[i]);
   else return __half2float(__half(__nv_cvt_fp8_to_halfraw(((const uint8_t*)p)[i], __NV_E4M3)));
 }
-__device__ __forceinline__ float exp_scale(int b) {   // 2^(b - 127)
-  return b ? __uint_as_float((unsigned)b << 23) : __uint_as_float(0x400000u);
-}
-
 // Part buffers of slot s: `rows` rows of (m, l) at part, of DH sums behind all the (m, l).
 struct PartView {
   float* ml;
@@ -226,18 +222,14 @@ __device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], 
         : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-// Two e4m3 codes (low 16 bits) as two fp16, as two bf16: exact, NaN stays NaN.
-__device__ __forceinline__ uint32_t e4m3x2_f16x2(uint32_t codes) {
-  const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)codes, __NV_E4M3);
-  return (uint32_t)h.x | (uint32_t)h.y << 16;
-}
 __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
   const __nv_bfloat162 x = __floats2bfloat162_rn(a, b);
   return *reinterpret_cast<const uint32_t*>(&x);
 }
+// Two e4m3 codes (low 16 bits) as two bf16: exact, NaN stays NaN.
 __device__ __forceinline__ uint32_t e4m3x2_bf16x2(uint32_t codes) {
-  const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)codes, __NV_E4M3);
-  const float2 f = __half22float2(__half2(h));
+  const uint32_t h = e4m3x2_f16x2(codes);
+  const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h));
   return pack_bf16(f.x, f.y);
 }
 __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {

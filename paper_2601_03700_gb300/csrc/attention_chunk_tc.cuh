@@ -29,7 +29,7 @@
 #include "kv_paged.h"
 #include "tc_ptx.cuh"
 
-#include <cuda_fp8.h>
+#include <cuda_fp16.h>
 
 namespace adept {
 namespace {
@@ -769,13 +769,13 @@ __global__ void __launch_bounds__(CW_THREADS) chunk_widen_kernel(const __grid_co
       for (int i = threadIdx.x; i < n; i += CW_THREADS) {
         const uint4 w = reinterpret_cast<const uint4*>(codes)[i];
         const int e = exps[i / (DH / 16)];
-        const float s = e ? __uint_as_float((unsigned)e << 23) : __uint_as_float(0x400000u);   // 2^(e - 127)
+        const float s = exp_scale(e);
         const uint32_t x[4] = {w.x, w.y, w.z, w.w};
         uint32_t y[8];
 #pragma unroll
         for (int q = 0; q < 8; ++q) {
-          const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(x[q >> 1] >> (q & 1 ? 16 : 0)), __NV_E4M3);
-          const float2 f = __half22float2(__half2(h));
+          const uint32_t h = e4m3x2_f16x2(x[q >> 1] >> (q & 1 ? 16 : 0));
+          const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h));
           const __nv_bfloat162 r = __floats2bfloat162_rn(f.x * s, f.y * s);
           y[q] = *reinterpret_cast<const uint32_t*>(&r);
         }

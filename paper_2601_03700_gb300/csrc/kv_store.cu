@@ -241,12 +241,11 @@ __global__ void __launch_bounds__(KS_THREADS) kv_gather_kernel(KvPaged c, int n_
       const long long r = row0 + it.r;
       float y[KS_EL];
       if constexpr (KT == KV_E4M3) {
-        // 2^e with e down to -127 (a byte of 0 is the subnormal 2^-127)
-        const float s = ex[q] ? __uint_as_float((unsigned)ex[q] << 23) : __uint_as_float(0x400000u);
+        const float s = exp_scale(ex[q]);
 #pragma unroll
         for (int j = 0; j < KS_EL / 2; ++j) {
-          const __half2_raw hr = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(x[q].w[j >> 1] >> (j & 1 ? 16 : 0)), __NV_E4M3);
-          const float2 f = __half22float2(__half2(hr));
+          const uint32_t h = e4m3x2_f16x2(x[q].w[j >> 1] >> (j & 1 ? 16 : 0));
+          const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h));
           y[2 * j] = f.x * s;
           y[2 * j + 1] = f.y * s;
         }
