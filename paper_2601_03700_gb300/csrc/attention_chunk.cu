@@ -13,7 +13,7 @@
 #include "kv_paged.h"
 #include "tc_ptx.cuh"
 
-#include <cuda_fp16.h>
+#include <cuda_fp8.h>
 
 #include <algorithm>
 
