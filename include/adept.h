@@ -161,8 +161,10 @@ ADEPT_API adept_status adept_decode_step(adept_model* m, int batch, const int32_
  * a prompt in one call or in pieces gives the same states, exits and cache up to rounding).
  * d_logits_out, d_next_token_out: row b is sequence b's last new token; rows of sequences without new
  * tokens are not written.  Decoder families only; not with ADEPT_OPT_ALL_AT_ONCE.
- * The first call allocates its workspace (outside any capture).
- * Errors: INVALID_ARG (NULL pointers, a negative length, no token, a sequence not reserved), CAPACITY
+ * The first call allocates its workspace.  The lengths come from the host: the call cannot be captured
+ * into a graph (nor adept_prefill of a model with an 8-bit cache).
+ * Errors: INVALID_ARG (NULL pointers, a negative length, no token, a sequence not reserved, a stream in
+ * capture), CAPACITY
  * (batch > max_batch, a sequence beyond max_seq, more tokens than the pass workspace), OOM. */
 ADEPT_API adept_status adept_extend(adept_model* m, int batch, const int32_t* h_lens, const int32_t* d_tokens, float delta,
                           const int32_t* d_forced_exit, int32_t* d_exit_layer_out, float* d_logits_out,

@@ -1836,6 +1836,15 @@ static adept_status extend_init(adept_model* m) {
   return dalloc(m, (void**)&m->ext_ws, std::max<size_t>(ws, 16));
 }
 
+// The chunks of a pass come from the host: a replayed graph would read them again, stale.
+static adept_status no_capture(adept_model* m, cudaStream_t st) {
+  cudaStreamCaptureStatus s = cudaStreamCaptureStatusNone;
+  const cudaError_t e = cudaStreamIsCapturing(st, &s);
+  if (e == cudaSuccess && s == cudaStreamCaptureStatusNone) return ADEPT_OK;
+  if (e != cudaSuccess) cudaGetLastError();
+  return fail(m, ADEPT_ERR_INVALID_ARG, "a pass of chunks cannot be captured into a graph");
+}
+
 // The chunks of a pass to the device: first token per sequence and the count, then the lengths before it.
 static adept_status put_chunks(adept_model* m, int batch, const int32_t* lens, const int* before, cudaStream_t st) {
   m->h_ext.assign((size_t)2 * batch + 1, 0);
@@ -1954,6 +1963,7 @@ adept_status adept_prefill(adept_model* m, int batch, int prompt_len, const int3
   TRY(check_cross_set(m, batch));
   cudaStream_t st = (cudaStream_t)stream;
   std::vector<int> lens(batch, prompt_len);
+  if (m->kv8) TRY(no_capture(m, st));
   TRY(reserve_seqs(m, batch, lens.data(), st));
   launch_set_float(st, m->d_delta, delta);
   m->launches += 1;
@@ -1999,8 +2009,9 @@ adept_status adept_extend(adept_model* m, int batch, const int32_t* h_lens, cons
   if (total < 1) return fail(m, ADEPT_ERR_INVALID_ARG, "no sequence has a new token");
   if (total > m->T_max)
     return fail(m, ADEPT_ERR_CAPACITY, "%lld new tokens above the pass workspace (%d rows)", total, m->T_max);
-  TRY(extend_init(m));
   cudaStream_t st = (cudaStream_t)stream;
+  TRY(no_capture(m, st));
+  TRY(extend_init(m));
   for (int b = 0; b < batch; ++b) e.max_kv = std::max(e.max_kv, m->h_seq_len[b]);   // (sequences without new tokens too)
   TRY(put_chunks(m, batch, h_lens, m->h_seq_len.data(), st));
   launch_set_float(st, m->d_delta, delta);

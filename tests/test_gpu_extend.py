@@ -199,3 +199,28 @@ def test_refusals_leave_the_model_as_it_was():
         adept.adept_extend(e.h, [1], t, 0.9)
     e.close()
     m.close()
+
+
+@pytest.mark.parametrize("kv", [None, "e4m3"])
+def test_a_stream_in_capture_is_refused(kv):
+    """The chunks' lengths come from the host: a replay would read them again."""
+    cfg = synth.ModelConfig(max_batch=2, max_seq=64, **CONFIGS["llama_gqa"])
+    if kv:
+        cfg.kv_type = kv
+    m = adept.Model(cfg, synth.make_weights(cfg, seed=32))
+    t = synth.make_tokens(33, 2, 10, cfg.vocab).cuda()
+    m.prefill(t, 9.0)
+    before = m.extend([3, 1], t.view(-1)[:4], 9.0)[1].clone()
+    m.prefill(t, 9.0)
+    x = torch.zeros(1, device="cuda")
+    torch.cuda.synchronize()
+    with torch.cuda.graph(torch.cuda.CUDAGraph()):
+        x += 1
+        with pytest.raises(adept.AdeptError, match="captured"):
+            adept.adept_extend(m.h, [3, 1], t.view(-1)[:4], 9.0)
+        if kv:
+            with pytest.raises(adept.AdeptError, match="captured"):
+                adept.adept_prefill(m.h, 2, 10, t.view(-1), 9.0)
+    assert torch.equal(m.extend([3, 1], t.view(-1)[:4], 9.0)[1], before)   # and nothing has moved
+    m.check()
+    m.close()
