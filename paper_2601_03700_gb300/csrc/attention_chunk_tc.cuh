@@ -60,7 +60,7 @@ struct CtParams {
 
 // ---- the key tiles of all tiles in a row ----
 
-// (Units fit 31 bits: the launcher refuses calls beyond.)
+// (Units fit 31 bits: the launcher refuses calls beyond, ct_total sequences that share rows.)
 // sum over i in [0, n) of floor((a i + b) / m); the sum, and a n + b, below 2^32
 __device__ unsigned floor_sum(unsigned n, unsigned m, unsigned a, unsigned b) {
   unsigned r = 0;
@@ -112,15 +112,21 @@ __device__ __forceinline__ int warp_scan(int v) {
   }
   return v;
 }
-// All units, taken together by a converged warp.
+// All units, taken together by a converged warp.  More than 31 bits hold, which takes row ranges that overlap: no work, flagged.
 __device__ int ct_total(const ChunkCall& a, int tq) {
-  int tot = 0;
+  long long tot = 0;
   for (int b = threadIdx.x & 31; b < a.c.n_seq; b += 32) {
     int q0, c, len;
     chunk_seq(a, b, q0, c, len);
     tot += ct_seq_units(a.row_pos, c, len, tq) * a.c.n_kv_heads;
   }
-  return (int)__reduce_add_sync(0xffffffffu, (unsigned)tot);
+  const long long hi = __reduce_add_sync(0xffffffffu, (unsigned)(tot >> 24));
+  tot = (hi << 24) + __reduce_add_sync(0xffffffffu, (unsigned)tot & 0xffffffu);
+  if (tot >> 31) {
+    a.c.flag(ERRW_POS);
+    return 0;
+  }
+  return (int)tot;
 }
 // The tile that unit u lies in.
 __device__ void ct_find(const ChunkCall& a, int tq, int u, CtTile& x) {

@@ -270,6 +270,22 @@ def test_inputs_out_of_range_are_flagged_and_left_out():
 
 # ---- writing and reading back ---------------------------------------------------------------
 
+def test_sequences_that_share_rows_beyond_any_count():
+    """Row ranges that go up and down (flagged) over and over: 4000 times 8192 rows at 8192 positions of 512 heads are 2^32 pairs of
+    tiles, though the call's 8192 rows are not; nothing is done."""
+    n, c = 8000, 8192
+    cache = adept.KVCache(1, 512, 64, n, c // 16)
+    cache.block_table.zero_()
+    start = torch.zeros(n + 1, dtype=torch.int32, device="cuda")
+    start[1::2] = c
+    q = torch.ones(c, 512, 64, dtype=torch.bfloat16, device="cuda")
+    out = torch.full_like(q, 7)
+    adept.adept_chunk_attention(cache, q, start, torch.full((n,), c, dtype=torch.int32, device="cuda"), c, c, out)
+    with pytest.raises(adept.AdeptError):
+        cache.check()
+    assert (out == 7).all()
+
+
 @pytest.mark.parametrize("src", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("dtype", ["f32", "bf16", "e4m3"])
 @pytest.mark.parametrize("hk,dh", [(3, 32), (5, 64), (1, 128), (2, 128)])
