@@ -129,6 +129,24 @@ def test_attention_of_longer_chunks(dtype, heads, hk, dh, new, past):
     assert torch.equal(out, attend(c, q, starts, lens)), "the same call gave other bits"
 
 
+@pytest.mark.parametrize("heads,hk,dh,new,past", [
+    (16, 4, 128, [1, 200, 3, 0, 17], [4600, 300, 90, 8, 0]),   # the few rows' keys split over the GPU, joined beside the longer chunks'
+    (4, 4, 64, [40, 1, 1], [60, 2300, 0]),
+    (16, 4, 128, [1, 200, 3], [700, 300, 90]),                 # over clusters
+    (16, 4, 128, [1, 2, 30], [3, 90, 50]),                     # not split
+    (16, 4, 128, [200, 300], [4600, 10]),                      # no sequence of few
+])
+def test_few_and_many_tokens_over_8_bit_entries(heads, hk, dh, new, past):
+    lens = [a + b for a, b in zip(new, past)]
+    c = make_cache("e4m3", hk, dh, lens, 7)
+    q, starts = make_q("bf16", new, heads, dh, 8, extra=2)
+    ws = c.attention_workspace(heads, q.shape[0], max(new), max(lens))
+    outs = [attend(c, q, starts, lens, workspace=ws) for _ in range(6)]
+    c.check()
+    assert_attention(c, q, starts, lens, outs[0])
+    assert all(torch.equal(outs[0], o) for o in outs)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "e4m3"])
 @pytest.mark.parametrize("bt", [1, 8, 48])
 def test_attention_over_other_block_sizes(dtype, bt):
