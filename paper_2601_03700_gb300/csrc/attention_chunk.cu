@@ -22,17 +22,26 @@ namespace {
 
 // ---------------------------------------------------------------------------------------------
 // Any type, head size, alignment and block size: CUDA-core kernel.  CTA = up to CG_ROWS new tokens of one query head x a
-// run of keys, 128 keys at a time: a thread per key for the scores, a warp per token for the softmax, a thread per
-// dimension for the weighted sum.
+// run of keys, 128 keys at a time: a thread per key for the scores, a warp per token for the softmax, for the weighted sum a
+// thread per four dimensions of every KG-th key.  Such calls are short and bound by latency, one load behind the other, so
+// all loads are of four elements, several under way.
 // ---------------------------------------------------------------------------------------------
 constexpr int CG_ROWS = 4, CG_KEYS = 128;
 
-// Element i of entry `e` of K or V as fp32; e4m3 codes without their exponent.
+// Elements i .. i + 3 of K or V as fp32; e4m3 codes without their exponent.
 template <int KT>
-__device__ __forceinline__ float kv_elem(const void* p, size_t i) {
-  if constexpr (KT == KV_F32) return ((const float*)p)[i];
-  else if constexpr (KT == KV_BF16) return __bfloat162float(((const bf16*)p)[i]);
-  else return __half2float(__half(__nv_cvt_fp8_to_halfraw(((const uint8_t*)p)[i], __NV_E4M3)));
+__device__ __forceinline__ float4 kv_four(const void* p, size_t i) {
+  if constexpr (KT == KV_F32) {
+    return *reinterpret_cast<const float4*>((const float*)p + i);
+  } else if constexpr (KT == KV_BF16) {
+    const uint2 w = *reinterpret_cast<const uint2*>((const bf16*)p + i);
+    return make_float4(__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xffff0000u), __uint_as_float(w.y << 16),
+                       __uint_as_float(w.y & 0xffff0000u));
+  } else {
+    const uint32_t w = *reinterpret_cast<const uint32_t*>((const uint8_t*)p + i), h0 = e4m3x2_f16x2(w), h1 = e4m3x2_f16x2(w >> 16);
+    const float2 x = __half22float2(*reinterpret_cast<const __half2*>(&h0)), y = __half22float2(*reinterpret_cast<const __half2*>(&h1));
+    return make_float4(x.x, x.y, y.x, y.y);
+  }
 }
 // Part buffers of slot s: `rows` rows of (m, l) at part, of DH sums behind all the (m, l).
 struct PartView {
@@ -46,11 +55,12 @@ template <int DH, int KT, typename T>
 __global__ void __launch_bounds__(CG_KEYS) chunk_any_kernel(const __grid_constant__ ChunkCall a, const __grid_constant__ SplitPlan p) {
   __shared__ SplitItem s_it;
   __shared__ int s_have;
-  __shared__ float s_q[CG_ROWS][DH];
+  constexpr int QD = DH / 4, KG = CG_KEYS / QD;   // fours of dimensions; key groups of the weighted sum
+  __shared__ __align__(16) float s_q[CG_ROWS][DH];
   __shared__ float s_p[CG_ROWS][CG_KEYS];
   __shared__ long long s_e[CG_KEYS];
   __shared__ float s_vs[CG_KEYS], s_corr[CG_ROWS];
-  __shared__ float s_red[CG_KEYS];
+  __shared__ __align__(16) float s_red[KG][CG_ROWS][DH];
   PDL_ENTRY();
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if (warp == 0) {
@@ -72,11 +82,10 @@ __global__ void __launch_bounds__(CG_KEYS) chunk_any_kernel(const __grid_constan
   for (int i = tid; i < n * DH; i += CG_KEYS)
     s_q[i / DH][i % DH] = to_f<T>(((const T*)a.q)[(size_t)(it.q0 + j0 + i / DH) * a.ld_q + (size_t)h * DH + i % DH]);
   const int k_end = min(it.u1 * CG_KEYS, max(max(lim[0], lim[1]), max(lim[2], lim[3])));
-  constexpr int KG = CG_KEYS / DH > 0 ? CG_KEYS / DH : 1;   // key groups of the weighted sum
-  const int d = tid % DH, kg = tid / DH;
-  float acc[CG_ROWS], m = -INFINITY, l = 0.f;   // (m, l of row `warp`)
+  const int d = tid % QD * 4, kg = tid / QD;
+  float acc[CG_ROWS][4], m = -INFINITY, l = 0.f;   // (m, l of row `warp`)
 #pragma unroll
-  for (int r = 0; r < CG_ROWS; ++r) acc[r] = 0.f;
+  for (int r = 0; r < CG_ROWS; ++r) acc[r][0] = acc[r][1] = acc[r][2] = acc[r][3] = 0.f;
   for (int k0 = it.u0 * CG_KEYS; k0 < k_end; k0 += CG_KEYS) {
     const int key = k0 + tid;
     long long e = -1;
@@ -88,9 +97,9 @@ __global__ void __launch_bounds__(CG_KEYS) chunk_any_kernel(const __grid_constan
       else
         a.c.flag(ERRW_POS);
     }
-    if (KT == KV_E4M3 && e >= 0) {
-      ks = exp_scale(a.c.k_exp[e]);
-      s_vs[tid] = exp_scale(a.c.v_exp[e]);
+    if (KT == KV_E4M3) {
+      if (e >= 0) ks = exp_scale(a.c.k_exp[e]);
+      s_vs[tid] = e >= 0 ? exp_scale(a.c.v_exp[e]) : 0.f;
     }
     s_e[tid] = e;
     __syncthreads();   // (and s_q; s_p and s_corr of the previous round are read)
@@ -98,10 +107,14 @@ __global__ void __launch_bounds__(CG_KEYS) chunk_any_kernel(const __grid_constan
 #pragma unroll
     for (int r = 0; r < CG_ROWS; ++r) dot[r] = 0.f;
     if (e >= 0) {
-      for (int i = 0; i < DH; ++i) {
-        const float x = kv_elem<KT>(a.c.k, (size_t)e * DH + i);
+#pragma unroll 8
+      for (int i = 0; i < DH; i += 4) {
+        const float4 x = kv_four<KT>(a.c.k, (size_t)e * DH + i);
 #pragma unroll
-        for (int r = 0; r < CG_ROWS; ++r) dot[r] = fmaf(x, s_q[r][i], dot[r]);
+        for (int r = 0; r < CG_ROWS; ++r) {
+          const float4 q = *reinterpret_cast<const float4*>(&s_q[r][i]);
+          dot[r] = fmaf(x.w, q.w, fmaf(x.z, q.z, fmaf(x.y, q.y, fmaf(x.x, q.x, dot[r]))));
+        }
       }
     }
 #pragma unroll
@@ -130,16 +143,33 @@ __global__ void __launch_bounds__(CG_KEYS) chunk_any_kernel(const __grid_constan
     }
     __syncthreads();
 #pragma unroll
-    for (int r = 0; r < CG_ROWS; ++r) acc[r] *= s_corr[r];
-    const int nk = min(CG_KEYS, k_end - k0);
-    for (int k = kg; k < nk; k += KG) {
-      const long long ev = s_e[k];
-      if (ev < 0) continue;
-      float x = kv_elem<KT>(a.c.v, (size_t)ev * DH + d);
-      if (KT == KV_E4M3) x *= s_vs[k];
+    for (int r = 0; r < CG_ROWS; ++r)
 #pragma unroll
-      for (int r = 0; r < CG_ROWS; ++r)
-        if (k0 + k < lim[r]) acc[r] = fmaf(s_p[r][k], x, acc[r]);
+      for (int x = 0; x < 4; ++x) acc[r][x] *= s_corr[r];
+    const int nk = min(CG_KEYS, k_end - k0);
+    for (int k1 = kg; k1 < nk; k1 += 4 * KG) {
+      float4 v[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int k = k1 + j * KG;
+        const long long ev = k < nk ? s_e[k] : -1;
+        v[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (ev >= 0) v[j] = kv_four<KT>(a.c.v, (size_t)ev * DH + d);
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int k = k1 + j * KG;
+        if (k >= nk) break;
+#pragma unroll
+        for (int r = 0; r < CG_ROWS; ++r) {
+          if (k0 + k >= lim[r]) continue;   // (0 times what a masked entry holds might be NaN)
+          const float w = s_p[r][k], vs = KT == KV_E4M3 ? s_vs[k] : 1.f;   // (no entry: 0 times 0)
+          acc[r][0] = fmaf(w, v[j].x * vs, acc[r][0]);
+          acc[r][1] = fmaf(w, v[j].y * vs, acc[r][1]);
+          acc[r][2] = fmaf(w, v[j].z * vs, acc[r][2]);
+          acc[r][3] = fmaf(w, v[j].w * vs, acc[r][3]);
+        }
+      }
     }
     __syncthreads();
   }
@@ -150,21 +180,19 @@ __global__ void __launch_bounds__(CG_KEYS) chunk_any_kernel(const __grid_constan
     pv.ml[warp * 2 + 1] = l;
   }
 #pragma unroll
-  for (int r = 0; r < CG_ROWS; ++r) {
-    s_red[tid] = acc[r];
-    __syncthreads();
+  for (int r = 0; r < CG_ROWS; ++r)
+    *reinterpret_cast<float4*>(&s_red[kg][r][d]) = make_float4(acc[r][0], acc[r][1], acc[r][2], acc[r][3]);
+  __syncthreads();
+  for (int i = tid; i < n * DH; i += CG_KEYS) {
+    const int r = i / DH, x = i % DH;
     float o = 0.f;
-    if (tid < DH)
-      for (int g = 0; g < KG; ++g) o += s_red[g * DH + tid];
-    if (tid < DH && r < n) {
-      const float sum = s_corr[r];
-      if (it.n_split > 1)
-        pv.o[r * DH + tid] = o;
-      else
-        ((T*)a.out)[(size_t)(it.q0 + j0 + r) * a.ld_out + (size_t)h * DH + tid] =
-            from_f<T>(lim[r] == 0 ? 0.f : o / sum);
-    }
-    __syncthreads();
+#pragma unroll
+    for (int g = 0; g < KG; ++g) o += s_red[g][r][x];
+    if (it.n_split > 1)
+      pv.o[r * DH + x] = o;
+    else
+      ((T*)a.out)[(size_t)(it.q0 + j0 + r) * a.ld_out + (size_t)h * DH + x] =
+          from_f<T>(chunk_lim(a, it.q0, it.c, it.len, j0 + r) == 0 ? 0.f : o / s_corr[r]);
   }
 }
 

@@ -288,6 +288,20 @@ def test_inputs_out_of_range_are_flagged_and_left_out():
 
 # ---- writing and reading back ---------------------------------------------------------------
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "e4m3"])
+@pytest.mark.parametrize("bt", [8, 16])
+def test_keys_of_a_missing_block_are_left_out(dtype, bt):
+    """The last block of positions is in no table: its rows attend what is before it, and the call says so."""
+    lens = [3 * bt, 10]
+    c = make_cache(dtype, 2, 64, lens, 19, bt=bt)
+    q, starts = make_q(dtype, [1, 2], 4, 64, 20)
+    c.block_table[0, 2] = -1
+    out = attend(c, q, starts, lens)
+    with pytest.raises(adept.AdeptError):
+        c.check()
+    assert_attention(c, q, starts, [2 * bt, 10], out)
+
+
 def test_sequences_that_share_rows_beyond_any_count():
     """Row ranges that go up and down (flagged) over and over: 4000 times 8192 rows at 8192 positions of 512 heads are 2^32 pairs of
     tiles, though the call's 8192 rows are not; nothing is done."""
