@@ -761,12 +761,13 @@ __global__ void __launch_bounds__(CF_WARPS * 32, 3) chunk_few_kernel(const __gri
 }
 
 // ---------------------------------------------------------------------------------------------
-// Join of split tiles: CTA = one tile; per row the splits' partials, taken in turn by as many groups of threads as the tile's
-// live elements leave room for, the groups joined in order at the end.
+// Join of split tiles: CTA (i, y) = part y of tile i's elements; per element the splits' partials, taken in turn by as many groups
+// of threads as the part leaves room for, the groups joined in order at the end.
 //   M = max m_i,  out = sum_i 2^(m_i - M) O_i / sum_i 2^(m_i - M) l_i
 // Four partials' loads are under way at a time: with one at a time a join of 14 took 9 us, most of it memory latency.
 // ---------------------------------------------------------------------------------------------
 constexpr int CJ_THREADS = 256;
+constexpr unsigned CJ_PARTS = 16;
 struct JoinAcc {
   float m, l, o[4];
   __device__ __forceinline__ void add(const float (&mi)[4], const float (&li)[4], const float4 (&oi)[4]) {
@@ -815,11 +816,13 @@ __global__ void __launch_bounds__(CJ_THREADS) chunk_join_kernel(const __grid_con
   const int group = a.n_heads / a.c.n_kv_heads;
   const int j0 = it.tile * p.tq, n = min(p.tq, it.c - j0);
   const PartView pv(a, p, rows, DH, it.slot0);
-  const int live = n * per_tok * (DH / 4);                       // elements of four columns
+  const int all = n * per_tok * (DH / 4), part = (all + (int)gridDim.y - 1) / (int)gridDim.y;   // elements of four columns
+  const int i0 = (int)blockIdx.y * part, live = min(part, all - i0);
+  if (live <= 0) return;
   const int groups = max(1, min(CJ_THREADS / live, (it.n_split + 3) / 4));
   const int gr = live < CJ_THREADS ? tid / live : 0;
   for (int i = live < CJ_THREADS ? tid % live : tid; i < live; i += CJ_THREADS) {
-    const int r = i / (DH / 4), d = i % (DH / 4) * 4, j = r / per_tok, g = it.group % sub * per_tok + r % per_tok;
+    const int r = (i0 + i) / (DH / 4), d = (i0 + i) % (DH / 4) * 4, j = r / per_tok, g = it.group % sub * per_tok + r % per_tok;
     JoinAcc x{-INFINITY, 0.f, {0.f, 0.f, 0.f, 0.f}};
     if (gr < groups) {
       for (int s0 = gr * 4; s0 < it.n_split; s0 += groups * 4) {
@@ -907,14 +910,23 @@ ChunkHow chunk_how(const KvPaged& c, int n_heads, int max_kv, bool aligned) {
 size_t how_bytes(const ChunkHow& w, const KvPaged& c) {
   return w.may_split ? (size_t)w.p.target * w.rows * (c.head_dim + 2) * sizeof(float) : 0;
 }
-// The most new tokens of a sequence whose rows are one tile of the few-row kernel.
-int few_tokens(const KvPaged& c, int n_heads) { return std::max(1, CF_ROWS / (n_heads / c.n_kv_heads)); }
+// The most new tokens of a sequence that the few-row kernel takes.  It reads K and V again for each tile of 16 rows, which costs by
+// the tiles of all sequences and heads; the tcgen05 kernel reads them once, but costs some 10 us more whatever the call, and
+// 8-bit entries have to be widened for it.  Few-row and tcgen05 kernel in us, over 4096 keys, tokens x heads on KV heads x d_h:
+//   bf16   8 x 32/8 x 128   15.7 17.2     16 x 32/8 x 128   19.3 17.8     32 x 32/32 x 128  30.8 24.4     16 x 32/32 x 128  23.7 23.8
+//          48 x 12/12 x 64  14.9 15.9     96 x 12/12 x 64   20.5 16.3     96 x 4/2 x 128    17.2 24.1     16 x (8 x 32/8 x 128)  107 51
+//   8-bit  16 x 32/8 x 128  20.3 26.6     48 x 32/8 x 128   34.6 34.7     64 x 32/32 x 128  42.4 57.5     96 x 32/32 x 128  57.2 59.8
+//          96 x 12/12 x 64  21.3 23.6     128 x 12/12 x 64  24.6 24.3     16 x (8 x 32/8 x 128)  85 127   16 x (32 x 32/8 x 128)  218 134
+// Where sequences of both kinds meet: over bf16 entries all go to the tcgen05 kernel (its tiles are mostly empty for few
+// tokens, but it reads K and V at the rate of the memory all the same), 8-bit ones are shared out (use_both).  7 sequences of a
+// token over 2000 keys beside one of 256 over 1000, 32 heads on 8: bf16 33.6 us, shared out 44.6; 8-bit 57.1 and 47.9.
+int few_tokens(const KvPaged& c, int n_heads) {
+  const long long tiles = 24ll * 128 / ((long long)c.n_seq * c.n_kv_heads * c.head_dim) + (c.type == KV_E4M3 ? 4 : 0);
+  return (int)std::max(1ll, tiles) * std::max(1, CF_ROWS / (n_heads / c.n_kv_heads));
+}
 bool use_tc(const KvPaged& c, int n_heads, int max_q, int max_kv, bool aligned) {
   return aligned && max_q > few_tokens(c, n_heads) && chunk_tc_takes(c, n_heads, max_kv);
 }
-// Sequences of few tokens in a call that also has longer ones: left to the tcgen05 kernel over bf16 entries (its tiles are
-// mostly empty then, but it reads K and V at the rate of the memory all the same), while 8-bit entries, which would have to
-// be widened for it, go to the few-row kernel.
 bool use_both(const KvPaged& c) { return c.type == KV_E4M3 && c.n_seq > 1; }
 
 template <int DH, int KT>
@@ -923,6 +935,9 @@ struct FewTag {};
 template <int DH, int KT, typename T>
 cudaError_t chunk_t(cudaStream_t st, const ChunkCall& a, const ChunkHow& w, int* launches) {
   const int max_c = std::min(a.max_q, a.c_hi);
+  SplitPlan one = w.p;
+  one.target = 0;
+  const long long tiles = split_items(one, a.c.n_seq, a.n_rows, max_c);   // at most
   const dim3 grid((unsigned)split_items(w.p, a.c.n_seq, a.n_rows, max_c));
   cudaError_t e = cudaErrorInvalidValue;
   ++*launches;
@@ -937,9 +952,7 @@ cudaError_t chunk_t(cudaStream_t st, const ChunkCall& a, const ChunkHow& w, int*
     // 500 keys 5.6 and 7.0 us, 1000 keys 6.3 and 7.2, 2000 keys 7.7 and 7.5; 32 heads of 128 on 8, 500 keys 6.8 and 8.4,
     // 2000 keys 9.1 and 11.4, 4000 keys 12.8 and 13.8, 3 sequences of up to 4000 14.3 and 14.4.  Clusters that had no room at
     // once (8 sequences, 512 CTAs): 14.2 and 10.0.
-    SplitPlan one = w.p;
-    one.target = 0;
-    const long long tiles = split_items(one, a.c.n_seq, a.n_rows, max_c), units = cdiv(a.max_kv, w.p.unit);
+    const long long units = cdiv(a.max_kv, w.p.unit);
     int cs = 8;
     while (cs > 1 && tiles * cs > w.p.target) cs >>= 1;
     if (cs > 1 && w.may_split && units * 32 <= DH * cs) {
@@ -962,7 +975,9 @@ cudaError_t chunk_t(cudaStream_t st, const ChunkCall& a, const ChunkHow& w, int*
   }
   if (e == cudaSuccess && w.may_split) {
     ++*launches;
-    e = launch_k(chunk_join_kernel<DH, T>, dim3((unsigned)w.p.target), dim3(CJ_THREADS), 0, st, a, w.p, w.rows, w.per_tok, w.sub);
+    // (more tiles than the target: none is split)
+    const unsigned x = (unsigned)std::min<long long>(tiles, w.p.target), y = std::min(CJ_PARTS, std::max(1u, w.p.target / x));
+    e = launch_k(chunk_join_kernel<DH, T>, dim3(x, y), dim3(CJ_THREADS), 0, st, a, w.p, w.rows, w.per_tok, w.sub);
   }
   return e;
 }
