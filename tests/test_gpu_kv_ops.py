@@ -129,6 +129,25 @@ def test_attention_of_longer_chunks(dtype, heads, hk, dh, new, past):
     assert torch.equal(out, attend(c, q, starts, lens)), "the same call gave other bits"
 
 
+@pytest.mark.parametrize("new,past", [
+    ([16, 1, 33, 0, 8, 400], [16, 300, 1, 40, 127, 5]),
+    ([300, 257, 17, 5], [64, 0, 0, 97]),
+    ([600], [45]),
+    ([9, 400, 2, 1, 270], [-3, -250, -1, 128, -15]),   # chunks longer than what is held: their first rows attend nothing
+])
+@pytest.mark.parametrize("heads,hk,dh", [(3, 3, 64), (8, 2, 128), (5, 1, 64), (24, 2, 128)])
+@pytest.mark.parametrize("dtype", ["bf16", "e4m3"])
+def test_attention_of_chunks_beside_a_long_one(dtype, heads, hk, dh, new, past):
+    lens = [a + b for a, b in zip(new, past)]
+    c = make_cache(dtype, hk, dh, lens, 9)
+    q, starts = make_q(dtype, new, heads, dh, 10, extra=3)
+    out = attend(c, q, starts, lens)
+    c.check()
+    assert_attention(c, q, starts, lens, out)
+    for b, (n, p) in enumerate(zip(new, past)):
+        assert (out[starts[b]:starts[b] + max(0, -p)] == 0).all()
+
+
 @pytest.mark.parametrize("heads,hk,dh,new,past", [
     (16, 4, 128, [1, 200, 3, 0, 17], [4600, 300, 90, 8, 0]),   # the few rows' keys split over the GPU, joined beside the longer chunks'
     (4, 4, 64, [40, 1, 1], [60, 2300, 0]),
