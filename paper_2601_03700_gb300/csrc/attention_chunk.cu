@@ -24,7 +24,9 @@ namespace {
 // Any type, head size, alignment and block size: CUDA-core kernel.  CTA = up to CG_ROWS new tokens of one query head x a
 // run of keys, 128 keys at a time: a thread per key for the scores, a warp per token for the softmax, for the weighted sum a
 // thread per four dimensions of every KG-th key.  Such calls are short and bound by latency, one load behind the other, so
-// all loads are of four elements, several under way.
+// all loads are of four elements, several under way: fp32, 22 rows of 4 heads of 64 over up to 101 keys in 7.9 us (17.8 with
+// one element a load, two key groups); 512 rows of 12 heads over 2560 keys in 379 us (9.6 TFLOP/s, each tile of 4 rows reading
+// K and V from L2 again).
 // ---------------------------------------------------------------------------------------------
 constexpr int CG_ROWS = 4, CG_KEYS = 128;
 
@@ -202,7 +204,7 @@ __global__ void __launch_bounds__(CG_KEYS) chunk_any_kernel(const __grid_constan
 // head's group) x a run of keys, CF_WARPS warps taking blocks in turn, each with a softmax and sums of its own, merged in
 // warp order at the end.
 //
-// A head's 16 positions of a block are one contiguous piece of the pool: each warp keeps CF_STAGES of them (K, V, exponents)
+// A head's 16 positions of a block are one contiguous piece of the pool: each warp keeps STAGES of them (K, V, exponents)
 // under way by bulk copies into a ring of its own, so no warp waits for another, and no register holds what is under way.
 // From the ring the words go straight into fragments: the order of the head's dimensions inside q.k is free, so a thread's
 // B fragments of S = Q K^T are whole 16-byte pieces of its key's row (Q is loaded in the same order), and the columns of O are
@@ -216,6 +218,10 @@ __global__ void __launch_bounds__(CG_KEYS) chunk_any_kernel(const __grid_constan
 // 1000 keys 7.1 and 19.2), in one of two ways.  Where a cluster of up to 8 CTAs a tile is enough (cs > 1), its CTAs take
 // equal shares and join through distributed shared memory, in one launch.  Else each tile gets as many as balance the GPU
 // (split_find), whose partials a second launch joins.
+//
+// Measured: a token of 32 heads of 128 over 30011 keys, 8 bits (248 MB) 54.5 us, 4.5 TB/s, bound by instruction issue (12 warps an
+// SM, half the issue slots and half the ALU's taken, each waiting on its own conversions and exponentials); bf16 (492 MB)
+// 81.2 us, 6.1 TB/s, near the memory's rate; 4 to 5 tokens of 4 sequences over 8.4 thousand keys, bf16 (139 MB), 32.7 us.
 // ---------------------------------------------------------------------------------------------
 constexpr int CF_WARPS = 4, CF_ROWS = 16;
 constexpr float CF_RAISE = 8.f;   // the running maximum is raised once a score exceeds it by 2^8: weights stay below 256
