@@ -463,8 +463,8 @@ ADEPT_API adept_status adept_kv_gather(const adept_kv_cache* c, int n_rows, int 
  *                they must not overlap.  Rows that no sequence holds are not written.
  *   d_q_start [n_seq + 1], d_kv_len [n_seq]   int32, read on the device
  *   d_row_pos [n_rows] or NULL   int32, read on the device: the rows' own positions, ascending within a
- *                sequence, each below its d_kv_len (rows of tokens that are still active where others have
- *                left); NULL: the last positions
+ *                sequence (else that sequence's rows hold anything), each below its d_kv_len (rows of
+ *                tokens that are still active where others have left); NULL: the last positions
  *   max_q_len, max_kv_len   bounds on a sequence's rows and positions; a sequence beyond them, or with
  *                rows outside 0 .. n_rows, flags DEVICE_INPUT and is left out, as is a key whose block
  *                is out of range

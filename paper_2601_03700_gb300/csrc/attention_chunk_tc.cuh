@@ -260,7 +260,7 @@ struct CtSeg {
     n_tok = min(2 * ts, x.c - t0);
     lim_lo = keys(a, 0);
     k_end = keys(a, n_tok - 1);
-    const int k_end0 = keys(a, min(ts, n_tok) - 1);
+    const int k_end0 = min(keys(a, min(ts, n_tok) - 1), k_end);   // (given positions might not ascend: nothing behind k_end is touched)
     nt0 = max(min(j_hi, (k_end0 + CT_BN - 1) / CT_BN) - j_lo, 0);
     nt1 = n_tok > ts ? max(min(j_hi, (k_end + CT_BN - 1) / CT_BN) - j_lo, 0) : 0;
     n_it = max(nt0, nt1);
@@ -396,7 +396,7 @@ __global__ void __launch_bounds__(CtShape<DH>::THREADS, 1) chunk_tc_kernel(const
       g.set(a, ts, x, u, u_end);
       seg += g.n_it > 0;
       const bool mine = tok >= 0 && tok < g.n_tok;
-      const int lim = mine ? g.keys(a, tok) : 0;
+      const int lim = mine ? min(g.keys(a, tok), g.k_end) : 0;
       const int sub_lo = sub * ts < g.n_tok ? g.keys(a, sub * ts) : 0;   // keys of the sub-tile's first token
       const int n_my = g.nt(sub);
       float m = -INFINITY, l = 0.f;

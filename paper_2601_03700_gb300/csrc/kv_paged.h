@@ -99,7 +99,7 @@ __device__ __forceinline__ void chunk_seq(const ChunkCall& a, int b, int& q0, in
 
 // Keys that new token j of a sequence attends.
 __device__ __forceinline__ int chunk_lim(const ChunkCall& a, int q0, int c, int len, int j) {
-  return a.row_pos ? min(max(a.row_pos[q0 + j] + 1, 0), len) : max(len - c + j + 1, 0);
+  return a.row_pos ? min(max(a.row_pos[q0 + j], -1), len - 1) + 1 : max(len - c + j + 1, 0);
 }
 
 // Item `id` of the plan (joined: tile `id`, its splits taken together), looked up by one converged warp; false: none.  32-bit

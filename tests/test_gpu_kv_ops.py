@@ -250,6 +250,25 @@ def test_rows_at_given_positions(dtype, heads, hk, dh, new, keep):
     assert torch.equal(out, again)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "e4m3"])
+@pytest.mark.parametrize("n", [6, 700])
+def test_positions_that_do_not_ascend_touch_no_other_sequence(dtype, n):
+    """A sequence's rows in descending, then in shuffled order of position: its own rows may hold anything."""
+    new, lens = [n, 20, n], [3000, 90, 3000]
+    c = make_cache(dtype, 2, 128, lens, 53)
+    q, starts = make_q(dtype, new, 8, 128, 54, extra=2)
+    want, tol = R.attention(c, q, starts, lens)
+    down = torch.arange(2999, 2999 - n, -1)
+    mixed = torch.randint(-5, 4000, (n,), generator=torch.Generator().manual_seed(55))
+    row_pos = _i32(torch.cat([down, torch.arange(70, 90), mixed, torch.zeros(2)]).long().tolist())
+    out = torch.full_like(q, -7.0)
+    adept.adept_chunk_attention(c, q, _i32(starts), _i32(lens), max(new), 3000, out, row_pos=row_pos)
+    torch.cuda.synchronize()
+    mid = slice(n, n + 20)
+    assert ((out[mid].double() - want[mid]).abs() <= tol[mid] + 1e-30).all()
+    assert (out[-2:] == -7).all()
+
+
 @pytest.mark.parametrize("dtype,heads,hk,dh", [("f32", 2, 1, 64), ("bf16", 8, 2, 128), ("e4m3", 4, 4, 64)])
 def test_rows_without_keys_are_zero(dtype, heads, hk, dh):
     c = make_cache(dtype, hk, dh, [4, 0, 20], 13)
