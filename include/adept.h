@@ -473,7 +473,7 @@ ADEPT_API adept_status adept_kv_gather(const adept_kv_cache* c, int n_rows, int 
  * For the same lengths a call's results are the same bits every time.
  * Errors: INVALID_ARG (bad cache, n_heads no multiple of n_kv_heads, max_kv_len above the table, a
  * stride below a row, NULL or misaligned pointers, a workspace too small), CAPACITY (n_rows *
- * n_heads above 2^30, or more than 2^31 tiles of 128 rows and 128 keys), CUDA. */
+ * n_heads or n_seq * n_heads above 2^30, or more than 2^31 tiles of 128 rows and 128 keys), CUDA. */
 ADEPT_API adept_status adept_chunk_attention(const adept_kv_cache* c, int n_heads, int n_rows, const void* d_q, int64_t ld_q,
                                    const int32_t* d_q_start, const int32_t* d_kv_len, const int32_t* d_row_pos,
                                    int max_q_len, int max_kv_len, void* d_out, int64_t ld_out, void* d_ws, int64_t ws_bytes, void* stream);

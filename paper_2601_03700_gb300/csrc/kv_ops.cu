@@ -33,6 +33,7 @@ adept_status view_of(const adept_kv_cache* c, KvPaged* v) {
   if ((long long)c->max_blocks_per_seq * c->block_tokens > (1ll << 30) || (long long)c->n_kv_heads * c->head_dim > (1 << 20))
     return bad(ADEPT_ERR_INVALID_ARG, "cache too large (2^30 positions a sequence, 2^20 elements a position)");
   if (!c->d_k || !c->d_v || !c->d_block_table) return bad(ADEPT_ERR_INVALID_ARG, "NULL cache pointer");
+  if (((uintptr_t)c->d_block_table | (uintptr_t)c->d_err) & 3) return bad(ADEPT_ERR_INVALID_ARG, "misaligned block table or error word");
   if (((uintptr_t)c->d_k | (uintptr_t)c->d_v) & 15) return bad(ADEPT_ERR_INVALID_ARG, "K and V must start on 16 bytes");
   if (c->kv_type == ADEPT_KV_E4M3 && (!c->d_k_exp || !c->d_v_exp))
     return bad(ADEPT_ERR_INVALID_ARG, "an e4m3 cache needs its exponents");
@@ -53,6 +54,7 @@ adept_status rows_ok(const KvPaged& v, int n_rows, int dtype, const void* k, int
   if (ld_k < w || ld_v < w) return bad(ADEPT_ERR_INVALID_ARG, "row stride below the %lld elements of a row", (long long)w);
   const uintptr_t m = dtype == ADEPT_DTYPE_BF16 ? 1 : 3;
   if (((uintptr_t)k | (uintptr_t)vv) & m) return bad(ADEPT_ERR_INVALID_ARG, "misaligned rows");
+  if (((uintptr_t)seq | (uintptr_t)pos) & 3) return bad(ADEPT_ERR_INVALID_ARG, "misaligned sequences or positions");
   return ADEPT_OK;
 }
 
@@ -68,7 +70,8 @@ adept_status call_ok(const KvPaged& v, int n_heads, int n_rows, int max_q, int m
   if (n_rows < 0 || max_q < 0 || max_kv < 0) return bad(ADEPT_ERR_INVALID_ARG, "negative size");
   if (max_kv > v.max_blocks * v.block_tokens)
     return bad(ADEPT_ERR_INVALID_ARG, "max_kv_len %d above the %d positions of a sequence", max_kv, v.max_blocks * v.block_tokens);
-  if ((long long)n_rows * n_heads > (1ll << 30)) return bad(ADEPT_ERR_CAPACITY, "n_rows * n_heads above 2^30");
+  if ((long long)n_rows * n_heads > (1ll << 30) || (long long)v.n_seq * n_heads >= (1ll << 30))
+    return bad(ADEPT_ERR_CAPACITY, "n_rows * n_heads above 2^30, or n_seq * n_heads");
   if (n_heads / v.n_kv_heads <= 128 && !chunk_tc_fits(v, n_heads, n_rows, max_q, max_kv))
     return bad(ADEPT_ERR_CAPACITY, "a call of more than 2^31 tiles");
   return ADEPT_OK;
@@ -117,6 +120,8 @@ adept_status adept_chunk_attention(const adept_kv_cache* c, int n_heads, int n_r
   if (ld_q < w || ld_out < w) return bad(ADEPT_ERR_INVALID_ARG, "row stride below the %lld elements of a row", (long long)w);
   const uintptr_t m = a.c.type == KV_F32 ? 3 : 1;
   if (((uintptr_t)d_q | (uintptr_t)d_out) & m) return bad(ADEPT_ERR_INVALID_ARG, "misaligned rows");
+  if (((uintptr_t)d_q_start | (uintptr_t)d_kv_len | (uintptr_t)d_row_pos) & 3)
+    return bad(ADEPT_ERR_INVALID_ARG, "misaligned lengths or positions");
   const int64_t need = (int64_t)chunk_workspace(a.c, n_heads, max_q_len, max_kv_len);
   if (need > 0 && (!d_ws || ws_bytes < need || ((uintptr_t)d_ws & 15)))
     return bad(ADEPT_ERR_INVALID_ARG, "workspace of %lld bytes, on 16 bytes, needed (adept_chunk_attention_workspace)", (long long)need);

@@ -87,6 +87,29 @@ def test_capacity(lib):
                                      None) == 3
 
 
+def test_capacity_of_sequences(lib):
+    """More tiles than a grid has CTAs."""
+    for n_seq, heads in ((2 ** 25, 64), (2 ** 16, 2 ** 15)):
+        c = ctypes.byref(cache(n_seq=n_seq))
+        assert lib.adept_chunk_attention_workspace(c, heads, 40, 5, 16) == -1
+        assert lib.adept_chunk_attention(c, heads, 40, 64, heads * 64, 64, 64, None, 5, 16, 64, heads * 64, 128, 2 ** 40, None) == 3
+
+
+@pytest.mark.parametrize("at", [dict(start=66), dict(kv_len=65), dict(row_pos=67), dict(table=514), dict(err=2)], ids=str)
+def test_misaligned_lengths_and_tables(lib, at):
+    a = dict(start=64, kv_len=64, row_pos=None, table=512, err=None)
+    a.update(at)
+    c = ctypes.byref(cache(kv_type=0, d_block_table=a["table"], d_err=a["err"]))
+    assert lib.adept_chunk_attention(c, 4, 40, 64, 256, a["start"], a["kv_len"], a["row_pos"], 40, 64, 64, 256, None, 0, None) == 1
+
+
+@pytest.mark.parametrize("seq,pos", [(65, 64), (64, 66)])
+def test_misaligned_places(lib, seq, pos):
+    c = ctypes.byref(cache())
+    assert lib.adept_kv_append(c, 1, 1, 64, 128, 64, 128, seq, pos, None) == 1
+    assert lib.adept_kv_gather(c, 1, 1, 64, 128, 64, 128, seq, pos, None) == 1
+
+
 def test_binding_checks_tensors(lib):
     import paper_2601_03700_gb300 as adept
     with pytest.raises(ValueError):
