@@ -200,7 +200,7 @@ __global__ void __launch_bounds__(CG_KEYS) chunk_any_kernel(const __grid_constan
 
 // ---------------------------------------------------------------------------------------------
 // bf16 queries over bf16 or e4m3 entries in blocks of 16 positions: warp-level matrix instructions (m16n8k16), for the calls
-// that are a stream of K and V (steps, checks of a few tokens).  CTA = a tile of 16 rows (token x query head of the KV
+// that are a stream of K and V (steps, checks of a few tokens).  CTA = a tile of ROWS rows (token x query head of the KV
 // head's group) x a run of keys, CF_WARPS warps taking blocks in turn, each with a softmax and sums of its own, merged in
 // warp order at the end.
 //
@@ -219,9 +219,15 @@ __global__ void __launch_bounds__(CG_KEYS) chunk_any_kernel(const __grid_constan
 // equal shares and join through distributed shared memory, in one launch.  Else each tile gets as many as balance the GPU
 // (split_find), whose partials a second launch joins.
 //
-// Measured: a token of 32 heads of 128 over 30011 keys, 8 bits (248 MB) 54.5 us, 4.5 TB/s, bound by instruction issue (12 warps an
-// SM, half the issue slots and half the ALU's taken, each waiting on its own conversions and exponentials); bf16 (492 MB)
-// 81.2 us, 6.1 TB/s, near the memory's rate; 4 to 5 tokens of 4 sequences over 8.4 thousand keys, bf16 (139 MB), 32.7 us.
+// ROWS = 8: where no tile has more than 8 rows the keys are the 16 rows of the matrix instructions and the queries their 8
+// columns (S^T = K Q^T, O^T = V^T P^T), which halves them and the softmax; the same words of K and V in the same registers, P's
+// fragments turned round in between.  For 8-bit entries, which are bound by instructions: a token of 32 heads of 128
+// over 30011 keys 47.3 us, 54.5 with 16 rows; 16 sequences of a token, 32 heads on 8, 21.4 and 23.8.  bf16 is bound by memory
+// and gains nothing (32 heads, 4000 keys 18.7 and 18.8; 8 sequences of 12 heads of 64 20.0 and 18.2).
+//
+// Measured: that token over 30011 keys, 8 bits (248 MB) 5.2 TB/s, bound by instruction issue (12 warps an SM, each waiting on its
+// own conversions and exponentials); over 30000 in bf16 (492 MB) 81.2 us, 6.1 TB/s, near the memory's rate; 4 to 5 tokens of
+// 4 sequences over 8.4 thousand keys, bf16 (139 MB), 32.7 us.
 // ---------------------------------------------------------------------------------------------
 constexpr int CF_WARPS = 4, CF_ROWS = 16;
 constexpr float CF_RAISE = 8.f;   // the running maximum is raised once a score exceeds it by 2^8: weights stay below 256
@@ -255,6 +261,12 @@ __device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], 
     asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
         : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// The transpose of an 8 x 8 matrix of 16-bit elements over the warp (lane: row lane / 4, columns 2 (lane % 4) and the next).
+__device__ __forceinline__ uint32_t turn8x8(uint32_t x) {
+  uint32_t y;
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
 }
 __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
   const __nv_bfloat162 x = __floats2bfloat162_rn(a, b);
@@ -321,7 +333,7 @@ __device__ __forceinline__ void cf_pairs(uint32_t k0, uint32_t k1, uint32_t k2, 
   }
 }
 
-template <int DH, int KT>
+template <int DH, int KT, int ROWS>
 struct FewShape {
   static constexpr int ES = KT == KV_BF16 ? 2 : 1;
   static constexpr int NB = KT == KV_BF16 ? 1 : 2;         // blocks of 16 keys per warp and round
@@ -331,21 +343,23 @@ struct FewShape {
   static constexpr int VVEC = DH * ES / 8 < 16 ? DH * ES / 8 : 16, VN = DH * ES / 8 / VVEC, VE = VVEC / ES;   // V pieces
   static constexpr int BLOCK = 16 * DH * ES;               // bytes of a block of one head
   static constexpr int STAGE = 2 * BLOCK + (KT == KV_E4M3 ? 32 : 0);   // K, V, exponents
-  static constexpr int RING = CF_WARPS * STAGES * STAGE, MERGE = CF_WARPS * CF_ROWS * (DH + 4) * 4;
+  static constexpr int RING = CF_WARPS * STAGES * STAGE, MERGE = CF_WARPS * ROWS * (DH + 4) * 4;
   static constexpr int SMEM = RING > MERGE ? RING : MERGE;
 };
 
-template <int DH, int KT>
+template <int DH, int KT, int ROWS>
 __global__ void __launch_bounds__(CF_WARPS * 32, 3) chunk_few_kernel(const __grid_constant__ ChunkCall a,
                                                                      const __grid_constant__ SplitPlan p, int per_tok, int sub,
                                                                      int cs) {
-  using F = FewShape<DH, KT>;
-  constexpr int KS = DH / 16;
+  using F = FewShape<DH, KT, ROWS>;
+  constexpr bool W8 = ROWS == 8;
+  constexpr int KS = DH / 16, NS = F::NB * (W8 ? 1 : 2), NO = DH / (W8 ? 16 : 8);   // k-steps; fragments of S in a round, of O
+  auto rh = [](int e) { return W8 ? e & 1 : e >> 1; };   // which of the thread's two rows element e of a fragment is of
   constexpr bool F16 = KT == KV_E4M3;   // S in fp16
   __shared__ SplitItem s_it;
   __shared__ int s_have, s_abort;
-  __shared__ float s_m[CF_WARPS][CF_ROWS], s_l[CF_WARPS][CF_ROWS];
-  __shared__ float s_cm[CF_ROWS], s_cl[CF_ROWS];   // of the CTA, for its cluster
+  __shared__ float s_m[CF_WARPS][ROWS], s_l[CF_WARPS][ROWS];
+  __shared__ float s_cm[ROWS], s_cl[ROWS];   // of the CTA, for its cluster
   __shared__ __align__(8) uint64_t s_full[CF_WARPS][F::STAGES];
   extern __shared__ __align__(128) uint8_t s_dyn[];   // the rings; then [warp][row][DH + 4] floats
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
@@ -428,16 +442,20 @@ __global__ void __launch_bounds__(CF_WARPS * 32, 3) chunk_few_kernel(const __gri
     __syncwarp();
     ++sent;
   };
-  // ---- this thread's two rows (g, g + 8): Q fragments, and the keys each attends
-  uint32_t qf[KS][4];
+  // ---- Q fragments of rows g (and g + 8); the keys that this thread's two rows of S attend: g and g + 8, or 2 t and 2 t + 1
+  uint32_t qf[KS][W8 ? 2 : 4];
   int lim[2];
   float rs[2];   // what a row's S is multiplied by
 #pragma unroll
   for (int r2 = 0; r2 < 2; ++r2) {
+    const int r = W8 ? 2 * t + r2 : g + 8 * r2;
+    lim[r2] = r < n_row && g0 + r % per_tok < group ? keys_of(r / per_tok) : 0;
+    rs[r2] = a.scale_log2;
+  }
+#pragma unroll
+  for (int r2 = 0; r2 < ROWS / 8; ++r2) {
     const int r = g + 8 * r2, j = r / per_tok, gq = g0 + r % per_tok;
     const bool on = r < n_row && gq < group;
-    lim[r2] = on ? keys_of(j) : 0;
-    rs[r2] = a.scale_log2;
     const bf16* q = (const bf16*)a.q + (size_t)(it.q0 + j0 + j) * a.ld_q + (size_t)(kvh * group + gq) * DH;
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
@@ -446,7 +464,7 @@ __global__ void __launch_bounds__(CF_WARPS * 32, 3) chunk_few_kernel(const __gri
       uint2 x = make_uint2(0, 0);
       if (on) x = *reinterpret_cast<const uint2*>(q + dim);
       qf[s][r2] = x.x;
-      qf[s][2 + r2] = x.y;
+      qf[s][ROWS / 8 + r2] = x.y;
     }
   }
   // blocks of this warp (whole rounds; those past b_end are not there)
@@ -455,13 +473,14 @@ __global__ void __launch_bounds__(CF_WARPS * 32, 3) chunk_few_kernel(const __gri
 
   if constexpr (F16) {
 #pragma unroll
-    for (int r2 = 0; r2 < 2; ++r2) {
+    for (int r2 = 0; r2 < ROWS / 8; ++r2) {
       unsigned top = 0;   // exponent field of the row's largest finite element
 #pragma unroll
       for (int s = 0; s < KS; ++s)
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          const unsigned lo = (qf[s][r2 + 2 * h] >> 7) & 0xffu, hi = (qf[s][r2 + 2 * h] >> 23) & 0xffu;
+          const uint32_t w = qf[s][r2 + ROWS / 8 * h];
+          const unsigned lo = (w >> 7) & 0xffu, hi = (w >> 23) & 0xffu;
           top = max(top, max(lo == 255u ? 0u : lo, hi == 255u ? 0u : hi));
         }
       top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
@@ -473,16 +492,21 @@ __global__ void __launch_bounds__(CF_WARPS * 32, 3) chunk_few_kernel(const __gri
       for (int s = 0; s < KS; ++s)
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          uint32_t& w = qf[s][r2 + 2 * h];
+          uint32_t& w = qf[s][r2 + ROWS / 8 * h];
           const __half2 y = __floats2half2_rn(__uint_as_float(w << 16) * up, __uint_as_float(w & 0xffff0000u) * up);
           w = *reinterpret_cast<const uint32_t*>(&y);
         }
     }
+    if constexpr (W8) {   // from the lanes that hold rows 2 t and 2 t + 1 of Q
+      const float of_g = rs[0];
+      rs[0] = __shfl_sync(0xffffffffu, of_g, 8 * t);
+      rs[1] = __shfl_sync(0xffffffffu, of_g, 8 * t + 4);
+    }
   }
 
-  float o[DH / 8][4], m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+  float o[NO][4], m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
 #pragma unroll
-  for (int j = 0; j < DH / 8; ++j) o[j][0] = o[j][1] = o[j][2] = o[j][3] = 0.f;
+  for (int j = 0; j < NO; ++j) o[j][0] = o[j][1] = o[j][2] = o[j][3] = 0.f;
 
   bool ok = true;
   unsigned cf_phase = 0;   // bit s: parity of stage s's next copy
@@ -504,28 +528,37 @@ __global__ void __launch_bounds__(CF_WARPS * 32, 3) chunk_few_kernel(const __gri
       break;
     }
     edge |= (b + F::NB) * 16 > lim_lo || (b + F::NB) * 16 > k_end;
-    // S = Q K^T
-    float s[2 * F::NB][4];
+    // S = Q K^T (W8: its transpose, K Q^T)
+    float s[NS][4];
 #pragma unroll
-    for (int i = 0; i < F::NB; ++i)
+    for (int i = 0; i < F::NB; ++i) {
+      Words<F::KVEC> k[2][F::KN];   // keys g and g + 8
 #pragma unroll
-      for (int nt = 0; nt < 2; ++nt) {
-        float(&d)[4] = s[2 * i + nt];
+      for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+        for (int c = 0; c < F::KN; ++c) k[nt][c] = lds<F::KVEC>(st[i] + (nt * 8 + g) * (DH * F::ES) + (c * 4 + t) * F::KVEC);
+#pragma unroll
+      for (int nt = 0; nt < (W8 ? 1 : 2); ++nt) {
+        float(&d)[4] = s[W8 ? i : 2 * i + nt];
         d[0] = d[1] = d[2] = d[3] = 0.f;
-        Words<F::KVEC> k[F::KN];
-#pragma unroll
-        for (int c = 0; c < F::KN; ++c) k[c] = lds<F::KVEC>(st[i] + (nt * 8 + g) * (DH * F::ES) + (c * 4 + t) * F::KVEC);
 #pragma unroll
         for (int c = 0; c < F::KN; ++c)
 #pragma unroll
           for (int w = 0; w < F::KE / 4; ++w) {
             const int ks = c * (F::KE / 4) + w;
-            if constexpr (KT == KV_BF16)
-              mma16816<false>(d, qf[ks], k[c].w[2 * w], k[c].w[2 * w + 1]);
-            else
-              mma16816<true>(d, qf[ks], e4m3x2_f16x2(k[c].w[w] & 0xffffu), e4m3x2_f16x2(k[c].w[w] >> 16));
+            auto lo = [&](int n) { return KT == KV_BF16 ? k[n][c].w[2 * w] : e4m3x2_f16x2(k[n][c].w[w] & 0xffffu); };
+            auto hi = [&](int n) { return KT == KV_BF16 ? k[n][c].w[2 * w + 1] : e4m3x2_f16x2(k[n][c].w[w] >> 16); };
+            if constexpr (W8) {
+              const uint32_t kf[4] = {lo(0), lo(1), hi(0), hi(1)};
+              mma16816<F16>(d, kf, qf[ks][0], qf[ks][1]);
+            } else {
+              mma16816<F16>(d, qf[ks], lo(nt), hi(nt));
+            }
           }
-        if constexpr (KT == KV_E4M3) {
+        if constexpr (KT == KV_E4M3 && W8) {
+          const float e0 = exp_scale(st[i][2 * F::BLOCK + g]), e1 = exp_scale(st[i][2 * F::BLOCK + 8 + g]);
+          d[0] *= e0 * rs[0]; d[1] *= e0 * rs[1]; d[2] *= e1 * rs[0]; d[3] *= e1 * rs[1];
+        } else if constexpr (KT == KV_E4M3) {
           const uint32_t e = *reinterpret_cast<const uint16_t*>(st[i] + 2 * F::BLOCK + nt * 8 + 2 * t);
           const float e0 = exp_scale(e & 0xff), e1 = exp_scale(e >> 8);
           d[0] *= e0 * rs[0]; d[1] *= e1 * rs[0]; d[2] *= e0 * rs[1]; d[3] *= e1 * rs[1];
@@ -534,15 +567,16 @@ __global__ void __launch_bounds__(CF_WARPS * 32, 3) chunk_few_kernel(const __gri
           for (int e = 0; e < 4; ++e) d[e] *= rs[0];
         }
       }
-    unsigned att = ~0u;   // bit (tile, element): the row attends the key
+    }
+    unsigned att = ~0u;   // bit (fragment, element): the row attends the key
     if (edge) {
       att = 0;
 #pragma unroll
-      for (int x = 0; x < 2 * F::NB; ++x)
+      for (int x = 0; x < NS; ++x)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const int key = b * 16 + x * 8 + 2 * t + (e & 1);
-          const bool on = here[x / 2] && key < min(lim[e >> 1], k_end);
+          const int key = b * 16 + (W8 ? x * 16 + g + 8 * (e >> 1) : x * 8 + 2 * t + (e & 1));
+          const bool on = here[W8 ? x : x / 2] && key < min(lim[rh(e)], k_end);
           att |= (unsigned)on << (x * 4 + e);
           if (!on) s[x][e] = -INFINITY;
         }
@@ -550,68 +584,92 @@ __global__ void __launch_bounds__(CF_WARPS * 32, 3) chunk_few_kernel(const __gri
     // softmax of the two rows
     float mx[2] = {-INFINITY, -INFINITY};
 #pragma unroll
-    for (int x = 0; x < 2 * F::NB; ++x) {
-      mx[0] = fmaxf(mx[0], fmaxf(s[x][0], s[x][1]));
-      mx[1] = fmaxf(mx[1], fmaxf(s[x][2], s[x][3]));
+    for (int x = 0; x < NS; ++x) {
+      mx[0] = fmaxf(mx[0], fmaxf(s[x][0], s[x][W8 ? 2 : 1]));
+      mx[1] = fmaxf(mx[1], fmaxf(s[x][W8 ? 1 : 2], s[x][3]));
     }
     float ref[2];
     bool raise = false;
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
-      mx[r] = fmaxf(mx[r], __shfl_xor_sync(0xffffffffu, mx[r], 1));
-      mx[r] = fmaxf(mx[r], __shfl_xor_sync(0xffffffffu, mx[r], 2));
+#pragma unroll
+      for (int w = W8 ? 4 : 1; w <= (W8 ? 16 : 2); w *= 2) mx[r] = fmaxf(mx[r], __shfl_xor_sync(0xffffffffu, mx[r], w));
       raise |= mx[r] > m[r] + CF_RAISE || (m[r] == -INFINITY && mx[r] > m[r]);
     }
     if (__any_sync(0xffffffffu, raise)) {
+      float f[2];
 #pragma unroll
       for (int r = 0; r < 2; ++r) {
-        const float mn = fmaxf(m[r], mx[r]), f = mn == -INFINITY ? 1.f : ex2_approx(m[r] - mn);
+        const float mn = fmaxf(m[r], mx[r]);
+        f[r] = mn == -INFINITY ? 1.f : ex2_approx(m[r] - mn);
         m[r] = mn;
-        l[r] *= f;
-#pragma unroll
-        for (int j = 0; j < DH / 8; ++j) {
-          o[j][2 * r] *= f;
-          o[j][2 * r + 1] *= f;
-        }
+        l[r] *= f[r];
       }
+#pragma unroll
+      for (int j = 0; j < NO; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[j][e] *= f[rh(e)];
     }
 #pragma unroll
     for (int r = 0; r < 2; ++r) ref[r] = m[r] == -INFINITY ? 0.f : m[r];
 #pragma unroll
-    for (int x = 0; x < 2 * F::NB; ++x)
+    for (int x = 0; x < NS; ++x)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        s[x][e] = ex2_approx(s[x][e] - ref[e >> 1]);
-        l[e >> 1] += s[x][e];
+        s[x][e] = ex2_approx(s[x][e] - ref[rh(e)]);
+        l[rh(e)] += s[x][e];
       }
-    // O += P V
+    // O += P V (W8: its transpose, V^T P^T, whose fragments of P^T are those of S's transpose turned round)
 #pragma unroll
     for (int i = 0; i < F::NB; ++i) {
-      uint32_t pf[4];
+      constexpr int NP = W8 ? 2 : 4;
+      uint32_t pf[NP];
+      float ve[4] = {1.f, 1.f, 1.f, 1.f};   // V's scales: of keys 2 t, 2 t + 1, and 8 on (W8: of keys g, g + 8)
       if constexpr (KT == KV_E4M3) {
-        const uint8_t* ve = st[i] + 2 * F::BLOCK + 16 + 2 * t;
-        const uint32_t x = *reinterpret_cast<const uint16_t*>(ve), y = *reinterpret_cast<const uint16_t*>(ve + 8);
-        const float e0 = exp_scale(x & 0xff), e1 = exp_scale(x >> 8), e2 = exp_scale(y & 0xff), e3 = exp_scale(y >> 8);
-        pf[0] = pack_bf16(s[2 * i][0] * e0, s[2 * i][1] * e1);
-        pf[1] = pack_bf16(s[2 * i][2] * e0, s[2 * i][3] * e1);
-        pf[2] = pack_bf16(s[2 * i + 1][0] * e2, s[2 * i + 1][1] * e3);
-        pf[3] = pack_bf16(s[2 * i + 1][2] * e2, s[2 * i + 1][3] * e3);
-      } else {
-        pf[0] = pack_bf16(s[2 * i][0], s[2 * i][1]);
-        pf[1] = pack_bf16(s[2 * i][2], s[2 * i][3]);
-        pf[2] = pack_bf16(s[2 * i + 1][0], s[2 * i + 1][1]);
-        pf[3] = pack_bf16(s[2 * i + 1][2], s[2 * i + 1][3]);
+        const uint8_t* vp = st[i] + 2 * F::BLOCK + 16;
+        if constexpr (W8) {
+          ve[0] = exp_scale(vp[g]);
+          ve[1] = exp_scale(vp[8 + g]);
+        } else {
+          const uint32_t x = *reinterpret_cast<const uint16_t*>(vp + 2 * t), y = *reinterpret_cast<const uint16_t*>(vp + 8 + 2 * t);
+          ve[0] = exp_scale(x & 0xff);
+          ve[1] = exp_scale(x >> 8);
+          ve[2] = exp_scale(y & 0xff);
+          ve[3] = exp_scale(y >> 8);
+        }
+      }
+      // fragment e of P: elements 2 e and 2 e + 1 of the block's S
+#pragma unroll
+      for (int e = 0; e < NP; ++e) {
+        const float(&x)[4] = s[W8 ? i : 2 * i + (e >> 1)];
+        const int at = (e & 1) * 2;
+        pf[e] = pack_bf16(x[at] * ve[W8 ? e : (e >> 1) * 2], x[at + 1] * ve[W8 ? e : (e >> 1) * 2 + 1]);
       }
       const uint8_t* vb = st[i] + F::BLOCK + g * F::VVEC;
       auto row = [&](int k, int c) { return lds<F::VVEC>(vb + (2 * t + (k & 1) + (k >> 1) * 8) * (DH * F::ES) + c * 8 * F::VVEC); };
+      uint32_t h0 = 0, h1 = 0;   // W8: the fragment of V before, the upper half of the matrix instruction's
       if (!edge) {
+        if constexpr (W8) {
+          pf[0] = turn8x8(pf[0]);
+          pf[1] = turn8x8(pf[1]);
+        }
 #pragma unroll
         for (int c = 0; c < F::VN; ++c) {
           const Words<F::VVEC> v0 = row(0, c), v1 = row(1, c), v2 = row(2, c), v3 = row(3, c);
 #pragma unroll
           for (int w = 0; w < F::VVEC / 4; ++w) {
             cf_pairs<KT>(v0.w[w], v1.w[w], v2.w[w], v3.w[w], [&](int e, uint32_t b0, uint32_t b1) {
-              mma16816<false>(o[c * F::VE + w * (4 / F::ES) + e], pf, b0, b1);
+              const int j = c * F::VE + w * (4 / F::ES) + e;
+              if constexpr (W8) {
+                if (j & 1) {
+                  const uint32_t vf[4] = {h0, b0, h1, b1};
+                  mma16816<false>(o[j / 2], vf, pf[0], pf[1]);
+                }
+                h0 = b0;
+                h1 = b1;
+              } else {
+                mma16816<false>(o[j], pf, b0, b1);
+              }
             });
           }
         }
@@ -619,12 +677,16 @@ __global__ void __launch_bounds__(CF_WARPS * 32, 3) chunk_few_kernel(const __gri
       }
       // V of keys that nobody here attends counts as zero; a NaN or infinite one that only some rows attend must not reach
       // the others through 0 * NaN: it counts as zero, and is put into the sums of its rows as NaN
-      uint32_t ones[4];
+      uint32_t ones[NP];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {   // fragment e: row half e & 1, key tile e >> 1
-        const unsigned bits = att >> ((2 * i + (e >> 1)) * 4 + (e & 1) * 2);
+      for (int e = 0; e < NP; ++e) {
+        const unsigned bits = att >> ((W8 ? i : 2 * i + (e >> 1)) * 4 + (e & 1) * 2);
         ones[e] = (bits & 1u ? 0x3f80u : 0u) | (bits & 2u ? 0x3f800000u : 0u);
         pf[e] &= (bits & 1u ? 0xffffu : 0u) | (bits & 2u ? 0xffff0000u : 0u);   // (an exponent of no entry may be anything)
+        if constexpr (W8) {
+          ones[e] = turn8x8(ones[e]);
+          pf[e] = turn8x8(pf[e]);
+        }
       }
 #pragma unroll
       for (int c = 0; c < F::VN; ++c) {
@@ -639,12 +701,29 @@ __global__ void __launch_bounds__(CF_WARPS * 32, 3) chunk_few_kernel(const __gri
 #pragma unroll
         for (int w = 0; w < F::VVEC / 4; ++w)
           cf_pairs<KT>(v[0].w[w], v[1].w[w], v[2].w[w], v[3].w[w], [&](int e, uint32_t b0, uint32_t b1) {
-            float(&d)[4] = o[c * F::VE + w * (4 / F::ES) + e];
+            const int j = c * F::VE + w * (4 / F::ES) + e;
+            if (W8 && !(j & 1)) {
+              h0 = b0;
+              h1 = b1;
+              return;
+            }
+            float(&d)[4] = o[W8 ? j / 2 : j];
             const uint32_t n0 = __vcmpeq2(b0 & 0x7f807f80u, 0x7f807f80u), n1 = __vcmpeq2(b1 & 0x7f807f80u, 0x7f807f80u);
-            mma16816<false>(d, pf, b0 & ~n0, b1 & ~n1);
-            if (__any_sync(0xffffffffu, (n0 | n1) != 0)) {
-              float cnt[4] = {0.f, 0.f, 0.f, 0.f};
-              mma16816<false>(cnt, ones, n0 & 0x3f803f80u, n1 & 0x3f803f80u);
+            float cnt[4] = {0.f, 0.f, 0.f, 0.f};
+            bool bad;
+            if constexpr (W8) {
+              const uint32_t n2 = __vcmpeq2(h0 & 0x7f807f80u, 0x7f807f80u), n3 = __vcmpeq2(h1 & 0x7f807f80u, 0x7f807f80u);
+              const uint32_t vf[4] = {h0 & ~n2, b0 & ~n0, h1 & ~n3, b1 & ~n1};
+              mma16816<false>(d, vf, pf[0], pf[1]);
+              bad = __any_sync(0xffffffffu, (n0 | n1 | n2 | n3) != 0);
+              const uint32_t nf[4] = {n2 & 0x3f803f80u, n0 & 0x3f803f80u, n3 & 0x3f803f80u, n1 & 0x3f803f80u};
+              if (bad) mma16816<false>(cnt, nf, ones[0], ones[1]);
+            } else {
+              mma16816<false>(d, pf, b0 & ~n0, b1 & ~n1);
+              bad = __any_sync(0xffffffffu, (n0 | n1) != 0);
+              if (bad) mma16816<false>(cnt, ones, n0 & 0x3f803f80u, n1 & 0x3f803f80u);
+            }
+            if (bad) {
 #pragma unroll
               for (int x = 0; x < 4; ++x)
                 if (cnt[x] > 0.f) d[x] = NAN;
@@ -674,21 +753,22 @@ __global__ void __launch_bounds__(CF_WARPS * 32, 3) chunk_few_kernel(const __gri
   float* s_o = reinterpret_cast<float*>(s_dyn);
 #pragma unroll
   for (int r = 0; r < 2; ++r) {
-    l[r] += __shfl_xor_sync(0xffffffffu, l[r], 1);
-    l[r] += __shfl_xor_sync(0xffffffffu, l[r], 2);
-    if (t == 0) {
-      s_m[warp][g + 8 * r] = m[r];
-      s_l[warp][g + 8 * r] = l[r];
+#pragma unroll
+    for (int w = W8 ? 4 : 1; w <= (W8 ? 16 : 2); w *= 2) l[r] += __shfl_xor_sync(0xffffffffu, l[r], w);
+    if ((W8 ? g : t) == 0) {
+      s_m[warp][W8 ? 2 * t + r : g + 8 * r] = m[r];
+      s_l[warp][W8 ? 2 * t + r : g + 8 * r] = l[r];
     }
   }
   constexpr int LD = DH + 4;
 #pragma unroll
-  for (int j = 0; j < DH / 8; ++j) {
-    const int c = j / F::VE, e = j % F::VE;
+  for (int jj = 0; jj < NO; ++jj) {
 #pragma unroll
-    for (int x = 0; x < 4; ++x)
-      if (g + 8 * (x >> 1) < n_row)
-        s_o[(warp * CF_ROWS + g + 8 * (x >> 1)) * LD + (c * 8 + 2 * t + (x & 1)) * F::VE + e] = o[j][x];
+    for (int x = 0; x < 4; ++x) {
+      const int j = W8 ? 2 * jj + (x >> 1) : jj, c = j / F::VE, e = j % F::VE;
+      const int r = W8 ? 2 * t + (x & 1) : g + 8 * (x >> 1), at = W8 ? g : 2 * t + (x & 1);
+      if (r < n_row) s_o[(warp * ROWS + r) * LD + (c * 8 + at) * F::VE + e] = o[jj][x];
+    }
   }
   __syncthreads();
   const PartView pv(a, p, CF_ROWS, DH, it.slot0 + it.split);
@@ -703,7 +783,7 @@ __global__ void __launch_bounds__(CF_WARPS * 32, 3) chunk_few_kernel(const __gri
 #pragma unroll
     for (int w = 0; w < CF_WARPS; ++w) {
       const float f = ex2_approx(s_m[w][r] - mref);
-      const float4 v = *reinterpret_cast<const float4*>(&s_o[(w * CF_ROWS + r) * LD + d]);
+      const float4 v = *reinterpret_cast<const float4*>(&s_o[(w * ROWS + r) * LD + d]);
       L += f * s_l[w][r];
       x[0] += f * v.x;
       x[1] += f * v.y;
@@ -935,8 +1015,35 @@ bool use_tc(const KvPaged& c, int n_heads, int max_q, int max_kv, bool aligned) 
 }
 bool use_both(const KvPaged& c) { return c.type == KV_E4M3 && c.n_seq > 1; }
 
-template <int DH, int KT>
+template <int DH, int KT, int ROWS>
 struct FewTag {};
+
+template <int DH, int KT, int ROWS>
+cudaError_t few_t(cudaStream_t st, const ChunkCall& a, const ChunkHow& w, dim3 grid, int cs) {
+  constexpr int smem = FewShape<DH, KT, ROWS>::SMEM;
+  const cudaError_t e = smem_once<FewTag<DH, KT, ROWS>>(chunk_few_kernel<DH, KT, ROWS>, smem);
+  if (e != cudaSuccess) return e;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(CF_WARPS * 32);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute at[2];
+  int n = 0;
+  if (g_pdl) {
+    at[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[n++].val.programmaticStreamSerializationAllowed = 1;
+  }
+  if (cs > 1) {
+    at[n].id = cudaLaunchAttributeClusterDimension;
+    at[n].val.clusterDim.x = (unsigned)cs;
+    at[n].val.clusterDim.y = at[n].val.clusterDim.z = 1;
+    ++n;
+  }
+  cfg.attrs = at;
+  cfg.numAttrs = (unsigned)n;
+  return cudaLaunchKernelEx(&cfg, chunk_few_kernel<DH, KT, ROWS>, a, w.p, w.per_tok, w.sub, cs);
+}
 
 template <int DH, int KT, typename T>
 cudaError_t chunk_t(cudaStream_t st, const ChunkCall& a, const ChunkHow& w, int* launches) {
@@ -950,9 +1057,6 @@ cudaError_t chunk_t(cudaStream_t st, const ChunkCall& a, const ChunkHow& w, int*
   if (!w.few) {
     e = launch_k(chunk_any_kernel<DH, KT, T>, grid, dim3(CG_KEYS), 0, st, a, w.p);
   } else if constexpr (KT != KV_F32) {
-    constexpr int smem = FewShape<DH, KT>::SMEM;
-    e = smem_once<FewTag<DH, KT>>(chunk_few_kernel<DH, KT>, smem);
-    if (e != cudaSuccess) return e;
     // A cluster per tile: the largest of 8, 4, 2 CTAs whose clusters find room at once, where that leaves a CTA a few rounds
     // (4 at heads of 128, 2 at 64, 1 at 32).  One call of a token each in a captured graph, cluster and split: 12 heads of 64,
     // 500 keys 5.6 and 7.0 us, 1000 keys 6.3 and 7.2, 2000 keys 7.7 and 7.5; 32 heads of 128 on 8, 500 keys 6.8 and 8.4,
@@ -961,23 +1065,18 @@ cudaError_t chunk_t(cudaStream_t st, const ChunkCall& a, const ChunkHow& w, int*
     const long long units = cdiv(a.max_kv, w.p.unit);
     int cs = 8;
     while (cs > 1 && tiles * cs > w.p.target) cs >>= 1;
-    if (cs > 1 && w.may_split && units * 32 <= DH * cs) {
-      cudaLaunchConfig_t cfg = {};
-      cfg.gridDim = dim3((unsigned)(tiles * cs));
-      cfg.blockDim = dim3(CF_WARPS * 32);
-      cfg.dynamicSmemBytes = smem;
-      cfg.stream = st;
-      cudaLaunchAttribute at[2];
-      at[0].id = cudaLaunchAttributeClusterDimension;
-      at[0].val.clusterDim.x = (unsigned)cs;
-      at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
-      at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-      at[1].val.programmaticStreamSerializationAllowed = 1;
-      cfg.attrs = at;
-      cfg.numAttrs = g_pdl ? 2 : 1;
-      return cudaLaunchKernelEx(&cfg, chunk_few_kernel<DH, KT>, a, w.p, w.per_tok, w.sub, cs);
+    const bool clusters = cs > 1 && w.may_split && units * 32 <= DH * cs;
+    const dim3 g = clusters ? dim3((unsigned)(tiles * cs)) : grid;
+    if (!clusters) cs = 1;
+    if constexpr (KT == KV_E4M3) {
+      if ((long long)max_c * (a.n_heads / a.c.n_kv_heads) <= 8)   // (no tile has more rows)
+        e = few_t<DH, KT, 8>(st, a, w, g, cs);
+      else
+        e = few_t<DH, KT, 16>(st, a, w, g, cs);
+    } else {
+      e = few_t<DH, KT, 16>(st, a, w, g, cs);
     }
-    e = launch_k(chunk_few_kernel<DH, KT>, grid, dim3(CF_WARPS * 32), smem, st, a, w.p, w.per_tok, w.sub, 1);
+    if (clusters) return e;
   }
   if (e == cudaSuccess && w.may_split) {
     ++*launches;

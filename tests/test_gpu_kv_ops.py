@@ -250,6 +250,13 @@ def test_rows_at_given_positions(dtype, heads, hk, dh, new, keep):
     assert torch.equal(out, again)
 
 
+@pytest.mark.parametrize("heads,hk,dh,new,past", [(8, 2, 128, 2, 30), (3, 3, 64, 8, 700), (4, 4, 32, 5, 20), (2, 1, 128, 4, 5000)])
+def test_eight_rows_over_8_bit_entries(heads, hk, dh, new, past):
+    """At most 8 rows a K/V head: NaN at later positions; rows at given positions."""
+    test_later_positions_may_hold_anything("e4m3", heads, hk, dh, new, past, math.nan)
+    test_rows_at_given_positions("e4m3", heads, hk, dh, [new, 1, 0, 2], 0.7)
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16", "e4m3"])
 @pytest.mark.parametrize("n", [6, 700])
 def test_positions_that_do_not_ascend_touch_no_other_sequence(dtype, n):
