@@ -209,7 +209,8 @@ __global__ void __launch_bounds__(CG_KEYS) chunk_any_kernel(const __grid_constan
 // From the ring the words go straight into fragments: the order of the head's dimensions inside q.k is free, so a thread's
 // B fragments of S = Q K^T are whole 16-byte pieces of its key's row (Q is loaded in the same order), and the columns of O are
 // dealt out so that a thread's B fragments of O = P V are 16-byte pieces of four keys' rows, pairs of keys packed by byte
-// permutes.
+// permutes.  (V lies in four groups 32 bytes apart: in one piece the rows that neighbours read lay under each other, 4 wavefronts
+// where one is enough.)
 // e4m3: K as fp16, one conversion for two codes (bf16 takes four instructions), with Q as fp16 too, each row moved by a power
 // of two so that its largest element lies in [2^14, 2^15): exact down to 2^-28 of it.  V as bf16, since P has to keep bf16's
 // range (a position of little weight may hold a V of any size).  K's exponent scales S, V's scales P.
@@ -342,7 +343,10 @@ struct FewShape {
   static constexpr int KVEC = DH * ES / 4 < 16 ? DH * ES / 4 : 16, KN = DH * ES / 4 / KVEC, KE = KVEC / ES;   // K pieces of a thread
   static constexpr int VVEC = DH * ES / 8 < 16 ? DH * ES / 8 : 16, VN = DH * ES / 8 / VVEC, VE = VVEC / ES;   // V pieces
   static constexpr int BLOCK = 16 * DH * ES;               // bytes of a block of one head
-  static constexpr int STAGE = 2 * BLOCK + (KT == KV_E4M3 ? 32 : 0);   // K, V, exponents
+  // V in groups of 4 keys, 32 bytes apart: the four keys' rows that neighbours read lie under different banks
+  static constexpr int GROUP = BLOCK / 4 + 32, EXPS = BLOCK + 4 * GROUP;
+  static constexpr int BYTES = 2 * BLOCK + (KT == KV_E4M3 ? 32 : 0);   // of a stage: K, V, exponents
+  static constexpr int STAGE = EXPS + (KT == KV_E4M3 ? 32 : 0);
   static constexpr int RING = CF_WARPS * STAGES * STAGE, MERGE = CF_WARPS * ROWS * (DH + 4) * 4;
   static constexpr int SMEM = RING > MERGE ? RING : MERGE;
 };
@@ -431,12 +435,14 @@ __global__ void __launch_bounds__(CF_WARPS * 32, 3) chunk_few_kernel(const __gri
       uint8_t* st = ring + i % F::STAGES * F::STAGE;
       uint64_t* bar = &s_full[warp][i % F::STAGES];
       const size_t e = ((size_t)blk * a.c.n_kv_heads + kvh) * 16;
-      mbar_expect_tx(bar, F::STAGE);
+      mbar_expect_tx(bar, F::BYTES);
       bulk_load(st, (const uint8_t*)a.c.k + e * (DH * F::ES), F::BLOCK, bar);
-      bulk_load(st + F::BLOCK, (const uint8_t*)a.c.v + e * (DH * F::ES), F::BLOCK, bar);
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        bulk_load(st + F::BLOCK + q * F::GROUP, (const uint8_t*)a.c.v + e * (DH * F::ES) + q * (F::BLOCK / 4), F::BLOCK / 4, bar);
       if constexpr (KT == KV_E4M3) {
-        bulk_load(st + 2 * F::BLOCK, a.c.k_exp + e, 16, bar);
-        bulk_load(st + 2 * F::BLOCK + 16, a.c.v_exp + e, 16, bar);
+        bulk_load(st + F::EXPS, a.c.k_exp + e, 16, bar);
+        bulk_load(st + F::EXPS + 16, a.c.v_exp + e, 16, bar);
       }
     }
     __syncwarp();
@@ -504,6 +510,9 @@ __global__ void __launch_bounds__(CF_WARPS * 32, 3) chunk_few_kernel(const __gri
     }
   }
 
+  // Which key of a block is which index of the matrix instructions is free, too: 4 q .. 4 q + 3 are 2 q, 2 q + 1, 8 + 2 q and
+  // 9 + 2 q, so that a thread's V rows are one group
+  const int key_g = 4 * (g >> 1) + (g & 1);   // index g; key_g + 2: index 8 + g
   float o[NO][4], m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
 #pragma unroll
   for (int j = 0; j < NO; ++j) o[j][0] = o[j][1] = o[j][2] = o[j][3] = 0.f;
@@ -532,11 +541,11 @@ __global__ void __launch_bounds__(CF_WARPS * 32, 3) chunk_few_kernel(const __gri
     float s[NS][4];
 #pragma unroll
     for (int i = 0; i < F::NB; ++i) {
-      Words<F::KVEC> k[2][F::KN];   // keys g and g + 8
+      Words<F::KVEC> k[2][F::KN];   // of keys key_g and key_g + 2
 #pragma unroll
       for (int nt = 0; nt < 2; ++nt)
 #pragma unroll
-        for (int c = 0; c < F::KN; ++c) k[nt][c] = lds<F::KVEC>(st[i] + (nt * 8 + g) * (DH * F::ES) + (c * 4 + t) * F::KVEC);
+        for (int c = 0; c < F::KN; ++c) k[nt][c] = lds<F::KVEC>(st[i] + (key_g + 2 * nt) * (DH * F::ES) + (c * 4 + t) * F::KVEC);
 #pragma unroll
       for (int nt = 0; nt < (W8 ? 1 : 2); ++nt) {
         float(&d)[4] = s[W8 ? i : 2 * i + nt];
@@ -556,10 +565,10 @@ __global__ void __launch_bounds__(CF_WARPS * 32, 3) chunk_few_kernel(const __gri
             }
           }
         if constexpr (KT == KV_E4M3 && W8) {
-          const float e0 = exp_scale(st[i][2 * F::BLOCK + g]), e1 = exp_scale(st[i][2 * F::BLOCK + 8 + g]);
+          const float e0 = exp_scale(st[i][F::EXPS + key_g]), e1 = exp_scale(st[i][F::EXPS + key_g + 2]);
           d[0] *= e0 * rs[0]; d[1] *= e0 * rs[1]; d[2] *= e1 * rs[0]; d[3] *= e1 * rs[1];
         } else if constexpr (KT == KV_E4M3) {
-          const uint32_t e = *reinterpret_cast<const uint16_t*>(st[i] + 2 * F::BLOCK + nt * 8 + 2 * t);
+          const uint32_t e = *reinterpret_cast<const uint16_t*>(st[i] + F::EXPS + 4 * t + 2 * nt);
           const float e0 = exp_scale(e & 0xff), e1 = exp_scale(e >> 8);
           d[0] *= e0 * rs[0]; d[1] *= e1 * rs[0]; d[2] *= e0 * rs[1]; d[3] *= e1 * rs[1];
         } else {
@@ -575,7 +584,7 @@ __global__ void __launch_bounds__(CF_WARPS * 32, 3) chunk_few_kernel(const __gri
       for (int x = 0; x < NS; ++x)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const int key = b * 16 + (W8 ? x * 16 + g + 8 * (e >> 1) : x * 8 + 2 * t + (e & 1));
+          const int key = b * 16 + (W8 ? x * 16 + key_g + 2 * (e >> 1) : (x >> 1) * 16 + 4 * t + 2 * (x & 1) + (e & 1));
           const bool on = here[W8 ? x : x / 2] && key < min(lim[rh(e)], k_end);
           att |= (unsigned)on << (x * 4 + e);
           if (!on) s[x][e] = -INFINITY;
@@ -624,18 +633,16 @@ __global__ void __launch_bounds__(CF_WARPS * 32, 3) chunk_few_kernel(const __gri
     for (int i = 0; i < F::NB; ++i) {
       constexpr int NP = W8 ? 2 : 4;
       uint32_t pf[NP];
-      float ve[4] = {1.f, 1.f, 1.f, 1.f};   // V's scales: of keys 2 t, 2 t + 1, and 8 on (W8: of keys g, g + 8)
+      float ve[4] = {1.f, 1.f, 1.f, 1.f};   // V's scales: of keys 4 t to 4 t + 3 (W8: of key_g, key_g + 2)
       if constexpr (KT == KV_E4M3) {
-        const uint8_t* vp = st[i] + 2 * F::BLOCK + 16;
+        const uint8_t* vp = st[i] + F::EXPS + 16;
         if constexpr (W8) {
-          ve[0] = exp_scale(vp[g]);
-          ve[1] = exp_scale(vp[8 + g]);
+          ve[0] = exp_scale(vp[key_g]);
+          ve[1] = exp_scale(vp[key_g + 2]);
         } else {
-          const uint32_t x = *reinterpret_cast<const uint16_t*>(vp + 2 * t), y = *reinterpret_cast<const uint16_t*>(vp + 8 + 2 * t);
-          ve[0] = exp_scale(x & 0xff);
-          ve[1] = exp_scale(x >> 8);
-          ve[2] = exp_scale(y & 0xff);
-          ve[3] = exp_scale(y >> 8);
+          const uint32_t x = *reinterpret_cast<const uint32_t*>(vp + 4 * t);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) ve[e] = exp_scale(x >> (8 * e) & 0xff);
         }
       }
       // fragment e of P: elements 2 e and 2 e + 1 of the block's S
@@ -645,8 +652,8 @@ __global__ void __launch_bounds__(CF_WARPS * 32, 3) chunk_few_kernel(const __gri
         const int at = (e & 1) * 2;
         pf[e] = pack_bf16(x[at] * ve[W8 ? e : (e >> 1) * 2], x[at + 1] * ve[W8 ? e : (e >> 1) * 2 + 1]);
       }
-      const uint8_t* vb = st[i] + F::BLOCK + g * F::VVEC;
-      auto row = [&](int k, int c) { return lds<F::VVEC>(vb + (2 * t + (k & 1) + (k >> 1) * 8) * (DH * F::ES) + c * 8 * F::VVEC); };
+      const uint8_t* vb = st[i] + F::BLOCK + t * F::GROUP + g * F::VVEC;
+      auto row = [&](int k, int c) { return lds<F::VVEC>(vb + k * (DH * F::ES) + c * 8 * F::VVEC); };   // key 4 t + k
       uint32_t h0 = 0, h1 = 0;   // W8: the fragment of V before, the upper half of the matrix instruction's
       if (!edge) {
         if constexpr (W8) {
@@ -694,7 +701,7 @@ __global__ void __launch_bounds__(CF_WARPS * 32, 3) chunk_few_kernel(const __gri
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
           v[k] = row(k, c);
-          if (!here[i] || (b + i) * 16 + 2 * t + (k & 1) + (k >> 1) * 8 >= k_end)
+          if (!here[i] || (b + i) * 16 + 4 * t + k >= k_end)
 #pragma unroll
             for (int w = 0; w < F::VVEC / 4; ++w) v[k].w[w] = 0;
         }
