@@ -222,13 +222,13 @@ __global__ void __launch_bounds__(CG_KEYS) chunk_any_kernel(const __grid_constan
 //
 // ROWS = 8: where no tile has more than 8 rows the keys are the 16 rows of the matrix instructions and the queries their 8
 // columns (S^T = K Q^T, O^T = V^T P^T), which halves them and the softmax; the same words of K and V in the same registers, P's
-// fragments turned round in between.  For 8-bit entries, which are bound by instructions: a token of 32 heads of 128
-// over 30011 keys 47.3 us, 54.5 with 16 rows; 16 sequences of a token, 32 heads on 8, 21.4 and 23.8.  bf16 is bound by memory
-// and gains nothing (32 heads, 4000 keys 18.7 and 18.8; 8 sequences of 12 heads of 64 20.0 and 18.2).
+// fragments turned round in between.  Against 16 rows: 8 bits, a token of 32 heads of 128 over 30011 keys 47.3 us for 54.5, 16
+// sequences of a token, 32 heads on 8, 21.4 for 23.8; bf16, a token of 32 heads over 2000 keys 9.8 for 10.6, 8 sequences over up to
+// 4000 56.3 for 57.2.
 //
-// Measured: that token over 30011 keys, 8 bits (248 MB) 5.2 TB/s, bound by instruction issue (12 warps an SM, each waiting on its
-// own conversions and exponentials); over 30000 in bf16 (492 MB) 81.2 us, 6.1 TB/s, near the memory's rate; 4 to 5 tokens of
-// 4 sequences over 8.4 thousand keys, bf16 (139 MB), 32.7 us.
+// Measured: that token over 30011 keys, 8 bits (248 MB) 45.5 us, 5.4 TB/s, bound by instruction issue and latency (12 warps an SM,
+// each waiting on its own conversions and reads); 8 sequences over up to 4000 keys in bf16 (295 MB) 56.3 us, 5.2 TB/s; 4 to 5
+// tokens of 4 sequences over 8.4 thousand keys, bf16 (139 MB), 31.2 us, 8 of them launches and the join.
 // ---------------------------------------------------------------------------------------------
 constexpr int CF_WARPS = 4, CF_ROWS = 16;
 constexpr float CF_RAISE = 8.f;   // the running maximum is raised once a score exceeds it by 2^8: weights stay below 256
@@ -1075,14 +1075,8 @@ cudaError_t chunk_t(cudaStream_t st, const ChunkCall& a, const ChunkHow& w, int*
     const bool clusters = cs > 1 && w.may_split && units * 32 <= DH * cs;
     const dim3 g = clusters ? dim3((unsigned)(tiles * cs)) : grid;
     if (!clusters) cs = 1;
-    if constexpr (KT == KV_E4M3) {
-      if ((long long)max_c * (a.n_heads / a.c.n_kv_heads) <= 8)   // (no tile has more rows)
-        e = few_t<DH, KT, 8>(st, a, w, g, cs);
-      else
-        e = few_t<DH, KT, 16>(st, a, w, g, cs);
-    } else {
-      e = few_t<DH, KT, 16>(st, a, w, g, cs);
-    }
+    const bool eight = (long long)max_c * (a.n_heads / a.c.n_kv_heads) <= 8;   // no tile has more rows
+    e = eight ? few_t<DH, KT, 8>(st, a, w, g, cs) : few_t<DH, KT, 16>(st, a, w, g, cs);
     if (clusters) return e;
   }
   if (e == cudaSuccess && w.may_split) {
