@@ -81,9 +81,11 @@ typedef struct {
                           cross-attend to up to max_src encoder states per sequence
                           (adept_set_cross_source); 0: no cross-attention */
   int kv_type;         /* 0: the cache holds the model's type; ADEPT_KV_E4M3 (bf16 decoders, blocks of 16):
-                          8-bit floats with an exponent per position and head, half the memory and half of what
-                          attention reads; one layer's cache in bf16 besides, for staging (not for the
-                          cross-attention's source cache) */
+                          8-bit floats with an exponent per position and head, about half the memory of a
+                          bf16 cache and half of what attention reads of it.  Held besides, in bf16: two layers'
+                          caches (staging of new entries, and what the attention of longer chunks widens entries
+                          into) and a block per sequence and layer (the steps' staging).  Not for the
+                          cross-attention's source cache */
 } adept_config;
 
 /* One named weight tensor.  `data` may be a host or a device pointer (it is read
@@ -477,7 +479,9 @@ ADEPT_API adept_status adept_kv_gather(const adept_kv_cache* c, int n_rows, int 
 ADEPT_API adept_status adept_chunk_attention(const adept_kv_cache* c, int n_heads, int n_rows, const void* d_q, int64_t ld_q,
                                    const int32_t* d_q_start, const int32_t* d_kv_len, const int32_t* d_row_pos,
                                    int max_q_len, int max_kv_len, void* d_out, int64_t ld_out, void* d_ws, int64_t ws_bytes, void* stream);
-/* Bytes of d_ws that such a call needs, or -1 (bad arguments). */
+/* Bytes of d_ws that such a call needs, or -1 (bad arguments); a call of smaller bounds or fewer sequences
+ * on the same pool needs no more.  For longer chunks over an 8-bit cache they hold K and V in bf16, for as many
+ * blocks as the pool has or as n_seq sequences of max_kv_len positions take, whichever are fewer. */
 ADEPT_API int64_t adept_chunk_attention_workspace(const adept_kv_cache* c, int n_heads, int n_rows, int max_q_len,
                                         int max_kv_len);
 /* Synchronise `stream`, then read and clear the cache's error word: DEVICE_INPUT, TIMEOUT or OK.

@@ -21,8 +21,19 @@ int ct_sms() {
 
 // Workspace: the parts, a word for time-outs, the widened K and V.
 size_t ct_parts_bytes(int dh) { return (ct_ws_floats(ct_sms(), dh) * 4 + 16 + 255) / 256 * 256; }
+// Widened entries lie as their blocks lie in the pool, or, where the call's sequences can hold fewer blocks than the pool has, in
+// order of (sequence, block): blocks per sequence then, else 0.  Never more than the pool, so that every size here grows with
+// n_seq and max_kv (a model takes its workspace once, for the largest of both).
+int ct_wide(const KvPaged& c, int max_kv) {
+  const long long per = cdiv(max_kv, 16);
+  return (long long)c.n_seq * per < c.n_blocks ? (int)per : 0;
+}
+size_t ct_wide_blocks(const KvPaged& c, int max_kv) {
+  const int per = ct_wide(c, max_kv);
+  return per ? (size_t)c.n_seq * per : (size_t)c.n_blocks;
+}
 size_t ct_wide_bytes(const KvPaged& c, int max_kv) {   // of K, or of V
-  return c.type == KV_E4M3 ? (size_t)c.n_seq * cdiv(max_kv, 16) * c.n_kv_heads * 16 * c.head_dim * 2 : 0;
+  return c.type == KV_E4M3 ? ct_wide_blocks(c, max_kv) * c.n_kv_heads * 16 * c.head_dim * 2 : 0;
 }
 
 void* wide_k(const ChunkCall& a) { return (char*)a.part + ct_parts_bytes(a.c.head_dim); }
@@ -37,8 +48,8 @@ cudaError_t launch_t(cudaStream_t st, CtParams& p, int* launches) {
   void *k = c.k, *v = c.v;
   uint64_t rows = (uint64_t)c.n_blocks * c.n_kv_heads * 16;
   if (c.type == KV_E4M3) {
-    p.wide = cdiv(p.a.max_kv, 16);
-    rows = (uint64_t)c.n_seq * p.wide * c.n_kv_heads * 16;
+    p.wide = ct_wide(c, p.a.max_kv);
+    rows = (uint64_t)ct_wide_blocks(c, p.a.max_kv) * c.n_kv_heads * 16;
     k = wide_k(p.a);
     v = wide_v(p.a);
   }
@@ -56,10 +67,9 @@ cudaError_t launch_t(cudaStream_t st, CtParams& p, int* launches) {
 
 }  // namespace
 
-bool chunk_tc_takes(const KvPaged& c, int n_heads, int max_kv) {
-  const long long blocks = c.type == KV_E4M3 ? (long long)c.n_seq * cdiv(max_kv, 16) : c.n_blocks;
+bool chunk_tc_takes(const KvPaged& c, int n_heads) {
   return c.type != KV_F32 && c.block_tokens == 16 && (c.head_dim == 64 || c.head_dim == 128) &&
-         n_heads / c.n_kv_heads <= CT_BM && blocks * c.n_kv_heads * 16 < (1ll << 31) && tc_gemm_supported();
+         n_heads / c.n_kv_heads <= CT_BM && (long long)c.n_blocks * c.n_kv_heads * 16 < (1ll << 31);
 }
 
 size_t chunk_tc_workspace(const KvPaged& c, int max_kv) { return ct_parts_bytes(c.head_dim) + 2 * ct_wide_bytes(c, max_kv); }
@@ -71,8 +81,8 @@ bool chunk_tc_fits(const KvPaged& c, int n_heads, int n_rows, int max_q, int max
 }
 
 cudaError_t launch_chunk_widen(cudaStream_t st, const ChunkCall& a, int* launches) {
-  const int wide = cdiv(a.max_kv, 16);
-  const dim3 grid((unsigned)std::min<long long>(ct_sms() * 8, 2ll * wide * a.c.n_seq));
+  const int wide = ct_wide(a.c, a.max_kv);
+  const dim3 grid((unsigned)std::min<long long>(ct_sms() * 8, 2ll * cdiv(a.max_kv, 16) * a.c.n_seq));
   ++*launches;
   return launch_k(a.c.head_dim == 128 ? chunk_widen_kernel<128> : chunk_widen_kernel<64>, grid, dim3(CW_THREADS), 0, st, a, wide,
                   (bf16*)wide_k(a), (bf16*)wide_v(a));

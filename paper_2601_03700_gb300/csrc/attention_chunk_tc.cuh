@@ -59,7 +59,7 @@ struct CtParams {
   CUtensorMap qmap;         // Q as [n_rows][n_heads][d_h], box {64, heads of a group, ts}
   int ts;                   // tokens of a sub-tile
   int runs;                 // CTAs
-  int wide;                 // > 0: the maps are of widened entries, `wide` blocks per sequence in order
+  int wide;                 // > 0: the maps are of widened entries, `wide` blocks per sequence in order (0: as the pool's)
   unsigned* no_err;         // where time-outs go without an error word (the workspace's last word)
 };
 
@@ -721,7 +721,9 @@ __global__ void __launch_bounds__(CtShape<DH>::THREADS, 1) chunk_tc_kernel(const
 }
 
 // Entries of 8 bits as bf16.  Work: the blocks of positions of this launch's sequences, K and V apart, all heads of one at a time;
-// CTA i of n takes the i-th of n equal runs of them (the lengths are known on the device only).
+// CTA i of n takes the i-th of n equal runs of them (the lengths are known on the device only).  A block goes to its place in
+// the pool, or (wide > 0) to block b of `wide` of its sequence; one that several sequences share is written more than once there,
+// with the same values.
 constexpr int CW_THREADS = 256;
 template <int DH>
 __global__ void __launch_bounds__(CW_THREADS) chunk_widen_kernel(const __grid_constant__ ChunkCall a, int wide, bf16* k_out,
@@ -772,7 +774,7 @@ __global__ void __launch_bounds__(CW_THREADS) chunk_widen_kernel(const __grid_co
   for (long long u = s_u0; u < s_u1; ++u) {
     const int blk = a.c.table[(size_t)seq * a.c.max_blocks + b], is_v = (int)(u & 1);
     if (blk >= 0 && blk < a.c.n_blocks) {
-      const size_t from = (size_t)blk * a.c.n_kv_heads * 16, to = ((size_t)seq * wide + b) * a.c.n_kv_heads * 16;
+      const size_t from = (size_t)blk * a.c.n_kv_heads * 16, to = (wide ? (size_t)seq * wide + b : (size_t)blk) * a.c.n_kv_heads * 16;
       const uint8_t* codes = (const uint8_t*)(is_v ? a.c.v : a.c.k) + from * DH;
       const uint8_t* exps = (is_v ? a.c.v_exp : a.c.k_exp) + from;
       bf16* out = (is_v ? v_out : k_out) + to * DH;

@@ -52,10 +52,12 @@ struct ChunkCall {
   float scale_log2;   // log2(e) / sqrt(head_dim)
   float* part;        // workspace
 };
+// Bytes of `part` that a call of these bounds needs; no call of fewer sequences or smaller bounds on the same pool needs more.
 size_t chunk_workspace(const KvPaged& c, int n_heads, int max_q, int max_kv);
 cudaError_t launch_chunk_attention(cudaStream_t st, const ChunkCall& a, int* launches);
-// The tcgen05 kernel (attention_chunk_tc.cu): what it takes (rows on 16 bytes besides), its workspace, its launches.
-bool chunk_tc_takes(const KvPaged& c, int n_heads, int max_kv);
+// The tcgen05 kernel (attention_chunk_tc.cu): what it takes (rows on 16 bytes and an sm_100-family GPU besides), its workspace,
+// its launches.
+bool chunk_tc_takes(const KvPaged& c, int n_heads);
 size_t chunk_tc_workspace(const KvPaged& c, int max_kv);
 // Whether a call's (tile, KV head, key tile) triples fit 31 bits (hours of work otherwise).
 bool chunk_tc_fits(const KvPaged& c, int n_heads, int n_rows, int max_q, int max_kv);

@@ -157,6 +157,7 @@ struct adept_model {
   std::vector<int> h_ext;
   int *d_ext = nullptr, *ext_start = nullptr, *ext_pos = nullptr;
   float* ext_ws = nullptr;
+  size_t ext_ws_bytes = 0;
   int32_t* calib_exit = nullptr; // threshold calibration: exit layers of a calibration pass
   // standardisation statistics of X_out handed from the O projection to the FFN input
   float2* tile_stats = nullptr;                // [DG_MAX_M][D / 32] (mean, M2) of X_out tiles
@@ -1169,6 +1170,10 @@ static void extend_attention(adept_model* m, cudaStream_t st, const ExtendPass& 
   a.max_kv = e.max_kv;
   a.scale_log2 = 1.4426950408889634f / sqrtf((float)m->dh);
   a.part = m->ext_ws;
+  if (chunk_workspace(a.c, a.n_heads, a.max_q, a.max_kv) > m->ext_ws_bytes) {
+    m->deferred = fail(m, ADEPT_ERR_CAPACITY, "chunk attention: a pass above the workspace");
+    return;
+  }
   int n = 0;
   const cudaError_t err = launch_chunk_attention(st, a, &n);
   m->launches += 1 + n;
@@ -1827,13 +1832,13 @@ static bool adamw_ok(const adept_adamw* hp) {
 static adept_status extend_init(adept_model* m) {
   if (m->ext_ws) return ADEPT_OK;
   const int B = m->cfg.max_batch;
-  // (the bound over every batch and length)
-  const size_t ws = std::max(chunk_workspace(paged_view(m, 0, B), m->H, m->T_max, m->max_blocks_per_seq * m->cfg.kv_block_tokens),
-                             chunk_workspace(paged_view(m, 0, B), m->H, 1, m->max_blocks_per_seq * m->cfg.kv_block_tokens));
+  // (no smaller batch, pass or length needs more)
+  const size_t ws = chunk_workspace(paged_view(m, 0, B), m->H, m->T_max, m->max_blocks_per_seq * m->cfg.kv_block_tokens);
   if (!m->d_ext) TRY(dalloc_t(m, &m->d_ext, (size_t)2 * B + 1));
   if (!m->ext_start) TRY(dalloc_t(m, &m->ext_start, (size_t)B + 1));
   if (!m->ext_pos) TRY(dalloc_t(m, &m->ext_pos, (size_t)m->T_max));
-  return dalloc(m, (void**)&m->ext_ws, std::max<size_t>(ws, 16));
+  m->ext_ws_bytes = std::max<size_t>(ws, 16);
+  return dalloc(m, (void**)&m->ext_ws, m->ext_ws_bytes);
 }
 
 // The chunks of a pass come from the host: a replayed graph would read them again, stale.
