@@ -1018,7 +1018,10 @@ int few_tokens(const KvPaged& c, int n_heads) {
   const long long tiles = 24ll * 128 / ((long long)c.n_seq * c.n_kv_heads * c.head_dim) + (c.type == KV_E4M3 ? 4 : 0);
   return (int)std::max(1ll, tiles) * std::max(1, CF_ROWS / (n_heads / c.n_kv_heads));
 }
-bool use_tc(const KvPaged& c, int n_heads, int max_q) { return max_q > few_tokens(c, n_heads) && chunk_tc_takes(c, n_heads); }
+// (no positions at all: the rows' zeros are the few-row kernel's, as there is nothing to widen or to map)
+bool use_tc(const KvPaged& c, int n_heads, int max_q, int max_kv) {
+  return max_kv > 0 && max_q > few_tokens(c, n_heads) && chunk_tc_takes(c, n_heads);
+}
 bool use_both(const KvPaged& c) { return c.type == KV_E4M3 && c.n_seq > 1; }
 
 template <int DH, int KT, int ROWS>
@@ -1112,7 +1115,7 @@ size_t round256(size_t x) { return (x + 255) / 256 * 256; }
 size_t chunk_workspace(const KvPaged& c, int n_heads, int max_q, int max_kv) {
   const size_t any = how_bytes(chunk_how(c, n_heads, max_kv, false), c), few = how_bytes(chunk_how(c, n_heads, max_kv, true), c);
   size_t tc = few;
-  if (use_tc(c, n_heads, max_q)) tc = (use_both(c) ? round256(few) : 0) + chunk_tc_workspace(c, max_kv);
+  if (use_tc(c, n_heads, max_q, max_kv)) tc = (use_both(c) ? round256(few) : 0) + chunk_tc_workspace(c, max_kv);
   return std::max(any, tc);
 }
 
@@ -1123,7 +1126,7 @@ cudaError_t launch_chunk_attention(cudaStream_t st, const ChunkCall& a0, int* la
   a.late = 0;
   *launches = 0;
   const bool aligned = (((uintptr_t)a.q | (uintptr_t)a.out) & 15) == 0 && a.ld_q % 8 == 0 && a.ld_out % 8 == 0;
-  if (!aligned || !use_tc(a.c, a.n_heads, a.max_q) || !tc_gemm_supported()) return chunk_simple(st, a, aligned, launches);
+  if (!aligned || !use_tc(a.c, a.n_heads, a.max_q, a.max_kv) || !tc_gemm_supported()) return chunk_simple(st, a, aligned, launches);
   if (a.c.type != KV_E4M3) return launch_chunk_tc(st, a, launches);
   ChunkCall t = a;   // the tcgen05 kernel's share
   if (use_both(a.c)) {
