@@ -469,7 +469,7 @@ ADEPT_API adept_status adept_kv_gather(const adept_kv_cache* c, int n_rows, int 
  *                tokens that are still active where others have left); NULL: the last positions
  *   max_q_len, max_kv_len   bounds on a sequence's rows and positions; a sequence beyond them, or with
  *                rows outside 0 .. n_rows, flags DEVICE_INPUT and is left out, as is a key whose block
- *                is out of range
+ *                is out of range (a row of such keys alone, or of scores that are all -infinity, gives zeros)
  *   d_ws         adept_chunk_attention_workspace bytes on 16 bytes (NULL where that is 0), of any
  *                contents; calls that may overlap on the GPU need one each
  * For the same lengths a call's results are the same bits every time.

@@ -3,8 +3,9 @@
 //
 //   out = sum_k exp(s_k - m) v_k / sum_k exp(s_k - m),   s_k = q . k_k / sqrt(head_dim),   m = max s_k
 //
-// in one pass over the keys with the running maximum and sum (fp32, exponentials in base 2).  A token without keys (a chunk
-// longer than kv_len) gives zeros.  What lies behind a token's position is never used: neither scores nor V entries of
+// in one pass over the keys with the running maximum and sum (fp32, exponentials in base 2).  A row that no key gives any weight
+// (a chunk longer than kv_len, no block there, all scores -infinity) gives zeros: its sum is zero, as no other row's is (the
+// score that last raised the maximum has weight 1, a NaN score gives a sum of NaN).  What lies behind a token's position is never used: neither scores nor V entries of
 // masked positions enter a sum, so NaN or infinities there do not spread.  Keys in blocks that the table does not hold
 // (negative, out of range) are left out and flagged.
 //
@@ -195,7 +196,7 @@ __global__ void __launch_bounds__(CG_KEYS) chunk_any_kernel(const __grid_constan
       pv.o[r * DH + x] = o;
     else
       ((T*)a.out)[(size_t)(it.q0 + j0 + r) * a.ld_out + (size_t)h * DH + x] =
-          from_f<T>(chunk_lim(a, it.q0, it.c, it.len, j0 + r) == 0 ? 0.f : o / s_corr[r]);
+          from_f<T>(s_corr[r] == 0.f ? 0.f : o / s_corr[r]);
   }
 }
 
@@ -808,7 +809,7 @@ __global__ void __launch_bounds__(CF_WARPS * 32, 3) chunk_few_kernel(const __gri
       *reinterpret_cast<float4*>(pv.o + r * DH + d) = make_float4(x[0], x[1], x[2], x[3]);
       if (d == 0) *reinterpret_cast<float2*>(pv.ml + r * 2) = make_float2(M, L);
     } else {
-      const float inv = keys_of(j) == 0 ? 0.f : 1.f / L;
+      const float inv = L == 0.f ? 0.f : 1.f / L;
       uint2 y = make_uint2(pack_bf16(x[0] * inv, x[1] * inv), pack_bf16(x[2] * inv, x[3] * inv));
       *reinterpret_cast<uint2*>((bf16*)a.out + (size_t)(it.q0 + j0 + j) * a.ld_out + (size_t)(kvh * group + gq) * DH + d) = y;
     }
@@ -845,7 +846,7 @@ __global__ void __launch_bounds__(CF_WARPS * 32, 3) chunk_few_kernel(const __gri
         x[2] += f * x8[c].z;
         x[3] += f * x8[c].w;
       }
-      const float inv = keys_of(j) == 0 ? 0.f : 1.f / L;
+      const float inv = L == 0.f ? 0.f : 1.f / L;
       *reinterpret_cast<uint2*>((bf16*)a.out + (size_t)(it.q0 + j0 + j) * a.ld_out + (size_t)(kvh * group + gq) * DH + d) =
           make_uint2(pack_bf16(x[0] * inv, x[1] * inv), pack_bf16(x[2] * inv, x[3] * inv));
     }
@@ -962,7 +963,7 @@ __global__ void __launch_bounds__(CJ_THREADS) chunk_join_kernel(const __grid_con
     const int h = it.group / sub * group + g;
     T* dst = (T*)a.out + (size_t)(it.q0 + j0 + j) * a.ld_out + (size_t)h * DH + d;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) dst[e] = from_f<T>(chunk_lim(a, it.q0, it.c, it.len, j0 + j) == 0 ? 0.f : x.o[e] / x.l);
+    for (int e = 0; e < 4; ++e) dst[e] = from_f<T>(x.l == 0.f ? 0.f : x.o[e] / x.l);
   }
 }
 

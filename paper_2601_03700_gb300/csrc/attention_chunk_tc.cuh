@@ -194,9 +194,8 @@ __device__ __forceinline__ int ct_start(int total, int runs, int i) { return tot
 // weighted V, four columns of all rows after the other (a warp of rows writes whole lines).
 struct CtNote {
   int u0;             // first unit of the tile, -1: the run begins with a tile, or is empty
-  int row0, kvh, pos0, n_tok;   // the tile's first row of Q, KV head, first position, tokens
-  int pad[3];         // (32 bytes: what follows is read 16 at a time)
-};
+  int row0, kvh, n_tok;   // the tile's first row of Q, KV head, tokens
+};   // (16 bytes, as what follows is read)
 struct CtWs {
   CtNote* note;
   float* ml;
@@ -375,7 +374,7 @@ __global__ void __launch_bounds__(CtShape<DH>::THREADS, 1) chunk_tc_kernel(const
   CtTile x = s_tile;
   if (tid == 0) {   // the join's note: what tile this run begins inside of
     const int t0 = x.tile * tq;
-    CtWs(p).note[run] = CtNote{u < u_end && u > x.u0 ? x.u0 : -1, x.q0 + t0, x.kvh, x.len - x.c + t0, min(tq, x.c - t0), {0, 0, 0}};
+    CtWs(p).note[run] = CtNote{u < u_end && u > x.u0 ? x.u0 : -1, x.q0 + t0, x.kvh, min(tq, x.c - t0)};
   }
   CtSeg g{};
   bool ok = true;
@@ -487,7 +486,7 @@ __global__ void __launch_bounds__(CtShape<DH>::THREADS, 1) chunk_tc_kernel(const
       if (sub == 0 || g.n_tok > ts) {
         if (g.whole) {
           // through the warp's stage, 32 columns at a time, so that whole sectors are written
-          const float inv = lim == 0 ? 0.f : 1.f / l;
+          const float inv = l == 0.f ? 0.f : 1.f / l;
           bf16* out = (bf16*)a.out + (size_t)(g.x.q0 + g.t0) * a.ld_out + (size_t)g.x.kvh * group * DH;
 #pragma unroll
           for (int c = 0; c < DH / 32; ++c) {
@@ -861,7 +860,7 @@ __global__ void __launch_bounds__(256) chunk_tc_join_kernel(const __grid_constan
         o[3] += x * v[k].w;
       }
     }
-    const float inv = (a.row_pos ? a.row_pos[n.row0 + tok] : n.pos0 + tok) < 0 ? 0.f : 1.f / l;
+    const float inv = l == 0.f ? 0.f : 1.f / l;
     const __nv_bfloat162 y0 = __floats2bfloat162_rn(o[0] * inv, o[1] * inv), y1 = __floats2bfloat162_rn(o[2] * inv, o[3] * inv);
     *reinterpret_cast<uint2*>((bf16*)a.out + (size_t)(n.row0 + tok) * a.ld_out + (size_t)(n.kvh * group + rr % group) * DH + d4 * 4) =
         make_uint2(*reinterpret_cast<const uint32_t*>(&y0), *reinterpret_cast<const uint32_t*>(&y1));

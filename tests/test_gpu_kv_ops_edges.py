@@ -1,9 +1,11 @@
-"""Calls at the edges of what the operators on a paged K/V cache take: sequences that hold nothing at all."""
+"""Calls at the edges of what the operators on a paged K/V cache take: sequences that hold nothing, or nothing that is there."""
+import math
+
 import pytest
 import torch
 
 import paper_2601_03700_gb300 as adept
-from test_gpu_kv_ops import _i32, _lib, make_q  # noqa: F401  (_lib: the module's fixture)
+from test_gpu_kv_ops import _i32, _lib, assert_attention, attend, make_cache, make_q  # noqa: F401  (_lib: the module's fixture)
 
 pytestmark = pytest.mark.gpu
 
@@ -19,3 +21,53 @@ def test_no_positions_at_all(dtype, new, heads, hk, dh):
     adept.adept_chunk_attention(c, q, _i32(starts), _i32([0] * len(new)), max(new), 0, out)
     c.check()
     assert (out[:-2] == 0).all() and (out[-2:] == -7).all()
+
+
+# the CUDA-core kernel whole and split, the few-row kernel whole, over a cluster and split, the tcgen05 kernel whole and in parts
+MISSING = [
+    ("f32", 4, 2, 64, [3, 20, 5], [50, 30, 9]),
+    ("f32", 4, 2, 64, [1, 2, 1], [1500, 700, 90]),
+    ("bf16", 4, 4, 32, [2, 3, 1], [900, 40, 3]),
+    ("bf16", 8, 2, 128, [4, 2, 1], [20, 30, 9]),
+    ("bf16", 8, 2, 128, [1, 2, 1], [700, 500, 60]),
+    ("e4m3", 8, 2, 128, [1, 2, 3], [700, 500, 60]),
+    ("bf16", 32, 32, 128, [1, 1, 1], [4000, 3000, 60]),
+    ("e4m3", 32, 32, 128, [5, 1, 2], [4000, 3000, 60]),
+    ("bf16", 32, 2, 64, [300, 290, 280], [0, 0, 20]),
+    ("bf16", 8, 2, 128, [200, 1, 40], [3000, 900, 10]),
+    ("e4m3", 8, 2, 128, [200, 1, 40], [3000, 900, 10]),
+    ("e4m3", 4, 4, 64, [300, 2, 1], [1000, 2000, 10]),
+]
+
+
+@pytest.mark.parametrize("dtype,heads,hk,dh,new,past", MISSING, ids=str)
+@pytest.mark.parametrize("gone", [0, 1])
+def test_rows_of_missing_blocks_alone_are_zero(dtype, heads, hk, dh, new, past, gone):
+    """A sequence none of whose blocks is there: flagged, its rows zero, the others' what they are."""
+    lens = [a + b for a, b in zip(new, past)]
+    c = make_cache(dtype, hk, dh, lens, 91)
+    q, starts = make_q(dtype, new, heads, dh, 92)
+    c.block_table[gone] = -1
+    out = attend(c, q, starts, lens)
+    with pytest.raises(adept.AdeptError) as ei:
+        c.check()
+    assert ei.value.status == 6
+    assert (out[starts[gone]:starts[gone + 1]] == 0).all()
+    held = [0 if b == gone else n for b, n in enumerate(lens)]   # (without keys the reference's rows are zero too)
+    assert_attention(c, q, starts, held, out)
+
+
+@pytest.mark.parametrize("dtype,heads,hk,dh,new,past", [m for m in MISSING if m[0] != "e4m3"], ids=str)
+def test_scores_of_minus_infinity_alone_give_zeros(dtype, heads, hk, dh, new, past):
+    """K of one head at -infinity in a column where Q is positive: that head's rows are zero, the others' what they are."""
+    lens = [a + b for a, b in zip(new, past)]
+    c = make_cache(dtype, hk, dh, lens, 93)
+    q, starts = make_q(dtype, new, heads, dh, 94)
+    q = q.clone()
+    q[..., 7] = q[..., 7].abs() + 1
+    clean = attend(c, q, starts, lens)
+    c.k[:, 0, :, 7] = -math.inf
+    out = attend(c, q, starts, lens)
+    c.check()
+    g = heads // hk
+    assert (out[:, :g] == 0).all() and torch.equal(out[:, g:], clean[:, g:])
