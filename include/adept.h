@@ -484,7 +484,8 @@ ADEPT_API adept_status adept_chunk_attention(const adept_kv_cache* c, int n_head
  * blocks as the pool has or as n_seq sequences of max_kv_len positions take, whichever are fewer. */
 ADEPT_API int64_t adept_chunk_attention_workspace(const adept_kv_cache* c, int n_heads, int n_rows, int max_q_len,
                                         int max_kv_len);
-/* Synchronise `stream`, then read and clear the cache's error word: DEVICE_INPUT, TIMEOUT or OK.
+/* Synchronise `stream`, then read and clear the cache's error word: DEVICE_INPUT, TIMEOUT or OK.  What calls on
+ * other streams set meanwhile is reported now or by the next check.
  * Errors: INVALID_ARG (no error word), CUDA. */
 ADEPT_API adept_status adept_kv_check(const adept_kv_cache* c, void* stream);
 

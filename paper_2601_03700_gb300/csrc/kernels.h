@@ -27,6 +27,10 @@ static __device__ __forceinline__ float exit_similarity(int metric, float ns, fl
   return metric == EXIT_LOCAL ? l : fminf(g, l);
 }
 
+// Waits for the stream, then takes the error word: reads it into *w and clears the bits that were read, on the stream.  Bits that
+// another stream sets meanwhile stay for the next call, and the clearing is over when this returns.
+cudaError_t take_error_word(cudaStream_t st, unsigned* word, unsigned* w);
+
 // Token -> (sequence, position) maps, identity row map, the pass's counters (all rows
 // active), if sim is given NaN for every (token, layer) similarity, and if tok_exit is
 // given N as every token's exit layer so far.  ext (else NULL): ragged chunks behind what ext_n

@@ -12,6 +12,14 @@
 namespace adept {
 
 // ---------------------------------------------------------------------------
+// error words
+// ---------------------------------------------------------------------------
+__global__ void clear_bits_kernel(unsigned* word, unsigned bits) {
+  PDL_ENTRY();
+  atomicAnd(word, ~bits);
+}
+
+// ---------------------------------------------------------------------------
 // pass set-up: token -> (sequence, position), identity row map, counters
 // ---------------------------------------------------------------------------
 // Thread t's part: counter t, token t.  ext (else NULL): a pass of ragged chunks behind what the sequences hold, of ext_n
@@ -1062,6 +1070,15 @@ __global__ void __launch_bounds__(256) read_kv_kernel(KVCacheView c, int row_byt
 // ---------------------------------------------------------------------------
 // launchers
 // ---------------------------------------------------------------------------
+cudaError_t take_error_word(cudaStream_t st, unsigned* word, unsigned* w) {
+  *w = 0;
+  cudaError_t e = cudaMemcpyAsync(w, word, sizeof *w, cudaMemcpyDeviceToHost, st);
+  if (e == cudaSuccess) e = cudaStreamSynchronize(st);
+  if (e != cudaSuccess || *w == 0) return e;
+  e = launch_k(clear_bits_kernel, 1, 1, 0, st, word, *w);
+  return e == cudaSuccess ? cudaStreamSynchronize(st) : e;
+}
+
 void launch_pass_init(cudaStream_t st, int n_tok, int prompt_len, int* tok_seq, int* tok_pos, int* row_tok, int* seq_len,
                       int seq_cap, int max_pos, unsigned* err, int* ctr, int n_ctr, float* sim, int n_layers,
                       int* tok_exit, const int* ext, int ext_n) {

@@ -2,6 +2,7 @@
 // launches on the caller's stream.  They hold no state and allocate nothing.
 #include "adept.h"
 #include "common.cuh"
+#include "kernels.h"
 #include "kv_paged.h"
 #include "model_view.h"
 
@@ -148,10 +149,9 @@ adept_status adept_kv_check(const adept_kv_cache* c, void* stream) {
   const adept_status s = view_of(c, &v);
   if (s != ADEPT_OK) return s;
   if (!v.err) return bad(ADEPT_ERR_INVALID_ARG, "the cache has no error word");
-  cudaError_t e = cudaStreamSynchronize((cudaStream_t)stream);
+  cudaStream_t st = (cudaStream_t)stream;
   unsigned w = 0;
-  if (e == cudaSuccess) e = cudaMemcpy(&w, v.err, sizeof w, cudaMemcpyDeviceToHost);
-  if (e == cudaSuccess) e = cudaMemset(v.err, 0, sizeof w);
+  const cudaError_t e = take_error_word(st, v.err, &w);
   if (e != cudaSuccess) {
     cudaGetLastError();
     return bad(ADEPT_ERR_CUDA, "reading the error word: %s", cudaGetErrorString(e));

@@ -71,3 +71,29 @@ def test_scores_of_minus_infinity_alone_give_zeros(dtype, heads, hk, dh, new, pa
     c.check()
     g = heads // hk
     assert (out[:, :g] == 0).all() and torch.equal(out[:, g:], clean[:, g:])
+
+
+def test_a_flag_set_right_behind_a_check_is_reported():
+    """Flags on a side stream, each right behind the check of the one before: every check reports its own."""
+    c = adept.KVCache(2, 1, 64, 1, 2)
+    c.block_table.zero_()
+    x = torch.ones(1, 1, 64, device="cuda")
+    seq, pos = _i32([0]), _i32([99])
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(2000):
+        adept.adept_kv_append(c, x, x, seq, pos, stream=side)
+        with pytest.raises(adept.AdeptError):
+            c.check(side)
+    c.check(side)
+    assert c.err.item() == 0
+
+
+def test_a_check_takes_what_it_reports_only():
+    """Bits that other streams set are reported by this check or the next, and cleared by that."""
+    c = adept.KVCache(2, 1, 64, 1, 2)
+    c.err.fill_(1 << 30)   # (a bit no kernel sets)
+    with pytest.raises(adept.AdeptError, match="0x40000000"):
+        c.check()
+    c.check()
+    c.check(torch.cuda.Stream())
