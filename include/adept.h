@@ -420,7 +420,7 @@ ADEPT_API int64_t adept_hsm_param_numel(const adept_model* m, int param);
  *     is stored as NaN.  What is read back is exact in fp32, and in bf16 above its subnormals (only
  *     an element that rounded up to 2^128 reads back as infinity).
  * The buffers are the caller's, on the current device; d_k, d_v and the exponents start on 16 bytes.  The calls
- * allocate nothing, hold no state between calls and can be captured into a graph; calls on one
+ * allocate nothing, hold no state between calls and (but for the check) can be captured into a graph; calls on one
  * cache are ordered by their streams as any other work on shared buffers is.
  * d_err (may be NULL): a device word that kernels set where an input read on the device is out of
  * range (zero it first); adept_kv_check reports and clears it. */
@@ -486,7 +486,7 @@ ADEPT_API int64_t adept_chunk_attention_workspace(const adept_kv_cache* c, int n
                                         int max_kv_len);
 /* Synchronise `stream`, then read and clear the cache's error word: DEVICE_INPUT, TIMEOUT or OK.  What calls on
  * other streams set meanwhile is reported now or by the next check.
- * Errors: INVALID_ARG (no error word), CUDA. */
+ * Errors: INVALID_ARG (no error word, a stream in capture), CUDA. */
 ADEPT_API adept_status adept_kv_check(const adept_kv_cache* c, void* stream);
 
 /* ---- failure injection (tests of the error paths; no GPU fault is involved) ------------

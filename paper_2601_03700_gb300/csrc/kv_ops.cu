@@ -150,8 +150,12 @@ adept_status adept_kv_check(const adept_kv_cache* c, void* stream) {
   if (s != ADEPT_OK) return s;
   if (!v.err) return bad(ADEPT_ERR_INVALID_ARG, "the cache has no error word");
   cudaStream_t st = (cudaStream_t)stream;
+  cudaStreamCaptureStatus cap = cudaStreamCaptureStatusNone;
+  cudaError_t e = cudaStreamIsCapturing(st, &cap);
+  if (e == cudaSuccess && cap != cudaStreamCaptureStatusNone)
+    return bad(ADEPT_ERR_INVALID_ARG, "a check waits for its stream, which cannot be captured into a graph");
   unsigned w = 0;
-  const cudaError_t e = take_error_word(st, v.err, &w);
+  if (e == cudaSuccess) e = take_error_word(st, v.err, &w);
   if (e != cudaSuccess) {
     cudaGetLastError();
     return bad(ADEPT_ERR_CUDA, "reading the error word: %s", cudaGetErrorString(e));

@@ -97,3 +97,18 @@ def test_a_check_takes_what_it_reports_only():
         c.check()
     c.check()
     c.check(torch.cuda.Stream())
+
+
+def test_a_check_in_capture_is_refused():
+    c = adept.KVCache(2, 1, 64, 1, 2)
+    x = torch.zeros(1, device="cuda")
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        x += 1
+        with pytest.raises(adept.AdeptError, match="captured") as ei:
+            c.check()
+    assert ei.value.status == 1
+    graph.replay()
+    assert x.item() == 1   # the capture is whole
+    c.check()
