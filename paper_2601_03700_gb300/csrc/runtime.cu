@@ -2308,11 +2308,13 @@ adept_status adept_check_device_status(adept_model* m, void* stream) {
   CUDA_TRY(m, cudaStreamSynchronize(st));
   CUDA_TRY(m, cudaGetLastError());
   unsigned w = 0;
-  CUDA_TRY(m, cudaMemcpy(&w, m->err_word, sizeof w, cudaMemcpyDeviceToHost));
-  CUDA_TRY(m, cudaMemset(m->err_word, 0, sizeof(unsigned)));
+  CUDA_TRY(m, take_error_word(st, m->err_word, &w));
   if (w & ERRW_TIMEOUT) {
     // a launch that gave up may have left arrival counters of the stream-K GEMM counted
-    if (m->ds_cnt) CUDA_TRY(m, cudaMemset(m->ds_cnt, 0, sizeof(int) * DS_CNT_CAP));
+    if (m->ds_cnt) {
+      CUDA_TRY(m, cudaMemsetAsync(m->ds_cnt, 0, sizeof(int) * DS_CNT_CAP, st));
+      CUDA_TRY(m, cudaStreamSynchronize(st));
+    }
     return fail(m, ADEPT_ERR_TIMEOUT, "a device-side wait timed out (word 0x%x)", w);
   }
   if (w) return fail(m, ADEPT_ERR_DEVICE_INPUT, "device-side input check failed (word 0x%x)", w);

@@ -19,11 +19,13 @@ def body(path, name):
     return text[m.end():end]
 
 
-@pytest.mark.parametrize("path,name", [("kv_ops.cu", "adept_kv_check")])
+@pytest.mark.parametrize("path,name", [("kv_ops.cu", "adept_kv_check"), ("runtime.cu", "adept_check_device_status")])
 def test_no_check_uses_the_legacy_stream(path, name):
     calls = body(path, name)
     assert "take_error_word(" in calls
     assert not re.search(r"\bcudaMem(set|cpy)\s*\(", calls)
+    cleared = calls.find("cudaMemsetAsync(")   # (counters besides: waited for)
+    assert cleared < 0 or calls.find("cudaStreamSynchronize(", cleared) > 0
 
 
 def test_the_word_is_read_and_cleared_on_the_stream():
