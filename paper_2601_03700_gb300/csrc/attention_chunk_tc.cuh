@@ -299,8 +299,11 @@ __global__ void __launch_bounds__(CtShape<DH>::THREADS, 1) chunk_tc_kernel(const
   __shared__ uint32_t s_tmem;
   __shared__ int s_abort;
   __shared__ int s_gone[4];      // blocks of a key tile that are not there, by tile % 4
-  __shared__ int s_pk[4][DH];    // least key with a non-finite V entry, per column (causal edge), by segment with keys % 4
-  __shared__ int s_poisoned[4];
+  // Least key with a non-finite V entry, per column (causal edge), and whether there is one: for each sub-tile, by its segments with
+  // keys % 4.  Each sub-tile has slots of its own because one without keys in a segment meets no barrier there: a slot that both
+  // read could be needed again while the other still reads.
+  __shared__ int s_pk[2][4][DH];
+  __shared__ int s_poisoned[2][4];
   __shared__ int s_tok[CT_ROWS], s_off[CT_ROWS];   // token of a row in the tile (-1: none), its head's first column in the group
   __shared__ CtTile s_tile;
   __shared__ int s_u0, s_u1;
@@ -390,14 +393,14 @@ __global__ void __launch_bounds__(CtShape<DH>::THREADS, 1) chunk_tc_kernel(const
     const CtWs ws(p);
     uint8_t* stage = sm + L::OFF_ST + warp * 2048;
     int ns = 0, no = 0, kt = 0;   // S tiles, outputs, key tiles so far
-    int seg = -1;   // segments with keys so far
+    int seg = -1;   // the sub-tile's segments with keys so far
     while (u < u_end) {
       g.set(a, ts, x, u, u_end);
-      seg += g.n_it > 0;
       const bool mine = tok >= 0 && tok < g.n_tok;
       const int lim = mine ? min(g.keys(a, tok), g.k_end) : 0;
       const int sub_lo = sub * ts < g.n_tok ? g.keys(a, sub * ts) : 0;   // keys of the sub-tile's first token
       const int n_my = g.nt(sub);
+      seg += n_my > 0;
       float m = -INFINITY, l = 0.f;
       for (int j = 0; j < n_my; ++j) {
         if (!(ok = mbar_wait_warp(&s_full[sub], (uint32_t)(ns & 1), abort_flag, err, wlim))) break;
@@ -478,10 +481,10 @@ __global__ void __launch_bounds__(CtShape<DH>::THREADS, 1) chunk_tc_kernel(const
 #pragma unroll
         for (int e = 0; e < DH; ++e) v[e] = 0.f;
       }
-      if (n_my > 0 && s_poisoned[seg & 3]) {
+      if (n_my > 0 && s_poisoned[sub][seg & 3]) {
 #pragma unroll
         for (int e = 0; e < DH; ++e)
-          if (s_pk[seg & 3][e] < lim) v[e] = NAN;
+          if (s_pk[sub][seg & 3][e] < lim) v[e] = NAN;
       }
       if (sub == 0 || g.n_tok > ts) {
         if (g.whole) {
@@ -624,7 +627,16 @@ __global__ void __launch_bounds__(CtShape<DH>::THREADS, 1) chunk_tc_kernel(const
     uint8_t* dst0 = kw ? sK : sV;
     int cnt = 0;   // tiles sent so far
     // V tile j (the vi-th, blocks `gone` of it not there): entries nobody attends to zero, non-finite ones noted
-    auto mend = [&](int j, int vi, int gone, int par) {
+    int seg0 = -1, seg1 = -1;   // segments with keys so far, of either sub-tile
+    // The segment's notes for a sub-tile begin (warp-converged): no key in any column yet.
+    auto note = [&](int sub, int slot) {
+      if (s_poisoned[sub][slot]) return;
+      __syncwarp();
+      for (int e = lane; e < DH; e += 32) s_pk[sub][slot][e] = 0x7fffffff;
+      s_poisoned[sub][slot] = 1;
+      __syncwarp();
+    };
+    auto mend = [&](int j, int vi, int gone) {
       const int s = vi & 1;
       if (!mbar_wait_warp(&v_full[s], (uint32_t)((vi >> 1) & 1), abort_flag, err, wlim)) return false;
       uint8_t* v = sV + s * L::KV_BYTES;
@@ -640,24 +652,30 @@ __global__ void __launch_bounds__(CtShape<DH>::THREADS, 1) chunk_tc_kernel(const
       __syncwarp();
 #pragma unroll 1
       for (int i0 = 0; i0 < n_key * 8; i0 += 128) {   // 16 keys: a fetched block, or zeros
-        uint4 y[4 * L::HALVES];
+        auto at = [&](int q) { return piece(q >> 2, (i0 >> 3) + (q & 3) * 4 + (lane >> 3), lane & 7); };
         uint32_t any = 0;
 #pragma unroll
         for (int q = 0; q < 4 * L::HALVES; ++q) {
-          y[q] = *piece(q >> 2, (i0 >> 3) + (q & 3) * 4 + (lane >> 3), lane & 7);
-          any |= ct_any_bad2(y[q].x) | ct_any_bad2(y[q].y) | ct_any_bad2(y[q].z) | ct_any_bad2(y[q].w);
+          const uint4 y = *at(q);
+          any |= ct_any_bad2(y.x) | ct_any_bad2(y.y) | ct_any_bad2(y.z) | ct_any_bad2(y.w);
         }
-        if (any) {
-#pragma unroll
+        if (__any_sync(0xffffffffu, any != 0)) {
+          const bool of0 = j < g.nt0, of1 = j < g.nt1;   // (a sub-tile through with its key tiles may be reading its notes)
+          if (of0) note(0, seg0 & 3);
+          if (of1) note(1, seg1 & 3);
+#pragma unroll 1
           for (int q = 0; q < 4 * L::HALVES; ++q) {
+            const uint4 y = *at(q);
             const int key = (i0 >> 3) + (q & 3) * 4 + (lane >> 3), col = (q >> 2) * 64 + (((lane & 7) ^ (key & 7)) << 3);
-            const uint32_t b[4] = {ct_bad2(y[q].x), ct_bad2(y[q].y), ct_bad2(y[q].z), ct_bad2(y[q].w)};
-            *piece(q >> 2, key, lane & 7) = make_uint4(y[q].x & ~b[0], y[q].y & ~b[1], y[q].z & ~b[2], y[q].w & ~b[3]);
+            const uint32_t b[4] = {ct_bad2(y.x), ct_bad2(y.y), ct_bad2(y.z), ct_bad2(y.w)};
+            *at(q) = make_uint4(y.x & ~b[0], y.y & ~b[1], y.z & ~b[2], y.w & ~b[3]);
 #pragma unroll
             for (int e = 0; e < 8; ++e)
-              if (b[e >> 1] >> ((e & 1) * 16) & 1) atomicMin(&s_pk[par][col + e], k0 + key);
+              if (b[e >> 1] >> ((e & 1) * 16) & 1) {
+                if (of0) atomicMin(&s_pk[0][seg0 & 3][col + e], k0 + key);
+                if (of1) atomicMin(&s_pk[1][seg1 & 3][col + e], k0 + key);
+              }
           }
-          s_poisoned[par] = 1;
         }
       }
       fence_async_shared();
@@ -665,14 +683,14 @@ __global__ void __launch_bounds__(CtShape<DH>::THREADS, 1) chunk_tc_kernel(const
       if (lane == 0) mbar_arrive(&v_fix[s]);
       return true;
     };
-    int seg = -1;   // segments with keys so far
     while (u < u_end && ok) {
       g.set(a, ts, x, u, u_end);
-      seg += g.n_it > 0;
+      seg0 += g.nt0 > 0;
+      seg1 += g.nt1 > 0;
       int gone = 0, gone_prev = 0;
       for (int j = 0; j <= g.n_it && ok; ++j) {
         gone_prev = gone;
-        if (!kw && j > 0 && (g.edge(j - 1) || gone_prev) && !(ok = mend(j - 1, cnt - 1, gone_prev, seg & 3))) break;
+        if (!kw && j > 0 && (g.edge(j - 1) || gone_prev) && !(ok = mend(j - 1, cnt - 1, gone_prev))) break;
         if (j == g.n_it) break;
         const int s = cnt & 1, row = lane < 8 ? g.row_of(a.c, p.wide, (g.j_lo + j) * 8 + lane) : -1;
         const unsigned on = __ballot_sync(0xffffffffu, row >= 0);
@@ -682,9 +700,11 @@ __global__ void __launch_bounds__(CtShape<DH>::THREADS, 1) chunk_tc_kernel(const
 #pragma unroll
         for (int b = 0; b < 8; ++b) rows8[b] = __shfl_sync(0xffffffffu, row, b);
         if (cnt >= 2 && !(ok = mbar_wait_warp(&empty[s], (uint32_t)(((cnt >> 1) - 1) & 1), abort_flag, err, wlim))) break;
-        if (!kw && j == 0) {   // the segment's notes (V of two tiles ago is through, so the segment before the last is written)
-          for (int e = lane; e < DH; e += 32) s_pk[seg & 3][e] = 0x7fffffff;
-          if (lane == 0) s_poisoned[seg & 3] = 0;
+        // No notes of the segment yet, in the place of those of the sub-tile's four segments before (k).  V of two tiles ago is through, so
+        // the sub-tile has handed over a P of its segment k + 2, behind its reading of the notes of k and k + 1.
+        if (!kw && j == 0) {
+          if (lane == 0 && g.nt0 > 0) s_poisoned[0][seg0 & 3] = 0;
+          if (lane == 0 && g.nt1 > 0) s_poisoned[1][seg1 & 3] = 0;
           __syncwarp();
         }
         if (elect_one()) {
