@@ -472,6 +472,9 @@ ADEPT_API adept_status adept_kv_gather(const adept_kv_cache* c, int n_rows, int 
  *                is out of range (a row of such keys alone, or of scores that are all -infinity, gives zeros)
  *   d_ws         adept_chunk_attention_workspace bytes on 16 bytes (NULL where that is 0), of any
  *                contents; calls that may overlap on the GPU need one each
+ * Sums run in fp32 over weights of up to 2^8, and scores are fp32: V elements above 2^100 may overflow the sums, products
+ * of Q and K beyond fp32's range make scores infinite or NaN, and elements of an 8-bit row whose largest is below 2^-100
+ * may lose bits.
  * For the same lengths a call's results are the same bits every time.
  * Errors: INVALID_ARG (bad cache, n_heads no multiple of n_kv_heads, max_kv_len above the table, a
  * stride below a row, NULL or misaligned pointers, a workspace too small), CAPACITY (n_rows *

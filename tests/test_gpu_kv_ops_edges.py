@@ -4,6 +4,7 @@ import math
 import pytest
 import torch
 
+import kv_reference as R
 import paper_2601_03700_gb300 as adept
 from test_gpu_kv_ops import _i32, _lib, assert_attention, attend, make_cache, make_q  # noqa: F401  (_lib: the module's fixture)
 
@@ -112,3 +113,86 @@ def test_a_check_in_capture_is_refused():
     graph.replay()
     assert x.item() == 1   # the capture is whole
     c.check()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "e4m3"])
+@pytest.mark.parametrize("heads,hk", [(128, 1), (160, 1), (258, 2), (21, 7)])
+@pytest.mark.parametrize("new,past", [([1], [300]), ([40, 3], [100, 20])])
+def test_many_query_heads_on_a_head(dtype, heads, hk, new, past):
+    lens = [a + b for a, b in zip(new, past)]
+    c = make_cache(dtype, hk, 64, lens, 97)
+    q, starts = make_q(dtype, new, heads, 64, 98)
+    out = attend(c, q, starts, lens)
+    c.check()
+    assert_attention(c, q, starts, lens, out)
+
+
+@pytest.mark.parametrize("dtype,heads,hk,dh,new,past", MISSING, ids=str)
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+def test_a_query_that_is_not_finite_reaches_no_other_row(dtype, heads, hk, dh, new, past, bad):
+    lens = [a + b for a, b in zip(new, past)]
+    c = make_cache(dtype, hk, dh, lens, 99)
+    q, starts = make_q(dtype, new, heads, dh, 100)
+    q = q.clone()
+    clean = attend(c, q, starts, lens)
+    row, head = starts[-1] // 2, heads - 1
+    q[row, head, 3] = bad
+    out = attend(c, q, starts, lens)
+    c.check()
+    assert not torch.isfinite(out[row, head]).any()
+    out[row, head] = clean[row, head]
+    assert torch.equal(out, clean)
+
+
+def test_few_and_many_tokens_over_8_bit_entries_on_several_streams():
+    """The form whose launches run side by side (widening, few rows, longer chunks), itself on three streams at once, with a
+    workspace each, and replayed from two graphs."""
+    new, past = [1, 200, 3, 0, 17], [4600, 300, 90, 8, 0]
+    lens = [a + b for a, b in zip(new, past)]
+    c = make_cache("e4m3", 4, 128, lens, 101)
+    q, starts = make_q("bf16", new, 16, 128, 102)
+    want = attend(c, q, starts, lens)
+    assert_attention(c, q, starts, lens, want)
+    at, n = _i32(starts), _i32(lens)
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    sets = [(torch.empty_like(want), c.attention_workspace(16, q.shape[0], max(new), max(lens))) for _ in streams]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for s, (out, ws) in zip(streams, sets):
+            with torch.cuda.stream(s):
+                out.fill_(-7)
+                adept.adept_chunk_attention(c, q, at, n, max(new), max(lens), out, ws)
+    torch.cuda.synchronize()
+    assert all(torch.equal(out, want) for out, _ in sets)
+    graphs = []
+    for out, ws in sets[:2]:
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            adept.adept_chunk_attention(c, q, at, n, max(new), max(lens), out, ws)
+    for _ in range(10):
+        for g, s, (out, _) in zip(graphs, streams, sets):
+            with torch.cuda.stream(s):
+                out.fill_(-7)
+                g.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(out, want) for out, _ in sets)
+    c.check()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "e4m3"])
+@pytest.mark.parametrize("heads,hk,dh,new,past", [(8, 2, 128, [3, 1], [700, 60]), (8, 2, 128, [200, 40], [700, 60]),
+                                                  (4, 4, 64, [150, 2], [90, 600])])
+@pytest.mark.parametrize("e", [100, -100])
+def test_values_far_from_one(dtype, heads, hk, dh, new, past, e):
+    """V around 2^100 and 2^-100, the bounds within which nothing overflows or loses bits."""
+    lens = [a + b for a, b in zip(new, past)]
+    c = make_cache(dtype, hk, dh, lens, 103)
+    if dtype == "e4m3":
+        c.v_exp.copy_((c.v_exp.int() + e).clamp(1, 254).to(torch.uint8))
+    else:
+        c.v.mul_(2.0 ** e)
+    q, starts = make_q(dtype, new, heads, dh, 104)
+    out = attend(c, q, starts, lens)
+    c.check()
+    want, tol = R.attention(c, q, starts, lens)
+    assert torch.isfinite(out).all() and ((out.double() - want).abs() <= tol).all()
