@@ -209,7 +209,7 @@ inline cudaError_t smem_once(K* kernel, int bytes) {
 
 // Items there can be at most: the target, or one per tile where there are more tiles.
 static inline long long split_items(const SplitPlan& p, int n_seq, int n_rows, int max_q) {
-  const long long by_seq = (long long)n_seq * ((max_q + p.tq - 1) / p.tq);
+  const long long by_seq = (long long)n_seq * (((long long)max_q + p.tq - 1) / p.tq);   // (max_q may be any bound)
   const long long by_rows = n_rows / p.tq + (long long)n_seq;
   const long long tiles = (by_seq < by_rows ? by_seq : by_rows) * p.groups;
   return tiles > p.target ? tiles : p.target;

@@ -196,3 +196,16 @@ def test_values_far_from_one(dtype, heads, hk, dh, new, past, e):
     c.check()
     want, tol = R.attention(c, q, starts, lens)
     assert torch.isfinite(out).all() and ((out.double() - want).abs() <= tol).all()
+
+
+@pytest.mark.parametrize("dtype,heads,hk,dh,new,past", MISSING, ids=str)
+def test_bounds_far_above_the_lengths(dtype, heads, hk, dh, new, past):
+    """max_q_len up to the largest int: the same rows (another kernel may take them)."""
+    lens = [a + b for a, b in zip(new, past)]
+    c = make_cache(dtype, hk, dh, lens, 105)
+    q, starts = make_q(dtype, new, heads, dh, 106)
+    for max_q in (2 ** 31 - 1, 2 ** 31 - 3, 2 ** 20):
+        out = torch.full_like(q, -7.0)
+        adept.adept_chunk_attention(c, q, _i32(starts), _i32(lens), max_q, 16 * c.block_table.shape[1], out)
+        c.check()
+        assert_attention(c, q, starts, lens, out)
