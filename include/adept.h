@@ -431,7 +431,7 @@ typedef struct {
   int head_dim;             /* 32, 64 or 128 */
   int block_tokens;
   int n_seq;                /* rows of the block table */
-  int max_blocks_per_seq;   /* its columns */
+  int max_blocks_per_seq;   /* its columns; at most 2^30 positions a row, and 2^20 elements a position */
   void* d_k;
   void* d_v;
   uint8_t* d_k_exp;         /* ADEPT_KV_E4M3 only */
@@ -476,7 +476,7 @@ ADEPT_API adept_status adept_kv_gather(const adept_kv_cache* c, int n_rows, int 
  * of Q and K beyond fp32's range make scores infinite or NaN, and elements of an 8-bit row whose largest is below 2^-100
  * may lose bits.
  * For the same lengths a call's results are the same bits every time.
- * Errors: INVALID_ARG (bad cache, n_heads no multiple of n_kv_heads, max_kv_len above the table, a
+ * Errors: INVALID_ARG (bad cache, n_heads no multiple of n_kv_heads or above 2^15, max_kv_len above the table, a
  * stride below a row, NULL or misaligned pointers, a workspace too small), CAPACITY (n_rows *
  * n_heads or n_seq * n_heads above 2^30, or more than 2^31 tiles of 128 rows and 128 keys), CUDA. */
 ADEPT_API adept_status adept_chunk_attention(const adept_kv_cache* c, int n_heads, int n_rows, const void* d_q, int64_t ld_q,

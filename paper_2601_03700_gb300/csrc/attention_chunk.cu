@@ -5,9 +5,9 @@
 //
 // in one pass over the keys with the running maximum and sum (fp32, exponentials in base 2).  A row that no key gives any weight
 // (a chunk longer than kv_len, no block there, all scores -infinity) gives zeros: its sum is zero, as no other row's is (the
-// score that last raised the maximum has weight 1, a NaN score gives a sum of NaN).  What lies behind a token's position is never used: neither scores nor V entries of
-// masked positions enter a sum, so NaN or infinities there do not spread.  Keys in blocks that the table does not hold
-// (negative, out of range) are left out and flagged.
+// score that last raised the maximum has weight 1, a NaN score gives a sum of NaN).  What lies behind a token's position is never
+// used: neither scores nor V entries of masked positions enter a sum, so NaN or infinities there do not spread.  Keys in blocks
+// that the table does not hold (negative, out of range) are left out and flagged.
 //
 // The split of the work, and the join of split tiles, are in kv_paged.h.
 #define ADEPT_TU_ID 14
@@ -26,8 +26,8 @@ namespace {
 // Any type, head size, alignment and block size: CUDA-core kernel.  CTA = up to CG_ROWS new tokens of one query head x a
 // run of keys, 128 keys at a time: a thread per key for the scores, a warp per token for the softmax, for the weighted sum a
 // thread per four dimensions of every KG-th key.  Such calls are short and bound by latency, one load behind the other, so
-// all loads are of four elements, several under way: fp32, 22 rows of 4 heads of 64 over up to 101 keys in 7.9 us (17.8 with
-// one element a load, two key groups); 512 rows of 12 heads over 2560 keys in 379 us (9.6 TFLOP/s, each tile of 4 rows reading
+// all loads are of four elements, several under way: fp32, 22 rows of 4 heads of 64 over up to 101 keys in 8.2 us (17.8 with
+// one element a load, two key groups); 512 rows of 12 heads over 2560 keys in 369 us (9.8 TFLOP/s, each tile of 4 rows reading
 // K and V from L2 again).
 // ---------------------------------------------------------------------------------------------
 constexpr int CG_ROWS = 4, CG_KEYS = 128;
@@ -217,20 +217,24 @@ __global__ void __launch_bounds__(CG_KEYS) chunk_any_kernel(const __grid_constan
 // of two so that its largest element lies in [2^14, 2^15): exact down to 2^-28 of it.  V as bf16, since P has to keep bf16's
 // range (a position of little weight may hold a V of any size).  K's exponent scales S, V's scales P.
 //
-// A tile's keys are split over CTAs even where they are few (12 heads of 64, 333 keys: 6.8 us split and joined, 9.0 by 12 CTAs;
-// 1000 keys 7.1 and 19.2), in one of two ways.  Where a cluster of up to 8 CTAs a tile is enough (cs > 1), its CTAs take
+// A tile's keys are split over CTAs even where they are few (12 heads of 64, 333 keys: 7.2 us split and joined, 7.7 by 12 CTAs;
+// 1000 keys 7.6 and 14.5), in one of two ways.  Where a cluster of up to 8 CTAs a tile is enough (cs > 1), its CTAs take
 // equal shares and join through distributed shared memory, in one launch.  Else each tile gets as many as balance the GPU
 // (split_find), whose partials a second launch joins.
 //
 // ROWS = 8: where no tile has more than 8 rows the keys are the 16 rows of the matrix instructions and the queries their 8
 // columns (S^T = K Q^T, O^T = V^T P^T), which halves them and the softmax; the same words of K and V in the same registers, P's
-// fragments turned round in between.  Against 16 rows: 8 bits, a token of 32 heads of 128 over 30011 keys 47.3 us for 54.5, 16
-// sequences of a token, 32 heads on 8, 21.4 for 23.8; bf16, a token of 32 heads over 2000 keys 9.8 for 10.6, 8 sequences over up to
-// 4000 56.3 for 57.2.
+// fragments turned round in between.  Against 16 rows: 8 bits, a token of 32 heads of 128 over 30011 keys 45.6 us for 53.2, 16
+// sequences of a token, 32 heads on 8, 21.0 for 24.2; bf16, a token of 32 heads over 2000 keys 11.3 for 12.1, 8 sequences over up to
+// 4000 56.9 for 57.8.
 //
-// Measured: that token over 30011 keys, 8 bits (248 MB) 45.5 us, 5.4 TB/s, bound by instruction issue and latency (12 warps an SM,
-// each waiting on its own conversions and reads); 8 sequences over up to 4000 keys in bf16 (295 MB) 56.3 us, 5.2 TB/s; 4 to 5
-// tokens of 4 sequences over 8.4 thousand keys, bf16 (139 MB), 31.2 us, 8 of them launches and the join.
+// P is rounded to bf16 (2^-8 relative at most) because the matrix instruction takes 16 bits of it and of V; the sums l take the
+// weights as they are, in fp32.  Against 64 bits an output is off by 2.3e-3 of its size (rms) where the rounding of the output alone
+// gives 1.7e-3.
+//
+// Measured: that token over 30011 keys, 8 bits (248 MB) 45.6 us, 5.4 TB/s, bound by instruction issue and latency (12 warps an SM,
+// each waiting on its own conversions and reads); 8 sequences over up to 4000 keys in bf16 (295 MB) 56.9 us, 5.2 TB/s; 4 to 5
+// tokens of 4 sequences over 8.4 thousand keys, bf16 (139 MB), 30.9 us, 8 of them launches and the join.
 // ---------------------------------------------------------------------------------------------
 constexpr int CF_WARPS = 4, CF_ROWS = 16;
 constexpr float CF_RAISE = 8.f;   // the running maximum is raised once a score exceeds it by 2^8: weights stay below 256
@@ -1008,13 +1012,14 @@ size_t how_bytes(const ChunkHow& w, const KvPaged& c) {
 // The most new tokens of a sequence that the few-row kernel takes.  It reads K and V again for each tile of 16 rows, which costs by
 // the tiles of all sequences and heads; the tcgen05 kernel reads them once, but costs some 10 us more whatever the call, and
 // 8-bit entries have to be widened for it.  Few-row and tcgen05 kernel in us, over 4096 keys, tokens x heads on KV heads x d_h:
-//   bf16   8 x 32/8 x 128   15.7 17.2     16 x 32/8 x 128   19.3 17.8     32 x 32/32 x 128  30.8 24.4     16 x 32/32 x 128  23.7 23.8
-//          48 x 12/12 x 64  14.9 15.9     96 x 12/12 x 64   20.5 16.3     96 x 4/2 x 128    17.2 24.1     16 x (8 x 32/8 x 128)  107 51
-//   8-bit  16 x 32/8 x 128  20.3 26.6     48 x 32/8 x 128   34.6 34.7     64 x 32/32 x 128  42.4 57.5     96 x 32/32 x 128  57.2 59.8
-//          96 x 12/12 x 64  21.3 23.6     128 x 12/12 x 64  24.6 24.3     16 x (8 x 32/8 x 128)  85 127   16 x (32 x 32/8 x 128)  218 134
+//   bf16   8 x 32/8 x 128   14.3 15.1     16 x 32/8 x 128   16.9 16.1     32 x 32/32 x 128  25.2 24.0     16 x 32/32 x 128  22.5 23.6
+//          48 x 12/12 x 64  14.0 14.1     96 x 12/12 x 64   18.3 14.8     96 x 4/2 x 128    15.4 18.8     16 x (8 x 32/8 x 128)   80 58
+//   8-bit  16 x 32/8 x 128  20.5 25.5     48 x 32/8 x 128   33.3 30.3     64 x 32/32 x 128  40.3 54.3     96 x 32/32 x 128  55.1 59.4
+//          96 x 12/12 x 64  19.7 23.1     128 x 12/12 x 64  23.6 23.5     16 x (8 x 32/8 x 128)   90 150  16 x (32 x 32/8 x 128)  225 157
+// (Of these the rule takes the slower kernel at 96 x 32/32 x 128 over 8 bits, by 8 %.)
 // Where sequences of both kinds meet: over bf16 entries all go to the tcgen05 kernel (its tiles are mostly empty for few
 // tokens, but it reads K and V at the rate of the memory all the same), 8-bit ones are shared out (use_both).  7 sequences of a
-// token over 2000 keys beside one of 256 over 1000, 32 heads on 8: bf16 33.6 us, shared out 44.6; 8-bit 57.1 and 47.9.
+// token over 2000 keys beside one of 256 over 1000, 32 heads on 8: bf16 30.8 us, shared out 41.7; 8-bit 54.6 and 43.3.
 int few_tokens(const KvPaged& c, int n_heads) {
   const long long tiles = 24ll * 128 / ((long long)c.n_seq * c.n_kv_heads * c.head_dim) + (c.type == KV_E4M3 ? 4 : 0);
   return (int)std::max(1ll, tiles) * std::max(1, CF_ROWS / (n_heads / c.n_kv_heads));
@@ -1068,10 +1073,11 @@ cudaError_t chunk_t(cudaStream_t st, const ChunkCall& a, const ChunkHow& w, int*
     e = launch_k(chunk_any_kernel<DH, KT, T>, grid, dim3(CG_KEYS), 0, st, a, w.p);
   } else if constexpr (KT != KV_F32) {
     // A cluster per tile: the largest of 8, 4, 2 CTAs whose clusters find room at once, where that leaves a CTA a few rounds
-    // (4 at heads of 128, 2 at 64, 1 at 32).  One call of a token each in a captured graph, cluster and split: 12 heads of 64,
-    // 500 keys 5.6 and 7.0 us, 1000 keys 6.3 and 7.2, 2000 keys 7.7 and 7.5; 32 heads of 128 on 8, 500 keys 6.8 and 8.4,
-    // 2000 keys 9.1 and 11.4, 4000 keys 12.8 and 13.8, 3 sequences of up to 4000 14.3 and 14.4.  Clusters that had no room at
-    // once (8 sequences, 512 CTAs): 14.2 and 10.0.
+    // (4 at heads of 128, 2 at 64, 1 at 32).  bf16, one call of a token each in a captured graph, cluster and split: 12 heads of 64,
+    // 500 keys 5.5 and 7.4 us, 1000 keys 6.2 and 7.6, 2000 keys 7.6 and 7.7; 32 heads of 128 on 8, 500 keys 6.7 and 7.9,
+    // 2000 keys 8.7 and 8.9, 4000 keys 12.0 and 10.1, 3 sequences of up to 4000 12.7 and 10.7.  (8 bits, 4000 keys: 11.7 and
+    // 10.5, where the rule, by rounds of twice the keys, still takes the cluster.)  Clusters that had no room at once: 8 sequences
+    // of 500 keys 14.6 and 10.5, 8 of up to 4000 keys and 32 heads 69 and 57.
     const long long units = cdiv(a.max_kv, w.p.unit);
     int cs = 8;
     while (cs > 1 && tiles * cs > w.p.target) cs >>= 1;

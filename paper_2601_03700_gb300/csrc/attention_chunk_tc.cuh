@@ -23,9 +23,11 @@
 // workspace, once for all the tiles that read them.  Turned by warps of this kernel, tile by tile, they came at 9000 cycles
 // a key tile (2048 of matrix instructions): a mixed batch took 121 us.
 //
-// Measured: 2048 tokens on 16384, 32 heads of 128 on 8, 375 us: 1.56 PFLOP/s, the tensor core 0.69 of the cycles busy, waiting
+// P is rounded to bf16, as the matrix instructions take it; the sums l take the weights as they are, in fp32.
+//
+// Measured: 2048 tokens on 16384, 32 heads of 128 on 8, 373 us: 1.57 PFLOP/s, the tensor core 0.69 of the cycles busy, waiting
 // for the softmax (a key tile of both sub-tiles takes 3085 cycles, its products 2048).  Short calls pay some 20 us beside their
-// key tiles: launch and set-up 4, the first S 4, parts out and joined 8 (256 tokens on 4096, 32 heads: 36 us, 10 of them key
+// key tiles: launch and set-up 4, the first S 4, parts out and joined 8 (256 tokens on 4096, 32 heads: 34 us, 10 of them key
 // tiles at that rate).
 // Every wait is bounded; a CTA that gives up sets the error word, drains its copies and matrix instructions and leaves.
 //
@@ -84,7 +86,7 @@ __device__ unsigned floor_sum(unsigned n, unsigned m, unsigned a, unsigned b) {
 }
 // Units of token tile t: its key tiles (with given positions, those of the whole sequence), and CT_TILE for what every tile costs
 // (its queries' way in, its output's way out: two to three key tiles' time.  Without that, 37 tokens on nothing beside 512 on 1531
-// put six tiles of one unit on the first SM: 49 us, 35 without the 37).
+// put six tiles of one unit on the first SM: 49 us, 32 with it).
 constexpr int CT_TILE = 2;
 __device__ __forceinline__ int ct_units(bool given, int c, int len, int tq, int t) {
   return CT_TILE + max(0, (given ? len + CT_BN - 1 : len - c + min((t + 1) * tq, c) + CT_BN - 1) / CT_BN);
@@ -827,8 +829,8 @@ __global__ void __launch_bounds__(CW_THREADS) chunk_widen_kernel(const __grid_co
 }
 
 // Join of the tiles that runs share: CTA (i, y) takes the tile that run i + 1 is the first to begin inside of, a sixteenth of its
-// rows in use (of all 256 by eighths: 20 rows of 32 heads on 8 over 4096 keys took 24.4 us, 18.9 now; 256 of 32 heads 37.5, 36.3;
-// by 32nds 18.9 and 37.6).  Parts: run i's (the tile's beginning), run i + 1's, ... in order.
+// rows in use (20 rows of 32 heads on 8 over 4096 keys 16.7 us, by eighths and by 32nds 17.7; 256 of 32 heads 34.4, 36.4 and 35.6;
+// 512 on 1531, 32 heads on 8, 31.5, 30.9 and 33.1).  Parts: run i's (the tile's beginning), run i + 1's, ... in order.
 constexpr int CJ_SPLIT = 16;
 template <int DH>
 __global__ void __launch_bounds__(256) chunk_tc_join_kernel(const __grid_constant__ CtParams p) {

@@ -67,7 +67,7 @@ adept_status launched(cudaError_t e) {
 
 adept_status call_ok(const KvPaged& v, int n_heads, int n_rows, int max_q, int max_kv) {
   if (n_heads < 1 || n_heads % v.n_kv_heads || n_heads > (1 << 15))
-    return bad(ADEPT_ERR_INVALID_ARG, "n_heads %d is no multiple of n_kv_heads %d", n_heads, v.n_kv_heads);
+    return bad(ADEPT_ERR_INVALID_ARG, "n_heads %d is no multiple of n_kv_heads %d, or above 2^15", n_heads, v.n_kv_heads);
   if (n_rows < 0 || max_q < 0 || max_kv < 0) return bad(ADEPT_ERR_INVALID_ARG, "negative size");
   if (max_kv > v.max_blocks * v.block_tokens)
     return bad(ADEPT_ERR_INVALID_ARG, "max_kv_len %d above the %d positions of a sequence", max_kv, v.max_blocks * v.block_tokens);

@@ -184,7 +184,7 @@ __device__ __forceinline__ bool split_find(const ChunkCall& a, const SplitPlan& 
   return false;
 }
 // Two e4m3 codes (low 16 bits) as two fp16: exact, NaN stays NaN.  (One instruction; through the toolkit's half2 type the few-row
-// kernel took 62.6 us where it takes 55.5.)
+// kernel took 62.6 us where it took 55.5.)
 __device__ __forceinline__ uint32_t e4m3x2_f16x2(uint32_t codes) {
   uint32_t h;
   asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((unsigned short)codes));
