@@ -168,7 +168,7 @@ def _prepare_verify(case, g):
     elif case["mode"] == "mixed":
         temp = torch.tensor([0.0, 0.7, 1.0, 1.3], device="cuda").repeat(len(d) // 4 + 1)[:len(d)].contiguous()
     return dict(target=logits.to(TYPES[case["target"]]), draft=None if case["draft"] == "none" else near.to(TYPES[case["draft"]]), tokens=tokens,
-                start=_i32(start), temp=temp, most=max(d) + 1, u=torch.rand(rows, generator=g, device="cuda"),
+                start=_i32(start), temp=temp, u=torch.rand(rows, generator=g, device="cuda"),
                 logprob=torch.zeros(rows, device="cuda"))
 
 
@@ -201,10 +201,9 @@ def prepare(case, seed):
     st = {"case": case}
     if case["kind"] == "verify":
         st.update(_prepare_verify(case, g))
-        n = case["seqs"]
         if own:
             import paper_2601_03700_gb300 as adept
-            st["ws"] = adept.verify_workspace(n, st["tokens"].numel(), case["vocab"])
+            st["ws"] = adept.verify_workspace(st["tokens"].numel())
         return st
     if case["kind"] == "round":
         lens, n_rows, blocks = _lengths(case), case["seqs"], case["blocks"]
@@ -382,7 +381,7 @@ def run(state):
             return _plain_verify(state)
         import paper_2601_03700_gb300 as adept
         accepted, nxt = (torch.empty(case["seqs"], dtype=torch.int32, device="cuda") for _ in range(2))
-        adept.adept_verify_drafts(state["target"], state["draft"], state["tokens"], state["start"], state["most"], state["u"], accepted, nxt,
+        adept.adept_verify_drafts(state["target"], state["draft"], state["tokens"], state["start"], state["u"], accepted, nxt,
                                   logprob=state["logprob"], temperature=state["temp"], workspace=state["ws"])
         return [accepted, nxt, state["logprob"]]
     if not own:
