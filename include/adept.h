@@ -492,6 +492,93 @@ ADEPT_API int64_t adept_chunk_attention_workspace(const adept_kv_cache* c, int n
  * Errors: INVALID_ARG (no error word, a stream in capture), CUDA. */
 ADEPT_API adept_status adept_kv_check(const adept_kv_cache* c, void* stream);
 
+/* ---- pages behind the sequences of a paged K/V cache -------------------------------------
+ * The block table of an adept_kv_cache, or of several (the layers of a model share one table), with a count per block: d_ref[i] =
+ * rows of the table that hold block i, plus what the program itself adds to keep a block (a prefix that no row holds at the
+ * moment); 0: free.  Rows may share blocks.  The table starts as all -1 with counts 0, or as the program sets both.
+ * The calls decide on the device, from the tables and lengths there, in row and block order: the same tables give the same
+ * result every time.  They allocate nothing, hold no state between calls and can be captured into a graph; calls on the
+ * same pages are ordered by their streams.  A row's entry that is neither -1 nor a block, a block that is held but
+ * counted as free, and lengths or rows out of range flag DEVICE_INPUT in d_err (adept_error_check); such an entry counts as -1, a row
+ * with such a length or source stays as it is.
+ *   d_ws   adept_kv_pages_workspace bytes on 16 bytes, of any contents; calls that may overlap on the GPU need one each
+ * Errors of all: INVALID_ARG (bad pages, NULL or misaligned pointers, a workspace too small), CUDA. */
+typedef struct {
+  int n_blocks;
+  int block_tokens;
+  int n_seq;                /* rows of the block table */
+  int max_blocks_per_seq;   /* its columns; at most 2^30 positions a row */
+  int32_t* d_block_table;
+  int32_t* d_ref;           /* [n_blocks], on 16 bytes */
+  uint32_t* d_err;          /* or NULL */
+} adept_kv_pages;
+ADEPT_API int64_t adept_kv_pages_workspace(const adept_kv_pages* p);
+
+/* Every row at once: row b becomes the first d_length[b] positions of what row d_source[b] held before the call (their blocks
+ * shared, counted once more), the rest of the row -1; blocks that nobody holds any more are free.  d_source[b] = b with the row's
+ * length: unchanged; a shorter length: cut back (drafts that were not accepted); d_source[b] < 0, or no positions: dropped;
+ * another row: a fork, or beams reordered.  Both [n_seq] int32. */
+ADEPT_API adept_status adept_kv_fork(const adept_kv_pages* p, const int32_t* d_source, const int32_t* d_length, void* d_ws, int64_t ws_bytes,
+                           void* stream);
+
+/* Makes positions d_length[b] .. d_new_length[b] - 1 of every row b writable: entries without a block get the free block of the
+ * lowest number (rows in order, a row's entries in order), and an entry whose block other rows hold too gets one of its own.
+ * Where such a block also holds positions below d_length[b], its contents have to follow: d_copy_src[b], d_copy_dst[b] name the
+ * blocks (-1: none), to be copied by adept_kv_copy_blocks before anything is written.  Of several rows that share that block and
+ * all grow, while nobody else holds it, the last keeps it.
+ * Rows are served in order while blocks last: row b if what the rows up to it ask for is there (a row that asks for no block
+ * always, unless it would keep a shared one that an earlier row did not get away from).  d_got[b] = d_new_length[b] where row b was served or holds what it
+ * needs, else d_length[b], and nothing of the row has changed.  d_new_length[b] <= d_length[b]: nothing is asked for.
+ * All [n_seq] int32.  CAPACITY: more than 4096 rows. */
+ADEPT_API adept_status adept_kv_reserve(const adept_kv_pages* p, const int32_t* d_length, const int32_t* d_new_length, int32_t* d_got,
+                              int32_t* d_copy_src, int32_t* d_copy_dst, void* d_ws, int64_t ws_bytes, void* stream);
+
+/* Moves the blocks in use to the front: with U of them in use (*d_used), the k-th in use past the first U goes to the k-th
+ * free one among those (both in ascending order), in the table and in the counts.  d_copy_src[k], d_copy_dst[k] ([n_blocks / 2]
+ * int32 each) name the moves, for adept_kv_copy_blocks; entries behind the last are -1.  Sources and targets are disjoint. */
+ADEPT_API adept_status adept_kv_compact(const adept_kv_pages* p, int32_t* d_used, int32_t* d_copy_src, int32_t* d_copy_dst, void* d_ws,
+                              int64_t ws_bytes, void* stream);
+
+/* Block d_dst[i] = block d_src[i], K and V (and exponents), in each of n_caches caches (an array of structs: the layers; of one
+ * type and size) for i < n_pairs; a pair with a negative number is left out, one out of range flags DEVICE_INPUT in the first cache's
+ * word.  Targets are distinct, and none is also a source (else it holds anything of either). */
+ADEPT_API adept_status adept_kv_copy_blocks(const adept_kv_cache* caches, int n_caches, int n_pairs, const int32_t* d_src, const int32_t* d_dst,
+                                  void* stream);
+
+/* ---- drafted tokens against the target's logits ------------------------------------------
+ * Sequence b's chunk is rows d_start[b] .. d_start[b + 1] - 1 (n_rows in all): d_tokens[r] is the chunk's token (its first the last
+ * one that was accepted, the others drafts, as a pass over the chunk takes them), row r of d_target the target's logits behind
+ * it.  With p_r = softmax(target_r / T), q_r = softmax(draft_r / T) (without d_draft: 1 at the draft itself) and x the draft
+ * d_tokens[r + 1], the drafts are accepted in order while log u_r + log q_r(x) < log p_r(x).  At the first that is not, the next
+ * token is drawn from w = max(p_r - q_r, 0) (from p_r where the sum of that is below 2^-20); behind the last draft, from
+ * w = p_r: the least i with w_0 + .. + w_i > (u + 2^-25) sum w, u the number of the sequence's last row.  With u uniform the tokens are
+ * distributed as the target's own.  T = 0 (greedy): drafts are accepted while they are the target's best token (the
+ * lowest of equals), and the next token is that; d_draft and d_u are not looked at.
+ *   d_target, d_draft   [n_rows][ld] ADEPT_DTYPE_* logits, -infinity allowed (a masked token); d_draft (may be NULL): row r is what
+ *                       d_tokens[r + 1] was drawn from, a sequence's last row is not read
+ *   d_start       [n_seq + 1] int32, ascending; a sequence may have no row (0 accepted, next token -1)
+ *   d_temperature [n_seq] fp32, 0 or 2^-10 .. 2^10; NULL: 1
+ *   d_u           [n_rows] fp32 in [0, 1)
+ *   d_accepted, d_next  [n_seq] int32: drafts accepted, the next token
+ *   d_logprob     [n_rows] fp32 or NULL: log p_r of each accepted draft (at its r), and of the next token at the row that it was drawn
+ *                 from (greedy: at T = 1); other rows are not written
+ *   d_err         error word or NULL
+ * Whatever the rows behind the deciding one hold does not enter.  A sequence whose rows are out of range, or which meets a token or
+ * number out of range, logits with NaN or +infinity, or with nothing above -infinity, gets -1, -1 and flags DEVICE_INPUT.
+ * Which draft is accepted and which token drawn follows from sums with a relative error of about 2^-40, whatever the logits' type; the log
+ * probabilities are off by some 10^-6.  The same call gives the same bits.
+ *   d_ws          adept_verify_workspace(n_rows) bytes on 16 bytes; calls that may overlap on the GPU need one each.  No
+ *                 smaller call needs more.
+ * Errors: INVALID_ARG (a size, type, stride or pointer), CAPACITY (above 2^24 rows or sequences), CUDA. */
+ADEPT_API adept_status adept_verify_drafts(int n_seq, int n_rows, int vocab, int target_dtype, const void* d_target, int64_t ld_target,
+                                 int draft_dtype, const void* d_draft, int64_t ld_draft, const int32_t* d_tokens,
+                                 const int32_t* d_start, const float* d_temperature, const float* d_u, int32_t* d_accepted,
+                                 int32_t* d_next, float* d_logprob, uint32_t* d_err, void* d_ws, int64_t ws_bytes, void* stream);
+ADEPT_API int64_t adept_verify_workspace(int n_rows);
+
+/* adept_kv_check for an error word by itself. */
+ADEPT_API adept_status adept_error_check(uint32_t* d_err, void* stream);
+
 /* ---- failure injection (tests of the error paths; no GPU fault is involved) ------------
  * adept_set_wait_limit: limit, in SM cycles, of the kernels' bounded waits on pipeline
  * progress (a ring slot being filled or released, an accumulator becoming ready) in the

@@ -42,6 +42,8 @@ ABI_SYMBOLS = [
     "adept_span_read", "adept_set_cross_source",
     "adept_kv_append", "adept_kv_gather", "adept_chunk_attention", "adept_chunk_attention_workspace", "adept_kv_check",
     "adept_extend",
+    "adept_kv_pages_workspace", "adept_kv_fork", "adept_kv_reserve", "adept_kv_compact", "adept_kv_copy_blocks",
+    "adept_verify_drafts", "adept_verify_workspace", "adept_error_check",
 ]
 
 
@@ -82,6 +84,12 @@ class AdeptKVCache(ctypes.Structure):
                 ("head_dim", ctypes.c_int), ("block_tokens", ctypes.c_int), ("n_seq", ctypes.c_int),
                 ("max_blocks_per_seq", ctypes.c_int), ("d_k", ctypes.c_void_p), ("d_v", ctypes.c_void_p),
                 ("d_k_exp", ctypes.c_void_p), ("d_v_exp", ctypes.c_void_p), ("d_block_table", ctypes.c_void_p),
+                ("d_err", ctypes.c_void_p)]
+
+
+class AdeptKVPages(ctypes.Structure):
+    _fields_ = [("n_blocks", ctypes.c_int), ("block_tokens", ctypes.c_int), ("n_seq", ctypes.c_int),
+                ("max_blocks_per_seq", ctypes.c_int), ("d_block_table", ctypes.c_void_p), ("d_ref", ctypes.c_void_p),
                 ("d_err", ctypes.c_void_p)]
 
 
@@ -154,6 +162,21 @@ def load_library(path: str = LIB_PATH):
     lib.adept_chunk_attention_workspace.restype = i64
     lib.adept_kv_check.argtypes = [kvp, st]
     lib.adept_kv_check.restype = c_int
+    pgp = ctypes.POINTER(AdeptKVPages)
+    lib.adept_kv_pages_workspace.argtypes = [pgp]
+    lib.adept_kv_pages_workspace.restype = i64
+    lib.adept_kv_fork.argtypes = [pgp, i32p, i32p, vp, i64, st]
+    lib.adept_kv_reserve.argtypes = [pgp, i32p, i32p, i32p, i32p, i32p, vp, i64, st]
+    lib.adept_kv_compact.argtypes = [pgp, i32p, i32p, i32p, vp, i64, st]
+    lib.adept_kv_copy_blocks.argtypes = [kvp, c_int, c_int, i32p, i32p, st]
+    lib.adept_verify_drafts.argtypes = [c_int, c_int, c_int, c_int, vp, i64, c_int, vp, i64, i32p, i32p, fp, fp, i32p, i32p, fp, vp, vp, i64,
+                                        st]
+    lib.adept_verify_workspace.argtypes = [c_int]
+    lib.adept_verify_workspace.restype = i64
+    lib.adept_error_check.argtypes = [vp, st]
+    for fn in (lib.adept_kv_fork, lib.adept_kv_reserve, lib.adept_kv_compact, lib.adept_kv_copy_blocks, lib.adept_verify_drafts,
+               lib.adept_error_check):
+        fn.restype = c_int
     for name in ABI_SYMBOLS:
         fn = getattr(lib, name)
         if fn.restype is ctypes.c_int or name in ("adept_model_load", "adept_prefill", "adept_decode_step",
@@ -407,16 +430,70 @@ def adept_set_alloc_fail_after(n: int):
 _KV_TORCH = {0: torch.float32, 1: torch.bfloat16, 2: torch.uint8}
 
 
+def _make(n: int, device, stream) -> torch.Tensor:
+    """n bytes of the call's stream's memory, which alone reuses them."""
+    if stream is not None and not hasattr(stream, "cuda_stream"):
+        stream = torch.cuda.ExternalStream(int(stream))
+    with torch.cuda.stream(stream):
+        return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+class KVPages:
+    """The pages behind one or more KVCaches (adept_kv_pages): block_table [n_seq, max_blocks_per_seq] int32 (-1: no block),
+    ref [n_blocks] int32 (rows that hold a block; 0: free) and err, the error word.  state: table and counts as one tensor, to
+    save and restore them."""
+
+    def __init__(self, n_blocks: int, n_seq: int, max_blocks_per_seq: int, block_tokens: int = 16, device="cuda"):
+        self.sizes = (n_blocks, n_seq, max_blocks_per_seq, block_tokens)
+        entries = n_seq * max_blocks_per_seq
+        at = (entries + 3) // 4 * 4   # (the counts start on 16 bytes)
+        self.state = torch.full((at + n_blocks,), -1, dtype=torch.int32, device=device)
+        self.block_table = self.state[:entries].view(n_seq, max_blocks_per_seq)
+        self.ref = self.state[at:].zero_()
+        self.err = torch.zeros(1, dtype=torch.int32, device=device)
+        self.device, self.index = self.state.device, self.state.get_device()   # (index < 0: not a GPU)
+        self.n_seq = n_seq
+        self._c = AdeptKVPages(n_blocks, block_tokens, n_seq, max_blocks_per_seq, self.block_table.data_ptr(), self.ref.data_ptr(),
+                               self.err.data_ptr())
+        self.ref_c = ctypes.byref(self._c)
+
+    def workspace(self, stream=None) -> torch.Tensor:
+        """A workspace for adept_kv_fork, adept_kv_reserve and adept_kv_compact calls on `stream`."""
+        n = load_library().adept_kv_pages_workspace(self.ref_c)
+        if n < 0:
+            _check(load_library(), None, 1)
+        return _make(n, self.device, stream)
+
+    def check(self, stream=None):
+        adept_error_check(self.err, stream)
+
+
+class KVLayers:
+    """Caches of one type and size on the same pages, a model's layers, for calls on all of them."""
+
+    def __init__(self, caches):
+        self.caches = list(caches)
+        if not self.caches or any(c.index != self.caches[0].index for c in self.caches):
+            raise ValueError("one or more caches on one device")
+        self.device, self.index = self.caches[0].device, self.caches[0].index
+        self.ref = (AdeptKVCache * len(self.caches))(*[c._c for c in self.caches])
+
+
 class KVCache:
     """A paged K/V cache in device tensors (adept_kv_cache): k, v [n_blocks, n_kv_heads, block_tokens, head_dim]
     (uint8 e4m3 codes for dtype "e4m3", with k_exp, v_exp [n_blocks, n_kv_heads, block_tokens], uint8), block_table
     [n_seq, max_blocks_per_seq] int32 (-1: no block) and err, the error word.  Tables and entries are the caller's to
-    set; the tensors stay where they are for the cache's life."""
+    set; the tensors stay where they are for the cache's life.  pages (a KVPages of the same sizes): the table and the error word
+    are those, which other layers' caches may share."""
 
     def __init__(self, n_blocks: int, n_kv_heads: int, head_dim: int, n_seq: int, max_blocks_per_seq: int,
-                 dtype: str = "bf16", block_tokens: int = 16, device="cuda"):
+                 dtype: str = "bf16", block_tokens: int = 16, device="cuda", pages: Optional[KVPages] = None):
         if dtype not in KV_TYPES:
             raise ValueError(f"dtype {dtype!r} unknown ({', '.join(KV_TYPES)})")
+        if pages is not None:
+            if (n_blocks, n_seq, max_blocks_per_seq, block_tokens) != pages.sizes:
+                raise ValueError(f"the cache's sizes are not those of its pages, {pages.sizes}")
+            device = pages.device
         t = KV_TYPES[dtype]
         shape = (n_blocks, n_kv_heads, block_tokens, head_dim)
         self.dtype = dtype
@@ -426,8 +503,11 @@ class KVCache:
         if dtype == "e4m3":   # 127: a scale of 1
             self.k_exp = torch.full(shape[:3], 127, dtype=torch.uint8, device=device)
             self.v_exp = torch.full_like(self.k_exp, 127)
-        self.block_table = torch.full((n_seq, max_blocks_per_seq), -1, dtype=torch.int32, device=device)
-        self.err = torch.zeros(1, dtype=torch.int32, device=device)
+        if pages is not None:
+            self.block_table, self.err = pages.block_table, pages.err
+        else:
+            self.block_table = torch.full((n_seq, max_blocks_per_seq), -1, dtype=torch.int32, device=device)
+            self.err = torch.zeros(1, dtype=torch.int32, device=device)
         self.device, self.index = self.k.device, self.k.get_device()   # (index < 0: not a GPU)
         self.q_dtype = torch.float32 if dtype == "f32" else torch.bfloat16
         self.n_seq, self.n_kv_heads, self.head_dim = n_seq, n_kv_heads, head_dim
@@ -444,10 +524,7 @@ class KVCache:
             _check(load_library(), None, 1)
         if n == 0:
             return None
-        if stream is not None and not hasattr(stream, "cuda_stream"):
-            stream = torch.cuda.ExternalStream(int(stream))
-        with torch.cuda.stream(stream):   # (memory of the call's stream, which alone reuses it)
-            return torch.empty(n, dtype=torch.uint8, device=self.device)
+        return _make(n, self.device, stream)
 
     def check(self, stream=None):
         adept_kv_check(self, stream)
@@ -482,14 +559,18 @@ def _call(cache: KVCache, fn, stream, *args):
     """fn(cache, *args, stream) with the cache's device as the current one."""
     if cache.index < 0:
         raise ValueError(f"the cache is on {cache.device}: the operators need a GPU")
-    lib = _lib
-    if torch.cuda.current_device() == cache.index:
-        st = fn(cache.ref, *args, _raw_stream(cache.index) if stream is None else _stream(stream))
+    _call_on(cache.index, fn, stream, cache.ref, *args)
+
+
+def _call_on(index: int, fn, stream, *args):
+    """fn(*args, stream) with GPU `index` as the current device."""
+    if torch.cuda.current_device() == index:
+        st = fn(*args, _raw_stream(index) if stream is None else _stream(stream))
     else:
-        with torch.cuda.device(cache.index):
-            st = fn(cache.ref, *args, _raw_stream(cache.index) if stream is None else _stream(stream))
+        with torch.cuda.device(index):
+            st = fn(*args, _raw_stream(index) if stream is None else _stream(stream))
     if st != ADEPT_OK:
-        _check(lib, None, st)
+        _check(_lib, None, st)
 
 
 def _raw_stream(index: int) -> int:
@@ -552,6 +633,120 @@ def adept_chunk_attention(cache: KVCache, q: torch.Tensor, q_start: torch.Tensor
 def adept_kv_check(cache: KVCache, stream=None):
     """Waits for the stream and raises where a kernel flagged an input out of range since the last check."""
     _call(cache, load_library().adept_kv_check, stream)
+
+
+def _pages_call(fn, pages: KVPages, workspace, stream, *args):
+    if pages.index < 0:
+        raise ValueError(f"the pages are on {pages.device}: the operators need a GPU")
+    if workspace is None:
+        workspace = pages.workspace(stream)
+    elif workspace.get_device() != pages.index or not workspace.is_contiguous():
+        raise ValueError(f"workspace must be contiguous on {pages.device}")
+    _call_on(pages.index, fn, stream, pages.ref_c, *args, workspace.data_ptr(), workspace.nbytes)
+
+
+def adept_kv_fork(pages: KVPages, source: torch.Tensor, length: torch.Tensor, workspace: Optional[torch.Tensor] = None, stream=None):
+    """Every row b of the pages at once: the first length[b] positions of what row source[b] held (< 0: none).  Forks, beams
+    reordered, rows cut back, rows dropped.  workspace: KVPages.workspace (None: one is made for the call)."""
+    fn, n = load_library().adept_kv_fork, pages.n_seq
+    _pages_call(fn, pages, workspace, stream, _index(pages, "source", source, n), _index(pages, "length", length, n))
+
+
+def adept_kv_reserve(pages: KVPages, length: torch.Tensor, new_length: torch.Tensor, got: torch.Tensor, copy_src: torch.Tensor,
+                     copy_dst: torch.Tensor, workspace: Optional[torch.Tensor] = None, stream=None):
+    """Makes positions length[b] .. new_length[b] - 1 of every row writable.  got: the length that each row has room for now;
+    copy_src, copy_dst: blocks that adept_kv_copy_blocks has to copy first (-1: none).  All [n_seq] int32."""
+    fn, n = load_library().adept_kv_reserve, pages.n_seq
+    _pages_call(fn, pages, workspace, stream, _index(pages, "length", length, n), _index(pages, "new_length", new_length, n),
+                _index(pages, "got", got, n), _index(pages, "copy_src", copy_src, n), _index(pages, "copy_dst", copy_dst, n))
+
+
+def adept_kv_compact(pages: KVPages, used: torch.Tensor, copy_src: torch.Tensor, copy_dst: torch.Tensor,
+                     workspace: Optional[torch.Tensor] = None, stream=None):
+    """Moves the blocks in use to the front of the pool.  used [1]: how many there are; copy_src, copy_dst [n_blocks // 2]: the moves
+    that adept_kv_copy_blocks has to make (-1 behind the last).  All int32."""
+    fn, n = load_library().adept_kv_compact, pages.sizes[0] // 2
+    _pages_call(fn, pages, workspace, stream, _index(pages, "used", used, 1), _index(pages, "copy_src", copy_src, n),
+                _index(pages, "copy_dst", copy_dst, n))
+
+
+def adept_kv_copy_blocks(layers, src: torch.Tensor, dst: torch.Tensor, stream=None):
+    """Block dst[i] = block src[i], K and V, in every cache of a KVLayers (or in one KVCache); a negative number: left out."""
+    fn, n = load_library().adept_kv_copy_blocks, src.shape[0]
+    s, d = _index(layers, "src", src, n), _index(layers, "dst", dst, n)
+    _call(layers, fn, stream, len(layers.caches) if isinstance(layers, KVLayers) else 1, n, s, d)
+
+
+def adept_error_check(err: torch.Tensor, stream=None):
+    """Waits for the stream and raises where a kernel flagged an input out of range in the word since the last check."""
+    if err.get_device() < 0:
+        raise ValueError(f"the error word is on {err.device}: the operators need a GPU")
+    fn = load_library().adept_error_check
+    _call_on(err.get_device(), fn, stream, err.data_ptr())
+
+
+# ---------------------------------------------------------------------------
+# drafted tokens
+# ---------------------------------------------------------------------------
+
+def verify_workspace(n_rows: int, device="cuda", stream=None) -> torch.Tensor:
+    """A workspace for adept_verify_drafts calls of up to n_rows rows on `stream`."""
+    n = load_library().adept_verify_workspace(n_rows)
+    if n < 0:
+        _check(load_library(), None, 1)
+    return _make(n, device, stream)
+
+
+def _vector(like: torch.Tensor, name: str, t: Optional[torch.Tensor], n: int, dtype):
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.get_device() != like.get_device() or t.shape != (n,) or not t.is_contiguous():
+        raise ValueError(f"{name} must be {n} contiguous {dtype} values on {like.device}")
+    return t.data_ptr()
+
+
+def _logits(like: torch.Tensor, name: str, t: torch.Tensor):
+    """(type, pointer, row stride) of [rows, vocab], dense within a row."""
+    if t.dtype is not torch.bfloat16 and t.dtype is not torch.float32:
+        raise ValueError(f"{name} must be float32 or bfloat16")
+    if t.dim() != 2 or t.shape != like.shape or t.get_device() != like.get_device():
+        raise ValueError(f"{name} must be {list(like.shape)} on {like.device}" if t is not like else f"{name} must be [rows, vocab]")
+    n, v = t.shape
+    ld = t.stride(0) if n > 1 else v
+    if n and ((v > 1 and t.stride(1) != 1) or ld < v):
+        raise ValueError(f"the rows of {name} must be dense and must not overlap")
+    return 1 if t.dtype is torch.bfloat16 else 0, t.data_ptr(), ld
+
+
+def adept_verify_drafts(target: torch.Tensor, draft: Optional[torch.Tensor], tokens: torch.Tensor, start: torch.Tensor, u: torch.Tensor,
+                        accepted: torch.Tensor, next_token: torch.Tensor, logprob: Optional[torch.Tensor] = None,
+                        temperature: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                        err: Optional[torch.Tensor] = None, stream=None):
+    """How many of each sequence's drafted tokens hold against the target's logits, and the token that comes next.  Sequence b's chunk is
+    rows start[b] .. start[b + 1]: tokens[r] its tokens (the last accepted one, then the drafts), target[r] the target's logits behind
+    them, draft[r] the logits that tokens[r + 1] was drawn from (None: drafts without probabilities), u[r] uniform numbers.
+    temperature [n_seq] (None: 1; 0: greedy).  logprob [rows]: log probabilities of the tokens taken.  err: a KVPages' or KVCache's word, or
+    one int32.  workspace: verify_workspace of as many rows (None: one is made for the call)."""
+    lib = load_library()
+    i32, f32 = torch.int32, torch.float32
+    td, tp, tl = _logits(target, "target", target)
+    dd, dp, dl = (td, None, 0) if draft is None else _logits(target, "draft", draft)
+    n, v = target.shape
+    n_seq = start.shape[0] - 1 if start.dim() == 1 else -1
+    if n_seq < 0:
+        raise ValueError("start must be n_seq + 1 values")
+    vec = lambda name, t, k, dt: _vector(target, name, t, k, dt)  # noqa: E731
+    args = (vec("tokens", tokens, n, i32), vec("start", start, n_seq + 1, i32), vec("temperature", temperature, n_seq, f32), vec("u", u, n, f32),
+            vec("accepted", accepted, n_seq, i32), vec("next_token", next_token, n_seq, i32), vec("logprob", logprob, n, f32),
+            vec("err", err, 1, i32))
+    if target.get_device() < 0:
+        raise ValueError(f"the logits are on {target.device}: the operators need a GPU")
+    if workspace is None:
+        workspace = verify_workspace(n, target.device, stream)
+    elif workspace.get_device() != target.get_device() or not workspace.is_contiguous():
+        raise ValueError(f"workspace must be contiguous on {target.device}")
+    _call_on(target.get_device(), lib.adept_verify_drafts, stream, n_seq, n, v, td, tp, tl, dd, dp, dl, *args, workspace.data_ptr(),
+             workspace.nbytes)
 
 
 # ---------------------------------------------------------------------------

@@ -4,7 +4,7 @@
 #include "common.cuh"
 #include "kernels.h"
 #include "kv_paged.h"
-#include "model_view.h"
+#include "op_status.h"
 
 #include <cmath>
 #include <cstdarg>
@@ -12,7 +12,7 @@
 
 using namespace adept;
 
-namespace {
+namespace adept {
 
 adept_status bad(adept_status s, const char* fmt, ...) {
   char buf[256];
@@ -22,6 +22,12 @@ adept_status bad(adept_status s, const char* fmt, ...) {
   va_end(ap);
   global_set_error(buf);
   return s;
+}
+
+adept_status launched(cudaError_t e) {
+  if (e == cudaSuccess) return ADEPT_OK;
+  cudaGetLastError();
+  return bad(ADEPT_ERR_CUDA, "kernel launch failed: %s", cudaGetErrorString(e));
 }
 
 adept_status view_of(const adept_kv_cache* c, KvPaged* v) {
@@ -45,6 +51,10 @@ adept_status view_of(const adept_kv_cache* c, KvPaged* v) {
   return ADEPT_OK;
 }
 
+}  // namespace adept
+
+namespace {
+
 adept_status rows_ok(const KvPaged& v, int n_rows, int dtype, const void* k, int64_t ld_k, const void* vv, int64_t ld_v,
                      const int32_t* seq, const int32_t* pos) {
   if (n_rows < 0) return bad(ADEPT_ERR_INVALID_ARG, "n_rows %d < 0", n_rows);
@@ -57,12 +67,6 @@ adept_status rows_ok(const KvPaged& v, int n_rows, int dtype, const void* k, int
   if (((uintptr_t)k | (uintptr_t)vv) & m) return bad(ADEPT_ERR_INVALID_ARG, "misaligned rows");
   if (((uintptr_t)seq | (uintptr_t)pos) & 3) return bad(ADEPT_ERR_INVALID_ARG, "misaligned sequences or positions");
   return ADEPT_OK;
-}
-
-adept_status launched(cudaError_t e) {
-  if (e == cudaSuccess) return ADEPT_OK;
-  cudaGetLastError();
-  return bad(ADEPT_ERR_CUDA, "kernel launch failed: %s", cudaGetErrorString(e));
 }
 
 adept_status call_ok(const KvPaged& v, int n_heads, int n_rows, int max_q, int max_kv) {
