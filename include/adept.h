@@ -555,7 +555,7 @@ ADEPT_API adept_status adept_kv_copy_blocks(const adept_kv_cache* caches, int n_
  * distributed as the target's own.  T = 0 (greedy): drafts are accepted while they are the target's best token (the
  * lowest of equals), and the next token is that; d_draft and d_u are not looked at.
  *   d_target, d_draft   [n_rows][ld] ADEPT_DTYPE_* logits, -infinity allowed (a masked token); d_draft (may be NULL): row r is what
- *                       d_tokens[r + 1] was drawn from, a sequence's last row is not read
+ *                       d_tokens[r + 1] was drawn from, a sequence's last row may hold anything
  *   d_start       [n_seq + 1] int32, ascending; a sequence may have no row (0 accepted, next token -1)
  *   d_temperature [n_seq] fp32, 0 or 2^-10 .. 2^10; NULL: 1
  *   d_u           [n_rows] fp32 in [0, 1)

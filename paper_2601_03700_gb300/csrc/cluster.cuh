@@ -2,12 +2,19 @@
 #pragma once
 #include "common.cuh"
 
+#include <atomic>
+
 namespace adept {
 
 __device__ __forceinline__ int cluster_rank() {
   int r;
   asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
   return r;
+}
+__device__ __forceinline__ int cluster_size() {
+  int n;
+  asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(n));
+  return n;
 }
 // All threads of the cluster, converged warps; orders their global and shared memory accesses.
 __device__ __forceinline__ void cluster_barrier() {
@@ -22,14 +29,28 @@ __device__ __forceinline__ uint32_t cluster_map(const void* p, int rank) {
 __device__ __forceinline__ void cluster_store(int* p, int rank, int v) {
   asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(cluster_map(p, rank)), "r"(v) : "memory");
 }
-__device__ __forceinline__ void cluster_store(double* p, int rank, double v) {
-  asm volatile("st.shared::cluster.f64 [%0], %1;" ::"r"(cluster_map(p, rank)), "d"(v) : "memory");
+__device__ __forceinline__ void cluster_store(long long* p, int rank, long long v) {
+  asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(cluster_map(p, rank)), "l"(v) : "memory");
+}
+
+// Lets a kernel run in clusters of 16, once per device (Tag: a type of the kernel's own).
+template <typename Tag, typename K>
+inline cudaError_t cluster16_once(K* kernel) {
+  static std::atomic<unsigned long long> done{0};   // bit per device
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  const unsigned long long bit = dev < 64 ? 1ull << dev : 0;
+  if (bit && (done.load() & bit)) return cudaSuccess;
+  e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+  if (e == cudaSuccess) done.fetch_or(bit);
+  return e;
 }
 
 template <typename... KArgs, typename... Args>
-inline cudaError_t launch_cluster(void (*kernel)(KArgs...), int grid, int cluster, int block, size_t smem, cudaStream_t st, Args&&... args) {
+inline cudaError_t launch_cluster(void (*kernel)(KArgs...), dim3 grid, int cluster, int block, size_t smem, cudaStream_t st, Args&&... args) {
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)grid);
+  cfg.gridDim = grid;
   cfg.blockDim = dim3((unsigned)block);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = st;

@@ -382,11 +382,11 @@ cudaError_t launch_kv_reserve(cudaStream_t st, const Pages& p, const int* length
   struct Tag;
   cudaError_t e = smem_once<Tag>(kv_reserve_kernel, PG_MAX_SEQ * 16 + 2 * PG_MAX_SEQ * 12);
   if (e != cudaSuccess) return e;
-  return launch_cluster(kv_reserve_kernel, PG_CTAS, PG_CTAS, PG_THREADS, smem, st, p, a);
+  return launch_cluster(kv_reserve_kernel, dim3(PG_CTAS), PG_CTAS, PG_THREADS, smem, st, p, a);
 }
 
 cudaError_t launch_kv_compact(cudaStream_t st, const Pages& p, int* used, int* src, int* dst, int* ws) {
-  return launch_cluster(kv_compact_kernel, PG_CTAS, PG_CTAS, PG_THREADS, 0, st, p, used, src, dst, ws);
+  return launch_cluster(kv_compact_kernel, dim3(PG_CTAS), PG_CTAS, PG_THREADS, 0, st, p, used, src, dst, ws);
 }
 
 cudaError_t launch_kv_copy_blocks(cudaStream_t st, const CopyLayers& c, int n_pairs, const int* src, const int* dst) {

@@ -16,27 +16,27 @@
 namespace adept {
 namespace {
 
-constexpr int VS_THREADS = 256;                  // rows' statistics
-constexpr int VD_THREADS = 512, VD_CTAS = 8;     // decision: threads of a CTA, CTAs of a sequence's cluster
-constexpr double VD_LEAST = 9.5367431640625e-07; // 2^-20: residual mass below which the token is drawn from p
+constexpr int VS_THREADS = 128, VS_LOADS = 4, VS_PARTS = 8;   // statistics: 16-byte loads of a thread under way (twice), CTAs of a row at most
+constexpr float VS_HUGE = 1e6f;
+constexpr int VD_THREADS = 512, VD_CTAS = 16, VD_LOADS = 4;   // decision: threads of a CTA, CTAs of a sequence at most, loads of a thread under way
+constexpr int VD_LEAST = 20;                     // max(p - q, 0) sums to less than 2^-this: the token is drawn from p
+constexpr int VD_FINE = 14;                      // to less than 2^-this: summed token by token
 constexpr int VD_TAB = 64;
 
-// Relative difference of the two sides of a test below which 32-bit sums do not decide it.  A sum's error: a thread's chain of
-// additions and rescalings, one for each of its 16-byte pieces, 2^-22 each; the exponentials' argument, rounded in three places
-// 2^-24 of up to log2 V + 2 units on average; 20 more for the joins.  Two sums.
-__device__ __forceinline__ double close_of(int vocab, int n_split) {
-  return 2 * 2.384185791015625e-07 * (vocab / (4 * VS_THREADS * n_split) + 1 + 22 + 20);
+// Difference of the logarithms of a test's two sides below which 32-bit sums do not decide it.  A sum's error: a thread's
+// chain of additions and rescalings, one for each of its 16-byte pieces, 2^-22 each; the exponents, rounded in three places 2^-24 of up to
+// log2 V + 2 units on average; 20 more for the joins.  Two sums, and three logarithms of 2^-23 of up to log V or log 2^-24.
+__device__ __forceinline__ float close_of(int vocab, int parts) {
+  return 2 * 2.384185791015625e-07f * (vocab / (4 * VS_THREADS * parts) + 1 + 22 + 20 + 12);
 }
 
 struct Stat {
   float m, z;   // maximum; sum of exp((l - m) / T)
-  int at;       // first index of the maximum
-  int pad;
+  int at;       // first index of the maximum (greedy sequences)
+  float l;      // the row's first part: the logit of the token that is held against it
 };
 
-// 1 / T in units of log 2; a greedy sequence (T = 0) has the probabilities of T = 1.
 __device__ __forceinline__ bool temp_ok(float t) { return t == 0.f || (t >= 9.765625e-4f && t <= 1024.f); }
-__device__ __forceinline__ double log2_scale(float t) { return 1.4426950408889634 / (t == 0.f ? 1.0 : (double)t); }
 
 // Sequence b's rows, false: out of range (or none).
 struct SeqRows {
@@ -51,218 +51,422 @@ __device__ __forceinline__ SeqRows seq_rows(const VerifyCall& a, int b) {
   return r;
 }
 
+// 16 bytes of logits.
 template <typename T>
-struct Vec;
-template <>
-struct Vec<float> {
-  static constexpr int N = 4;
-  static __device__ __forceinline__ void get(const float* p, float (&x)[4]) {
-    const float4 v = __ldcs(reinterpret_cast<const float4*>(p));
-    x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w;
+struct Vec {
+  static constexpr int N = 16 / (int)sizeof(T);
+  static __device__ __forceinline__ uint4 none() {   // -infinity
+    const uint32_t w = sizeof(T) == 4 ? 0xff800000u : 0xff80ff80u;
+    return make_uint4(w, w, w, w);
   }
-};
-template <>
-struct Vec<bf16> {
-  static constexpr int N = 8;
-  static __device__ __forceinline__ void get(const bf16* p, float (&x)[8]) {
-    const uint4 v = __ldcs(reinterpret_cast<const uint4*>(p));
+  static __device__ __forceinline__ float at(const uint4& v, int i) {
     const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(i & 1 ? w[i >> 1] & 0xffff0000u : w[i >> 1] << 16);
+    if constexpr (sizeof(T) == 4) return __uint_as_float(w[i]);
+    return __uint_as_float(i & 1 ? w[i >> 1] & 0xffff0000u : w[i >> 1] << 16);
   }
 };
 
-// The maximum starts at the type's lowest value, not at -infinity: rows that begin with masked tokens need no special case
-// (lowest - lowest = 0, -infinity - lowest = -infinity).
+// Maximum so far and z = sum of 2^(l c - M) with M = m c as fp32 has it: one fused operation, one exponential and one addition an
+// element.  What M's rounding makes of z (off) is a factor that all its terms have.  Where |m c| is large M is m c itself.
 struct Running {
-  float m = -FLT_MAX, z = 0.f;
-  int at = 0x7fffffff;
-  __device__ __forceinline__ void join(float om, float oz, int oat, float c) {
-    if (om > m || (om == m && oat < at)) at = oat;
-    const float nm = fmaxf(m, om);
-    z = z * ex2_approx((m - nm) * c) + oz * ex2_approx((om - nm) * c);
-    m = nm;
+  float m = -INFINITY, z = 0.f;
+  int at = -1;   // where the maximum was first met (what add was given; joined: any of them)
+  static __device__ __forceinline__ float off(float m, float c) {
+    const float M = __fmul_rn(m, c);
+    return fabsf(M) < VS_HUGE ? __fmaf_rn(m, c, -M) : 0.f;
   }
-  template <int N>
-  __device__ __forceinline__ void add(const float (&x)[N], int i0, float c) {
-    float g = x[0];
+  __device__ __forceinline__ void raise(float to, float c) {
+    if (m != -INFINITY) z *= ex2_approx((m - to) * c - off(m, c) + off(to, c));   // (else z is 0, or NaN)
+    m = to;
+  }
+  __device__ __forceinline__ void join(float om, float oz, float c) {
+    if (om > m) raise(om, c);
+    z += om == -INFINITY ? oz : oz * ex2_approx((om - m) * c - off(om, c) + off(m, c));
+  }
+  template <typename T, int L>   // L 16-byte pieces
+  __device__ __forceinline__ void add(const uint4 (&w)[L], int i0, float c) {
+    using V = Vec<T>;
+    float g = -INFINITY;
 #pragma unroll
-    for (int i = 1; i < N; ++i) g = fmaxf(g, x[i]);
+    for (int i = 0; i < L; ++i)
+#pragma unroll
+      for (int k = 0; k < V::N; ++k) g = fmaxf(g, V::at(w[i], k));
     if (g > m) {
-      z *= ex2_approx((m - g) * c);
-      m = g;
-      at = 0x7fffffff;
-    }
-    if (at == 0x7fffffff) {
-#pragma unroll
-      for (int i = N - 1; i >= 0; --i)
-        if (x[i] == m) at = i0 + i;
+      raise(g, c);
+      at = i0;
     }
     float s = 0.f;
+    const float M = __fmul_rn(m, c);
+    if (fabsf(M) < VS_HUGE) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) s += ex2_approx((x[i] - m) * c);
+      for (int i = 0; i < L; ++i)
+#pragma unroll
+        for (int k = 0; k < V::N; ++k) s += ex2_approx(__fmaf_rn(V::at(w[i], k), c, -M));
+    } else {   // (or nothing above -infinity was there yet)
+      const float ref = m == -INFINITY ? 0.f : m;
+#pragma unroll
+      for (int i = 0; i < L; ++i)
+#pragma unroll
+        for (int k = 0; k < V::N; ++k) s += ex2_approx((V::at(w[i], k) - ref) * c);
+    }
     z += s;
   }
 };
 
+// Statistics of part blockIdx.x % parts of row blockIdx.x / parts, the target's (blockIdx.y = 0) or the draft's.
 template <typename T>
-__device__ void row_stats(const T* x, int V, float c, int split, int n_split, Stat* out) {
-  constexpr int N = Vec<T>::N;
+__device__ __forceinline__ void row_stats(const VerifyCall& a, const T* x, bool draft, int r, int part, int parts, Stat* out) {
+  using V = Vec<T>;
+  __shared__ int s_seq, s_at;
   __shared__ float s_m[VS_THREADS / 32], s_z[VS_THREADS / 32];
-  __shared__ int s_at[VS_THREADS / 32];
-  const int tid = threadIdx.x;
+  const int tid = threadIdx.x, lane = tid & 31, n = a.vocab;
   // elements before the first 16-byte boundary, 16-byte pieces, the rest
-  const int head = min(V, (int)((16 - ((uintptr_t)x & 15)) & 15) / (int)sizeof(T));
-  const int nv = (V - head) / N, v0 = (int)((long long)nv * split / n_split), v1 = (int)((long long)nv * (split + 1) / n_split);
-  Running r;
-  if (split == 0 && tid < head) {
-    const float y[1] = {to_f<T>(x[tid])};
-    r.add(y, tid, c);
-  }
-  for (int v = v0 + tid; v < v1; v += VS_THREADS) {
-    float y[N];
-    Vec<T>::get(x + head + (size_t)v * N, y);
-    r.add(y, head + v * N, c);
-  }
-  const int tail = head + nv * N + tid;
-  if (split == n_split - 1 && tail < V) {
-    const float y[1] = {to_f<T>(x[tail])};
-    r.add(y, tail, c);
-  }
+  const int head = min(n, (int)((16 - ((uintptr_t)x & 15)) & 15) / (int)sizeof(T));
+  const int nv = (n - head) / V::N, v0 = (int)((long long)nv * part / parts), v1 = (int)((long long)nv * (part + 1) / parts);
+  const uint4* body = reinterpret_cast<const uint4*>(x + head);
+  auto load = [&](int v, uint4 (&w)[VS_LOADS]) {
 #pragma unroll
-  for (int o = 16; o; o >>= 1)
-    r.join(__shfl_xor_sync(0xffffffffu, r.m, o), __shfl_xor_sync(0xffffffffu, r.z, o), __shfl_xor_sync(0xffffffffu, r.at, o), c);
-  if ((tid & 31) == 0) {
-    s_m[tid >> 5] = r.m;
-    s_z[tid >> 5] = r.z;
-    s_at[tid >> 5] = r.at;
-  }
-  __syncthreads();
+    for (int i = 0; i < VS_LOADS; ++i) w[i] = v + i * VS_THREADS < v1 ? __ldcs(body + v + i * VS_THREADS) : V::none();
+  };
+  // the first loads are under way while the row's sequence is looked up
+  int v = v0 + tid;
+  uint4 w[VS_LOADS];
+  load(v, w);
+  uint4 ends[1] = {V::none()};   // what lies beside the 16-byte pieces: an element each
+  const int past = head + nv * V::N + tid - 32;
+  const bool first = part == 0 && tid < head, last = part == parts - 1 && tid >= 32 && past < n;
+  int end_at = first ? tid : past;
+  if (first || last) ends[0].x = sizeof(T) == 4 ? *reinterpret_cast<const uint32_t*>(x + end_at) : 0xff800000u | *reinterpret_cast<const uint16_t*>(x + end_at);
+  int id = -1;   // the token that the row's distribution is held against
   if (tid == 0) {
-    for (int w = 1; w < VS_THREADS / 32; ++w) r.join(s_m[w], s_z[w], s_at[w], c);
-    *out = Stat{r.m, r.z, r.at, 0};
+    s_seq = 0x7fffffff;
+    if (part == 0 && r + 1 < a.n_rows) id = a.tokens[r + 1];
   }
-}
-
-// Statistics of part blockIdx.x % n_split of row blockIdx.x / n_split: the target's (blockIdx.y = 0) or the draft's.
-template <typename TT, typename TD>
-__global__ void __launch_bounds__(VS_THREADS) verify_stats_kernel(VerifyCall a, int n_split, Stat* stats) {
-  PDL_ENTRY();
-  __shared__ int s_seq;
-  const int r = (int)(blockIdx.x / n_split), split = (int)(blockIdx.x % n_split), tid = threadIdx.x;
-  if (tid == 0) s_seq = 0x7fffffff;
   __syncthreads();
   for (int b = tid; b < a.n_seq; b += VS_THREADS) {
     const SeqRows q = seq_rows(a, b);
     if (q.ok && q.s <= r && r < q.e) atomicMin(&s_seq, b);
   }
+  const float held = id >= 0 && id < n ? to_f<T>(x[id]) : -INFINITY;
   __syncthreads();
   if (s_seq == 0x7fffffff) return;   // nobody's row
   const float t = a.temp ? a.temp[s_seq] : 1.f;
   if (!temp_ok(t)) return;
-  if (blockIdx.y && (t == 0.f || r == a.start[s_seq + 1] - 1)) return;   // a draft row that nothing is held against
-  Stat* out = stats + ((size_t)blockIdx.y * a.n_rows + r) * n_split + split;
-  const float c = (float)log2_scale(t);
+  if (draft && (t == 0.f || r == a.start[s_seq + 1] - 1)) return;   // a draft row that nothing is held against
+  const float c = 1.44269504088896f / (t == 0.f ? 1.f : t);   // (a greedy sequence has the probabilities of T = 1)
+  Running run;
+  if (first) run.add<T>(ends, -2, c);
+  while (v < v1) {   // the next loads under way before these are used
+    uint4 next[VS_LOADS];
+    const int u = v + VS_LOADS * VS_THREADS;
+    load(u, next);
+    run.add<T>(w, v, c);
+#pragma unroll
+    for (int i = 0; i < VS_LOADS; ++i) w[i] = next[i];
+    v = u;
+  }
+  if (last) run.add<T>(ends, -2, c);
+  const float mine = run.m;
+  auto warp_join = [&](int o0) {
+    for (int o = o0; o; o >>= 1) run.join(__shfl_xor_sync(0xffffffffu, run.m, o), __shfl_xor_sync(0xffffffffu, run.z, o), c);
+  };
+  const int where = run.at;
+  warp_join(16);
+  if (lane == 0) {
+    s_m[tid >> 5] = run.m;
+    s_z[tid >> 5] = run.z;
+  }
+  if (tid == 0) s_at = 0x7fffffff;
+  __syncthreads();
+  run.m = s_m[lane % (VS_THREADS / 32)];
+  run.z = s_z[lane % (VS_THREADS / 32)];
+  warp_join(VS_THREADS / 64);
+  if (t == 0.f) {   // (uniform) the first index of the maximum: the threads that met it look at those pieces again
+    if (mine == run.m) {
+      if (where == -2) {
+        atomicMin(&s_at, end_at);
+      } else if (where >= 0) {
+        load(where, w);
+#pragma unroll
+        for (int i = VS_LOADS - 1; i >= 0; --i)
+#pragma unroll
+          for (int k = V::N - 1; k >= 0; --k)
+            if (V::at(w[i], k) == mine) end_at = head + (where + i * VS_THREADS) * V::N + k;
+        atomicMin(&s_at, end_at);
+      }
+    }
+    __syncthreads();
+  }
+  if (tid == 0) *out = Stat{run.m, run.z * ex2_approx(-Running::off(run.m, c)), s_at, held};
+}
+
+template <typename TT, typename TD>
+__global__ void __launch_bounds__(VS_THREADS, 7) verify_stats_kernel(VerifyCall a, int parts, Stat* stats) {
+  PDL_ENTRY();
+  const int r = (int)blockIdx.x / parts, part = (int)blockIdx.x % parts;
+  Stat* out = stats + ((size_t)blockIdx.y * a.n_rows + r) * parts + part;
   if (blockIdx.y == 0)
-    row_stats((const TT*)a.target + r * a.ld_t, a.vocab, c, split, n_split, out);
+    row_stats(a, (const TT*)a.target + r * a.ld_t, false, r, part, parts, out);
   else
-    row_stats((const TD*)a.draft + r * a.ld_d, a.vocab, c, split, n_split, out);
+    row_stats(a, (const TD*)a.draft + r * a.ld_d, true, r, part, parts, out);
 }
 
 // ---------------------------------------------------------------------------------------------
-// Weights of two 32-bit parts.
+// Numbers of two 32-bit parts, h + l with |l| at most half a step of h: about 2^-46 relative.  64-bit arithmetic runs at
+// two operations a cycle and SM here: with the sums and the joins in it a call of one chunk of 4 drafts over 50257 tokens took 54 us,
+// without it 25.
 // ---------------------------------------------------------------------------------------------
 struct Two {
   float h, l;
 };
-__device__ __forceinline__ Two two_of(double x) {
-  const float h = (float)x;
-  return Two{h, (float)(x - (double)h)};
+__device__ __forceinline__ Two norm2(float h, float l) {   // |l| <= |h|, or h = 0
+  const float s = __fadd_rn(h, l);
+  return Two{s, __fsub_rn(l, __fsub_rn(s, h))};
 }
-// Sum of two-part numbers, each thread's own (Knuth's two-sum; the low parts add up beside it).
-struct Sum2 {
-  float h = 0.f, l = 0.f;
-  __device__ __forceinline__ void add(Two x) {
-    const float s = __fadd_rn(h, x.h), t = __fsub_rn(s, h);
-    l = __fadd_rn(l, __fadd_rn(__fadd_rn(__fsub_rn(h, __fsub_rn(s, t)), __fsub_rn(x.h, t)), x.l));
-    h = s;
-  }
-  __device__ __forceinline__ double value() const { return (double)h + (double)l; }
+// a + b = s + e (Knuth)
+__device__ __forceinline__ Two sum_of(float a, float b) {
+  const float s = __fadd_rn(a, b), t = __fsub_rn(s, a);
+  return Two{s, __fadd_rn(__fsub_rn(a, __fsub_rn(s, t)), __fsub_rn(b, t))};
+}
+__device__ __forceinline__ Two operator+(Two a, Two b) {
+  const Two s = sum_of(a.h, b.h);
+  return norm2(s.h, __fadd_rn(s.l, __fadd_rn(a.l, b.l)));
+}
+__device__ __forceinline__ Two operator*(Two a, Two b) {
+  const float p = __fmul_rn(a.h, b.h);
+  return norm2(p, __fmaf_rn(a.h, b.h, -p) + __fmaf_rn(a.h, b.l, a.l * b.h));
+}
+__device__ __forceinline__ Two operator/(Two a, Two b) {   // (one step of division by the first part, then of the remainder)
+  const float q = __fdiv_rn(a.h, b.h);
+  const float p = __fmul_rn(q, b.h), e = __fmaf_rn(q, b.h, -p);
+  const float r = __fsub_rn(a.h, p) - e + __fmaf_rn(-q, b.l, a.l);
+  return norm2(q, __fdiv_rn(r, b.h));
+}
+
+// Sums over threads in whole numbers, so that any order gives the same: of 2^-58 times the power of two in the row's sum of weights,
+// as the 32-bit sums have it.
+__device__ __forceinline__ float unit_of(float z) { return __uint_as_float((312u << 23) - (__float_as_uint(z) & 0x7f800000u)); }   // in one
+__device__ __forceinline__ long long whole(Two v, float unit) { return max(__float2ll_rn(v.h * unit) + __float2ll_rn(v.l * unit), 0ll); }
+__device__ __forceinline__ long long warp_sum(long long v) {   // 0 <= v < 2^61, the sum below 2^62
+  constexpr unsigned M = (1u << 27) - 1;
+  const unsigned a = __reduce_add_sync(0xffffffffu, (unsigned)v & M), b = __reduce_add_sync(0xffffffffu, (unsigned)(v >> 27) & M),
+                 c = __reduce_add_sync(0xffffffffu, (unsigned)(v >> 54));
+  return (long long)a + ((long long)b << 27) + ((long long)c << 54);
+}
+__device__ __forceinline__ Two two_of(long long v) {
+  const float h = __ll2float_rn(v);
+  return Two{h, __ll2float_rn(v - __float2ll_rn(h))};
+}
+// a / b to 2^-44: one step of division by the first part, then of the remainder
+__device__ __forceinline__ Two quotient(Two a, Two b) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(b.h));
+  const float q = a.h * r;
+  return norm2(q, r * (__fmaf_rn(-q, b.h, a.h) + __fmaf_rn(-q, b.l, a.l)));
+}
+
+// 2^(k / 64) in two parts; a CTA's copy.
+struct VdTab {
+  float h[VD_TAB], l[VD_TAB];
+};
+__device__ const float2 VD_POW[VD_TAB] = {
+    {0x1.0000000000000p+0f, 0x0.0p+0f}, {0x1.02c9a40000000p+0f, -0x1.887fa00000000p-28f},
+    {0x1.059b0e0000000p+0f, -0x1.9d4f520000000p-25f}, {0x1.0874520000000p+0f, -0x1.e2990e0000000p-26f},
+    {0x1.0b55860000000p+0f, 0x1.9f31220000000p-25f}, {0x1.0e3ec40000000p+0f, -0x1.a585cc0000000p-25f},
+    {0x1.11301e0000000p+0f, -0x1.fdb4960000000p-25f}, {0x1.1429aa0000000p+0f, 0x1.d525bc0000000p-25f},
+    {0x1.172b840000000p+0f, -0x1.c157420000000p-27f}, {0x1.1a35be0000000p+0f, 0x1.6df96e0000000p-25f},
+    {0x1.1d48740000000p+0f, -0x1.d2e8ca0000000p-25f}, {0x1.2063b80000000p+0f, 0x1.0c519a0000000p-25f},
+    {0x1.2387a60000000p+0f, 0x1.ceac480000000p-25f}, {0x1.26b4560000000p+0f, 0x1.789f380000000p-26f},
+    {0x1.29e9e00000000p+0f, -0x1.5c04240000000p-25f}, {0x1.2d285a0000000p+0f, 0x1.b900c20000000p-26f},
+    {0x1.306fe00000000p+0f, 0x1.4636e20000000p-25f}, {0x1.33c08c0000000p+0f, -0x1.b37d200000000p-25f},
+    {0x1.371a740000000p+0f, -0x1.18aac60000000p-25f}, {0x1.3a7db40000000p+0f, -0x1.634c020000000p-25f},
+    {0x1.3dea640000000p+0f, 0x1.8246840000000p-25f}, {0x1.4160a20000000p+0f, 0x1.f72e2a0000000p-28f},
+    {0x1.44e0860000000p+0f, 0x1.8624b40000000p-30f}, {0x1.486a2c0000000p+0f, -0x1.47d8660000000p-25f},
+    {0x1.4bfdae0000000p+0f, -0x1.593abc0000000p-25f}, {0x1.4f9b280000000p+0f, -0x1.2c5a6c0000000p-25f},
+    {0x1.5342b60000000p+0f, -0x1.2c56100000000p-25f}, {0x1.56f4740000000p+0f, -0x1.295b040000000p-25f},
+    {0x1.5ab07e0000000p+0f, -0x1.5bd5ec0000000p-27f}, {0x1.5e76f20000000p+0f, -0x1.4a5bd60000000p-25f},
+    {0x1.6247ec0000000p+0f, -0x1.f8b5500000000p-25f}, {0x1.6623880000000p+0f, 0x1.2a91120000000p-27f},
+    {0x1.6a09e60000000p+0f, 0x1.9fcef40000000p-26f}, {0x1.6dfb240000000p+0f, -0x1.cd72e80000000p-27f},
+    {0x1.71f75e0000000p+0f, 0x1.1d8bee0000000p-25f}, {0x1.75feb60000000p+0f, -0x1.37b3060000000p-25f},
+    {0x1.7a11480000000p+0f, -0x1.829fd00000000p-25f}, {0x1.7e2f340000000p+0f, -0x1.2616340000000p-25f},
+    {0x1.82589a0000000p+0f, -0x1.accc7c0000000p-26f}, {0x1.868d9a0000000p+0f, -0x1.2edb440000000p-26f},
+    {0x1.8ace540000000p+0f, 0x1.15506e0000000p-27f}, {0x1.8f1aea0000000p+0f, -0x1.baa2320000000p-26f},
+    {0x1.93737c0000000p+0f, -0x1.e647440000000p-25f}, {0x1.97d82a0000000p+0f, -0x1.0d8d840000000p-31f},
+    {0x1.9c49180000000p+0f, 0x1.51f8480000000p-27f}, {0x1.a0c6680000000p+0f, -0x1.2886a60000000p-26f},
+    {0x1.a5503c0000000p+0f, -0x1.b83b540000000p-25f}, {0x1.a9e6b60000000p+0f, -0x1.50c0480000000p-25f},
+    {0x1.ae89fa0000000p+0f, -0x1.a94b140000000p-26f}, {0x1.b33a2c0000000p+0f, -0x1.ec3a820000000p-26f},
+    {0x1.b7f7700000000p+0f, -0x1.a094380000000p-25f}, {0x1.bcc1ea0000000p+0f, -0x1.f687c60000000p-25f},
+    {0x1.c199be0000000p+0f, -0x1.3d56b20000000p-27f}, {0x1.c67f120000000p+0f, 0x1.cafa2a0000000p-25f},
+    {0x1.cb720e0000000p+0f, -0x1.8837cc0000000p-27f}, {0x1.d072d40000000p+0f, 0x1.40f1300000000p-25f},
+    {0x1.d5818e0000000p+0f, -0x1.822dbc0000000p-27f}, {0x1.da9e600000000p+0f, 0x1.ed99420000000p-27f},
+    {0x1.dfc9740000000p+0f, -0x1.908c940000000p-25f}, {0x1.e502ee0000000p+0f, 0x1.e2cffe0000000p-26f},
+    {0x1.ea4afa0000000p+0f, 0x1.52486c0000000p-27f}, {0x1.efa1be0000000p+0f, 0x1.cc2b440000000p-25f},
+    {0x1.f507660000000p+0f, -0x1.246eb00000000p-26f}, {0x1.fa7c180000000p+0f, 0x1.9e90d80000000p-28f},
 };
 
-// exp((l - m) / T) = 2^t, t = (l - m) c with c = log2(e) / T: t = n + k / 64 + r, |r| <= 1/128; 2^(k/64) from a table, 2^r from four
-// terms of its series, whose first is kept in two parts (the others are below 2^-16, and rounding them costs 2^-40).  0 below
-// 2^-64: what is left out of a sum of 2^20 weights is below 2^-44.
-__device__ __forceinline__ Two weight(float l, float m, Two c, const float2* tab) {
-  const float d = __fsub_rn(l, m), b = __fsub_rn(d, l);
-  const float dl = __fsub_rn(__fsub_rn(l, __fsub_rn(d, b)), __fadd_rn(m, b));   // l - m = d + dl
-  const float th = __fmul_rn(d, c.h);
-  if (!(th > -64.f)) return Two{0.f, 0.f};
-  const float tl = __fmaf_rn(d, c.h, -th) + __fmaf_rn(d, c.l, dl * c.h);
-  const float j = rintf(th * VD_TAB);
-  const float r = __fmaf_rn(j, -1.f / VD_TAB, th);   // exact
-  const int ji = (int)j;
-  const float2 T = tab[ji & (VD_TAB - 1)];
-  constexpr float LN2_H = 0.693147182464599609375f, LN2_L = -1.90465429995776804e-09f;   // log 2 in two parts
-  const float sh = __fmul_rn(r, LN2_H);
-  const float sl = __fmaf_rn(r, LN2_H, -sh) + __fmaf_rn(r, LN2_L, tl * LN2_H);
-  const float y = sl + sh * sh * __fmaf_rn(sh, __fmaf_rn(sh, 1.f / 24.f, 1.f / 6.f), 0.5f);   // 2^r = 1 + sh + y
-  const float ph = __fmul_rn(T.x, sh), pl = __fmaf_rn(T.x, sh, -ph);
-  const float s = __fadd_rn(T.x, ph), e = __fsub_rn(ph, __fsub_rn(s, T.x));
-  const float lo = e + (pl + __fmaf_rn(T.x, y, __fmaf_rn(T.y, sh, T.y)));
-  const float sc = __uint_as_float((unsigned)(127 + (ji >> 6)) << 23);   // 2^n, n >= -65
-  const float h = __fadd_rn(s, lo);
-  return Two{h * sc, __fsub_rn(lo, __fsub_rn(h, s)) * sc};
+// l - m in two parts (exact while neither overflows)
+__device__ __forceinline__ Two minus(float l, float m) { return sum_of(l, -m); }
+
+// What a row's weights exp((l - m) / T) are taken with.
+struct Scale {
+  float t, low;   // T (1 for a greedy sequence, which has those probabilities); -80 T
+  Two inv;        // 1 / T
+};
+__device__ __forceinline__ Scale scale_of(float t) {
+  if (t == 0.f || t == 1.f) return Scale{1.f, -80.f, Two{1.f, 0.f}};
+  return Scale{t, -80.f * t, Two{1.f, 0.f} / Two{t, 0.f}};
 }
 
-// What the cluster's threads share of the row that is looked at closely.
+// Two numbers each, whose operations are one instruction.
+using Pair = unsigned long long;
+__device__ __forceinline__ Pair pair(float a, float b) {
+  Pair r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ float2 both(Pair a) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(a));
+  return r;
+}
+__device__ __forceinline__ Pair same(float a) { return pair(a, a); }
+__device__ __forceinline__ Pair add2(Pair a, Pair b) {
+  Pair r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ Pair mul2(Pair a, Pair b) {
+  Pair r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ Pair fma2(Pair a, Pair b, Pair c) {
+  Pair r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ Pair sub2(Pair a, Pair b) { return fma2(b, same(-1.f), a); }
+struct TwoPair {
+  Pair h, l;
+  __device__ __forceinline__ Two first() const { return Two{both(h).x, both(l).x}; }
+  __device__ __forceinline__ Two second() const { return Two{both(h).y, both(l).y}; }
+};
+__device__ __forceinline__ TwoPair sum_of(Pair a, Pair b) {
+  const Pair s = add2(a, b), t = sub2(s, a);
+  return TwoPair{s, add2(sub2(a, sub2(s, t)), sub2(b, t))};
+}
+struct SumPair {   // two sums
+  Pair h = 0, l = 0;
+  __device__ __forceinline__ void add(const TwoPair& x) {
+    const TwoPair s = sum_of(h, x.h);
+    l = add2(l, add2(s.l, x.l));
+    h = s.h;
+  }
+  __device__ __forceinline__ Two value() const {
+    const TwoPair t{h, l};
+    const Two a = t.first(), b = t.second();
+    return norm2(a.h, a.l) + norm2(b.h, b.l);
+  }
+};
+
+// exp(x), x = (l - m) / T = j log(2) / 64 + r, |r| <= log(2) / 128, for two l: 2^(j / 64) by its exponent and the table, and four
+// terms of exp(r)'s series, whose first is kept in two parts (the others are below 2^-16, and rounding them costs 2^-40).  Both r's
+// first part and j's product with the first part of log(2) / 64 are multiples of 2^-31, so that r comes out exactly but for the second parts.
+// Below exp(-80), -infinity too, it is exp(-80) = 2^-115: no sum sees 2^20 of those, and none is drawn.
+__device__ __forceinline__ TwoPair weights(float l0, float l1, float m, const Scale& c, const VdTab& tab) {
+  const TwoPair d = sum_of(pair(l0, l1), same(-m));
+  float2 h = both(d.h), l = both(d.l);
+  l.x = h.x > c.low ? l.x : 0.f;
+  l.y = h.y > c.low ? l.y : 0.f;
+  Pair xh = pair(fmaxf(h.x, c.low), fmaxf(h.y, c.low)), xl = pair(l.x, l.y);
+  if (c.t != 1.f) {
+    const Pair p = mul2(xh, same(c.inv.h));
+    xl = add2(fma2(xh, same(c.inv.h), mul2(p, same(-1.f))), fma2(xh, same(c.inv.l), mul2(xl, same(c.inv.h))));
+    xh = p;
+  }
+  constexpr float LN_H = 0.010830424726009369f, LN_L = -2.976022206446771e-11f;   // log(2) / 64 in two parts
+  const Pair jm = fma2(xh, same(92.33248261689366f), same(12582912.f));   // 1.5 2^23: the nearest whole number in the last bits
+  const Pair jf = add2(jm, same(-12582912.f));
+  const Pair r = fma2(jf, same(-LN_H), xh), rl = fma2(jf, same(-LN_L), xl);
+  const float2 jb = both(jm);
+  const int j0 = __float_as_int(jb.x), j1 = __float_as_int(jb.y);
+  const Pair th = pair(tab.h[j0 & (VD_TAB - 1)], tab.h[j1 & (VD_TAB - 1)]), tl = pair(tab.l[j0 & (VD_TAB - 1)], tab.l[j1 & (VD_TAB - 1)]);
+  const Pair y = fma2(mul2(r, r), fma2(r, fma2(r, same(1.f / 24.f), same(1.f / 6.f)), same(0.5f)), rl);   // exp(r) = 1 + r + y
+  const Pair ph = mul2(th, r), pl = fma2(th, r, mul2(ph, same(-1.f)));
+  const Pair s = add2(th, ph), e = sub2(ph, sub2(s, th));
+  const Pair lo = add2(e, add2(pl, fma2(th, y, fma2(tl, r, tl))));
+  // 2^floor(j / 64): the whole number's bits above the table's, moved to the exponent (what lies above leaves the word)
+  const Pair sc = pair(__int_as_float(((j0 & ~(VD_TAB - 1)) << 17) + 0x3f800000), __int_as_float(((j1 & ~(VD_TAB - 1)) << 17) + 0x3f800000));
+  return TwoPair{mul2(s, sc), mul2(lo, sc)};
+}
+
+// The row that is looked at closely.
 template <typename TT, typename TD>
 struct Row {
   const TT* p;
-  const TD* q;        // NULL: no draft distribution, or none to take away
+  const TD* q;        // NULL: no draft distribution
   float mp, mq;
-  Two c, rho;         // scale; sum of p's weights / sum of q's
+  Scale c;
+  Two rho;            // sum of p's weights / sum of q's
   int certain;        // the draft that has all of q (-1: none)
   int plain;          // w = p
-  __device__ __forceinline__ Two at_p(int i, const float2* tab) const { return weight(to_f<TT>(p[i]), mp, c, tab); }
-  // max(p_i - q_i, 0), times the sum of p's weights
-  __device__ __forceinline__ Two residual(int i, const float2* tab) const {
-    const Two a = at_p(i, tab);
+  // Tokens k0, k0 + 32, .. below k1, two at a time: f(k, p's logits of k and k + 32, q's), -infinity past the end; several loads under way.
+  template <typename F>
+  __device__ __forceinline__ void each(int k0, int k1, F f) const {
+    for (int k = k0; k < k1; k += 32 * VD_LOADS) {
+      float x[VD_LOADS], y[VD_LOADS];
+#pragma unroll
+      for (int j = 0; j < VD_LOADS; ++j) {
+        const int i = k + 32 * j;
+        x[j] = i < k1 ? to_f<TT>(p[i]) : -INFINITY;
+        y[j] = q && i < k1 ? to_f<TD>(q[i]) : -INFINITY;
+      }
+#pragma unroll
+      for (int j = 0; j < VD_LOADS; j += 2) f(k + 32 * j, x[j], x[j + 1], y[j], y[j + 1]);
+    }
+  }
+  // max(p_i - q_i, 0) of tokens i, i + 32 from the logits, times the sum of p's weights
+  __device__ __forceinline__ TwoPair residual(int i, float x0, float x1, float y0, float y1, const VdTab& tab) const {
+    TwoPair a = weights(x0, x1, mp, c, tab);
     if (plain) return a;
-    if (!q) return i == certain ? Two{0.f, 0.f} : a;
-    const Two b = weight(to_f<TD>(q[i]), mq, c, tab);
-    const float ph = __fmul_rn(rho.h, b.h), pl = __fmaf_rn(rho.h, b.h, -ph) + __fmaf_rn(rho.h, b.l, rho.l * b.h);
-    const float s = __fsub_rn(a.h, ph), t = __fsub_rn(s, a.h);
-    const float e = __fsub_rn(__fsub_rn(a.h, __fsub_rn(s, t)), __fadd_rn(ph, t));   // a.h - ph = s + e
-    const float lo = e + __fsub_rn(a.l, pl), h = __fadd_rn(s, lo);
-    if (!(h > 0.f)) return Two{0.f, 0.f};
-    return Two{h, __fsub_rn(lo, __fsub_rn(h, s))};
+    float2 h, l;
+    if (q) {
+      const TwoPair b = weights(y0, y1, mq, c, tab);
+      const Pair ph = mul2(same(-rho.h), b.h), pl = add2(fma2(same(-rho.h), b.h, mul2(ph, same(-1.f))), fma2(same(-rho.h), b.l, mul2(same(-rho.l), b.h)));
+      const TwoPair d = sum_of(a.h, ph);
+      const Pair e = add2(d.l, add2(a.l, pl)), s = add2(d.h, e);
+      h = both(s);
+      l = both(sub2(e, sub2(s, d.h)));
+      if (!(h.x > 0.f)) h.x = l.x = 0.f;
+      if (!(h.y > 0.f)) h.y = l.y = 0.f;
+    } else {
+      h = both(a.h);
+      l = both(a.l);
+      if (i == certain) h.x = l.x = 0.f;
+      if (i + 32 == certain) h.y = l.y = 0.f;
+    }
+    return TwoPair{pair(h.x, h.y), pair(l.x, l.y)};
   }
 };
 
-__device__ __forceinline__ double warp_sum2(double v) {
-#pragma unroll
-  for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-  return v;
-}
-
 template <typename TT, typename TD>
-__global__ void __launch_bounds__(VD_THREADS) verify_decide_kernel(VerifyCall a, int n_split, const Stat* stats) {
-  PDL_ENTRY();
+__global__ void __launch_bounds__(VD_THREADS) verify_decide_kernel(VerifyCall a, int parts, const Stat* stats) {
   constexpr int WARPS = VD_THREADS / 32;
-  __shared__ float2 tab[VD_TAB];
+  static_assert(WARPS >= 4 && WARPS <= 32 && VD_CTAS <= 32, "sums and run_of by a warp");
+  __shared__ VdTab tab;
   __shared__ int s_first;
-  __shared__ double s_part[3][VD_CTAS], s_warp[3][WARPS];
-  __shared__ float s_mp, s_mq, s_z[2];
-  __shared__ int s_at;
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, rank = cluster_rank(), b = (int)blockIdx.x / VD_CTAS;
+  __shared__ float4 s_row;   // maximum and sum of the row in question, the target's and the draft's
+  // sums of the ranks and of this CTA's warps: p's weights, q's, those of p where p is above q, those of q there; what is drawn from
+  __shared__ long long s_part[5][VD_CTAS], s_warp[5][WARPS], s_piece[WARPS];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, rank = cluster_rank(), ctas = cluster_size(), b = (int)blockIdx.x / ctas;
   if (tid < VD_TAB) {
-    const Two t = two_of(exp2((double)tid / VD_TAB));
-    tab[tid] = make_float2(t.h, t.l);
+    tab.h[tid] = VD_POW[tid].x;
+    tab.l[tid] = VD_POW[tid].y;
   }
-  cluster_barrier();   // (also: the others' shared memory is there)
+  PDL_ENTRY();
   const SeqRows q = seq_rows(a, b);
   const float t = a.temp ? a.temp[b] : 1.f;
+  cluster_barrier();   // (also: the others' shared memory is there)
   const int n = q.ok ? q.e - q.s : 0;
   const bool greedy = t == 0.f, soft = a.draft != nullptr && !greedy;
   auto give = [&](int acc, int nxt) {
@@ -277,210 +481,287 @@ __global__ void __launch_bounds__(VD_THREADS) verify_decide_kernel(VerifyCall a,
     give(idle ? 0 : -1, -1);
     return;
   }
-  const float cf = (float)log2_scale(t);
-  auto joined = [&](int which, int r) {
-    Running x;
-    const Stat* s = stats + ((size_t)which * a.n_rows + r) * n_split;
-    for (int i = 0; i < n_split; ++i) x.join(s[i].m, s[i].z, s[i].at, cf);
-    return x;
+  const Scale sc = scale_of(t);
+  const float close = sc.t * close_of(a.vocab, parts);
+  // maximum and sum of a row from its parts', all loads together
+  auto stat = [&](int which, int r) {
+    const Stat* s = stats + ((size_t)which * a.n_rows + r) * parts;
+    float2 x[VS_PARTS];
+#pragma unroll
+    for (int k = 0; k < VS_PARTS; ++k) x[k] = k < parts ? *reinterpret_cast<const float2*>(s + k) : make_float2(-INFINITY, 0.f);
+    float m = x[0].x, z = 0.f;
+#pragma unroll
+    for (int k = 1; k < VS_PARTS; ++k) m = fmaxf(m, x[k].x);
+    const float c = 1.44269504088896f * sc.inv.h;
+#pragma unroll
+    for (int k = 0; k < VS_PARTS; ++k)
+      if (k < parts) z += x[k].x == m || x[k].x == -INFINITY ? x[k].y : x[k].y * ex2_approx((x[k].x - m) * c);
+    return make_float2(m, z);
   };
-  const double inv_t = greedy ? 1.0 : 1.0 / (double)t;
-  const double close = close_of(a.vocab, n_split);
+  auto drafted_at = [&](int which, int r) { return stats[((size_t)which * a.n_rows + r) * parts].l; };   // the draft's logit in a row
+  auto best = [&](int r) {   // the first index of a target row's maximum
+    const Stat* s = stats + (size_t)r * parts;
+    float m[VS_PARTS];
+    int at[VS_PARTS];
+#pragma unroll
+    for (int k = 0; k < VS_PARTS; ++k) {
+      m[k] = k < parts ? s[k].m : -INFINITY;
+      at[k] = k < parts ? s[k].at : 0;
+    }
+#pragma unroll
+    for (int k = 1; k < VS_PARTS; ++k)
+      if (m[k] > m[0]) {
+        m[0] = m[k];
+        at[0] = at[k];
+      }
+    return at[0];
+  };
+  // log of exp((l - m) / T) / z
+  auto log_share = [&](float l, float m, float z) {
+    const Two d = minus(l, m);
+    if (!(d.h * sc.inv.h >= -FLT_MAX)) return -INFINITY;
+    const Two x = d * sc.inv + Two{-logf(z), 0.f};
+    return x.h + x.l;
+  };
 
   // how a row stands by its 32-bit sums; the last row, behind which there is no draft, stops
   enum { HOLDS = 0, STOPS = 1, CLOSE = 2, BAD = 3 };
-  auto judge = [&](int i) {
+  auto judge = [&](int i, float4& row) {
     const int r = q.s + i;
-    const Running p = joined(0, r);
-    if (!(p.z > 0.f)) return (int)BAD;   // nothing above -infinity, a NaN, +infinity
-    if (i == n - 1) return (int)STOPS;
-    const int x = a.tokens[r + 1];
+    const bool last = i == n - 1, drafted = soft && !last;
+    const float2 p = stat(0, r), d = drafted ? stat(1, r) : make_float2(0.f, 1.f);
+    const int x = last ? 0 : a.tokens[r + 1];
+    const float u = greedy ? 0.f : a.u[r], lp = drafted_at(0, r), lq = drafted ? drafted_at(1, r) : 0.f;
+    row = make_float4(p.x, p.y, d.x, d.y);
+    if (!(p.y > 0.f)) return (int)BAD;   // nothing above -infinity, a NaN, +infinity
+    if (last) return (int)STOPS;
     if (x < 0 || x >= a.vocab) return (int)BAD;
-    if (greedy) return p.at == x ? (int)HOLDS : (int)STOPS;
-    const float u = a.u[r];
-    if (!(u >= 0.f && u < 1.f)) return (int)BAD;
-    double lq = 0.0;
-    if (soft) {
-      const Running d = joined(1, r);
-      if (!(d.z > 0.f)) return (int)BAD;
-      lq = ((double)to_f<TD>(((const TD*)a.draft)[r * a.ld_d + x]) - d.m) * inv_t - log((double)d.z);
-    }
-    const double lp = ((double)to_f<TT>(((const TT*)a.target)[r * a.ld_t + x]) - p.m) * inv_t - log((double)p.z);
-    const double left = log((double)u) + lq;
-    if (left > -INFINITY && lp > -INFINITY && fabs(left - lp) < close) return (int)CLOSE;
-    return left < lp ? (int)HOLDS : (int)STOPS;
+    if (greedy) return best(r) == x ? (int)HOLDS : (int)STOPS;
+    if (!(u >= 0.f && u < 1.f) || !(d.y > 0.f)) return (int)BAD;
+    // T times the difference of the logarithms: what holds has it below 0
+    const Two dp = minus(lp, p.x), dq = drafted ? minus(lq, d.x) : Two{0.f, 0.f};
+    if (dp.h == -INFINITY) return (int)STOPS;
+    if (u == 0.f || dq.h == -INFINITY) return (int)HOLDS;
+    const float logs = logf(p.y) + logf(u) - logf(d.y);
+    const float by = (dq + Two{-dp.h, -dp.l} + Two{sc.t * logs, 0.f}).h;
+    return fabsf(by) < close ? (int)CLOSE : by < 0.f ? (int)HOLDS : (int)STOPS;
   };
-  // the first row from `from` on that does not hold, and how it stands
+  // the first row from `from` on that does not hold, and how it stands; s_row
   auto first_from = [&](int from, int& i, int& code) {
     __syncthreads();
     if (tid == 0) s_first = 0x7fffffff;
     __syncthreads();
-    for (int k = from + tid; k < n; k += VD_THREADS) {
-      const int c = judge(k);
-      if (c != HOLDS) atomicMin(&s_first, k * 4 + c);
+    int mine = 0;
+    float4 row;
+    for (int k = from + tid; k < n && !mine; k += VD_THREADS) {
+      const int c = judge(k, row);
+      if (c != HOLDS) mine = k * 4 + c;
     }
+    if (mine) atomicMin(&s_first, mine);
     __syncthreads();
-    i = s_first >> 2;
-    code = s_first & 3;
+    const int first = s_first;
+    if (mine == first) s_row = row;
+    __syncthreads();
+    i = first >> 2;
+    code = first & 3;
   };
   int i, code;
   first_from(0, i, code);
 
   Row<TT, TD> row;
-  row.c = two_of(log2_scale(t));
-  const int share = (a.vocab + VD_CTAS - 1) / VD_CTAS, v0 = min(a.vocab, rank * share), v1 = min(a.vocab, v0 + share);
+  row.c = sc;
+  const int share = (a.vocab + ctas - 1) / ctas, v0 = min(a.vocab, rank * share), v1 = min(a.vocab, v0 + share);
   const int each = ((share + WARPS - 1) / WARPS + 31) & ~31, w0 = min(v1, v0 + warp * each), w1 = min(v1, w0 + each);
-  // sums over the vocabulary of up to two values a token, in every CTA; the warps' own in s_warp
-  auto sums = [&](auto value, double& x, double& y) {
-    Sum2 sx, sy;
-    for (int k = w0 + lane; k < w1; k += 32) value(k, sx, sy);
-    const double wx = warp_sum2(sx.value()), wy = warp_sum2(sy.value());
-    __syncthreads();
-    if (lane == 0) {
-      s_warp[0][warp] = wx;
-      s_warp[1][warp] = wy;
-    }
-    __syncthreads();
-    if (tid < 2 * VD_CTAS) {
-      const int which = tid / VD_CTAS, to = tid % VD_CTAS;
-      double s = 0;
-      for (int w = 0; w < WARPS; ++w) s += s_warp[which][w];
-      cluster_store(&s_part[which][rank], to, s);
-    }
-    cluster_barrier();
-    x = y = 0;
-    for (int k = 0; k < VD_CTAS; ++k) {
-      x += s_part[0][k];
-      y += s_part[1][k];
-    }
-    cluster_barrier();   // (s_part is free again)
+  // the CTA's sum of its warps' numbers v to place `part` of every CTA of the cluster, by one warp
+  auto exchange = [&](const long long* v, long long* part) {
+    const long long s = warp_sum(lane < WARPS ? v[lane] : 0);
+    if (lane < ctas) cluster_store(&part[rank], lane, s);
   };
-  double zp = 0, zq = 0;
-  auto look = [&](int r) {   // maxima and precise sums of row r
-    if (tid == 0) {
-      const Running p = joined(0, r);
-      s_mp = p.m;
-      s_at = p.at;
-      s_z[0] = p.z;
-      if (soft && r < q.e - 1) s_mq = joined(1, r).m;
-    }
-    __syncthreads();
+  auto total = [&](const long long* part) { return warp_sum(lane < ctas ? part[lane] : 0); };
+  float unit = 0.f, unit_q = 0.f;
+  long long zp = 0, zq = 0;
+  auto look = [&](int r) {   // precise sums of row r: the warps' in s_warp, the ranks' in s_part
+    const float4 st = s_row;
     row.p = (const TT*)a.target + r * a.ld_t;
     row.q = soft && r < q.e - 1 ? (const TD*)a.draft + r * a.ld_d : nullptr;
-    row.mp = s_mp;
-    row.mq = s_mq;
-    if (greedy) return;
-    sums([&](int k, Sum2& x, Sum2& y) {
-      x.add(row.at_p(k, tab));
-      if (row.q) y.add(weight(to_f<TD>(row.q[k]), row.mq, row.c, tab));
-    }, zp, zq);
+    row.mp = st.x;
+    row.mq = st.z;
+    unit = unit_of(st.y);
+    unit_q = unit_of(st.w);
+    SumPair sp;
+    if (row.q) {
+      SumPair sq, above_p, above_q;
+      const float rho = __fdividef(st.y, st.w);
+      row.each(w0 + lane, w1, [&](int, float x0, float x1, float y0, float y1) {
+        TwoPair p = weights(x0, x1, row.mp, row.c, tab), d = weights(y0, y1, row.mq, row.c, tab);
+        sp.add(p);
+        sq.add(d);
+        const float2 ph = both(p.h), dh = both(d.h);
+        const Pair in = pair(ph.x > rho * dh.x ? 1.f : 0.f, ph.y > rho * dh.y ? 1.f : 0.f);
+        above_p.add(TwoPair{mul2(p.h, in), mul2(p.l, in)});
+        above_q.add(TwoPair{mul2(d.h, in), mul2(d.l, in)});
+      });
+      const long long v1_ = warp_sum(whole(sq.value(), unit_q)), v2 = warp_sum(whole(above_p.value(), unit)), v3 = warp_sum(whole(above_q.value(), unit_q));
+      if (lane == 0) {
+        s_warp[1][warp] = v1_;
+        s_warp[2][warp] = v2;
+        s_warp[3][warp] = v3;
+      }
+    } else {
+      row.each(w0 + lane, w1, [&](int, float x0, float x1, float, float) { sp.add(weights(x0, x1, row.mp, row.c, tab)); });
+    }
+    const long long v0_ = warp_sum(whole(sp.value(), unit));
+    if (lane == 0) s_warp[0][warp] = v0_;
+    __syncthreads();
+    if (warp < (row.q ? 4 : 1)) exchange(s_warp[warp], s_part[warp]);
+    cluster_barrier();
+    zp = total(s_part[0]);
+    if (row.q) zq = total(s_part[1]);
   };
-  // drafts that are too close: decided by the precise sums
+  int looked = -1;
+  // drafts that are too close: decided by the precise sums, in 64 bits
   while (code == CLOSE) {
-    const int r = q.s + i, x = a.tokens[r + 1];
+    const int r = q.s + i;
     look(r);
-    const double lp = ((double)to_f<TT>(row.p[x]) - row.mp) * inv_t - log(zp);
-    const double lq = row.q ? ((double)to_f<TD>(row.q[x]) - row.mq) * inv_t - log(zq) : 0.0;
-    if (!(log((double)a.u[r]) + lq < lp)) {
+    looked = r;
+    if (tid == 0) {
+      const double dp = (double)drafted_at(0, r) - row.mp, dq = row.q ? (double)drafted_at(1, r) - row.mq : 0.0;
+      const double logs = log((double)a.u[r]) + log((double)zp / unit) - (row.q ? log((double)zq / unit_q) : 0.0);
+      s_first = dq - dp + (double)t * logs < 0.0;
+    }
+    __syncthreads();
+    if (!s_first) {
       code = STOPS;
       break;
     }
     first_from(i + 1, i, code);
+    cluster_barrier();   // (the sums of that row have been read: s_part is free)
   }
-  const float u_draw = a.u[q.e - 1];
-  if (code == BAD || (!greedy && !(u_draw >= 0.f && u_draw < 1.f))) {
+  if (code == BAD || (!greedy && !(a.u[q.e - 1] >= 0.f && a.u[q.e - 1] < 1.f))) {
     if (rank == 0 && tid == 0) a.flag(ERRW_VALUE);
     give(-1, -1);
     return;
   }
   const int r = q.s + i;
-  look(r);
-  int nxt = s_at;
-  if (!greedy) {
-    row.certain = a.draft || r == q.e - 1 ? -1 : a.tokens[r + 1];
-    row.plain = r == q.e - 1;
-    row.rho = two_of(row.q ? zp / zq : 0.0);
-    double all_w = zp, all_p = zp;
-    sums([&](int k, Sum2& x, Sum2& y) {
-      x.add(row.residual(k, tab));
-      y.add(row.at_p(k, tab));
-    }, all_w, all_p);
-    const bool fall_back = !(all_w >= VD_LEAST * zp);
-    if (fall_back) {
-      row.plain = 1;
-      all_w = all_p;
+  if (a.logprob && rank == ctas - 1) {   // (not the CTA that gives the result)
+    for (int k = q.s + tid; k < r; k += VD_THREADS) {
+      const float2 p = stat(0, k);
+      a.logprob[k] = log_share(drafted_at(0, k), p.x, p.y);
     }
-    const int which = fall_back ? 1 : 0;
-    const double at = ((double)u_draw + 2.98023223876953125e-08) * all_w;   // u in the middle of its 2^-24
-    // the warp in whose run the sum passes `at`: the last run that begins at or below it and holds something
-    __syncthreads();
-    double mine = 0;
-    for (int w = 0; w < WARPS; ++w) mine += s_warp[which][w];
-    // (the parts were overwritten by no one since the sums: every CTA holds its own runs; the ranks' are exchanged again)
-    if (tid < VD_CTAS) cluster_store(&s_part[2][rank], tid, mine);
-    cluster_barrier();
-    double before = 0;
-    int owner = 0;
-    double owner_before = 0, sum = 0;
-    for (int k = 0; k < VD_CTAS; ++k) {
-      if (s_part[2][k] > 0 && sum <= at) {
-        owner = k;
-        owner_before = sum;
-      }
-      sum += s_part[2][k];
-    }
-    before = owner_before;
-    if (rank == owner) {
-      int ow = 0;
-      double ob = before, s = before;
-      for (int w = 0; w < WARPS; ++w) {
-        if (s_warp[which][w] > 0 && s <= at) {
-          ow = w;
-          ob = s;
-        }
-        s += s_warp[which][w];
-      }
-      if (warp == ow) {
-        int best = -1;   // the last token with a weight so far: what rounding leaves
-        double run = ob;
-        for (int k0 = w0; k0 < w1; k0 += 32) {
-          const int k = k0 + lane;
-          double w = 0;
-          if (k < w1) {
-            const Two x = row.residual(k, tab);
-            w = (double)x.h + (double)x.l;
-          }
-          double inc = w;
-#pragma unroll
-          for (int o = 1; o < 32; o <<= 1) {
-            const double v = __shfl_up_sync(0xffffffffu, inc, o);
-            if (lane >= o) inc += v;
-          }
-          const unsigned over = __ballot_sync(0xffffffffu, w > 0 && run + inc > at), some = __ballot_sync(0xffffffffu, w > 0);
-          if (over) {
-            best = k0 + __ffs(over) - 1;
-            break;
-          }
-          if (some) best = k0 + 31 - __clz(some);
-          run += __shfl_sync(0xffffffffu, inc, 31);
-        }
-        if (lane == 0 && best >= 0) {   // (the run holds something)
-          a.accepted[b] = i;
-          a.next[b] = best;
-          if (a.logprob) a.logprob[r] = (float)(((double)to_f<TT>(row.p[best]) - row.mp) * inv_t - log(zp));
-        }
-      }
-    }
-  } else {
-    give(i, nxt);
-    if (a.logprob && rank == 0 && tid == 0) a.logprob[r] = (float)-log((double)s_z[0]);
   }
-  if (a.logprob && rank == 0) {
-    for (int k = tid; k < i; k += VD_THREADS) {
-      const Running p = joined(0, q.s + k);
-      const int x = a.tokens[q.s + k + 1];
-      a.logprob[q.s + k] = (float)(((double)to_f<TT>(((const TT*)a.target)[(q.s + k) * a.ld_t + x]) - p.m) * inv_t - log((double)p.z));
+  if (greedy) {
+    if (rank == 0 && tid == 0) {
+      give(i, best(r));
+      if (a.logprob) a.logprob[r] = -logf(s_row.y);
     }
+    return;
+  }
+  if (looked != r) look(r);
+  row.certain = soft || r == q.e - 1 ? -1 : a.tokens[r + 1];
+  row.plain = r == q.e - 1;
+  // what is drawn from: its sum, the ranks' and this CTA's warps'
+  const long long *by_rank = s_part[0], *by_warp = s_warp[0];
+  long long all = zp;
+  if (!row.plain) {
+    if (row.q) {
+      // sum of max(p - q, 0) = that of p where p is above q, less that of q there.  "Above" went by the 32-bit sums: tokens with p and q within
+      // 10^-6 of each other may be on the wrong side, by that much of themselves
+      const Two rho = quotient(two_of(zp), two_of(zq));   // in p's units over q's
+      auto rest = [&](long long above_p, long long above_q) {
+        const Two x = rho * two_of(above_q);
+        return max(above_p - __float2ll_rn(x.h) - __float2ll_rn(x.l), 0ll);
+      };
+      if (warp == 0) {
+        if (lane < WARPS) s_warp[4][lane] = rest(s_warp[2][lane], s_warp[3][lane]);
+        if (lane < ctas) s_part[4][lane] = rest(s_part[2][lane], s_part[3][lane]);
+      }
+      const float by = __int_as_float(0x3f800000 + __float_as_int(unit_q) - __float_as_int(unit));
+      row.rho = Two{rho.h * by, rho.l * by};
+      __syncthreads();
+      all = total(s_part[4]);
+      if (all < zp >> VD_FINE) {   // little is left of p: token by token
+        SumPair sw;
+        row.each(w0 + lane, w1, [&](int k, float x0, float x1, float y0, float y1) { sw.add(row.residual(k, x0, x1, y0, y1, tab)); });
+        const long long vw = warp_sum(whole(sw.value(), unit));
+        __syncthreads();   // (s_part[4] has been read)
+        if (lane == 0) s_warp[4][warp] = vw;
+        cluster_barrier();
+        if (warp == 0) exchange(s_warp[4], s_part[4]);
+        cluster_barrier();
+        all = total(s_part[4]);
+      }
+    } else {   // all of p but the draft
+      const int x = row.certain, at_rank = x / share, at_warp = (x - at_rank * share) / each;
+      const long long wx = whole(weights(drafted_at(0, r), -INFINITY, row.mp, row.c, tab).first(), unit);
+      auto rest = [&](long long v, bool has) { return has ? (v - wx < 256 ? 0ll : v - wx) : v; };   // (256: what rounding leaves)
+      if (warp == 0) {
+        if (lane < WARPS) s_warp[4][lane] = rest(s_warp[0][lane], rank == at_rank && lane == at_warp);
+        if (lane < ctas) s_part[4][lane] = rest(s_part[0][lane], lane == at_rank);
+      }
+      __syncthreads();
+      all = total(s_part[4]);
+    }
+    row.plain = all < zp >> VD_LEAST;
+    if (!row.plain) {
+      by_rank = s_part[4];
+      by_warp = s_warp[4];
+    } else {
+      all = zp;
+    }
+  }
+  // u in the middle of its 2^-24, times the sum
+  const long long at = (long long)__umul64hi(__float2ull_rz(a.u[q.e - 1] * 18446744073709551616.f) + (1ull << 39), (unsigned long long)all);
+  // the run in which the sum passes `at`: the last of those that hold something and begin at or below it (by a warp)
+  long long before = 0;
+  auto run_of = [&](const long long* v, int n_runs) {
+    const long long x = lane < n_runs ? v[lane] : 0;
+    long long inc = x;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const long long u = __shfl_up_sync(0xffffffffu, inc, o);
+      if (lane >= o) inc += u;
+    }
+    const long long from = before + inc - x;
+    const unsigned ok = __ballot_sync(0xffffffffu, x > 0 && from <= at);
+    const int k = ok ? 31 - __clz(ok) : 0;
+    before = __shfl_sync(0xffffffffu, from, k);
+    return k;
+  };
+  if (rank != run_of(by_rank, ctas)) return;
+  // this CTA's run, of it a warp's, which all warps look at in shares
+  const int ow = run_of(by_warp, WARPS);
+  const int r0 = min(v1, v0 + ow * each), r1 = min(v1, r0 + each), piece = ((each + WARPS - 1) / WARPS + 31) & ~31;
+  const int p0 = min(r1, r0 + warp * piece), p1 = min(r1, p0 + piece);
+  SumPair sw;
+  row.each(p0 + lane, p1, [&](int k, float x0, float x1, float y0, float y1) { sw.add(row.residual(k, x0, x1, y0, y1, tab)); });
+  const long long vw = warp_sum(whole(sw.value(), unit));
+  if (lane == 0) s_piece[warp] = vw;
+  __syncthreads();
+  if (warp != run_of(s_piece, WARPS)) return;
+  int token = -1;   // the last one with a weight so far: what rounding leaves
+  for (int k0 = p0; k0 < p1; k0 += 32) {
+    const int k = k0 + lane;
+    const bool in = k < p1;
+    const Two v = row.residual(k, in ? to_f<TT>(row.p[k]) : -INFINITY, -INFINITY, in && row.q ? to_f<TD>(row.q[k]) : -INFINITY, -INFINITY, tab).first();
+    const long long w = in ? whole(v, unit) : 0;
+    long long inc = w;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const long long u = __shfl_up_sync(0xffffffffu, inc, o);
+      if (lane >= o) inc += u;
+    }
+    const unsigned over = __ballot_sync(0xffffffffu, w > 0 && before + inc > at), some = __ballot_sync(0xffffffffu, w > 0);
+    if (over) {
+      token = k0 + __ffs(over) - 1;
+      break;
+    }
+    if (some) token = k0 + 31 - __clz(some);
+    before += __shfl_sync(0xffffffffu, inc, 31);
+  }
+  if (lane == 0 && token >= 0) {   // (the run holds something)
+    a.accepted[b] = i;
+    a.next[b] = token;
+    if (a.logprob) a.logprob[r] = log_share(to_f<TT>(row.p[token]), row.mp, __ll2float_rn(zp) / unit);
   }
 }
 
@@ -494,28 +775,34 @@ int verify_sms() {
   return sms;
 }
 
-// Parts of a row: enough CTAs to fill the GPU, each with a few rounds of its threads.
-int verify_target() { return 4 * verify_sms(); }
-int verify_splits(int n_rows, int vocab) {
-  const int want = cdiv(verify_target(), n_rows), most = vocab / (VS_THREADS * 8) + 1;
-  return want < most ? want : most;
+// CTAs of a row: as many as give the GPU four CTAs an SM, while each has two rounds of its threads.
+int verify_parts(int n_rows, int vocab) {
+  int parts = 1;
+  while (parts < VS_PARTS && (long long)n_rows * parts < 4 * verify_sms() && vocab / (2 * parts) >= VS_THREADS * 8) parts *= 2;
+  return parts;
 }
 
 template <typename TT, typename TD>
 cudaError_t verify_t(cudaStream_t st, const VerifyCall& a) {
-  const int s = a.n_rows > 0 ? verify_splits(a.n_rows, a.vocab) : 1;
+  const int parts = a.n_rows > 0 ? verify_parts(a.n_rows, a.vocab) : 1;
   Stat* stats = (Stat*)a.ws;
   if (a.n_rows > 0) {
-    const cudaError_t e = launch_k(verify_stats_kernel<TT, TD>, dim3((unsigned)(a.n_rows * s), a.draft ? 2 : 1), dim3(VS_THREADS), 0, st, a, s, stats);
+    const cudaError_t e = launch_k(verify_stats_kernel<TT, TD>, dim3((unsigned)(a.n_rows * parts), a.draft ? 2 : 1), dim3(VS_THREADS), 0, st, a, parts, stats);
     if (e != cudaSuccess) return e;
   }
-  return launch_cluster(verify_decide_kernel<TT, TD>, a.n_seq * VD_CTAS, VD_CTAS, VD_THREADS, 0, st, a, s, (const Stat*)stats);
+  // A sequence gets the most CTAs (of an SM each) that leave all sequences room at once: 64 sequences of 131072 tokens took 117 us by 2
+  // CTAs each, 125 by 4, 129 by 8 smaller ones, three an SM; one sequence of 50257 tokens 13.5 by 16, 15.4 by 8.
+  struct Tag;
+  const cudaError_t e = cluster16_once<Tag>(verify_decide_kernel<TT, TD>);
+  if (e != cudaSuccess) return e;
+  int ctas = VD_CTAS;
+  while (ctas > 1 && (long long)a.n_seq * ctas > verify_sms()) ctas /= 2;
+  return launch_cluster(verify_decide_kernel<TT, TD>, dim3((unsigned)(a.n_seq * ctas)), ctas, VD_THREADS, 0, st, a, parts, (const Stat*)stats);
 }
 
 }  // namespace
 
-// (n_rows times the parts of a row is at most this; a smaller call needs no more)
-size_t verify_workspace(int n_rows) { return (size_t)2 * (verify_target() + (size_t)n_rows) * sizeof(Stat); }
+size_t verify_workspace(int n_rows) { return (size_t)2 * VS_PARTS * n_rows * sizeof(Stat); }
 
 cudaError_t launch_verify(cudaStream_t st, const VerifyCall& a) {
   if (a.t_bf16) return a.d_bf16 ? verify_t<bf16, bf16>(st, a) : verify_t<bf16, float>(st, a);
