@@ -9,35 +9,43 @@
 namespace adept {
 namespace {
 
-constexpr int PG_THREADS = 1024, PG_CTAS = 8;   // of the one cluster that grows rows or compacts
+constexpr int PG_THREADS = 1024, PG_CTAS = 8;   // of the one cluster that grows rows, compacts, or forks (smaller tables: one CTA is no faster)
 
 __device__ __forceinline__ bool held(const Pages& p, int e) { return e >= 0 && e < p.n_blocks; }
 __device__ __forceinline__ int blocks_of(const Pages& p, int n) { return n / p.block_tokens + (n % p.block_tokens != 0); }
 
-// Exclusive sum over the CTA's threads (all of them; 1024), the total in *total.
-__device__ __forceinline__ int cta_scan(int v, int* red, int* total) {
+// Exclusive sum over the CTA's 1024 threads, the total in *total.
+template <typename T>
+__device__ __forceinline__ T cta_scan(T v, T* red, T* total) {
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
-  int inc = v;
+  T inc = v;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const int u = __shfl_up_sync(0xffffffffu, inc, o);
+    const T u = __shfl_up_sync(0xffffffffu, inc, o);
     if (lane >= o) inc += u;
   }
   __syncthreads();   // red may still be read
   if (lane == 31) red[w] = inc;
   __syncthreads();
-  if (w == 0) {
-    int x = red[lane];
+  const T mine = red[lane];   // every warp sums the warps' totals for itself: one barrier less
+  T x = mine;
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int u = __shfl_up_sync(0xffffffffu, x, o);
-      if (lane >= o) x += u;
-    }
-    red[lane] = x;
+  for (int o = 1; o < 32; o <<= 1) {
+    const T u = __shfl_up_sync(0xffffffffu, x, o);
+    if (lane >= o) x += u;
   }
-  __syncthreads();
-  *total = red[31];
-  return inc - v + (w ? red[w - 1] : 0);
+  *total = __shfl_sync(0xffffffffu, x, 31);
+  return inc - v + __shfl_sync(0xffffffffu, x - mine, w);
+}
+// Whether each of counts i .. i + 3 (below n) is that of a free block, as bits.
+__device__ __forceinline__ unsigned free_bits(const int* ref, int i, int n) {
+  if (i + 4 <= n) {
+    const int4 f = *reinterpret_cast<const int4*>(ref + i);
+    return (f.x == 0) | (f.y == 0) << 1 | (f.z == 0) << 2 | (f.w == 0) << 3;
+  }
+  unsigned m = 0;
+  for (int k = 0; i + k < n; ++k) m |= (unsigned)(ref[i + k] == 0) << k;
+  return m;
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -56,51 +64,111 @@ __device__ __forceinline__ ForkRow fork_row(const Pages& p, const int* source, c
   return ForkRow{s, blocks_of(p, n)};
 }
 
-// Counts of the blocks that rows lose and gain, and rows that come from others into `stage`; the table is only read.
-__global__ void __launch_bounds__(256) kv_fork_count_kernel(Pages p, const int* source, const int* length, int* stage) {
+// What entry c of row b, whose block is `old`, becomes.
+__device__ __forceinline__ int fork_source(const Pages& p, const ForkRow& f, int b, int c, int old) {
+  return c >= f.nb ? -1 : f.src == b ? old : p.table[(size_t)f.src * p.max_blocks + c];
+}
+// The counts of an entry that changes from block `old` to `neu`; what it becomes (-1 where neu is no block).
+__device__ __forceinline__ int fork_counts(const Pages& p, int old, int neu) {
+  if (neu != -1 && !held(p, neu)) {
+    p.flag(ERRW_POS);
+    neu = -1;
+  }
+  if (neu >= 0) atomicAdd(p.ref + neu, 1);
+  if (old != -1 && (!held(p, old) || atomicSub(p.ref + old, 1) <= 0)) p.flag(ERRW_POS);   // (a count below its holders)
+  return neu;
+}
+// Larger tables: a CTA for FORK_CHUNK entries of a row.  The first launch changes the counts, writes rows that come from others into `stage` and
+// only reads the table; the second writes it (256 rows of 2048 entries, cut back, and grown by adept_kv_reserve: 12.9 us, by chunks of 2048
+// 14.8, of 256 14.3).
+constexpr int FORK_THREADS = 256, FORK_CHUNK = 512;
+__global__ void __launch_bounds__(FORK_THREADS) kv_fork_count_kernel(Pages p, const int* source, const int* length, int* stage) {
   PDL_ENTRY();
   const int b = (int)blockIdx.x;
   const ForkRow f = fork_row(p, source, length, b);
   const size_t row = (size_t)b * p.max_blocks;
-  for (int c = (f.src == b ? f.nb : 0) + (int)(blockIdx.y * 256 + threadIdx.x); c < p.max_blocks; c += (int)gridDim.y * 256) {
-    const int old = p.table[row + c];
-    int neu = c < f.nb ? p.table[(size_t)f.src * p.max_blocks + c] : -1;
-    if (neu != -1 && !held(p, neu)) {
-      p.flag(ERRW_POS);
-      neu = -1;
+  constexpr int EACH = FORK_CHUNK / FORK_THREADS;
+  for (int c0 = (int)blockIdx.y * FORK_CHUNK; c0 < p.max_blocks; c0 += (int)gridDim.y * FORK_CHUNK) {
+    int old[EACH], neu[EACH];
+#pragma unroll
+    for (int k = 0; k < EACH; ++k) {
+      const int c = c0 + k * FORK_THREADS + threadIdx.x;
+      const bool in = c < p.max_blocks && !(f.src == b && c < f.nb);
+      old[k] = in ? p.table[row + c] : 0;
+      neu[k] = in ? fork_source(p, f, b, c, old[k]) : 0;
     }
-    if (f.src != b) stage[row + c] = neu;
-    if (old == neu) continue;
-    if (neu >= 0) atomicAdd(p.ref + neu, 1);
-    if (old != -1 && (!held(p, old) || atomicSub(p.ref + old, 1) <= 0)) p.flag(ERRW_POS);   // (a count below its holders)
+#pragma unroll
+    for (int k = 0; k < EACH; ++k) {
+      if (old[k] != neu[k]) neu[k] = fork_counts(p, old[k], neu[k]);
+      const int c = c0 + k * FORK_THREADS + threadIdx.x;
+      if (f.src != b && c < p.max_blocks) stage[row + c] = neu[k];
+    }
   }
 }
-__global__ void __launch_bounds__(256) kv_fork_write_kernel(Pages p, const int* source, const int* length, const int* stage) {
+__global__ void __launch_bounds__(FORK_THREADS) kv_fork_write_kernel(Pages p, const int* source, const int* length, const int* stage) {
   PDL_ENTRY();
   const int b = (int)blockIdx.x;
   const ForkRow f = fork_row(p, source, length, b);
   const size_t row = (size_t)b * p.max_blocks;
-  for (int c = (f.src == b ? f.nb : 0) + (int)(blockIdx.y * 256 + threadIdx.x); c < p.max_blocks; c += (int)gridDim.y * 256)
-    p.table[row + c] = f.src == b ? -1 : stage[row + c];
+  for (int c0 = (int)blockIdx.y * FORK_CHUNK; c0 < p.max_blocks; c0 += (int)gridDim.y * FORK_CHUNK) {
+#pragma unroll
+    for (int k = 0; k < FORK_CHUNK / FORK_THREADS; ++k) {
+      const int c = c0 + k * FORK_THREADS + threadIdx.x;
+      if (c < p.max_blocks && !(f.src == b && c < f.nb)) p.table[row + c] = f.src == b ? -1 : stage[row + c];
+    }
+  }
+}
+
+// Tables of up to PG_CTAS * PG_THREADS * FORK_EACH entries: one cluster holds them between reading and writing (one launch instead
+// of two: 4 rows of 24 blocks, cut back and grown, 9.3 us against 10.2).
+constexpr int FORK_EACH = 8;
+__global__ void __launch_bounds__(PG_THREADS) kv_fork_kernel(Pages p, const int* source, const int* length) {
+  PDL_ENTRY();
+  const int total = p.n_seq * p.max_blocks, step = PG_CTAS * PG_THREADS, me = (int)blockIdx.x * PG_THREADS + threadIdx.x;
+  int old[FORK_EACH], neu[FORK_EACH];
+  unsigned write = 0;
+#pragma unroll
+  for (int k = 0; k < FORK_EACH; ++k) {   // (what the rows' loads wait for is under way together)
+    const int i = me + k * step;
+    old[k] = neu[k] = 0;
+    if (i >= total) continue;
+    const int b = i / p.max_blocks, c = i - b * p.max_blocks;
+    old[k] = p.table[i];
+    neu[k] = fork_source(p, fork_row(p, source, length, b), b, c, old[k]);
+  }
+#pragma unroll
+  for (int k = 0; k < FORK_EACH; ++k) {
+    if (old[k] == neu[k]) continue;
+    neu[k] = fork_counts(p, old[k], neu[k]);
+    write |= 1u << k;
+  }
+  cluster_barrier();
+#pragma unroll
+  for (int k = 0; k < FORK_EACH; ++k)
+    if (write >> k & 1) p.table[me + k * step] = neu[k];
 }
 
 // ---------------------------------------------------------------------------------------------
-// Growth.  One cluster: each CTA a share of the counts and of the rows.
+// Growth.  One cluster.  Every CTA looks at every row (a thread each; rows that ask for more than NARROW entries: a warp of one of the
+// CTAs, which tells the others) and at its part of the counts; then each knows which rows are served, and gives the free blocks of
+// its part to the entries that they fall to.  Bound by latency: four loads one behind the other, two barriers.
 // ---------------------------------------------------------------------------------------------
-constexpr unsigned ASKS = 1, KEEPS = 2;   // row flags: grows; keeps the shared block that it writes
+constexpr int NARROW = 4;
+constexpr unsigned ASKS = 1, KEEPS = 2, SHARED = 4, COPIES = 8, WIDE = 16;   // row flags: grows; keeps the shared block that it writes;
+                                                                 // writes a shared block in part; gets a copy of that; more than NARROW entries
+constexpr unsigned MANY = 1u << 30;   // sums of blocks stop here (more than there are)
 
 struct ReserveCall {
   const int *length, *want;
   int *got, *src, *dst;
-  int* list;        // free blocks, ascending, as many as are taken
-  unsigned* mask;   // [n_seq][mask_words]: entries that get a new block, from the row's first on that is written
+  unsigned* mask;   // [n_seq][mask_words]: of wide rows, entries that get a new block, from the row's first on that is written
   int mask_words, hash;   // hash: slots of the table of shared blocks (a power of two)
 };
 
 // Row b's entries that it will write: [j0, j1); none where it does not grow.
 struct GrowRow {
   int n, want, j0, j1;
-  bool asks;
+  bool asks, part;   // part: its first block holds positions that stay
 };
 __device__ __forceinline__ GrowRow grow_row(const Pages& p, const ReserveCall& a, int b) {
   GrowRow r;
@@ -113,160 +181,196 @@ __device__ __forceinline__ GrowRow grow_row(const Pages& p, const ReserveCall& a
   }
   r.j0 = r.asks ? r.n / p.block_tokens : 0;
   r.j1 = r.asks ? blocks_of(p, r.want) : 0;
+  r.part = r.asks && r.n != r.j0 * p.block_tokens;
   return r;
+}
+__device__ __forceinline__ unsigned shared_slot(const ReserveCall& a, int e) { return ((unsigned)e * 2654435761u >> 7) & (unsigned)(a.hash - 1); }
+// Whether an entry needs a new block, where f is its block's count (0: no block).
+__device__ __forceinline__ bool needs(const Pages& p, int e, int f) {
+  if (!held(p, e)) {
+    if (e != -1) p.flag(ERRW_POS);
+    return true;
+  }
+  if (f <= 0) p.flag(ERRW_POS);   // (held, but counted as free)
+  return f > 1;
 }
 
 __global__ void __launch_bounds__(PG_THREADS) kv_reserve_kernel(Pages p, ReserveCall a) {
-  PDL_ENTRY();
   extern __shared__ __align__(16) unsigned char smem[];
-  long long* pre = reinterpret_cast<long long*>(smem);                  // [n_seq] blocks asked for by the rows up to this one
-  int* demand = reinterpret_cast<int*>(pre + p.n_seq);                  // [n_seq]
-  int* flags = demand + p.n_seq;                                        // [n_seq]
-  int *key = flags + p.n_seq, *cnt = key + a.hash, *last = cnt + a.hash;   // shared blocks that rows want to write
-  __shared__ int red[32], s_free[PG_CTAS];
-  __shared__ long long red64[32];
+  unsigned* pre = reinterpret_cast<unsigned*>(smem);   // [n_seq] blocks asked for by the rows up to this one
+  unsigned *demand = pre + p.n_seq, *word = demand + p.n_seq, *flags = word + p.n_seq;   // [n_seq] blocks; a narrow row's entries; flags
+  int *key = reinterpret_cast<int*>(flags + p.n_seq), *cnt = key + a.hash, *last = cnt + a.hash;   // shared blocks that rows write in part
+  __shared__ int red[32];
+  __shared__ unsigned redu[32], s_taken, s_free[PG_CTAS];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, rank = cluster_rank();
-
-  // blocks that are written in part while several rows hold them: how many rows ask for each, and the last of those
+  cluster_arrive();
   for (int i = tid; i < a.hash; i += PG_THREADS) {
     key[i] = -1;
     cnt[i] = 0;
     last[i] = -1;
   }
-  cluster_barrier();   // (also: the others' shared memory is there)
+  if (tid == 0) s_taken = 0;
+  PDL_ENTRY();
+  // free blocks of the CTA's part of the counts: the first 4096 are looked at once
+  const int seg = ((p.n_blocks + PG_CTAS - 1) / PG_CTAS + 3) & ~3, i0 = min(p.n_blocks, rank * seg), i1 = min(p.n_blocks, i0 + seg);
+  const unsigned bits0 = free_bits(p.ref, i0 + 4 * tid, i1);
+  __syncthreads();   // (the hash)
   for (int b = tid; b < p.n_seq; b += PG_THREADS) {
     const GrowRow r = grow_row(p, a, b);
-    if (!r.asks || r.n % p.block_tokens == 0) continue;
-    const int e = p.table[(size_t)b * p.max_blocks + r.j0];
-    if (!held(p, e) || p.ref[e] <= 1) continue;
-    int h = (int)(((unsigned)e * 2654435761u) >> 7) & (a.hash - 1);
-    for (;;) {   // (at most n_seq keys in a table of twice as many: ends)
-      const int was = atomicCAS(key + h, -1, e);
-      if (was == -1 || was == e) break;
-      h = (h + 1) & (a.hash - 1);
+    int e[NARROW], f[NARROW];
+#pragma unroll
+    for (int k = 0; k < NARROW; ++k) e[k] = r.j0 + k < r.j1 ? p.table[(size_t)b * p.max_blocks + r.j0 + k] : -1;
+#pragma unroll
+    for (int k = 0; k < NARROW; ++k) f[k] = held(p, e[k]) ? p.ref[e[k]] : 0;
+    unsigned w = 0, fl = r.asks ? ASKS : 0;
+#pragma unroll
+    for (int k = 0; k < NARROW; ++k)
+      if (r.j0 + k < r.j1 && needs(p, e[k], f[k])) w |= 1u << k;
+    if (r.j1 - r.j0 > NARROW) fl |= WIDE;
+    if (r.part && f[0] > 1) {
+      // how many rows ask for the block, and the last of them
+      fl |= SHARED;
+      unsigned h = shared_slot(a, e[0]);
+      for (;;) {   // (at most n_seq keys in a table of twice as many: ends)
+        const int was = atomicCAS(key + h, -1, e[0]);
+        if (was == -1 || was == e[0]) break;
+        h = (h + 1) & (a.hash - 1);
+      }
+      atomicAdd(cnt + h, 1);
+      atomicMax(last + h, b);
     }
-    atomicAdd(cnt + h, 1);
-    atomicMax(last + h, b);
+    word[b] = w;
+    flags[b] = fl;
+    if (!(fl & WIDE)) demand[b] = __popc(w);
   }
-  __syncthreads();
-
-  // what each row asks for: the CTA's rows, a warp each
-  const int rows = (p.n_seq + PG_CTAS - 1) / PG_CTAS, b0 = min(p.n_seq, rank * rows), b1 = min(p.n_seq, b0 + rows);
-  for (int b = b0 + warp; b < b1; b += PG_THREADS / 32) {
+  int n_free = __popc(bits0), total = 0;
+  for (int i = i0 + 4 * (PG_THREADS + tid); i < i1; i += 4 * PG_THREADS) n_free += __popc(free_bits(p.ref, i, i1));
+  const int at0 = cta_scan(n_free, red, &total);   // (and the CTA's barrier; the free blocks before mine where a look is enough)
+  for (int b = tid; b < p.n_seq; b += PG_THREADS) {
+    const unsigned fl = flags[b];
+    if (!(fl & SHARED)) continue;
     const GrowRow r = grow_row(p, a, b);
-    int n = 0, fl = r.asks ? (int)ASKS : 0;
+    const int e = p.table[(size_t)b * p.max_blocks + r.j0];
+    unsigned h = shared_slot(a, e);
+    while (key[h] != e && key[h] != -1) h = (h + 1) & (a.hash - 1);
+    if (key[h] == e && cnt[h] == p.ref[e] && last[h] == b) {
+      flags[b] = fl | KEEPS;
+      word[b] &= ~1u;
+      if (!(fl & WIDE)) demand[b] -= 1;
+    } else {
+      flags[b] = fl | COPIES;
+    }
+  }
+  cluster_wait();   // the others' shared memory is there
+  __syncthreads();
+  // wide rows, of the CTA's share of them
+  for (int b = rank + PG_CTAS * warp; b < p.n_seq; b += PG_CTAS * (PG_THREADS / 32)) {
+    if (!(flags[b] & WIDE)) continue;
+    const GrowRow r = grow_row(p, a, b);
+    unsigned n = 0;
     for (int j = r.j0; j < r.j1; j += 32) {
       const int c = j + lane;
-      bool need = false, keep = false;
-      if (c < r.j1) {
+      bool need = false;
+      if (c == r.j0) {
+        need = word[b] & 1;
+      } else if (c < r.j1) {
         const int e = p.table[(size_t)b * p.max_blocks + c];
-        if (!held(p, e)) {
-          need = true;
-          if (e != -1) p.flag(ERRW_POS);
-        } else {
-          const int f = p.ref[e];
-          if (f <= 0) p.flag(ERRW_POS);   // (held, but counted as free)
-          need = f > 1;
-          if (need && c == r.j0 && r.n % p.block_tokens) {
-            int h = (int)(((unsigned)e * 2654435761u) >> 7) & (a.hash - 1);
-            while (key[h] != e && key[h] != -1) h = (h + 1) & (a.hash - 1);
-            keep = key[h] == e && cnt[h] == f && last[h] == b;
-            need = !keep;
-          }
-        }
+        need = needs(p, e, held(p, e) ? p.ref[e] : 0);
       }
       const unsigned m = __ballot_sync(0xffffffffu, need);
-      if (__any_sync(0xffffffffu, keep)) fl |= (int)KEEPS;
       if (lane == 0) a.mask[(size_t)b * a.mask_words + (j - r.j0) / 32] = m;
       n += __popc(m);
     }
-    if (lane < PG_CTAS) {
-      cluster_store(demand + b, lane, n);
-      cluster_store(flags + b, lane, fl);
-    }
+    if (lane < PG_CTAS) cluster_store(reinterpret_cast<int*>(demand + b), lane, (int)n);
   }
-  // free blocks of the CTA's part of the counts
-  const int seg = ((p.n_blocks + PG_CTAS - 1) / PG_CTAS + 3) & ~3, i0 = min(p.n_blocks, rank * seg), i1 = min(p.n_blocks, i0 + seg);
-  int n_free = 0;
-  for (int i = i0 + tid; i < i1; i += PG_THREADS) n_free += p.ref[i] == 0;
-  int total = 0;
-  cta_scan(n_free, red, &total);
-  if (tid < PG_CTAS) cluster_store(s_free + rank, tid, total);
+  if (tid < PG_CTAS) cluster_store(reinterpret_cast<int*>(s_free + rank), tid, total);
   cluster_barrier();
 
   // sums over the rows, in row order
-  long long asked = 0, taken = 0, mine_free = 0, all_free = 0;
+  unsigned mine_free = 0, all_free = 0, asked = 0;
+#pragma unroll
   for (int r = 0; r < PG_CTAS; ++r) {
     if (r < rank) mine_free += s_free[r];
     all_free += s_free[r];
   }
   for (int c0 = 0; c0 < p.n_seq; c0 += PG_THREADS) {
-    const int b = c0 + tid;
-    long long v = b < p.n_seq ? demand[b] : 0;
+    const int b = c0 + tid, here = min(p.n_seq - c0, PG_THREADS);
+    unsigned v = b < p.n_seq ? min(demand[b], MANY) : 0;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-      const long long u = __shfl_up_sync(0xffffffffu, v, o);
-      if (lane >= o) v += u;
+      const unsigned u = __shfl_up_sync(0xffffffffu, v, o);
+      if (lane >= o) v = min(v + u, MANY);
+    }
+    if (lane == 31) redu[warp] = v;
+    __syncthreads();
+    unsigned before = asked;
+    for (int w = 0; w * 32 < here; ++w) {   // (as few warps as hold rows)
+      if (w == warp) v = min(v + before, MANY);
+      before = min(before + redu[w], MANY);
+    }
+    asked = before;
+    if (b < p.n_seq) {
+      pre[b] = v;
+      // (the sums do not fall: the rows that are served are those up to the last that fits, and rows that ask for nothing)
+      if (v <= all_free) atomicMax(&s_taken, v);
     }
     __syncthreads();
-    if (lane == 31) red64[warp] = v;
-    __syncthreads();
-    for (int w = 0; w < warp; ++w) v += red64[w];
-    v += asked;
-    if (b < p.n_seq) pre[b] = v;
-    for (int w = 0; w < PG_THREADS / 32; ++w) asked += red64[w];
   }
-  __syncthreads();
-  // (the sums do not fall: the rows that are served are those up to the last that fits, and rows that ask for nothing)
-  for (int lo = 0, hi = p.n_seq; lo < hi;) {
-    const int mid = (lo + hi) / 2;
-    if (pre[mid] <= all_free) {
-      taken = pre[mid];
-      lo = mid + 1;
+  const unsigned taken = s_taken;
+  // the first `taken` free blocks, in ascending order, to the entries that ask, in order
+  auto give = [&](unsigned k, int id) {
+    int b = 0;
+    for (int hi = p.n_seq; b < hi;) {   // the first row with a larger sum
+      const int mid = (b + hi) / 2;
+      if (pre[mid] > k)
+        hi = mid;
+      else
+        b = mid + 1;
+    }
+    unsigned q = k - (pre[b] - demand[b]);
+    const GrowRow r = grow_row(p, a, b);
+    int c = r.j0;
+    if (demand[b] == (unsigned)(r.j1 - r.j0)) {
+      c += (int)q;   // all of them
+    } else if (!(flags[b] & WIDE)) {
+      unsigned w = word[b];
+      for (; q; --q) w &= w - 1;
+      c += __ffs(w) - 1;
     } else {
-      hi = mid;
+      const unsigned* m = a.mask + (size_t)b * a.mask_words;
+      unsigned w = *m;
+      for (int n = __popc(w); q >= (unsigned)n; n = __popc(w)) {
+        q -= n;
+        c += 32;
+        w = *++m;
+      }
+      for (; q; --q) w &= w - 1;
+      c += __ffs(w) - 1;
     }
-  }
-  // the first `taken` free blocks, in ascending order
-  long long base = mine_free;
-  for (int i = i0; i < i1 && base < taken; i += PG_THREADS) {
-    const int id = i + tid;
-    const bool f = id < i1 && p.ref[id] == 0;
-    const int at = cta_scan(f ? 1 : 0, red, &total);
-    if (f && base + at < taken) a.list[base + at] = id;
+    int* at = p.table + (size_t)b * p.max_blocks + c;
+    const int e = *at;
+    *at = id;
+    p.ref[id] = 1;
+    if (!held(p, e)) return;
+    atomicSub(p.ref + e, 1);
+    if (c == r.j0 && r.part) {
+      a.src[b] = e;
+      a.dst[b] = id;
+    }
+  };
+  unsigned base = mine_free;
+  for (int i = i0; i < i1 && base < taken; i += 4 * PG_THREADS) {
+    const unsigned bits = i == i0 ? bits0 : free_bits(p.ref, i + 4 * tid, i1);
+    unsigned k = base + (i1 - i0 <= 4 * PG_THREADS ? at0 : cta_scan(__popc(bits), red, &total));
+    for (unsigned m = bits; m && k < taken; m &= m - 1, ++k) give(k, i + 4 * tid + __ffs(m) - 1);
     base += total;
   }
-  cluster_barrier();
-
-  for (int b = b0 + warp; b < b1; b += PG_THREADS / 32) {
-    const GrowRow r = grow_row(p, a, b);
-    const bool served = r.asks && (pre[b] <= all_free || (demand[b] == 0 && !(flags[b] & KEEPS)));
-    int src = -1, dst = -1;
-    long long k = pre[b] - demand[b];
-    if (served && demand[b]) {
-      for (int j = r.j0; j < r.j1; j += 32) {
-        const unsigned m = a.mask[(size_t)b * a.mask_words + (j - r.j0) / 32];
-        if (m >> lane & 1) {
-          const int c = j + lane, id = a.list[k + __popc(m & ((1u << lane) - 1))];
-          int* at = p.table + (size_t)b * p.max_blocks + c;
-          const int e = *at;
-          *at = id;
-          p.ref[id] = 1;
-          if (held(p, e)) {
-            atomicSub(p.ref + e, 1);
-            if (c == r.j0 && r.n % p.block_tokens) {
-              src = e;
-              dst = id;
-            }
-          }
-        }
-        k += __popc(m);
-      }
-    }
-    if (lane == 0) {   // (the entry that is written in part is the row's first: lane 0's)
-      a.got[b] = served ? r.want : r.n;
-      a.src[b] = src;
-      a.dst[b] = dst;
+  if (rank == 0) {
+    for (int b = tid; b < p.n_seq; b += PG_THREADS) {
+      const unsigned fl = flags[b];
+      const bool served = (fl & ASKS) && (pre[b] <= all_free || (demand[b] == 0 && !(fl & KEEPS)));
+      a.got[b] = served ? a.want[b] : a.length[b];
+      if (!served || !(fl & COPIES)) a.src[b] = a.dst[b] = -1;   // (else written with the block)
     }
   }
 }
@@ -274,19 +378,28 @@ __global__ void __launch_bounds__(PG_THREADS) kv_reserve_kernel(Pages p, Reserve
 // ---------------------------------------------------------------------------------------------
 // Compaction: with U blocks in use, the k-th of those in use past the first U ids goes to the k-th free one below U.
 // ---------------------------------------------------------------------------------------------
+__device__ __forceinline__ unsigned used_bits(const int* ref, int i, int n) {
+  if (i + 4 <= n) {
+    const int4 f = *reinterpret_cast<const int4*>(ref + i);
+    return (f.x > 0) | (f.y > 0) << 1 | (f.z > 0) << 2 | (f.w > 0) << 3;
+  }
+  unsigned m = 0;
+  for (int k = 0; i + k < n; ++k) m |= (unsigned)(ref[i + k] > 0) << k;
+  return m;
+}
 __global__ void __launch_bounds__(PG_THREADS) kv_compact_kernel(Pages p, int* used, int* src, int* dst, int* remap) {
   PDL_ENTRY();
   __shared__ int red[32], s_used[PG_CTAS], s_low;
-  const int tid = threadIdx.x, rank = cluster_rank();
-  const int seg = (p.n_blocks + PG_CTAS - 1) / PG_CTAS, i0 = min(p.n_blocks, rank * seg), i1 = min(p.n_blocks, i0 + seg);
+  const int tid = threadIdx.x, rank = cluster_rank(), ctas = PG_CTAS;
+  const int seg = ((p.n_blocks + ctas - 1) / ctas + 3) & ~3, i0 = min(p.n_blocks, rank * seg), i1 = min(p.n_blocks, i0 + seg);
   int n = 0, total = 0;
-  for (int i = i0 + tid; i < i1; i += PG_THREADS) n += p.ref[i] > 0;
+  for (int i = i0 + 4 * tid; i < i1; i += 4 * PG_THREADS) n += __popc(used_bits(p.ref, i, i1));
   cta_scan(n, red, &total);
   cluster_barrier();   // the others' shared memory is there
-  if (tid < PG_CTAS) cluster_store(s_used + rank, tid, total);
+  if (tid < ctas) cluster_store(s_used + rank, tid, total);
   cluster_barrier();
   int U = 0, before = 0;
-  for (int r = 0; r < PG_CTAS; ++r) {
+  for (int r = 0; r < ctas; ++r) {
     if (r < rank) before += s_used[r];
     U += s_used[r];
   }
@@ -294,24 +407,30 @@ __global__ void __launch_bounds__(PG_THREADS) kv_compact_kernel(Pages p, int* us
   // blocks in use below U: counted by the CTA that holds id U (ids end at U where all are in use)
   if (U == p.n_blocks ? rank == 0 : (U >= i0 && U < i1)) {
     n = 0;
-    for (int i = i0 + tid; i < min(i1, U); i += PG_THREADS) n += p.ref[i] > 0;
+    for (int i = i0 + 4 * tid; i < min(i1, U); i += 4 * PG_THREADS) n += __popc(used_bits(p.ref, i, min(i1, U)));
     cta_scan(n, red, &total);
-    if (tid < PG_CTAS) cluster_store(&s_low, tid, U == p.n_blocks ? U : before + total);
+    if (tid < ctas) cluster_store(&s_low, tid, U == p.n_blocks ? U : before + total);
   }
   cluster_barrier();
   const int low = s_low, moves = U - low;
-  for (int i = i0; i < i1; i += PG_THREADS) {
-    const int id = i + tid;
-    const bool u = id < i1 && p.ref[id] > 0;
-    const int at = before + cta_scan(u ? 1 : 0, red, &total);   // in use before id
-    if (id < i1 && id < U && !u) dst[id - at] = id;
-    if (id < i1 && id >= U) {
-      if (u) src[at - low] = id;
-      remap[id] = -1;
+  for (int i = i0; i < i1; i += 4 * PG_THREADS) {
+    const unsigned u = used_bits(p.ref, i + 4 * tid, i1);
+    int at = before + cta_scan(__popc(u), red, &total);   // in use before the id
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int id = i + 4 * tid + j;
+      if (id >= i1) break;
+      if (u >> j & 1) {
+        if (id >= U) src[at - low] = id;
+        ++at;
+      } else if (id < U) {
+        dst[id - at] = id;
+      }
+      if (id >= U) remap[id] = -1;
     }
     before += total;
   }
-  const int all = PG_CTAS * PG_THREADS, me = rank * PG_THREADS + tid;
+  const int all = ctas * PG_THREADS, me = rank * PG_THREADS + tid;
   for (int k = moves + me; k < p.n_blocks / 2; k += all) src[k] = dst[k] = -1;
   cluster_barrier();
   for (int k = me; k < moves; k += all) {
@@ -334,49 +453,118 @@ __global__ void __launch_bounds__(PG_THREADS) kv_compact_kernel(Pages p, int* us
 }
 
 // ---------------------------------------------------------------------------------------------
-// Blocks copied in every layer.
+// Blocks copied in every layer.  Bound by HBM (a block that several pairs copy is read from L2 but once).  The CTAs take pieces of 32 KB in
+// turn, of the pairs that name a block: where most do not (a row that writes into no shared block), those cost a look at their
+// numbers.
 // ---------------------------------------------------------------------------------------------
-__global__ void __launch_bounds__(256) kv_copy_kernel(const __grid_constant__ CopyLayers c, int n_pairs, const int* src, const int* dst) {
+constexpr int CP_THREADS = 256, CP_LOADS = 8, CP_PIECE = CP_THREADS * CP_LOADS, CP_PAIRS = 1024;   // 16-byte loads; pairs looked at together
+
+__global__ void __launch_bounds__(CP_THREADS) kv_copy_kernel(const __grid_constant__ CopyLayers c, int n_pairs, const int* src, const int* dst) {
   PDL_ENTRY();
-  const int l = (int)blockIdx.z >> 1, is_v = (int)blockIdx.z & 1;
-  char* pool = (char*)(is_v ? c.v[l] : c.k[l]);
-  uint8_t* ex = is_v ? c.v_exp[l] : c.k_exp[l];
-  for (int i = (int)blockIdx.y; i < n_pairs; i += (int)gridDim.y) {
-    const int s = src[i], d = dst[i];
-    if (s < 0 || d < 0 || s == d) continue;
-    if (s >= c.n_blocks || d >= c.n_blocks) {
-      c.err ? (void)atomicOr(c.err, (unsigned)ERRW_POS) : (void)0;
-      continue;
+  __shared__ int2 live[CP_PAIRS];
+  __shared__ int s_warp[CP_THREADS / 32];
+  constexpr int EACH = CP_PAIRS / CP_THREADS;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const unsigned vecs = (unsigned)(c.block_bytes / 16), pieces = (vecs + CP_PIECE - 1) / CP_PIECE, arrays = 2u * c.n_layers;
+  for (int i0 = 0; i0 < n_pairs; i0 += CP_PAIRS) {
+    // the pairs that name a block, in order (the same in every CTA)
+    int2 mine[EACH];
+    int n = 0;
+#pragma unroll
+    for (int k = 0; k < EACH; ++k) {
+      const int i = i0 + tid * EACH + k;
+      mine[k] = i < n_pairs ? make_int2(src[i], dst[i]) : make_int2(-1, -1);
+      bool ok = mine[k].x >= 0 && mine[k].y >= 0 && mine[k].x != mine[k].y;
+      if (ok && (mine[k].x >= c.n_blocks || mine[k].y >= c.n_blocks)) {
+        ok = false;
+        if (c.err) atomicOr(c.err, (unsigned)ERRW_POS);
+      }
+      if (!ok) mine[k].x = -1;
+      n += ok;
     }
-    const uint4* from = reinterpret_cast<const uint4*>(pool + s * c.block_bytes);
-    uint4* to = reinterpret_cast<uint4*>(pool + d * c.block_bytes);
-    for (long long j = blockIdx.x * 256 + threadIdx.x; j < c.block_bytes / 16; j += gridDim.x * 256) to[j] = from[j];
-    for (long long j = blockIdx.x * 256 + threadIdx.x; j < c.exp_bytes; j += gridDim.x * 256)
-      ex[(size_t)d * c.exp_bytes + j] = ex[(size_t)s * c.exp_bytes + j];
+    int at = n;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int u = __shfl_up_sync(0xffffffffu, at, o);
+      if (lane >= o) at += u;
+    }
+    __syncthreads();   // the last pairs' list has been used
+    if (lane == 31) s_warp[warp] = at;
+    __syncthreads();
+    at -= n;
+    int total = 0;
+#pragma unroll
+    for (int w = 0; w < CP_THREADS / 32; ++w) {
+      if (w < warp) at += s_warp[w];
+      total += s_warp[w];
+    }
+#pragma unroll
+    for (int k = 0; k < EACH; ++k)
+      if (mine[k].x >= 0) live[at++] = mine[k];
+    __syncthreads();
+    const unsigned long long items = (unsigned long long)total * arrays * pieces;
+    for (unsigned long long it = blockIdx.x; it < items; it += gridDim.x) {
+      const unsigned long long q = it / pieces;
+      const unsigned piece = (unsigned)(it - q * pieces), pr = (unsigned)(q / arrays), ar = (unsigned)(q - (unsigned long long)pr * arrays);
+      const int2 p = live[pr];
+      char* pool = (char*)(ar & 1 ? c.v[ar >> 1] : c.k[ar >> 1]);
+      const uint4* from = reinterpret_cast<const uint4*>(pool + p.x * c.block_bytes);
+      uint4* to = reinterpret_cast<uint4*>(pool + p.y * c.block_bytes);
+      uint4 w[CP_LOADS];
+      const unsigned v0 = piece * CP_PIECE + tid;
+#pragma unroll
+      for (int k = 0; k < CP_LOADS; ++k)
+        if (v0 + k * CP_THREADS < vecs) w[k] = from[v0 + k * CP_THREADS];
+#pragma unroll
+      for (int k = 0; k < CP_LOADS; ++k)
+        if (v0 + k * CP_THREADS < vecs) __stcs(to + v0 + k * CP_THREADS, w[k]);
+      if (piece == 0 && c.exp_bytes) {
+        uint8_t* ex = ar & 1 ? c.v_exp[ar >> 1] : c.k_exp[ar >> 1];
+        const uint8_t* ef = ex + (size_t)p.x * c.exp_bytes;
+        uint8_t* et = ex + (size_t)p.y * c.exp_bytes;
+        if ((c.exp_bytes & 15) == 0) {
+          for (int j = tid; j < c.exp_bytes / 16; j += CP_THREADS) reinterpret_cast<uint4*>(et)[j] = reinterpret_cast<const uint4*>(ef)[j];
+        } else {
+          for (int j = tid; j < c.exp_bytes; j += CP_THREADS) et[j] = ef[j];
+        }
+      }
+    }
   }
 }
 
+int sm_count() {
+  static const int sms = [] {
+    int dev = 0, n = 0;
+    cudaGetDevice(&dev);
+    cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev);
+    return n > 0 ? n : 1;
+  }();
+  return sms;
+}
 int mask_words(const Pages& p) { return p.max_blocks / 32 + 1; }
 
 }  // namespace
 
 size_t pages_workspace(const Pages& p) {
-  const size_t fork = (size_t)p.n_seq * p.max_blocks, grow = (size_t)p.n_blocks + (size_t)p.n_seq * mask_words(p);
-  return (fork > grow ? fork : grow) * sizeof(int);
+  const size_t fork = (size_t)p.n_seq * p.max_blocks, grow = (size_t)p.n_seq * mask_words(p), move = p.n_blocks;
+  const size_t most = fork > grow ? fork : grow;
+  return (most > move ? most : move) * sizeof(int);
 }
 
 cudaError_t launch_kv_fork(cudaStream_t st, const Pages& p, const int* source, const int* length, int* ws) {
-  int cy = cdiv(p.max_blocks, 256);
-  if (cy > 64) cy = 64;
-  cudaError_t e = launch_k(kv_fork_count_kernel, dim3((unsigned)p.n_seq, (unsigned)cy), dim3(256), 0, st, p, source, length, ws);
-  if (e == cudaSuccess)
-    e = launch_k(kv_fork_write_kernel, dim3((unsigned)p.n_seq, (unsigned)cy), dim3(256), 0, st, p, source, length, (const int*)ws);
+  const long long entries = (long long)p.n_seq * p.max_blocks;
+  if (entries <= PG_CTAS * PG_THREADS * FORK_EACH)
+    return launch_cluster(kv_fork_kernel, dim3(PG_CTAS), PG_CTAS, PG_THREADS, 0, st, p, source, length);
+  const int chunks = cdiv(p.max_blocks, FORK_CHUNK);
+  const dim3 g((unsigned)p.n_seq, (unsigned)(chunks < 65535 ? chunks : 65535));
+  cudaError_t e = launch_k(kv_fork_count_kernel, g, dim3(FORK_THREADS), 0, st, p, source, length, ws);
+  if (e == cudaSuccess) e = launch_k(kv_fork_write_kernel, g, dim3(FORK_THREADS), 0, st, p, source, length, (const int*)ws);
   return e;
 }
 
 cudaError_t launch_kv_reserve(cudaStream_t st, const Pages& p, const int* length, const int* want, int* got, int* src, int* dst,
                               int* ws) {
-  ReserveCall a{length, want, got, src, dst, ws, reinterpret_cast<unsigned*>(ws + p.n_blocks), mask_words(p), 32};
+  ReserveCall a{length, want, got, src, dst, reinterpret_cast<unsigned*>(ws), mask_words(p), 32};
   while (a.hash < 2 * p.n_seq) a.hash *= 2;
   const size_t smem = (size_t)p.n_seq * 16 + (size_t)a.hash * 12;
   struct Tag;
@@ -390,9 +578,8 @@ cudaError_t launch_kv_compact(cudaStream_t st, const Pages& p, int* used, int* s
 }
 
 cudaError_t launch_kv_copy_blocks(cudaStream_t st, const CopyLayers& c, int n_pairs, const int* src, const int* dst) {
-  const long long pieces = (c.block_bytes / 16 + 255) / 256;
-  const dim3 g((unsigned)(pieces < 8 ? pieces : 8), (unsigned)(n_pairs < 65535 ? n_pairs : 65535), (unsigned)(2 * c.n_layers));
-  return launch_k(kv_copy_kernel, g, dim3(256), 0, st, c, n_pairs, src, dst);
+  const long long vecs = c.block_bytes / 16, items = n_pairs * 2ll * c.n_layers * ((vecs + CP_PIECE - 1) / CP_PIECE), most = 32ll * sm_count();
+  return launch_k(kv_copy_kernel, dim3((unsigned)(items < most ? items : most)), dim3(CP_THREADS), 0, st, c, n_pairs, src, dst);
 }
 
 }  // namespace adept

@@ -14,6 +14,7 @@ adept_status pages_of(const adept_kv_pages* p, Pages* v) {
     return bad(ADEPT_ERR_INVALID_ARG, "non-positive size of the pages");
   if ((long long)p->max_blocks_per_seq * p->block_tokens > (1ll << 30))
     return bad(ADEPT_ERR_INVALID_ARG, "rows too long (2^30 positions)");
+  if (p->n_blocks > (1 << 30)) return bad(ADEPT_ERR_INVALID_ARG, "n_blocks %d above 2^30", p->n_blocks);
   if (!p->d_block_table || !p->d_ref) return bad(ADEPT_ERR_INVALID_ARG, "NULL block table or counts");
   if (((uintptr_t)p->d_block_table | (uintptr_t)p->d_err) & 3) return bad(ADEPT_ERR_INVALID_ARG, "misaligned block table or error word");
   if ((uintptr_t)p->d_ref & 15) return bad(ADEPT_ERR_INVALID_ARG, "the counts must start on 16 bytes");

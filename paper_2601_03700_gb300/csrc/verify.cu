@@ -201,7 +201,7 @@ __device__ __forceinline__ void row_stats(const VerifyCall& a, const T* x, bool 
 }
 
 template <typename TT, typename TD>
-__global__ void __launch_bounds__(VS_THREADS, 7) verify_stats_kernel(VerifyCall a, int parts, Stat* stats) {
+__global__ void __launch_bounds__(VS_THREADS, 8) verify_stats_kernel(VerifyCall a, int parts, Stat* stats) {
   PDL_ENTRY();
   const int r = (int)blockIdx.x / parts, part = (int)blockIdx.x % parts;
   Stat* out = stats + ((size_t)blockIdx.y * a.n_rows + r) * parts + part;
