@@ -172,6 +172,25 @@ ADEPT_API adept_status adept_extend(adept_model* m, int batch, const int32_t* h_
                           const int32_t* d_forced_exit, int32_t* d_exit_layer_out, float* d_logits_out,
                           int32_t* d_next_token_out, float* d_sim_out, void* stream);
 
+/* adept_extend, and the chunks verified: h_lens[b] tokens of sequence b, the last accepted one and then drafts (of its own earlier
+ * exits, another model, a look-up), against this pass's logits.  d_logits_out [sum of h_lens][vocab] fp32 (not NULL) receives those
+ * of every token; d_draft, d_temperature, d_u, d_accepted_out, d_next_token_out and d_logprob_out are those of adept_verify_drafts, whose
+ * d_start are the chunks' (a sequence without tokens: 0, -1).  The sequences hold their whole chunks afterwards: adept_seq_trim takes away what
+ * was not accepted (of 1 + d drafts' tokens, 1 + accepted stay).
+ * Drafts of the model's own: generation steps with a threshold that lets tokens leave early, then adept_seq_trim back to where
+ * they began, and this call over the same tokens at the threshold that is to hold (+infinity: full depth), which writes their K/V anew.
+ * The first call allocates its workspace.  Errors: as adept_extend, and INVALID_ARG for what adept_verify_drafts refuses; a sequence that
+ * the verification leaves out flags DEVICE_INPUT. */
+ADEPT_API adept_status adept_extend_verify(adept_model* m, int batch, const int32_t* h_lens, const int32_t* d_tokens, float delta,
+                                 const int32_t* d_forced_exit, int draft_dtype, const void* d_draft, int64_t ld_draft,
+                                 const float* d_temperature, const float* d_u, int32_t* d_exit_layer_out, float* d_logits_out,
+                                 int32_t* d_accepted_out, int32_t* d_next_token_out, float* d_logprob_out, float* d_sim_out,
+                                 void* stream);
+
+/* Cuts sequences 0..batch-1 back to their first h_lens[b] positions (at most what they hold; their blocks stay reserved), for what is
+ * enqueued on `stream` after it.  Not in a captured stream.  Errors: INVALID_ARG, CAPACITY (batch > max_batch), CUDA. */
+ADEPT_API adept_status adept_seq_trim(adept_model* m, int batch, const int32_t* h_lens, void* stream);
+
 /* Threshold calibration (Sec. 4.1: delta is set to meet the computation budget; Sec. 5.1):
  * bisection on delta in [lo, hi] over prompt passes of the calibration batch d_tokens
  * [batch, prompt_len] (threshold exits, no forced exits) until the batch's reduction in

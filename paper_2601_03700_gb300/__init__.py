@@ -43,7 +43,7 @@ ABI_SYMBOLS = [
     "adept_kv_append", "adept_kv_gather", "adept_chunk_attention", "adept_chunk_attention_workspace", "adept_kv_check",
     "adept_extend",
     "adept_kv_pages_workspace", "adept_kv_fork", "adept_kv_reserve", "adept_kv_compact", "adept_kv_copy_blocks",
-    "adept_verify_drafts", "adept_verify_workspace", "adept_error_check",
+    "adept_verify_drafts", "adept_verify_workspace", "adept_error_check", "adept_extend_verify", "adept_seq_trim",
 ]
 
 
@@ -152,6 +152,11 @@ def load_library(path: str = LIB_PATH):
     lib.adept_hsm_param_numel.restype = ctypes.c_int64
     lib.adept_extend.argtypes = [vp, c_int, ctypes.POINTER(ctypes.c_int32), i32p, c_float, i32p, i32p, fp, i32p, fp, st]
     lib.adept_extend.restype = c_int
+    lib.adept_extend_verify.argtypes = [vp, c_int, ctypes.POINTER(ctypes.c_int32), i32p, c_float, i32p, c_int, vp, ctypes.c_int64, fp, fp, i32p,
+                                        fp, i32p, i32p, fp, fp, st]
+    lib.adept_extend_verify.restype = c_int
+    lib.adept_seq_trim.argtypes = [vp, c_int, ctypes.POINTER(ctypes.c_int32), st]
+    lib.adept_seq_trim.restype = c_int
     kvp, i64 = ctypes.POINTER(AdeptKVCache), ctypes.c_int64
     for fn in (lib.adept_kv_append, lib.adept_kv_gather):
         fn.argtypes = [kvp, c_int, c_int, vp, i64, vp, i64, i32p, i32p, st]
@@ -279,6 +284,28 @@ def adept_extend(m, lens, tokens: torch.Tensor, delta: float, forced: Optional[t
     arr = (ctypes.c_int32 * n)(*[int(x) for x in lens])
     _check(lib, m, lib.adept_extend(m, n, arr, _ptr(tokens), float(delta), _ptr(forced), _ptr(exit_layer_out),
                                      _ptr(logits_out), _ptr(next_token_out), _ptr(sim_out), _stream(stream)))
+
+
+def adept_extend_verify(m, lens, tokens: torch.Tensor, delta: float, u: torch.Tensor, logits_out: torch.Tensor, accepted_out: torch.Tensor,
+                        next_token_out: torch.Tensor, draft: Optional[torch.Tensor] = None, temperature: Optional[torch.Tensor] = None,
+                        forced: Optional[torch.Tensor] = None, exit_layer_out: Optional[torch.Tensor] = None,
+                        logprob_out: Optional[torch.Tensor] = None, sim_out: Optional[torch.Tensor] = None, stream=None):
+    """adept_extend over chunks of the last accepted token and drafts, which are verified against its logits (logits_out: of every
+    token).  u, draft, temperature, accepted_out, next_token_out, logprob_out: as in adept_verify_drafts."""
+    lib = load_library()
+    n = len(lens)
+    arr = (ctypes.c_int32 * n)(*[int(x) for x in lens])
+    dt, dp, ld = (0, None, 0) if draft is None else _logits(draft, "draft", draft)
+    _check(lib, m, lib.adept_extend_verify(m, n, arr, _ptr(tokens), float(delta), _ptr(forced), dt, dp, ld, _ptr(temperature), _ptr(u),
+                                            _ptr(exit_layer_out), _ptr(logits_out), _ptr(accepted_out), _ptr(next_token_out),
+                                            _ptr(logprob_out), _ptr(sim_out), _stream(stream)))
+
+
+def adept_seq_trim(m, lens, stream=None):
+    """Cuts sequences 0..len(lens)-1 back to their first lens[b] positions."""
+    lib = load_library()
+    arr = (ctypes.c_int32 * len(lens))(*[int(x) for x in lens])
+    _check(lib, m, lib.adept_seq_trim(m, len(lens), arr, _stream(stream)))
 
 
 def adept_skip_kv_fill(m, n_tokens: int, h_mapped: torch.Tensor, exit_layer: torch.Tensor, seq: torch.Tensor,
@@ -697,10 +724,10 @@ def verify_workspace(n_rows: int, device="cuda", stream=None) -> torch.Tensor:
     return _make(n, device, stream)
 
 
-def _vector(like: torch.Tensor, name: str, t: Optional[torch.Tensor], n: int, dtype):
+def _vector(like: torch.Tensor, index: int, name: str, t: Optional[torch.Tensor], n: int, dtype):
     if t is None:
         return None
-    if t.dtype is not dtype or t.get_device() != like.get_device() or t.shape != (n,) or not t.is_contiguous():
+    if t.dtype is not dtype or t.get_device() != index or t.shape != (n,) or not t.is_contiguous():
         raise ValueError(f"{name} must be {n} contiguous {dtype} values on {like.device}")
     return t.data_ptr()
 
@@ -735,18 +762,18 @@ def adept_verify_drafts(target: torch.Tensor, draft: Optional[torch.Tensor], tok
     n_seq = start.shape[0] - 1 if start.dim() == 1 else -1
     if n_seq < 0:
         raise ValueError("start must be n_seq + 1 values")
-    vec = lambda name, t, k, dt: _vector(target, name, t, k, dt)  # noqa: E731
-    args = (vec("tokens", tokens, n, i32), vec("start", start, n_seq + 1, i32), vec("temperature", temperature, n_seq, f32), vec("u", u, n, f32),
-            vec("accepted", accepted, n_seq, i32), vec("next_token", next_token, n_seq, i32), vec("logprob", logprob, n, f32),
-            vec("err", err, 1, i32))
-    if target.get_device() < 0:
+    at = target.get_device()
+    args = (_vector(target, at, "tokens", tokens, n, i32), _vector(target, at, "start", start, n_seq + 1, i32),
+            _vector(target, at, "temperature", temperature, n_seq, f32), _vector(target, at, "u", u, n, f32),
+            _vector(target, at, "accepted", accepted, n_seq, i32), _vector(target, at, "next_token", next_token, n_seq, i32),
+            _vector(target, at, "logprob", logprob, n, f32), _vector(target, at, "err", err, 1, i32))
+    if at < 0:
         raise ValueError(f"the logits are on {target.device}: the operators need a GPU")
     if workspace is None:
         workspace = verify_workspace(n, target.device, stream)
-    elif workspace.get_device() != target.get_device() or not workspace.is_contiguous():
+    elif workspace.get_device() != at or not workspace.is_contiguous():
         raise ValueError(f"workspace must be contiguous on {target.device}")
-    _call_on(target.get_device(), lib.adept_verify_drafts, stream, n_seq, n, v, td, tp, tl, dd, dp, dl, *args, workspace.data_ptr(),
-             workspace.nbytes)
+    _call_on(at, lib.adept_verify_drafts, stream, n_seq, n, v, td, tp, tl, dd, dp, dl, *args, workspace.data_ptr(), workspace.nbytes)
 
 
 # ---------------------------------------------------------------------------
@@ -798,6 +825,27 @@ class Model:
         adept_extend(self.h, lens, tokens.to(torch.int32).contiguous().view(-1), delta,
                      None if forced is None else forced.to(torch.int32).contiguous().view(-1), ex, lg, nx, sim, stream)
         return ex, lg, nx, sim
+
+    def verify(self, lens, tokens: torch.Tensor, delta: float, u: torch.Tensor, draft: Optional[torch.Tensor] = None,
+               temperature: Optional[torch.Tensor] = None, forced: Optional[torch.Tensor] = None, stream=None):
+        """adept_extend_verify over chunks of lens[b] tokens (the last accepted one, then drafts): drafts accepted and next token per
+        sequence, then logits, log probabilities of the tokens taken (NaN elsewhere), exit layers and similarities per token."""
+        n, dev = int(sum(int(x) for x in lens)), tokens.device
+        if any(t is not None and t.shape[:1] != (n,) for t in (tokens, u, draft, forced)):
+            raise ValueError(f"tokens, u, draft logits and forced exits must have sum(lens) = {n} rows")
+        if draft is not None and draft.shape[-1] != self.n_out or temperature is not None and temperature.shape != (len(lens),):
+            raise ValueError("draft must be [tokens, vocab], temperature one number a sequence")
+        ex, _, nx, sim = self._outs(n, len(lens), dev)
+        acc = torch.empty_like(nx)
+        lg = torch.empty(n, self.n_out, dtype=torch.float32, device=dev)
+        lp = torch.full((n,), float("nan"), dtype=torch.float32, device=dev)
+        adept_extend_verify(self.h, lens, tokens.to(torch.int32).contiguous(), delta, u.float().contiguous(), lg, acc, nx, draft,
+                            None if temperature is None else temperature.float().contiguous(),
+                            None if forced is None else forced.to(torch.int32).contiguous(), ex, lp, sim, stream)
+        return acc, nx, lg, lp, ex, sim
+
+    def trim(self, lens, stream=None):
+        adept_seq_trim(self.h, lens, stream)
 
     def decode_step(self, tokens: torch.Tensor, delta: float, forced: Optional[torch.Tensor] = None, stream=None):
         B = tokens.numel()

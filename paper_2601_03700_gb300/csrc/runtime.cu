@@ -4,6 +4,7 @@
 #include "adept.h"
 #include "common.cuh"
 #include "kernels.h"
+#include "serve_ops.h"
 #include "gemm_tc.h"
 #include "gemm_decode.h"
 #include "gemm_stream.h"
@@ -158,6 +159,7 @@ struct adept_model {
   int *d_ext = nullptr, *ext_start = nullptr, *ext_pos = nullptr;
   float* ext_ws = nullptr;
   size_t ext_ws_bytes = 0;
+  void *ver_x = nullptr, *ver_ws = nullptr;   // adept_extend_verify (made at its first call): head input rows, the verification's workspace
   int32_t* calib_exit = nullptr; // threshold calibration: exit layers of a calibration pass
   // standardisation statistics of X_out handed from the O projection to the FFN input
   float2* tile_stats = nullptr;                // [DG_MAX_M][D / 32] (mean, M2) of X_out tiles
@@ -1861,6 +1863,54 @@ static adept_status put_chunks(adept_model* m, int batch, const int32_t* lens, c
   return ADEPT_OK;
 }
 
+extern "C" {
+static adept_status check_cross_set(adept_model* m, int batch);
+}
+
+// The pass of adept_extend: checks, and the chunks' tokens through the layers; *total: how many there are.  ready(): what else the call
+// has to have before anything is enqueued.
+template <typename F>
+static adept_status extend_pass(adept_model* m, int batch, const int32_t* h_lens, const int32_t* d_tokens, float delta,
+                                const int32_t* d_forced_exit, int32_t* d_exit_layer_out, float* d_sim_out, cudaStream_t st, F ready,
+                                int* total_out) {
+  if (m->cfg.family == ADEPT_FAMILY_BERT) return fail(m, ADEPT_ERR_INVALID_ARG, "adept_extend needs a decoder model");
+  if (!h_lens || !d_tokens) return fail(m, ADEPT_ERR_INVALID_ARG, "h_lens or d_tokens is NULL");
+  if (batch < 1) return fail(m, ADEPT_ERR_INVALID_ARG, "batch must be positive");
+  if (batch > m->cfg.max_batch) return fail(m, ADEPT_ERR_CAPACITY, "batch %d > max_batch %d", batch, m->cfg.max_batch);
+  if (std::isnan(delta)) return fail(m, ADEPT_ERR_INVALID_ARG, "delta is NaN");
+  if (m->all_at_once)
+    return fail(m, ADEPT_ERR_INVALID_ARG, "all-at-once exits are defined for whole prompts (adept_prefill)");
+  TRY(check_cross_set(m, batch));
+  long long total = 0;
+  ExtendPass e{0, 0};
+  for (int b = 0; b < batch; ++b) {
+    if (h_lens[b] < 0) return fail(m, ADEPT_ERR_INVALID_ARG, "length %d of sequence %d", h_lens[b], b);
+    if (h_lens[b] == 0) continue;
+    if (m->seq_blocks[b].empty())
+      return fail(m, ADEPT_ERR_INVALID_ARG, "sequence %d is not reserved (adept_prefill or adept_seq_reserve)", b);
+    if ((long long)m->h_seq_len[b] + h_lens[b] > m->cfg.max_seq)
+      return fail(m, ADEPT_ERR_CAPACITY, "sequence %d: %d positions and %d new tokens, max_seq %d", b, m->h_seq_len[b], h_lens[b],
+                  m->cfg.max_seq);
+    total += h_lens[b];
+    e.max_len = std::max(e.max_len, h_lens[b]);
+    e.max_kv = std::max(e.max_kv, m->h_seq_len[b] + h_lens[b]);
+  }
+  if (total < 1) return fail(m, ADEPT_ERR_INVALID_ARG, "no sequence has a new token");
+  if (total > m->T_max)
+    return fail(m, ADEPT_ERR_CAPACITY, "%lld new tokens above the pass workspace (%d rows)", total, m->T_max);
+  TRY(no_capture(m, st));
+  TRY(extend_init(m));
+  TRY(ready());
+  for (int b = 0; b < batch; ++b) e.max_kv = std::max(e.max_kv, m->h_seq_len[b]);   // (sequences without new tokens too)
+  TRY(put_chunks(m, batch, h_lens, m->h_seq_len.data(), st));
+  launch_set_float(st, m->d_delta, delta);
+  m->launches += 1;
+  TRY(run_pass(m, (int)total, batch, 0, false, d_tokens, d_forced_exit, d_exit_layer_out, d_sim_out, st, &e));
+  for (int b = 0; b < batch; ++b) m->h_seq_len[b] += h_lens[b];
+  *total_out = (int)total;
+  return ADEPT_OK;
+}
+
 // ---------------------------------------------------------------------------
 // C ABI
 // ---------------------------------------------------------------------------
@@ -1989,40 +2039,9 @@ adept_status adept_extend(adept_model* m, int batch, const int32_t* h_lens, cons
                           int32_t* d_next_token_out, float* d_sim_out, void* stream) {
   if (!m) return ADEPT_ERR_INVALID_ARG;
   g_pdl = !m->profile;
-  if (m->cfg.family == ADEPT_FAMILY_BERT) return fail(m, ADEPT_ERR_INVALID_ARG, "adept_extend needs a decoder model");
-  if (!h_lens || !d_tokens) return fail(m, ADEPT_ERR_INVALID_ARG, "h_lens or d_tokens is NULL");
-  if (batch < 1) return fail(m, ADEPT_ERR_INVALID_ARG, "batch must be positive");
-  if (batch > m->cfg.max_batch) return fail(m, ADEPT_ERR_CAPACITY, "batch %d > max_batch %d", batch, m->cfg.max_batch);
-  if (std::isnan(delta)) return fail(m, ADEPT_ERR_INVALID_ARG, "delta is NaN");
-  if (m->all_at_once)
-    return fail(m, ADEPT_ERR_INVALID_ARG, "all-at-once exits are defined for whole prompts (adept_prefill)");
-  TRY(check_cross_set(m, batch));
-  long long total = 0;
-  ExtendPass e{0, 0};
-  for (int b = 0; b < batch; ++b) {
-    if (h_lens[b] < 0) return fail(m, ADEPT_ERR_INVALID_ARG, "length %d of sequence %d", h_lens[b], b);
-    if (h_lens[b] == 0) continue;
-    if (m->seq_blocks[b].empty())
-      return fail(m, ADEPT_ERR_INVALID_ARG, "sequence %d is not reserved (adept_prefill or adept_seq_reserve)", b);
-    if ((long long)m->h_seq_len[b] + h_lens[b] > m->cfg.max_seq)
-      return fail(m, ADEPT_ERR_CAPACITY, "sequence %d: %d positions and %d new tokens, max_seq %d", b, m->h_seq_len[b], h_lens[b],
-                  m->cfg.max_seq);
-    total += h_lens[b];
-    e.max_len = std::max(e.max_len, h_lens[b]);
-    e.max_kv = std::max(e.max_kv, m->h_seq_len[b] + h_lens[b]);
-  }
-  if (total < 1) return fail(m, ADEPT_ERR_INVALID_ARG, "no sequence has a new token");
-  if (total > m->T_max)
-    return fail(m, ADEPT_ERR_CAPACITY, "%lld new tokens above the pass workspace (%d rows)", total, m->T_max);
   cudaStream_t st = (cudaStream_t)stream;
-  TRY(no_capture(m, st));
-  TRY(extend_init(m));
-  for (int b = 0; b < batch; ++b) e.max_kv = std::max(e.max_kv, m->h_seq_len[b]);   // (sequences without new tokens too)
-  TRY(put_chunks(m, batch, h_lens, m->h_seq_len.data(), st));
-  launch_set_float(st, m->d_delta, delta);
-  m->launches += 1;
-  TRY(run_pass(m, (int)total, batch, 0, false, d_tokens, d_forced_exit, d_exit_layer_out, d_sim_out, st, &e));
-  for (int b = 0; b < batch; ++b) m->h_seq_len[b] += h_lens[b];
+  int total = 0;
+  TRY(extend_pass(m, batch, h_lens, d_tokens, delta, d_forced_exit, d_exit_layer_out, d_sim_out, st, [] { return ADEPT_OK; }, &total));
   // the head over all rows; where a sequence brought nothing its outputs are left as they were
   bool all = true;
   for (int b = 0; b < batch; ++b) all &= h_lens[b] > 0;
@@ -2038,6 +2057,61 @@ adept_status adept_extend(adept_model* m, int batch, const int32_t* h_lens, cons
   }
   span_collect(m, st);
   return check_launch(m);
+}
+
+adept_status adept_extend_verify(adept_model* m, int batch, const int32_t* h_lens, const int32_t* d_tokens, float delta,
+                                 const int32_t* d_forced_exit, int draft_dtype, const void* d_draft, int64_t ld_draft,
+                                 const float* d_temperature, const float* d_u, int32_t* d_exit_layer_out, float* d_logits_out,
+                                 int32_t* d_accepted_out, int32_t* d_next_token_out, float* d_logprob_out, float* d_sim_out,
+                                 void* stream) {
+  if (!m) return ADEPT_ERR_INVALID_ARG;
+  g_pdl = !m->profile;
+  if (!d_u || !d_logits_out || !d_accepted_out || !d_next_token_out)
+    return fail(m, ADEPT_ERR_INVALID_ARG, "d_u, d_logits_out, d_accepted_out or d_next_token_out is NULL");
+  if (draft_dtype != ADEPT_DTYPE_F32 && draft_dtype != ADEPT_DTYPE_BF16) return fail(m, ADEPT_ERR_INVALID_ARG, "dtype %d unknown", draft_dtype);
+  if (d_draft && (ld_draft < m->V || ((uintptr_t)d_draft & (draft_dtype == ADEPT_DTYPE_BF16 ? 1 : 3))))
+    return fail(m, ADEPT_ERR_INVALID_ARG, "draft logits: a row stride below the vocabulary, or misaligned");
+  if (((uintptr_t)d_temperature | (uintptr_t)d_u | (uintptr_t)d_logits_out | (uintptr_t)d_accepted_out | (uintptr_t)d_next_token_out |
+       (uintptr_t)d_logprob_out) & 3)
+    return fail(m, ADEPT_ERR_INVALID_ARG, "misaligned numbers or results");
+  if (m->V > (1 << 20)) return fail(m, ADEPT_ERR_INVALID_ARG, "vocab %d above 2^20", m->V);
+  cudaStream_t st = (cudaStream_t)stream;
+  int total = 0;
+  auto ready = [m]() -> adept_status {
+    if (!m->ver_x) TRY(dalloc(m, &m->ver_x, (size_t)m->T_max * m->D * m->esz));
+    if (!m->ver_ws) TRY(dalloc(m, &m->ver_ws, verify_workspace(m->T_max)));
+    return ADEPT_OK;
+  };
+  TRY(extend_pass(m, batch, h_lens, d_tokens, delta, d_forced_exit, d_exit_layer_out, d_sim_out, st, ready, &total));
+  // the head over every token of the chunks
+  GemmProblem p;
+  memset(&p, 0, sizeof p);
+  p.a_rows = total;
+  p.A = m->ver_x; p.lda = m->D; p.B = m->w_head; p.ldb = m->D; p.rows = DevRange{nullptr, nullptr, total}; p.N = m->V; p.K = m->D;
+  p.Bt = m->t_head; p.bt_nkb = cdiv(m->D, TW_KB);
+  p.epi = epi_base(); p.epi.kind = EPI_F32; p.epi.bias = m->b_head; p.epi.out_f32 = d_logits_out; p.epi.ld_f32 = m->V;
+  gemm_std(m, st, p, total, m->final_, m->D, nullptr, attn_norm_mode(m), m->cfg.norm_eps, m->gemm_cls);
+  const VerifyCall v{batch, total, m->V, 0, draft_dtype == ADEPT_DTYPE_BF16, d_logits_out, d_draft, m->V, ld_draft, d_tokens, m->d_ext,
+                     d_temperature, d_u, d_accepted_out, d_next_token_out, d_logprob_out, m->err_word, m->ver_ws};
+  note_error(m, launch_verify(st, v), "verifying the drafts");
+  m->launches += 2;
+  span_collect(m, st);
+  return check_launch(m);
+}
+
+adept_status adept_seq_trim(adept_model* m, int batch, const int32_t* h_lens, void* stream) {
+  if (!m) return ADEPT_ERR_INVALID_ARG;
+  if (!h_lens) return fail(m, ADEPT_ERR_INVALID_ARG, "h_lens is NULL");
+  if (batch < 1) return fail(m, ADEPT_ERR_INVALID_ARG, "batch must be positive");
+  if (batch > m->cfg.max_batch) return fail(m, ADEPT_ERR_CAPACITY, "batch %d > max_batch %d", batch, m->cfg.max_batch);
+  for (int b = 0; b < batch; ++b)
+    if (h_lens[b] < 0 || h_lens[b] > m->h_seq_len[b])
+      return fail(m, ADEPT_ERR_INVALID_ARG, "sequence %d holds %d positions, not %d", b, m->h_seq_len[b], h_lens[b]);
+  cudaStream_t st = (cudaStream_t)stream;
+  TRY(no_capture(m, st));
+  for (int b = 0; b < batch; ++b) m->h_seq_len[b] = h_lens[b];
+  CUDA_TRY(m, cudaMemcpyAsync(m->d_seq_len, m->h_seq_len.data(), batch * sizeof(int), cudaMemcpyHostToDevice, st));
+  return ADEPT_OK;
 }
 
 adept_status adept_set_cross_source(adept_model* m, int n_seq, const int32_t* h_src_len, const float* d_states,
