@@ -554,7 +554,8 @@ ADEPT_API adept_status adept_kv_reserve(const adept_kv_pages* p, const int32_t* 
 
 /* Moves the blocks in use to the front: with U of them in use (*d_used), the k-th in use past the first U goes to the k-th
  * free one among those (both in ascending order), in the table and in the counts.  d_copy_src[k], d_copy_dst[k] ([n_blocks / 2]
- * int32 each) name the moves, for adept_kv_copy_blocks; entries behind the last are -1.  Sources and targets are disjoint. */
+ * int32 each) name the moves, for adept_kv_copy_blocks, and for the program where it holds blocks itself; entries behind the last are -1.  Sources and targets are
+ * disjoint. */
 ADEPT_API adept_status adept_kv_compact(const adept_kv_pages* p, int32_t* d_used, int32_t* d_copy_src, int32_t* d_copy_dst, void* d_ws,
                               int64_t ws_bytes, void* stream);
 
@@ -584,7 +585,7 @@ ADEPT_API adept_status adept_kv_copy_blocks(const adept_kv_cache* caches, int n_
  *   d_err         error word or NULL
  * Whatever the rows behind the deciding one hold does not enter.  A sequence whose rows are out of range, or which meets a token or
  * number out of range, logits with NaN or +infinity, or with nothing above -infinity, gets -1, -1 and flags DEVICE_INPUT.
- * Which draft is accepted and which token drawn follows from sums with a relative error of about 2^-40, whatever the logits' type; the log
+ * Which draft is accepted and which token drawn follows from sums with a relative error of 2^-34 at most (2^-40 as a rule), whatever the logits' type; the log
  * probabilities are off by some 10^-6.  The same call gives the same bits.
  *   d_ws          adept_verify_workspace(n_rows) bytes on 16 bytes; calls that may overlap on the GPU need one each.  No
  *                 smaller call needs more.

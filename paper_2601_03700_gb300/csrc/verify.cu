@@ -21,6 +21,10 @@ constexpr float VS_HUGE = 1e6f;
 constexpr int VD_THREADS = 512, VD_CTAS = 16, VD_LOADS = 4;   // decision: threads of a CTA, CTAs of a sequence at most, loads of a thread under way
 constexpr int VD_LEAST = 20;                     // max(p - q, 0) sums to less than 2^-this: the token is drawn from p
 constexpr int VD_FINE = 14;                      // to less than 2^-this: summed token by token
+constexpr float VD_NEAR = 3.814697265625e-06f;   // 2^-18: p and q nearer than this may be taken for either above the other
+constexpr float VD_SURE = 5.820766091346741e-11f;   // 2^-34: what that may make of the sum, else those tokens are looked at again
+constexpr int VD_NEARS = 64;                     // as many as a CTA remembers; with more, the sum is taken token by token
+constexpr long long VD_NOTHING = 1 << 14;        // of the sums' 2^-58: what rounding leaves of nothing
 constexpr int VD_TAB = 64;
 
 // Difference of the logarithms of a test's two sides below which 32-bit sums do not decide it.  A sum's error: a thread's
@@ -410,7 +414,8 @@ struct Row {
   Two rho;            // sum of p's weights / sum of q's
   int certain;        // the draft that has all of q (-1: none)
   int plain;          // w = p
-  // Tokens k0, k0 + 32, .. below k1, two at a time: f(k, p's logits of k and k + 32, q's), -infinity past the end; several loads under way.
+  // Tokens k0, k0 + 32, .. below k1, VD_LOADS at a time, whose loads are under way together: f(first of them, p's logits, q's), -infinity
+  // past the end.
   template <typename F>
   __device__ __forceinline__ void each(int k0, int k1, F f) const {
     for (int k = k0; k < k1; k += 32 * VD_LOADS) {
@@ -421,44 +426,93 @@ struct Row {
         x[j] = i < k1 ? to_f<TT>(p[i]) : -INFINITY;
         y[j] = q && i < k1 ? to_f<TD>(q[i]) : -INFINITY;
       }
-#pragma unroll
-      for (int j = 0; j < VD_LOADS; j += 2) f(k + 32 * j, x[j], x[j + 1], y[j], y[j + 1]);
+      f(k, x, y);
     }
   }
-  // max(p_i - q_i, 0) of tokens i, i + 32 from the logits, times the sum of p's weights
+  // p - q of two tokens from the logits, times the sum of p's weights
+  __device__ __forceinline__ TwoPair gap(float x0, float x1, float y0, float y1, const VdTab& tab) const {
+    const TwoPair a = weights(x0, x1, mp, c, tab), b = weights(y0, y1, mq, c, tab);
+    const Pair ph = mul2(same(-rho.h), b.h), pl = add2(fma2(same(-rho.h), b.h, mul2(ph, same(-1.f))), fma2(same(-rho.h), b.l, mul2(same(-rho.l), b.h)));
+    const TwoPair d = sum_of(a.h, ph);
+    const Pair e = add2(d.l, add2(a.l, pl)), s = add2(d.h, e);
+    return TwoPair{s, sub2(e, sub2(s, d.h))};
+  }
+  // what tokens i and i + 32 are drawn with: max(p - q, 0)
   __device__ __forceinline__ TwoPair residual(int i, float x0, float x1, float y0, float y1, const VdTab& tab) const {
-    TwoPair a = weights(x0, x1, mp, c, tab);
-    if (plain) return a;
-    float2 h, l;
-    if (q) {
-      const TwoPair b = weights(y0, y1, mq, c, tab);
-      const Pair ph = mul2(same(-rho.h), b.h), pl = add2(fma2(same(-rho.h), b.h, mul2(ph, same(-1.f))), fma2(same(-rho.h), b.l, mul2(same(-rho.l), b.h)));
-      const TwoPair d = sum_of(a.h, ph);
-      const Pair e = add2(d.l, add2(a.l, pl)), s = add2(d.h, e);
-      h = both(s);
-      l = both(sub2(e, sub2(s, d.h)));
-      if (!(h.x > 0.f)) h.x = l.x = 0.f;
-      if (!(h.y > 0.f)) h.y = l.y = 0.f;
-    } else {
-      h = both(a.h);
-      l = both(a.l);
-      if (i == certain) h.x = l.x = 0.f;
-      if (i + 32 == certain) h.y = l.y = 0.f;
-    }
+    if (plain) return weights(x0, x1, mp, c, tab);
+    const TwoPair d = q ? gap(x0, x1, y0, y1, tab) : weights(x0, x1, mp, c, tab);
+    float2 h = both(d.h), l = both(d.l);
+    if (q ? !(h.x > 0.f) : i == certain) h.x = l.x = 0.f;
+    if (q ? !(h.y > 0.f) : i + 32 == certain) h.y = l.y = 0.f;
     return TwoPair{pair(h.x, h.y), pair(l.x, l.y)};
   }
 };
 
+// The warp's sum of tokens k0 .. k1 - 1's residuals.
+template <typename TT, typename TD>
+__device__ __forceinline__ long long residual_sum(const Row<TT, TD>& row, int k0, int k1, float unit, const VdTab& tab) {
+  SumPair sw;
+  row.each(k0 + (threadIdx.x & 31), k1, [&](int k, const float (&x)[VD_LOADS], const float (&y)[VD_LOADS]) {
+#pragma unroll
+    for (int j = 0; j < VD_LOADS; j += 2) sw.add(row.residual(k + 32 * j, x[j], x[j + 1], y[j], y[j + 1], tab));
+  });
+  return warp_sum(whole(sw.value(), unit));
+}
+// (for what seldom runs, out of the kernel's way)
+template <typename TT, typename TD>
+__device__ __noinline__ long long residual_sum_seldom(Row<TT, TD> row, int k0, int k1, float unit, const VdTab& tab) {
+  return residual_sum(row, k0, k1, unit, tab);
+}
+// The token among k0 .. k1 - 1 with which the sum, `sum` before them, passes `at`; else the last with a weight (what rounding leaves), or -1.
+template <typename TT, typename TD>
+__device__ __forceinline__ int walk(const Row<TT, TD>& row, int k0, int k1, long long sum, long long at, float unit, const VdTab& tab) {
+  const int lane = threadIdx.x & 31;
+  int token = -1;
+  for (; k0 < k1; k0 += 32) {
+    const int k = k0 + lane;
+    const bool in = k < k1;
+    const Two v = row.residual(k, in ? to_f<TT>(row.p[k]) : -INFINITY, -INFINITY, in && row.q ? to_f<TD>(row.q[k]) : -INFINITY, -INFINITY, tab).first();
+    const long long w = in ? whole(v, unit) : 0;
+    long long inc = w;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const long long u = __shfl_up_sync(0xffffffffu, inc, o);
+      if (lane >= o) inc += u;
+    }
+    const unsigned over = __ballot_sync(0xffffffffu, w > 0 && sum + inc > at), some = __ballot_sync(0xffffffffu, w > 0);
+    if (over) return k0 + __ffs(over) - 1;
+    if (some) token = k0 + 31 - __clz(some);
+    sum += __shfl_sync(0xffffffffu, inc, 31);
+  }
+  return token;
+}
+// A token whose p is next to its q: what the sum of p's above q, less q's there, has to be mended by (0: it was on its side).
+template <typename TT, typename TD>
+__device__ __noinline__ long long mend(Row<TT, TD> row, int k, float rho32, float unit, const VdTab& tab) {
+  const float x = to_f<TT>(row.p[k]), y = to_f<TD>(row.q[k]);
+  const bool above = __fmaf_rn(both(weights(y, y, row.mq, row.c, tab).h).x, -rho32, both(weights(x, x, row.mp, row.c, tab).h).x) > 0.f;
+  const Two d = row.gap(x, x, y, y, tab).first();
+  return above == (d.h > 0.f) ? 0 : whole(d.h > 0.f ? d : Two{-d.h, -d.l}, unit);
+}
+
 template <typename TT, typename TD>
 __global__ void __launch_bounds__(VD_THREADS) verify_decide_kernel(VerifyCall a, int parts, const Stat* stats) {
   constexpr int WARPS = VD_THREADS / 32;
-  static_assert(WARPS >= 4 && WARPS <= 32 && VD_CTAS <= 32, "sums and run_of by a warp");
+  static_assert(WARPS >= 5 && WARPS <= 32 && VD_CTAS <= 32, "sums and run_of by a warp");
   __shared__ VdTab tab;
   __shared__ int s_first;
   __shared__ float4 s_row;   // maximum and sum of the row in question, the target's and the draft's
-  // sums of the ranks and of this CTA's warps: p's weights, q's, those of p where p is above q, those of q there; what is drawn from
-  __shared__ long long s_part[5][VD_CTAS], s_warp[5][WARPS], s_piece[WARPS];
+  // sums of the ranks and of this CTA's warps: p's weights, q's, those of p where p is above q, those of q there, those of q next to p; what
+  // is drawn from
+  enum { OF_P, OF_Q, P_ABOVE, Q_ABOVE, Q_NEAR, DRAWN, MENDED, SUMS };
+  __shared__ int s_near[VD_NEARS], s_nears;   // tokens with p next to q, and how many there are
+  __shared__ unsigned long long s_mend;
+  __shared__ long long s_at;   // the draw's number in the sum of what is drawn from
+  __shared__ int s_how;
+  __shared__ Two s_rho;
+  __shared__ long long s_part[SUMS][VD_CTAS], s_warp[SUMS][WARPS], s_piece[WARPS];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, rank = cluster_rank(), ctas = cluster_size(), b = (int)blockIdx.x / ctas;
+  if (tid == 0) s_mend = s_nears = 0;
   if (tid < VD_TAB) {
     tab.h[tid] = VD_POW[tid].x;
     tab.l[tid] = VD_POW[tid].y;
@@ -579,6 +633,7 @@ __global__ void __launch_bounds__(VD_THREADS) verify_decide_kernel(VerifyCall a,
   };
   auto total = [&](const long long* part) { return warp_sum(lane < ctas ? part[lane] : 0); };
   float unit = 0.f, unit_q = 0.f;
+  float rho32 = 0.f;   // Zp / Zq by the 32-bit sums
   long long zp = 0, zq = 0;
   auto look = [&](int r) {   // precise sums of row r: the warps' in s_warp, the ranks' in s_part
     const float4 st = s_row;
@@ -591,32 +646,61 @@ __global__ void __launch_bounds__(VD_THREADS) verify_decide_kernel(VerifyCall a,
     SumPair sp;
     if (row.q) {
       SumPair sq, above_p, above_q;
-      const float rho = __fdividef(st.y, st.w);
-      row.each(w0 + lane, w1, [&](int, float x0, float x1, float y0, float y1) {
-        TwoPair p = weights(x0, x1, row.mp, row.c, tab), d = weights(y0, y1, row.mq, row.c, tab);
-        sp.add(p);
-        sq.add(d);
-        const float2 ph = both(p.h), dh = both(d.h);
-        const Pair in = pair(ph.x > rho * dh.x ? 1.f : 0.f, ph.y > rho * dh.y ? 1.f : 0.f);
-        above_p.add(TwoPair{mul2(p.h, in), mul2(p.l, in)});
-        above_q.add(TwoPair{mul2(d.h, in), mul2(d.l, in)});
+      float near = 0.f;
+      rho32 = __fdividef(st.y, st.w);
+      row.each(w0 + lane, w1, [&](int k, const float (&x)[VD_LOADS], const float (&y)[VD_LOADS]) {
+        bool by[VD_LOADS], any = false;
+        float qh[VD_LOADS];
+#pragma unroll
+        for (int j = 0; j < VD_LOADS; j += 2) {
+          const TwoPair p = weights(x[j], x[j + 1], row.mp, row.c, tab), d = weights(y[j], y[j + 1], row.mq, row.c, tab);
+          sp.add(p);
+          sq.add(d);
+          const float2 g = both(fma2(d.h, same(-rho32), p.h)), lim = both(mul2(p.h, same(VD_NEAR))), dh = both(d.h);
+          const Pair in = pair(g.x > 0.f ? 1.f : 0.f, g.y > 0.f ? 1.f : 0.f);
+          above_p.add(TwoPair{mul2(p.h, in), mul2(p.l, in)});
+          above_q.add(TwoPair{mul2(d.h, in), mul2(d.l, in)});
+          by[j] = fabsf(g.x) < lim.x;
+          by[j + 1] = fabsf(g.y) < lim.y;
+          any |= by[j] || by[j + 1];
+          qh[j] = dh.x;
+          qh[j + 1] = dh.y;
+        }
+        if (any) {
+#pragma unroll
+          for (int j = 0; j < VD_LOADS; ++j)
+            if (by[j]) {
+              near += qh[j];
+              const int at = atomicAdd(&s_nears, 1);
+              if (at < VD_NEARS) s_near[at] = k + 32 * j;
+            }
+        }
       });
-      const long long v1_ = warp_sum(whole(sq.value(), unit_q)), v2 = warp_sum(whole(above_p.value(), unit)), v3 = warp_sum(whole(above_q.value(), unit_q));
+      const long long of_q = warp_sum(whole(sq.value(), unit_q)), p_above = warp_sum(whole(above_p.value(), unit)),
+                      q_above = warp_sum(whole(above_q.value(), unit_q)), q_near = warp_sum(whole(Two{near, 0.f}, unit_q));
       if (lane == 0) {
-        s_warp[1][warp] = v1_;
-        s_warp[2][warp] = v2;
-        s_warp[3][warp] = v3;
+        s_warp[OF_Q][warp] = of_q;
+        s_warp[P_ABOVE][warp] = p_above;
+        s_warp[Q_ABOVE][warp] = q_above;
+        s_warp[Q_NEAR][warp] = q_near;
       }
     } else {
-      row.each(w0 + lane, w1, [&](int, float x0, float x1, float, float) { sp.add(weights(x0, x1, row.mp, row.c, tab)); });
+      row.each(w0 + lane, w1, [&](int, const float (&x)[VD_LOADS], const float (&)[VD_LOADS]) {
+#pragma unroll
+        for (int j = 0; j < VD_LOADS; j += 2) sp.add(weights(x[j], x[j + 1], row.mp, row.c, tab));
+      });
     }
-    const long long v0_ = warp_sum(whole(sp.value(), unit));
-    if (lane == 0) s_warp[0][warp] = v0_;
+    const long long of_p = warp_sum(whole(sp.value(), unit));
+    if (lane == 0) s_warp[OF_P][warp] = of_p;
     __syncthreads();
-    if (warp < (row.q ? 4 : 1)) exchange(s_warp[warp], s_part[warp]);
+    if (row.q && warp == Q_NEAR && s_nears > VD_NEARS) {   // (a sum that says so)
+      if (lane == 0) s_warp[Q_NEAR][0] = 1ll << 58;
+      __syncwarp();
+    }
+    if (warp < (row.q ? DRAWN : OF_Q)) exchange(s_warp[warp], s_part[warp]);
     cluster_barrier();
-    zp = total(s_part[0]);
-    if (row.q) zq = total(s_part[1]);
+    zp = total(s_part[OF_P]);
+    if (row.q) zq = total(s_part[OF_Q]);
   };
   int looked = -1;
   // drafts that are too close: decided by the precise sums, in 64 bits
@@ -635,6 +719,7 @@ __global__ void __launch_bounds__(VD_THREADS) verify_decide_kernel(VerifyCall a,
       break;
     }
     first_from(i + 1, i, code);
+    if (tid == 0) s_nears = 0;
     cluster_barrier();   // (the sums of that row have been read: s_part is free)
   }
   if (code == BAD || (!greedy && !(a.u[q.e - 1] >= 0.f && a.u[q.e - 1] < 1.f))) {
@@ -659,58 +744,82 @@ __global__ void __launch_bounds__(VD_THREADS) verify_decide_kernel(VerifyCall a,
   if (looked != r) look(r);
   row.certain = soft || r == q.e - 1 ? -1 : a.tokens[r + 1];
   row.plain = r == q.e - 1;
-  // what is drawn from: its sum, the ranks' and this CTA's warps'
-  const long long *by_rank = s_part[0], *by_warp = s_warp[0];
-  long long all = zp;
-  if (!row.plain) {
-    if (row.q) {
-      // sum of max(p - q, 0) = that of p where p is above q, less that of q there.  "Above" went by the 32-bit sums: tokens with p and q within
-      // 10^-6 of each other may be on the wrong side, by that much of themselves
+  // What is drawn from: its sum, the ranks' and this CTA's warps'.  One warp settles it (conversions of 64 bits run at a few a cycle and SM).
+  enum { PLAIN = 0, RESIDUAL = 1, WRONG_SIDES = 2, BY_TOKEN = 3 };
+  auto settle = [&](long long all) {   // by all lanes of the warp: the sum and the draw's number in it
+    const bool fall_back = !row.plain && all < zp >> VD_LEAST;
+    const long long sum = fall_back ? zp : all;
+    // u in the middle of its 2^-24, times the sum
+    s_at = (long long)__umul64hi(__float2ull_rz(a.u[q.e - 1] * 18446744073709551616.f) + (1ull << 39), (unsigned long long)sum);
+    return row.plain || fall_back ? PLAIN : RESIDUAL;
+  };
+  if (row.plain) {
+    if (warp == 0) s_how = settle(zp);
+  } else if (row.q) {
+    // sum of max(p - q, 0) = that of p where p is above q, less that of q there.  "Above" went by the 32-bit sums' quotient: a token whose p
+    // and q are nearer than that is off may be on the wrong side, which changes the sum by that much of its q
+    if (warp == 0) {
       const Two rho = quotient(two_of(zp), two_of(zq));   // in p's units over q's
+      const float by = __int_as_float(0x3f800000 + __float_as_int(unit_q) - __float_as_int(unit));
+      const float off = fabsf(rho32 - rho.h * by) / (rho.h * by) + 2.384185791015625e-07f;   // (and the comparison's roundings)
       auto rest = [&](long long above_p, long long above_q) {
         const Two x = rho * two_of(above_q);
-        return max(above_p - __float2ll_rn(x.h) - __float2ll_rn(x.l), 0ll);
+        const long long v = above_p - __float2ll_rn(x.h) - __float2ll_rn(x.l);
+        return v < VD_NOTHING ? 0ll : v;
       };
-      if (warp == 0) {
-        if (lane < WARPS) s_warp[4][lane] = rest(s_warp[2][lane], s_warp[3][lane]);
-        if (lane < ctas) s_part[4][lane] = rest(s_part[2][lane], s_part[3][lane]);
-      }
-      const float by = __int_as_float(0x3f800000 + __float_as_int(unit_q) - __float_as_int(unit));
-      row.rho = Two{rho.h * by, rho.l * by};
-      __syncthreads();
-      all = total(s_part[4]);
-      if (all < zp >> VD_FINE) {   // little is left of p: token by token
-        SumPair sw;
-        row.each(w0 + lane, w1, [&](int k, float x0, float x1, float y0, float y1) { sw.add(row.residual(k, x0, x1, y0, y1, tab)); });
-        const long long vw = warp_sum(whole(sw.value(), unit));
-        __syncthreads();   // (s_part[4] has been read)
-        if (lane == 0) s_warp[4][warp] = vw;
-        cluster_barrier();
-        if (warp == 0) exchange(s_warp[4], s_part[4]);
-        cluster_barrier();
-        all = total(s_part[4]);
-      }
-    } else {   // all of p but the draft
-      const int x = row.certain, at_rank = x / share, at_warp = (x - at_rank * share) / each;
-      const long long wx = whole(weights(drafted_at(0, r), -INFINITY, row.mp, row.c, tab).first(), unit);
-      auto rest = [&](long long v, bool has) { return has ? (v - wx < 256 ? 0ll : v - wx) : v; };   // (256: what rounding leaves)
-      if (warp == 0) {
-        if (lane < WARPS) s_warp[4][lane] = rest(s_warp[0][lane], rank == at_rank && lane == at_warp);
-        if (lane < ctas) s_part[4][lane] = rest(s_part[0][lane], lane == at_rank);
-      }
-      __syncthreads();
-      all = total(s_part[4]);
+      if (lane < WARPS) s_warp[DRAWN][lane] = rest(s_warp[P_ABOVE][lane], s_warp[Q_ABOVE][lane]);
+      const long long part = lane < ctas ? rest(s_part[P_ABOVE][lane], s_part[Q_ABOVE][lane]) : 0;
+      if (lane < ctas) s_part[DRAWN][lane] = part;
+      const long long all = warp_sum(part), q_near = total(s_part[Q_NEAR]);
+      s_rho = Two{rho.h * by, rho.l * by};
+      if (all < zp >> VD_FINE || off > VD_NEAR || q_near >= 1ll << 58)
+        s_how = BY_TOKEN;
+      else if (off * rho.h * __ll2float_rn(q_near) > VD_SURE * __ll2float_rn(all))
+        s_how = WRONG_SIDES;
+      else
+        s_how = settle(all);
     }
-    row.plain = all < zp >> VD_LEAST;
-    if (!row.plain) {
-      by_rank = s_part[4];
-      by_warp = s_warp[4];
-    } else {
-      all = zp;
+    __syncthreads();
+    row.rho = s_rho;
+    const int how = s_how;
+    if (how >= WRONG_SIDES) {   // (uniform over the cluster)
+      if (how == BY_TOKEN) {
+        const long long vw = residual_sum_seldom(row, w0, w1, unit, tab);
+        if (lane == 0) s_warp[DRAWN][warp] = vw;
+        cluster_barrier();   // (and every CTA has read its s_part)
+        if (warp == 0) exchange(s_warp[DRAWN], s_part[DRAWN]);
+      } else {
+        if (tid < s_nears) {
+          const int k = s_near[tid];
+          const unsigned long long more = (unsigned long long)mend(row, k, rho32, unit, tab);
+          if (more) {
+            atomicAdd(reinterpret_cast<unsigned long long*>(&s_warp[DRAWN][(k - v0) / each]), more);
+            atomicAdd(&s_mend, more);
+          }
+        }
+        __syncthreads();
+        if (tid < ctas) cluster_store(&s_part[MENDED][rank], tid, (long long)s_mend);
+      }
+      cluster_barrier();
+      if (warp == 0) {
+        if (how == WRONG_SIDES && lane < ctas) s_part[DRAWN][lane] += s_part[MENDED][lane];
+        __syncwarp();
+        s_how = settle(total(s_part[DRAWN]));
+      }
     }
+  } else if (warp == 0) {   // all of p but the draft
+    const int x = row.certain, at_rank = x / share, at_warp = (x - at_rank * share) / each;
+    const long long wx = whole(weights(drafted_at(0, r), -INFINITY, row.mp, row.c, tab).first(), unit);
+    auto rest = [&](long long v, bool has) { return has ? (v - wx < VD_NOTHING ? 0ll : v - wx) : v; };
+    if (lane < WARPS) s_warp[DRAWN][lane] = rest(s_warp[OF_P][lane], rank == at_rank && lane == at_warp);
+    const long long part = lane < ctas ? rest(s_part[OF_P][lane], lane == at_rank) : 0;
+    if (lane < ctas) s_part[DRAWN][lane] = part;
+    s_how = settle(warp_sum(part));
   }
-  // u in the middle of its 2^-24, times the sum
-  const long long at = (long long)__umul64hi(__float2ull_rz(a.u[q.e - 1] * 18446744073709551616.f) + (1ull << 39), (unsigned long long)all);
+  __syncthreads();
+  row.plain = s_how == PLAIN;
+  const long long at = s_at;
+  const long long *by_rank = s_part[row.plain ? OF_P : DRAWN], *by_warp = s_warp[row.plain ? OF_P : DRAWN];
   // the run in which the sum passes `at`: the last of those that hold something and begin at or below it (by a warp)
   long long before = 0;
   auto run_of = [&](const long long* v, int n_runs) {
@@ -732,36 +841,17 @@ __global__ void __launch_bounds__(VD_THREADS) verify_decide_kernel(VerifyCall a,
   const int ow = run_of(by_warp, WARPS);
   const int r0 = min(v1, v0 + ow * each), r1 = min(v1, r0 + each), piece = ((each + WARPS - 1) / WARPS + 31) & ~31;
   const int p0 = min(r1, r0 + warp * piece), p1 = min(r1, p0 + piece);
-  SumPair sw;
-  row.each(p0 + lane, p1, [&](int k, float x0, float x1, float y0, float y1) { sw.add(row.residual(k, x0, x1, y0, y1, tab)); });
-  const long long vw = warp_sum(whole(sw.value(), unit));
+  const long long vw = residual_sum(row, p0, p1, unit, tab);
   if (lane == 0) s_piece[warp] = vw;
   __syncthreads();
   if (warp != run_of(s_piece, WARPS)) return;
-  int token = -1;   // the last one with a weight so far: what rounding leaves
-  for (int k0 = p0; k0 < p1; k0 += 32) {
-    const int k = k0 + lane;
-    const bool in = k < p1;
-    const Two v = row.residual(k, in ? to_f<TT>(row.p[k]) : -INFINITY, -INFINITY, in && row.q ? to_f<TD>(row.q[k]) : -INFINITY, -INFINITY, tab).first();
-    const long long w = in ? whole(v, unit) : 0;
-    long long inc = w;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const long long u = __shfl_up_sync(0xffffffffu, inc, o);
-      if (lane >= o) inc += u;
-    }
-    const unsigned over = __ballot_sync(0xffffffffu, w > 0 && before + inc > at), some = __ballot_sync(0xffffffffu, w > 0);
-    if (over) {
-      token = k0 + __ffs(over) - 1;
-      break;
-    }
-    if (some) token = k0 + 31 - __clz(some);
-    before += __shfl_sync(0xffffffffu, inc, 31);
-  }
-  if (lane == 0 && token >= 0) {   // (the run holds something)
+  int token = -1;
+  for (int again = 0; again < 2 && token < 0; ++again)   // (again: a run of tokens with p next to q, on the wrong sides; odds of 2^-34)
+    token = again ? walk(row, 0, a.vocab, 0, at, unit, tab) : walk(row, p0, p1, before, at, unit, tab);
+  if (lane == 0) {
     a.accepted[b] = i;
     a.next[b] = token;
-    if (a.logprob) a.logprob[r] = log_share(to_f<TT>(row.p[token]), row.mp, __ll2float_rn(zp) / unit);
+    if (a.logprob) a.logprob[r] = log_share(to_f<TT>(row.p[max(token, 0)]), row.mp, __ll2float_rn(zp) / unit);
   }
 }
 

@@ -335,3 +335,44 @@ def test_a_larger_calls_workspace_serves_a_smaller_call():
         c = make(drafts, vocab, 49)
         want = call(c)
         assert all(torch.equal(a, b) for a, b in zip(call(c, ws=ws), want))
+
+
+@pytest.mark.parametrize("noise", [0.0, 1e-7, 1e-6, 1e-5])
+@pytest.mark.parametrize("share", [0.5, 0.98])
+def test_tokens_that_both_give_nearly_the_same(noise, share):
+    """Most tokens with the same probability in target and draft, but for noise of the order of fp32's steps, the others exchanged in
+    pairs (so that both sums are the same): which side a token is on hangs on the sums' last bits."""
+    B, V = 48, 20002
+    g = torch.Generator().manual_seed(60)
+    t = (2.0 * torch.randn(B * 2, V, generator=g)).double()
+    d = t.clone()
+    n = int(V * (1 - share)) // 2 * 2
+    d[:, 0:n:2], d[:, 1:n:2] = t[:, 1:n:2], t[:, 0:n:2]
+    d[:, n:] += noise * torch.randn(B * 2, V - n, generator=g)
+    t, d = t.float(), d.float()
+    # drafts that the draft gives much more than the target
+    x = (torch.log_softmax(d[0::2], 1) - torch.log_softmax(t[0::2], 1)).argmax(1)
+    tokens = torch.stack([torch.zeros(B, dtype=torch.int64), x], 1).reshape(-1).int()
+    c = dict(target=t.cuda(), draft=d.cuda(), tokens=tokens, start=list(range(0, 2 * B + 1, 2)), u=torch.rand(2 * B, generator=g))
+    acc, _ = check(c)
+    assert acc.count(0) > B // 2
+    check(c, [0.6] * B)
+
+
+@pytest.mark.parametrize("noise", [1e-7, 3e-7, 1e-6])
+def test_few_tokens_that_both_give_nearly_the_same(noise):
+    """Twelve tokens that hold half of both distributions, in the same ratio to each other but for that noise, before 400000 small ones
+    whose borders lie 10^-6 apart: the twelve move the drawn token where they are counted on the wrong side."""
+    B, V = 16, 400000
+    g = torch.Generator().manual_seed(61)
+    t = torch.randn(B * 2, V, generator=g).double()
+    d = t.clone()
+    d[:, 0::2], d[:, 1::2] = t[:, 1::2], t[:, 0::2]
+    big = torch.logsumexp(t, 1, keepdim=True) - math.log(12) + 0.1 * torch.randn(B * 2, 12, generator=g).double()
+    t[:, :12], d[:, :12] = big, big + noise * torch.randn(B * 2, 12, generator=g)
+    t, d = t.float(), d.float()
+    x = (torch.log_softmax(d[0::2], 1) - torch.log_softmax(t[0::2], 1)).argmax(1)
+    tokens = torch.stack([torch.zeros(B, dtype=torch.int64), x], 1).reshape(-1).int()
+    c = dict(target=t.cuda(), draft=d.cuda(), tokens=tokens, start=list(range(0, 2 * B + 1, 2)), u=torch.rand(2 * B, generator=g))
+    acc, _ = check(c)
+    assert acc.count(0) > B // 2
