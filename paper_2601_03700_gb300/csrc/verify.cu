@@ -4,10 +4,13 @@
 // tokens[r + 1] holds where log u_r + log q_r(x) < log p_r(x); at the first row whose draft does not, the next token is drawn from
 // max(p_r - q_r, 0), at the last row from p_r.
 //
-// Two launches.  The first streams every row once (HBM-bound) and leaves its maximum, the sum of exp((l - max) / T) and the
-// first index of the maximum.  The second, a cluster per sequence, decides.  Sums of 32 bits decide a draft unless the two
-// sides are closer than their errors (close_of); those, and the drawing, go by weights of two 32-bit parts each (2^-40 relative):
-// with a vocabulary of V tokens the cumulative sum has V steps, and an error of 2^-24 would move the drawn token with odds of V 2^-23.
+// Two launches.  The first streams every row once, each in parts of a CTA, and leaves per part the maximum, the sum of exp((l - max) / T), the
+// maximum's first index (greedy sequences) and the draft's logit: HBM-bound, 437 MB at 6.1 TB/s (64 chunks of 8 drafts over 131072
+// tokens, fp32 and bf16).  The second, a cluster per sequence, decides.  Sums of 32 bits decide a draft unless the two sides are closer
+// than their errors (close_of); those, and the drawing, go by weights of two 32-bit parts each (2^-40 relative): with a vocabulary of
+// V tokens the cumulative sum has V steps, and an error of 2^-24 would move the drawn token with odds of V 2^-23.  It reads one row of
+// the target and one of the draft a sequence, most of it from L2, and is bound by the weights' arithmetic (about 40 operations a
+// weight) where there are many sequences, by the chain loads -> sums -> barrier -> sums where there are few.
 #include "cluster.cuh"
 #include "serve_ops.h"
 
@@ -18,7 +21,7 @@ namespace {
 
 constexpr int VS_THREADS = 128, VS_LOADS = 4, VS_PARTS = 8;   // statistics: 16-byte loads of a thread under way (twice), CTAs of a row at most
 constexpr float VS_HUGE = 1e6f;
-constexpr int VD_THREADS = 512, VD_CTAS = 16, VD_LOADS = 4;   // decision: threads of a CTA, CTAs of a sequence at most, loads of a thread under way
+constexpr int VD_THREADS = 512, VD_CTAS = 16, VD_LOADS = 2;   // decision: threads of a CTA, CTAs of a sequence at most, tokens of a thread at a time
 constexpr int VD_LEAST = 20;                     // max(p - q, 0) sums to less than 2^-this: the token is drawn from p
 constexpr int VD_FINE = 14;                      // to less than 2^-this: summed token by token
 constexpr float VD_NEAR = 3.814697265625e-06f;   // 2^-18: p and q nearer than this may be taken for either above the other
@@ -414,19 +417,29 @@ struct Row {
   Two rho;            // sum of p's weights / sum of q's
   int certain;        // the draft that has all of q (-1: none)
   int plain;          // w = p
-  // Tokens k0, k0 + 32, .. below k1, VD_LOADS at a time, whose loads are under way together: f(first of them, p's logits, q's), -infinity
-  // past the end.
+  // Tokens k0, k0 + 32, .. below k1, VD_LOADS at a time: f(first of them, p's logits, q's), -infinity past the end.  The next ones' loads are
+  // under way meanwhile (64 chunks over 131072 tokens: 122 -> 120 us; four at a time 116, but one chunk over 50257 15.0 -> 15.7).
   template <typename F>
   __device__ __forceinline__ void each(int k0, int k1, F f) const {
-    for (int k = k0; k < k1; k += 32 * VD_LOADS) {
-      float x[VD_LOADS], y[VD_LOADS];
+    auto load = [&](int k, float (&x)[VD_LOADS], float (&y)[VD_LOADS]) {
 #pragma unroll
       for (int j = 0; j < VD_LOADS; ++j) {
         const int i = k + 32 * j;
         x[j] = i < k1 ? to_f<TT>(p[i]) : -INFINITY;
         y[j] = q && i < k1 ? to_f<TD>(q[i]) : -INFINITY;
       }
+    };
+    float x[VD_LOADS], y[VD_LOADS];
+    if (k0 < k1) load(k0, x, y);
+    for (int k = k0; k < k1; k += 32 * VD_LOADS) {
+      float u[VD_LOADS], v[VD_LOADS];
+      load(k + 32 * VD_LOADS, u, v);
       f(k, x, y);
+#pragma unroll
+      for (int j = 0; j < VD_LOADS; ++j) {
+        x[j] = u[j];
+        y[j] = v[j];
+      }
     }
   }
   // p - q of two tokens from the logits, times the sum of p's weights
