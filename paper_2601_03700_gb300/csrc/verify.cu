@@ -525,7 +525,10 @@ __global__ void __launch_bounds__(VD_THREADS) verify_decide_kernel(VerifyCall a,
   __shared__ Two s_rho;
   __shared__ long long s_part[SUMS][VD_CTAS], s_warp[SUMS][WARPS], s_piece[WARPS];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, rank = cluster_rank(), ctas = cluster_size(), b = (int)blockIdx.x / ctas;
-  if (tid == 0) s_mend = s_nears = 0;
+  if (tid == 0) {
+    s_mend = 0;
+    s_nears = 0;
+  }
   if (tid < VD_TAB) {
     tab.h[tid] = VD_POW[tid].x;
     tab.l[tid] = VD_POW[tid].y;
@@ -669,7 +672,8 @@ __global__ void __launch_bounds__(VD_THREADS) verify_decide_kernel(VerifyCall a,
           const TwoPair p = weights(x[j], x[j + 1], row.mp, row.c, tab), d = weights(y[j], y[j + 1], row.mq, row.c, tab);
           sp.add(p);
           sq.add(d);
-          const float2 g = both(fma2(d.h, same(-rho32), p.h)), lim = both(mul2(p.h, same(VD_NEAR))), dh = both(d.h);
+          // (less 10^-36: masked tokens, and those past the end, are next to nothing)
+          const float2 g = both(fma2(d.h, same(-rho32), p.h)), lim = both(fma2(p.h, same(VD_NEAR), same(-1e-36f))), dh = both(d.h);
           const Pair in = pair(g.x > 0.f ? 1.f : 0.f, g.y > 0.f ? 1.f : 0.f);
           above_p.add(TwoPair{mul2(p.h, in), mul2(p.l, in)});
           above_q.add(TwoPair{mul2(d.h, in), mul2(d.l, in)});

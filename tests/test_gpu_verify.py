@@ -376,3 +376,22 @@ def test_few_tokens_that_both_give_nearly_the_same(noise):
     c = dict(target=t.cuda(), draft=d.cuda(), tokens=tokens, start=list(range(0, 2 * B + 1, 2)), u=torch.rand(2 * B, generator=g))
     acc, _ = check(c)
     assert acc.count(0) > B // 2
+
+
+def test_masked_tokens_where_both_sums_are_the_same():
+    """Target and draft with the same sum of weights, and thousands of tokens masked in both: those are next to each other in p and q, but
+    nothing of either; vocabularies that end within a warp's tokens."""
+    for V in (4099, 20011):
+        g = torch.Generator().manual_seed(V)
+        B = 24
+        t = 2.0 * torch.randn(2 * B, V, generator=g)
+        t[:, torch.rand(V, generator=g) < 0.6] = -math.inf
+        keep = (t[0] > -math.inf).nonzero()[:, 0]
+        keep = keep[:len(keep) // 2 * 2]
+        d = t.clone()
+        d[:, keep[0::2]], d[:, keep[1::2]] = t[:, keep[1::2]], t[:, keep[0::2]]
+        x = (torch.log_softmax(d[0::2][:, keep], 1) - torch.log_softmax(t[0::2][:, keep], 1)).argmax(1)
+        tokens = torch.stack([torch.zeros(B, dtype=torch.int64), keep[x]], 1).reshape(-1).int()
+        c = dict(target=t.cuda(), draft=d.cuda(), tokens=tokens, start=list(range(0, 2 * B + 1, 2)), u=torch.rand(2 * B, generator=g))
+        acc, nxt = check(c)
+        assert acc.count(0) > B // 2 and all(i in keep for i in nxt)
