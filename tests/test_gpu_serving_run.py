@@ -123,3 +123,68 @@ def test_rounds_of_drafts(dtype):
         held(history)
         pages.check()
     assert total > 0
+
+
+def test_a_round_captured_and_replayed():
+    """A whole round whose lengths never leave the device (rows grown, chunk written and attended, verified, cut back), captured once and
+    replayed: the same bits as calls one by one."""
+    B, D, cols, blocks = 4, 3, 10, 48
+    n = B * (D + 1)
+    g = torch.Generator(device="cuda").manual_seed(9)
+    rnd = lambda *s: torch.randn(*s, generator=g, device="cuda")  # noqa: E731
+    emb, w_out = rnd(V, (H + 2 * HK), DH).bfloat16(), rnd(H * DH, V) / 16
+    drafts = [torch.randint(V, (B, D), generator=g, device="cuda", dtype=torch.int32) for _ in range(8)]
+    us = [torch.rand(n, generator=g, device="cuda") for _ in range(8)]
+
+    class State:
+        def __init__(self):
+            self.pages = adept.KVPages(blocks, B, cols, block_tokens=BT)
+            self.cache = adept.KVCache(blocks, HK, DH, B, cols, pages=self.pages)
+            self.layers = adept.KVLayers([self.cache])
+            self.len, self.tok = i32([0] * B), i32([[7, 0, 0, 0]] * B)
+            self.own, self.start = i32(list(range(B))), i32([b * (D + 1) for b in range(B + 1)])
+            self.seq = self.own.repeat_interleave(D + 1).contiguous()
+            self.got, self.src, self.dst, self.acc, self.nxt = (i32([0] * B) for _ in range(5))
+            self.draft, self.u = torch.zeros_like(drafts[0]), torch.zeros_like(us[0])
+            self.q, self.att = (torch.zeros(n, H, DH, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+            self.ws = [self.pages.workspace(), self.cache.attention_workspace(H, n, D + 1, cols * BT), adept.verify_workspace(n)]
+            self.logits = torch.zeros(n, V, device="cuda")
+
+        def round(self):
+            want = self.len + (D + 1)
+            adept.adept_kv_reserve(self.pages, self.len, want, self.got, self.src, self.dst, workspace=self.ws[0])
+            adept.adept_kv_copy_blocks(self.layers, self.src, self.dst)
+            self.tok[:, 1:] = self.draft
+            x = emb[self.tok.view(-1).long()]
+            pos = (self.len[:, None] + torch.arange(D + 1, device="cuda", dtype=torch.int32)).view(-1).contiguous()
+            adept.adept_kv_append(self.cache, x[:, H:H + HK], x[:, H + HK:], self.seq, pos)
+            self.q.copy_(x[:, :H])
+            adept.adept_chunk_attention(self.cache, self.q, self.start, want, D + 1, cols * BT, self.att, self.ws[1])
+            torch.matmul(self.att.float().view(n, -1), w_out, out=self.logits)
+            adept.adept_verify_drafts(self.logits, None, self.tok.view(-1), self.start, self.u, self.acc, self.nxt, workspace=self.ws[2],
+                                      err=self.pages.err)
+            self.len += 1 + self.acc
+            self.tok[:, 0] = self.nxt
+            adept.adept_kv_fork(self.pages, self.own, self.len, workspace=self.ws[0])
+
+        def all(self):
+            return [self.pages.state, self.cache.k, self.cache.v, self.len, self.tok, self.acc, self.nxt, self.logits]
+
+    one, two = State(), State()
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        State().round()
+    s.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        two.round()
+    for d, u in zip(drafts, us):
+        for st in (one, two):
+            st.draft.copy_(d)
+            st.u.copy_(u)
+        one.round()
+        graph.replay()
+        assert all(torch.equal(x, y) for x, y in zip(one.all(), two.all()))
+    one.pages.check()
+    two.pages.check()
+    assert int(one.len.max()) > 8 and int((one.pages.block_table >= 0).sum()) == sum(-(-int(x) // BT) for x in one.len)
