@@ -50,6 +50,31 @@ inline cudaError_t cluster16_once(K* kernel) {
   return e;
 }
 
+// Clusters of `ctas` CTAs of a kernel (no dynamic shared memory) that an idle GPU holds at once, asked for once (ctas: a power of two up to 16).
+template <typename Tag, typename K>
+inline int clusters_at_once(K* kernel, int ctas, int threads) {
+  static std::atomic<int> known[5];   // 0: not asked yet
+  int at = 0;
+  while (1 << at < ctas) ++at;
+  int n = known[at].load();
+  if (n > 0) return n;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)ctas);
+  cfg.blockDim = dim3((unsigned)threads);
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = (unsigned)ctas;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  if (cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess || n < 1) {
+    cudaGetLastError();
+    n = 1;
+  }
+  known[at].store(n);
+  return n;
+}
+
 template <typename... KArgs, typename... Args>
 inline cudaError_t launch_cluster(void (*kernel)(KArgs...), dim3 grid, int cluster, int block, size_t smem, cudaStream_t st, Args&&... args) {
   cudaLaunchConfig_t cfg = {};

@@ -897,13 +897,18 @@ cudaError_t verify_t(cudaStream_t st, const VerifyCall& a) {
     const cudaError_t e = launch_k(verify_stats_kernel<TT, TD>, dim3((unsigned)(a.n_rows * parts), a.draft ? 2 : 1), dim3(VS_THREADS), 0, st, a, parts, stats);
     if (e != cudaSuccess) return e;
   }
-  // A sequence gets the most CTAs (of an SM each) that leave all sequences room at once: 64 sequences of 131072 tokens took 117 us by 2
-  // CTAs each, 125 by 4, 129 by 8 smaller ones, three an SM; one sequence of 50257 tokens 13.5 by 16, 15.4 by 8.
+  // A sequence gets the most CTAs (of an SM each) whose clusters find room for all sequences at once, or nearly: 64 sequences of 131072 tokens took
+  // 117 us by 2 CTAs each, 125 by 4, 129 by 8 smaller ones, three an SM; one sequence of 50257 tokens 15.0 by 16 CTAs, 17.0 by 8; eight
+  // of 32000, of whose clusters of 16 seven find room, 19.7 by 16, 17.9 by 8; sixteen chunks of which one waits (some of them greedy,
+  // and done at once) 19.1 by 8, 21.2 by 4.
   struct Tag;
   const cudaError_t e = cluster16_once<Tag>(verify_decide_kernel<TT, TD>);
   if (e != cudaSuccess) return e;
   int ctas = VD_CTAS;
-  while (ctas > 1 && (long long)a.n_seq * ctas > verify_sms()) ctas /= 2;
+  for (; ctas > 1; ctas /= 2) {
+    const int n = clusters_at_once<Tag>(verify_decide_kernel<TT, TD>, ctas, VD_THREADS);
+    if (a.n_seq <= n + n / 8) break;
+  }
   return launch_cluster(verify_decide_kernel<TT, TD>, dim3((unsigned)(a.n_seq * ctas)), ctas, VD_THREADS, 0, st, a, parts, (const Stat*)stats);
 }
 
