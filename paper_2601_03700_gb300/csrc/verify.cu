@@ -21,7 +21,8 @@ namespace {
 
 constexpr int VS_THREADS = 128, VS_LOADS = 4, VS_PARTS = 8;   // statistics: 16-byte loads of a thread under way (twice), CTAs of a row at most
 constexpr float VS_HUGE = 1e6f;
-constexpr int VD_THREADS = 512, VD_CTAS = 16, VD_LOADS = 2;   // decision: threads of a CTA, CTAs of a sequence at most, tokens of a thread at a time
+constexpr int VD_THREADS = 512, VD_CTAS = 16;    // decision: threads of a CTA, CTAs of a sequence at most
+constexpr int VD_MANY = 32;                      // tokens a thread from which on it takes four at a time, else two
 constexpr int VD_LEAST = 20;                     // max(p - q, 0) sums to less than 2^-this: the token is drawn from p
 constexpr int VD_FINE = 14;                      // to less than 2^-this: summed token by token
 constexpr float VD_NEAR = 3.814697265625e-06f;   // 2^-18: p and q nearer than this may be taken for either above the other
@@ -408,7 +409,7 @@ __device__ __forceinline__ TwoPair weights(float l0, float l1, float m, const Sc
 }
 
 // The row that is looked at closely.
-template <typename TT, typename TD>
+template <typename TT, typename TD, int LOADS>
 struct Row {
   const TT* p;
   const TD* q;        // NULL: no draft distribution
@@ -417,26 +418,27 @@ struct Row {
   Two rho;            // sum of p's weights / sum of q's
   int certain;        // the draft that has all of q (-1: none)
   int plain;          // w = p
-  // Tokens k0, k0 + 32, .. below k1, VD_LOADS at a time: f(first of them, p's logits, q's), -infinity past the end.  The next ones' loads are
-  // under way meanwhile (64 chunks over 131072 tokens: 122 -> 120 us; four at a time 116, but one chunk over 50257 15.0 -> 15.7).
+  // Tokens k0, k0 + 32, .. below k1, LOADS at a time: f(first of them, p's logits, q's), -infinity past the end.  The next ones' loads are
+  // under way meanwhile.  Two at a time where a thread has few (one chunk over 50257 tokens, 6 a thread: 15.0 us, by four 15.7), four where it has
+  // many (64 chunks over 131072, 128 a thread: 116 us, by two 120).
   template <typename F>
   __device__ __forceinline__ void each(int k0, int k1, F f) const {
-    auto load = [&](int k, float (&x)[VD_LOADS], float (&y)[VD_LOADS]) {
+    auto load = [&](int k, float (&x)[LOADS], float (&y)[LOADS]) {
 #pragma unroll
-      for (int j = 0; j < VD_LOADS; ++j) {
+      for (int j = 0; j < LOADS; ++j) {
         const int i = k + 32 * j;
         x[j] = i < k1 ? to_f<TT>(p[i]) : -INFINITY;
         y[j] = q && i < k1 ? to_f<TD>(q[i]) : -INFINITY;
       }
     };
-    float x[VD_LOADS], y[VD_LOADS];
+    float x[LOADS], y[LOADS];
     if (k0 < k1) load(k0, x, y);
-    for (int k = k0; k < k1; k += 32 * VD_LOADS) {
-      float u[VD_LOADS], v[VD_LOADS];
-      load(k + 32 * VD_LOADS, u, v);
+    for (int k = k0; k < k1; k += 32 * LOADS) {
+      float u[LOADS], v[LOADS];
+      load(k + 32 * LOADS, u, v);
       f(k, x, y);
 #pragma unroll
-      for (int j = 0; j < VD_LOADS; ++j) {
+      for (int j = 0; j < LOADS; ++j) {
         x[j] = u[j];
         y[j] = v[j];
       }
@@ -462,23 +464,23 @@ struct Row {
 };
 
 // The warp's sum of tokens k0 .. k1 - 1's residuals.
-template <typename TT, typename TD>
-__device__ __forceinline__ long long residual_sum(const Row<TT, TD>& row, int k0, int k1, float unit, const VdTab& tab) {
+template <typename TT, typename TD, int LOADS>
+__device__ __forceinline__ long long residual_sum(const Row<TT, TD, LOADS>& row, int k0, int k1, float unit, const VdTab& tab) {
   SumPair sw;
-  row.each(k0 + (threadIdx.x & 31), k1, [&](int k, const float (&x)[VD_LOADS], const float (&y)[VD_LOADS]) {
+  row.each(k0 + (threadIdx.x & 31), k1, [&](int k, const float (&x)[LOADS], const float (&y)[LOADS]) {
 #pragma unroll
-    for (int j = 0; j < VD_LOADS; j += 2) sw.add(row.residual(k + 32 * j, x[j], x[j + 1], y[j], y[j + 1], tab));
+    for (int j = 0; j < LOADS; j += 2) sw.add(row.residual(k + 32 * j, x[j], x[j + 1], y[j], y[j + 1], tab));
   });
   return warp_sum(whole(sw.value(), unit));
 }
 // (for what seldom runs, out of the kernel's way)
-template <typename TT, typename TD>
-__device__ __noinline__ long long residual_sum_seldom(Row<TT, TD> row, int k0, int k1, float unit, const VdTab& tab) {
+template <typename TT, typename TD, int LOADS>
+__device__ __noinline__ long long residual_sum_seldom(Row<TT, TD, LOADS> row, int k0, int k1, float unit, const VdTab& tab) {
   return residual_sum(row, k0, k1, unit, tab);
 }
 // The token among k0 .. k1 - 1 with which the sum, `sum` before them, passes `at`; else the last with a weight (what rounding leaves), or -1.
-template <typename TT, typename TD>
-__device__ __forceinline__ int walk(const Row<TT, TD>& row, int k0, int k1, long long sum, long long at, float unit, const VdTab& tab) {
+template <typename TT, typename TD, int LOADS>
+__device__ __forceinline__ int walk(const Row<TT, TD, LOADS>& row, int k0, int k1, long long sum, long long at, float unit, const VdTab& tab) {
   const int lane = threadIdx.x & 31;
   int token = -1;
   for (; k0 < k1; k0 += 32) {
@@ -500,15 +502,15 @@ __device__ __forceinline__ int walk(const Row<TT, TD>& row, int k0, int k1, long
   return token;
 }
 // A token whose p is next to its q: what the sum of p's above q, less q's there, has to be mended by (0: it was on its side).
-template <typename TT, typename TD>
-__device__ __noinline__ long long mend(Row<TT, TD> row, int k, float rho32, float unit, const VdTab& tab) {
+template <typename TT, typename TD, int LOADS>
+__device__ __noinline__ long long mend(Row<TT, TD, LOADS> row, int k, float rho32, float unit, const VdTab& tab) {
   const float x = to_f<TT>(row.p[k]), y = to_f<TD>(row.q[k]);
   const bool above = __fmaf_rn(both(weights(y, y, row.mq, row.c, tab).h).x, -rho32, both(weights(x, x, row.mp, row.c, tab).h).x) > 0.f;
   const Two d = row.gap(x, x, y, y, tab).first();
   return above == (d.h > 0.f) ? 0 : whole(d.h > 0.f ? d : Two{-d.h, -d.l}, unit);
 }
 
-template <typename TT, typename TD>
+template <typename TT, typename TD, int LOADS>
 __global__ void __launch_bounds__(VD_THREADS) verify_decide_kernel(VerifyCall a, int parts, const Stat* stats) {
   constexpr int WARPS = VD_THREADS / 32;
   static_assert(WARPS >= 5 && WARPS <= 32 && VD_CTAS <= 32, "sums and run_of by a warp");
@@ -638,7 +640,7 @@ __global__ void __launch_bounds__(VD_THREADS) verify_decide_kernel(VerifyCall a,
   int i, code;
   first_from(0, i, code);
 
-  Row<TT, TD> row;
+  Row<TT, TD, LOADS> row;
   row.c = sc;
   const int share = (a.vocab + ctas - 1) / ctas, v0 = min(a.vocab, rank * share), v1 = min(a.vocab, v0 + share);
   const int each = ((share + WARPS - 1) / WARPS + 31) & ~31, w0 = min(v1, v0 + warp * each), w1 = min(v1, w0 + each);
@@ -664,11 +666,11 @@ __global__ void __launch_bounds__(VD_THREADS) verify_decide_kernel(VerifyCall a,
       SumPair sq, above_p, above_q;
       float near = 0.f;
       rho32 = __fdividef(st.y, st.w);
-      row.each(w0 + lane, w1, [&](int k, const float (&x)[VD_LOADS], const float (&y)[VD_LOADS]) {
-        bool by[VD_LOADS], any = false;
-        float qh[VD_LOADS];
+      row.each(w0 + lane, w1, [&](int k, const float (&x)[LOADS], const float (&y)[LOADS]) {
+        bool by[LOADS], any = false;
+        float qh[LOADS];
 #pragma unroll
-        for (int j = 0; j < VD_LOADS; j += 2) {
+        for (int j = 0; j < LOADS; j += 2) {
           const TwoPair p = weights(x[j], x[j + 1], row.mp, row.c, tab), d = weights(y[j], y[j + 1], row.mq, row.c, tab);
           sp.add(p);
           sq.add(d);
@@ -685,7 +687,7 @@ __global__ void __launch_bounds__(VD_THREADS) verify_decide_kernel(VerifyCall a,
         }
         if (any) {
 #pragma unroll
-          for (int j = 0; j < VD_LOADS; ++j)
+          for (int j = 0; j < LOADS; ++j)
             if (by[j]) {
               near += qh[j];
               const int at = atomicAdd(&s_nears, 1);
@@ -702,9 +704,9 @@ __global__ void __launch_bounds__(VD_THREADS) verify_decide_kernel(VerifyCall a,
         s_warp[Q_NEAR][warp] = q_near;
       }
     } else {
-      row.each(w0 + lane, w1, [&](int, const float (&x)[VD_LOADS], const float (&)[VD_LOADS]) {
+      row.each(w0 + lane, w1, [&](int, const float (&x)[LOADS], const float (&)[LOADS]) {
 #pragma unroll
-        for (int j = 0; j < VD_LOADS; j += 2) sp.add(weights(x[j], x[j + 1], row.mp, row.c, tab));
+        for (int j = 0; j < LOADS; j += 2) sp.add(weights(x[j], x[j + 1], row.mp, row.c, tab));
       });
     }
     const long long of_p = warp_sum(whole(sp.value(), unit));
@@ -902,14 +904,17 @@ cudaError_t verify_t(cudaStream_t st, const VerifyCall& a) {
   // of 32000, of whose clusters of 16 seven find room, 19.7 by 16, 17.9 by 8; sixteen chunks of which one waits (some of them greedy,
   // and done at once) 19.1 by 8, 21.2 by 4.
   struct Tag;
-  const cudaError_t e = cluster16_once<Tag>(verify_decide_kernel<TT, TD>);
+  struct Tag4;
+  auto two = verify_decide_kernel<TT, TD, 2>, four = verify_decide_kernel<TT, TD, 4>;
+  cudaError_t e = cluster16_once<Tag>(two);
+  if (e == cudaSuccess) e = cluster16_once<Tag4>(four);
   if (e != cudaSuccess) return e;
   int ctas = VD_CTAS;
   for (; ctas > 1; ctas /= 2) {
-    const int n = clusters_at_once<Tag>(verify_decide_kernel<TT, TD>, ctas, VD_THREADS);
+    const int n = clusters_at_once<Tag>(two, ctas, VD_THREADS);
     if (a.n_seq <= n + n / 8) break;
   }
-  return launch_cluster(verify_decide_kernel<TT, TD>, dim3((unsigned)(a.n_seq * ctas)), ctas, VD_THREADS, 0, st, a, parts, (const Stat*)stats);
+  return launch_cluster(a.vocab / ctas >= VD_MANY * VD_THREADS ? four : two, dim3((unsigned)(a.n_seq * ctas)), ctas, VD_THREADS, 0, st, a, parts, (const Stat*)stats);
 }
 
 }  // namespace

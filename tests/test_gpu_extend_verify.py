@@ -177,6 +177,7 @@ def test_refusals():
         refused(status, lambda: m.trim(lens))
     m.trim([2, 0])
     g = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()   # (what the side stream reads is made on this one)
     s = torch.cuda.Stream()
     with torch.cuda.stream(s):
         g.capture_begin()

@@ -257,6 +257,7 @@ def test_another_stream_and_graphs():
         adept.adept_kv_reserve(p, length, want, *out, workspace=ws)
         adept.adept_kv_copy_blocks(c, out[1], out[2])
 
+    torch.cuda.synchronize()   # (what the side stream reads is made on this one)
     s = torch.cuda.Stream()
     with torch.cuda.stream(s):
         run()

@@ -171,6 +171,7 @@ def test_a_round_captured_and_replayed():
             return [self.pages.state, self.cache.k, self.cache.v, self.len, self.tok, self.acc, self.nxt, self.logits]
 
     one, two = State(), State()
+    torch.cuda.synchronize()   # (what the side stream reads is made on this one)
     s = torch.cuda.Stream()
     with torch.cuda.stream(s):
         State().round()

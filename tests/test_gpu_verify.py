@@ -314,6 +314,7 @@ def test_captured_and_replayed():
     out = [torch.zeros(3, dtype=torch.int32, device="cuda") for _ in range(2)]
     ws = adept.verify_workspace(10)
     run = lambda: adept.adept_verify_drafts(*x, *out, workspace=ws)  # noqa: E731
+    torch.cuda.synchronize()   # (what the side stream reads is made on this one)
     s = torch.cuda.Stream()
     with torch.cuda.stream(s):
         run()
