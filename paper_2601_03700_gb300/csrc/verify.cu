@@ -637,9 +637,6 @@ __global__ void __launch_bounds__(VD_THREADS) verify_decide_kernel(VerifyCall a,
     i = first >> 2;
     code = first & 3;
   };
-  int i, code;
-  first_from(0, i, code);
-
   Row<TT, TD, LOADS> row;
   row.c = sc;
   const int share = (a.vocab + ctas - 1) / ctas, v0 = min(a.vocab, rank * share), v1 = min(a.vocab, v0 + share);
@@ -721,27 +718,28 @@ __global__ void __launch_bounds__(VD_THREADS) verify_decide_kernel(VerifyCall a,
     zp = total(s_part[OF_P]);
     if (row.q) zq = total(s_part[OF_Q]);
   };
-  int looked = -1;
-  // drafts that are too close: decided by the precise sums, in 64 bits
-  while (code == CLOSE) {
+  // The row that stops.  (A loop, so that judging and looking, most of the kernel's code, are there once: instructions come from L2, and
+  // with two copies of each 16 chunks took 19.1 us where they take 18.4.)
+  int i = -1, code = BAD;
+  const bool draws = greedy || (a.u[q.e - 1] >= 0.f && a.u[q.e - 1] < 1.f);
+  while (draws) {
+    first_from(i + 1, i, code);
+    if (code == BAD || greedy) break;
     const int r = q.s + i;
     look(r);
-    looked = r;
+    if (code == STOPS) break;
+    // a draft that is too close: decided by the precise sums, in 64 bits
     if (tid == 0) {
       const double dp = (double)drafted_at(0, r) - row.mp, dq = row.q ? (double)drafted_at(1, r) - row.mq : 0.0;
       const double logs = log((double)a.u[r]) + log((double)zp / unit) - (row.q ? log((double)zq / unit_q) : 0.0);
       s_first = dq - dp + (double)t * logs < 0.0;
     }
     __syncthreads();
-    if (!s_first) {
-      code = STOPS;
-      break;
-    }
-    first_from(i + 1, i, code);
+    if (!s_first) break;
+    cluster_barrier();   // (the sums of that row have been read: s_part is free, and the next row's list is empty)
     if (tid == 0) s_nears = 0;
-    cluster_barrier();   // (the sums of that row have been read: s_part is free)
   }
-  if (code == BAD || (!greedy && !(a.u[q.e - 1] >= 0.f && a.u[q.e - 1] < 1.f))) {
+  if (code == BAD) {
     if (rank == 0 && tid == 0) a.flag(ERRW_VALUE);
     give(-1, -1);
     return;
@@ -760,7 +758,6 @@ __global__ void __launch_bounds__(VD_THREADS) verify_decide_kernel(VerifyCall a,
     }
     return;
   }
-  if (looked != r) look(r);
   row.certain = soft || r == q.e - 1 ? -1 : a.tokens[r + 1];
   row.plain = r == q.e - 1;
   // What is drawn from: its sum, the ranks' and this CTA's warps'.  One warp settles it (conversions of 64 bits run at a few a cycle and SM).
@@ -866,7 +863,7 @@ __global__ void __launch_bounds__(VD_THREADS) verify_decide_kernel(VerifyCall a,
   if (warp != run_of(s_piece, WARPS)) return;
   int token = -1;
   for (int again = 0; again < 2 && token < 0; ++again)   // (again: a run of tokens with p next to q, on the wrong sides; odds of 2^-34)
-    token = again ? walk(row, 0, a.vocab, 0, at, unit, tab) : walk(row, p0, p1, before, at, unit, tab);
+    token = walk(row, again ? 0 : p0, again ? a.vocab : p1, again ? 0 : before, at, unit, tab);
   if (lane == 0) {
     a.accepted[b] = i;
     a.next[b] = token;
