@@ -396,3 +396,32 @@ def test_masked_tokens_where_both_sums_are_the_same():
         c = dict(target=t.cuda(), draft=d.cuda(), tokens=tokens, start=list(range(0, 2 * B + 1, 2)), u=torch.rand(2 * B, generator=g))
         acc, nxt = check(c)
         assert acc.count(0) > B // 2 and all(i in keep for i in nxt)
+
+
+@pytest.mark.parametrize("scale,offset", [(1.0, 1e4), (1.0, -1e4), (1.0, 3e6), (1e3, 0.0), (1e6, -1e7), (1e30, 0.0), (1e37, 0.0), (1e-4, 0.0), (1e-30, 0.0), (0.0, 7.0)])
+def test_logits_of_any_size(scale, offset):
+    """Far from zero, far apart, next to each other, all the same."""
+    c = make([3, 2, 0, 4], 2003, 70)
+    for k in ("target", "draft"):
+        c[k] = (c[k] * scale + offset).contiguous()
+    check(c)
+    check(c, draft=False)
+    check(c, [0.0, 2.0 ** -10, 1024.0, 0.5])
+    check({**c, "target": c["target"].bfloat16(), "draft": c["draft"].bfloat16()})
+
+
+@pytest.mark.parametrize("t", [2.0 ** -10, 0.01, 0.3, 3.0, 100.0, 1024.0])
+def test_temperatures(t):
+    c = make([4] * 12, 5000, 71)
+    check(c, [t] * 12)
+    check(c, [t] * 12, draft=False)
+
+
+def test_drafts_that_were_never_likely():
+    """Tokens with shares down to 2^-100 and below as drafts: tested by their logarithms."""
+    c = make([3] * 16, 700, 72, spread=40.0, near=20.0)
+    g = torch.Generator().manual_seed(73)
+    c["tokens"] = torch.randint(700, c["tokens"].shape, generator=g).int()
+    c["u"][::2] = 1e-30
+    check(c)
+    check(c, draft=False)
