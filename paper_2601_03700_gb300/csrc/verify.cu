@@ -598,7 +598,7 @@ __global__ void __launch_bounds__(VD_THREADS) verify_decide_kernel(VerifyCall a,
 
   // how a row stands by its 32-bit sums; the last row, behind which there is no draft, stops
   enum { HOLDS = 0, STOPS = 1, CLOSE = 2, BAD = 3 };
-  auto judge = [&](int i, float4& row) {
+  auto stands = [&](int i, float4& row) {
     const int r = q.s + i;
     const bool last = i == n - 1, drafted = soft && !last;
     const float2 p = stat(0, r), d = drafted ? stat(1, r) : make_float2(0.f, 1.f);
@@ -626,7 +626,7 @@ __global__ void __launch_bounds__(VD_THREADS) verify_decide_kernel(VerifyCall a,
     int mine = 0;
     float4 row;
     for (int k = from + tid; k < n && !mine; k += VD_THREADS) {
-      const int c = judge(k, row);
+      const int c = stands(k, row);
       if (c != HOLDS) mine = k * 4 + c;
     }
     if (mine) atomicMin(&s_first, mine);
@@ -718,7 +718,7 @@ __global__ void __launch_bounds__(VD_THREADS) verify_decide_kernel(VerifyCall a,
     zp = total(s_part[OF_P]);
     if (row.q) zq = total(s_part[OF_Q]);
   };
-  // The row that stops.  (A loop, so that judging and looking, most of the kernel's code, are there once: instructions come from L2, and
+  // The row that stops.  (A loop, so that both steps, most of the kernel's code, are there once: instructions come from L2, and
   // with two copies of each 16 chunks took 19.1 us where they take 18.4.)
   int i = -1, code = BAD;
   const bool draws = greedy || (a.u[q.e - 1] >= 0.f && a.u[q.e - 1] < 1.f);

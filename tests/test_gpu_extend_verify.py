@@ -231,3 +231,46 @@ def test_the_head_over_many_tokens():
     last = m.extend([170, 130], tokens, float("inf"))[1]
     assert_rows_close(lg[[169, 299]].cpu().numpy(), last.cpu().numpy(), 2e-2, "logits")
     m.close()
+
+
+def test_a_decoder_with_cross_attention():
+    """An encoder-decoder's decoder: drafts verified behind its source, its logits as the chunk's without drafts."""
+    cfg = synth.ModelConfig(family=synth.GPT2, n_layers=4, d_model=384, n_heads=6, head_dim=64, d_ffn=512, vocab=500, max_pos=256, dtype="bf16",
+                            max_batch=2, max_seq=128, max_src=40)
+    m = adept.Model(cfg, synth.make_weights(cfg, seed=7))
+    prompt = synth.make_tokens(8, 2, 10, cfg.vocab).cuda()
+    states = torch.randn(60, cfg.d_model, device="cuda")
+    u = torch.rand(7, device="cuda")
+    chunk = synth.make_tokens(9, 1, 7, cfg.vocab).cuda().view(-1).int()
+    with pytest.raises(adept.AdeptError):
+        m.verify([4, 3], chunk, 0.9, u)   # no source yet
+    m.set_cross_source([40, 20], states)
+    m.prefill(prompt, float("inf"))
+    acc, nx, lg, *_ = m.verify([4, 3], chunk, float("inf"), u)
+    m.check()
+    exp = verify(lg.cpu(), None, chunk.tolist(), [0, 4, 7], u.cpu())
+    assert (acc.tolist(), nx.tolist()) == exp[:2]
+    m.trim([10, 10])
+    last = m.extend([4, 3], chunk, float("inf"))[1]
+    assert_rows_close(lg[[3, 6]].cpu().numpy(), last.cpu().numpy(), 2e-2, "logits")
+    m.close()
+
+
+def test_profiled_and_without_graphs():
+    """The passes' other modes: events around launches, no captured steps, SIMT products."""
+    cfg, m = make("llama_gqa")
+    out = []
+    for option in (None, adept.OPT_PROFILE, adept.OPT_DECODE_GRAPH, adept.OPT_GEMM_SIMT):
+        if option is not None:
+            adept.adept_set_option(m.h, option, 0 if option == adept.OPT_DECODE_GRAPH else 1)
+        m.prefill(synth.make_tokens(1, 3, 12, cfg.vocab).cuda(), float("inf"))
+        tok = synth.make_tokens(2, 1, 9, cfg.vocab).cuda().view(-1).int()
+        acc, nx, lg, *_ = m.verify([2, 3, 4], tok, float("inf"), torch.full((9,), 0.5, device="cuda"))
+        m.check()
+        assert (acc.tolist(), nx.tolist()) == verify(lg.cpu(), None, tok.tolist(), [0, 2, 5, 9], torch.full((9,), 0.5))[:2]
+        out.append(lg.cpu().numpy())
+        if option is not None:
+            adept.adept_set_option(m.h, option, 1 if option == adept.OPT_DECODE_GRAPH else 0)
+    for x in out[1:]:
+        assert_rows_close(x, out[0], 2e-2, "logits")
+    m.close()

@@ -425,3 +425,18 @@ def test_drafts_that_were_never_likely():
     c["u"][::2] = 1e-30
     check(c)
     check(c, draft=False)
+
+
+@pytest.mark.parametrize("t", [0.3, 0.7, 2.0])
+def test_next_to_the_border_at_a_temperature(t):
+    B, V = 64, 3001
+    c = make([3] * B, V, 80, near=0.3, td=F32, dd=BF16)
+    lt, ld = (torch.log_softmax(c[k].double() / torch.tensor(t).float().double().item(), 1).cpu() for k in ("target", "draft"))
+    r = torch.arange(4 * B - 1)
+    x = c["tokens"][1:].long()
+    ratio = (lt[r, x] - ld[r, x]).exp()
+    near = ratio.float() * (1 + torch.randint(-3, 4, ratio.shape, generator=torch.Generator().manual_seed(81)) * 2.0 ** -23)
+    use = ratio < 0.999
+    c["u"][:-1][use] = near[use]
+    acc, _ = check(c, [float(torch.tensor(t).float())] * B)
+    assert 0 < sum(acc) < 3 * B

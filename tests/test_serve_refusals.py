@@ -145,3 +145,11 @@ def test_binding_checks_verifications(lib):
             adept.adept_verify_drafts(**{**good, key: bad})
     with pytest.raises(ValueError, match="GPU"):
         adept.adept_verify_drafts(**good)
+
+
+def test_the_check_takes_the_word_on_its_stream():
+    """As the other checks: cudaMemset works on the legacy stream, for which others do not wait."""
+    import re
+    from test_error_words import body
+    calls = body("serve_ops.cu", "adept_error_check")
+    assert "take_error_word(" in calls and not re.search(r"\bcudaMem(set|cpy)\s*\(", calls)
