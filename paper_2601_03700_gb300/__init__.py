@@ -682,7 +682,7 @@ def adept_kv_fork(pages: KVPages, source: torch.Tensor, length: torch.Tensor, wo
 def adept_kv_reserve(pages: KVPages, length: torch.Tensor, new_length: torch.Tensor, got: torch.Tensor, copy_src: torch.Tensor,
                      copy_dst: torch.Tensor, workspace: Optional[torch.Tensor] = None, stream=None):
     """Makes positions length[b] .. new_length[b] - 1 of every row writable.  got: the length that each row has room for now;
-    copy_src, copy_dst: blocks that adept_kv_copy_blocks has to copy first (-1: none).  All [n_seq] int32."""
+    copy_src, copy_dst: blocks that adept_kv_copy_blocks has to copy first (-1: none).  All [n_seq] int32; got may be length or new_length."""
     fn, n = load_library().adept_kv_reserve, pages.n_seq
     _pages_call(fn, pages, workspace, stream, _index(pages, "length", length, n), _index(pages, "new_length", new_length, n),
                 _index(pages, "got", got, n), _index(pages, "copy_src", copy_src, n), _index(pages, "copy_dst", copy_dst, n))

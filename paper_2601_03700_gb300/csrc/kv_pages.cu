@@ -154,8 +154,9 @@ __global__ void __launch_bounds__(PG_THREADS) kv_fork_kernel(Pages p, const int*
 // its part to the entries that they fall to.  Bound by latency: four loads one behind the other, two barriers.
 // ---------------------------------------------------------------------------------------------
 constexpr int NARROW = 4, WORDS = 8;
-constexpr unsigned ASKS = 1, KEEPS = 2, SHARED = 4, COPIES = 8, WIDE = 16;   // row flags: grows; keeps the shared block that it writes;
-                                                                 // writes a shared block in part; gets a copy of that; more than NARROW entries
+constexpr unsigned ASKS = 1, KEEPS = 2, SHARED = 4, COPIES = 8, WIDE = 16, PART = 32;   // row flags: grows; keeps the shared block that it writes;
+                            // writes a shared block in part; gets a copy of that; more than NARROW entries; its first holds positions that stay
+constexpr int RELEASED = -0x7fffffff - 1;   // count of a block that its last holder has left, while free blocks are still being looked for
 constexpr unsigned MANY = 1u << 30;   // sums of blocks stop here (more than there are)
 
 struct ReserveCall {
@@ -199,10 +200,13 @@ __global__ void __launch_bounds__(PG_THREADS) kv_reserve_kernel(Pages p, Reserve
   extern __shared__ __align__(16) unsigned char smem[];
   unsigned* pre = reinterpret_cast<unsigned*>(smem);   // [n_seq] blocks asked for by the rows up to this one
   unsigned *demand = pre + p.n_seq, *word = demand + p.n_seq, *flags = word + p.n_seq;   // [n_seq] blocks; a narrow row's entries; flags
-  int *key = reinterpret_cast<int*>(flags + p.n_seq), *cnt = key + a.hash, *last = cnt + a.hash;   // shared blocks that rows write in part
+  int *first = reinterpret_cast<int*>(flags + p.n_seq), *width = first + p.n_seq;        // [n_seq] its entries: first .. first + width - 1
+  int *key = width + p.n_seq, *cnt = key + a.hash, *last = cnt + a.hash;   // shared blocks that rows write in part
   __shared__ int red[32];
   __shared__ unsigned redu[32], s_taken, s_free[PG_CTAS];
+  __shared__ int s_freed, s_any;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, rank = cluster_rank();
+  if (tid == 0) s_freed = s_any = 0;
   cluster_arrive();
   for (int i = tid; i < a.hash; i += PG_THREADS) {
     key[i] = -1;
@@ -239,8 +243,11 @@ __global__ void __launch_bounds__(PG_THREADS) kv_reserve_kernel(Pages p, Reserve
       atomicAdd(cnt + h, 1);
       atomicMax(last + h, b);
     }
+    if (r.part) fl |= PART;
     word[b] = w;
     flags[b] = fl;
+    first[b] = r.j0;
+    width[b] = r.j1 - r.j0;
     if (!(fl & WIDE)) demand[b] = __popc(w);
   }
   int n_free = __popc(bits0), total = 0;
@@ -322,6 +329,7 @@ __global__ void __launch_bounds__(PG_THREADS) kv_reserve_kernel(Pages p, Reserve
     __syncthreads();
   }
   const unsigned taken = s_taken;
+  const bool looked_at = seg <= 4 * PG_THREADS;   // every count was read before the first changes (the same in all CTAs)
   // The first `taken` free blocks, in ascending order, to the entries that ask, in order.  (With a thread's four entries looked up before the
   // first is written, 64 prompts of 16000 positions took 19 us instead of 27, but 4 rows that grow by 9, as most calls', 0.4 more.)
   auto give = [&](unsigned k, int id) {
@@ -333,10 +341,10 @@ __global__ void __launch_bounds__(PG_THREADS) kv_reserve_kernel(Pages p, Reserve
       else
         b = mid + 1;
     }
+    // (not the row's lengths again: d_got may be written over them by another CTA)
     unsigned q = k - (pre[b] - demand[b]);
-    const GrowRow r = grow_row(p, a, b);
-    int c = r.j0;
-    if (demand[b] == (unsigned)(r.j1 - r.j0)) {
+    int c = first[b];
+    if (demand[b] == (unsigned)width[b]) {
       c += (int)q;   // all of them
     } else if (!(flags[b] & WIDE)) {
       unsigned w = word[b];
@@ -358,8 +366,18 @@ __global__ void __launch_bounds__(PG_THREADS) kv_reserve_kernel(Pages p, Reserve
     *at = id;
     p.ref[id] = 1;
     if (!held(p, e)) return;
-    atomicSub(p.ref + e, 1);
-    if (c == r.j0 && r.part) {
+    if (looked_at) {
+      atomicSub(p.ref + e, 1);
+    } else {   // counts are still to be read: a block that becomes free here is none of the free ones
+      int* ref = p.ref + e;
+      for (int was = *(volatile int*)ref, seen; was != RELEASED; was = seen) {
+        seen = atomicCAS(ref, was, was == 1 ? RELEASED : was - 1);
+        if (seen != was) continue;
+        if (was == 1) s_freed = 1;
+        break;
+      }
+    }
+    if (c == first[b] && (flags[b] & PART)) {
       a.src[b] = e;
       a.dst[b] = id;
     }
@@ -370,6 +388,14 @@ __global__ void __launch_bounds__(PG_THREADS) kv_reserve_kernel(Pages p, Reserve
     unsigned k = base + (i1 - i0 <= 4 * PG_THREADS ? at0 : cta_scan(__popc(bits), red, &total));
     for (unsigned m = bits; m && k < taken; m &= m - 1, ++k) give(k, i + 4 * tid + __ffs(m) - 1);
     base += total;
+  }
+  if (!looked_at) {
+    __syncthreads();
+    if (tid < PG_CTAS && s_freed) cluster_store(&s_any, tid, 1);
+    cluster_barrier();
+    if (s_any)
+      for (int i = i0 + tid; i < i1; i += PG_THREADS)
+        if (p.ref[i] == RELEASED) p.ref[i] = 0;
   }
   if (rank == 0) {
     for (int b = tid; b < p.n_seq; b += PG_THREADS) {
@@ -572,9 +598,9 @@ cudaError_t launch_kv_reserve(cudaStream_t st, const Pages& p, const int* length
                               int* ws) {
   ReserveCall a{length, want, got, src, dst, reinterpret_cast<unsigned*>(ws), mask_words(p), 32};
   while (a.hash < 2 * p.n_seq) a.hash *= 2;
-  const size_t smem = (size_t)p.n_seq * 16 + (size_t)a.hash * 12;
+  const size_t smem = (size_t)p.n_seq * 24 + (size_t)a.hash * 12;
   struct Tag;
-  cudaError_t e = smem_once<Tag>(kv_reserve_kernel, PG_MAX_SEQ * 16 + 2 * PG_MAX_SEQ * 12);
+  cudaError_t e = smem_once<Tag>(kv_reserve_kernel, PG_MAX_SEQ * 24 + 2 * PG_MAX_SEQ * 12);
   if (e != cudaSuccess) return e;
   return launch_cluster(kv_reserve_kernel, dim3(PG_CTAS), PG_CTAS, PG_THREADS, smem, st, p, a);
 }

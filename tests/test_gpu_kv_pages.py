@@ -233,6 +233,43 @@ def test_the_most_rows():
     adept.adept_kv_fork(big, z, z)
 
 
+@pytest.mark.parametrize("n_blocks", [16000, 200000])
+def test_blocks_that_become_free_are_not_given(n_blocks):
+    """Two rows get away from 400 blocks that only they hold; the third row's come from those that were free before.  In the larger pool counts are
+    read after the first blocks have been given."""
+    p = Both(n_blocks, 4, 1000)
+    low, shared = n_blocks // 200, n_blocks // 10
+    ref = [0] * low + [1] * (shared - low) + [2] * 400 + [0] * (n_blocks - shared - 400)
+    row = list(range(shared, shared + 400)) + [-1] * 600
+    p.plain.ref, p.plain.table = list(ref), [list(row), list(row), [-1] * 1000, [-1] * 1000]
+    p.gpu.ref.copy_(i32(ref))
+    p.gpu.block_table[:2] = i32(row)
+    got = p.reserve([0, 0, 0, 0], [6400, 6400, 9600, 300])[0]
+    assert got == [6400, 6400, 9600, 300] and p.plain.ref[shared:shared + 400] == [0] * 400
+
+
+def test_results_over_the_lengths():
+    p, q = (adept.KVPages(9000, 300, 40) for _ in range(2))
+    want = i32([(b * 7) % 400 for b in range(300)])
+    for step in (0, 1, 150, 40):
+        length = want.clone() if step else torch.zeros_like(want)
+        more = want + step
+        out = [[torch.empty_like(want) for _ in range(3)] for _ in range(2)]
+        adept.adept_kv_reserve(p, length, more, *out[0])
+        for place in ((length, 0), (more, 1)):
+            if place[1] == 0:
+                save = q.block_table.clone(), q.ref.clone()
+            else:
+                q.block_table.copy_(save[0])
+                q.ref.copy_(save[1])
+            args = [length.clone(), more.clone()]
+            adept.adept_kv_reserve(q, *args, args[place[1]], *out[1][1:])
+            assert torch.equal(args[place[1]], out[0][0])
+            assert torch.equal(out[0][1], out[1][1]) and torch.equal(out[0][2], out[1][2])
+            assert torch.equal(p.block_table, q.block_table) and torch.equal(p.ref, q.ref)
+        want = out[0][0]
+
+
 def test_a_long_row():
     """A row of 2^30 positions in blocks of one, of which the last are reserved."""
     p = adept.KVPages(300, 1, 1 << 26, block_tokens=16)
