@@ -590,7 +590,8 @@ ADEPT_API adept_status adept_kv_copy_blocks(const adept_kv_cache* caches, int n_
  * probabilities are off by some 10^-6.  The same call gives the same bits.
  *   d_ws          adept_verify_workspace(n_rows) bytes on 16 bytes; calls that may overlap on the GPU need one each.  No
  *                 smaller call needs more.
- * Errors: INVALID_ARG (a size, type, stride or pointer), CAPACITY (above 2^24 rows or sequences), CUDA. */
+ * The results overlap neither what is read nor each other.
+ * Errors: INVALID_ARG (a size, type, stride or pointer), CAPACITY (above 2^24 rows or 2^16 sequences), CUDA. */
 ADEPT_API adept_status adept_verify_drafts(int n_seq, int n_rows, int vocab, int target_dtype, const void* d_target, int64_t ld_target,
                                  int draft_dtype, const void* d_draft, int64_t ld_draft, const int32_t* d_tokens,
                                  const int32_t* d_start, const float* d_temperature, const float* d_u, int32_t* d_accepted,

@@ -129,7 +129,8 @@ adept_status adept_verify_drafts(int n_seq, int n_rows, int vocab, int target_dt
                                  int32_t* d_next, float* d_logprob, uint32_t* d_err, void* d_ws, int64_t ws_bytes, void* stream) {
   if (n_seq < 0 || n_rows < 0) return bad(ADEPT_ERR_INVALID_ARG, "negative size");
   if (vocab < 1 || vocab > (1 << 20)) return bad(ADEPT_ERR_INVALID_ARG, "vocab %d outside 1 .. 2^20", vocab);
-  if (n_rows > (1 << 24) || n_seq > (1 << 24)) return bad(ADEPT_ERR_CAPACITY, "more than 2^24 rows or sequences");
+  // (every row looks for its sequence among all)
+  if (n_rows > (1 << 24) || n_seq > (1 << 16)) return bad(ADEPT_ERR_CAPACITY, "more than 2^24 rows or 2^16 sequences");
   for (const int dt : {target_dtype, draft_dtype})
     if (dt != ADEPT_DTYPE_F32 && dt != ADEPT_DTYPE_BF16) return bad(ADEPT_ERR_INVALID_ARG, "dtype %d unknown", dt);
   if (n_seq == 0) return ADEPT_OK;

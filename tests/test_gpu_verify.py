@@ -272,6 +272,19 @@ def test_no_rows_and_no_sequences():
     assert call(c)[0].numel() == 0
 
 
+def test_the_most_sequences():
+    n, g = 1 << 16, torch.Generator().manual_seed(44)
+    c = dict(target=torch.randn(n, 4, generator=g).cuda(), draft=torch.zeros(n, 4).cuda(), tokens=torch.zeros(n, dtype=torch.int32),
+             start=list(range(n + 1)), u=torch.rand(n, generator=g))
+    w = c["target"].cpu().double().softmax(1)
+    want = (w.cumsum(1) <= (c["u"].double() + 2.0 ** -25).unsqueeze(1) * w.sum(1, keepdim=True)).sum(1)
+    acc, nxt, lp = (t.cpu() for t in call(c))
+    assert not acc.any() and torch.equal(nxt.long(), want)
+    assert (lp - w.gather(1, want.unsqueeze(1))[:, 0].log()).abs().max() <= lp_tol(4, 16)
+    acc, nxt, _ = (t.cpu() for t in call(c, [0.0] * n))
+    assert not acc.any() and torch.equal(nxt.long(), w.argmax(1))
+
+
 def test_the_largest_vocabulary():
     c = make([2, 1], 1 << 20, 43)
     check(c)

@@ -88,6 +88,11 @@ def test_bad_verifications(lib, bad):
     assert lib.adept_verify_drafts(*a.values(), None) == (3 if max(a["n_seq"], a["n_rows"]) > 2 ** 24 else 1)
 
 
+def test_as_many_sequences_as_a_verification_takes(lib):
+    assert lib.adept_verify_drafts(*{**GOOD, "n_seq": 2 ** 16 + 1}.values(), None) == 3
+    assert lib.adept_verify_drafts(*{**GOOD, "n_seq": 2 ** 16, "vocab": 0}.values(), None) == 1
+
+
 def test_verification_workspaces(lib):
     assert lib.adept_verify_workspace(-1) == -1 and lib.adept_verify_workspace(2 ** 24 + 1) == -1
     sizes = [lib.adept_verify_workspace(n) for n in (0, 1, 2, 100, 5000, 2 ** 24)]
