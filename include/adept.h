@@ -586,8 +586,9 @@ ADEPT_API adept_status adept_kv_copy_blocks(const adept_kv_cache* caches, int n_
  *   d_err         error word or NULL
  * Whatever the rows behind the deciding one hold does not enter.  A sequence whose rows are out of range, or which meets a token or
  * number out of range, logits with NaN or +infinity, or with nothing above -infinity, gets -1, -1 and flags DEVICE_INPUT.
- * Which draft is accepted and which token drawn follows from sums with a relative error of 2^-34 at most (2^-40 as a rule), whatever the logits' type; the log
- * probabilities are off by some 10^-6.  The same call gives the same bits.
+ * Which draft is accepted follows from sums of weights that are off by 2^-36 at most (2^-40 as a rule), whatever the logits' type, and so does
+ * a token drawn from p_r.  max(p_r - q_r, 0) has the errors of both: where it sums to s (1 to 2^-20), the sums that it is drawn by are off by
+ * 2^-33 / s at most (2^-40 / s as a rule).  The log probabilities are off by some 10^-6.  The same call gives the same bits.
  *   d_ws          adept_verify_workspace(n_rows) bytes on 16 bytes; calls that may overlap on the GPU need one each.  No
  *                 smaller call needs more.
  * The results overlap neither what is read nor each other.

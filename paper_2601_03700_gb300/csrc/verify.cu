@@ -7,7 +7,7 @@
 // Two launches.  The first streams every row once, each in parts of a CTA, and leaves per part the maximum, the sum of exp((l - max) / T), the
 // maximum's first index (greedy sequences) and the draft's logit: HBM-bound, 437 MB at 6.1 TB/s (64 chunks of 8 drafts over 131072
 // tokens, fp32 and bf16).  The second, a cluster per sequence, decides.  Sums of 32 bits decide a draft unless the two sides are closer
-// than their errors (close_of); those, and the drawing, go by weights of two 32-bit parts each (2^-40 relative): with a vocabulary of
+// than their errors (close_of); those, and the drawing, go by weights of two 32-bit parts each (2^-37 relative at most): with a vocabulary of
 // V tokens the cumulative sum has V steps, and an error of 2^-24 would move the drawn token with odds of V 2^-23.  It reads one row of
 // the target and one of the draft a sequence, most of it from L2, and is bound by the weights' arithmetic (about 40 operations a
 // weight) where there are many sequences, by the chain loads -> sums -> barrier -> sums where there are few.  One launch, in which a
@@ -378,9 +378,11 @@ struct SumPair {   // two sums
   }
 };
 
-// exp(x), x = (l - m) / T = j log(2) / 64 + r, |r| <= log(2) / 128, for two l: 2^(j / 64) by its exponent and the table, and four
-// terms of exp(r)'s series, whose first is kept in two parts (the others are below 2^-16, and rounding them costs 2^-40).  Both r's
-// first part and j's product with the first part of log(2) / 64 are multiples of 2^-31, so that r comes out exactly but for the second parts.
+// exp(x), x = (l - m) / T = j log(2) / 64 + r + rl, |r| <= log(2) / 128, for two l: 2^(j / 64) by its exponent and the table, and four
+// terms of the series of exp(r + rl), whose first is kept in two parts.  The others are below 2^-16: rounding them costs 2^-40 a step, 2^-37 +
+// 2^-45 |x| in all at most (2^-37.7 the largest of 2.8 million, at temperatures from 2^-10 to 100).  rl, what x's rounding leaves, is
+// up to 2^-22 at x = -7: in the first term alone it left weights 2^-26 off.  Both r and j's product with the first part of log(2) / 64
+// are multiples of 2^-31, so that r comes out exactly but for the second parts.
 // Below exp(-80), -infinity too, it is exp(-80) = 2^-115: no sum sees 2^20 of those, and none is drawn.
 __device__ __forceinline__ TwoPair weights(float l0, float l1, float m, const Scale& c, const VdTab& tab) {
   const TwoPair d = sum_of(pair(l0, l1), same(-m));
@@ -400,7 +402,7 @@ __device__ __forceinline__ TwoPair weights(float l0, float l1, float m, const Sc
   const float2 jb = both(jm);
   const int j0 = __float_as_int(jb.x), j1 = __float_as_int(jb.y);
   const Pair th = pair(tab.h[j0 & (VD_TAB - 1)], tab.h[j1 & (VD_TAB - 1)]), tl = pair(tab.l[j0 & (VD_TAB - 1)], tab.l[j1 & (VD_TAB - 1)]);
-  const Pair y = fma2(mul2(r, r), fma2(r, fma2(r, same(1.f / 24.f), same(1.f / 6.f)), same(0.5f)), rl);   // exp(r) = 1 + r + y
+  const Pair v = add2(r, rl), y = fma2(mul2(v, v), fma2(v, fma2(v, same(1.f / 24.f), same(1.f / 6.f)), same(0.5f)), rl);   // exp(r + rl) = 1 + r + y
   const Pair ph = mul2(th, r), pl = fma2(th, r, mul2(ph, same(-1.f)));
   const Pair s = add2(th, ph), e = sub2(ph, sub2(s, th));
   const Pair lo = add2(e, add2(pl, fma2(th, y, fma2(tl, r, tl))));
