@@ -383,7 +383,8 @@ struct SumPair {   // two sums
 // 2^-45 |x| in all at most (2^-37.7 the largest of 2.8 million, at temperatures from 2^-10 to 100).  rl, what x's rounding leaves, is
 // up to 2^-22 at x = -7: in the first term alone it left weights 2^-26 off.  Both r and j's product with the first part of log(2) / 64
 // are multiples of 2^-31, so that r comes out exactly but for the second parts.
-// Below exp(-80), -infinity too, it is exp(-80) = 2^-115: no sum sees 2^20 of those, and none is drawn.
+// The first part of the result is the nearest to it: which of p and q is above the other goes by those, and sums of many second parts would
+// round them off.  Below exp(-80), -infinity too, it is exp(-80) = 2^-115: no sum sees 2^20 of those, and none is drawn.
 __device__ __forceinline__ TwoPair weights(float l0, float l1, float m, const Scale& c, const VdTab& tab) {
   const TwoPair d = sum_of(pair(l0, l1), same(-m));
   float2 h = both(d.h), l = both(d.l);
@@ -408,7 +409,8 @@ __device__ __forceinline__ TwoPair weights(float l0, float l1, float m, const Sc
   const Pair lo = add2(e, add2(pl, fma2(th, y, fma2(tl, r, tl))));
   // 2^floor(j / 64): the whole number's bits above the table's, moved to the exponent (what lies above leaves the word)
   const Pair sc = pair(__int_as_float(((j0 & ~(VD_TAB - 1)) << 17) + 0x3f800000), __int_as_float(((j1 & ~(VD_TAB - 1)) << 17) + 0x3f800000));
-  return TwoPair{mul2(s, sc), mul2(lo, sc)};
+  const Pair w = add2(s, lo);   // (lo is up to 2^-15 of s)
+  return TwoPair{mul2(w, sc), mul2(sub2(lo, sub2(w, s)), sc)};
 }
 
 // The row that is looked at closely.

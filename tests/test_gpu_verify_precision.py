@@ -21,9 +21,9 @@ def _lib():
 
 def pair(kind, t, seed=90):
     """Logits of a target and of a draft that is the target but for noise, fp32.  eight: eight tokens, the first, hold half of both."""
-    V, noise = {"eight": (1 << 17, 2e-3), "small": (32000, 1e-4)}[kind]
+    V, noise = {"few": (1 << 17, 2e-3), "eight": (1 << 17, 2e-3), "many": (32000, 1e-3), "small": (32000, 1e-4)}[kind]
     g = torch.Generator().manual_seed(seed)
-    x = (3.0 * t if kind == "small" else 1.0) * torch.randn(V, generator=g).double()
+    x = (3.0 * t if kind in ("many", "small") else 1.0) * torch.randn(V, generator=g).double()
     if kind == "eight":
         x[:8] = t * (torch.logsumexp(x / t, 0) - math.log(8)) + 0.3 * torch.randn(8, generator=g).double()
     p = x.float()
@@ -39,7 +39,8 @@ def next_to_borders(w, least, n):
     return (k[off.argsort()[:n]] * 2.0 ** -24).float()
 
 
-@pytest.mark.parametrize("kind,t", [("eight", 0.7), ("small", 0.3), ("small", 0.7)])
+@pytest.mark.parametrize("t", [0.3, 0.7, 1.0])
+@pytest.mark.parametrize("kind", ["few", "eight", "many", "small"])
 def test_drawn_where_target_and_draft_are_close(kind, t):
     """max(p - q, 0) sums to s, 2^-8 to 2^-15; a weight is off by 2^-39 or so, every one by its own, so that those of a row's sums
     average to 2^-40 of p at most, 2^-40 / s of what is drawn from: borders are that far from u, or farther."""
