@@ -25,7 +25,7 @@ constexpr float VS_HUGE = 1e6f;
 constexpr int VD_THREADS = 512, VD_CTAS = 16;    // decision: threads of a CTA, CTAs of a sequence at most
 constexpr int VD_MANY = 32;                      // tokens a thread from which on it takes four at a time, else two
 constexpr int VD_LEAST = 20;                     // max(p - q, 0) sums to less than 2^-this: the token is drawn from p
-constexpr int VD_FINE = 14;                      // to less than 2^-this: summed token by token
+constexpr int VD_FINE = 14;                      // to less than 2^-this (or p without the draft): summed token by token
 constexpr float VD_NEAR = 3.814697265625e-06f;   // 2^-18: p and q nearer than this may be taken for either above the other
 constexpr float VD_SURE = 5.820766091346741e-11f;   // 2^-34: what that may make of the sum, else those tokens are looked at again
 constexpr int VD_NEARS = 64;                     // as many as a CTA remembers; with more, the sum is taken token by token
@@ -776,10 +776,10 @@ __global__ void __launch_bounds__(VD_THREADS) verify_decide_kernel(VerifyCall a,
   };
   if (row.plain) {
     if (warp == 0) s_how = settle(zp);
-  } else if (row.q) {
+  } else {
     // sum of max(p - q, 0) = that of p where p is above q, less that of q there.  "Above" went by the 32-bit sums' quotient: a token whose p
     // and q are nearer than that is off may be on the wrong side, which changes the sum by that much of its q
-    if (warp == 0) {
+    if (warp == 0 && row.q) {
       const Two rho = quotient(two_of(zp), two_of(zq));   // in p's units over q's
       const float by = __int_as_float(0x3f800000 + __float_as_int(unit_q) - __float_as_int(unit));
       const float off = fabsf(rho32 - rho.h * by) / (rho.h * by) + 2.384185791015625e-07f;   // (and the comparison's roundings)
@@ -800,8 +800,18 @@ __global__ void __launch_bounds__(VD_THREADS) verify_decide_kernel(VerifyCall a,
       else
         s_how = settle(all);
     }
+    if (warp == 0 && !row.q) {   // all of p but the draft (p's sums are rounded to 2^-45 or so: where little is left, the others are summed by themselves)
+      const int x = row.certain, at_rank = x / share, at_warp = (x - at_rank * share) / each;
+      const long long wx = whole(weights(drafted_at(0, r), -INFINITY, row.mp, row.c, tab).first(), unit);
+      auto rest = [&](long long v, bool has) { return has ? (v - wx < VD_NOTHING ? 0ll : v - wx) : v; };
+      if (lane < WARPS) s_warp[DRAWN][lane] = rest(s_warp[OF_P][lane], rank == at_rank && lane == at_warp);
+      const long long part = lane < ctas ? rest(s_part[OF_P][lane], lane == at_rank) : 0;
+      if (lane < ctas) s_part[DRAWN][lane] = part;
+      const long long all = warp_sum(part);
+      s_how = all < zp >> VD_FINE ? (int)BY_TOKEN : settle(all);
+    }
     __syncthreads();
-    row.rho = s_rho;
+    if (row.q) row.rho = s_rho;
     const int how = s_how;
     if (how >= WRONG_SIDES) {   // (uniform over the cluster)
       if (how == BY_TOKEN) {
@@ -828,14 +838,6 @@ __global__ void __launch_bounds__(VD_THREADS) verify_decide_kernel(VerifyCall a,
         s_how = settle(total(s_part[DRAWN]));
       }
     }
-  } else if (warp == 0) {   // all of p but the draft
-    const int x = row.certain, at_rank = x / share, at_warp = (x - at_rank * share) / each;
-    const long long wx = whole(weights(drafted_at(0, r), -INFINITY, row.mp, row.c, tab).first(), unit);
-    auto rest = [&](long long v, bool has) { return has ? (v - wx < VD_NOTHING ? 0ll : v - wx) : v; };
-    if (lane < WARPS) s_warp[DRAWN][lane] = rest(s_warp[OF_P][lane], rank == at_rank && lane == at_warp);
-    const long long part = lane < ctas ? rest(s_part[OF_P][lane], lane == at_rank) : 0;
-    if (lane < ctas) s_part[DRAWN][lane] = part;
-    s_how = settle(warp_sum(part));
   }
   __syncthreads();
   row.plain = s_how == PLAIN;

@@ -64,3 +64,34 @@ def test_drawn_where_target_and_draft_are_close(kind, t):
     assert verify(target[:2], draft[:2], [0, x], [0, 2], u[:2], [t])[1] == want[:1]
     assert not acc.any()
     assert nxt.tolist() == want
+
+
+def drawn_without_probabilities(target, x, u):
+    """The token behind a refused draft x of one row, for every number in u."""
+    n = len(u)
+    acc, nxt = (torch.full((n,), -7, dtype=torch.int32, device="cuda") for _ in range(2))
+    both = torch.full((2 * n,), 1 - 2.0 ** -24)
+    both[1::2] = torch.tensor(u)
+    adept.adept_verify_drafts(target.expand(2 * n, -1).contiguous().cuda(), None, torch.tensor([0, x] * n, dtype=torch.int32).cuda(),
+                              torch.arange(0, 2 * n + 1, 2, dtype=torch.int32).cuda(), both.cuda(), acc, nxt)
+    assert not acc.any()
+    return nxt.tolist()
+
+
+@pytest.mark.parametrize("V", [32000, 50257])
+@pytest.mark.parametrize("lg", [-19.9, -18.0, -14.0, -9.0])
+def test_a_refused_draft_that_has_nearly_all_of_the_target(V, lg):
+    """All but s = 2^lg of p is the draft's.  Token 10, a few places before it, has 2^-24.2 of the rest: u = 0, which stands for 2^-25, draws
+    it, and no other u does."""
+    x, s = 50, 2.0 ** lg
+    g = torch.Generator().manual_seed(91)
+    w = torch.rand(V, generator=g, dtype=torch.float64) * (torch.rand(V, generator=g) < 0.01)
+    w[:4000] = 0.0
+    w *= s / w.sum()
+    w[10], w[x] = s * 2.0 ** -24.2, 1 - s
+    target = w.log().float()
+    assert float(logs(target, 1)[x]) < math.log(1 - 2.0 ** -24)   # refused
+    u = [0.0, 2.0 ** -24, 0.25, 0.5, 0.75, 1 - 2.0 ** -24]
+    want = [verify(target.expand(2, V), None, [0, x], [0, 2], torch.tensor([1 - 2.0 ** -24, v]))[1][0] for v in u]
+    assert want[0] == 10 and 10 not in want[1:]
+    assert drawn_without_probabilities(target, x, u) == want
