@@ -556,7 +556,7 @@ ADEPT_API adept_status adept_kv_reserve(const adept_kv_pages* p, const int32_t* 
 /* Moves the blocks in use to the front: with U of them in use (*d_used), the k-th in use past the first U goes to the k-th
  * free one among those (both in ascending order), in the table and in the counts.  d_copy_src[k], d_copy_dst[k] ([n_blocks / 2]
  * int32 each) name the moves, for adept_kv_copy_blocks, and for the program where it holds blocks itself; entries behind the last are -1.  Sources and targets are
- * disjoint. */
+ * disjoint.  An entry that is flagged stays in the table, unless another block has come to the number that it names: then it is -1. */
 ADEPT_API adept_status adept_kv_compact(const adept_kv_pages* p, int32_t* d_used, int32_t* d_copy_src, int32_t* d_copy_dst, void* d_ws,
                               int64_t ws_bytes, void* stream);
 

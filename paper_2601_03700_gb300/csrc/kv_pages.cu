@@ -458,7 +458,7 @@ __global__ void __launch_bounds__(PG_THREADS) kv_compact_kernel(Pages p, int* us
       } else if (id < U) {
         dst[id - at] = id;
       }
-      if (id >= U) remap[id] = -1;
+      if (moves) remap[id] = id < U && (u >> j & 1) ? id : -1;
     }
     before += total;
   }
@@ -472,15 +472,21 @@ __global__ void __launch_bounds__(PG_THREADS) kv_compact_kernel(Pages p, int* us
     remap[s] = d;
   }
   cluster_barrier();
+  // What an entry is now: remap, where it was counted as held.  (Without moves ids below U are those in use.)
   const size_t entries = (size_t)p.n_seq * p.max_blocks;
-  for (size_t i = me; i < entries; i += all) {
-    const int e = p.table[i];
-    if (e < U && e >= -1) continue;
-    const int to = held(p, e) ? remap[e] : -1;
-    if (to >= 0)
-      p.table[i] = to;
-    else
-      p.flag(ERRW_POS);   // (out of range, or a block that is counted as free)
+  constexpr int EACH = 4;   // (an entry and its look-up are two loads one behind the other: 4 at a time)
+  for (size_t i0 = me; i0 < entries; i0 += (size_t)EACH * all) {
+    int e[EACH], to[EACH];
+#pragma unroll
+    for (int k = 0; k < EACH; ++k) e[k] = i0 + (size_t)k * all < entries ? p.table[i0 + (size_t)k * all] : -1;
+#pragma unroll
+    for (int k = 0; k < EACH; ++k) to[k] = e[k] == -1 || (!moves && e[k] >= 0 && e[k] < U) ? e[k] : moves && held(p, e[k]) ? remap[e[k]] : -1;
+#pragma unroll
+    for (int k = 0; k < EACH; ++k) {
+      if (to[k] == e[k]) continue;
+      if (to[k] == -1) p.flag(ERRW_POS);   // no block, or one that is counted as free: left as it is, unless a block has come there
+      if (to[k] >= 0 || (e[k] >= 0 && e[k] < U)) p.table[i0 + (size_t)k * all] = to[k];
+    }
   }
 }
 

@@ -1,0 +1,72 @@
+"""Block tables whose entries and counts do not agree: flagged where a call meets them, and no two rows end up on one block because of
+it."""
+import pytest
+import torch
+
+import paper_2601_03700_gb300 as adept
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _lib():
+    if not torch.cuda.is_available():
+        pytest.skip("no CUDA device")
+    adept.load_library()
+
+
+def i32(x):
+    return torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+def pages(n_blocks, table, ref):
+    p = adept.KVPages(n_blocks, len(table), len(table[0]))
+    p.block_table.copy_(i32(table))
+    p.ref.copy_(i32(ref))
+    return p
+
+
+def flagged(p):
+    with pytest.raises(adept.AdeptError) as ei:
+        p.check()
+    assert ei.value.status == 6
+    p.check()
+
+
+def compact(p):
+    n = p.ref.numel() // 2
+    used, src, dst = i32([-9]), *(torch.full((n,), -9, dtype=torch.int32, device="cuda") for _ in range(2))
+    adept.adept_kv_compact(p, used, src, dst)
+    return used.tolist()[0], src.tolist(), dst.tolist()
+
+
+def test_compaction_onto_a_block_that_a_row_holds():
+    """Row 0 holds block 0, which is counted as free: row 1's block moves there, and row 0 holds it no more."""
+    p = pages(2, [[0], [1]], [0, 1])
+    assert compact(p) == (1, [1], [0])
+    assert p.block_table.tolist() == [[-1], [0]] and p.ref.tolist() == [1, 0]
+    flagged(p)
+
+
+def test_compaction_of_a_large_table():
+    """Counted as free below the border, at it and past it, among 40000 entries that are sound."""
+    n = 50000
+    table, ref = torch.full((40, 1000), -1, dtype=torch.int32), torch.zeros(n, dtype=torch.int32)
+    order = torch.randperm(n, generator=torch.Generator().manual_seed(3))[:40000].int()
+    table.view(-1)[:] = order
+    ref[order.long()] = 1
+    bad = [int((table.view(-1) == b).nonzero()[0, 0]) for b in sorted(order.tolist())[5:39000:3000]]   # entries
+    ids = table.view(-1)[bad].tolist()
+    ref[ids] = 0
+    p = pages(n, table.tolist(), ref.tolist())
+    used, src, dst = compact(p)
+    flagged(p)
+    assert used == 40000 - len(bad)
+    held = [i for i in order.tolist() if i not in ids]
+    move = {s: d for s, d in zip(src, dst) if s >= 0}
+    assert sorted(move) == sorted(i for i in held if i >= used)
+    want = [[move.get(e, e) for e in row] for row in table.tolist()]
+    for at, e in zip(bad, ids):   # below the border a block may have come there
+        want[at // 1000][at % 1000] = -1 if e < used else e
+    assert p.block_table.tolist() == want
+    assert p.ref.tolist() == [1] * used + [0] * (n - used)
