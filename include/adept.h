@@ -549,6 +549,7 @@ ADEPT_API adept_status adept_kv_fork(const adept_kv_pages* p, const int32_t* d_s
  * always, unless it would keep a shared one that an earlier row did not get away from).  d_got[b] = d_new_length[b] where row b was served or holds what it
  * needs, else d_length[b], and nothing of the row has changed.  d_new_length[b] <= d_length[b]: nothing is asked for.
  * All [n_seq] int32; d_got may be d_length or d_new_length, else nothing overlaps.  A block that the call frees is given by the next.
+ * Checked are the entries that a row asks to write; one whose block is counted as free is -1 from then on, whether the row is served or not.
  * CAPACITY: more than 4096 rows. */
 ADEPT_API adept_status adept_kv_reserve(const adept_kv_pages* p, const int32_t* d_length, const int32_t* d_new_length, int32_t* d_got,
                               int32_t* d_copy_src, int32_t* d_copy_dst, void* d_ws, int64_t ws_bytes, void* stream);

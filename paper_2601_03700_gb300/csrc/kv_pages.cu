@@ -186,13 +186,18 @@ __device__ __forceinline__ GrowRow grow_row(const Pages& p, const ReserveCall& a
   return r;
 }
 __device__ __forceinline__ unsigned shared_slot(const ReserveCall& a, int e) { return ((unsigned)e * 2654435761u >> 7) & (unsigned)(a.hash - 1); }
-// Whether an entry needs a new block, where f is its block's count (0: no block).
-__device__ __forceinline__ bool needs(const Pages& p, int e, int f) {
+// Whether entry *at = e needs a new block, where f is its block's count (0: no block).  A block that is counted as free may be given to
+// any row: the entry becomes -1.  (Every CTA that looks at it comes to the same, whether it still finds the block or not.)
+__device__ __forceinline__ bool needs(const Pages& p, int* at, int e, int f) {
   if (!held(p, e)) {
     if (e != -1) p.flag(ERRW_POS);
     return true;
   }
-  if (f <= 0) p.flag(ERRW_POS);   // (held, but counted as free)
+  if (f <= 0) {
+    p.flag(ERRW_POS);
+    *at = -1;
+    return true;
+  }
   return f > 1;
 }
 
@@ -229,7 +234,7 @@ __global__ void __launch_bounds__(PG_THREADS) kv_reserve_kernel(Pages p, Reserve
     unsigned w = 0, fl = r.asks ? ASKS : 0;
 #pragma unroll
     for (int k = 0; k < NARROW; ++k)
-      if (r.j0 + k < r.j1 && needs(p, e[k], f[k])) w |= 1u << k;
+      if (r.j0 + k < r.j1 && needs(p, p.table + (size_t)b * p.max_blocks + r.j0 + k, e[k], f[k])) w |= 1u << k;
     if (r.j1 - r.j0 > NARROW) fl |= WIDE;
     if (r.part && f[0] > 1) {
       // how many rows ask for the block, and the last of them
@@ -274,7 +279,7 @@ __global__ void __launch_bounds__(PG_THREADS) kv_reserve_kernel(Pages p, Reserve
   for (int b = rank + PG_CTAS * warp; b < p.n_seq; b += PG_CTAS * (PG_THREADS / 32)) {
     if (!(flags[b] & WIDE)) continue;
     const GrowRow r = grow_row(p, a, b);
-    const int* row = p.table + (size_t)b * p.max_blocks;
+    int* row = p.table + (size_t)b * p.max_blocks;
     unsigned n = 0;
     for (int j = r.j0; j < r.j1; j += 32 * WORDS) {   // (a long prompt's row: WORDS words' loads under way together)
       int e[WORDS], f[WORDS];
@@ -288,7 +293,7 @@ __global__ void __launch_bounds__(PG_THREADS) kv_reserve_kernel(Pages p, Reserve
 #pragma unroll
       for (int k = 0; k < WORDS; ++k) {
         const int c = j + 32 * k + lane;
-        const unsigned m = __ballot_sync(0xffffffffu, c == r.j0 ? word[b] & 1 : c < r.j1 && needs(p, e[k], f[k]));
+        const unsigned m = __ballot_sync(0xffffffffu, c == r.j0 ? word[b] & 1 : c < r.j1 && needs(p, row + c, e[k], f[k]));
         if (lane == 0 && j + 32 * k < r.j1) a.mask[(size_t)b * a.mask_words + (j - r.j0) / 32 + k] = m;
         n += __popc(m);
       }

@@ -70,3 +70,39 @@ def test_compaction_of_a_large_table():
         want[at // 1000][at % 1000] = -1 if e < used else e
     assert p.block_table.tolist() == want
     assert p.ref.tolist() == [1] * used + [0] * (n - used)
+
+
+def reserve(p, length, want):
+    out = [torch.full((len(length),), -9, dtype=torch.int32, device="cuda") for _ in range(3)]
+    adept.adept_kv_reserve(p, i32(length), i32(want), *out)
+    return [o.tolist() for o in out]
+
+
+@pytest.mark.parametrize("blocks", [3, 9])   # of a row: few, many
+def test_growth_into_an_entry_that_is_counted_as_free(blocks):
+    """Row 0 holds block 0 behind its length, counted as free: the entry counts as -1 and gets a block like the others; block 0 is
+    given once."""
+    n = 4 * blocks
+    p = pages(n, [[blocks, 0] + [-1] * blocks, [-1] * (blocks + 2)], [0] * blocks + [1] + [0] * (n - blocks - 1))
+    got, src, dst = reserve(p, [16, 0], [16 + 16 * blocks, 20])
+    assert (got, src, dst) == ([16 + 16 * blocks, 20], [-1, -1], [-1, -1])
+    free = [i for i in range(n) if i != blocks]
+    assert p.block_table.tolist() == [[blocks] + free[:blocks] + [-1], free[blocks:blocks + 2] + [-1] * blocks]
+    assert p.ref.tolist() == [int(i in [blocks] + free[:blocks + 2]) for i in range(n)]
+    flagged(p)
+
+
+def test_growth_into_a_first_block_that_is_counted_as_free():
+    """The block of positions that stay: its row gets another, without a copy, and nobody's count falls below 0."""
+    p = pages(6, [[2, -1], [4, -1]], [1, 1, 0, 1, 1, 0])
+    assert reserve(p, [5, 5], [9, 9]) == [[9, 9], [-1, -1], [-1, -1]]
+    assert p.block_table.tolist() == [[2, -1], [4, -1]] and p.ref.tolist() == [1, 1, 1, 1, 1, 0]
+    flagged(p)
+
+
+def test_growth_that_is_not_served():
+    """Nothing else of the row changes."""
+    p = pages(4, [[0, 3, -1], [1, 2, -1]], [1, 1, 1, 0])
+    assert reserve(p, [16, 20], [48, 30]) == [[16, 30], [-1, -1], [-1, -1]]   # two blocks asked for, one free
+    assert p.block_table.tolist() == [[0, -1, -1], [1, 2, -1]] and p.ref.tolist() == [1, 1, 1, 0]
+    flagged(p)
