@@ -535,8 +535,9 @@ ADEPT_API int64_t adept_kv_pages_workspace(const adept_kv_pages* p);
 
 /* Every row at once: row b becomes the first d_length[b] positions of what row d_source[b] held before the call (their blocks
  * shared, counted once more), the rest of the row -1; blocks that nobody holds any more are free.  d_source[b] = b with the row's
- * length: unchanged; a shorter length: cut back (drafts that were not accepted); d_source[b] < 0, or no positions: dropped;
- * another row: a fork, or beams reordered.  Both [n_seq] int32. */
+ * length: unchanged; a shorter length: cut back (drafts that were not accepted); d_source[b] < 0, or no positions (a length of 0 or
+ * less): dropped; another row: a fork, or beams reordered.  Both [n_seq] int32.  Checked are the entries that a row takes from another,
+ * which are -1 where they are flagged, and those that it gives up, whose block's count then stays as it is. */
 ADEPT_API adept_status adept_kv_fork(const adept_kv_pages* p, const int32_t* d_source, const int32_t* d_length, void* d_ws, int64_t ws_bytes,
                            void* stream);
 

@@ -68,21 +68,61 @@ __device__ __forceinline__ ForkRow fork_row(const Pages& p, const int* source, c
 __device__ __forceinline__ int fork_source(const Pages& p, const ForkRow& f, int b, int c, int old) {
   return c >= f.nb ? -1 : f.src == b ? old : p.table[(size_t)f.src * p.max_blocks + c];
 }
-// The counts of an entry that changes from block `old` to `neu`; what it becomes (-1 where neu is no block).
-__device__ __forceinline__ int fork_counts(const Pages& p, int old, int neu) {
-  if (neu != -1 && !held(p, neu)) {
-    p.flag(ERRW_POS);
-    neu = -1;
-  }
-  if (neu >= 0) atomicAdd(p.ref + neu, 1);
-  if (old != -1 && (!held(p, old) || atomicSub(p.ref + old, 1) <= 0)) p.flag(ERRW_POS);   // (a count below its holders)
-  return neu;
+// The count of an entry that a row takes from another (1: no block), read before any count changes.
+__device__ __forceinline__ int fork_count(const Pages& p, int e) { return held(p, e) ? p.ref[e] : e == -1; }
+// Such an entry: -1 where it is no block, or one that is counted as free.
+__device__ __forceinline__ int fork_taken(const Pages& p, int e, int count) {
+  if (count > 0) return e;
+  p.flag(ERRW_POS);
+  return -1;
 }
-// Larger tables: a CTA for FORK_CHUNK entries of a row.  The first launch changes the counts, writes rows that come from others into `stage` and
-// only reads the table; the second writes it (256 rows of 2048 entries, cut back, and grown by adept_kv_reserve: 12.9 us, by chunks of 2048
-// 14.8, of 256 14.3).
+// The counts of entries that change from blocks `old` to `neu`, blocks or -1 (all on their way before the first is looked at).
+template <int N>
+__device__ __forceinline__ void fork_counts(const Pages& p, const int (&old)[N], const int (&neu)[N]) {
+  int was[N];
+#pragma unroll
+  for (int k = 0; k < N; ++k) {
+    was[k] = 1;
+    if (old[k] == neu[k]) continue;
+    if (neu[k] >= 0) atomicAdd(p.ref + neu[k], 1);
+    if (held(p, old[k])) was[k] = atomicSub(p.ref + old[k], 1);
+    else if (old[k] != -1) p.flag(ERRW_POS);
+  }
+#pragma unroll
+  for (int k = 0; k < N; ++k)
+    if (was[k] <= 0) {   // counted as free, or for fewer rows than hold it
+      atomicAdd(p.ref + old[k], 1);
+      p.flag(ERRW_POS);
+    }
+}
+// Larger tables: a CTA for FORK_CHUNK entries of a row.  The first launch only reads: rows that come from others go into `stage`; the
+// second changes counts and table (256 rows of 2048 entries, cut back, and grown by adept_kv_reserve: 12.4 us, by chunks of 256 14.7, of 1024
+// 12.2, but 4096 rows of 512 cut back 10.0, by chunks of 1024 10.4, of 256 18.4).
 constexpr int FORK_THREADS = 256, FORK_CHUNK = 512;
-__global__ void __launch_bounds__(FORK_THREADS) kv_fork_count_kernel(Pages p, const int* source, const int* length, int* stage) {
+__global__ void __launch_bounds__(FORK_THREADS) kv_fork_read_kernel(Pages p, const int* source, const int* length, int* stage) {
+  PDL_ENTRY();
+  const int b = (int)blockIdx.x;
+  const ForkRow f = fork_row(p, source, length, b);
+  if (f.src == b) return;
+  const size_t row = (size_t)b * p.max_blocks;
+  constexpr int EACH = FORK_CHUNK / FORK_THREADS;
+  for (int c0 = (int)blockIdx.y * FORK_CHUNK; c0 < p.max_blocks; c0 += (int)gridDim.y * FORK_CHUNK) {
+    int neu[EACH], n[EACH];
+#pragma unroll
+    for (int k = 0; k < EACH; ++k) {
+      const int c = c0 + k * FORK_THREADS + threadIdx.x;
+      neu[k] = c < p.max_blocks ? fork_source(p, f, b, c, -1) : -1;
+    }
+#pragma unroll
+    for (int k = 0; k < EACH; ++k) n[k] = fork_count(p, neu[k]);
+#pragma unroll
+    for (int k = 0; k < EACH; ++k) {
+      const int c = c0 + k * FORK_THREADS + threadIdx.x;
+      if (c < p.max_blocks) stage[row + c] = fork_taken(p, neu[k], n[k]);
+    }
+  }
+}
+__global__ void __launch_bounds__(FORK_THREADS) kv_fork_write_kernel(Pages p, const int* source, const int* length, const int* stage) {
   PDL_ENTRY();
   const int b = (int)blockIdx.x;
   const ForkRow f = fork_row(p, source, length, b);
@@ -94,58 +134,33 @@ __global__ void __launch_bounds__(FORK_THREADS) kv_fork_count_kernel(Pages p, co
     for (int k = 0; k < EACH; ++k) {
       const int c = c0 + k * FORK_THREADS + threadIdx.x;
       const bool in = c < p.max_blocks && !(f.src == b && c < f.nb);
-      old[k] = in ? p.table[row + c] : 0;
-      neu[k] = in ? fork_source(p, f, b, c, old[k]) : 0;
+      old[k] = in ? p.table[row + c] : -1;
+      neu[k] = in && f.src != b ? stage[row + c] : -1;
     }
 #pragma unroll
-    for (int k = 0; k < EACH; ++k) {
-      if (old[k] != neu[k]) neu[k] = fork_counts(p, old[k], neu[k]);
-      const int c = c0 + k * FORK_THREADS + threadIdx.x;
-      if (f.src != b && c < p.max_blocks) stage[row + c] = neu[k];
-    }
-  }
-}
-__global__ void __launch_bounds__(FORK_THREADS) kv_fork_write_kernel(Pages p, const int* source, const int* length, const int* stage) {
-  PDL_ENTRY();
-  const int b = (int)blockIdx.x;
-  const ForkRow f = fork_row(p, source, length, b);
-  const size_t row = (size_t)b * p.max_blocks;
-  for (int c0 = (int)blockIdx.y * FORK_CHUNK; c0 < p.max_blocks; c0 += (int)gridDim.y * FORK_CHUNK) {
-#pragma unroll
-    for (int k = 0; k < FORK_CHUNK / FORK_THREADS; ++k) {
-      const int c = c0 + k * FORK_THREADS + threadIdx.x;
-      if (c < p.max_blocks && !(f.src == b && c < f.nb)) p.table[row + c] = f.src == b ? -1 : stage[row + c];
-    }
+    for (int k = 0; k < EACH; ++k)
+      if (old[k] != neu[k]) p.table[row + c0 + k * FORK_THREADS + threadIdx.x] = neu[k];
+    fork_counts(p, old, neu);
   }
 }
 
-// Tables of up to PG_CTAS * PG_THREADS * FORK_EACH entries: one cluster holds them between reading and writing (one launch instead
-// of two: 4 rows of 24 blocks, cut back and grown, 9.3 us against 10.2).
-constexpr int FORK_EACH = 8;
+// Tables of up to an entry a thread of one cluster: those hold them between reading and writing (4096 entries, all rows moved, 3.3 us; two entries a
+// thread, of 16384, 4.8 where the two launches take 4.0).
 __global__ void __launch_bounds__(PG_THREADS) kv_fork_kernel(Pages p, const int* source, const int* length) {
   PDL_ENTRY();
-  const int total = p.n_seq * p.max_blocks, step = PG_CTAS * PG_THREADS, me = (int)blockIdx.x * PG_THREADS + threadIdx.x;
-  int old[FORK_EACH], neu[FORK_EACH];
-  unsigned write = 0;
-#pragma unroll
-  for (int k = 0; k < FORK_EACH; ++k) {   // (what the rows' loads wait for is under way together)
-    const int i = me + k * step;
-    old[k] = neu[k] = 0;
-    if (i >= total) continue;
+  const int i = (int)blockIdx.x * PG_THREADS + threadIdx.x;
+  int old[1] = {-1}, neu[1] = {-1}, n = 1;   // n: the count of a block that is taken from another row, else 1
+  if (i < p.n_seq * p.max_blocks) {
     const int b = i / p.max_blocks, c = i - b * p.max_blocks;
-    old[k] = p.table[i];
-    neu[k] = fork_source(p, fork_row(p, source, length, b), b, c, old[k]);
+    const ForkRow f = fork_row(p, source, length, b);
+    old[0] = p.table[i];
+    neu[0] = fork_source(p, f, b, c, old[0]);
+    if (f.src != b) n = fork_count(p, neu[0]);
   }
-#pragma unroll
-  for (int k = 0; k < FORK_EACH; ++k) {
-    if (old[k] == neu[k]) continue;
-    neu[k] = fork_counts(p, old[k], neu[k]);
-    write |= 1u << k;
-  }
-  cluster_barrier();
-#pragma unroll
-  for (int k = 0; k < FORK_EACH; ++k)
-    if (write >> k & 1) p.table[me + k * step] = neu[k];
+  cluster_barrier();   // table and counts have been read
+  neu[0] = fork_taken(p, neu[0], n);
+  if (old[0] != neu[0]) p.table[i] = neu[0];
+  fork_counts(p, old, neu);
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -596,11 +611,10 @@ size_t pages_workspace(const Pages& p) {
 
 cudaError_t launch_kv_fork(cudaStream_t st, const Pages& p, const int* source, const int* length, int* ws) {
   const long long entries = (long long)p.n_seq * p.max_blocks;
-  if (entries <= PG_CTAS * PG_THREADS * FORK_EACH)
-    return launch_cluster(kv_fork_kernel, dim3(PG_CTAS), PG_CTAS, PG_THREADS, 0, st, p, source, length);
+  if (entries <= PG_CTAS * PG_THREADS) return launch_cluster(kv_fork_kernel, dim3(PG_CTAS), PG_CTAS, PG_THREADS, 0, st, p, source, length);
   const int chunks = cdiv(p.max_blocks, FORK_CHUNK);
   const dim3 g((unsigned)p.n_seq, (unsigned)(chunks < 65535 ? chunks : 65535));
-  cudaError_t e = launch_k(kv_fork_count_kernel, g, dim3(FORK_THREADS), 0, st, p, source, length, ws);
+  cudaError_t e = launch_k(kv_fork_read_kernel, g, dim3(FORK_THREADS), 0, st, p, source, length, ws);
   if (e == cudaSuccess) e = launch_k(kv_fork_write_kernel, g, dim3(FORK_THREADS), 0, st, p, source, length, (const int*)ws);
   return e;
 }

@@ -106,3 +106,43 @@ def test_growth_that_is_not_served():
     assert reserve(p, [16, 20], [48, 30]) == [[16, 30], [-1, -1], [-1, -1]]   # two blocks asked for, one free
     assert p.block_table.tolist() == [[0, -1, -1], [1, 2, -1]] and p.ref.tolist() == [1, 1, 1, 0]
     flagged(p)
+
+
+def fork(p, source, length):
+    adept.adept_kv_fork(p, i32(source), i32(length))
+
+
+@pytest.mark.parametrize("cols", [4, 30000])   # in one launch, in two
+@pytest.mark.parametrize("entry", [1, 9, -3])
+def test_fork_of_an_entry_that_is_no_block(cols, entry):
+    """Row 0's second entry is counted as free (1), or no block (9, -3).  Rows that take it get -1 there, a row that has the same number there
+    already too; no count changes for it."""
+    rest = [-1] * (cols - 2)
+    p = pages(8, [[0, entry] + rest, [2, entry] + rest, [3, -1] + rest], [1, 0, 1, 1, 0, 0, 0, 0])
+    fork(p, [0, 0, 0], [32, 32, 32])
+    assert p.block_table[:, :3].tolist() == [[0, entry, -1], [0, -1, -1], [0, -1, -1]]
+    assert p.ref.tolist() == [3, 0, 0, 0, 0, 0, 0, 0]
+    flagged(p)
+
+
+@pytest.mark.parametrize("cols", [4, 30000])
+def test_fork_that_drops_an_entry_counted_as_free(cols):
+    rest = [-1] * (cols - 2)
+    p = pages(8, [[0, 1] + rest, [2, 1] + rest, [3, -1] + rest], [1, 0, 1, 1, 0, 0, 0, 0])
+    fork(p, [0, 1, 2], [16, 16, 16])
+    assert p.block_table[:, :2].tolist() == [[0, -1], [2, -1], [3, -1]]
+    assert p.ref.tolist() == [1, 0, 1, 1, 0, 0, 0, 0]
+    flagged(p)
+
+
+@pytest.mark.parametrize("cols", [4, 30000])
+def test_fork_takes_what_another_row_drops(cols):
+    """Not a fault: row 0 drops the block that row 1 takes from it, whichever comes first."""
+    rest = [-1] * (cols - 1)
+    for _ in range(20):
+        p = pages(8, [[5] + rest, [6] + rest], [0, 0, 0, 0, 0, 1, 1, 0])
+        fork(p, [1, 0], [16, 16])
+        assert p.block_table[:, 0].tolist() == [6, 5] and p.ref.tolist() == [0, 0, 0, 0, 0, 1, 1, 0]
+        fork(p, [-1, 0], [16, 16])
+        assert p.block_table[:, 0].tolist() == [-1, 6] and p.ref.tolist() == [0, 0, 0, 0, 0, 0, 1, 0]
+        p.check()
