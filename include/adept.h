@@ -581,13 +581,13 @@ ADEPT_API adept_status adept_kv_copy_blocks(const adept_kv_cache* caches, int n_
  *                       d_tokens[r + 1] was drawn from, a sequence's last row may hold anything
  *   d_start       [n_seq + 1] int32, ascending; a sequence may have no row (0 accepted, next token -1)
  *   d_temperature [n_seq] fp32, 0 or 2^-10 .. 2^10; NULL: 1
- *   d_u           [n_rows] fp32 in [0, 1)
+ *   d_u           [n_rows] fp32 in [0, 1) (not NULL, also where every sequence is greedy)
  *   d_accepted, d_next  [n_seq] int32: drafts accepted, the next token
  *   d_logprob     [n_rows] fp32 or NULL: log p_r of each accepted draft (at its r), and of the next token at the row that it was drawn
  *                 from (greedy: at T = 1); other rows are not written
  *   d_err         error word or NULL
- * Whatever the rows behind the deciding one hold does not enter.  A sequence whose rows are out of range, or which meets a token or
- * number out of range, logits with NaN or +infinity, or with nothing above -infinity, gets -1, -1 and flags DEVICE_INPUT.
+ * Whatever the rows behind the deciding one hold does not enter.  A sequence whose rows are out of range, or which meets a row of a sequence
+ * before it, a token or number out of range, logits with NaN or +infinity, or with nothing above -infinity, gets -1, -1 and flags DEVICE_INPUT.
  * Which draft is accepted follows from sums of weights that are off by 2^-36 at most (2^-40 as a rule), whatever the logits' type, and so does
  * a token drawn from p_r.  max(p_r - q_r, 0) has the errors of both: where it sums to s (1 to 2^-20), the sums that it is drawn by are off by
  * 2^-33 / s at most (2^-40 / s as a rule).  The log probabilities are off by some 10^-6.  The same call gives the same bits.

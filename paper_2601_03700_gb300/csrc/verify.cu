@@ -122,9 +122,10 @@ struct Running {
   }
 };
 
-// Statistics of part blockIdx.x % parts of row blockIdx.x / parts, the target's (blockIdx.y = 0) or the draft's.
+// Statistics of part blockIdx.x % parts of row blockIdx.x / parts, the target's (blockIdx.y = 0) or the draft's, for the first sequence that
+// names the row: *owner.
 template <typename T>
-__device__ __forceinline__ void row_stats(const VerifyCall& a, const T* x, bool draft, int r, int part, int parts, Stat* out) {
+__device__ __forceinline__ void row_stats(const VerifyCall& a, const T* x, bool draft, int r, int part, int parts, Stat* out, int* owner) {
   using V = Vec<T>;
   __shared__ int s_seq, s_at;
   __shared__ float s_m[VS_THREADS / 32], s_z[VS_THREADS / 32];
@@ -158,6 +159,7 @@ __device__ __forceinline__ void row_stats(const VerifyCall& a, const T* x, bool 
   }
   const float held = id >= 0 && id < n ? to_f<T>(x[id]) : -INFINITY;
   __syncthreads();
+  if (!draft && part == 0 && tid == 0) *owner = s_seq;
   if (s_seq == 0x7fffffff) return;   // nobody's row
   const float t = a.temp ? a.temp[s_seq] : 1.f;
   if (!temp_ok(t)) return;
@@ -210,14 +212,14 @@ __device__ __forceinline__ void row_stats(const VerifyCall& a, const T* x, bool 
 }
 
 template <typename TT, typename TD>
-__global__ void __launch_bounds__(VS_THREADS, 8) verify_stats_kernel(VerifyCall a, int parts, Stat* stats) {
+__global__ void __launch_bounds__(VS_THREADS, 8) verify_stats_kernel(VerifyCall a, int parts, Stat* stats, int* owner) {
   PDL_ENTRY();
   const int r = (int)blockIdx.x / parts, part = (int)blockIdx.x % parts;
   Stat* out = stats + ((size_t)blockIdx.y * a.n_rows + r) * parts + part;
   if (blockIdx.y == 0)
-    row_stats(a, (const TT*)a.target + r * a.ld_t, false, r, part, parts, out);
+    row_stats(a, (const TT*)a.target + r * a.ld_t, false, r, part, parts, out, owner + r);
   else
-    row_stats(a, (const TD*)a.draft + r * a.ld_d, true, r, part, parts, out);
+    row_stats(a, (const TD*)a.draft + r * a.ld_d, true, r, part, parts, out, nullptr);
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -516,7 +518,7 @@ __device__ __noinline__ long long mend(Row<TT, TD, LOADS> row, int k, float rho3
 }
 
 template <typename TT, typename TD, int LOADS>
-__global__ void __launch_bounds__(VD_THREADS) verify_decide_kernel(VerifyCall a, int parts, const Stat* stats) {
+__global__ void __launch_bounds__(VD_THREADS) verify_decide_kernel(VerifyCall a, int parts, const Stat* stats, const int* owner) {
   constexpr int WARPS = VD_THREADS / 32;
   static_assert(WARPS >= 5 && WARPS <= 32 && VD_CTAS <= 32, "sums and run_of by a warp");
   __shared__ VdTab tab;
@@ -607,10 +609,10 @@ __global__ void __launch_bounds__(VD_THREADS) verify_decide_kernel(VerifyCall a,
     const int r = q.s + i;
     const bool last = i == n - 1, drafted = soft && !last;
     const float2 p = stat(0, r), d = drafted ? stat(1, r) : make_float2(0.f, 1.f);
-    const int x = last ? 0 : a.tokens[r + 1];
+    const int x = last ? 0 : a.tokens[r + 1], whose = owner[r];
     const float u = greedy ? 0.f : a.u[r], lp = drafted_at(0, r), lq = drafted ? drafted_at(1, r) : 0.f;
     row = make_float4(p.x, p.y, d.x, d.y);
-    if (!(p.y > 0.f)) return (int)BAD;   // nothing above -infinity, a NaN, +infinity
+    if (whose != b || !(p.y > 0.f)) return (int)BAD;   // another sequence's row too; nothing above -infinity, a NaN, +infinity
     if (last) return (int)STOPS;
     if (x < 0 || x >= a.vocab) return (int)BAD;
     if (greedy) return best(r) == x ? (int)HOLDS : (int)STOPS;
@@ -899,8 +901,9 @@ template <typename TT, typename TD>
 cudaError_t verify_t(cudaStream_t st, const VerifyCall& a) {
   const int parts = a.n_rows > 0 ? verify_parts(a.n_rows, a.vocab) : 1;
   Stat* stats = (Stat*)a.ws;
+  int* owner = (int*)(stats + (size_t)2 * VS_PARTS * a.n_rows);   // [n_rows] the sequence that a row's statistics are for
   if (a.n_rows > 0) {
-    const cudaError_t e = launch_k(verify_stats_kernel<TT, TD>, dim3((unsigned)(a.n_rows * parts), a.draft ? 2 : 1), dim3(VS_THREADS), 0, st, a, parts, stats);
+    const cudaError_t e = launch_k(verify_stats_kernel<TT, TD>, dim3((unsigned)(a.n_rows * parts), a.draft ? 2 : 1), dim3(VS_THREADS), 0, st, a, parts, stats, owner);
     if (e != cudaSuccess) return e;
   }
   // A sequence gets the most CTAs (of an SM each) whose clusters find room for all sequences at once, or nearly: 64 sequences of 131072 tokens took
@@ -918,12 +921,12 @@ cudaError_t verify_t(cudaStream_t st, const VerifyCall& a) {
     const int n = clusters_at_once<Tag>(two, ctas, VD_THREADS);
     if (a.n_seq <= n + n / 8) break;
   }
-  return launch_cluster(a.vocab / ctas >= VD_MANY * VD_THREADS ? four : two, dim3((unsigned)(a.n_seq * ctas)), ctas, VD_THREADS, 0, st, a, parts, (const Stat*)stats);
+  return launch_cluster(a.vocab / ctas >= VD_MANY * VD_THREADS ? four : two, dim3((unsigned)(a.n_seq * ctas)), ctas, VD_THREADS, 0, st, a, parts, (const Stat*)stats, (const int*)owner);
 }
 
 }  // namespace
 
-size_t verify_workspace(int n_rows) { return (size_t)2 * VS_PARTS * n_rows * sizeof(Stat); }
+size_t verify_workspace(int n_rows) { return (size_t)n_rows * (2 * VS_PARTS * sizeof(Stat) + sizeof(int)); }
 
 cudaError_t launch_verify(cudaStream_t st, const VerifyCall& a) {
   if (a.t_bf16) return a.d_bf16 ? verify_t<bf16, bf16>(st, a) : verify_t<bf16, float>(st, a);
