@@ -253,6 +253,7 @@ def adept_model_load(cfg, weights: Dict[str, torch.Tensor], stream=None):
     h = ctypes.c_void_p()
     st = lib.adept_model_load(ctypes.byref(c), ctypes.byref(table), _stream(stream), ctypes.byref(h))
     _check(lib, None, st)
+    h.vocab, h.n_layers = c.vocab, c.n_layers   # for the checks of adept_extend_verify
     return h
 
 
@@ -291,11 +292,34 @@ def adept_extend_verify(m, lens, tokens: torch.Tensor, delta: float, u: torch.Te
                         forced: Optional[torch.Tensor] = None, exit_layer_out: Optional[torch.Tensor] = None,
                         logprob_out: Optional[torch.Tensor] = None, sim_out: Optional[torch.Tensor] = None, stream=None):
     """adept_extend over chunks of the last accepted token and drafts, which are verified against its logits (logits_out: of every
-    token).  u, draft, temperature, accepted_out, next_token_out, logprob_out: as in adept_verify_drafts."""
+    token, [tokens, vocab]).  u, draft, temperature, accepted_out, next_token_out, logprob_out: as in adept_verify_drafts.  Buffers may be
+    larger than lens asks for."""
     lib = load_library()
     n = len(lens)
-    arr = (ctypes.c_int32 * n)(*[int(x) for x in lens])
+    lens = [int(x) for x in lens]
+    arr = (ctypes.c_int32 * n)(*lens)
+    rows, i32, f32 = sum(lens), torch.int32, torch.float32
+    vocab, layers = getattr(m, "vocab", 1), getattr(m, "n_layers", 1)   # (of a handle that adept_model_load gave)
+    for name, t, need, dtype in (
+            ("tokens", tokens, rows, i32), ("u", u, rows, f32), ("forced", forced, rows, i32), ("exit_layer_out", exit_layer_out, rows, i32),
+            ("logprob_out", logprob_out, rows, f32), ("logits_out", logits_out, rows * vocab, f32), ("sim_out", sim_out, rows * layers, f32),
+            ("temperature", temperature, n, f32), ("accepted_out", accepted_out, n, i32), ("next_token_out", next_token_out, n, i32)):
+        if t is None:
+            continue
+        if t.dtype is not dtype or not t.is_contiguous() or t.get_device() != tokens.get_device():
+            raise ValueError(f"{name} must be contiguous {dtype} values on {tokens.device}")
+        if min(lens, default=-1) >= 0 and t.numel() < need:   # (the library refuses a negative length)
+            raise AdeptError(3, f"{name} has {t.numel()} elements, {need} are needed")
     dt, dp, ld = (0, None, 0) if draft is None else _logits(draft, "draft", draft)
+    if draft is not None:
+        if draft.get_device() != tokens.get_device():
+            raise ValueError(f"draft must be on {tokens.device}")
+        if min(lens, default=-1) >= 0 and draft.shape[0] < rows:
+            raise AdeptError(3, f"draft has {draft.shape[0]} rows, {rows} are needed")
+        if draft.shape[1] < vocab:
+            raise AdeptError(1, f"draft has {draft.shape[1]} columns, the vocabulary {vocab}")
+    if tokens.get_device() < 0:
+        raise ValueError(f"the tokens are on {tokens.device}: the pass needs a GPU")
     _check(lib, m, lib.adept_extend_verify(m, n, arr, _ptr(tokens), float(delta), _ptr(forced), dt, dp, ld, _ptr(temperature), _ptr(u),
                                             _ptr(exit_layer_out), _ptr(logits_out), _ptr(accepted_out), _ptr(next_token_out),
                                             _ptr(logprob_out), _ptr(sim_out), _stream(stream)))
