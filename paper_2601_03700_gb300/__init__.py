@@ -210,6 +210,13 @@ def _stream(stream):
     return ctypes.c_void_p(stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream))
 
 
+def _on(stream):
+    """The call's stream as the current one: what is made and converted for the call is ordered with it and of its memory."""
+    if stream is None:
+        return contextlib.nullcontext()
+    return torch.cuda.stream(stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream)))
+
+
 def _check(lib, model_handle, status: int):
     if status != ADEPT_OK:
         msg = lib.adept_last_error(model_handle).decode(errors="replace")
@@ -244,7 +251,8 @@ def adept_model_load(cfg, weights: Dict[str, torch.Tensor], stream=None):
     lib = load_library()
     c = make_config(cfg)
     names = list(weights.keys())
-    keep = [weights[n].contiguous() for n in names]
+    with _on(stream):
+        keep = [weights[n].contiguous() for n in names]
     arr = (AdeptTensor * len(names))()
     enc = [n.encode() for n in names]
     for i, (n, t) in enumerate(zip(enc, keep)):
@@ -483,9 +491,7 @@ _KV_TORCH = {0: torch.float32, 1: torch.bfloat16, 2: torch.uint8}
 
 def _make(n: int, device, stream) -> torch.Tensor:
     """n bytes of the call's stream's memory, which alone reuses them."""
-    if stream is not None and not hasattr(stream, "cuda_stream"):
-        stream = torch.cuda.ExternalStream(int(stream))
-    with torch.cuda.stream(stream):
+    with _on(stream):
         return torch.empty(n, dtype=torch.uint8, device=device)
 
 
@@ -805,6 +811,9 @@ def adept_verify_drafts(target: torch.Tensor, draft: Optional[torch.Tensor], tok
 # ---------------------------------------------------------------------------
 
 class Model:
+    """A model and its calls.  With `stream`, outputs are made and inputs converted on it too: the caller orders it behind what makes the inputs, and
+    what reads the outputs behind it."""
+
     def __init__(self, cfg, weights: Dict[str, torch.Tensor], stream=None):
         self.cfg = cfg
         self.h = adept_model_load(cfg, weights, stream)
@@ -831,10 +840,11 @@ class Model:
 
     def prefill(self, tokens: torch.Tensor, delta: float, forced: Optional[torch.Tensor] = None, stream=None):
         B, P = tokens.shape
-        ex, lg, nx, sim = self._outs(B * P, B, tokens.device)
-        adept_prefill(self.h, B, P, tokens.to(torch.int32).contiguous().view(-1), delta,
-                      None if forced is None else forced.to(torch.int32).contiguous().view(-1), ex, lg, nx, sim,
-                      stream)
+        with _on(stream):
+            ex, lg, nx, sim = self._outs(B * P, B, tokens.device)
+            adept_prefill(self.h, B, P, tokens.to(torch.int32).contiguous().view(-1), delta,
+                          None if forced is None else forced.to(torch.int32).contiguous().view(-1), ex, lg, nx, sim,
+                          stream)
         return ex, lg, nx, sim
 
     def extend(self, lens, tokens: torch.Tensor, delta: float, forced: Optional[torch.Tensor] = None, stream=None):
@@ -843,11 +853,12 @@ class Model:
         n = int(sum(int(x) for x in lens))
         if tokens.numel() != n or (forced is not None and forced.numel() != n):
             raise ValueError(f"tokens (and forced exits) must have sum(lens) = {n} elements")
-        ex, lg, nx, sim = self._outs(n, len(lens), tokens.device)
-        lg.zero_()
-        nx.zero_()
-        adept_extend(self.h, lens, tokens.to(torch.int32).contiguous().view(-1), delta,
-                     None if forced is None else forced.to(torch.int32).contiguous().view(-1), ex, lg, nx, sim, stream)
+        with _on(stream):
+            ex, lg, nx, sim = self._outs(n, len(lens), tokens.device)
+            lg.zero_()
+            nx.zero_()
+            adept_extend(self.h, lens, tokens.to(torch.int32).contiguous().view(-1), delta,
+                         None if forced is None else forced.to(torch.int32).contiguous().view(-1), ex, lg, nx, sim, stream)
         return ex, lg, nx, sim
 
     def verify(self, lens, tokens: torch.Tensor, delta: float, u: torch.Tensor, draft: Optional[torch.Tensor] = None,
@@ -859,13 +870,14 @@ class Model:
             raise ValueError(f"tokens, u, draft logits and forced exits must have sum(lens) = {n} rows")
         if draft is not None and draft.shape[-1] != self.n_out or temperature is not None and temperature.shape != (len(lens),):
             raise ValueError("draft must be [tokens, vocab], temperature one number a sequence")
-        ex, _, nx, sim = self._outs(n, len(lens), dev)
-        acc = torch.empty_like(nx)
-        lg = torch.empty(n, self.n_out, dtype=torch.float32, device=dev)
-        lp = torch.full((n,), float("nan"), dtype=torch.float32, device=dev)
-        adept_extend_verify(self.h, lens, tokens.to(torch.int32).contiguous(), delta, u.float().contiguous(), lg, acc, nx, draft,
-                            None if temperature is None else temperature.float().contiguous(),
-                            None if forced is None else forced.to(torch.int32).contiguous(), ex, lp, sim, stream)
+        with _on(stream):
+            ex, _, nx, sim = self._outs(n, len(lens), dev)
+            acc = torch.empty_like(nx)
+            lg = torch.empty(n, self.n_out, dtype=torch.float32, device=dev)
+            lp = torch.full((n,), float("nan"), dtype=torch.float32, device=dev)
+            adept_extend_verify(self.h, lens, tokens.to(torch.int32).contiguous(), delta, u.float().contiguous(), lg, acc, nx, draft,
+                                None if temperature is None else temperature.float().contiguous(),
+                                None if forced is None else forced.to(torch.int32).contiguous(), ex, lp, sim, stream)
         return acc, nx, lg, lp, ex, sim
 
     def trim(self, lens, stream=None):
@@ -873,14 +885,16 @@ class Model:
 
     def decode_step(self, tokens: torch.Tensor, delta: float, forced: Optional[torch.Tensor] = None, stream=None):
         B = tokens.numel()
-        ex, lg, nx, sim = self._outs(B, B, tokens.device)
-        adept_decode_step(self.h, B, tokens.to(torch.int32).contiguous().view(-1), delta,
-                          None if forced is None else forced.to(torch.int32).contiguous().view(-1), ex, lg, nx, sim,
-                          stream)
+        with _on(stream):
+            ex, lg, nx, sim = self._outs(B, B, tokens.device)
+            adept_decode_step(self.h, B, tokens.to(torch.int32).contiguous().view(-1), delta,
+                              None if forced is None else forced.to(torch.int32).contiguous().view(-1), ex, lg, nx, sim,
+                              stream)
         return ex, lg, nx, sim
 
     def set_cross_source(self, src_len, states: torch.Tensor, stream=None):
-        adept_set_cross_source(self.h, src_len, states.float().contiguous(), stream)
+        with _on(stream):
+            adept_set_cross_source(self.h, src_len, states.float().contiguous(), stream)
 
     def final_states(self, rows: int) -> torch.Tensor:
         out = torch.empty(rows, self.cfg.d_model, dtype=torch.float32, device="cuda")
