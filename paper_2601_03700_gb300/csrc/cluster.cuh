@@ -50,14 +50,19 @@ inline cudaError_t cluster16_once(K* kernel) {
   return e;
 }
 
-// Clusters of `ctas` CTAs of a kernel (no dynamic shared memory) that an idle GPU holds at once, asked for once (ctas: a power of two up to 16).
+// Clusters of `ctas` CTAs of a kernel (no dynamic shared memory) that an idle GPU holds at once, 0 where not one or where that cannot be
+// told; asked for once per device (Tag: a type of the kernel's own; ctas: a power of two up to 16).
 template <typename Tag, typename K>
 inline int clusters_at_once(K* kernel, int ctas, int threads) {
-  static std::atomic<int> known[5];   // 0: not asked yet
-  int at = 0;
+  static std::atomic<int> known[64][5];   // one more than there are; 0: not asked yet
+  int at = 0, dev = 0;
   while (1 << at < ctas) ++at;
-  int n = known[at].load();
-  if (n > 0) return n;
+  if (cudaGetDevice(&dev) != cudaSuccess) {
+    cudaGetLastError();
+    return 0;
+  }
+  int n = dev < 64 ? known[dev][at].load() : 0;
+  if (n > 0) return n - 1;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)ctas);
   cfg.blockDim = dim3((unsigned)threads);
@@ -67,11 +72,12 @@ inline int clusters_at_once(K* kernel, int ctas, int threads) {
   attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  if (cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess || n < 1) {
+  if (cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess) {
     cudaGetLastError();
-    n = 1;
+    return 0;   // (not kept: it may have been for a moment)
   }
-  known[at].store(n);
+  if (n < 0) n = 0;
+  if (dev < 64) known[dev][at].store(n + 1);
   return n;
 }
 

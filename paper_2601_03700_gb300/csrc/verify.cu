@@ -897,6 +897,19 @@ int verify_parts(int n_rows, int vocab) {
   return parts;
 }
 
+// CTAs of a sequence: the most (of an SM each) whose clusters find room for all sequences at once, or nearly: 64 sequences of 131072 tokens took
+// 117 us by 2 CTAs each, 125 by 4, 129 by 8 smaller ones, three an SM; one sequence of 50257 tokens 15.0 by 16 CTAs, 17.0 by 8; eight
+// of 32000, of whose clusters of 16 seven find room, 19.7 by 16, 17.9 by 8; sixteen chunks of which one waits (some of them greedy,
+// and done at once) 19.1 by 8, 21.2 by 4.  at_once(c): how many clusters of c find room.
+template <typename F>
+int verify_ctas(int n_seq, F at_once) {
+  for (int ctas = VD_CTAS; ctas > 1; ctas /= 2) {
+    const int n = at_once(ctas);
+    if (n > 0 && n_seq <= n + n / 8) return ctas;
+  }
+  return 1;
+}
+
 template <typename TT, typename TD>
 cudaError_t verify_t(cudaStream_t st, const VerifyCall& a) {
   const int parts = a.n_rows > 0 ? verify_parts(a.n_rows, a.vocab) : 1;
@@ -906,22 +919,15 @@ cudaError_t verify_t(cudaStream_t st, const VerifyCall& a) {
     const cudaError_t e = launch_k(verify_stats_kernel<TT, TD>, dim3((unsigned)(a.n_rows * parts), a.draft ? 2 : 1), dim3(VS_THREADS), 0, st, a, parts, stats, owner);
     if (e != cudaSuccess) return e;
   }
-  // A sequence gets the most CTAs (of an SM each) whose clusters find room for all sequences at once, or nearly: 64 sequences of 131072 tokens took
-  // 117 us by 2 CTAs each, 125 by 4, 129 by 8 smaller ones, three an SM; one sequence of 50257 tokens 15.0 by 16 CTAs, 17.0 by 8; eight
-  // of 32000, of whose clusters of 16 seven find room, 19.7 by 16, 17.9 by 8; sixteen chunks of which one waits (some of them greedy,
-  // and done at once) 19.1 by 8, 21.2 by 4.
   struct Tag;
   struct Tag4;
   auto two = verify_decide_kernel<TT, TD, 2>, four = verify_decide_kernel<TT, TD, 4>;
   cudaError_t e = cluster16_once<Tag>(two);
   if (e == cudaSuccess) e = cluster16_once<Tag4>(four);
   if (e != cudaSuccess) return e;
-  int ctas = VD_CTAS;
-  for (; ctas > 1; ctas /= 2) {
-    const int n = clusters_at_once<Tag>(two, ctas, VD_THREADS);
-    if (a.n_seq <= n + n / 8) break;
-  }
-  return launch_cluster(a.vocab / ctas >= VD_MANY * VD_THREADS ? four : two, dim3((unsigned)(a.n_seq * ctas)), ctas, VD_THREADS, 0, st, a, parts, (const Stat*)stats, (const int*)owner);
+  auto is_four = [&](int ctas) { return a.vocab / ctas >= VD_MANY * VD_THREADS; };
+  const int ctas = verify_ctas(a.n_seq, [&](int c) { return is_four(c) ? clusters_at_once<Tag4>(four, c, VD_THREADS) : clusters_at_once<Tag>(two, c, VD_THREADS); });
+  return launch_cluster(is_four(ctas) ? four : two, dim3((unsigned)(a.n_seq * ctas)), ctas, VD_THREADS, 0, st, a, parts, (const Stat*)stats, (const int*)owner);
 }
 
 }  // namespace
@@ -934,3 +940,12 @@ cudaError_t launch_verify(cudaStream_t st, const VerifyCall& a) {
 }
 
 }  // namespace adept
+
+// Host-side check of the rule (no device work): at_once[i] clusters of 2^i CTAs find room.
+extern "C" __attribute__((visibility("default"))) int adept_debug_verify_ctas(int n_seq, const int* at_once) {
+  return adept::verify_ctas(n_seq, [&](int c) {
+    int i = 0;
+    while (1 << i < c) ++i;
+    return at_once[i];
+  });
+}
