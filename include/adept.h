@@ -518,8 +518,8 @@ ADEPT_API adept_status adept_kv_check(const adept_kv_cache* c, void* stream);
  * The calls decide on the device, from the tables and lengths there, in row and block order: the same tables give the same
  * result every time.  They allocate nothing, hold no state between calls and can be captured into a graph; calls on the
  * same pages are ordered by their streams.  A row's entry that is neither -1 nor a block, a block that is held but
- * counted as free, and lengths or rows out of range flag DEVICE_INPUT in d_err (adept_error_check); such an entry counts as -1, a row
- * with such a length or source stays as it is.
+ * counted as free, and lengths or rows out of range flag DEVICE_INPUT in d_err (adept_error_check) where a call meets them (below: which
+ * entries it checks); such an entry counts as -1, a row with such a length or source stays as it is.
  *   d_ws   adept_kv_pages_workspace bytes on 16 bytes, of any contents; calls that may overlap on the GPU need one each
  * Errors of all: INVALID_ARG (bad pages, NULL or misaligned pointers, a workspace too small), CUDA. */
 typedef struct {
@@ -558,7 +558,7 @@ ADEPT_API adept_status adept_kv_reserve(const adept_kv_pages* p, const int32_t* 
 /* Moves the blocks in use to the front: with U of them in use (*d_used), the k-th in use past the first U goes to the k-th
  * free one among those (both in ascending order), in the table and in the counts.  d_copy_src[k], d_copy_dst[k] ([n_blocks / 2]
  * int32 each) name the moves, for adept_kv_copy_blocks, and for the program where it holds blocks itself; entries behind the last are -1.  Sources and targets are
- * disjoint.  An entry that is flagged stays in the table, unless another block has come to the number that it names: then it is -1. */
+ * disjoint.  Checked are all entries; one that is flagged stays in the table, unless another block has come to the number that it names: then it is -1. */
 ADEPT_API adept_status adept_kv_compact(const adept_kv_pages* p, int32_t* d_used, int32_t* d_copy_src, int32_t* d_copy_dst, void* d_ws,
                               int64_t ws_bytes, void* stream);
 

@@ -5,13 +5,13 @@
 // max(p_r - q_r, 0), at the last row from p_r.
 //
 // Two launches.  The first streams every row once, each in parts of a CTA, and leaves per part the maximum, the sum of exp((l - max) / T), the
-// maximum's first index (greedy sequences) and the draft's logit: HBM-bound, 437 MB at 6.1 TB/s (64 chunks of 8 drafts over 131072
+// maximum's first index (greedy sequences) and the draft's logit: HBM-bound, 437 MB at 6.2 TB/s (64 chunks of 8 drafts over 131072
 // tokens, fp32 and bf16).  The second, a cluster per sequence, decides.  Sums of 32 bits decide a draft unless the two sides are closer
 // than their errors (close_of); those, and the drawing, go by weights of two 32-bit parts each (2^-37 relative at most): with a vocabulary of
 // V tokens the cumulative sum has V steps, and an error of 2^-24 would move the drawn token with odds of V 2^-23.  It reads one row of
 // the target and one of the draft a sequence, most of it from L2, and is bound by the weights' arithmetic (about 40 operations a
 // weight) where there are many sequences, by the chain loads -> sums -> barrier -> sums where there are few.  One launch, in which a
-// cluster takes its rows' statistics as well, was no faster: one chunk of 4 drafts over 50257 tokens 15.8 us where two take 14.7.
+// cluster takes its rows' statistics as well, was no faster: one chunk of 4 drafts over 50257 tokens 15.8 us where two took 14.7.
 #include "cluster.cuh"
 #include "serve_ops.h"
 
@@ -426,8 +426,8 @@ struct Row {
   int certain;        // the draft that has all of q (-1: none)
   int plain;          // w = p
   // Tokens k0, k0 + 32, .. below k1, LOADS at a time: f(first of them, p's logits, q's), -infinity past the end.  The next ones' loads are
-  // under way meanwhile.  Two at a time where a thread has few (one chunk over 50257 tokens, 6 a thread: 15.0 us, by four 15.7), four where it has
-  // many (64 chunks over 131072, 128 a thread: 116 us, by two 120).
+  // under way meanwhile.  Two at a time where a thread has few (one chunk over 50257 tokens, 6 a thread: 14.5 us, by four 15.0), four where it has
+  // many (64 chunks over 131072, 128 a thread: 119 us, by two 128).
   template <typename F>
   __device__ __forceinline__ void each(int k0, int k1, F f) const {
     auto load = [&](int k, float (&x)[LOADS], float (&y)[LOADS]) {
@@ -898,9 +898,9 @@ int verify_parts(int n_rows, int vocab) {
 }
 
 // CTAs of a sequence: the most (of an SM each) whose clusters find room for all sequences at once, or nearly: 64 sequences of 131072 tokens took
-// 117 us by 2 CTAs each, 125 by 4, 129 by 8 smaller ones, three an SM; one sequence of 50257 tokens 15.0 by 16 CTAs, 17.0 by 8; eight
-// of 32000, of whose clusters of 16 seven find room, 19.7 by 16, 17.9 by 8; sixteen chunks of which one waits (some of them greedy,
-// and done at once) 19.1 by 8, 21.2 by 4.  at_once(c): how many clusters of c find room.
+// 119 us by 2 CTAs each, 126 by 4; one sequence of 50257 tokens 14.5 by 16 CTAs, 16.2 by 8; eight of 32000, of whose clusters of 16 seven find
+// room, 18.6 by 16, 17.6 by 8; sixteen chunks of which one waits (some of them greedy, and done at once) 18.5 by 8, 21.2 by 4.
+// at_once(c): how many clusters of c find room.
 template <typename F>
 int verify_ctas(int n_seq, F at_once) {
   for (int ctas = VD_CTAS; ctas > 1; ctas /= 2) {
